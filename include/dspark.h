@@ -479,6 +479,88 @@ int dspark_sts_calibrate(const float* conf, int N, int gamma, const int32_t* acc
                          double* out_ece_after, double* out_ece_grid, void* workspace, size_t workspace_bytes, void* stream);
 int dspark_sts_apply(const float* conf, int N, int gamma, const float* T, float* out, void* stream);
 
+/* ------------------------------------------------------------------------------------
+ * The vocabulary projection: what makes the logit rows that the verifiers read (the target's rows of Section 5.3's flat
+ * ragged batch, the drafter's base logits U of Section 3.1), and the loss that trains it (L_ce, the cross-entropy term of
+ * the drafter's training objective).  The paper states no kernel for either.
+ *
+ * dspark_rms_norm_quant -- the norm in front of the projection, with the residual's addition and an int8 output.  Per row
+ *     h = x + residual, rounded to the row's type;   y = h * rsqrt(mean(h^2) + eps) * weight;
+ *     scale = max|y| / 127;   q = y / scale, rounded to the nearest integer (a half to the even one).
+ *   The integer is that of the exact quotient 127 (h weight) / max|h weight| (the norm's factor cancels).
+ *   x, residual        device [rows, >= d] of `dtype` (DSPARK_F32 / DSPARK_BF16); residual NULL: h = x
+ *   weight             device [d] of `dtype`
+ *   n_live             device int32 or NULL (= rows): only the first *n_live rows are computed, at most `rows`; what the
+ *                      outputs hold behind them is left as it was (row_offsets + R is the count of a ragged batch)
+ *   out_residual       device [rows, >= d] of `dtype` or NULL: h; may be `residual` or `x` itself (same stride)
+ *   out_q, out_scale   device int8 [rows, >= d], device fp32 [rows]
+ *   out_norm           device [rows, >= d] of `dtype` or NULL: y (what the confidence head reads); may be x itself
+ *   A row of zeros gives q = 0 and scale 0.  A row that holds NaN or an infinity, or whose sum of squares or a product
+ *   h * weight passes the range of fp32, gives q = 0 and a scale of NaN: its logits are then NaN and a verifier reports
+ *   DSPARK_DEV_BAD_ROW.  Outputs must not overlap otherwise.  No workspace.
+ * Limits: d <= 16 384.  Errors: INVALID_ARG, SHAPE, ALIGNMENT (a pointer not aligned to its element), CUDA.
+ */
+int dspark_rms_norm_quant(const void* x, int64_t x_row_stride, const void* residual, int64_t residual_row_stride,
+                          const void* weight, int dtype, int rows, int d, float eps, const int32_t* n_live,
+                          void* out_residual, int64_t out_residual_row_stride, int8_t* out_q, int64_t out_q_row_stride,
+                          float* out_scale, void* out_norm, int64_t out_norm_row_stride, void* stream);
+
+/* dspark_lm_head_quantize -- the weight of dspark_lm_head_int8, once when the weights are loaded: per row (vocabulary entry)
+ *     scale = max|w| / 127,  q = rint(127 w / max|w|)  (a half to the even integer).
+ *   W   device bf16 [V, >= K];  out_q  device int8 [V, >= K];  out_scale  device fp32 [V]
+ *   A row of zeros gives scale 0, a row with NaN or an infinity a scale of NaN.  Errors: INVALID_ARG, ALIGNMENT, CUDA.
+ *
+ * dspark_lm_head_int8 -- logits of every row from 8-bit operands:
+ *     logits[r, v] = (sum_k x_q[r, k] w_q[v, k]) * x_scale[r] * w_scale[v],
+ *   the sum in 32-bit integers on the tensor cores (exact), the two products in fp32, one rounding to the output type.
+ *   x_q, x_scale   device int8 [rows, >= K], fp32 [rows]: what dspark_rms_norm_quant writes
+ *   w_q, w_scale   device int8 [V, >= K], fp32 [V]
+ *   n_live         device int32 or NULL (= rows): rows behind the first *n_live are not computed, their logits left as they were
+ *   out_logits     device bf16 / fp32 [rows, >= V], any row stride: the verifiers' target (or draft) logits
+ * x_q and w_q need 16-byte aligned addresses and row strides that are multiples of 16 (the columns between K and the stride
+ * are not read into the sum); any K and V.  Limits: rows <= 2^20, V <= 2^24, K <= 65 536 (the sums stay below 2^31).
+ * Errors: INVALID_ARG, SHAPE, ALIGNMENT, CUDA.
+ */
+int dspark_lm_head_quantize(const void* W, int64_t w_row_stride, int V, int K, int8_t* out_q, int64_t out_q_row_stride,
+                            float* out_scale, void* stream);
+int dspark_lm_head_int8(const int8_t* x_q, int64_t x_row_stride, const float* x_scale, const int8_t* w_q, int64_t w_row_stride,
+                        const float* w_scale, int rows, int V, int K, const int32_t* n_live, void* out_logits, int out_dtype,
+                        int64_t out_row_stride, int32_t* dev_status, void* stream);
+
+/* dspark_lm_head_loss, dspark_lm_head_loss_backward -- softmax cross entropy of hidden states against the vocabulary, in
+ * pieces of the vocabulary, without keeping the logits:
+ *     z = hidden weight^T,   lse[n] = log sum_v exp z[n, v],   loss[n] = lse[n] - z[n, labels[n]],
+ *     G[n, v] = grad_loss[n] (exp(z[n, v] - lse[n]) - [v = labels[n]]),
+ *     grad_hidden = G weight,   grad_weight = G^T hidden.
+ *   hidden         device bf16 [N, >= d], any row stride
+ *   weight         device bf16 [V, >= d], 16-byte aligned, row stride a multiple of 8
+ *   labels         device int32 [N]; a negative label: the row is ignored -- loss and lse 0, gradient zeros, and nothing the
+ *                  row holds (padding, NaN) reaches grad_weight; it costs no work.  A label >= V is ignored the same way
+ *                  and sets DSPARK_DEV_BAD_TOKEN.
+ *   out_loss, out_lse   device fp32 [N]
+ *   lse            device fp32 [N]: what the forward call left (entries of ignored rows are not used)
+ *   grad_loss      device fp32 [N]: dL / dloss[n] -- the weights of a mean or of the block's positions
+ *   out_grad_hidden device bf16 [N, >= d], out_grad_weight device bf16 [V, >= d]: any row stride, written (not added to);
+ *                  either may be NULL, not both
+ *   workspace      dspark_lm_head_loss_workspace_bytes(N, V, d), 256-byte aligned, any content; one call at a time
+ * Products are bf16 with fp32 accumulation, softmax statistics fp32 (combined in fp64).  G is rounded to bf16 for its two
+ * products (what that loses of the label's entry is added back to grad_hidden in fp32); sums over pieces and slices are
+ * fp32 in a fixed order: the same inputs give the same bits.  A row whose loss is not finite sets DSPARK_DEV_BAD_ROW; its
+ * loss and gradients are what the arithmetic gives (NaN reaches grad_weight, as in the formula).
+ * Limits: N <= 2^20, V <= 2^24, d <= 65 536.  Errors: INVALID_ARG, SHAPE, ALIGNMENT, WORKSPACE, CUDA.
+ * Resources (all three contractions): one CTA per SM with 193 KB of shared memory, all 512 tensor-memory columns of the SM;
+ * a wait that ran out sets DSPARK_DEV_TIMEOUT in *dev_status and the outputs are unspecified.
+ */
+size_t dspark_lm_head_loss_workspace_bytes(int N, int V, int d);
+int dspark_lm_head_loss(const void* hidden, int64_t hidden_row_stride, const void* weight, int64_t weight_row_stride,
+                        const int32_t* labels, int N, int V, int d, float* out_loss, float* out_lse, int32_t* dev_status,
+                        void* workspace, size_t workspace_bytes, void* stream);
+int dspark_lm_head_loss_backward(const void* hidden, int64_t hidden_row_stride, const void* weight, int64_t weight_row_stride,
+                                 const int32_t* labels, const float* lse, const float* grad_loss, int N, int V, int d,
+                                 void* out_grad_hidden, int64_t grad_hidden_row_stride, void* out_grad_weight,
+                                 int64_t grad_weight_row_stride, int32_t* dev_status, void* workspace, size_t workspace_bytes,
+                                 void* stream);
+
 /* The two uniforms of (seed, request, position) exactly as the verifier draws them
  * (host computation; for tests and for replaying a step). */
 void dspark_uniforms(uint64_t seed, uint32_t request, uint32_t position,
@@ -496,7 +578,8 @@ enum {
     DSPARK_K_SCHEDULE = 0, DSPARK_K_OFFSETS = 1, DSPARK_K_STREAM = 2, DSPARK_K_DECIDE = 3,
     DSPARK_K_RESIDUAL = 4, DSPARK_K_FINALIZE = 5, DSPARK_K_GREEDY_STREAM = 6, DSPARK_K_GREEDY_DECIDE = 7,
     DSPARK_K_ROW_SCALE = 8, DSPARK_K_MARKOV_GEMM = 9, DSPARK_K_MARKOV_DRAW = 10, DSPARK_K_TRUNCATE = 11,
-    DSPARK_K_COUNT = 12
+    DSPARK_K_RMS_NORM = 12, DSPARK_K_HEAD_INT8 = 13, DSPARK_K_HEAD_ROWS = 14, DSPARK_K_HEAD_LOSS = 15,
+    DSPARK_K_HEAD_GRAD = 16, DSPARK_K_COUNT = 17
 };
 int dspark_ktimer_create(int capacity, dspark_ktimer_t** out);
 int dspark_ktimer_destroy(dspark_ktimer_t* t);

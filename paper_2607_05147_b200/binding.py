@@ -22,7 +22,8 @@ DSPARK_SCHED_EARLY_STOP, DSPARK_SCHED_GLOBAL, DSPARK_SCHED_TOPK = 0, 1, 2
 DEV_BAD_OFFSETS, DEV_BAD_TOKEN, DEV_BAD_ROW, DEV_TIMEOUT = 1, 2, 4, 8
 DEV_CONF_CLAMPED, DEV_BUDGET_LT_R, DEV_ALL_NEG_INF, DEV_BAD_TEMPERATURE = 16, 32, 64, 128
 (K_SCHEDULE, K_OFFSETS, K_STREAM, K_DECIDE, K_RESIDUAL, K_FINALIZE, K_GREEDY_STREAM, K_GREEDY_DECIDE,
- K_ROW_SCALE, K_MARKOV_GEMM, K_MARKOV_DRAW, K_TRUNCATE, K_COUNT) = range(13)
+ K_ROW_SCALE, K_MARKOV_GEMM, K_MARKOV_DRAW, K_TRUNCATE, K_RMS_NORM, K_HEAD_INT8, K_HEAD_ROWS, K_HEAD_LOSS, K_HEAD_GRAD,
+ K_COUNT) = range(18)
 
 EXPORTS = [
     "dspark_profile_create", "dspark_profile_destroy", "dspark_profile_table",
@@ -36,6 +37,8 @@ EXPORTS = [
     "dspark_markov_logits", "dspark_markov_draft_step", "dspark_markov_draft_step_stats", "dspark_markov_set_epilogue_path",
     "dspark_truncate_target", "dspark_verify_truncated",
     "dspark_sts_workspace_bytes", "dspark_sts_calibrate", "dspark_sts_apply",
+    "dspark_rms_norm_quant", "dspark_lm_head_quantize", "dspark_lm_head_int8",
+    "dspark_lm_head_loss_workspace_bytes", "dspark_lm_head_loss", "dspark_lm_head_loss_backward",
     "dspark_ktimer_create", "dspark_ktimer_destroy", "dspark_ktimer_attach", "dspark_ktimer_reset",
     "dspark_ktimer_read", "dspark_set_stream_path", "dspark_set_wait_poll_limit", "dspark_status_string", "dspark_kernel_name",
     "dspark_version",
@@ -106,6 +109,13 @@ def lib() -> C.CDLL:
         L.dspark_sts_workspace_bytes.restype = sz
         L.dspark_sts_calibrate.argtypes = [vp, i32, i32, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, sz, vp]
         L.dspark_sts_apply.argtypes = [vp, i32, i32, vp, vp, vp]
+        L.dspark_rms_norm_quant.argtypes = [vp, i64, vp, i64, vp, i32, i32, i32, C.c_float, vp, vp, i64, vp, i64, vp, vp, i64, vp]
+        L.dspark_lm_head_quantize.argtypes = [vp, i64, i32, i32, vp, i64, vp, vp]
+        L.dspark_lm_head_int8.argtypes = [vp, i64, vp, vp, i64, vp, i32, i32, i32, vp, vp, i32, i64, vp, vp]
+        L.dspark_lm_head_loss_workspace_bytes.argtypes = [i32, i32, i32]
+        L.dspark_lm_head_loss_workspace_bytes.restype = sz
+        L.dspark_lm_head_loss.argtypes = [vp, i64, vp, i64, vp, i32, i32, i32, vp, vp, vp, vp, sz, vp]
+        L.dspark_lm_head_loss_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, i32, i32, i32, vp, i64, vp, i64, vp, vp, sz, vp]
         L.dspark_uniforms.argtypes = [u64, C.c_uint32, C.c_uint32, C.POINTER(C.c_float), C.POINTER(C.c_float)]
         L.dspark_uniforms.restype = None
         L.dspark_ktimer_create.argtypes = [i32, C.POINTER(vp)]
@@ -596,6 +606,131 @@ def dspark_sts_apply(conf: torch.Tensor, T: torch.Tensor, out: torch.Tensor) -> 
         raise DsparkError("T needs gamma entries")
     _check(lib().dspark_sts_apply(_dev(conf, "conf", torch.float32), conf.shape[0], conf.shape[1],
                                   _dev(T, "T", torch.float32), _dev(out, "out", torch.float32), _stream()), "dspark_sts_apply")
+
+
+# -------------------------------------------------------------------- vocabulary projection ----
+def _rows(t: Optional[torch.Tensor], name: str, dtype, rows: int, cols: int):
+    """(address, row stride) of a 2-D matrix with unit inner stride on the current device, at least rows x cols."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise DsparkError(f"{name} must be a CUDA tensor on the current device (no CPU path exists)")
+    if t.dtype != dtype:
+        raise DsparkError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise DsparkError(f"{name} must be 2-D with unit inner stride and rows that do not overlap")
+    if t.shape[0] < rows or t.shape[1] != cols:
+        raise DsparkError(f"{name} must be [{rows}, {cols}], got {list(t.shape)}")
+    # the stride of a single row carries no meaning: any aligned number that is wide enough does
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else -(-cols // 16) * 16
+
+
+def _vec(t: Optional[torch.Tensor], name: str, dtype, n: int):
+    """Address of a contiguous vector of at least n entries on the current device."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise DsparkError(f"{name} must be a CUDA tensor on the current device (no CPU path exists)")
+    if t.dtype != dtype:
+        raise DsparkError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.numel() < n or not t.is_contiguous():
+        raise DsparkError(f"{name} must be contiguous with {n} entries")
+    return t.data_ptr()
+
+
+def _need(t, name: str):
+    if t is None:
+        raise DsparkError(f"{name} is needed")
+    return t
+
+
+def dspark_rms_norm_quant(x: torch.Tensor, weight: torch.Tensor, eps: float, *, residual: Optional[torch.Tensor] = None,
+                          out_residual: Optional[torch.Tensor] = None, out_q: torch.Tensor, out_scale: torch.Tensor,
+                          out_norm: Optional[torch.Tensor] = None, n_live: Optional[torch.Tensor] = None) -> None:
+    """int8 rows and their scales of the normalised x (+ residual); n_live: CUDA int32 count of the rows to compute."""
+    if x.dim() != 2 or x.dtype not in (torch.float32, torch.bfloat16):
+        raise DsparkError("x must be a float32 or bfloat16 matrix")
+    rows, d = x.shape
+    xp, xs = _rows(x, "x", x.dtype, rows, d)
+    rp, rs = _rows(residual, "residual", x.dtype, rows, d)
+    hp, hs = _rows(out_residual, "out_residual", x.dtype, rows, d)
+    qp, qs = _rows(_need(out_q, "out_q"), "out_q", torch.int8, rows, d)
+    yp, ys = _rows(out_norm, "out_norm", x.dtype, rows, d)
+    rc = lib().dspark_rms_norm_quant(xp, xs, rp, rs, _vec(weight, "weight", x.dtype, d),
+                                     DSPARK_F32 if x.dtype == torch.float32 else DSPARK_BF16, rows, d, float(eps),
+                                     _vec(n_live, "n_live", torch.int32, 1), hp, hs, qp, qs,
+                                     _vec(_need(out_scale, "out_scale"), "out_scale", torch.float32, rows), yp, ys, _stream())
+    _check(rc, "dspark_rms_norm_quant")
+
+
+def dspark_lm_head_quantize(W: torch.Tensor, out_q: torch.Tensor, out_scale: torch.Tensor) -> None:
+    """int8 rows and scales of the bf16 vocabulary matrix [V, K] (once, when the weights are loaded)."""
+    V, K = W.shape
+    wp, ws = _rows(W, "W", torch.bfloat16, V, K)
+    qp, qs = _rows(out_q, "out_q", torch.int8, V, K)
+    _check(lib().dspark_lm_head_quantize(wp, ws, V, K, qp, qs, _vec(out_scale, "out_scale", torch.float32, V), _stream()),
+           "dspark_lm_head_quantize")
+
+
+def dspark_lm_head_int8(x_q: torch.Tensor, x_scale: torch.Tensor, w_q: torch.Tensor, w_scale: torch.Tensor, *,
+                        out_logits: torch.Tensor, n_live: Optional[torch.Tensor] = None, dev_status: torch.Tensor) -> None:
+    """Logit rows (bf16 or fp32) from int8 hidden states and weights; n_live: CUDA int32 count of the rows to compute."""
+    rows, K = x_q.shape
+    V = w_q.shape[0]
+    if out_logits.dtype not in (torch.float32, torch.bfloat16):
+        raise DsparkError("out_logits must be float32 or bfloat16")
+    xp, xs = _rows(x_q, "x_q", torch.int8, rows, K)
+    wp, ws = _rows(w_q, "w_q", torch.int8, V, K)
+    op, os_ = _rows(out_logits, "out_logits", out_logits.dtype, rows, V)
+    rc = lib().dspark_lm_head_int8(xp, xs, _vec(x_scale, "x_scale", torch.float32, rows), wp, ws,
+                                   _vec(w_scale, "w_scale", torch.float32, V), rows, V, K, _vec(n_live, "n_live", torch.int32, 1),
+                                   op, DSPARK_F32 if out_logits.dtype == torch.float32 else DSPARK_BF16, os_,
+                                   _vec(_need(dev_status, "dev_status"), "dev_status", torch.int32, 1), _stream())
+    _check(rc, "dspark_lm_head_int8")
+
+
+def dspark_lm_head_loss_workspace_bytes(N: int, V: int, d: int) -> int:
+    return int(lib().dspark_lm_head_loss_workspace_bytes(N, V, d))
+
+
+def _loss_args(hidden, weight, labels):
+    if hidden.dim() != 2 or weight.dim() != 2:
+        raise DsparkError("hidden and weight must be matrices")
+    N, d = hidden.shape
+    V = weight.shape[0]
+    hp, hs = _rows(hidden, "hidden", torch.bfloat16, N, d)
+    wp, ws = _rows(weight, "weight", torch.bfloat16, V, d)
+    return (hp, hs, wp, ws, _vec(labels, "labels", torch.int32, N)), N, V, d
+
+
+def _ws(workspace: torch.Tensor):
+    nbytes = workspace.numel() * workspace.element_size()
+    return _vec(workspace, "workspace", workspace.dtype, 0), nbytes
+
+
+def dspark_lm_head_loss(hidden: torch.Tensor, weight: torch.Tensor, labels: torch.Tensor, *, out_loss: torch.Tensor,
+                        out_lse: torch.Tensor, dev_status: torch.Tensor, workspace: torch.Tensor) -> None:
+    """Cross entropy of every row of `hidden` [N, d] against `weight` [V, d]; a negative label: the row is ignored."""
+    head, N, V, d = _loss_args(hidden, weight, labels)
+    rc = lib().dspark_lm_head_loss(*head, N, V, d, _vec(_need(out_loss, "out_loss"), "out_loss", torch.float32, N),
+                                   _vec(_need(out_lse, "out_lse"), "out_lse", torch.float32, N),
+                                   _vec(_need(dev_status, "dev_status"), "dev_status", torch.int32, 1), *_ws(workspace), _stream())
+    _check(rc, "dspark_lm_head_loss")
+
+
+def dspark_lm_head_loss_backward(hidden: torch.Tensor, weight: torch.Tensor, labels: torch.Tensor, lse: torch.Tensor,
+                                 grad_loss: torch.Tensor, *, out_grad_hidden: Optional[torch.Tensor] = None,
+                                 out_grad_weight: Optional[torch.Tensor] = None, dev_status: torch.Tensor,
+                                 workspace: torch.Tensor) -> None:
+    """Gradients of sum_n grad_loss[n] * loss[n]; lse: what dspark_lm_head_loss left for the same rows."""
+    head, N, V, d = _loss_args(hidden, weight, labels)
+    hp, hs = _rows(out_grad_hidden, "out_grad_hidden", torch.bfloat16, N, d)
+    wp, ws = _rows(out_grad_weight, "out_grad_weight", torch.bfloat16, V, d)
+    rc = lib().dspark_lm_head_loss_backward(*head, _vec(_need(lse, "lse"), "lse", torch.float32, N),
+                                            _vec(_need(grad_loss, "grad_loss"), "grad_loss", torch.float32, N), N, V, d, hp, hs, wp, ws,
+                                            _vec(_need(dev_status, "dev_status"), "dev_status", torch.int32, 1), *_ws(workspace),
+                                            _stream())
+    _check(rc, "dspark_lm_head_loss_backward")
 
 
 def dspark_uniforms(seed: int, request: int, position: int):

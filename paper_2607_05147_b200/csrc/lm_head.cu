@@ -1,0 +1,845 @@
+// The vocabulary projection: int8 logits for serving (dspark_lm_head_int8) and the cross entropy of a hidden state
+// against the vocabulary with its gradients (dspark_lm_head_loss, dspark_lm_head_loss_backward), logits never kept.
+//
+// All of it is one persistent tcgen05 contraction  D[m, n] = sum_k A[m, k] B[n, k]  with five epilogues:
+//
+//   mode        A                    B                    D (tensor memory)      epilogue
+//   Int8Logits  w_q   [V, K]         x_q   [rows, K]      vocabulary x rows      sx * sw * D -> bf16 / fp32 logits
+//   LossStats   H     [rows, d]      W     [V, d]         rows x vocabulary      softmax statistics, label's logit
+//   LossGrad    H                    W (a piece)          rows x piece           G = g (softmax - onehot) -> bf16
+//   GradHidden  G     [rows, piece]  W^T (a piece)        rows x d               fp32 partial sums of G W
+//   GradWeight  G^T   [piece, rows]  H^T   [d, rows]      piece x d              dW = G^T H -> bf16
+//
+// A tile is 128 x (up to) 256: the accumulator is 256 of the 512 tensor-memory columns, so one is filled while the
+// other is read.  A producer thread brings 128-byte wide tiles of both operands into a ring of stages by tensor-map
+// copies (128-byte swizzle), one thread issues tcgen05.mma, eight warps read accumulators back, each owning a lane
+// quarter and every other group of 32 columns.  Where the contraction runs over an operand's rows (the gradients), the
+// tile is loaded as it lies in memory, [64 k][64 mn] boxes, and the MMA descriptor says so (mn-major): nothing is
+// transposed in memory.
+//
+// Tile order: the index of the row tiles runs fastest, so that all row tiles of one stretch of the vocabulary run side
+// by side and the weight is fetched from HBM once.
+#include <cuda_bf16.h>
+#include <cstring>
+#include <math.h>
+
+#include "common.cuh"
+#include "tcgen05.cuh"
+
+namespace dspark {
+
+enum HeadMode { kInt8Logits = 0, kLossStats = 1, kLossGrad = 2, kGradHidden = 3, kGradWeight = 4 };
+
+constexpr int kHeadM = 128;
+constexpr int kHeadN = 256;                       // columns of one accumulator at most
+constexpr int kRowBytes = 128;                    // bytes of k in one stage: 64 bf16 or 128 int8
+constexpr int kTileABytes = kHeadM * kRowBytes;   // 16 KB
+constexpr int kBoxMnBytes = 64 * kRowBytes;       // [64 k][64 mn] of bf16: 8 KB
+constexpr int kHeadMaxStages = 10;
+constexpr int kHeadRingBytes = 4 * (kTileABytes + kHeadN * kRowBytes);   // 192 KB
+constexpr int kHeadEpiWarps = 8;
+constexpr int kHeadThreads = (2 + kHeadEpiWarps) * 32;
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct HeadParams {
+    int m, n, k;                    // extents; the one that counts rows is bounded by *live
+    int n_tile, stages;
+    int slices, kb_slice;           // the k blocks cut into slices (GradHidden), 1 otherwise
+    int piece0;                     // first vocabulary entry of the piece (LossGrad, GradHidden, GradWeight)
+    int V;
+    const int32_t* live;            // number of rows that count, NULL: all
+    int32_t* dev_status;
+    void* out; long long out_stride; int out_bf16;
+    const float* row_scale; const float* col_scale;                 // Int8Logits
+    float2* stats; long long stats_stride;                          // LossStats: [2 n_tiles][rows] (reference, sum)
+    const int32_t* labels; float* z_label;
+    const float* lse2; const float* grad; float* label_err;         // LossGrad: lse * log2(e), dL/dloss
+    int accumulate;                                                 // GradHidden: add to what the pieces before left
+};
+
+// ---- descriptors ------------------------------------------------------------------------------------
+// 128-byte swizzle (layout type 2), descriptor version 1.  k-major: rows of 128 B, groups of 8 rows 1 024 B apart
+// (stride offset); the leading offset is not used.  mn-major: 64 mn elements per 128 B, one k per row; groups of 8 k
+// 1 024 B apart (stride offset), the next 64 mn elements 8 KB further (leading offset).
+__device__ __forceinline__ uint64_t head_desc(uint32_t addr, bool mn_major)
+{
+    const uint64_t lead = mn_major ? (uint64_t)(kBoxMnBytes >> 4) : 1ull;
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (lead << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+
+template <bool kInt8>
+__device__ __forceinline__ void head_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    if (kInt8)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b)
+{
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// Stores 32 consecutive bf16 of a row, `n` of them valid.
+__device__ __forceinline__ void store_row32(__nv_bfloat16* p, const float (&v)[32], int n, bool vec)
+{
+    if (vec && n >= 32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            reinterpret_cast<uint4*>(p)[i] = make_uint4(bf16_pair(v[8 * i], v[8 * i + 1]), bf16_pair(v[8 * i + 2], v[8 * i + 3]),
+                                                        bf16_pair(v[8 * i + 4], v[8 * i + 5]), bf16_pair(v[8 * i + 6], v[8 * i + 7]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if (i < n) p[i] = __float2bfloat16_rn(v[i]);
+    }
+}
+
+template <int kMode>
+__global__ void __launch_bounds__(kHeadThreads, 1)
+lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b)
+{
+    constexpr bool kInt8 = kMode == kInt8Logits;
+    constexpr bool kAMn = kMode == kGradWeight;
+    constexpr bool kBMn = kMode == kGradHidden || kMode == kGradWeight;
+    constexpr bool kRowsOnN = kMode == kInt8Logits;         // which tile index runs fastest: the one over rows
+    constexpr int kBlockK = kInt8 ? 128 : 64;
+
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);   // swizzle atoms: 1 KB
+    __shared__ __align__(8) uint64_t full[kHeadMaxStages], empty[kHeadMaxStages], acc_full[2], acc_empty[2], mma_done;
+    __shared__ uint32_t s_tmem_base;
+    __shared__ int s_abort;
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (tid == 0) {
+        for (int s = 0; s < P.stages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+        for (int s = 0; s < 2; ++s) { mbar_init(&acc_full[s], 1); mbar_init(&acc_empty[s], kHeadEpiWarps); }
+        mbar_init(&mma_done, 1);
+        s_abort = 0;
+        mbar_fence_init();
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                     ::"r"(smem_u32(&s_tmem_base)), "r"(2 * kHeadN) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    pdl_wait();
+    const uint32_t tmem = s_tmem_base;
+    volatile int* abort_flag = &s_abort;
+    auto give_up = [&]() { atomicOr(P.dev_status, DSPARK_DEV_TIMEOUT); *abort_flag = 1; };
+
+    // extents of this call: the row count may live on the device
+    int m = P.m, n = P.n, k = P.k;
+    if (P.live) {
+        int live = *P.live;
+        live = live < 0 ? 0 : live;
+        int& rows = kMode == kGradWeight ? k : (kRowsOnN ? n : m);
+        rows = live < rows ? live : rows;
+    }
+    const int m_tiles = (m + kHeadM - 1) / kHeadM, n_tiles = (n + P.n_tile - 1) / P.n_tile;
+    const int k_blocks = (k + kBlockK - 1) / kBlockK;
+    const int n_units = m_tiles * n_tiles * P.slices;
+    struct Unit { int m0, n0, kb0, kb1, slice, nt; };
+    auto unit = [&](int u) {
+        Unit r;
+        int mt, nt;
+        if (kRowsOnN) { nt = u % n_tiles; u /= n_tiles; mt = u % m_tiles; r.slice = u / m_tiles; }
+        else { mt = u % m_tiles; u /= m_tiles; nt = u % n_tiles; r.slice = u / n_tiles; }
+        r.m0 = mt * kHeadM; r.n0 = nt * P.n_tile; r.nt = nt;
+        r.kb0 = r.slice * P.kb_slice;
+        r.kb0 = r.kb0 < k_blocks ? r.kb0 : k_blocks;
+        r.kb1 = r.kb0 + P.kb_slice < k_blocks ? r.kb0 + P.kb_slice : k_blocks;
+        return r;
+    };
+    const int stage_bytes = kTileABytes + P.n_tile * kRowBytes;
+    const int first = (int)blockIdx.x, step = (int)gridDim.x;
+
+    if (warp == 0) {
+        // ---------------- producer: operand tiles ---------------------------------------------------------
+        if (lane == 0) {
+            const uint64_t pol = l2_policy_evict_normal();
+            int issued = 0, s = 0;
+            uint32_t ph = 0;
+            for (int u = first; u < n_units && !*abort_flag; u += step) {
+                const Unit w = unit(u);
+                for (int kb = w.kb0; kb < w.kb1; ++kb) {
+                    if (!mbar_wait_bounded(&empty[s], ph ^ 1u)) { give_up(); break; }
+                    unsigned char* a = smem + (size_t)s * stage_bytes;
+                    unsigned char* b = a + kTileABytes;
+                    mbar_arrive_expect_tx(&full[s], (uint32_t)stage_bytes);
+                    const int kx = kb * kBlockK;
+                    if (kAMn) {
+#pragma unroll
+                        for (int j = 0; j < kHeadM / 64; ++j) tma_load_2d(a + j * kBoxMnBytes, &map_a, w.m0 + j * 64, kx, &full[s], pol);
+                    } else {
+                        tma_load_2d(a, &map_a, kx, w.m0, &full[s], pol);
+                    }
+                    if (kBMn) {
+                        const int k0 = kx + (kMode == kGradHidden ? P.piece0 : 0);
+                        for (int j = 0; j < P.n_tile / 64; ++j) tma_load_2d(b + j * kBoxMnBytes, &map_b, w.n0 + j * 64, k0, &full[s], pol);
+                    } else {
+                        tma_load_2d(b, &map_b, kx, w.n0 + (kMode == kLossGrad ? P.piece0 : 0), &full[s], pol);
+                    }
+                    ++issued;
+                    if (++s == P.stages) { s = 0; ph ^= 1u; }
+                }
+            }
+            if (*abort_flag) {
+                // somebody gave up: leave only after the copies already issued have landed (bounded)
+                for (int i = issued > P.stages ? issued - P.stages : 0; i < issued; ++i)
+                    mbar_wait_bounded(&full[i % P.stages], (uint32_t)(i / P.stages) & 1u);
+            }
+        }
+    } else if (warp == 1) {
+        // ---------------- MMA issuer ---------------------------------------------------------------------
+        if (lane == 0) {
+            const uint32_t idesc = ((kInt8 ? 2u : 1u) << 4) | (1u << 7) | (1u << 10) | ((kAMn ? 1u : 0u) << 15) |
+                                   ((kBMn ? 1u : 0u) << 16) | ((uint32_t)(P.n_tile >> 3) << 17) | ((uint32_t)(kHeadM >> 4) << 24);
+            constexpr uint32_t kStepA = kAMn ? 2048 : 32, kStepB = kBMn ? 2048 : 32;
+            int s = 0, t = 0;
+            uint32_t ph = 0;
+            bool issued = false;
+            for (int u = first; u < n_units && !*abort_flag; u += step) {
+                const Unit w = unit(u);
+                if (w.kb0 == w.kb1) continue;               // nothing to add up: the epilogue knows
+                const uint32_t acc = (uint32_t)(t & 1), aph = (uint32_t)(t >> 1) & 1u;
+                if (!mbar_wait_bounded(&acc_empty[acc], aph ^ 1u)) { give_up(); break; }
+                tc_fence_after();
+                bool ok = true;
+                for (int kb = w.kb0; kb < w.kb1; ++kb) {
+                    ok = mbar_wait_bounded(&full[s], ph);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t a0 = smem_u32(smem + (size_t)s * stage_bytes), b0 = a0 + kTileABytes;
+#pragma unroll
+                    for (int ks = 0; ks < 4; ++ks)
+                        head_mma<kInt8>(tmem + acc * kHeadN, head_desc(a0 + ks * kStepA, kAMn), head_desc(b0 + ks * kStepB, kBMn),
+                                        idesc, (kb > w.kb0 || ks > 0) ? 1u : 0u);
+                    umma_commit(&empty[s]);
+                    issued = true;
+                    if (++s == P.stages) { s = 0; ph ^= 1u; }
+                }
+                if (!ok) { give_up(); break; }
+                umma_commit(&acc_full[acc]);
+                ++t;
+            }
+            if (issued) {                                   // tensor memory is returned only after the last product
+                umma_commit(&mma_done);
+                mbar_wait_bounded(&mma_done, 0u);
+            }
+        }
+    } else {
+        // ---------------- epilogue -----------------------------------------------------------------------
+        const int q = warp & 3, half = (warp - 2) >> 2;
+        const uint32_t lane_base = (uint32_t)(q * 32) << 16;
+        const int chunks = P.n_tile / 32;
+        int t = 0;
+        for (int u = first; u < n_units && !*abort_flag; u += step) {
+            const Unit w = unit(u);
+            const bool any = w.kb0 < w.kb1;
+            const uint32_t acc = (uint32_t)(t & 1), aph = (uint32_t)(t >> 1) & 1u;
+            if (any) {
+                if (!__all_sync(0xffffffffu, mbar_wait_bounded(&acc_full[acc], aph))) {
+                    if (lane == 0) give_up();
+                    break;
+                }
+                tc_fence_after();
+                ++t;
+            }
+            const uint32_t acc_addr = tmem + lane_base + acc * kHeadN;
+            const int row = w.m0 + q * 32 + lane;           // row of D
+            const bool warp_live = w.m0 + q * 32 < m || kMode == kLossGrad;
+            auto load = [&](int c, float (&v)[32]) {
+                if (any) tmem_load32(acc_addr + (uint32_t)(c * 32), v);
+                else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = 0.f;
+                }
+            };
+            if (warp_live) {
+                if (kMode == kInt8Logits) {
+                    const float sw = row < m ? P.col_scale[row] : 0.f;
+                    for (int c = half; c < chunks; c += 2) {
+                        const int col0 = w.n0 + c * 32;
+                        if (col0 >= n) break;
+                        float v[32];
+                        load(c, v);
+                        const float sx = col0 + lane < n ? P.row_scale[col0 + lane] : 0.f;
+                        const int valid = n - col0;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            const float z = (float)__float_as_int(v[i]) * __shfl_sync(0xffffffffu, sx, i) * sw;
+                            if (i < valid && row < m) {
+                                const long long at = (long long)(col0 + i) * P.out_stride + row;
+                                if (P.out_bf16) ((__nv_bfloat16*)P.out)[at] = __float2bfloat16_rn(z);
+                                else ((float*)P.out)[at] = z;
+                            }
+                        }
+                    }
+                } else if (kMode == kLossStats) {
+                    const int label = row < m ? P.labels[row] : -1;
+                    float ref = -INFINITY, sum = 0.f;
+                    for (int c = half; c < chunks; c += 2) {
+                        const int col0 = w.n0 + c * 32;
+                        if (col0 >= n) break;
+                        float z[32];
+                        load(c, z);
+                        if (label >= col0 && label < col0 + 32) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (label == col0 + i) P.z_label[row] = z[i];
+                        }
+                        if (n - col0 < 32) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (i >= n - col0) z[i] = -INFINITY;
+                        }
+                        float mx = z[0];
+#pragma unroll
+                        for (int i = 1; i < 32; ++i) mx = fmaxf(mx, z[i]);
+                        // references in the log2 domain: whatever rounding mx * log2(e) suffers, it is the same number
+                        // that is subtracted here and added back at the end
+                        const float now = fmaxf(ref, mx * kLog2e);
+                        const float base = now == -INFINITY ? 0.f : now;
+                        sum *= ex2_approx(ref - base);
+                        const uint64_t sc = pack2(kLog2e, kLog2e), no = pack2(-base, -base);
+                        uint64_t a = pack2(0.f, 0.f), b = pack2(0.f, 0.f);
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4) {
+                            float t0, t1, t2, t3;
+                            unpack2(fma2(pack2(z[i], z[i + 1]), sc, no), t0, t1);
+                            unpack2(fma2(pack2(z[i + 2], z[i + 3]), sc, no), t2, t3);
+                            a = add2(a, pack2(ex2_approx(t0), ex2_approx(t1)));
+                            b = add2(b, pack2(ex2_approx(t2), ex2_approx(t3)));
+                        }
+                        float s0, s1;
+                        unpack2(add2(a, b), s0, s1);
+                        sum += s0 + s1;
+                        ref = now;
+                    }
+                    if (row < m) P.stats[(size_t)(w.nt * 2 + half) * P.stats_stride + row] = make_float2(ref, sum);
+                } else if (kMode == kLossGrad) {
+                    // rows past the last one that counts are written as zeros: the product over rows reads them
+                    const bool live = row < m;
+                    const int label = live ? P.labels[row] - P.piece0 : -1;
+                    const float lse2 = live ? P.lse2[row] : 0.f, g = live ? P.grad[row] : 0.f;
+                    __nv_bfloat16* out = (__nv_bfloat16*)P.out + (long long)row * P.out_stride;
+                    for (int c = half; c < chunks; c += 2) {
+                        const int col0 = w.n0 + c * 32;
+                        float z[32];
+                        load(c, z);
+                        const int valid = live ? P.V - P.piece0 - col0 : 0;     // vocabulary entries from here on
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            float p = ex2_approx(fmaf(z[i], kLog2e, -lse2));
+                            if (label == col0 + i) p -= 1.f;
+                            z[i] = i < valid ? p * g : 0.f;
+                        }
+                        if (label >= col0 && label < col0 + 32) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (label == col0 + i) P.label_err[row] = z[i] - __bfloat162float(__float2bfloat16_rn(z[i]));
+                        }
+                        store_row32(out + col0, z, 32, true);
+                    }
+                } else if (kMode == kGradHidden) {
+                    float* out = (float*)P.out + ((long long)w.slice * P.m + row) * P.out_stride;
+                    for (int c = half; c < chunks; c += 2) {
+                        const int col0 = w.n0 + c * 32;
+                        if (col0 >= n) break;
+                        float v[32];
+                        load(c, v);
+                        if (row >= m) continue;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            if (col0 + 4 * i >= n) break;   // the row pitch is a multiple of 4
+                            float4* cell = reinterpret_cast<float4*>(out + col0 + 4 * i);
+                            float4 o = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                            if (P.accumulate) {
+                                const float4 before = *cell;
+                                o.x += before.x; o.y += before.y; o.z += before.z; o.w += before.w;
+                            }
+                            *cell = o;
+                        }
+                    }
+                } else {
+                    __nv_bfloat16* out = (__nv_bfloat16*)P.out + (long long)(P.piece0 + row) * P.out_stride;
+                    const bool vec = ((uintptr_t)P.out & 15u) == 0 && (P.out_stride & 7) == 0;
+                    for (int c = half; c < chunks; c += 2) {
+                        const int col0 = w.n0 + c * 32;
+                        if (col0 >= n) break;
+                        float v[32];
+                        load(c, v);
+                        if (row < m) store_row32(out + col0, v, n - col0, vec);
+                    }
+                }
+            }
+            if (any) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&acc_empty[acc]);
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kHeadN) : "memory");
+    }
+}
+
+// ---- rows that count, in order ------------------------------------------------------------------------
+// A row whose label is negative is ignored: it is left out of the products altogether, so it costs nothing and nothing
+// it holds (padding, NaN) can reach a gradient.  The rows that count are copied next to each other, in order; each CTA
+// counts the labels before its own 32 rows.  The last CTA fills up the last block of 64 rows with zeros (the product
+// over rows reads it) and leaves the count.
+struct GatherParams {
+    const __nv_bfloat16* h; long long h_stride;
+    const int32_t* labels;
+    int N, V, d;
+    __nv_bfloat16* rows; long long rows_stride;     // compact copy
+    int32_t* live; int32_t* idx; int32_t* label;
+    float* loss; float* lse;                        // forward: zeros of the ignored rows
+    const float* lse_in; const float* grad_in; float* lse2; float* grad;    // backward
+    __nv_bfloat16* dh; long long dh_stride;         // backward: zeros of the ignored rows
+    int32_t* dev_status;
+};
+constexpr int kGatherRows = 32, kGatherThreads = 256;
+
+__global__ void __launch_bounds__(kGatherThreads) lm_head_gather_kernel(const __grid_constant__ GatherParams P)
+{
+    __shared__ int s_count[kGatherThreads / 32];
+    __shared__ int s_slot[kGatherRows];
+    pdl_wait();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int r0 = blockIdx.x * kGatherRows;
+    auto counts = [&](int label) { return label >= 0 && label < P.V; };
+    int before = 0;
+    for (int i = tid; i < r0; i += kGatherThreads) before += counts(P.labels[i]);
+    before = __reduce_add_sync(0xffffffffu, before);
+    if (lane == 0) s_count[warp] = before;
+    __syncthreads();
+    before = 0;
+    for (int w = 0; w < kGatherThreads / 32; ++w) before += s_count[w];
+    const int row = r0 + lane;
+    const int label = row < P.N ? P.labels[row] : -1;
+    const bool in = counts(label);
+    const unsigned mask = __ballot_sync(0xffffffffu, in);
+    const int slot = before + __popc(mask & ((1u << lane) - 1u));
+    if (warp == 0) {
+        s_slot[lane] = in ? slot : -1;
+        if (in) {
+            P.idx[slot] = row;
+            P.label[slot] = label;
+            if (P.lse2) { P.lse2[slot] = P.lse_in[row] * kLog2e; P.grad[slot] = P.grad_in[row]; }
+        } else if (row < P.N) {
+            if (P.loss) { P.loss[row] = 0.f; P.lse[row] = 0.f; }
+            if (label >= P.V) atomicOr(P.dev_status, DSPARK_DEV_BAD_TOKEN);
+        }
+    }
+    __syncthreads();
+    const bool vec = P.d % 8 == 0 && ((uintptr_t)P.h & 15u) == 0 && P.h_stride % 8 == 0;
+    for (int r = warp; r < kGatherRows && r0 + r < P.N; r += kGatherThreads / 32) {
+        const int to = s_slot[r];
+        const __nv_bfloat16* src = P.h + (long long)(r0 + r) * P.h_stride;
+        if (to >= 0) {
+            __nv_bfloat16* dst = P.rows + (long long)to * P.rows_stride;
+            if (vec) for (int i = lane; i < P.d / 8; i += 32) reinterpret_cast<uint4*>(dst)[i] = reinterpret_cast<const uint4*>(src)[i];
+            else for (int i = lane; i < P.d; i += 32) dst[i] = src[i];
+        } else if (P.dh) {
+            __nv_bfloat16* dst = P.dh + (long long)(r0 + r) * P.dh_stride;
+            for (int i = lane; i < P.d; i += 32) dst[i] = __float2bfloat16_rn(0.f);
+        }
+    }
+    if (blockIdx.x == gridDim.x - 1) {
+        const int total = before + __popc(mask);
+        if (tid == 0) *P.live = total;
+        const int end = (total + 63) & ~63;
+        for (int r = total + warp; r < end; r += kGatherThreads / 32)
+            for (int i = lane; i < P.d; i += 32) P.rows[(long long)r * P.rows_stride + i] = __float2bfloat16_rn(0.f);
+    }
+}
+
+// ---- loss of every row from the statistics of the vocabulary tiles --------------------------------------
+// 32 rows per CTA, one per lane; the warps share the entries.  lse = ln 2 * (R + log2(sum s_i 2^(r_i - R))), in 64 bits.
+struct LossParams {
+    const float2* stats; long long stats_stride; int entries;
+    const float* z_label; const int32_t* idx; const int32_t* live;
+    float* loss; float* lse; int32_t* dev_status;
+};
+constexpr int kLossWarps = 16;
+
+__global__ void __launch_bounds__(kLossWarps * 32) lm_head_loss_kernel(const __grid_constant__ LossParams P)
+{
+    __shared__ float s_ref[kLossWarps][32];
+    __shared__ double s_sum[kLossWarps][32];
+    pdl_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int row = blockIdx.x * 32 + lane, live = *P.live;
+    if (blockIdx.x * 32 >= live) return;
+    float ref = -INFINITY;
+    double sum = 0.0;
+    if (row < live) {
+        for (int e = warp; e < P.entries; e += kLossWarps) {
+            const float2 v = P.stats[(size_t)e * P.stats_stride + row];
+            const float now = fmaxf(ref, v.x);
+            const float base = now == -INFINITY ? 0.f : now;
+            sum = sum * (double)ex2_approx(ref - base) + (double)(v.y * ex2_approx(v.x - base));
+            ref = now;
+        }
+    }
+    s_ref[warp][lane] = ref;
+    s_sum[warp][lane] = sum;
+    __syncthreads();
+    if (warp || row >= live) return;
+    float top = -INFINITY;
+    for (int w = 0; w < kLossWarps; ++w) top = fmaxf(top, s_ref[w][lane]);
+    const float base = top == -INFINITY ? 0.f : top;
+    double total = 0.0;
+    for (int w = 0; w < kLossWarps; ++w) total += s_sum[w][lane] * (double)ex2_approx(s_ref[w][lane] - base);
+    const double lse = ((double)base + log2(total)) * 0.69314718055994530942;
+    const int at = P.idx[row];
+    const float loss = (float)(lse - (double)P.z_label[row]);
+    P.loss[at] = loss;
+    P.lse[at] = (float)lse;
+    if (!(fabsf(loss) < INFINITY)) atomicOr(P.dev_status, DSPARK_DEV_BAD_ROW);
+}
+
+// ---- gradient of the hidden states from the slices' partial sums ---------------------------------------
+// The label's entry of G is most of the row: what its rounding to bf16 lost is added back here, times the label's row of
+// W.  The sum runs over the slices in order: the same bits every time.
+struct HiddenParams {
+    const float* part; long long part_stride; int slices, m;
+    const float* label_err; const int32_t* label; const int32_t* idx; const int32_t* live;
+    const __nv_bfloat16* w; long long w_stride;
+    int d;
+    __nv_bfloat16* dh; long long dh_stride;
+};
+__global__ void __launch_bounds__(256) lm_head_grad_hidden_kernel(const __grid_constant__ HiddenParams P)
+{
+    pdl_wait();
+    const int row = blockIdx.x;
+    if (row >= *P.live) return;
+    const float err = P.label_err[row];
+    const __nv_bfloat16* w = P.w + (long long)P.label[row] * P.w_stride;
+    __nv_bfloat16* out = P.dh + (long long)P.idx[row] * P.dh_stride;
+    for (int c = threadIdx.x; c < P.d; c += 256) {
+        float sum = err * __bfloat162float(w[c]);
+        for (int s = 0; s < P.slices; ++s) sum += P.part[((long long)s * P.m + row) * P.part_stride + c];
+        out[c] = __float2bfloat16_rn(sum);
+    }
+}
+
+// ---- int8 weights ------------------------------------------------------------------------------------------
+// One row (a vocabulary entry) per CTA: q = rint(127 w / max|w|), scale = max|w| / 127.
+__global__ void __launch_bounds__(256) lm_head_quantize_kernel(const __nv_bfloat16* __restrict__ W, long long w_stride, int K,
+                                                               int8_t* __restrict__ q, long long q_stride, float* __restrict__ scale)
+{
+    __shared__ float s_top[8];
+    pdl_wait();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const __nv_bfloat16* w = W + (long long)blockIdx.x * w_stride;
+    int8_t* out = q + (long long)blockIdx.x * q_stride;
+    float top = 0.f;
+    for (int i = tid; i < K; i += 256) {
+        const float a = fabsf(__bfloat162float(w[i]));
+        top = (a > top || a != a) ? a : top;
+    }
+    const bool bad = __syncthreads_or(!(top < INFINITY)) != 0;
+    top = warp_max_f32(top);
+    if (lane == 0) s_top[warp] = top;
+    __syncthreads();
+    top = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, s_top[i]);
+    for (int i = tid; i < K; i += 256) {
+        // 127 w has 15 significant bits: the correctly rounded quotient keeps a half a half
+        const float v = (bad || top == 0.f) ? 0.f : rintf(__fdiv_rn(127.f * __bfloat162float(w[i]), top));
+        out[i] = (int8_t)v;
+    }
+    if (tid == 0) scale[blockIdx.x] = bad ? NAN : top / 127.f;
+}
+
+// ---- host side ---------------------------------------------------------------------------------------------
+static size_t up(size_t x, size_t to) { return (x + to - 1) / to * to; }
+
+// 2-D operand [rows, cols] of `es`-byte elements; boxes of box_cols x box_rows, 128-byte swizzle, zeros outside
+static bool operand_map(CUtensorMap* map, const void* base, int es, long long rows, long long cols, long long pitch_bytes, int box_cols, int box_rows)
+{
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)pitch_bytes};
+    const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
+    const cuuint32_t estr[2] = {1, 1};
+    return fn(map, es == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims,
+              strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+static int device_sms()
+{
+    static std::atomic<int> sms[64];
+    int dev = 0;
+    cudaGetDevice(&dev);
+    int v = sms[dev & 63].load(std::memory_order_relaxed);
+    if (!v) {
+        cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev);
+        sms[dev & 63].store(v, std::memory_order_relaxed);
+    }
+    return v;
+}
+
+template <int kMode>
+static int head_launch(HeadParams P, const CUtensorMap& a, const CUtensorMap& b, cudaStream_t s, int timer_id)
+{
+    constexpr int kSmem = kHeadRingBytes + 1024;
+    static std::atomic<unsigned long long> ready{0};        // one bit per device
+    int dev = 0;
+    cudaGetDevice(&dev);
+    const unsigned long long bit = 1ull << (dev & 63);
+    if (!(ready.load(std::memory_order_relaxed) & bit)) {
+        if (cudaFuncSetAttribute(lm_head_kernel<kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess)
+            return launch_status();
+        ready.fetch_or(bit, std::memory_order_relaxed);
+    }
+    P.stages = kHeadRingBytes / (kTileABytes + P.n_tile * kRowBytes);
+    if (P.stages > kHeadMaxStages) P.stages = kHeadMaxStages;
+    const long long units = (long long)((P.m + kHeadM - 1) / kHeadM) * ((P.n + P.n_tile - 1) / P.n_tile) * P.slices;
+    const int sms = device_sms();
+    KernelTimerScope timer(timer_id, s);
+    launch_pdl(lm_head_kernel<kMode>, dim3((unsigned)(units < sms ? units : sms)), dim3(kHeadThreads), kSmem, s, P, a, b);
+    return launch_status();
+}
+
+constexpr int kMaxRows = 1 << 20, kMaxVocab = 1 << 24, kMaxWidth = 1 << 16;
+
+struct LossWs {
+    size_t live, idx, label, z_label, lse2, grad, label_err, rows, stats, G, part, total;
+    long long n_pad, d_pitch, part_pitch;
+    int piece, slices, n_tile_d;
+};
+static LossWs loss_layout(int N, int V, int d)
+{
+    LossWs w;
+    w.n_pad = (long long)up((size_t)N, kHeadM);
+    w.d_pitch = (long long)up((size_t)d, 8);
+    w.part_pitch = (long long)up((size_t)d, 4);
+    size_t o = 0;
+    auto take = [&](size_t bytes) { const size_t at = o; o += up(bytes, 256); return at; };
+    w.live = take(4);
+    w.idx = take(4 * (size_t)w.n_pad); w.label = take(4 * (size_t)w.n_pad); w.z_label = take(4 * (size_t)w.n_pad);
+    w.lse2 = take(4 * (size_t)w.n_pad); w.grad = take(4 * (size_t)w.n_pad); w.label_err = take(4 * (size_t)w.n_pad);
+    w.rows = take(2 * (size_t)w.n_pad * (size_t)w.d_pitch);
+    const size_t common = o;
+    // forward: two entries per vocabulary tile and row
+    w.stats = take(2 * up((size_t)V, kHeadN) / kHeadN * (size_t)w.n_pad * sizeof(float2));
+    const size_t forward = o;
+    // backward: the piece of G that is kept at a time is about 64 MB, half of the L2, and not narrower than 2 048
+    // entries, below which adding the partial sums of dH would cost more than the products
+    o = common;
+    long long piece = (64ll << 20) / (2 * w.n_pad) / kHeadN * kHeadN;
+    if (piece < 2048) piece = 2048;
+    const long long all = (long long)up((size_t)V, kHeadN);
+    if (piece > all) piece = all;
+    w.piece = (int)piece;
+    w.n_tile_d = d >= kHeadN ? kHeadN : (int)up((size_t)d, 64);
+    const long long tiles = w.n_pad / kHeadM * ((d + w.n_tile_d - 1) / w.n_tile_d);
+    long long slices = 296 / tiles;                         // two tiles an SM
+    const long long most = piece / 64 / 8;                  // at least 8 k blocks a slice
+    if (slices > most) slices = most;
+    if (slices > 64) slices = 64;
+    if (slices < 1) slices = 1;
+    w.slices = (int)slices;
+    w.G = take(2 * (size_t)w.n_pad * (size_t)piece);
+    w.part = take(4 * (size_t)slices * (size_t)w.n_pad * (size_t)w.part_pitch);
+    w.total = o > forward ? o : forward;
+    return w;
+}
+
+static int loss_check(const void* hidden, int64_t h_stride, const void* weight, int64_t w_stride, const void* labels, int N, int V, int d,
+                      const void* dev_status, const void* workspace, size_t workspace_bytes, const LossWs& w)
+{
+    if (!hidden || !weight || !labels || !dev_status || h_stride < d || w_stride < d) return DSPARK_ERR_INVALID_ARG;
+    if (!workspace || workspace_bytes < w.total) return DSPARK_ERR_WORKSPACE;
+    if (((uintptr_t)workspace & 255u) || ((uintptr_t)hidden & 1u) || ((uintptr_t)weight & 15u) || (w_stride & 7) || ((uintptr_t)labels & 3u))
+        return DSPARK_ERR_ALIGNMENT;
+    return DSPARK_OK;
+}
+
+}  // namespace dspark
+
+using namespace dspark;
+
+extern "C" {
+
+int dspark_lm_head_quantize(const void* W, int64_t w_row_stride, int V, int K, int8_t* out_q, int64_t out_q_row_stride,
+                            float* out_scale, void* stream)
+{
+    if (!W || !out_q || !out_scale || V < 1 || K < 1 || w_row_stride < K || out_q_row_stride < K) return DSPARK_ERR_INVALID_ARG;
+    if (((uintptr_t)W & 1u) || ((uintptr_t)out_scale & 3u)) return DSPARK_ERR_ALIGNMENT;
+    launch_pdl(lm_head_quantize_kernel, dim3(V), dim3(256), 0, (cudaStream_t)stream, (const __nv_bfloat16*)W, (long long)w_row_stride, K,
+               out_q, (long long)out_q_row_stride, out_scale);
+    return launch_status();
+}
+
+int dspark_lm_head_int8(const int8_t* x_q, int64_t x_row_stride, const float* x_scale, const int8_t* w_q, int64_t w_row_stride,
+                        const float* w_scale, int rows, int V, int K, const int32_t* n_live, void* out_logits, int out_dtype,
+                        int64_t out_row_stride, int32_t* dev_status, void* stream)
+{
+    if (!x_q || !x_scale || !w_q || !w_scale || !out_logits || !dev_status || rows < 1 || V < 1 || K < 1) return DSPARK_ERR_INVALID_ARG;
+    if (out_dtype != DSPARK_F32 && out_dtype != DSPARK_BF16) return DSPARK_ERR_INVALID_ARG;
+    if (x_row_stride < K || w_row_stride < K || out_row_stride < V) return DSPARK_ERR_INVALID_ARG;
+    if (rows > kMaxRows || V > kMaxVocab || K > kMaxWidth) return DSPARK_ERR_SHAPE;
+    if (((uintptr_t)x_q & 15u) || ((uintptr_t)w_q & 15u) || (x_row_stride & 15) || (w_row_stride & 15) || ((uintptr_t)x_scale & 3u) ||
+        ((uintptr_t)w_scale & 3u) || ((uintptr_t)out_logits & (out_dtype == DSPARK_BF16 ? 1u : 3u)) || ((uintptr_t)n_live & 3u))
+        return DSPARK_ERR_ALIGNMENT;
+    HeadParams P;
+    memset(&P, 0, sizeof P);
+    P.m = V; P.n = rows; P.k = K; P.V = V;
+    P.n_tile = rows >= kHeadN ? kHeadN : (int)up((size_t)rows, 32);
+    P.slices = 1; P.kb_slice = (K + 127) / 128;
+    P.live = n_live; P.dev_status = dev_status;
+    P.out = out_logits; P.out_stride = out_row_stride; P.out_bf16 = out_dtype == DSPARK_BF16;
+    P.row_scale = x_scale; P.col_scale = w_scale;
+    CUtensorMap a, b;
+    if (!operand_map(&a, w_q, 1, V, K, w_row_stride, kRowBytes, kHeadM) || !operand_map(&b, x_q, 1, rows, K, x_row_stride, kRowBytes, P.n_tile))
+        return DSPARK_ERR_CUDA;
+    return head_launch<kInt8Logits>(P, a, b, (cudaStream_t)stream, DSPARK_K_HEAD_INT8);
+}
+
+size_t dspark_lm_head_loss_workspace_bytes(int N, int V, int d)
+{
+    if (N < 1 || V < 1 || d < 1 || N > kMaxRows || V > kMaxVocab || d > kMaxWidth) return 0;
+    return loss_layout(N, V, d).total;
+}
+
+int dspark_lm_head_loss(const void* hidden, int64_t hidden_row_stride, const void* weight, int64_t weight_row_stride,
+                        const int32_t* labels, int N, int V, int d, float* out_loss, float* out_lse, int32_t* dev_status,
+                        void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!out_loss || !out_lse || N < 1 || V < 1 || d < 1) return DSPARK_ERR_INVALID_ARG;
+    if (N > kMaxRows || V > kMaxVocab || d > kMaxWidth) return DSPARK_ERR_SHAPE;
+    const LossWs w = loss_layout(N, V, d);
+    const int rc0 = loss_check(hidden, hidden_row_stride, weight, weight_row_stride, labels, N, V, d, dev_status, workspace, workspace_bytes, w);
+    if (rc0 != DSPARK_OK) return rc0;
+    if (((uintptr_t)out_loss | (uintptr_t)out_lse) & 3u) return DSPARK_ERR_ALIGNMENT;
+    unsigned char* ws = (unsigned char*)workspace;
+    cudaStream_t s = (cudaStream_t)stream;
+    GatherParams g;
+    memset(&g, 0, sizeof g);
+    g.h = (const __nv_bfloat16*)hidden; g.h_stride = hidden_row_stride; g.labels = labels; g.N = N; g.V = V; g.d = d;
+    g.rows = (__nv_bfloat16*)(ws + w.rows); g.rows_stride = w.d_pitch;
+    g.live = (int32_t*)(ws + w.live); g.idx = (int32_t*)(ws + w.idx); g.label = (int32_t*)(ws + w.label);
+    g.loss = out_loss; g.lse = out_lse; g.dev_status = dev_status;
+    {
+        KernelTimerScope timer(DSPARK_K_HEAD_ROWS, s);
+        launch_pdl(lm_head_gather_kernel, dim3((N + kGatherRows - 1) / kGatherRows), dim3(kGatherThreads), 0, s, g);
+    }
+    HeadParams P;
+    memset(&P, 0, sizeof P);
+    P.m = N; P.n = V; P.k = d; P.V = V;
+    P.n_tile = kHeadN; P.slices = 1; P.kb_slice = (d + 63) / 64;
+    P.live = g.live; P.dev_status = dev_status;
+    P.stats = (float2*)(ws + w.stats); P.stats_stride = w.n_pad; P.labels = g.label; P.z_label = (float*)(ws + w.z_label);
+    CUtensorMap a, b;
+    if (!operand_map(&a, g.rows, 2, w.n_pad, d, w.d_pitch * 2, 64, kHeadM) || !operand_map(&b, weight, 2, V, d, weight_row_stride * 2, 64, kHeadN))
+        return DSPARK_ERR_CUDA;
+    const int rc = head_launch<kLossStats>(P, a, b, s, DSPARK_K_HEAD_LOSS);
+    if (rc != DSPARK_OK) return rc;
+    LossParams L;
+    L.stats = P.stats; L.stats_stride = w.n_pad; L.entries = 2 * ((V + kHeadN - 1) / kHeadN);
+    L.z_label = P.z_label; L.idx = g.idx; L.live = g.live; L.loss = out_loss; L.lse = out_lse; L.dev_status = dev_status;
+    {
+        KernelTimerScope timer(DSPARK_K_HEAD_ROWS, s);
+        launch_pdl(lm_head_loss_kernel, dim3((N + 31) / 32), dim3(kLossWarps * 32), 0, s, L);
+    }
+    return launch_status();
+}
+
+int dspark_lm_head_loss_backward(const void* hidden, int64_t hidden_row_stride, const void* weight, int64_t weight_row_stride,
+                                 const int32_t* labels, const float* lse, const float* grad_loss, int N, int V, int d,
+                                 void* out_grad_hidden, int64_t grad_hidden_row_stride, void* out_grad_weight,
+                                 int64_t grad_weight_row_stride, int32_t* dev_status, void* workspace, size_t workspace_bytes,
+                                 void* stream)
+{
+    if (!lse || !grad_loss || (!out_grad_hidden && !out_grad_weight) || N < 1 || V < 1 || d < 1) return DSPARK_ERR_INVALID_ARG;
+    if ((out_grad_hidden && grad_hidden_row_stride < d) || (out_grad_weight && grad_weight_row_stride < d)) return DSPARK_ERR_INVALID_ARG;
+    if (N > kMaxRows || V > kMaxVocab || d > kMaxWidth) return DSPARK_ERR_SHAPE;
+    const LossWs w = loss_layout(N, V, d);
+    const int rc0 = loss_check(hidden, hidden_row_stride, weight, weight_row_stride, labels, N, V, d, dev_status, workspace, workspace_bytes, w);
+    if (rc0 != DSPARK_OK) return rc0;
+    if ((((uintptr_t)lse | (uintptr_t)grad_loss) & 3u) || (((uintptr_t)out_grad_hidden | (uintptr_t)out_grad_weight) & 1u))
+        return DSPARK_ERR_ALIGNMENT;
+    unsigned char* ws = (unsigned char*)workspace;
+    cudaStream_t s = (cudaStream_t)stream;
+    GatherParams g;
+    memset(&g, 0, sizeof g);
+    g.h = (const __nv_bfloat16*)hidden; g.h_stride = hidden_row_stride; g.labels = labels; g.N = N; g.V = V; g.d = d;
+    g.rows = (__nv_bfloat16*)(ws + w.rows); g.rows_stride = w.d_pitch;
+    g.live = (int32_t*)(ws + w.live); g.idx = (int32_t*)(ws + w.idx); g.label = (int32_t*)(ws + w.label);
+    g.lse_in = lse; g.grad_in = grad_loss; g.lse2 = (float*)(ws + w.lse2); g.grad = (float*)(ws + w.grad);
+    g.dh = (__nv_bfloat16*)out_grad_hidden; g.dh_stride = grad_hidden_row_stride; g.dev_status = dev_status;
+    {
+        KernelTimerScope timer(DSPARK_K_HEAD_ROWS, s);
+        launch_pdl(lm_head_gather_kernel, dim3((N + kGatherRows - 1) / kGatherRows), dim3(kGatherThreads), 0, s, g);
+    }
+    void* G = ws + w.G;
+    CUtensorMap rows_k, w_k, g_k, w_mn, g_mn, rows_mn;
+    if (!operand_map(&rows_k, g.rows, 2, w.n_pad, d, w.d_pitch * 2, 64, kHeadM) ||
+        !operand_map(&w_k, weight, 2, V, d, weight_row_stride * 2, 64, kHeadN) ||
+        !operand_map(&g_k, G, 2, w.n_pad, w.piece, (long long)w.piece * 2, 64, kHeadM) ||
+        !operand_map(&w_mn, weight, 2, V, d, weight_row_stride * 2, 64, 64) ||
+        !operand_map(&g_mn, G, 2, w.n_pad, w.piece, (long long)w.piece * 2, 64, 64) ||
+        !operand_map(&rows_mn, g.rows, 2, w.n_pad, d, w.d_pitch * 2, 64, 64))
+        return DSPARK_ERR_CUDA;
+    for (int v0 = 0; v0 < V; v0 += w.piece) {
+        const int here = V - v0 < w.piece ? V - v0 : w.piece;
+        HeadParams P;
+        memset(&P, 0, sizeof P);
+        P.V = V; P.piece0 = v0; P.live = g.live; P.dev_status = dev_status; P.slices = 1;
+        HeadParams Q = P;
+        Q.m = N; Q.n = here; Q.k = d; Q.n_tile = kHeadN; Q.kb_slice = (d + 63) / 64;
+        Q.out = G; Q.out_stride = w.piece; Q.labels = g.label; Q.lse2 = g.lse2; Q.grad = g.grad; Q.label_err = (float*)(ws + w.label_err);
+        int rc = head_launch<kLossGrad>(Q, rows_k, w_k, s, DSPARK_K_HEAD_LOSS);
+        if (rc != DSPARK_OK) return rc;
+        if (out_grad_hidden) {
+            Q = P;
+            Q.m = N; Q.n = d; Q.k = here; Q.n_tile = w.n_tile_d; Q.slices = w.slices;
+            Q.kb_slice = (w.piece / 64 + w.slices - 1) / w.slices;
+            Q.out = ws + w.part; Q.out_stride = w.part_pitch; Q.accumulate = v0 > 0;
+            rc = head_launch<kGradHidden>(Q, g_k, w_mn, s, DSPARK_K_HEAD_GRAD);
+            if (rc != DSPARK_OK) return rc;
+        }
+        if (out_grad_weight) {
+            Q = P;
+            Q.m = here; Q.n = d; Q.k = N; Q.n_tile = w.n_tile_d; Q.kb_slice = (N + 63) / 64;
+            Q.out = out_grad_weight; Q.out_stride = grad_weight_row_stride;
+            rc = head_launch<kGradWeight>(Q, g_mn, rows_mn, s, DSPARK_K_HEAD_GRAD);
+            if (rc != DSPARK_OK) return rc;
+        }
+    }
+    if (out_grad_hidden) {
+        HiddenParams Hp;
+        Hp.part = (const float*)(ws + w.part); Hp.part_stride = w.part_pitch; Hp.slices = w.slices; Hp.m = N;
+        Hp.label_err = (const float*)(ws + w.label_err); Hp.label = g.label; Hp.idx = g.idx; Hp.live = g.live;
+        Hp.w = (const __nv_bfloat16*)weight; Hp.w_stride = weight_row_stride; Hp.d = d;
+        Hp.dh = g.dh; Hp.dh_stride = grad_hidden_row_stride;
+        KernelTimerScope timer(DSPARK_K_HEAD_ROWS, s);
+        launch_pdl(lm_head_grad_hidden_kernel, dim3(N), dim3(256), 0, s, Hp);
+    }
+    return launch_status();
+}
+
+}  // extern "C"
