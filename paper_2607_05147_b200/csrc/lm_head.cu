@@ -44,6 +44,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 struct HeadParams {
     int m, n, k;                    // extents; the one that counts rows is bounded by *live
     int n_tile, stages;
+    int box_n;                      // rows of a k-major B box: n_tile, or less where the operand has less
     int slices, kb_slice;           // the k blocks cut into slices (GradHidden), 1 otherwise
     int piece0;                     // first vocabulary entry of the piece (LossGrad, GradHidden, GradWeight)
     int V;
@@ -98,6 +99,22 @@ __device__ __forceinline__ void store_row32(__nv_bfloat16* p, const float (&v)[3
 #pragma unroll
         for (int i = 0; i < 32; ++i)
             if (i < n) p[i] = __float2bfloat16_rn(v[i]);
+    }
+}
+
+__device__ __forceinline__ void put(float* p, float v) { *p = v; }
+__device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+
+// One element to each of the first `n` of 32 rows.
+template <typename T>
+__device__ __forceinline__ void store_column32(T* p, long long stride, const float (&v)[32], int n)
+{
+    if (n >= 32) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) { put(p, v[i]); p += stride; }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) { if (i < n) put(p, v[i]); p += stride; }
     }
 }
 
@@ -162,6 +179,7 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
         return r;
     };
     const int stage_bytes = kTileABytes + P.n_tile * kRowBytes;
+    const uint32_t load_bytes = (uint32_t)(kTileABytes + (kBMn ? P.n_tile : P.box_n) * kRowBytes);
     const int first = (int)blockIdx.x, step = (int)gridDim.x;
 
     if (warp == 0) {
@@ -176,7 +194,7 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
                     if (!mbar_wait_bounded(&empty[s], ph ^ 1u)) { give_up(); break; }
                     unsigned char* a = smem + (size_t)s * stage_bytes;
                     unsigned char* b = a + kTileABytes;
-                    mbar_arrive_expect_tx(&full[s], (uint32_t)stage_bytes);
+                    mbar_arrive_expect_tx(&full[s], load_bytes);
                     const int kx = kb * kBlockK;
                     if (kAMn) {
 #pragma unroll
@@ -268,23 +286,20 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
             };
             if (warp_live) {
                 if (kMode == kInt8Logits) {
-                    const float sw = row < m ? P.col_scale[row] : 0.f;
+                    const bool in = row < m;
+                    const float sw = in ? P.col_scale[row] : 0.f;
                     for (int c = half; c < chunks; c += 2) {
                         const int col0 = w.n0 + c * 32;
                         if (col0 >= n) break;
+                        const float sx = col0 + lane < n ? P.row_scale[col0 + lane] : 0.f;
                         float v[32];
                         load(c, v);
-                        const float sx = col0 + lane < n ? P.row_scale[col0 + lane] : 0.f;
-                        const int valid = n - col0;
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            const float z = (float)__float_as_int(v[i]) * __shfl_sync(0xffffffffu, sx, i) * sw;
-                            if (i < valid && row < m) {
-                                const long long at = (long long)(col0 + i) * P.out_stride + row;
-                                if (P.out_bf16) ((__nv_bfloat16*)P.out)[at] = __float2bfloat16_rn(z);
-                                else ((float*)P.out)[at] = z;
-                            }
-                        }
+                        for (int i = 0; i < 32; ++i) v[i] = (float)__float_as_int(v[i]) * __shfl_sync(0xffffffffu, sx, i) * sw;
+                        // lanes are neighbouring vocabulary entries: a warp stores 32 neighbours of one row at a time
+                        const int valid = in ? n - col0 : 0;
+                        if (P.out_bf16) store_column32((__nv_bfloat16*)P.out + (long long)col0 * P.out_stride + row, P.out_stride, v, valid);
+                        else store_column32((float*)P.out + (long long)col0 * P.out_stride + row, P.out_stride, v, valid);
                     }
                 } else if (kMode == kLossStats) {
                     const int label = row < m ? P.labels[row] : -1;
@@ -402,7 +417,7 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
 // ---- rows that count, in order ------------------------------------------------------------------------
 // A row whose label is negative is ignored: it is left out of the products altogether, so it costs nothing and nothing
 // it holds (padding, NaN) can reach a gradient.  The rows that count are copied next to each other, in order; each CTA
-// counts the labels before its own 32 rows.  The last CTA fills up the last block of 64 rows with zeros (the product
+// counts the labels before its own rows.  The last CTA fills up the last block of 64 rows with zeros (the product
 // over rows reads it) and leaves the count.
 struct GatherParams {
     const __nv_bfloat16* h; long long h_stride;
@@ -415,8 +430,10 @@ struct GatherParams {
     __nv_bfloat16* dh; long long dh_stride;         // backward: zeros of the ignored rows
     int32_t* dev_status;
 };
-constexpr int kGatherRows = 32, kGatherThreads = 256;
+constexpr int kGatherThreads = 256;
 
+// kGatherRows: 8, a row per warp, while counting the labels of the rows before costs nothing; 32 for long inputs
+template <int kGatherRows>
 __global__ void __launch_bounds__(kGatherThreads) lm_head_gather_kernel(const __grid_constant__ GatherParams P)
 {
     __shared__ int s_count[kGatherThreads / 32];
@@ -433,11 +450,11 @@ __global__ void __launch_bounds__(kGatherThreads) lm_head_gather_kernel(const __
     before = 0;
     for (int w = 0; w < kGatherThreads / 32; ++w) before += s_count[w];
     const int row = r0 + lane;
-    const int label = row < P.N ? P.labels[row] : -1;
+    const int label = lane < kGatherRows && row < P.N ? P.labels[row] : -1;
     const bool in = counts(label);
     const unsigned mask = __ballot_sync(0xffffffffu, in);
     const int slot = before + __popc(mask & ((1u << lane) - 1u));
-    if (warp == 0) {
+    if (warp == 0 && lane < kGatherRows) {
         s_slot[lane] = in ? slot : -1;
         if (in) {
             P.idx[slot] = row;
@@ -471,43 +488,62 @@ __global__ void __launch_bounds__(kGatherThreads) lm_head_gather_kernel(const __
     }
 }
 
+static void gather_launch(const GatherParams& g, cudaStream_t s)
+{
+    if (g.N <= 16384) launch_pdl(lm_head_gather_kernel<8>, dim3((g.N + 7) / 8), dim3(kGatherThreads), 0, s, g);
+    else launch_pdl(lm_head_gather_kernel<32>, dim3((g.N + 31) / 32), dim3(kGatherThreads), 0, s, g);
+}
+
 // ---- loss of every row from the statistics of the vocabulary tiles --------------------------------------
-// 32 rows per CTA, one per lane; the warps share the entries.  lse = ln 2 * (R + log2(sum s_i 2^(r_i - R))), in 64 bits.
+// Eight rows per CTA, 128 threads per row, each taking every 128th entry (eight loads in flight): at V = 129 280 a row has
+// 1 010 entries.  lse = ln 2 * (R + log2(sum s_i 2^(r_i - R))), the sum over threads in 64 bits.
 struct LossParams {
     const float2* stats; long long stats_stride; int entries;
     const float* z_label; const int32_t* idx; const int32_t* live;
     float* loss; float* lse; int32_t* dev_status;
 };
-constexpr int kLossWarps = 16;
+constexpr int kLossRows = 8, kLossThreads = 1024, kLossPer = 8;
 
-__global__ void __launch_bounds__(kLossWarps * 32) lm_head_loss_kernel(const __grid_constant__ LossParams P)
+__global__ void __launch_bounds__(kLossThreads) lm_head_loss_kernel(const __grid_constant__ LossParams P)
 {
-    __shared__ float s_ref[kLossWarps][32];
-    __shared__ double s_sum[kLossWarps][32];
+    __shared__ float s_ref[kLossThreads / 32][kLossRows];
+    __shared__ double s_sum[kLossThreads / 32][kLossRows];
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int row = blockIdx.x * 32 + lane, live = *P.live;
-    if (blockIdx.x * 32 >= live) return;
-    float ref = -INFINITY;
-    double sum = 0.0;
-    if (row < live) {
-        for (int e = warp; e < P.entries; e += kLossWarps) {
-            const float2 v = P.stats[(size_t)e * P.stats_stride + row];
-            const float now = fmaxf(ref, v.x);
-            const float base = now == -INFINITY ? 0.f : now;
-            sum = sum * (double)ex2_approx(ref - base) + (double)(v.y * ex2_approx(v.x - base));
-            ref = now;
+    const int row = blockIdx.x * kLossRows + (lane & 7), live = *P.live;
+    if (blockIdx.x * kLossRows >= live) return;
+    const int first = (int)threadIdx.x >> 3;
+    float ref = -INFINITY, sum = 0.f;
+    for (int e0 = first; e0 < P.entries; e0 += 128 * kLossPer) {
+        float2 v[kLossPer];
+        float now = ref;
+#pragma unroll
+        for (int i = 0; i < kLossPer; ++i) {
+            const int e = e0 + 128 * i;
+            v[i] = e < P.entries && row < live ? P.stats[(size_t)e * P.stats_stride + row] : make_float2(-INFINITY, 0.f);
         }
+#pragma unroll
+        for (int i = 0; i < kLossPer; ++i) now = fmaxf(now, v[i].x);
+        const float base = now == -INFINITY ? 0.f : now;
+        sum *= ex2_approx(ref - base);
+#pragma unroll
+        for (int i = 0; i < kLossPer; ++i) sum = fmaf(v[i].y, ex2_approx(v[i].x - base), sum);
+        ref = now;
     }
-    s_ref[warp][lane] = ref;
-    s_sum[warp][lane] = sum;
+    float top = ref;
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+    double part = (double)(sum * ex2_approx(ref - (top == -INFINITY ? 0.f : top)));
+    part += __shfl_xor_sync(0xffffffffu, part, 8);
+    part += __shfl_xor_sync(0xffffffffu, part, 16);
+    if (lane < kLossRows) { s_ref[warp][lane] = top; s_sum[warp][lane] = part; }
     __syncthreads();
-    if (warp || row >= live) return;
-    float top = -INFINITY;
-    for (int w = 0; w < kLossWarps; ++w) top = fmaxf(top, s_ref[w][lane]);
+    if (warp || lane >= kLossRows || row >= live) return;
+    top = -INFINITY;
+    for (int w = 0; w < kLossThreads / 32; ++w) top = fmaxf(top, s_ref[w][lane]);
     const float base = top == -INFINITY ? 0.f : top;
     double total = 0.0;
-    for (int w = 0; w < kLossWarps; ++w) total += s_sum[w][lane] * (double)ex2_approx(s_ref[w][lane] - base);
+    for (int w = 0; w < kLossThreads / 32; ++w) total += s_sum[w][lane] * (double)ex2_approx(s_ref[w][lane] - base);
     const double lse = ((double)base + log2(total)) * 0.69314718055994530942;
     const int at = P.idx[row];
     const float loss = (float)(lse - (double)P.z_label[row]);
@@ -708,13 +744,17 @@ int dspark_lm_head_int8(const int8_t* x_q, int64_t x_row_stride, const float* x_
     HeadParams P;
     memset(&P, 0, sizeof P);
     P.m = V; P.n = rows; P.k = K; P.V = V;
-    P.n_tile = rows >= kHeadN ? kHeadN : (int)up((size_t)rows, 32);
+    // row tiles of one size, and no taller a box than there are rows: a box that reaches past the last row costs the copy
+    // engine more than one that does not (one row of 32: 170 us instead of 90 at V = 129 280, K = 4 096)
+    const int row_tiles = (rows + kHeadN - 1) / kHeadN;
+    P.n_tile = (int)up((size_t)((rows + row_tiles - 1) / row_tiles), 32);
+    P.box_n = rows < P.n_tile ? rows : P.n_tile;
     P.slices = 1; P.kb_slice = (K + 127) / 128;
     P.live = n_live; P.dev_status = dev_status;
     P.out = out_logits; P.out_stride = out_row_stride; P.out_bf16 = out_dtype == DSPARK_BF16;
     P.row_scale = x_scale; P.col_scale = w_scale;
     CUtensorMap a, b;
-    if (!operand_map(&a, w_q, 1, V, K, w_row_stride, kRowBytes, kHeadM) || !operand_map(&b, x_q, 1, rows, K, x_row_stride, kRowBytes, P.n_tile))
+    if (!operand_map(&a, w_q, 1, V, K, w_row_stride, kRowBytes, kHeadM) || !operand_map(&b, x_q, 1, rows, K, x_row_stride, kRowBytes, P.box_n))
         return DSPARK_ERR_CUDA;
     return head_launch<kInt8Logits>(P, a, b, (cudaStream_t)stream, DSPARK_K_HEAD_INT8);
 }
@@ -745,16 +785,16 @@ int dspark_lm_head_loss(const void* hidden, int64_t hidden_row_stride, const voi
     g.loss = out_loss; g.lse = out_lse; g.dev_status = dev_status;
     {
         KernelTimerScope timer(DSPARK_K_HEAD_ROWS, s);
-        launch_pdl(lm_head_gather_kernel, dim3((N + kGatherRows - 1) / kGatherRows), dim3(kGatherThreads), 0, s, g);
+        gather_launch(g, s);
     }
     HeadParams P;
     memset(&P, 0, sizeof P);
     P.m = N; P.n = V; P.k = d; P.V = V;
-    P.n_tile = kHeadN; P.slices = 1; P.kb_slice = (d + 63) / 64;
+    P.n_tile = kHeadN; P.box_n = V < kHeadN ? V : kHeadN; P.slices = 1; P.kb_slice = (d + 63) / 64;
     P.live = g.live; P.dev_status = dev_status;
     P.stats = (float2*)(ws + w.stats); P.stats_stride = w.n_pad; P.labels = g.label; P.z_label = (float*)(ws + w.z_label);
     CUtensorMap a, b;
-    if (!operand_map(&a, g.rows, 2, w.n_pad, d, w.d_pitch * 2, 64, kHeadM) || !operand_map(&b, weight, 2, V, d, weight_row_stride * 2, 64, kHeadN))
+    if (!operand_map(&a, g.rows, 2, w.n_pad, d, w.d_pitch * 2, 64, kHeadM) || !operand_map(&b, weight, 2, V, d, weight_row_stride * 2, 64, P.box_n))
         return DSPARK_ERR_CUDA;
     const int rc = head_launch<kLossStats>(P, a, b, s, DSPARK_K_HEAD_LOSS);
     if (rc != DSPARK_OK) return rc;
@@ -763,7 +803,7 @@ int dspark_lm_head_loss(const void* hidden, int64_t hidden_row_stride, const voi
     L.z_label = P.z_label; L.idx = g.idx; L.live = g.live; L.loss = out_loss; L.lse = out_lse; L.dev_status = dev_status;
     {
         KernelTimerScope timer(DSPARK_K_HEAD_ROWS, s);
-        launch_pdl(lm_head_loss_kernel, dim3((N + 31) / 32), dim3(kLossWarps * 32), 0, s, L);
+        launch_pdl(lm_head_loss_kernel, dim3((N + kLossRows - 1) / kLossRows), dim3(kLossThreads), 0, s, L);
     }
     return launch_status();
 }
@@ -793,12 +833,13 @@ int dspark_lm_head_loss_backward(const void* hidden, int64_t hidden_row_stride, 
     g.dh = (__nv_bfloat16*)out_grad_hidden; g.dh_stride = grad_hidden_row_stride; g.dev_status = dev_status;
     {
         KernelTimerScope timer(DSPARK_K_HEAD_ROWS, s);
-        launch_pdl(lm_head_gather_kernel, dim3((N + kGatherRows - 1) / kGatherRows), dim3(kGatherThreads), 0, s, g);
+        gather_launch(g, s);
     }
     void* G = ws + w.G;
+    const int box_v = V < kHeadN ? V : kHeadN;
     CUtensorMap rows_k, w_k, g_k, w_mn, g_mn, rows_mn;
     if (!operand_map(&rows_k, g.rows, 2, w.n_pad, d, w.d_pitch * 2, 64, kHeadM) ||
-        !operand_map(&w_k, weight, 2, V, d, weight_row_stride * 2, 64, kHeadN) ||
+        !operand_map(&w_k, weight, 2, V, d, weight_row_stride * 2, 64, box_v) ||
         !operand_map(&g_k, G, 2, w.n_pad, w.piece, (long long)w.piece * 2, 64, kHeadM) ||
         !operand_map(&w_mn, weight, 2, V, d, weight_row_stride * 2, 64, 64) ||
         !operand_map(&g_mn, G, 2, w.n_pad, w.piece, (long long)w.piece * 2, 64, 64) ||
@@ -810,7 +851,7 @@ int dspark_lm_head_loss_backward(const void* hidden, int64_t hidden_row_stride, 
         memset(&P, 0, sizeof P);
         P.V = V; P.piece0 = v0; P.live = g.live; P.dev_status = dev_status; P.slices = 1;
         HeadParams Q = P;
-        Q.m = N; Q.n = here; Q.k = d; Q.n_tile = kHeadN; Q.kb_slice = (d + 63) / 64;
+        Q.m = N; Q.n = here; Q.k = d; Q.n_tile = kHeadN; Q.box_n = box_v; Q.kb_slice = (d + 63) / 64;
         Q.out = G; Q.out_stride = w.piece; Q.labels = g.label; Q.lse2 = g.lse2; Q.grad = g.grad; Q.label_err = (float*)(ws + w.label_err);
         int rc = head_launch<kLossGrad>(Q, rows_k, w_k, s, DSPARK_K_HEAD_LOSS);
         if (rc != DSPARK_OK) return rc;

@@ -11,9 +11,10 @@
 // several rows in flight), to a CTA of d / 16 threads (bf16; d / 8 in fp32)
 // beyond that.
 //
-// Rounding: q is the integer nearest to the exact quotient 127 t / max|t|, t = h w, ties to even.  In fp32 the
-// quotient of two bf16 products is within 3e-5 of the exact one, so an element that lies within 2e-4 of a half (one
-// in 2 500) is decided by a 64-bit division of the exact products; everything else by one multiplication.
+// Rounding: q is the integer nearest to the exact quotient 127 t / max|t|, t = h w, ties to even.  One multiply-add,
+// t * (127 / max|t|) + 1.5 * 2^23, leaves that integer in the low byte of its result; a second one gives the distance to
+// it.  The factor and the product are off by at most 127 * 3 * 2^-24 = 2.3e-5 together, so an element whose distance is
+// beyond 0.5 - 4e-5 (one in 12 000) is decided by a 64-bit division of the exact products.
 #include <cuda_bf16.h>
 #include <math.h>
 
@@ -78,6 +79,18 @@ template <> struct Elem<__nv_bfloat16> {
     static __device__ __forceinline__ float round(float v) { return __bfloat162float(__float2bfloat16_rn(v)); }
 };
 
+// maximum of |b| and a that keeps a NaN
+__device__ __forceinline__ float max_abs_nan(float a, float b)
+{
+    float m;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(fabsf(b)));
+    return m;
+}
+__device__ __forceinline__ double max_abs_nan(double a, double b)
+{
+    b = fabs(b);
+    return (b > a || b != b) ? b : a;
+}
 __device__ __forceinline__ float warp_max_any(float v)
 {
 #pragma unroll
@@ -94,51 +107,58 @@ __device__ __forceinline__ double warp_max_any(double v)
 // A row is spread over `width` threads: vector v of a thread holds the elements of vector v * width + lane (kVec), or
 // its element e is column (v * kPer + e) * width + lane (rows or pitches that break the 16-byte rule).
 // kWarp: one warp per row, several rows per CTA; otherwise one CTA per row.
-template <typename T, int kVpt, bool kVec, bool kWarp>
-__global__ void __launch_bounds__(kWarp ? 256 : kNormMaxThreads) rms_norm_quant_kernel(const __grid_constant__ NormParams P)
+template <typename T, int kVpt, bool kVec, bool kWarp, int kThreads>
+__global__ void __launch_bounds__(kThreads) rms_norm_quant_kernel(const __grid_constant__ NormParams P)
 {
     typedef Elem<T> E;
     typedef typename E::Product Prod;
     constexpr int kPer = E::kPer;
     __shared__ float s_sum[kNormMaxThreads / 32];
     __shared__ Prod s_top[kNormMaxThreads / 32];
-    pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const long long row = kWarp ? (long long)blockIdx.x * (blockDim.x >> 5) + warp : (long long)blockIdx.x;
-    long long live = P.rows;
-    if (P.n_live) { const int n = *P.n_live; live = n < P.rows ? n : P.rows; }
-    if (row >= live) return;                                // a whole warp or CTA: nobody is left at the barrier
     const int width = kWarp ? 32 : (int)blockDim.x;
     const int me = kWarp ? lane : (int)threadIdx.x;
+    const long long row = kWarp ? (long long)blockIdx.x * (blockDim.x >> 5) + warp : (long long)blockIdx.x;
+    pdl_wait();
+    if (P.n_live) {
+        if (row >= (long long)*P.n_live) return;            // a whole warp or CTA: nobody is left at the barrier
+    }
+    if (row >= P.rows) return;
     const T* x = (const T*)P.x + row * P.x_stride;
     const T* res = P.res ? (const T*)P.res + row * P.res_stride : nullptr;
     T* h_out = P.h_out ? (T*)P.h_out + row * P.h_stride : nullptr;
     T* y_out = P.y ? (T*)P.y + row * P.y_stride : nullptr;
     int8_t* q_out = P.q + row * P.q_stride;
 
-    float h[kVpt][kPer];
-    float sum = 0.f;
-    Prod top = 0;
+    // the row and the weight; h is stored at once, t = h w is what stays
+    float h[kVpt][kPer], w[kVpt][kPer];
     if (kVec) {
-        uint4 xv[kVpt], rv[kVpt];
+        uint4 xv[kVpt], rv[kVpt], wv[kVpt];
 #pragma unroll
         for (int v = 0; v < kVpt; ++v) {
             const int at = v * width + me;
-            xv[v] = rv[v] = make_uint4(0, 0, 0, 0);
+            xv[v] = rv[v] = wv[v] = make_uint4(0, 0, 0, 0);
             if (at * kPer < P.d) {
                 xv[v] = __ldcs(reinterpret_cast<const uint4*>(x) + at);
                 if (res) rv[v] = __ldcs(reinterpret_cast<const uint4*>(res) + at);
+                wv[v] = __ldg(reinterpret_cast<const uint4*>(P.w) + at);
             }
         }
 #pragma unroll
         for (int v = 0; v < kVpt; ++v) {
+            const int at = v * width + me;
+            E::unpack(wv[v], w[v]);
             E::unpack(xv[v], h[v]);
+            uint4 hv = xv[v];
             if (res) {
                 float r[kPer];
                 E::unpack(rv[v], r);
 #pragma unroll
-                for (int e = 0; e < kPer; ++e) h[v][e] = E::round(h[v][e] + r[e]);
+                for (int e = 0; e < kPer; ++e) h[v][e] += r[e];
+                hv = E::pack(h[v]);                         // rounds
+                E::unpack(hv, h[v]);
             }
+            if (h_out && at * kPer < P.d) reinterpret_cast<uint4*>(h_out)[at] = hv;
         }
     } else {
 #pragma unroll
@@ -146,41 +166,25 @@ __global__ void __launch_bounds__(kWarp ? 256 : kNormMaxThreads) rms_norm_quant_
 #pragma unroll
             for (int e = 0; e < kPer; ++e) {
                 const int col = (v * kPer + e) * width + me;
-                h[v][e] = 0.f;
+                h[v][e] = w[v][e] = 0.f;
                 if (col < P.d) {
                     h[v][e] = E::load(x, col);
+                    w[v][e] = E::load(P.w, col);
                     if (res) h[v][e] = E::round(h[v][e] + E::load(res, col));
+                    if (h_out) E::store(h_out, col, h[v][e]);
                 }
             }
     }
-    auto weights = [&](int v, float (&w)[kPer]) {
-        if (kVec) {
-            const int at = v * width + me;
-            uint4 wv = make_uint4(0, 0, 0, 0);
-            if (at * kPer < P.d) wv = __ldg(reinterpret_cast<const uint4*>(P.w) + at);
-            E::unpack(wv, w);
-        } else {
+    float sum = 0.f;
+    Prod top = 0;
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) {
-                const int col = (v * kPer + e) * width + me;
-                w[e] = col < P.d ? E::load(P.w, col) : 0.f;
-            }
-        }
-    };
-#pragma unroll
-    for (int v = 0; v < kVpt; ++v) {
-        float w[kPer];
-        weights(v, w);
+    for (int v = 0; v < kVpt; ++v)
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
             sum = fmaf(h[v][e], h[v][e], sum);
-            const Prod t = (Prod)h[v][e] * (Prod)w[e];
-            const Prod a = t < 0 ? -t : t;
-            // a NaN or an infinity of x shows in the sum; one of the weights only here
-            top = (a > top || a != a) ? a : top;
+            top = max_abs_nan(top, (Prod)h[v][e] * (Prod)w[v][e]);
         }
-    }
-    // a NaN maximum loses every comparison in the reduction, so it travels in the sum
+    // an infinite or NaN maximum (of the row or of the weights) travels in the sum
     if (!(top <= (Prod)3.4e38)) sum = NAN;
     sum = warp_sum_f32(sum);
     top = warp_max_any(top);
@@ -194,37 +198,47 @@ __global__ void __launch_bounds__(kWarp ? 256 : kNormMaxThreads) rms_norm_quant_
         top = warp_max_any(top);
     }
     const bool bad = !(sum < INFINITY);                     // NaN or infinity in the row, or beyond fp32's range
-    const float rstd = 1.f / sqrtf(sum / (float)P.d + P.eps);
-    const bool zero = bad || top == 0;
     const float topf = (float)top;
+    const float rstd = rsqrtf(sum / (float)P.d + P.eps);
     if (me == 0) P.scale[row] = bad ? NAN : (top == 0 ? 0.f : topf * rstd * (1.f / 127.f));
-    const float inv = 127.f / topf;
-    const bool slow = !(inv < 1e35f);                       // products next to the smallest fp32 numbers
-    auto quant = [&](float he, float we) -> int {
-        const float r = he * we * inv;
-        float n = rintf(r);
-        if (slow || fabsf(r - n) > 0.4998f) n = (float)rint(((double)he * (double)we * 127.0) / (double)top);
-        return zero ? 0 : (int)n;
-    };
+    const bool zero = bad || top == 0;
+    float inv = zero ? 0.f : 127.f / topf;
+    // products next to the smallest fp32 numbers: every element is decided by the division
+    const float limit = inv < 1e35f ? 0.49996f : -1.f;
+    if (!(inv < 1e35f)) inv = 0.f;
+    constexpr float kMagic = 12582912.f;                    // 1.5 * 2^23: the integer ends up in the low bits
+    auto divided = [&](float he, float we) -> int { return (int)rint(((double)he * (double)we * 127.0) / (double)top); };
 #pragma unroll
     for (int v = 0; v < kVpt; ++v) {
-        float w[kPer];
-        weights(v, w);
+        uint32_t bits[kPer];
+        float far = 0.f;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+            const float t = zero ? 0.f : h[v][e] * w[v][e];
+            const float m = fmaf(t, inv, kMagic);
+            far = fmaxf(far, fabsf(fmaf(t, inv, kMagic - m)));
+            bits[e] = __float_as_uint(m);
+        }
+        if (far > limit && !zero) {
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                const float t = h[v][e] * w[v][e];
+                if (fabsf(fmaf(t, inv, kMagic - __uint_as_float(bits[e]))) > limit) bits[e] = (uint32_t)divided(h[v][e], w[v][e]);
+            }
+        }
         if (kVec) {
             const int at = v * width + me;
             if (at * kPer >= P.d) continue;
             uint32_t packed[kPer / 4];
 #pragma unroll
-            for (int i = 0; i < kPer / 4; ++i) packed[i] = 0;
-#pragma unroll
-            for (int e = 0; e < kPer; ++e) packed[e >> 2] |= (uint32_t)(quant(h[v][e], w[e]) & 255) << (8 * (e & 3));
+            for (int i = 0; i < kPer / 4; ++i)
+                packed[i] = __byte_perm(__byte_perm(bits[4 * i], bits[4 * i + 1], 0x0040), __byte_perm(bits[4 * i + 2], bits[4 * i + 3], 0x0040), 0x5410);
             if (kPer == 8) *reinterpret_cast<uint2*>(q_out + (long long)at * 8) = make_uint2(packed[0], packed[kPer / 4 - 1]);
             else *reinterpret_cast<uint32_t*>(q_out + (long long)at * 4) = packed[0];
-            if (h_out) reinterpret_cast<uint4*>(h_out)[at] = E::pack(h[v]);
             if (y_out) {
                 float y[kPer];
 #pragma unroll
-                for (int e = 0; e < kPer; ++e) y[e] = (h[v][e] * w[e]) * rstd;
+                for (int e = 0; e < kPer; ++e) y[e] = (h[v][e] * w[v][e]) * rstd;
                 reinterpret_cast<uint4*>(y_out)[at] = E::pack(y);
             }
         } else {
@@ -232,9 +246,8 @@ __global__ void __launch_bounds__(kWarp ? 256 : kNormMaxThreads) rms_norm_quant_
             for (int e = 0; e < kPer; ++e) {
                 const int col = (v * kPer + e) * width + me;
                 if (col >= P.d) continue;
-                q_out[col] = (int8_t)quant(h[v][e], w[e]);
-                if (h_out) E::store(h_out, col, h[v][e]);
-                if (y_out) E::store(y_out, col, (h[v][e] * w[e]) * rstd);
+                q_out[col] = (int8_t)(bits[e] & 255u);
+                if (y_out) E::store(y_out, col, (h[v][e] * w[v][e]) * rstd);
             }
         }
     }
@@ -249,22 +262,24 @@ static void norm_launch(const NormParams& P, cudaStream_t s)
         const int per = (vectors + 31) / 32;
         const int warps = P.rows >= 8 * 148 ? 8 : 1;
         const dim3 grid((unsigned)((P.rows + warps - 1) / warps)), block(warps * 32);
-        if (per <= 1) launch_pdl(rms_norm_quant_kernel<T, 1, kVec, true>, grid, block, 0, s, P);
-        else if (per <= 2) launch_pdl(rms_norm_quant_kernel<T, 2, kVec, true>, grid, block, 0, s, P);
-        else if (kPer == 8 || per <= 4) launch_pdl(rms_norm_quant_kernel<T, 4, kVec, true>, grid, block, 0, s, P);
-        else if constexpr (kPer == 4) launch_pdl(rms_norm_quant_kernel<T, 8, kVec, true>, grid, block, 0, s, P);
+        if (per <= 1) launch_pdl(rms_norm_quant_kernel<T, 1, kVec, true, 256>, grid, block, 0, s, P);
+        else if (per <= 2) launch_pdl(rms_norm_quant_kernel<T, 2, kVec, true, 256>, grid, block, 0, s, P);
+        else if (kPer == 8 || per <= 4) launch_pdl(rms_norm_quant_kernel<T, 4, kVec, true, 256>, grid, block, 0, s, P);
+        else if constexpr (kPer == 4) launch_pdl(rms_norm_quant_kernel<T, 8, kVec, true, 256>, grid, block, 0, s, P);
         return;
     }
     // two vectors a thread while that fits a CTA, four beyond (fp32 rows of more than 8 192 elements)
     constexpr bool kFour = kNormMaxD / kPer > 2 * kNormMaxThreads;
     const int per = kFour && vectors > 2 * kNormMaxThreads ? 4 : 2;
     const int threads = (((vectors + per - 1) / per) + 31) & ~31;
+    const dim3 grid(P.rows), block(threads);
     if constexpr (kFour)
         if (per == 4) {
-            launch_pdl(rms_norm_quant_kernel<T, 4, kVec, false>, dim3(P.rows), dim3(threads), 0, s, P);
+            launch_pdl(rms_norm_quant_kernel<T, 4, kVec, false, kNormMaxThreads>, grid, block, 0, s, P);
             return;
         }
-    launch_pdl(rms_norm_quant_kernel<T, 2, kVec, false>, dim3(P.rows), dim3(threads), 0, s, P);
+    if (threads <= 512) launch_pdl(rms_norm_quant_kernel<T, 2, kVec, false, 512>, grid, block, 0, s, P);
+    else launch_pdl(rms_norm_quant_kernel<T, 2, kVec, false, kNormMaxThreads>, grid, block, 0, s, P);
 }
 
 }  // namespace dspark
