@@ -163,7 +163,8 @@ def _logits(t: torch.Tensor, name: str):
 
 
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    # the handle of torch.cuda.current_stream() without the Stream object around it (3 us less per call)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 # ------------------------------------------------------------------------------- profile ----
@@ -609,30 +610,33 @@ def dspark_sts_apply(conf: torch.Tensor, T: torch.Tensor, out: torch.Tensor) -> 
 
 
 # -------------------------------------------------------------------- vocabulary projection ----
+def _here(t: torch.Tensor, name: str, dtype) -> None:
+    dev = t.get_device()                                    # -1: a CPU tensor
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise DsparkError(f"{name} must be a CUDA tensor on the current device (no CPU path exists)")
+    if t.dtype is not dtype:
+        raise DsparkError(f"{name} must be {dtype}, got {t.dtype}")
+
+
 def _rows(t: Optional[torch.Tensor], name: str, dtype, rows: int, cols: int):
     """(address, row stride) of a 2-D matrix with unit inner stride on the current device, at least rows x cols."""
     if t is None:
         return None, 0
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise DsparkError(f"{name} must be a CUDA tensor on the current device (no CPU path exists)")
-    if t.dtype != dtype:
-        raise DsparkError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
-        raise DsparkError(f"{name} must be 2-D with unit inner stride and rows that do not overlap")
-    if t.shape[0] < rows or t.shape[1] != cols:
-        raise DsparkError(f"{name} must be [{rows}, {cols}], got {list(t.shape)}")
+    _here(t, name, dtype)
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or shape[0] < rows or shape[1] != cols:
+        raise DsparkError(f"{name} must be [{rows}, {cols}], got {list(shape)}")
+    if (stride[1] != 1 and cols > 1) or (stride[0] < cols and shape[0] > 1):
+        raise DsparkError(f"{name} must have unit inner stride and rows that do not overlap")
     # the stride of a single row carries no meaning: any aligned number that is wide enough does
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else -(-cols // 16) * 16
+    return t.data_ptr(), stride[0] if shape[0] > 1 else -(-cols // 16) * 16
 
 
 def _vec(t: Optional[torch.Tensor], name: str, dtype, n: int):
     """Address of a contiguous vector of at least n entries on the current device."""
     if t is None:
         return None
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise DsparkError(f"{name} must be a CUDA tensor on the current device (no CPU path exists)")
-    if t.dtype != dtype:
-        raise DsparkError(f"{name} must be {dtype}, got {t.dtype}")
+    _here(t, name, dtype)
     if t.numel() < n or not t.is_contiguous():
         raise DsparkError(f"{name} must be contiguous with {n} entries")
     return t.data_ptr()

@@ -17,6 +17,7 @@
 // beyond 0.5 - 4e-5 (one in 12 000) is decided by a 64-bit division of the exact products.
 #include <cuda_bf16.h>
 #include <math.h>
+#include <type_traits>
 
 #include "common.cuh"
 
@@ -38,6 +39,8 @@ struct NormParams {
 constexpr int kNormVec = 16;                    // bytes of one vector of x
 constexpr int kNormMaxThreads = 1024;
 constexpr int kNormMaxD = 16384;
+constexpr int kNormMaxStages = 8;
+constexpr int kNormStreamRows = 592;             // four rows an SM: below, a row per CTA starts sooner than a ring fills
 
 template <typename T> struct Elem;
 template <> struct Elem<float> {
@@ -91,12 +94,7 @@ __device__ __forceinline__ double max_abs_nan(double a, double b)
     b = fabs(b);
     return (b > a || b != b) ? b : a;
 }
-__device__ __forceinline__ float warp_max_any(float v)
-{
-#pragma unroll
-    for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-    return v;
-}
+__device__ __forceinline__ float warp_max_any(float v) { return warp_max_f32(v); }
 __device__ __forceinline__ double warp_max_any(double v)
 {
 #pragma unroll
@@ -104,9 +102,173 @@ __device__ __forceinline__ double warp_max_any(double v)
     return v;
 }
 
-// A row is spread over `width` threads: vector v of a thread holds the elements of vector v * width + lane (kVec), or
-// its element e is column (v * kPer + e) * width + lane (rows or pitches that break the 16-byte rule).
-// kWarp: one warp per row, several rows per CTA; otherwise one CTA per row.
+// The integer of an element that lies next to a half, n (with its distance's sign) the nearer one in fp32.  bf16: the
+// product has 16 significant bits, so 254 t and (2 n +- 1) max|t| are exact in fp32 and their comparison decides.
+// fp32: the quotient of the exact products in 64 bits.
+__device__ __forceinline__ int next_to_half(float h, float w, float top, float n, float distance)
+{
+    float t = h * w, m = top;
+    if (top > 1e36f) { t *= 0x1p-16f; m *= 0x1p-16f; }
+    const float odd = 2.f * n + (distance < 0.f ? -1.f : 1.f);
+    const float diff = 254.f * t - odd * m;                 // both exact, so the sign of the difference is
+    const int below = (int)floorf(0.5f * odd);              // the two integers next to the half
+    return diff > 0.f ? below + 1 : diff < 0.f ? below : below + (below & 1);
+}
+__device__ __forceinline__ int next_to_half(float h, float w, double top, float, float) { return (int)rint(((double)h * (double)w * 127.0) / top); }
+
+// What a group of threads (a warp or a CTA) keeps of a row: vector v of a thread holds the elements of vector
+// v * width + me (kVec), or its element e is column (v * kPer + e) * width + me (rows or pitches that break the 16-byte
+// rule).
+template <typename T, int kVpt, bool kVec>
+struct NormRow {
+    typedef Elem<T> E;
+    typedef typename E::Product Prod;
+    static constexpr int kPer = E::kPer;
+    // a vector of the weight, packed as it lies in memory (kVec) or element by element
+    struct Packed { uint4 v; __device__ __forceinline__ void get(float (&w)[kPer]) const { E::unpack(v, w); } };
+    struct Single {
+        float v[kPer];
+        __device__ __forceinline__ void get(float (&w)[kPer]) const
+        {
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) w[e] = v[e];
+        }
+    };
+    typedef typename std::conditional<kVec, Packed, Single>::type Weight;
+    float h[kVpt][kPer];
+
+    // h = x + residual from the vectors of both, rounded, and stored
+    __device__ __forceinline__ void add(const uint4 (&xv)[kVpt], const uint4 (&rv)[kVpt], bool with_residual, T* h_out, int d, int width, int me)
+    {
+#pragma unroll
+        for (int v = 0; v < kVpt; ++v) {
+            const int at = v * width + me;
+            E::unpack(xv[v], h[v]);
+            uint4 hv = xv[v];
+            if (with_residual) {
+                float r[kPer];
+                E::unpack(rv[v], r);
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) h[v][e] += r[e];
+                hv = E::pack(h[v]);                         // rounds
+                E::unpack(hv, h[v]);
+            }
+            if (h_out && at * kPer < d) reinterpret_cast<uint4*>(h_out)[at] = hv;
+        }
+    }
+    __device__ __forceinline__ void statistics(const Weight (&weight)[kVpt], float& sum, Prod& top) const
+    {
+        sum = 0.f;
+        top = 0;
+#pragma unroll
+        for (int v = 0; v < kVpt; ++v) {
+            float w[kPer];
+            weight[v].get(w);
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                sum = fmaf(h[v][e], h[v][e], sum);
+                top = max_abs_nan(top, (Prod)h[v][e] * (Prod)w[e]);
+            }
+        }
+        // an infinite or NaN maximum (of the row or of the weights) travels in the sum
+        if (!(top <= (Prod)3.4e38)) sum = NAN;
+    }
+    __device__ __forceinline__ void finish(const NormParams& P, long long row, const Weight (&weight)[kVpt], float sum, Prod top, int width, int me)
+    {
+        const bool bad = !(sum < INFINITY);                 // NaN or infinity in the row, or beyond fp32's range
+        float topf = (float)top, rstd = rsqrtf(sum / (float)P.d + P.eps);
+        if (me == 0) P.scale[row] = bad ? NAN : (top == 0 ? 0.f : topf * rstd * (1.f / 127.f));
+        const bool zero = bad || top == 0;
+        if (topf < 1e-33f) {                                // next to the smallest fp32 numbers: brought up by 2^64
+#pragma unroll
+            for (int v = 0; v < kVpt; ++v)
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) h[v][e] *= 0x1p64f;
+            topf *= 0x1p64f;
+            top *= (Prod)0x1p64;
+            rstd *= 0x1p-64f;
+        }
+        const float inv = zero ? 0.f : 127.f / topf;
+        constexpr float limit = 0.49996f;
+        constexpr float kMagic = 12582912.f;                // 1.5 * 2^23: the integer ends up in the low bits
+        int8_t* q_out = P.q + row * P.q_stride;
+        T* y_out = P.y ? (T*)P.y + row * P.y_stride : nullptr;
+#pragma unroll
+        for (int v = 0; v < kVpt; ++v) {
+            float w[kPer];
+            weight[v].get(w);
+            uint32_t bits[kPer];
+            float far = 0.f;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                const float t = zero ? 0.f : h[v][e] * w[e];
+                const float m = fmaf(t, inv, kMagic);
+                far = fmaxf(far, fabsf(fmaf(t, inv, kMagic - m)));
+                bits[e] = __float_as_uint(m);
+            }
+            if (far > limit && !zero) {
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) {
+                    const float n = __uint_as_float(bits[e]) - kMagic, distance = fmaf(h[v][e] * w[e], inv, -n);
+                    if (fabsf(distance) > limit) bits[e] = (uint32_t)next_to_half(h[v][e], w[e], top, n, distance);
+                }
+            }
+            if (kVec) {
+                const int at = v * width + me;
+                if (at * kPer >= P.d) continue;
+                uint32_t packed[kPer / 4];
+#pragma unroll
+                for (int i = 0; i < kPer / 4; ++i)
+                    packed[i] = __byte_perm(__byte_perm(bits[4 * i], bits[4 * i + 1], 0x0040), __byte_perm(bits[4 * i + 2], bits[4 * i + 3], 0x0040), 0x5410);
+                if (kPer == 8) *reinterpret_cast<uint2*>(q_out + (long long)at * 8) = make_uint2(packed[0], packed[kPer / 4 - 1]);
+                else *reinterpret_cast<uint32_t*>(q_out + (long long)at * 4) = packed[0];
+                if (y_out) {
+                    float y[kPer];
+#pragma unroll
+                    for (int e = 0; e < kPer; ++e) y[e] = (h[v][e] * w[e]) * rstd;
+                    reinterpret_cast<uint4*>(y_out)[at] = E::pack(y);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) {
+                    const int col = (v * kPer + e) * width + me;
+                    if (col >= P.d) continue;
+                    q_out[col] = (int8_t)(bits[e] & 255u);
+                    if (y_out) E::store(y_out, col, (h[v][e] * w[e]) * rstd);
+                }
+            }
+        }
+    }
+};
+
+// Sum and maximum over a group; the CTA's group passes through shared memory (two sets in turn, so that one barrier a row
+// is enough).
+template <bool kWarp, typename Prod>
+__device__ __forceinline__ void group_reduce(float& sum, Prod& top, float* s_sum, Prod* s_top)
+{
+    sum = warp_sum_f32(sum);
+    top = warp_max_any(top);
+    if (!kWarp) {
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = (int)blockDim.x >> 5;
+        if (lane == 0) { s_sum[warp] = sum; s_top[warp] = top; }
+        __syncthreads();
+        if (n_warps <= 8) {                                 // broadcast reads: a shorter chain than shuffles
+            sum = 0.f;
+            top = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < n_warps) { sum += s_sum[i]; top = s_top[i] > top ? s_top[i] : top; }
+        } else {
+            sum = lane < n_warps ? s_sum[lane] : 0.f;
+            top = lane < n_warps ? s_top[lane] : (Prod)0;
+            sum = warp_sum_f32(sum);
+            top = warp_max_any(top);
+        }
+    }
+}
+
+// One row per group, loaded straight into registers: few rows, or rows that break the 16-byte rule.
+// kWarp: a warp per row, several rows per CTA; otherwise a CTA per row.
 template <typename T, int kVpt, bool kVec, bool kWarp, int kThreads>
 __global__ void __launch_bounds__(kThreads) rms_norm_quant_kernel(const __grid_constant__ NormParams P)
 {
@@ -115,10 +277,9 @@ __global__ void __launch_bounds__(kThreads) rms_norm_quant_kernel(const __grid_c
     constexpr int kPer = E::kPer;
     __shared__ float s_sum[kNormMaxThreads / 32];
     __shared__ Prod s_top[kNormMaxThreads / 32];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int width = kWarp ? 32 : (int)blockDim.x;
-    const int me = kWarp ? lane : (int)threadIdx.x;
-    const long long row = kWarp ? (long long)blockIdx.x * (blockDim.x >> 5) + warp : (long long)blockIdx.x;
+    const int me = kWarp ? (int)threadIdx.x & 31 : (int)threadIdx.x;
+    const long long row = kWarp ? (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : (long long)blockIdx.x;
     pdl_wait();
     if (P.n_live) {
         if (row >= (long long)*P.n_live) return;            // a whole warp or CTA: nobody is left at the barrier
@@ -127,130 +288,150 @@ __global__ void __launch_bounds__(kThreads) rms_norm_quant_kernel(const __grid_c
     const T* x = (const T*)P.x + row * P.x_stride;
     const T* res = P.res ? (const T*)P.res + row * P.res_stride : nullptr;
     T* h_out = P.h_out ? (T*)P.h_out + row * P.h_stride : nullptr;
-    T* y_out = P.y ? (T*)P.y + row * P.y_stride : nullptr;
-    int8_t* q_out = P.q + row * P.q_stride;
-
-    // the row and the weight; h is stored at once, t = h w is what stays
-    float h[kVpt][kPer], w[kVpt][kPer];
-    if (kVec) {
-        uint4 xv[kVpt], rv[kVpt], wv[kVpt];
+    NormRow<T, kVpt, kVec> r;
+    typename NormRow<T, kVpt, kVec>::Weight w[kVpt];
+    if constexpr (kVec) {
+        uint4 xv[kVpt], rv[kVpt];
 #pragma unroll
         for (int v = 0; v < kVpt; ++v) {
             const int at = v * width + me;
-            xv[v] = rv[v] = wv[v] = make_uint4(0, 0, 0, 0);
+            xv[v] = rv[v] = w[v].v = make_uint4(0, 0, 0, 0);
             if (at * kPer < P.d) {
-                xv[v] = __ldcs(reinterpret_cast<const uint4*>(x) + at);
-                if (res) rv[v] = __ldcs(reinterpret_cast<const uint4*>(res) + at);
-                wv[v] = __ldg(reinterpret_cast<const uint4*>(P.w) + at);
+                xv[v] = reinterpret_cast<const uint4*>(x)[at];
+                if (res) rv[v] = reinterpret_cast<const uint4*>(res)[at];
+                w[v].v = __ldg(reinterpret_cast<const uint4*>(P.w) + at);
             }
         }
-#pragma unroll
-        for (int v = 0; v < kVpt; ++v) {
-            const int at = v * width + me;
-            E::unpack(wv[v], w[v]);
-            E::unpack(xv[v], h[v]);
-            uint4 hv = xv[v];
-            if (res) {
-                float r[kPer];
-                E::unpack(rv[v], r);
-#pragma unroll
-                for (int e = 0; e < kPer; ++e) h[v][e] += r[e];
-                hv = E::pack(h[v]);                         // rounds
-                E::unpack(hv, h[v]);
-            }
-            if (h_out && at * kPer < P.d) reinterpret_cast<uint4*>(h_out)[at] = hv;
-        }
+        r.add(xv, rv, res != nullptr, h_out, P.d, width, me);
     } else {
 #pragma unroll
         for (int v = 0; v < kVpt; ++v)
 #pragma unroll
             for (int e = 0; e < kPer; ++e) {
                 const int col = (v * kPer + e) * width + me;
-                h[v][e] = w[v][e] = 0.f;
+                r.h[v][e] = w[v].v[e] = 0.f;
                 if (col < P.d) {
-                    h[v][e] = E::load(x, col);
-                    w[v][e] = E::load(P.w, col);
-                    if (res) h[v][e] = E::round(h[v][e] + E::load(res, col));
-                    if (h_out) E::store(h_out, col, h[v][e]);
+                    r.h[v][e] = E::load(x, col);
+                    w[v].v[e] = E::load(P.w, col);
+                    if (res) r.h[v][e] = E::round(r.h[v][e] + E::load(res, col));
+                    if (h_out) E::store(h_out, col, r.h[v][e]);
                 }
             }
     }
-    float sum = 0.f;
-    Prod top = 0;
-#pragma unroll
-    for (int v = 0; v < kVpt; ++v)
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) {
-            sum = fmaf(h[v][e], h[v][e], sum);
-            top = max_abs_nan(top, (Prod)h[v][e] * (Prod)w[v][e]);
-        }
-    // an infinite or NaN maximum (of the row or of the weights) travels in the sum
-    if (!(top <= (Prod)3.4e38)) sum = NAN;
-    sum = warp_sum_f32(sum);
-    top = warp_max_any(top);
-    if (!kWarp) {
-        if (lane == 0) { s_sum[warp] = sum; s_top[warp] = top; }
-        __syncthreads();
-        const int n_warps = (int)blockDim.x >> 5;
-        sum = lane < n_warps ? s_sum[lane] : 0.f;
-        top = lane < n_warps ? s_top[lane] : (Prod)0;
-        sum = warp_sum_f32(sum);
-        top = warp_max_any(top);
+    float sum;
+    Prod top;
+    r.statistics(w, sum, top);
+    group_reduce<kWarp>(sum, top, s_sum, s_top);
+    r.finish(P, row, w, sum, top, width, me);
+}
+
+// Many rows: persistent groups walk the rows, each with a ring of `stages` rows of x and the residual in shared memory that
+// bulk copies keep filled, so that the loads of the next rows are in flight while one is reduced and written.  The barrier
+// of the reduction (a warp: __syncwarp) is what frees a stage.  The weight stays in registers.
+// kCtas: CTAs an SM that the registers have to allow.  Occupancy is what hides the chain of a row (shared memory,
+// reduction, barrier, store).
+template <typename T, int kVpt, bool kWarp, int kThreads, int kCtas>
+__global__ void __launch_bounds__(kThreads, kCtas) rms_norm_quant_stream_kernel(const __grid_constant__ NormParams P, int stages)
+{
+    typedef Elem<T> E;
+    typedef typename E::Product Prod;
+    constexpr int kPer = E::kPer;
+    constexpr int kGroups = kWarp ? kThreads / 32 : 1;
+    extern __shared__ __align__(128) unsigned char s_ring[];
+    __shared__ __align__(8) uint64_t full[kGroups][kNormMaxStages];
+    __shared__ float s_sum[2][kNormMaxThreads / 32];
+    __shared__ Prod s_top[2][kNormMaxThreads / 32];
+    const int group = kWarp ? (int)threadIdx.x >> 5 : 0;
+    const int width = kWarp ? 32 : (int)blockDim.x;
+    const int me = kWarp ? (int)threadIdx.x & 31 : (int)threadIdx.x;
+    const uint32_t row_bytes = (uint32_t)(P.d * sizeof(T));
+    const uint32_t stage_bytes = row_bytes * (P.res ? 2 : 1);
+    unsigned char* ring = s_ring + (size_t)group * stages * stage_bytes;
+    if (threadIdx.x == 0) {
+        for (int g = 0; g < kGroups; ++g)
+            for (int s = 0; s < stages; ++s) mbar_init(&full[g][s], 1);
+        mbar_fence_init();
     }
-    const bool bad = !(sum < INFINITY);                     // NaN or infinity in the row, or beyond fp32's range
-    const float topf = (float)top;
-    const float rstd = rsqrtf(sum / (float)P.d + P.eps);
-    if (me == 0) P.scale[row] = bad ? NAN : (top == 0 ? 0.f : topf * rstd * (1.f / 127.f));
-    const bool zero = bad || top == 0;
-    float inv = zero ? 0.f : 127.f / topf;
-    // products next to the smallest fp32 numbers: every element is decided by the division
-    const float limit = inv < 1e35f ? 0.49996f : -1.f;
-    if (!(inv < 1e35f)) inv = 0.f;
-    constexpr float kMagic = 12582912.f;                    // 1.5 * 2^23: the integer ends up in the low bits
-    auto divided = [&](float he, float we) -> int { return (int)rint(((double)he * (double)we * 127.0) / (double)top); };
+    __syncthreads();
+    pdl_wait();
+    long long live = P.rows;
+    if (P.n_live) { const int n = *P.n_live; live = n < P.rows ? n : P.rows; }
+    const long long first = (long long)blockIdx.x * kGroups + group, step = (long long)gridDim.x * kGroups;
+    const uint64_t pol = l2_policy_evict_first();
+    auto request = [&](long long row, int s) {
+        mbar_arrive_expect_tx(&full[group][s], stage_bytes);
+        bulk_g2s_hint(ring + s * stage_bytes, (const T*)P.x + row * P.x_stride, row_bytes, &full[group][s], pol);
+        if (P.res) bulk_g2s_hint(ring + s * stage_bytes + row_bytes, (const T*)P.res + row * P.res_stride, row_bytes, &full[group][s], pol);
+    };
+    if (me == 0)
+        for (int s = 0; s < stages; ++s)
+            if (first + s * step < live) request(first + s * step, s);
+    typename NormRow<T, kVpt, true>::Weight w[kVpt];
 #pragma unroll
     for (int v = 0; v < kVpt; ++v) {
-        uint32_t bits[kPer];
-        float far = 0.f;
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) {
-            const float t = zero ? 0.f : h[v][e] * w[v][e];
-            const float m = fmaf(t, inv, kMagic);
-            far = fmaxf(far, fabsf(fmaf(t, inv, kMagic - m)));
-            bits[e] = __float_as_uint(m);
-        }
-        if (far > limit && !zero) {
-#pragma unroll
-            for (int e = 0; e < kPer; ++e) {
-                const float t = h[v][e] * w[v][e];
-                if (fabsf(fmaf(t, inv, kMagic - __uint_as_float(bits[e]))) > limit) bits[e] = (uint32_t)divided(h[v][e], w[v][e]);
-            }
-        }
-        if (kVec) {
-            const int at = v * width + me;
-            if (at * kPer >= P.d) continue;
-            uint32_t packed[kPer / 4];
-#pragma unroll
-            for (int i = 0; i < kPer / 4; ++i)
-                packed[i] = __byte_perm(__byte_perm(bits[4 * i], bits[4 * i + 1], 0x0040), __byte_perm(bits[4 * i + 2], bits[4 * i + 3], 0x0040), 0x5410);
-            if (kPer == 8) *reinterpret_cast<uint2*>(q_out + (long long)at * 8) = make_uint2(packed[0], packed[kPer / 4 - 1]);
-            else *reinterpret_cast<uint32_t*>(q_out + (long long)at * 4) = packed[0];
-            if (y_out) {
-                float y[kPer];
-#pragma unroll
-                for (int e = 0; e < kPer; ++e) y[e] = (h[v][e] * w[v][e]) * rstd;
-                reinterpret_cast<uint4*>(y_out)[at] = E::pack(y);
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < kPer; ++e) {
-                const int col = (v * kPer + e) * width + me;
-                if (col >= P.d) continue;
-                q_out[col] = (int8_t)(bits[e] & 255u);
-                if (y_out) E::store(y_out, col, (h[v][e] * w[v][e]) * rstd);
-            }
-        }
+        const int at = v * width + me;
+        w[v].v = make_uint4(0, 0, 0, 0);
+        if (at * kPer < P.d) w[v].v = __ldg(reinterpret_cast<const uint4*>(P.w) + at);
     }
+    int s = 0, turn = 0;
+    uint32_t ph = 0;
+    for (long long row = first; row < live; row += step) {
+        // The copy is this group's own and lands; a wait that ran out all the same gives the row up as one that cannot be
+        // normalised, and its stage is not filled again.
+        const bool ok = mbar_wait_bounded(&full[group][s], ph);
+        const unsigned char* stage = ring + s * stage_bytes;
+        uint4 xv[kVpt], rv[kVpt];
+#pragma unroll
+        for (int v = 0; v < kVpt; ++v) {
+            const int at = v * width + me;
+            xv[v] = rv[v] = make_uint4(0, 0, 0, 0);
+            if (at * kPer < P.d) {
+                xv[v] = reinterpret_cast<const uint4*>(stage)[at];
+                if (P.res) rv[v] = reinterpret_cast<const uint4*>(stage + row_bytes)[at];
+            }
+        }
+        NormRow<T, kVpt, true> r;
+        r.add(xv, rv, P.res != nullptr, P.h_out ? (T*)P.h_out + row * P.h_stride : nullptr, P.d, width, me);
+        float sum;
+        Prod top;
+        r.statistics(w, sum, top);
+        if (!ok) sum = NAN;
+        group_reduce<kWarp>(sum, top, s_sum[turn & 1], s_top[turn & 1]);
+        if (kWarp) __syncwarp();
+        if (me == 0 && ok && row + stages * step < live) request(row + stages * step, s);
+        r.finish(P, row, w, sum, top, width, me);
+        if (++s == stages) { s = 0; ph ^= 1u; }
+        ++turn;
+    }
+}
+
+template <typename T, int kVpt, bool kWarp, int kThreads, int kCtas>
+static bool norm_stream(const NormParams& P, int threads, cudaStream_t s)
+{
+    constexpr int kSmemPerSm = 200 * 1024, kMost = 200 * 1024;
+    const int groups = kWarp ? kThreads / 32 : 1;
+    const int stage = P.d * (int)sizeof(T) * (P.res ? 2 : 1) * groups;
+    // as many CTAs as the registers allow, the ring cut to what they leave of the shared memory
+    int ctas = kCtas * kThreads / threads;
+    int stages = kSmemPerSm / ctas / stage;
+    if (stages < 2) { ctas = 1; stages = kSmemPerSm / stage; }
+    if (stages < 2) return false;
+    if (stages > kNormMaxStages) stages = kNormMaxStages;
+    static std::atomic<unsigned long long> ready{0};        // one bit per device
+    int dev = 0, sms = 0;
+    cudaGetDevice(&dev);
+    cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    const unsigned long long bit = 1ull << (dev & 63);
+    if (!(ready.load(std::memory_order_relaxed) & bit)) {
+        if (cudaFuncSetAttribute(rms_norm_quant_stream_kernel<T, kVpt, kWarp, kThreads, kCtas>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost) !=
+            cudaSuccess)
+            return false;
+        ready.fetch_or(bit, std::memory_order_relaxed);
+    }
+    const long long want = ((long long)P.rows + groups - 1) / groups, cap = (long long)sms * ctas;
+    launch_pdl(rms_norm_quant_stream_kernel<T, kVpt, kWarp, kThreads, kCtas>, dim3((unsigned)(want < cap ? want : cap)), dim3(threads),
+               (size_t)stages * stage, s, P, stages);
+    return true;
 }
 
 template <typename T, bool kVec>
@@ -258,8 +439,19 @@ static void norm_launch(const NormParams& P, cudaStream_t s)
 {
     constexpr int kPer = Elem<T>::kPer;
     const int vectors = (P.d + kPer - 1) / kPer;
-    if (P.d <= 1024) {                                      // a warp per row, 8 rows per CTA (fewer when there are few rows)
+    // a warp per row; rows of more than 256 elements only where there are enough of them to fill the SMs with warps
+    if (P.d <= 256 || (P.d <= 1024 && P.rows >= 8 * 148)) {
         const int per = (vectors + 31) / 32;
+        if constexpr (kVec) {
+            if (P.rows >= kNormStreamRows * 8) {
+                bool done;
+                if (per <= 1) done = norm_stream<T, 1, true, 256, 5>(P, 256, s);
+                else if (per <= 2) done = norm_stream<T, 2, true, 256, 4>(P, 256, s);
+                else if (kPer == 8 || per <= 4) done = norm_stream<T, 4, true, 256, 2>(P, 256, s);
+                else done = norm_stream<T, kPer == 4 ? 8 : 4, true, 256, 1>(P, 256, s);
+                if (done) return;
+            }
+        }
         const int warps = P.rows >= 8 * 148 ? 8 : 1;
         const dim3 grid((unsigned)((P.rows + warps - 1) / warps)), block(warps * 32);
         if (per <= 1) launch_pdl(rms_norm_quant_kernel<T, 1, kVec, true, 256>, grid, block, 0, s, P);
@@ -277,6 +469,12 @@ static void norm_launch(const NormParams& P, cudaStream_t s)
         if (per == 4) {
             launch_pdl(rms_norm_quant_kernel<T, 4, kVec, false, kNormMaxThreads>, grid, block, 0, s, P);
             return;
+        }
+    if constexpr (kVec)
+        if (P.rows >= kNormStreamRows) {
+            const bool done = threads <= 256 ? norm_stream<T, 2, false, 256, 4>(P, threads, s)
+                            : threads <= 512 ? norm_stream<T, 2, false, 512, 2>(P, threads, s) : norm_stream<T, 2, false, kNormMaxThreads, 1>(P, threads, s);
+            if (done) return;
         }
     if (threads <= 512) launch_pdl(rms_norm_quant_kernel<T, 2, kVec, false, 512>, grid, block, 0, s, P);
     else launch_pdl(rms_norm_quant_kernel<T, 2, kVec, false, kNormMaxThreads>, grid, block, 0, s, P);
