@@ -68,17 +68,96 @@ __device__ __forceinline__ uint64_t head_desc(uint32_t addr, bool mn_major)
     return (uint64_t)((addr & 0x3FFFFu) >> 4) | (lead << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
 
-template <bool kInt8>
+template <bool kInt8, int kCtas>
 __device__ __forceinline__ void head_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
 {
-    if (kInt8)
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                     "tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}"
-                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+#define DSPARK_HEAD_MMA(GROUP, KIND)                                                       \
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"                       \
+                 "tcgen05.mma.cta_group::" GROUP ".kind::" KIND " [%0], %1, %2, %3, p;\n\t}" \
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory")
+    if (kInt8 && kCtas == 1) DSPARK_HEAD_MMA("1", "i8");
+    if (kInt8 && kCtas == 2) DSPARK_HEAD_MMA("2", "i8");
+    if (!kInt8 && kCtas == 1) DSPARK_HEAD_MMA("1", "f16");
+    if (!kInt8 && kCtas == 2) DSPARK_HEAD_MMA("2", "f16");
+#undef DSPARK_HEAD_MMA
+}
+
+// ---- pairs of CTAs -------------------------------------------------------------------------------------
+// kCtas = 2: the two CTAs of a cluster share a tile of 256 rows.  Each holds 128 rows of A and half of B's columns in its
+// shared memory and 128 rows of D in its tensor memory; the first one (the leader) issues the products for both.  B passes
+// from the L2 once per pair instead of once per CTA: at 128 x 256 tiles the copies (48 KB a k block) kept the tensor cores
+// waiting for a third of the time.  Barriers: `full` is the leader's (both CTAs' copies count on it), `empty` and
+// `acc_full` each CTA's own (the products' completion is announced to both), `acc_empty` and `unit_empty` the leader's.
+template <int kCtas>
+__device__ __forceinline__ uint32_t pair_rank()
+{
+    uint32_t r = 0;
+    if (kCtas == 2) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+// address of the same variable in CTA `rank` of the cluster
+__device__ __forceinline__ uint32_t pair_address(const void* p, uint32_t rank)
+{
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
+    return a;
+}
+template <int kCtas>
+__device__ __forceinline__ void pair_arrive(uint64_t* bar, uint32_t rank)
+{
+    if (kCtas == 1) mbar_arrive(bar);
+    else asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(pair_address(bar, rank)) : "memory");
+}
+// bounded wait on a barrier of this CTA that the other CTA may arrive on
+template <int kCtas>
+__device__ __forceinline__ bool pair_wait(uint64_t* bar, uint32_t parity)
+{
+    if constexpr (kCtas == 1) return mbar_wait_bounded(bar, parity);
+    else for (uint32_t i = 0; i < kWaitPollLimit; ++i) {
+        uint32_t ok;
+        asm volatile("{\n\t.reg .pred p;\n\t"
+                     "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+                     "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+        if (ok) return true;
+    }
+    return false;
+}
+template <int kCtas>
+__device__ __forceinline__ void pair_sync()
+{
+    if (kCtas == 2) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    else __syncthreads();
+}
+// completion of the products issued so far, announced on `bar` of both CTAs
+template <int kCtas>
+__device__ __forceinline__ void pair_commit(uint64_t* bar)
+{
+    if (kCtas == 1) umma_commit(bar);
     else
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                     "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                     ::"r"(smem_u32(bar)), "h"((uint16_t)3) : "memory");
+}
+// tensor-map loads into this CTA's shared memory, counted on the leader's barrier (bit 24 of a shared address is the rank)
+template <int kCtas>
+__device__ __forceinline__ void pair_load_2d(void* dst, const CUtensorMap* map, int x, int y, uint64_t* bar, uint64_t policy)
+{
+    if (kCtas == 1) tma_load_2d(dst, map, x, y, bar, policy);
+    else
+        asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint "
+                     "[%0], [%1, {%2, %3}], [%4], %5;"
+                     ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(smem_u32(bar) & 0xFEFFFFFFu), "l"(policy)
+                     : "memory");
+}
+template <int kCtas>
+__device__ __forceinline__ void pair_load_3d(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar, uint64_t policy)
+{
+    if (kCtas == 1) tma_load_3d(dst, map, x, y, z, bar, policy);
+    else
+        asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint "
+                     "[%0], [%1, {%2, %3, %4}], [%5], %6;"
+                     ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar) & 0xFEFFFFFFu),
+                     "l"(policy)
+                     : "memory");
 }
 
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b)
@@ -136,68 +215,85 @@ struct HeadShared {
     int abort;
 };
 
+template <int kCtas>
 __device__ __forceinline__ uint32_t head_setup(HeadShared& S, int stages, int warp)
 {
     if (threadIdx.x == 0) {
         for (int s = 0; s < stages; ++s) { mbar_init(&S.full[s], 1); mbar_init(&S.empty[s], 1); }
-        for (int s = 0; s < 2; ++s) { mbar_init(&S.acc_full[s], 1); mbar_init(&S.acc_empty[s], kHeadEpiWarps); }
-        for (int s = 0; s < kUnitSlots; ++s) { mbar_init(&S.unit_full[s], 1); mbar_init(&S.unit_empty[s], 1 + kHeadEpiWarps); }
+        for (int s = 0; s < 2; ++s) { mbar_init(&S.acc_full[s], 1); mbar_init(&S.acc_empty[s], kCtas * kHeadEpiWarps); }
+        // read by: the issuer, the epilogue warps, the other CTA's producer
+        for (int s = 0; s < kUnitSlots; ++s) { mbar_init(&S.unit_full[s], 1); mbar_init(&S.unit_empty[s], kCtas * (1 + kHeadEpiWarps)); }
         mbar_init(&S.mma_done, 1);
         S.abort = 0;
         mbar_fence_init();
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
-                     ::"r"(smem_u32(&S.tmem_base)), "r"(2 * kHeadN) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        if (kCtas == 1) {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&S.tmem_base)), "r"(2 * kHeadN) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&S.tmem_base)), "r"(2 * kHeadN) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        }
     }
     tc_fence_before();
     __syncthreads();
+    pair_sync<kCtas>();
     tc_fence_after();
     pdl_wait();
     return S.tmem_base;
 }
+// Both CTAs of a pair meet before either leaves: each may still be written to by the other until then.
+template <int kCtas>
 __device__ __forceinline__ void head_takedown(uint32_t tmem, int warp)
 {
     tc_fence_before();
     __syncthreads();
+    pair_sync<kCtas>();
     if (warp == 1) {
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kHeadN) : "memory");
+        if (kCtas == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kHeadN) : "memory");
+        else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kHeadN) : "memory");
     }
 }
-// somebody gave up: the producer leaves only after the copies it has issued have landed (bounded)
-__device__ __forceinline__ void head_drain(HeadShared& S, int stages, int issued)
+// Somebody gave up: the leader's producer leaves only after the copies of the stages it has announced have landed (bounded);
+// those of the other CTA count on the same barriers, so it just gives its last ones the time.
+__device__ __forceinline__ void head_drain(HeadShared& S, int stages, int issued, bool leader)
 {
-    for (int i = issued > stages ? issued - stages : 0; i < issued; ++i) mbar_wait_bounded(&S.full[i % stages], (uint32_t)(i / stages) & 1u);
+    if (leader)
+        for (int i = issued > stages ? issued - stages : 0; i < issued; ++i) mbar_wait_bounded(&S.full[i % stages], (uint32_t)(i / stages) & 1u);
+    else
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
 }
 // tensor memory is returned only after the last product
-__device__ __forceinline__ void head_finish_products(HeadShared& S, bool issued)
+__device__ __forceinline__ void head_finish_products(HeadShared& S, bool issued, int ctas)
 {
     if (issued) {
-        umma_commit(&S.mma_done);
+        if (ctas == 1) umma_commit(&S.mma_done);
+        else asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(&S.mma_done)) : "memory");
         mbar_wait_bounded(&S.mma_done, 0u);
     }
 }
+template <int kCtas>
 __device__ __forceinline__ uint32_t head_idesc(bool int8, bool a_mn, bool b_mn, int n)
 {
     return ((int8 ? 2u : 1u) << 4) | (1u << 7) | (1u << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
-           ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kHeadM >> 4) << 24);
+           ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kCtas * kHeadM >> 4) << 24);
 }
 
 // ---- logits and softmax statistics ----------------------------------------------------------------------
-template <int kMode>
+template <int kMode, int kCtas>
 __global__ void __launch_bounds__(kHeadThreads, 1)
 lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b)
 {
     constexpr bool kInt8 = kMode == kInt8Logits;
-    constexpr int kBlockK = kInt8 ? 128 : 64;
+    constexpr int kBlockK = kInt8 ? 128 : 64, kM = kCtas * kHeadM;
 
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);   // swizzle atoms: 1 KB
     __shared__ HeadShared S;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t tmem = head_setup(S, P.stages, warp);
+    const uint32_t tmem = head_setup<kCtas>(S, P.stages, warp), rank = pair_rank<kCtas>();
     volatile int* abort_flag = &S.abort;
     auto give_up = [&]() { atomicOr(P.dev_status, DSPARK_DEV_TIMEOUT); *abort_flag = 1; };
 
@@ -209,17 +305,17 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
         int& rows = kInt8 ? n : m;
         rows = live < rows ? live : rows;
     }
-    const int m_tiles = (m + kHeadM - 1) / kHeadM, n_tiles = (n + P.n_tile - 1) / P.n_tile;
+    const int m_tiles = (m + kM - 1) / kM, n_tiles = (n + P.n_tile - 1) / P.n_tile;
     const int k_blocks = (P.k + kBlockK - 1) / kBlockK;
     const int n_units = m_tiles * n_tiles;
     // unit -> tile; the index over rows runs fastest
     auto tile = [&](int u, int& m0, int& nt) {
-        if (kInt8) { nt = u % n_tiles; m0 = u / n_tiles * kHeadM; }
-        else { m0 = u % m_tiles * kHeadM; nt = u / m_tiles; }
+        if (kInt8) { nt = u % n_tiles; m0 = u / n_tiles * kM; }
+        else { m0 = u % m_tiles * kM; nt = u / m_tiles; }
     };
-    const int stage_bytes = kTileABytes + P.n_tile * kRowBytes;
-    const uint32_t load_bytes = (uint32_t)(kTileABytes + P.box_n * kRowBytes);
-    const int first = (int)blockIdx.x, step = (int)gridDim.x;
+    const int stage_bytes = kTileABytes + P.n_tile / kCtas * kRowBytes;
+    const uint32_t load_bytes = (uint32_t)(kCtas * (kTileABytes + P.box_n * kRowBytes));
+    const int first = (int)blockIdx.x / kCtas, step = (int)gridDim.x / kCtas;
 
     if (warp == 0) {
         // ---------------- producer: operand tiles ---------------------------------------------------------
@@ -233,25 +329,25 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
                 for (int kb = 0; kb < k_blocks; ++kb) {
                     if (!mbar_wait_bounded(&S.empty[s], ph ^ 1u)) { give_up(); break; }
                     unsigned char* a = smem + (size_t)s * stage_bytes;
-                    mbar_arrive_expect_tx(&S.full[s], load_bytes);
-                    tma_load_2d(a, &map_a, kb * kBlockK, m0, &S.full[s], pol);
-                    tma_load_2d(a + kTileABytes, &map_b, kb * kBlockK, nt * P.n_tile, &S.full[s], pol);
+                    if (rank == 0) mbar_arrive_expect_tx(&S.full[s], load_bytes);
+                    pair_load_2d<kCtas>(a, &map_a, kb * kBlockK, m0 + (int)rank * kHeadM, &S.full[s], pol);
+                    pair_load_2d<kCtas>(a + kTileABytes, &map_b, kb * kBlockK, nt * P.n_tile + (int)rank * (P.n_tile / kCtas), &S.full[s], pol);
                     ++issued;
                     if (++s == P.stages) { s = 0; ph ^= 1u; }
                 }
             }
-            if (*abort_flag) head_drain(S, P.stages, issued);
+            if (*abort_flag) head_drain(S, P.stages, issued, rank == 0);
         }
     } else if (warp == 1) {
-        // ---------------- MMA issuer ---------------------------------------------------------------------
-        if (lane == 0) {
-            const uint32_t idesc = head_idesc(kInt8, false, false, P.n_tile);
+        // ---------------- MMA issuer (of a pair: the leader's) -------------------------------------------
+        if (lane == 0 && rank == 0) {
+            const uint32_t idesc = head_idesc<kCtas>(kInt8, false, false, P.n_tile);
             int s = 0, t = 0;
             uint32_t ph = 0;
             bool issued = false;
             for (int u = first; u < n_units && !*abort_flag; u += step, ++t) {
                 const uint32_t acc = (uint32_t)(t & 1), aph = (uint32_t)(t >> 1) & 1u;
-                bool ok = mbar_wait_bounded(&S.acc_empty[acc], aph ^ 1u);
+                bool ok = pair_wait<kCtas>(&S.acc_empty[acc], aph ^ 1u);
                 tc_fence_after();
                 for (int kb = 0; ok && kb < k_blocks; ++kb) {
                     ok = mbar_wait_bounded(&S.full[s], ph);
@@ -260,16 +356,16 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
                     const uint32_t a0 = smem_u32(smem + (size_t)s * stage_bytes), b0 = a0 + kTileABytes;
 #pragma unroll
                     for (int ks = 0; ks < 4; ++ks)
-                        head_mma<kInt8>(tmem + acc * kHeadN, head_desc(a0 + ks * 32, false), head_desc(b0 + ks * 32, false), idesc,
+                        head_mma<kInt8, kCtas>(tmem + acc * kHeadN, head_desc(a0 + ks * 32, false), head_desc(b0 + ks * 32, false), idesc,
                                         (kb > 0 || ks > 0) ? 1u : 0u);
-                    umma_commit(&S.empty[s]);
+                    pair_commit<kCtas>(&S.empty[s]);
                     issued = true;
                     if (++s == P.stages) { s = 0; ph ^= 1u; }
                 }
                 if (!ok) { give_up(); break; }
-                umma_commit(&S.acc_full[acc]);
+                pair_commit<kCtas>(&S.acc_full[acc]);
             }
-            head_finish_products(S, issued);
+            head_finish_products(S, issued, kCtas);
         }
     } else {
         // ---------------- epilogue -----------------------------------------------------------------------
@@ -287,9 +383,9 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
             }
             tc_fence_after();
             const uint32_t acc_addr = tmem + lane_base + acc * kHeadN;
-            const int row = m0 + q * 32 + lane, n0 = nt * P.n_tile;
+            const int row0 = m0 + (int)rank * kHeadM + q * 32, row = row0 + lane, n0 = nt * P.n_tile;
             const bool in = row < m;
-            if (m0 + q * 32 < m) {
+            if (row0 < m) {
                 if (kInt8) {
                     const float sw = in ? P.col_scale[row] : 0.f;
                     for (int c = half; c < chunks; c += 2) {
@@ -353,10 +449,10 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&S.acc_empty[acc]);
+            if (lane == 0) pair_arrive<kCtas>(&S.acc_empty[acc], 0);
         }
     }
-    head_takedown(tmem, warp);
+    head_takedown<kCtas>(tmem, warp);
 }
 
 // ---- gradients -------------------------------------------------------------------------------------------
@@ -365,8 +461,8 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
 //     C(0)  C(1) AB(0)  C(2) AB(1)  ...  C(P-1) AB(P-2)  AB(P-1)
 // C(p): the tiles of G of piece p; AB(p): the tiles of dH's partial sums over piece p, then those of dW's rows of it.  G of
 // three pieces is kept.  A unit waits (bounded) until what it needs is done: AB(p) for C(p) and, dH adding to what the
-// piece before left, for AB(p-1); C(p) for AB(p-3), whose piece of G it overwrites.  All of that was handed out earlier,
-// by at least a phase, to CTAs that are running: the waits end, and are short.  A separate launch per product and piece
+// piece before left, for the dH tiles of piece p-1; C(p) for AB(p-3), whose piece of G it overwrites.  All of that was
+// handed out earlier, by at least a phase, to CTAs that are running: the waits end, and are short.  A separate launch per product and piece
 // (the first form) left SMs idle at the end of each of three launches a piece: 6.9 ms instead of 5.4 ms at 4 096 rows,
 // d 2 048.
 struct BackParams {
@@ -375,9 +471,11 @@ struct BackParams {
     int n_tile_d, d_tiles;
     int slices, kb_slice;           // k blocks of a piece, cut for GradHidden
     int want_h, want_w;
+    int box_v;                      // rows of a box of w_k
+    int w_blocks;                   // 1: w_mn is the three-dimensional view (d a multiple of 64), 0: two-dimensional
     const int32_t* live;
     int32_t* dev_status;
-    int32_t* sync;                  // [0] next unit, [1 + 2 p] warps done with C(p), [2 + 2 p] with AB(p); zeros at the start
+    int32_t* sync;                  // [0] next unit, [1 + 3 p + kind] warps done with the units of that kind of piece p; zeros at the start
     __nv_bfloat16* G;               // three buffers [n_pad][piece]
     const int32_t* labels; const float* lse2; const float* grad; float* label_err;
     float* part; long long part_stride;
@@ -407,21 +505,24 @@ __device__ __forceinline__ void store8(float* p, const float* v)
                  ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
 }
 
+template <int kCtas>
 __global__ void __launch_bounds__(kHeadThreads, 1)
 lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_constant__ BackMaps M)
 {
-    constexpr int kStages = kHeadRingBytes / (kTileABytes + kHeadN * kRowBytes);
-    constexpr int kStageBytes = kTileABytes + kHeadN * kRowBytes;
+    constexpr int kM = kCtas * kHeadM;
+    constexpr int kStageBytes = kTileABytes + kHeadN / kCtas * kRowBytes;
+    constexpr int kStages = kHeadRingBytes / kStageBytes;
+    constexpr int kDone = kCtas * kHeadEpiWarps;            // arrivals of a unit
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     __shared__ HeadShared S;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t tmem = head_setup(S, kStages, warp);
+    const uint32_t tmem = head_setup<kCtas>(S, kStages, warp), rank = pair_rank<kCtas>();
     volatile int* abort_flag = &S.abort;
     auto give_up = [&]() { atomicOr(P.dev_status, DSPARK_DEV_TIMEOUT); *abort_flag = 1; };
 
     const int live = *P.live;
-    const int m_tiles = (live + kHeadM - 1) / kHeadM;
+    const int m_tiles = (live + kM - 1) / kM;
 
     if (warp == 0) {
         // ---------------- producer: units, then operand tiles ----------------------------------------------
@@ -432,7 +533,7 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
             auto here = [&](int p) { return p == P.pieces - 1 ? last : P.piece; };
             auto count_c = [&](int p) { return m_tiles * ((here(p) + kHeadN - 1) / kHeadN); };
             const int count_a = P.want_h ? m_tiles * P.d_tiles * P.slices : 0;
-            auto count_ab = [&](int p) { return count_a + (P.want_w ? (here(p) + kHeadM - 1) / kHeadM * P.d_tiles : 0); };
+            auto count_b = [&](int p) { return P.want_w ? (here(p) + kM - 1) / kM * P.d_tiles : 0; };
             int issued = 0, s = 0, slot = 0;
             uint32_t ph = 0, sph = 0;
             // The walk over the phases: units arrive in rising order, so the phase only moves forward.
@@ -447,93 +548,110 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
                 if (phase == n_phases - 1) { phase_c = false; phase_piece = P.pieces - 1; }
                 else if (phase & 1) { phase_c = true; phase_piece = (phase + 1) / 2; }
                 else { phase_c = false; phase_piece = phase / 2 - 1; }
-                phase_count = phase_c ? count_c(phase_piece) : count_ab(phase_piece);
+                phase_count = phase_c ? count_c(phase_piece) : count_a + count_b(phase_piece);
             };
             // A unit is asked for while the one before it is being loaded, and a phase that was seen done is not looked at
             // again: either costs a round trip to the L2, which is most of what the ring holds.
-            int next = atomicAdd(P.sync, 1), c_done = -1, ab_done = -1;
-            auto wait_c = [&](int p) {
-                if (p <= c_done) return true;
-                c_done = p;
-                return wait_for_count(P.sync + 1 + 2 * p, count_c(p) * kHeadEpiWarps);
-            };
-            auto wait_ab = [&](int p) {
-                if (p <= ab_done) return true;
-                ab_done = p;
-                return wait_for_count(P.sync + 2 + 2 * p, count_ab(p) * kHeadEpiWarps);
+            int next = rank == 0 ? atomicAdd(P.sync, 1) : 0, seen[3] = {-1, -1, -1};
+            auto wait_for = [&](int kind, int p) {
+                if (p <= seen[kind]) return true;
+                seen[kind] = p;
+                const int count = kind == kLossGrad ? count_c(p) : kind == kGradHidden ? count_a : count_b(p);
+                return wait_for_count(P.sync + 1 + 3 * p + kind, count * kDone);
             };
             for (;;) {
-                if (!mbar_wait_bounded(&S.unit_empty[slot], sph ^ 1u)) { give_up(); break; }
-                if (*abort_flag) break;
-                const int u = next;
-                while (phase < n_phases && u - phase_first >= phase_count) next_phase();
-                int kind = kEnd, m0 = 0, n0 = 0, kb0 = 0, kb1 = 0, slice = 0;
-                const int p = phase_piece;
-                if (phase < n_phases) {
-                    int i = u - phase_first;
-                    const int piece_blocks = (here(p) + 63) / 64;
+                int kind = kEnd, m0 = 0, n0 = 0, kb0 = 0, kb1 = 0, p = 0;
+                if (rank == 0) {
+                    // ---- the next unit: its tile, and what it has to wait for ----
+                    if (!pair_wait<kCtas>(&S.unit_empty[slot], sph ^ 1u)) { give_up(); break; }
+                    if (*abort_flag) break;
+                    const int u = next;
+                    int slice = 0;
                     bool ok = true;
-                    if (phase_c) {
-                        kind = kLossGrad;
-                        m0 = i % m_tiles * kHeadM; n0 = i / m_tiles * kHeadN;
-                        kb1 = (P.d + 63) / 64;
-                        if (p >= 3) ok = wait_ab(p - 3);
-                    } else {
-                        ok = wait_c(p);
-                        if (i < count_a) {
-                            kind = kGradHidden;
-                            m0 = i % m_tiles * kHeadM; i /= m_tiles;
-                            n0 = i % P.d_tiles * P.n_tile_d; slice = i / P.d_tiles;
-                            kb0 = slice * P.kb_slice;
-                            kb0 = kb0 < piece_blocks ? kb0 : piece_blocks;
-                            kb1 = kb0 + P.kb_slice < piece_blocks ? kb0 + P.kb_slice : piece_blocks;
-                            if (p >= 1) ok = ok && wait_ab(p - 1);
+                    while (phase < n_phases && u - phase_first >= phase_count) next_phase();
+                    p = phase_piece;
+                    if (phase < n_phases) {
+                        int i = u - phase_first;
+                        const int piece_blocks = (here(p) + 63) / 64;
+                        if (phase_c) {
+                            kind = kLossGrad;
+                            m0 = i % m_tiles * kM; n0 = i / m_tiles * kHeadN;
+                            kb1 = (P.d + 63) / 64;
+                            if (p >= 3) ok = wait_for(kGradHidden, p - 3) && wait_for(kGradWeight, p - 3);
                         } else {
-                            kind = kGradWeight;
-                            i -= count_a;
-                            n0 = i % P.d_tiles * P.n_tile_d; m0 = i / P.d_tiles * kHeadM;
-                            kb1 = row_blocks;
+                            ok = wait_for(kLossGrad, p);
+                            if (i < count_a) {
+                                kind = kGradHidden;
+                                m0 = i % m_tiles * kM; i /= m_tiles;
+                                n0 = i % P.d_tiles * P.n_tile_d; slice = i / P.d_tiles;
+                                kb0 = slice * P.kb_slice;
+                                kb0 = kb0 < piece_blocks ? kb0 : piece_blocks;
+                                kb1 = kb0 + P.kb_slice < piece_blocks ? kb0 + P.kb_slice : piece_blocks;
+                                if (p >= 1) ok = ok && wait_for(kGradHidden, p - 1);
+                            } else {
+                                kind = kGradWeight;
+                                i -= count_a;
+                                n0 = i % P.d_tiles * P.n_tile_d; m0 = i / P.d_tiles * kM;
+                                kb1 = row_blocks;
+                            }
                         }
-                        fence_proxy_async_all();            // G was written by ordinary stores and is read by copies
+                        if (!ok) { give_up(); break; }
                     }
-                    if (!ok) { give_up(); break; }
+                    const int4 u0 = make_int4(kind, m0, n0, kb0), u1 = make_int4(kb1, p, slice, 0);
+                    S.unit[slot][0] = u0;
+                    S.unit[slot][1] = u1;
+                    mbar_arrive(&S.unit_full[slot]);
+                    if (kCtas == 2) {
+                        const uint32_t to = pair_address(&S.unit[slot][0], 1);
+                        asm volatile("st.shared::cluster.v4.s32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(u0.x), "r"(u0.y), "r"(u0.z), "r"(u0.w) : "memory");
+                        asm volatile("st.shared::cluster.v4.s32 [%0], {%1,%2,%3,%4};" ::"r"(to + 16), "r"(u1.x), "r"(u1.y), "r"(u1.z), "r"(u1.w) : "memory");
+                        pair_arrive<kCtas>(&S.unit_full[slot], 1);
+                    }
+                } else {
+                    // ---- the unit that the leader has taken ----
+                    if (!pair_wait<kCtas>(&S.unit_full[slot], sph)) { give_up(); break; }
+                    const int4 u0 = S.unit[slot][0], u1 = S.unit[slot][1];
+                    pair_arrive<kCtas>(&S.unit_empty[slot], 0);
+                    kind = u0.x; m0 = u0.y; n0 = u0.z; kb0 = u0.w; kb1 = u1.x; p = u1.y;
                 }
-                S.unit[slot][0] = make_int4(kind, m0, n0, kb0);
-                S.unit[slot][1] = make_int4(kb1, p, slice, 0);
-                mbar_arrive(&S.unit_full[slot]);
                 if (++slot == kUnitSlots) { slot = 0; sph ^= 1u; }
                 if (kind == kEnd) break;
-                next = atomicAdd(P.sync, 1);
+                if (kind != kLossGrad) fence_proxy_async_all();            // G was written by ordinary stores and is read by copies
+                if (rank == 0) next = atomicAdd(P.sync, 1);
                 const int v0 = p * P.piece, g0 = p % 3 * P.n_pad;          // first entry of the piece, first row of its G
-                const uint32_t load_bytes = (uint32_t)(kTileABytes + (kind == kLossGrad ? (P.V < kHeadN ? P.V : kHeadN) : P.n_tile_d) * kRowBytes);
+                const int half_d = P.n_tile_d / kCtas;                     // columns of B in this CTA
+                const uint32_t load_bytes = (uint32_t)(kCtas * (kTileABytes + (kind == kLossGrad ? P.box_v : half_d) * kRowBytes));
                 for (int kb = kb0; kb < kb1; ++kb) {
                     if (!mbar_wait_bounded(&S.empty[s], ph ^ 1u)) { give_up(); break; }
                     unsigned char* a = smem + (size_t)s * kStageBytes;
                     unsigned char* b = a + kTileABytes;
                     uint64_t* bar = &S.full[s];
-                    mbar_arrive_expect_tx(bar, load_bytes);
-                    const int kx = kb * 64;
+                    if (rank == 0) mbar_arrive_expect_tx(bar, load_bytes);
+                    const int kx = kb * 64, mr = m0 + (int)rank * kHeadM;
                     if (kind == kLossGrad) {
-                        tma_load_2d(a, &M.rows_k, kx, m0, bar, pol);
-                        tma_load_2d(b, &M.w_k, kx, v0 + n0, bar, pol);
-                    } else if (kind == kGradHidden) {
-                        tma_load_2d(a, &M.g_k, kx, g0 + m0, bar, pol);
-                        for (int j = 0; j < P.n_tile_d; j += 64) tma_load_2d(b + j * kRowBytes, &M.w_mn, n0 + j, v0 + kx, bar, pol);
+                        pair_load_2d<kCtas>(a, &M.rows_k, kx, mr, bar, pol);
+                        pair_load_2d<kCtas>(b, &M.w_k, kx, v0 + n0 + (int)rank * (kHeadN / kCtas), bar, pol);
                     } else {
-#pragma unroll
-                        for (int j = 0; j < kHeadM; j += 64) tma_load_2d(a + j * kRowBytes, &M.g_mn, m0 + j, g0 + kx, bar, pol);
-                        for (int j = 0; j < P.n_tile_d; j += 64) tma_load_2d(b + j * kRowBytes, &M.rows_mn, n0 + j, kx, bar, pol);
+                        const int nr = n0 + (int)rank * half_d;
+                        if (kind == kGradHidden) {
+                            pair_load_2d<kCtas>(a, &M.g_k, kx, g0 + mr, bar, pol);
+                            if (P.w_blocks) pair_load_3d<kCtas>(b, &M.w_mn, 0, v0 + kx, nr / 64, bar, pol);
+                            else for (int j = 0; j < half_d; j += 64) pair_load_2d<kCtas>(b + j * kRowBytes, &M.w_mn, nr + j, v0 + kx, bar, pol);
+                        } else {
+                            pair_load_3d<kCtas>(a, &M.g_mn, 0, g0 + kx, mr / 64, bar, pol);
+                            pair_load_3d<kCtas>(b, &M.rows_mn, 0, kx, nr / 64, bar, pol);
+                        }
                     }
                     ++issued;
                     if (++s == kStages) { s = 0; ph ^= 1u; }
                 }
                 if (*abort_flag) break;
             }
-            if (*abort_flag) head_drain(S, kStages, issued);
+            if (*abort_flag) head_drain(S, kStages, issued, rank == 0);
         }
     } else if (warp == 1) {
-        // ---------------- MMA issuer ---------------------------------------------------------------------
-        if (lane == 0) {
+        // ---------------- MMA issuer (of a pair: the leader's) -------------------------------------------
+        if (lane == 0 && rank == 0) {
             int s = 0, t = 0, slot = 0;
             uint32_t ph = 0, sph = 0;
             bool issued = false, ok = true;
@@ -547,10 +665,10 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
                 if (kind == kEnd) break;
                 if (kb0 == kb1) continue;                   // nothing to add up: the epilogue knows
                 const bool a_mn = kind == kGradWeight, b_mn = kind != kLossGrad;
-                const uint32_t idesc = head_idesc(false, a_mn, b_mn, kind == kLossGrad ? kHeadN : P.n_tile_d);
+                const uint32_t idesc = head_idesc<kCtas>(false, a_mn, b_mn, kind == kLossGrad ? kHeadN : P.n_tile_d);
                 const uint32_t step_a = a_mn ? 2048 : 32, step_b = b_mn ? 2048 : 32;
                 const uint32_t acc = (uint32_t)(t & 1), aph = (uint32_t)(t >> 1) & 1u;
-                ok = mbar_wait_bounded(&S.acc_empty[acc], aph ^ 1u);
+                ok = pair_wait<kCtas>(&S.acc_empty[acc], aph ^ 1u);
                 tc_fence_after();
                 for (int kb = kb0; ok && kb < kb1; ++kb) {
                     ok = mbar_wait_bounded(&S.full[s], ph);
@@ -559,18 +677,18 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
                     const uint32_t a0 = smem_u32(smem + (size_t)s * kStageBytes), b0 = a0 + kTileABytes;
 #pragma unroll
                     for (int ks = 0; ks < 4; ++ks)
-                        head_mma<false>(tmem + acc * kHeadN, head_desc(a0 + ks * step_a, a_mn), head_desc(b0 + ks * step_b, b_mn), idesc,
+                        head_mma<false, kCtas>(tmem + acc * kHeadN, head_desc(a0 + ks * step_a, a_mn), head_desc(b0 + ks * step_b, b_mn), idesc,
                                         (kb > kb0 || ks > 0) ? 1u : 0u);
-                    umma_commit(&S.empty[s]);
+                    pair_commit<kCtas>(&S.empty[s]);
                     issued = true;
                     if (++s == kStages) { s = 0; ph ^= 1u; }
                 }
                 if (!ok) break;
-                umma_commit(&S.acc_full[acc]);
+                pair_commit<kCtas>(&S.acc_full[acc]);
                 ++t;
             }
             if (!ok) give_up();
-            head_finish_products(S, issued);
+            head_finish_products(S, issued, kCtas);
         }
     } else {
         // ---------------- epilogue -----------------------------------------------------------------------
@@ -581,15 +699,15 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
         int t = 0, slot = 0;
         uint32_t sph = 0;
         while (!*abort_flag) {
-            if (!__all_sync(0xffffffffu, mbar_wait_bounded(&S.unit_full[slot], sph))) {
+            if (!__all_sync(0xffffffffu, pair_wait<kCtas>(&S.unit_full[slot], sph))) {
                 if (lane == 0) give_up();
                 break;
             }
             const int4 u0 = S.unit[slot][0], u1 = S.unit[slot][1];
             __syncwarp();
-            if (lane == 0) mbar_arrive(&S.unit_empty[slot]);
+            if (lane == 0) pair_arrive<kCtas>(&S.unit_empty[slot], 0);
             if (++slot == kUnitSlots) { slot = 0; sph ^= 1u; }
-            const int kind = u0.x, m0 = u0.y, n0 = u0.z, p = u1.y;
+            const int kind = u0.x, row0 = u0.y + (int)rank * kHeadM + q * 32, n0 = u0.z, p = u1.y;
             const bool any = u0.w < u1.x;
             if (kind == kEnd) break;
             const uint32_t acc = (uint32_t)(t & 1), aph = (uint32_t)(t >> 1) & 1u;
@@ -602,7 +720,7 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
                 ++t;
             }
             const uint32_t acc_addr = tmem + lane_base + acc * kHeadN;
-            const int row = m0 + q * 32 + lane;
+            const int row = row0 + lane;
             auto load = [&](int c, float (&v)[32]) {
                 __syncwarp();
                 if (any) tmem_load32(acc_addr + (uint32_t)(c * 32), v);
@@ -642,7 +760,7 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
                 }
             } else if (kind == kGradHidden) {
                 float* out = P.part + ((long long)u1.z * P.n_pad + row) * P.part_stride;
-                if (m0 + q * 32 < live)
+                if (row0 < live)
                     for (int c = half; c < P.n_tile_d / 32; c += 2) {
                         const int col0 = n0 + c * 32;
                         if (col0 >= P.d) break;
@@ -661,7 +779,7 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
                         }
                     }
             } else {
-                const int first = p * P.piece + m0 + q * 32;               // vocabulary entry of lane 0
+                const int first = p * P.piece + row0;               // vocabulary entry of lane 0
                 const int rows = P.V - first < 32 ? P.V - first : 32;
                 __nv_bfloat16* out = P.dw + (long long)first * P.dw_stride;
                 if (rows > 0)
@@ -681,13 +799,13 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
             if (kind != kGradWeight) fence_proxy_async_all();
             __syncwarp();
             if (lane == 0) {
-                if (any) mbar_arrive(&S.acc_empty[acc]);
+                if (any) pair_arrive<kCtas>(&S.acc_empty[acc], 0);
                 __threadfence();
-                atomicAdd(P.sync + (kind == kLossGrad ? 1 : 2) + 2 * p, 1);
+                atomicAdd(P.sync + 1 + 3 * p + kind, 1);
             }
         }
     }
-    head_takedown(tmem, warp);
+    head_takedown<kCtas>(tmem, warp);
 }
 
 // ---- rows that count, in order ------------------------------------------------------------------------
@@ -907,6 +1025,20 @@ static bool operand_map(CUtensorMap* map, const void* base, int es, long long ro
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The same matrix by blocks of 64 columns, [block][row][64]: one copy brings `blocks` mn-major boxes of `box_rows` rows that
+// lie behind one another in shared memory.  The columns of the last block past `cols` are read: the matrix has them.
+static bool block_map(CUtensorMap* map, const void* base, long long rows, long long cols, long long pitch_bytes, int box_rows, int blocks)
+{
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {64, (cuuint64_t)rows, (cuuint64_t)((cols + 63) / 64)};
+    const cuuint64_t strides[2] = {(cuuint64_t)pitch_bytes, 128};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, (cuuint32_t)blocks};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 static int device_sms()
 {
     static std::atomic<int> sms[64];
@@ -934,28 +1066,48 @@ static bool allow_smem(Kernel kernel, int bytes, std::atomic<unsigned long long>
     return true;
 }
 
-template <int kMode>
+// launch_pdl with clusters of kCtas CTAs
+template <int kCtas, typename... KArgs, typename... Args>
+static void launch_pairs(void (*kernel)(KArgs...), int ctas, size_t smem, cudaStream_t stream, Args... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3(kHeadThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = kCtas; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = kCtas > 1 ? 2 : 1;
+    cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+template <int kMode, int kCtas>
 static int head_launch(HeadParams P, const CUtensorMap& a, const CUtensorMap& b, cudaStream_t s, int timer_id)
 {
     constexpr int kSmem = kHeadRingBytes + 1024;
     static std::atomic<unsigned long long> ready{0};
-    if (!allow_smem(lm_head_kernel<kMode>, kSmem, ready)) return launch_status();
-    P.stages = kHeadRingBytes / (kTileABytes + P.n_tile * kRowBytes);
+    if (!allow_smem(lm_head_kernel<kMode, kCtas>, kSmem, ready)) return launch_status();
+    P.stages = kHeadRingBytes / (kTileABytes + P.n_tile / kCtas * kRowBytes);
     if (P.stages > kHeadMaxStages) P.stages = kHeadMaxStages;
-    const long long units = (long long)((P.m + kHeadM - 1) / kHeadM) * ((P.n + P.n_tile - 1) / P.n_tile);
-    const int sms = device_sms();
+    const long long units = (long long)((P.m + kCtas * kHeadM - 1) / (kCtas * kHeadM)) * ((P.n + P.n_tile - 1) / P.n_tile);
+    const int groups = device_sms() / kCtas;
     KernelTimerScope timer(timer_id, s);
-    launch_pdl(lm_head_kernel<kMode>, dim3((unsigned)(units < sms ? units : sms)), dim3(kHeadThreads), kSmem, s, P, a, b);
+    launch_pairs<kCtas>(lm_head_kernel<kMode, kCtas>, kCtas * (int)(units < groups ? units : groups), kSmem, s, P, a, b);
     return launch_status();
 }
 
+template <int kCtas>
 static int back_launch(const BackParams& P, const BackMaps& M, cudaStream_t s)
 {
     constexpr int kSmem = kHeadRingBytes + 1024 + kHeadEpiWarps * kTurnBytes;
     static std::atomic<unsigned long long> ready{0};
-    if (!allow_smem(lm_head_backward_kernel, kSmem, ready)) return launch_status();
+    if (!allow_smem(lm_head_backward_kernel<kCtas>, kSmem, ready)) return launch_status();
     KernelTimerScope timer(DSPARK_K_HEAD_GRAD, s);
-    launch_pdl(lm_head_backward_kernel, dim3(device_sms()), dim3(kHeadThreads), kSmem, s, P, M);
+    launch_pairs<kCtas>(lm_head_backward_kernel<kCtas>, device_sms() / kCtas * kCtas, kSmem, s, P, M);
     return launch_status();
 }
 
@@ -965,14 +1117,17 @@ static long long kPieceBytes = getenv("PIECE") ? atoll(getenv("PIECE")) << 20 : 
 struct LossWs {
     size_t live, sync, idx, label, z_label, lse2, grad, label_err, rows, stats, G, part, total;
     long long n_pad, d_pitch, part_pitch;
-    int piece, pieces, n_sync, slices, kb_slice, n_tile_d, d_tiles;
+    int ctas, piece, pieces, n_sync, slices, kb_slice, n_tile_d, d_tiles;
 };
 static LossWs loss_layout(int N, int V, int d)
 {
     LossWs w;
-    w.n_pad = (long long)up((size_t)N, kHeadM);
-    w.d_pitch = w.part_pitch = (long long)up((size_t)d, 8);
-    w.n_tile_d = d >= kHeadN ? kHeadN : (int)up((size_t)d, 64);
+    w.ctas = N > kHeadM ? 2 : 1;                            // one row tile of 128 rows: the second CTA of a pair would hold none
+    if (getenv("CTAS")) w.ctas = atoi(getenv("CTAS"));
+    w.n_pad = (long long)up((size_t)N, w.ctas * kHeadM);
+    w.d_pitch = (long long)up((size_t)d, 64);               // whole blocks of columns (block_map)
+    w.part_pitch = (long long)up((size_t)d, 8);
+    w.n_tile_d = d >= kHeadN ? kHeadN : (int)up((size_t)d, 64 * w.ctas);
     w.d_tiles = (d + w.n_tile_d - 1) / w.n_tile_d;
     // A piece of the vocabulary is such that neither its rows of W nor its columns of G take more than kPieceBytes, and not
     // narrower than 2 048 entries, below which adding the partial sums of dH would cost more than the products.
@@ -983,11 +1138,11 @@ static LossWs loss_layout(int N, int V, int d)
     if (piece > all) piece = all;
     w.piece = (int)piece;
     w.pieces = (int)((V + piece - 1) / piece);
-    w.n_sync = 1 + 2 * w.pieces;
+    w.n_sync = 1 + 3 * w.pieces;
     // k blocks of the units of one piece, over the SMs: a slice of dH's sum over the piece is at most half of an SM's share
-    const long long m_tiles = w.n_pad / kHeadM, blocks = piece / 64;
+    const long long m_tiles = w.n_pad / (w.ctas * kHeadM), blocks = piece / 64;
     const long long work = 2 * m_tiles * w.d_tiles * blocks + m_tiles * (piece / kHeadN) * ((d + 63) / 64);
-    long long most = work / 296;
+    long long most = work / (2 * 148 / w.ctas);
     if (most < 8) most = 8;
     long long slices = (blocks + most - 1) / most;
     if (slices > 64) slices = 64;
@@ -1057,14 +1212,16 @@ int dspark_lm_head_int8(const int8_t* x_q, int64_t x_row_stride, const float* x_
     // engine more than one that does not (one row of 32: 170 us instead of 90 at V = 129 280, K = 4 096)
     const int row_tiles = (rows + kHeadN - 1) / kHeadN;
     P.n_tile = (int)up((size_t)((rows + row_tiles - 1) / row_tiles), 32);
-    P.box_n = rows < P.n_tile ? rows : P.n_tile;
+    const int ctas = getenv("CTAS") ? atoi(getenv("CTAS")) : 2, part = P.n_tile / ctas;
+    P.box_n = rows < part ? rows : part;
     P.live = n_live; P.dev_status = dev_status;
     P.out = out_logits; P.out_stride = out_row_stride; P.out_bf16 = out_dtype == DSPARK_BF16;
     P.row_scale = x_scale; P.col_scale = w_scale;
     CUtensorMap a, b;
     if (!operand_map(&a, w_q, 1, V, K, w_row_stride, kRowBytes, kHeadM) || !operand_map(&b, x_q, 1, rows, K, x_row_stride, kRowBytes, P.box_n))
         return DSPARK_ERR_CUDA;
-    return head_launch<kInt8Logits>(P, a, b, (cudaStream_t)stream, DSPARK_K_HEAD_INT8);
+    return ctas == 2 ? head_launch<kInt8Logits, 2>(P, a, b, (cudaStream_t)stream, DSPARK_K_HEAD_INT8)
+                     : head_launch<kInt8Logits, 1>(P, a, b, (cudaStream_t)stream, DSPARK_K_HEAD_INT8);
 }
 
 size_t dspark_lm_head_loss_workspace_bytes(int N, int V, int d)
@@ -1098,13 +1255,13 @@ int dspark_lm_head_loss(const void* hidden, int64_t hidden_row_stride, const voi
     HeadParams P;
     memset(&P, 0, sizeof P);
     P.m = N; P.n = V; P.k = d;
-    P.n_tile = kHeadN; P.box_n = V < kHeadN ? V : kHeadN;
+    P.n_tile = kHeadN; P.box_n = V < kHeadN / w.ctas ? V : kHeadN / w.ctas;
     P.live = g.live; P.dev_status = dev_status;
     P.stats = (float2*)(ws + w.stats); P.stats_stride = w.n_pad; P.labels = g.label; P.z_label = (float*)(ws + w.z_label);
     CUtensorMap a, b;
     if (!operand_map(&a, g.rows, 2, w.n_pad, d, w.d_pitch * 2, 64, kHeadM) || !operand_map(&b, weight, 2, V, d, weight_row_stride * 2, 64, P.box_n))
         return DSPARK_ERR_CUDA;
-    const int rc = head_launch<kLossStats>(P, a, b, s, DSPARK_K_HEAD_LOSS);
+    const int rc = w.ctas == 2 ? head_launch<kLossStats, 2>(P, a, b, s, DSPARK_K_HEAD_LOSS) : head_launch<kLossStats, 1>(P, a, b, s, DSPARK_K_HEAD_LOSS);
     if (rc != DSPARK_OK) return rc;
     LossParams L;
     L.stats = P.stats; L.stats_stride = w.n_pad; L.entries = 2 * ((V + kHeadN - 1) / kHeadN);
@@ -1145,27 +1302,29 @@ int dspark_lm_head_loss_backward(const void* hidden, int64_t hidden_row_stride, 
         gather_launch(g, s);
     }
     BackMaps M;
-    const int box_v = V < kHeadN ? V : kHeadN;
+    const int box_v = V < kHeadN / w.ctas ? V : kHeadN / w.ctas;
     const long long g_pitch = (long long)w.piece * 2;
     if (!operand_map(&M.rows_k, g.rows, 2, w.n_pad, d, w.d_pitch * 2, 64, kHeadM) ||
         !operand_map(&M.w_k, weight, 2, V, d, weight_row_stride * 2, 64, box_v) ||
         !operand_map(&M.g_k, ws + w.G, 2, 3 * w.n_pad, w.piece, g_pitch, 64, kHeadM) ||
-        !operand_map(&M.w_mn, weight, 2, V, d, weight_row_stride * 2, 64, 64) ||
-        !operand_map(&M.g_mn, ws + w.G, 2, 3 * w.n_pad, w.piece, g_pitch, 64, 64) ||
-        !operand_map(&M.rows_mn, g.rows, 2, w.n_pad, d, w.d_pitch * 2, 64, 64))
+        !(d % 64 == 0 ? block_map(&M.w_mn, weight, V, d, weight_row_stride * 2, 64, w.n_tile_d / w.ctas / 64)
+                      : operand_map(&M.w_mn, weight, 2, V, d, weight_row_stride * 2, 64, 64)) ||
+        !block_map(&M.g_mn, ws + w.G, 3 * w.n_pad, w.piece, g_pitch, 64, kHeadM / 64) ||
+        !block_map(&M.rows_mn, g.rows, w.n_pad, d, w.d_pitch * 2, 64, w.n_tile_d / w.ctas / 64))
         return DSPARK_ERR_CUDA;
     BackParams P;
     memset(&P, 0, sizeof P);
     P.n_pad = (int)w.n_pad; P.V = V; P.d = d;
     P.piece = w.piece; P.pieces = w.pieces; P.n_tile_d = w.n_tile_d; P.d_tiles = w.d_tiles;
     P.slices = w.slices; P.kb_slice = w.kb_slice;
+    P.box_v = box_v; P.w_blocks = d % 64 == 0;
     P.want_h = out_grad_hidden != nullptr; P.want_w = out_grad_weight != nullptr;
     P.live = g.live; P.dev_status = dev_status; P.sync = g.sync;
     P.G = (__nv_bfloat16*)(ws + w.G);
     P.labels = g.label; P.lse2 = g.lse2; P.grad = g.grad; P.label_err = (float*)(ws + w.label_err);
     P.part = (float*)(ws + w.part); P.part_stride = w.part_pitch;
     P.dw = (__nv_bfloat16*)out_grad_weight; P.dw_stride = grad_weight_row_stride;
-    const int rc = back_launch(P, M, s);
+    const int rc = w.ctas == 2 ? back_launch<2>(P, M, s) : back_launch<1>(P, M, s);
     if (rc != DSPARK_OK) return rc;
     if (out_grad_hidden) {
         HiddenParams Hp;
