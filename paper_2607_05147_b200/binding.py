@@ -610,19 +610,26 @@ def dspark_sts_apply(conf: torch.Tensor, T: torch.Tensor, out: torch.Tensor) -> 
 
 
 # -------------------------------------------------------------------- vocabulary projection ----
-def _here(t: torch.Tensor, name: str, dtype) -> None:
-    dev = t.get_device()                                    # -1: a CPU tensor
-    if dev < 0 or dev != torch.cuda.current_device():
+def _here(t: torch.Tensor, name: str, dtype, dev: int) -> None:
+    if t.get_device() != dev:                               # -1: a CPU tensor
         raise DsparkError(f"{name} must be a CUDA tensor on the current device (no CPU path exists)")
     if t.dtype is not dtype:
         raise DsparkError(f"{name} must be {dtype}, got {t.dtype}")
 
 
-def _rows(t: Optional[torch.Tensor], name: str, dtype, rows: int, cols: int):
+def _device_of(t: torch.Tensor, name: str) -> int:
+    """The current device, which `t` has to be on."""
+    dev = t.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise DsparkError(f"{name} must be a CUDA tensor on the current device (no CPU path exists)")
+    return dev
+
+
+def _rows(t: Optional[torch.Tensor], name: str, dtype, rows: int, cols: int, dev: int):
     """(address, row stride) of a 2-D matrix with unit inner stride on the current device, at least rows x cols."""
     if t is None:
         return None, 0
-    _here(t, name, dtype)
+    _here(t, name, dtype, dev)
     shape, stride = t.shape, t.stride()
     if len(shape) != 2 or shape[0] < rows or shape[1] != cols:
         raise DsparkError(f"{name} must be [{rows}, {cols}], got {list(shape)}")
@@ -632,14 +639,20 @@ def _rows(t: Optional[torch.Tensor], name: str, dtype, rows: int, cols: int):
     return t.data_ptr(), stride[0] if shape[0] > 1 else -(-cols // 16) * 16
 
 
-def _vec(t: Optional[torch.Tensor], name: str, dtype, n: int):
+def _vec(t: Optional[torch.Tensor], name: str, dtype, n: int, dev: int):
     """Address of a contiguous vector of at least n entries on the current device."""
     if t is None:
         return None
-    _here(t, name, dtype)
+    _here(t, name, dtype, dev)
     if t.numel() < n or not t.is_contiguous():
         raise DsparkError(f"{name} must be contiguous with {n} entries")
     return t.data_ptr()
+
+
+def _matrix(t, name: str):
+    if t is None or t.dim() != 2:
+        raise DsparkError(f"{name} must be a matrix")
+    return t.shape
 
 
 def _need(t, name: str):
@@ -652,44 +665,53 @@ def dspark_rms_norm_quant(x: torch.Tensor, weight: torch.Tensor, eps: float, *, 
                           out_residual: Optional[torch.Tensor] = None, out_q: torch.Tensor, out_scale: torch.Tensor,
                           out_norm: Optional[torch.Tensor] = None, n_live: Optional[torch.Tensor] = None) -> None:
     """int8 rows and their scales of the normalised x (+ residual); n_live: CUDA int32 count of the rows to compute."""
-    if x.dim() != 2 or x.dtype not in (torch.float32, torch.bfloat16):
-        raise DsparkError("x must be a float32 or bfloat16 matrix")
-    rows, d = x.shape
-    xp, xs = _rows(x, "x", x.dtype, rows, d)
-    rp, rs = _rows(residual, "residual", x.dtype, rows, d)
-    hp, hs = _rows(out_residual, "out_residual", x.dtype, rows, d)
-    qp, qs = _rows(_need(out_q, "out_q"), "out_q", torch.int8, rows, d)
-    yp, ys = _rows(out_norm, "out_norm", x.dtype, rows, d)
-    rc = lib().dspark_rms_norm_quant(xp, xs, rp, rs, _vec(weight, "weight", x.dtype, d),
-                                     DSPARK_F32 if x.dtype == torch.float32 else DSPARK_BF16, rows, d, float(eps),
-                                     _vec(n_live, "n_live", torch.int32, 1), hp, hs, qp, qs,
-                                     _vec(_need(out_scale, "out_scale"), "out_scale", torch.float32, rows), yp, ys, _stream())
+    rows, d = _matrix(x, "x")
+    dtype = x.dtype
+    if dtype is torch.bfloat16:
+        code = DSPARK_BF16
+    elif dtype is torch.float32:
+        code = DSPARK_F32
+    else:
+        raise DsparkError("x must be float32 or bfloat16")
+    dev = _device_of(x, "x")
+    xp, xs = _rows(x, "x", dtype, rows, d, dev)
+    rp, rs = _rows(residual, "residual", dtype, rows, d, dev)
+    hp, hs = _rows(out_residual, "out_residual", dtype, rows, d, dev)
+    qp, qs = _rows(_need(out_q, "out_q"), "out_q", torch.int8, rows, d, dev)
+    yp, ys = _rows(out_norm, "out_norm", dtype, rows, d, dev)
+    rc = lib().dspark_rms_norm_quant(xp, xs, rp, rs, _vec(_need(weight, "weight"), "weight", dtype, d, dev), code, rows, d, float(eps),
+                                     _vec(n_live, "n_live", torch.int32, 1, dev), hp, hs, qp, qs,
+                                     _vec(_need(out_scale, "out_scale"), "out_scale", torch.float32, rows, dev), yp, ys, _stream())
     _check(rc, "dspark_rms_norm_quant")
 
 
 def dspark_lm_head_quantize(W: torch.Tensor, out_q: torch.Tensor, out_scale: torch.Tensor) -> None:
     """int8 rows and scales of the bf16 vocabulary matrix [V, K] (once, when the weights are loaded)."""
-    V, K = W.shape
-    wp, ws = _rows(W, "W", torch.bfloat16, V, K)
-    qp, qs = _rows(out_q, "out_q", torch.int8, V, K)
-    _check(lib().dspark_lm_head_quantize(wp, ws, V, K, qp, qs, _vec(out_scale, "out_scale", torch.float32, V), _stream()),
-           "dspark_lm_head_quantize")
+    V, K = _matrix(W, "W")
+    dev = _device_of(W, "W")
+    wp, ws = _rows(W, "W", torch.bfloat16, V, K, dev)
+    qp, qs = _rows(_need(out_q, "out_q"), "out_q", torch.int8, V, K, dev)
+    _check(lib().dspark_lm_head_quantize(wp, ws, V, K, qp, qs, _vec(_need(out_scale, "out_scale"), "out_scale", torch.float32, V, dev),
+                                         _stream()), "dspark_lm_head_quantize")
 
 
 def dspark_lm_head_int8(x_q: torch.Tensor, x_scale: torch.Tensor, w_q: torch.Tensor, w_scale: torch.Tensor, *,
                         out_logits: torch.Tensor, n_live: Optional[torch.Tensor] = None, dev_status: torch.Tensor) -> None:
     """Logit rows (bf16 or fp32) from int8 hidden states and weights; n_live: CUDA int32 count of the rows to compute."""
-    rows, K = x_q.shape
-    V = w_q.shape[0]
-    if out_logits.dtype not in (torch.float32, torch.bfloat16):
+    rows, K = _matrix(x_q, "x_q")
+    V = _matrix(w_q, "w_q")[0]
+    out_dtype = _need(out_logits, "out_logits").dtype
+    if out_dtype is not torch.float32 and out_dtype is not torch.bfloat16:
         raise DsparkError("out_logits must be float32 or bfloat16")
-    xp, xs = _rows(x_q, "x_q", torch.int8, rows, K)
-    wp, ws = _rows(w_q, "w_q", torch.int8, V, K)
-    op, os_ = _rows(out_logits, "out_logits", out_logits.dtype, rows, V)
-    rc = lib().dspark_lm_head_int8(xp, xs, _vec(x_scale, "x_scale", torch.float32, rows), wp, ws,
-                                   _vec(w_scale, "w_scale", torch.float32, V), rows, V, K, _vec(n_live, "n_live", torch.int32, 1),
-                                   op, DSPARK_F32 if out_logits.dtype == torch.float32 else DSPARK_BF16, os_,
-                                   _vec(_need(dev_status, "dev_status"), "dev_status", torch.int32, 1), _stream())
+    dev = _device_of(x_q, "x_q")
+    xp, xs = _rows(x_q, "x_q", torch.int8, rows, K, dev)
+    wp, ws = _rows(w_q, "w_q", torch.int8, V, K, dev)
+    op, os_ = _rows(out_logits, "out_logits", out_dtype, rows, V, dev)
+    rc = lib().dspark_lm_head_int8(xp, xs, _vec(_need(x_scale, "x_scale"), "x_scale", torch.float32, rows, dev), wp, ws,
+                                   _vec(_need(w_scale, "w_scale"), "w_scale", torch.float32, V, dev), rows, V, K,
+                                   _vec(n_live, "n_live", torch.int32, 1, dev), op,
+                                   DSPARK_F32 if out_dtype is torch.float32 else DSPARK_BF16, os_,
+                                   _vec(_need(dev_status, "dev_status"), "dev_status", torch.int32, 1, dev), _stream())
     _check(rc, "dspark_lm_head_int8")
 
 
@@ -698,27 +720,27 @@ def dspark_lm_head_loss_workspace_bytes(N: int, V: int, d: int) -> int:
 
 
 def _loss_args(hidden, weight, labels):
-    if hidden.dim() != 2 or weight.dim() != 2:
-        raise DsparkError("hidden and weight must be matrices")
-    N, d = hidden.shape
-    V = weight.shape[0]
-    hp, hs = _rows(hidden, "hidden", torch.bfloat16, N, d)
-    wp, ws = _rows(weight, "weight", torch.bfloat16, V, d)
-    return (hp, hs, wp, ws, _vec(labels, "labels", torch.int32, N)), N, V, d
+    N, d = _matrix(hidden, "hidden")
+    V = _matrix(weight, "weight")[0]
+    dev = _device_of(hidden, "hidden")
+    hp, hs = _rows(hidden, "hidden", torch.bfloat16, N, d, dev)
+    wp, ws = _rows(weight, "weight", torch.bfloat16, V, d, dev)
+    return (hp, hs, wp, ws, _vec(_need(labels, "labels"), "labels", torch.int32, N, dev)), N, V, d, dev
 
 
-def _ws(workspace: torch.Tensor):
-    nbytes = workspace.numel() * workspace.element_size()
-    return _vec(workspace, "workspace", workspace.dtype, 0), nbytes
+def _loss_scratch(dev_status, workspace, dev):
+    _need(workspace, "workspace")
+    return (_vec(_need(dev_status, "dev_status"), "dev_status", torch.int32, 1, dev), _vec(workspace, "workspace", workspace.dtype, 0, dev),
+            workspace.numel() * workspace.element_size(), _stream())
 
 
 def dspark_lm_head_loss(hidden: torch.Tensor, weight: torch.Tensor, labels: torch.Tensor, *, out_loss: torch.Tensor,
                         out_lse: torch.Tensor, dev_status: torch.Tensor, workspace: torch.Tensor) -> None:
     """Cross entropy of every row of `hidden` [N, d] against `weight` [V, d]; a negative label: the row is ignored."""
-    head, N, V, d = _loss_args(hidden, weight, labels)
-    rc = lib().dspark_lm_head_loss(*head, N, V, d, _vec(_need(out_loss, "out_loss"), "out_loss", torch.float32, N),
-                                   _vec(_need(out_lse, "out_lse"), "out_lse", torch.float32, N),
-                                   _vec(_need(dev_status, "dev_status"), "dev_status", torch.int32, 1), *_ws(workspace), _stream())
+    head, N, V, d, dev = _loss_args(hidden, weight, labels)
+    rc = lib().dspark_lm_head_loss(*head, N, V, d, _vec(_need(out_loss, "out_loss"), "out_loss", torch.float32, N, dev),
+                                   _vec(_need(out_lse, "out_lse"), "out_lse", torch.float32, N, dev),
+                                   *_loss_scratch(dev_status, workspace, dev))
     _check(rc, "dspark_lm_head_loss")
 
 
@@ -727,13 +749,12 @@ def dspark_lm_head_loss_backward(hidden: torch.Tensor, weight: torch.Tensor, lab
                                  out_grad_weight: Optional[torch.Tensor] = None, dev_status: torch.Tensor,
                                  workspace: torch.Tensor) -> None:
     """Gradients of sum_n grad_loss[n] * loss[n]; lse: what dspark_lm_head_loss left for the same rows."""
-    head, N, V, d = _loss_args(hidden, weight, labels)
-    hp, hs = _rows(out_grad_hidden, "out_grad_hidden", torch.bfloat16, N, d)
-    wp, ws = _rows(out_grad_weight, "out_grad_weight", torch.bfloat16, V, d)
-    rc = lib().dspark_lm_head_loss_backward(*head, _vec(_need(lse, "lse"), "lse", torch.float32, N),
-                                            _vec(_need(grad_loss, "grad_loss"), "grad_loss", torch.float32, N), N, V, d, hp, hs, wp, ws,
-                                            _vec(_need(dev_status, "dev_status"), "dev_status", torch.int32, 1), *_ws(workspace),
-                                            _stream())
+    head, N, V, d, dev = _loss_args(hidden, weight, labels)
+    hp, hs = _rows(out_grad_hidden, "out_grad_hidden", torch.bfloat16, N, d, dev)
+    wp, ws = _rows(out_grad_weight, "out_grad_weight", torch.bfloat16, V, d, dev)
+    rc = lib().dspark_lm_head_loss_backward(*head, _vec(_need(lse, "lse"), "lse", torch.float32, N, dev),
+                                            _vec(_need(grad_loss, "grad_loss"), "grad_loss", torch.float32, N, dev), N, V, d, hp, hs, wp, ws,
+                                            *_loss_scratch(dev_status, workspace, dev))
     _check(rc, "dspark_lm_head_loss_backward")
 
 

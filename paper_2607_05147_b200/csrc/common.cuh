@@ -115,6 +115,8 @@ __device__ __forceinline__ float ex2_approx(float x)
 // returns once that kernel has completed and its writes are visible, and must precede any read of
 // its results.
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// The exception: a kernel whose successor is known and only sets itself up before its own pdl_wait() lets it start.
+__device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // Waits (bounded) until a 64-bit cell in global memory holds `tag`: how the CTAs of a grid learn that CTA 0
 // has zeroed the grid's work counters.  The tag is unique per launch (next_launch_tag), so whatever an

@@ -20,7 +20,6 @@
 // Tile order: the index of the row tiles runs fastest, so that all row tiles of one stretch of the vocabulary run side
 // by side and the weight is fetched from HBM once.
 #include <cuda_bf16.h>
-#include <cstdlib>
 #include <cstring>
 #include <math.h>
 
@@ -41,6 +40,8 @@ constexpr int kHeadMaxStages = 10;
 constexpr int kHeadRingBytes = 4 * (kTileABytes + kHeadN * kRowBytes);   // 192 KB
 constexpr int kHeadEpiWarps = 8;
 constexpr int kUnitSlots = 4;
+// the int8 epilogue converts and stores every element one by one: twice the warps
+__host__ __device__ constexpr int head_epi_warps(int mode) { return mode == kInt8Logits ? 16 : kHeadEpiWarps; }
 constexpr int kHeadThreads = (2 + kHeadEpiWarps) * 32;
 constexpr int kTurnPitch = 34;                   // bf16: 17 words, so that rows fall into different banks
 constexpr int kTurnBytes = 32 * kTurnPitch * 2;   // one warp's block
@@ -52,7 +53,7 @@ struct HeadParams {
     int box_n;                      // rows of a B box: n_tile, or less where the operand has less
     const int32_t* live;            // number of rows that count, NULL: all
     int32_t* dev_status;
-    void* out; long long out_stride; int out_bf16;                  // Int8Logits
+    void* out; long long out_stride; int out_bf16;                  // Int8Logits; out_bf16 2: pairs of entries may be stored
     const float* row_scale; const float* col_scale;
     float2* stats; long long stats_stride;                          // LossStats: [2 n_tiles][rows] (reference, sum)
     const int32_t* labels; float* z_label;
@@ -216,13 +217,13 @@ struct HeadShared {
 };
 
 template <int kCtas>
-__device__ __forceinline__ uint32_t head_setup(HeadShared& S, int stages, int warp)
+__device__ __forceinline__ uint32_t head_setup(HeadShared& S, int stages, int epi_warps, int warp)
 {
     if (threadIdx.x == 0) {
         for (int s = 0; s < stages; ++s) { mbar_init(&S.full[s], 1); mbar_init(&S.empty[s], 1); }
-        for (int s = 0; s < 2; ++s) { mbar_init(&S.acc_full[s], 1); mbar_init(&S.acc_empty[s], kCtas * kHeadEpiWarps); }
+        for (int s = 0; s < 2; ++s) { mbar_init(&S.acc_full[s], 1); mbar_init(&S.acc_empty[s], kCtas * epi_warps); }
         // read by: the issuer, the epilogue warps, the other CTA's producer
-        for (int s = 0; s < kUnitSlots; ++s) { mbar_init(&S.unit_full[s], 1); mbar_init(&S.unit_empty[s], kCtas * (1 + kHeadEpiWarps)); }
+        for (int s = 0; s < kUnitSlots; ++s) { mbar_init(&S.unit_full[s], 1); mbar_init(&S.unit_empty[s], kCtas * (1 + epi_warps)); }
         mbar_init(&S.mma_done, 1);
         S.abort = 0;
         mbar_fence_init();
@@ -283,17 +284,19 @@ __device__ __forceinline__ uint32_t head_idesc(bool int8, bool a_mn, bool b_mn, 
 
 // ---- logits and softmax statistics ----------------------------------------------------------------------
 template <int kMode, int kCtas>
-__global__ void __launch_bounds__(kHeadThreads, 1)
+__global__ void __launch_bounds__((2 + head_epi_warps(kMode)) * 32, 1)
 lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b)
 {
     constexpr bool kInt8 = kMode == kInt8Logits;
     constexpr int kBlockK = kInt8 ? 128 : 64, kM = kCtas * kHeadM;
+    constexpr int kParts = head_epi_warps(kMode) / 4;       // warps per lane quarter
+    constexpr int kMaxChunks = kHeadN / 32 / kParts;        // groups of 32 columns of one warp
 
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);   // swizzle atoms: 1 KB
     __shared__ HeadShared S;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t tmem = head_setup<kCtas>(S, P.stages, warp), rank = pair_rank<kCtas>();
+    const uint32_t tmem = head_setup<kCtas>(S, P.stages, head_epi_warps(kMode), warp), rank = pair_rank<kCtas>();
     volatile int* abort_flag = &S.abort;
     auto give_up = [&]() { atomicOr(P.dev_status, DSPARK_DEV_TIMEOUT); *abort_flag = 1; };
 
@@ -336,6 +339,10 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
                     if (++s == P.stages) { s = 0; ph ^= 1u; }
                 }
             }
+            for (int i = 0; i < P.stages && !*abort_flag; ++i) {   // the last announcements of free stages have arrived
+                if (!mbar_wait_bounded(&S.empty[s], ph ^ 1u)) break;
+                if (++s == P.stages) { s = 0; ph ^= 1u; }
+            }
             if (*abort_flag) head_drain(S, P.stages, issued, rank == 0);
         }
     } else if (warp == 1) {
@@ -369,43 +376,76 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
         }
     } else {
         // ---------------- epilogue -----------------------------------------------------------------------
-        const int q = warp & 3, half = (warp - 2) >> 2;
+        const int q = warp & 3, part = (warp - 2) >> 2;
         const uint32_t lane_base = (uint32_t)(q * 32) << 16;
         const int chunks = P.n_tile / 32;
+        float* scales = (float*)(smem + kHeadRingBytes) + (warp - 2) * kMaxChunks * 32;
         int t = 0;
         for (int u = first; u < n_units && !*abort_flag; u += step, ++t) {
             int m0, nt;
             tile(u, m0, nt);
             const uint32_t acc = (uint32_t)(t & 1), aph = (uint32_t)(t >> 1) & 1u;
+            const int row0 = m0 + (int)rank * kHeadM + q * 32, row = row0 + lane, n0 = nt * P.n_tile;
+            const bool in = row < m;
+            // what the tile needs besides the accumulator, asked for while it is being computed
+            float sw = 0.f;
+            int label = -1;
+            if (kInt8) {
+                if (in) sw = P.col_scale[row];
+                __syncwarp();                               // the scales of the tile before have been read
+#pragma unroll
+                for (int j = 0; j < kMaxChunks; ++j) {
+                    const int c = part + j * kParts, col = n0 + c * 32 + lane;
+                    scales[j * 32 + lane] = c < chunks && col < n ? P.row_scale[col] : 0.f;
+                }
+                __syncwarp();
+            } else if (in) {
+                label = P.labels[row];
+            }
             if (!__all_sync(0xffffffffu, mbar_wait_bounded(&S.acc_full[acc], aph))) {
                 if (lane == 0) give_up();
                 break;
             }
             tc_fence_after();
             const uint32_t acc_addr = tmem + lane_base + acc * kHeadN;
-            const int row0 = m0 + (int)rank * kHeadM + q * 32, row = row0 + lane, n0 = nt * P.n_tile;
-            const bool in = row < m;
             if (row0 < m) {
                 if (kInt8) {
-                    const float sw = in ? P.col_scale[row] : 0.f;
-                    for (int c = half; c < chunks; c += 2) {
+                    for (int c = part; c < chunks; c += kParts) {
                         const int col0 = n0 + c * 32;
                         if (col0 >= n) break;
-                        const float sx = col0 + lane < n ? P.row_scale[col0 + lane] : 0.f;
+                        const float* chunk_scales = scales + (c - part) / kParts * 32;
                         float v[32];
                         __syncwarp();
                         tmem_load32(acc_addr + (uint32_t)(c * 32), v);
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] = (float)__float_as_int(v[i]) * __shfl_sync(0xffffffffu, sx, i) * sw;
-                        // lanes are neighbouring vocabulary entries: a warp stores 32 neighbours of one row at a time
-                        const int valid = in ? n - col0 : 0;
-                        if (P.out_bf16) store_column32((__nv_bfloat16*)P.out + (long long)col0 * P.out_stride + row, P.out_stride, v, valid);
-                        else store_column32((float*)P.out + (long long)col0 * P.out_stride + row, P.out_stride, v, valid);
+                        for (int i = 0; i < 32; i += 4) {
+                            const float4 sx = *reinterpret_cast<const float4*>(chunk_scales + i);
+                            v[i] = (float)__float_as_int(v[i]) * sx.x * sw;
+                            v[i + 1] = (float)__float_as_int(v[i + 1]) * sx.y * sw;
+                            v[i + 2] = (float)__float_as_int(v[i + 2]) * sx.z * sw;
+                            v[i + 3] = (float)__float_as_int(v[i + 3]) * sx.w * sw;
+                        }
+                        // lanes are neighbouring vocabulary entries: a warp stores 32 neighbours of one row at a time, or,
+                        // bf16 rows that pairs of entries may be stored to, 32 neighbours of two rows
+                        if (P.out_bf16 == 2 && row0 + 32 <= m) {
+                            __nv_bfloat16* p = (__nv_bfloat16*)P.out + (long long)(col0 + (lane & 1)) * P.out_stride + (row & ~1);
+                            const int valid = n - col0 - (lane & 1);
+#pragma unroll
+                            for (int i = 0; i < 32; i += 2) {
+                                const float other = __shfl_xor_sync(0xffffffffu, (lane & 1) ? v[i] : v[i + 1], 1);
+                                const uint32_t w = (lane & 1) ? bf16_pair(other, v[i + 1]) : bf16_pair(v[i], other);
+                                if (i < valid) *reinterpret_cast<uint32_t*>(p) = w;
+                                p += 2 * P.out_stride;
+                            }
+                        } else {
+                            const int valid = in ? n - col0 : 0;
+                            if (P.out_bf16) store_column32((__nv_bfloat16*)P.out + (long long)col0 * P.out_stride + row, P.out_stride, v, valid);
+                            else store_column32((float*)P.out + (long long)col0 * P.out_stride + row, P.out_stride, v, valid);
+                        }
                     }
                 } else {
-                    const int label = in ? P.labels[row] : -1;
                     float ref = -INFINITY, sum = 0.f;
-                    for (int c = half; c < chunks; c += 2) {
+                    for (int c = part; c < chunks; c += kParts) {
                         const int col0 = n0 + c * 32;
                         if (col0 >= n) break;
                         float z[32];
@@ -444,7 +484,7 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
                         sum += s0 + s1;
                         ref = now;
                     }
-                    if (in) P.stats[(size_t)(nt * 2 + half) * P.stats_stride + row] = make_float2(ref, sum);
+                    if (in) P.stats[(size_t)(nt * kParts + part) * P.stats_stride + row] = make_float2(ref, sum);
                 }
             }
             tc_fence_before();
@@ -517,10 +557,11 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     __shared__ HeadShared S;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t tmem = head_setup<kCtas>(S, kStages, warp), rank = pair_rank<kCtas>();
+    const uint32_t tmem = head_setup<kCtas>(S, kStages, kHeadEpiWarps, warp), rank = pair_rank<kCtas>();
     volatile int* abort_flag = &S.abort;
     auto give_up = [&]() { atomicOr(P.dev_status, DSPARK_DEV_TIMEOUT); *abort_flag = 1; };
 
+    if (P.want_h) pdl_trigger();                            // the sum of the slices is the next launch, and ours
     const int live = *P.live;
     const int m_tiles = (live + kM - 1) / kM;
 
@@ -647,6 +688,10 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
                 }
                 if (*abort_flag) break;
             }
+            for (int i = 0; i < kStages && !*abort_flag; ++i) {   // the last announcements of free stages have arrived
+                if (!mbar_wait_bounded(&S.empty[s], ph ^ 1u)) break;
+                if (++s == kStages) { s = 0; ph ^= 1u; }
+            }
             if (*abort_flag) head_drain(S, kStages, issued, rank == 0);
         }
     } else if (warp == 1) {
@@ -711,6 +756,10 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
             const bool any = u0.w < u1.x;
             if (kind == kEnd) break;
             const uint32_t acc = (uint32_t)(t & 1), aph = (uint32_t)(t >> 1) & 1u;
+            const int row = row0 + lane;
+            int label = -1;
+            float lse2 = 0.f, g = 0.f;
+            if (kind == kLossGrad && row < live) { label = P.labels[row]; lse2 = P.lse2[row]; g = P.grad[row]; }
             if (any) {
                 if (!__all_sync(0xffffffffu, mbar_wait_bounded(&S.acc_full[acc], aph))) {
                     if (lane == 0) give_up();
@@ -720,7 +769,6 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
                 ++t;
             }
             const uint32_t acc_addr = tmem + lane_base + acc * kHeadN;
-            const int row = row0 + lane;
             auto load = [&](int c, float (&v)[32]) {
                 __syncwarp();
                 if (any) tmem_load32(acc_addr + (uint32_t)(c * 32), v);
@@ -733,8 +781,7 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
                 // rows past the last one that counts are written as zeros: the product over rows reads them
                 const bool in = row < live;
                 const int v0 = p * P.piece;
-                const int label = in ? P.labels[row] - v0 : -1;
-                const float lse2 = in ? P.lse2[row] : 0.f, g = in ? P.grad[row] : 0.f;
+                label -= v0;
                 __nv_bfloat16* out = P.G + ((long long)(p % 3) * P.n_pad + row) * P.piece;
                 for (int c = half; c < kHeadN / 32; c += 2) {
                     const int col0 = n0 + c * 32;
@@ -800,7 +847,9 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
             __syncwarp();
             if (lane == 0) {
                 if (any) pair_arrive<kCtas>(&S.acc_empty[acc], 0);
-                __threadfence();
+                // Nobody in this launch reads dW: what is counted for it is that G has been read.  (The fence waits for the
+                // stores: a microsecond or two, as long as a short unit's products take.)
+                if (kind != kGradWeight) __threadfence();
                 atomicAdd(P.sync + 1 + 3 * p + kind, 1);
             }
         }
@@ -834,6 +883,7 @@ __global__ void __launch_bounds__(kGatherThreads) lm_head_gather_kernel(const __
     __shared__ int s_count[kGatherThreads / 32];
     __shared__ int s_slot[kGatherRows];
     pdl_wait();
+    pdl_trigger();                                          // the contraction may set up its barriers and tensor memory
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int r0 = blockIdx.x * kGatherRows;
     for (int i = blockIdx.x * kGatherThreads + tid; i < P.n_sync; i += gridDim.x * kGatherThreads) P.sync[i] = 0;
@@ -960,22 +1010,28 @@ struct HiddenParams {
     int d;
     __nv_bfloat16* dh; long long dh_stride;
 };
-__global__ void __launch_bounds__(256) lm_head_grad_hidden_kernel(const __grid_constant__ HiddenParams P)
+constexpr int kHiddenThreads = 128;               // four columns each
+__global__ void __launch_bounds__(kHiddenThreads) lm_head_grad_hidden_kernel(const __grid_constant__ HiddenParams P)
 {
     pdl_wait();
     const int row = blockIdx.x;
     if (row >= *P.live) return;
-    const float err = P.label_err[row];
-    const __nv_bfloat16* w = P.w + (long long)P.label[row] * P.w_stride;
-    __nv_bfloat16* out = P.dh + (long long)P.idx[row] * P.dh_stride;
-    for (int c = threadIdx.x; c < P.d; c += 256) {
-        float sum = err * __bfloat162float(w[c]);
-        const float* part = P.part + (long long)row * P.part_stride + c;
-        const long long step = (long long)P.m * P.part_stride;
-#pragma unroll 8
-        for (int s = 0; s < P.slices; ++s) sum += part[s * step];
-        out[c] = __float2bfloat16_rn(sum);
+    const int c = (int)(blockIdx.y * kHiddenThreads + threadIdx.x) * 4;
+    if (c >= P.d) return;
+    const float* part = P.part + (long long)row * P.part_stride + c;       // the pitch is a multiple of 8
+    const long long step = (long long)P.m * P.part_stride;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 16
+    for (int s = 0; s < P.slices; ++s) {
+        const float4 v = *reinterpret_cast<const float4*>(part + s * step);
+        sum[0] += v.x; sum[1] += v.y; sum[2] += v.z; sum[3] += v.w;
     }
+    const float err = P.label_err[row];
+    const __nv_bfloat16* w = P.w + (long long)P.label[row] * P.w_stride + c;
+    __nv_bfloat16* out = P.dh + (long long)P.idx[row] * P.dh_stride + c;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (c + i < P.d) out[i] = __float2bfloat16_rn(fmaf(err, __bfloat162float(w[i]), sum[i]));
 }
 
 // ---- int8 weights ------------------------------------------------------------------------------------------
@@ -1068,11 +1124,11 @@ static bool allow_smem(Kernel kernel, int bytes, std::atomic<unsigned long long>
 
 // launch_pdl with clusters of kCtas CTAs
 template <int kCtas, typename... KArgs, typename... Args>
-static void launch_pairs(void (*kernel)(KArgs...), int ctas, size_t smem, cudaStream_t stream, Args... args)
+static void launch_pairs(void (*kernel)(KArgs...), int ctas, int threads, size_t smem, cudaStream_t stream, Args... args)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)ctas);
-    cfg.blockDim = dim3(kHeadThreads);
+    cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
@@ -1088,7 +1144,7 @@ static void launch_pairs(void (*kernel)(KArgs...), int ctas, size_t smem, cudaSt
 template <int kMode, int kCtas>
 static int head_launch(HeadParams P, const CUtensorMap& a, const CUtensorMap& b, cudaStream_t s, int timer_id)
 {
-    constexpr int kSmem = kHeadRingBytes + 1024;
+    constexpr int kSmem = kHeadRingBytes + 1024 + (kMode == kInt8Logits ? kHeadN * 16 : 0);   // four lane quarters x 256 scales
     static std::atomic<unsigned long long> ready{0};
     if (!allow_smem(lm_head_kernel<kMode, kCtas>, kSmem, ready)) return launch_status();
     P.stages = kHeadRingBytes / (kTileABytes + P.n_tile / kCtas * kRowBytes);
@@ -1096,7 +1152,7 @@ static int head_launch(HeadParams P, const CUtensorMap& a, const CUtensorMap& b,
     const long long units = (long long)((P.m + kCtas * kHeadM - 1) / (kCtas * kHeadM)) * ((P.n + P.n_tile - 1) / P.n_tile);
     const int groups = device_sms() / kCtas;
     KernelTimerScope timer(timer_id, s);
-    launch_pairs<kCtas>(lm_head_kernel<kMode, kCtas>, kCtas * (int)(units < groups ? units : groups), kSmem, s, P, a, b);
+    launch_pairs<kCtas>(lm_head_kernel<kMode, kCtas>, kCtas * (int)(units < groups ? units : groups), (2 + head_epi_warps(kMode)) * 32, kSmem, s, P, a, b);
     return launch_status();
 }
 
@@ -1107,12 +1163,12 @@ static int back_launch(const BackParams& P, const BackMaps& M, cudaStream_t s)
     static std::atomic<unsigned long long> ready{0};
     if (!allow_smem(lm_head_backward_kernel<kCtas>, kSmem, ready)) return launch_status();
     KernelTimerScope timer(DSPARK_K_HEAD_GRAD, s);
-    launch_pairs<kCtas>(lm_head_backward_kernel<kCtas>, device_sms() / kCtas * kCtas, kSmem, s, P, M);
+    launch_pairs<kCtas>(lm_head_backward_kernel<kCtas>, device_sms() / kCtas * kCtas, kHeadThreads, kSmem, s, P, M);
     return launch_status();
 }
 
 constexpr int kMaxRows = 1 << 20, kMaxVocab = 1 << 24, kMaxWidth = 1 << 16;
-static long long kPieceBytes = getenv("PIECE") ? atoll(getenv("PIECE")) << 20 : 32ll << 20;
+constexpr long long kPieceBytes = 32ll << 20;
 
 struct LossWs {
     size_t live, sync, idx, label, z_label, lse2, grad, label_err, rows, stats, G, part, total;
@@ -1123,17 +1179,20 @@ static LossWs loss_layout(int N, int V, int d)
 {
     LossWs w;
     w.ctas = N > kHeadM ? 2 : 1;                            // one row tile of 128 rows: the second CTA of a pair would hold none
-    if (getenv("CTAS")) w.ctas = atoi(getenv("CTAS"));
     w.n_pad = (long long)up((size_t)N, w.ctas * kHeadM);
     w.d_pitch = (long long)up((size_t)d, 64);               // whole blocks of columns (block_map)
     w.part_pitch = (long long)up((size_t)d, 8);
     w.n_tile_d = d >= kHeadN ? kHeadN : (int)up((size_t)d, 64 * w.ctas);
     w.d_tiles = (d + w.n_tile_d - 1) / w.n_tile_d;
-    // A piece of the vocabulary is such that neither its rows of W nor its columns of G take more than kPieceBytes, and not
-    // narrower than 2 048 entries, below which adding the partial sums of dH would cost more than the products.
-    const long long widest = w.n_pad > d ? w.n_pad : d;
+    // A piece of the vocabulary: at most 32 MB of G and 128 MB of W, so that the three pieces of G stay in or near the L2
+    // and few rows (G small) do not make pieces whose phases are shorter than the waits between them; not narrower than
+    // 2 048 entries, below which adding the partial sums of dH would cost more than the products.  Measured with 16 / 32 /
+    // 64 MB: 128 rows, d 1024 221 / 206 / 205 us; 1000 rows, d 1024 727 / 681 / 662; 2867 rows, d 2048 3465 / 3436 / 3304
+    // (twice the workspace); 600 rows, V 40 000, d 300 174 / 154 / 166.
     const long long all = (long long)up((size_t)V, kHeadN);
-    long long piece = kPieceBytes / (2 * widest) / kHeadN * kHeadN;
+    long long piece = kPieceBytes / (2 * w.n_pad) / kHeadN * kHeadN;
+    const long long by_w = 4 * kPieceBytes / (2 * d) / kHeadN * kHeadN;
+    if (piece > by_w) piece = by_w;
     if (piece < 2048) piece = 2048;
     if (piece > all) piece = all;
     w.piece = (int)piece;
@@ -1212,10 +1271,12 @@ int dspark_lm_head_int8(const int8_t* x_q, int64_t x_row_stride, const float* x_
     // engine more than one that does not (one row of 32: 170 us instead of 90 at V = 129 280, K = 4 096)
     const int row_tiles = (rows + kHeadN - 1) / kHeadN;
     P.n_tile = (int)up((size_t)((rows + row_tiles - 1) / row_tiles), 32);
-    const int ctas = getenv("CTAS") ? atoi(getenv("CTAS")) : 2, part = P.n_tile / ctas;
+    // Pairs where the products bound the call, single CTAs where the weight's bytes or the stores do (V = 129 280, single /
+    // pair: 256 rows K 1024 43 / 46 us, 512 rows K 1024 74 / 75, 256 rows K 2048 71 / 67, 1482 rows K 4096 597 / 558).
+    const int ctas = rows > kHeadM && (long long)rows * K >= 1ll << 19 ? 2 : 1, part = P.n_tile / ctas;
     P.box_n = rows < part ? rows : part;
     P.live = n_live; P.dev_status = dev_status;
-    P.out = out_logits; P.out_stride = out_row_stride; P.out_bf16 = out_dtype == DSPARK_BF16;
+    P.out = out_logits; P.out_stride = out_row_stride; P.out_bf16 = out_dtype != DSPARK_BF16 ? 0 : (((uintptr_t)out_logits & 3u) == 0 && (out_row_stride & 1) == 0) ? 2 : 1;
     P.row_scale = x_scale; P.col_scale = w_scale;
     CUtensorMap a, b;
     if (!operand_map(&a, w_q, 1, V, K, w_row_stride, kRowBytes, kHeadM) || !operand_map(&b, x_q, 1, rows, K, x_row_stride, kRowBytes, P.box_n))
@@ -1333,7 +1394,7 @@ int dspark_lm_head_loss_backward(const void* hidden, int64_t hidden_row_stride, 
         Hp.w = (const __nv_bfloat16*)weight; Hp.w_stride = weight_row_stride; Hp.d = d;
         Hp.dh = g.dh; Hp.dh_stride = grad_hidden_row_stride;
         KernelTimerScope timer(DSPARK_K_HEAD_ROWS, s);
-        launch_pdl(lm_head_grad_hidden_kernel, dim3(N), dim3(256), 0, s, Hp);
+        launch_pdl(lm_head_grad_hidden_kernel, dim3(N, (d + 4 * kHiddenThreads - 1) / (4 * kHiddenThreads)), dim3(kHiddenThreads), 0, s, Hp);
     }
     return launch_status();
 }

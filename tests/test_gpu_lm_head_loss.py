@@ -207,6 +207,13 @@ def test_several_pieces_of_the_vocabulary():
     check(h, w, labels, gl)
 
 
+@pytest.mark.parametrize("N,V,d", [(20000, 12001, 64), (100, 70000, 4096), (1500, 60001, 72)])
+def test_many_pieces(N, V, d):
+    # six, five and six pieces: the fourth overwrites the first one's G; with pairs of CTAs and without
+    h, w, labels, gl = make(N, V, d, 18, ignored=0.1)
+    check(h, w, labels, gl)
+
+
 def test_full_vocabulary():
     h, w, labels, gl = make(70, 129280, 256, 17)
     check(h, w, labels, gl)
