@@ -194,16 +194,31 @@ __device__ __forceinline__ void store_block32(__nv_bfloat16* p, long long stride
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
-// One element to each of the first `n` of 32 rows.
+// One element to each of 16 rows from `row` on, the first `n` of which exist.
 template <typename T>
-__device__ __forceinline__ void store_column32(T* p, long long stride, const float (&v)[32], int n)
+__device__ __forceinline__ void store_column16(T* p, long long stride, int row, int n, const float* v)
 {
-    if (n >= 32) {
+    p += row * stride;
+    if (n >= 16) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) { put(p, v[i]); p += stride; }
-    } else {
+        for (int i = 0; i < 16; ++i) { put(p, v[i]); p += stride; }
+    } else if (n > 0) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) { if (i < n) put(p, v[i]); p += stride; }
+        for (int i = 0; i < 16; ++i) { if (i < n) put(p, v[i]); p += stride; }
+    }
+}
+// The same for bf16 in pairs: even lanes store the even rows' entries (their own and the next lane's), odd lanes the odd
+// rows'.  p: the pair's first entry in row 0.
+__device__ __forceinline__ void store_pairs16(__nv_bfloat16* p, long long stride, int row, int n, const float* v, int lane)
+{
+    const int odd = lane & 1;
+    p += (row + odd) * stride;
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+        const float other = __shfl_xor_sync(0xffffffffu, odd ? v[i] : v[i + 1], 1);
+        const uint32_t w = odd ? bf16_pair(other, v[i + 1]) : bf16_pair(v[i], other);
+        if (i + odd < n) *reinterpret_cast<uint32_t*>(p) = w;
+        p += 2 * stride;
     }
 }
 
@@ -316,7 +331,14 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
         if (kInt8) { nt = u % n_tiles; m0 = u / n_tiles * kM; }
         else { m0 = u % m_tiles * kM; nt = u / m_tiles; }
     };
-    const int stage_bytes = kTileABytes + P.n_tile / kCtas * kRowBytes;
+    const int share = P.n_tile / kCtas;                     // B rows of one CTA
+    // First B row of a CTA.  Int8Logits: a box that would reach past the last row is moved back -- the copy engine takes
+    // some 24 clocks for each row outside, more than the products leave it -- and a few rows are computed twice.
+    auto b_start = [&](int nt, int r) {
+        const int at = nt * P.n_tile + r * share;
+        return kInt8 ? (at < P.n - P.box_n ? at : P.n - P.box_n) : at;
+    };
+    const int stage_bytes = kTileABytes + share * kRowBytes;
     const uint32_t load_bytes = (uint32_t)(kCtas * (kTileABytes + P.box_n * kRowBytes));
     const int first = (int)blockIdx.x / kCtas, step = (int)gridDim.x / kCtas;
 
@@ -334,7 +356,7 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
                     unsigned char* a = smem + (size_t)s * stage_bytes;
                     if (rank == 0) mbar_arrive_expect_tx(&S.full[s], load_bytes);
                     pair_load_2d<kCtas>(a, &map_a, kb * kBlockK, m0 + (int)rank * kHeadM, &S.full[s], pol);
-                    pair_load_2d<kCtas>(a + kTileABytes, &map_b, kb * kBlockK, nt * P.n_tile + (int)rank * (P.n_tile / kCtas), &S.full[s], pol);
+                    pair_load_2d<kCtas>(a + kTileABytes, &map_b, kb * kBlockK, b_start(nt, (int)rank), &S.full[s], pol);
                     ++issued;
                     if (++s == P.stages) { s = 0; ph ^= 1u; }
                 }
@@ -378,7 +400,7 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
         // ---------------- epilogue -----------------------------------------------------------------------
         const int q = warp & 3, part = (warp - 2) >> 2;
         const uint32_t lane_base = (uint32_t)(q * 32) << 16;
-        const int chunks = P.n_tile / 32;
+        const int chunks = (P.n_tile + 31) / 32;
         float* scales = (float*)(smem + kHeadRingBytes) + (warp - 2) * kMaxChunks * 32;
         int t = 0;
         for (int u = first; u < n_units && !*abort_flag; u += step, ++t) {
@@ -387,6 +409,12 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
             const uint32_t acc = (uint32_t)(t & 1), aph = (uint32_t)(t >> 1) & 1u;
             const int row0 = m0 + (int)rank * kHeadM + q * 32, row = row0 + lane, n0 = nt * P.n_tile;
             const bool in = row < m;
+            // Int8Logits: the row of the batch that a column of the accumulator is (past the last one: none)
+            const int start0 = b_start(nt, 0), start1 = kCtas == 2 ? b_start(nt, 1) : 0;
+            auto row_of = [&](int col) {
+                if (col >= P.n_tile) return 1 << 30;
+                return kCtas == 2 && col >= share ? start1 + col - share : start0 + col;
+            };
             // what the tile needs besides the accumulator, asked for while it is being computed
             float sw = 0.f;
             int label = -1;
@@ -395,8 +423,8 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
                 __syncwarp();                               // the scales of the tile before have been read
 #pragma unroll
                 for (int j = 0; j < kMaxChunks; ++j) {
-                    const int c = part + j * kParts, col = n0 + c * 32 + lane;
-                    scales[j * 32 + lane] = c < chunks && col < n ? P.row_scale[col] : 0.f;
+                    const int r = row_of((part + j * kParts) * 32 + lane);
+                    scales[j * 32 + lane] = r < n ? P.row_scale[r] : 0.f;
                 }
                 __syncwarp();
             } else if (in) {
@@ -411,8 +439,9 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
             if (row0 < m) {
                 if (kInt8) {
                     for (int c = part; c < chunks; c += kParts) {
-                        const int col0 = n0 + c * 32;
-                        if (col0 >= n) break;
+                        // a CTA's share is a multiple of 16 rows: the 32 columns are two runs of 16 neighbouring rows
+                        const int r0 = row_of(c * 32), r1 = row_of(c * 32 + 16);
+                        if (r0 >= n && r1 >= n) continue;
                         const float* chunk_scales = scales + (c - part) / kParts * 32;
                         float v[32];
                         __syncwarp();
@@ -428,19 +457,14 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
                         // lanes are neighbouring vocabulary entries: a warp stores 32 neighbours of one row at a time, or,
                         // bf16 rows that pairs of entries may be stored to, 32 neighbours of two rows
                         if (P.out_bf16 == 2 && row0 + 32 <= m) {
-                            __nv_bfloat16* p = (__nv_bfloat16*)P.out + (long long)(col0 + (lane & 1)) * P.out_stride + (row & ~1);
-                            const int valid = n - col0 - (lane & 1);
-#pragma unroll
-                            for (int i = 0; i < 32; i += 2) {
-                                const float other = __shfl_xor_sync(0xffffffffu, (lane & 1) ? v[i] : v[i + 1], 1);
-                                const uint32_t w = (lane & 1) ? bf16_pair(other, v[i + 1]) : bf16_pair(v[i], other);
-                                if (i < valid) *reinterpret_cast<uint32_t*>(p) = w;
-                                p += 2 * P.out_stride;
-                            }
+                            store_pairs16((__nv_bfloat16*)P.out + (row & ~1), P.out_stride, r0, n - r0, v, lane);
+                            store_pairs16((__nv_bfloat16*)P.out + (row & ~1), P.out_stride, r1, n - r1, v + 16, lane);
+                        } else if (P.out_bf16) {
+                            store_column16((__nv_bfloat16*)P.out + row, P.out_stride, r0, in ? n - r0 : 0, v);
+                            store_column16((__nv_bfloat16*)P.out + row, P.out_stride, r1, in ? n - r1 : 0, v + 16);
                         } else {
-                            const int valid = in ? n - col0 : 0;
-                            if (P.out_bf16) store_column32((__nv_bfloat16*)P.out + (long long)col0 * P.out_stride + row, P.out_stride, v, valid);
-                            else store_column32((float*)P.out + (long long)col0 * P.out_stride + row, P.out_stride, v, valid);
+                            store_column16((float*)P.out + row, P.out_stride, r0, in ? n - r0 : 0, v);
+                            store_column16((float*)P.out + row, P.out_stride, r1, in ? n - r1 : 0, v + 16);
                         }
                     }
                 } else {
@@ -1267,14 +1291,14 @@ int dspark_lm_head_int8(const int8_t* x_q, int64_t x_row_stride, const float* x_
     HeadParams P;
     memset(&P, 0, sizeof P);
     P.m = V; P.n = rows; P.k = K;
-    // row tiles of one size, and no taller a box than there are rows: a box that reaches past the last row costs the copy
-    // engine more than one that does not (one row of 32: 170 us instead of 90 at V = 129 280, K = 4 096)
-    const int row_tiles = (rows + kHeadN - 1) / kHeadN;
-    P.n_tile = (int)up((size_t)((rows + row_tiles - 1) / row_tiles), 32);
     // Pairs where the products bound the call, single CTAs where the weight's bytes or the stores do (V = 129 280, single /
     // pair: 256 rows K 1024 43 / 46 us, 512 rows K 1024 74 / 75, 256 rows K 2048 71 / 67, 1482 rows K 4096 597 / 558).
-    const int ctas = rows > kHeadM && (long long)rows * K >= 1ll << 19 ? 2 : 1, part = P.n_tile / ctas;
-    P.box_n = rows < part ? rows : part;
+    const int ctas = rows > kHeadM && (long long)rows * K >= 1ll << 19 ? 2 : 1;
+    // row tiles of one size, and no taller a box than there are rows (one row of 32 in a box: 170 us instead of 84 at
+    // K = 4 096)
+    const int row_tiles = (rows + kHeadN - 1) / kHeadN;
+    P.n_tile = (int)up((size_t)((rows + row_tiles - 1) / row_tiles), 16 * ctas);
+    P.box_n = rows < P.n_tile / ctas ? rows : P.n_tile / ctas;
     P.live = n_live; P.dev_status = dev_status;
     P.out = out_logits; P.out_stride = out_row_stride; P.out_bf16 = out_dtype != DSPARK_BF16 ? 0 : (((uintptr_t)out_logits & 3u) == 0 && (out_row_stride & 1) == 0) ? 2 : 1;
     P.row_scale = x_scale; P.col_scale = w_scale;

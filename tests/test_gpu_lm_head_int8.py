@@ -49,6 +49,16 @@ def test_rows_behind_the_last_one_are_left(live):
     check(*operands(300, 700, 200, 3), torch.bfloat16, live=live)
 
 
+@pytest.mark.parametrize("n", [2, 17, 130, 200, 257, 300, 352, 511, 513, 700])
+@pytest.mark.parametrize("K", [512, 4096])
+def test_row_tiles_that_are_moved_back(n, K):
+    # single CTAs and pairs; tiles whose boxes would reach past the last row; with and without a smaller live count
+    ops = operands(n, 390, K, n + K)
+    for live in (None, n - 1, n // 2 + 1):
+        check(*ops, torch.bfloat16, live=live)
+        check(*ops, torch.float32, live=live, out_pad=1)
+
+
 def test_row_pitches_offsets_and_odd_strides():
     ops = operands(70, 333, 100, 4, pad=True)
     for pad, off in ((0, 0), (1, 0), (0, 1), (5, 3)):
