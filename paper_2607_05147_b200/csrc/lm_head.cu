@@ -167,16 +167,22 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b)
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// 32 consecutive bf16 of this lane's row (p 32-byte aligned): two whole sectors
+// 32 consecutive bf16 of this lane's row (p 32-byte aligned): two whole sectors.  kOnce: nobody reads them soon
+template <bool kOnce>
 __device__ __forceinline__ void store_row32(__nv_bfloat16* p, const float (&v)[32])
 {
+#define DSPARK_STORE8(HINT)                                                                                                            \
+    asm volatile("st.global" HINT ".v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"                                                         \
+                 ::"l"(p + i), "r"(bf16_pair(v[i], v[i + 1])), "r"(bf16_pair(v[i + 2], v[i + 3])), "r"(bf16_pair(v[i + 4], v[i + 5])), \
+                   "r"(bf16_pair(v[i + 6], v[i + 7])), "r"(bf16_pair(v[i + 8], v[i + 9])), "r"(bf16_pair(v[i + 10], v[i + 11])),       \
+                   "r"(bf16_pair(v[i + 12], v[i + 13])), "r"(bf16_pair(v[i + 14], v[i + 15]))                                          \
+                 : "memory")
 #pragma unroll
-    for (int i = 0; i < 32; i += 16)
-        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
-                     ::"l"(p + i), "r"(bf16_pair(v[i], v[i + 1])), "r"(bf16_pair(v[i + 2], v[i + 3])), "r"(bf16_pair(v[i + 4], v[i + 5])),
-                       "r"(bf16_pair(v[i + 6], v[i + 7])), "r"(bf16_pair(v[i + 8], v[i + 9])), "r"(bf16_pair(v[i + 10], v[i + 11])),
-                       "r"(bf16_pair(v[i + 12], v[i + 13])), "r"(bf16_pair(v[i + 14], v[i + 15]))
-                     : "memory");
+    for (int i = 0; i < 32; i += 16) {
+        if (kOnce) DSPARK_STORE8(".L2::evict_first");
+        else DSPARK_STORE8("");
+    }
+#undef DSPARK_STORE8
 }
 // The same for rows that are not aligned or end inside: the 32 x 32 block of the warp is turned in shared memory (an odd
 // pitch of 17 words), so that 32 lanes store neighbours of one row.  `rows` and `n`: rows and columns that exist.
@@ -592,7 +598,9 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
     if (warp == 0) {
         // ---------------- producer: units, then operand tiles ----------------------------------------------
         if (lane == 0) {
-            const uint64_t pol = l2_policy_evict_normal();
+            // W is read for G and, a phase later, for dH, and then no more: kept until then (dW is stored past it); 128 rows,
+            // d 1024 205 -> 199 us
+            const uint64_t pol = l2_policy_evict_normal(), pol_keep = l2_policy_evict_last(), pol_done = l2_policy_evict_first();
             const int last = P.V - (P.pieces - 1) * P.piece;               // entries of the last piece
             const int row_blocks = (live + 63) / 64;
             auto here = [&](int p) { return p == P.pieces - 1 ? last : P.piece; };
@@ -695,13 +703,13 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
                     const int kx = kb * 64, mr = m0 + (int)rank * kHeadM;
                     if (kind == kLossGrad) {
                         pair_load_2d<kCtas>(a, &M.rows_k, kx, mr, bar, pol);
-                        pair_load_2d<kCtas>(b, &M.w_k, kx, v0 + n0 + (int)rank * (kHeadN / kCtas), bar, pol);
+                        pair_load_2d<kCtas>(b, &M.w_k, kx, v0 + n0 + (int)rank * (kHeadN / kCtas), bar, pol_keep);
                     } else {
                         const int nr = n0 + (int)rank * half_d;
                         if (kind == kGradHidden) {
                             pair_load_2d<kCtas>(a, &M.g_k, kx, g0 + mr, bar, pol);
-                            if (P.w_blocks) pair_load_3d<kCtas>(b, &M.w_mn, 0, v0 + kx, nr / 64, bar, pol);
-                            else for (int j = 0; j < half_d; j += 64) pair_load_2d<kCtas>(b + j * kRowBytes, &M.w_mn, nr + j, v0 + kx, bar, pol);
+                            if (P.w_blocks) pair_load_3d<kCtas>(b, &M.w_mn, 0, v0 + kx, nr / 64, bar, pol_done);
+                            else for (int j = 0; j < half_d; j += 64) pair_load_2d<kCtas>(b + j * kRowBytes, &M.w_mn, nr + j, v0 + kx, bar, pol_done);
                         } else {
                             pair_load_3d<kCtas>(a, &M.g_mn, 0, g0 + kx, mr / 64, bar, pol);
                             pair_load_3d<kCtas>(b, &M.rows_mn, 0, kx, nr / 64, bar, pol);
@@ -827,7 +835,7 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
                         for (int i = 0; i < 32; ++i)
                             if (i >= valid) z[i] = 0.f;
                     }
-                    store_row32(out + col0, z);
+                    store_row32<false>(out + col0, z);
                 }
             } else if (kind == kGradHidden) {
                 float* out = P.part + ((long long)u1.z * P.n_pad + row) * P.part_stride;
@@ -860,7 +868,7 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
                         float v[32];
                         load(c, v);
                         if (dw_vec && P.d - col0 >= 32) {
-                            if (lane < rows) store_row32(out + lane * P.dw_stride + col0, v);
+                            if (lane < rows) store_row32<true>(out + lane * P.dw_stride + col0, v);
                         } else {
                             store_block32(out + col0, P.dw_stride, v, rows, P.d - col0, turn, lane);
                         }
