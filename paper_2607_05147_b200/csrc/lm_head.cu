@@ -38,10 +38,8 @@ constexpr int kTileABytes = kHeadM * kRowBytes;   // 16 KB
 constexpr int kBoxMnBytes = 64 * kRowBytes;       // [64 k][64 mn] of bf16: 8 KB
 constexpr int kHeadMaxStages = 10;
 constexpr int kHeadRingBytes = 4 * (kTileABytes + kHeadN * kRowBytes);   // 192 KB
-constexpr int kHeadEpiWarps = 8;
+constexpr int kHeadEpiWarps = 8;                   // 16 take issue slots and polls from the issuer: backward 5 % slower, statistics 2 x
 constexpr int kUnitSlots = 4;
-// the int8 epilogue converts and stores every element one by one: twice the warps
-__host__ __device__ constexpr int head_epi_warps(int mode) { return mode == kInt8Logits ? 16 : kHeadEpiWarps; }
 constexpr int kHeadThreads = (2 + kHeadEpiWarps) * 32;
 constexpr int kTurnPitch = 34;                   // bf16: 17 words, so that rows fall into different banks
 constexpr int kTurnBytes = 32 * kTurnPitch * 2;   // one warp's block
@@ -238,13 +236,13 @@ struct HeadShared {
 };
 
 template <int kCtas>
-__device__ __forceinline__ uint32_t head_setup(HeadShared& S, int stages, int epi_warps, int warp)
+__device__ __forceinline__ uint32_t head_setup(HeadShared& S, int stages, int warp)
 {
     if (threadIdx.x == 0) {
         for (int s = 0; s < stages; ++s) { mbar_init(&S.full[s], 1); mbar_init(&S.empty[s], 1); }
-        for (int s = 0; s < 2; ++s) { mbar_init(&S.acc_full[s], 1); mbar_init(&S.acc_empty[s], kCtas * epi_warps); }
+        for (int s = 0; s < 2; ++s) { mbar_init(&S.acc_full[s], 1); mbar_init(&S.acc_empty[s], kCtas * kHeadEpiWarps); }
         // read by: the issuer, the epilogue warps, the other CTA's producer
-        for (int s = 0; s < kUnitSlots; ++s) { mbar_init(&S.unit_full[s], 1); mbar_init(&S.unit_empty[s], kCtas * (1 + epi_warps)); }
+        for (int s = 0; s < kUnitSlots; ++s) { mbar_init(&S.unit_full[s], 1); mbar_init(&S.unit_empty[s], kCtas * (1 + kHeadEpiWarps)); }
         mbar_init(&S.mma_done, 1);
         S.abort = 0;
         mbar_fence_init();
@@ -305,19 +303,20 @@ __device__ __forceinline__ uint32_t head_idesc(bool int8, bool a_mn, bool b_mn, 
 
 // ---- logits and softmax statistics ----------------------------------------------------------------------
 template <int kMode, int kCtas>
-__global__ void __launch_bounds__((2 + head_epi_warps(kMode)) * 32, 1)
+__global__ void __launch_bounds__(kHeadThreads, 1)
 lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b)
 {
     constexpr bool kInt8 = kMode == kInt8Logits;
     constexpr int kBlockK = kInt8 ? 128 : 64, kM = kCtas * kHeadM;
-    constexpr int kParts = head_epi_warps(kMode) / 4;       // warps per lane quarter
+    constexpr int kParts = kHeadEpiWarps / 4;       // warps per lane quarter
     constexpr int kMaxChunks = kHeadN / 32 / kParts;        // groups of 32 columns of one warp
+    constexpr int kPerAcc = kInt8 ? 1 << 20 : kCtas == 2 ? 8 : 4;   // k blocks of one accumulator: integers are exact, see below
 
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);   // swizzle atoms: 1 KB
     __shared__ HeadShared S;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t tmem = head_setup<kCtas>(S, P.stages, head_epi_warps(kMode), warp), rank = pair_rank<kCtas>();
+    const uint32_t tmem = head_setup<kCtas>(S, P.stages, warp), rank = pair_rank<kCtas>();
     volatile int* abort_flag = &S.abort;
     auto give_up = [&]() { atomicOr(P.dev_status, DSPARK_DEV_TIMEOUT); *abort_flag = 1; };
 
@@ -380,26 +379,28 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
             int s = 0, t = 0;
             uint32_t ph = 0;
             bool issued = false;
-            for (int u = first; u < n_units && !*abort_flag; u += step, ++t) {
-                const uint32_t acc = (uint32_t)(t & 1), aph = (uint32_t)(t >> 1) & 1u;
-                bool ok = pair_wait<kCtas>(&S.acc_empty[acc], aph ^ 1u);
-                tc_fence_after();
-                for (int kb = 0; ok && kb < k_blocks; ++kb) {
-                    ok = mbar_wait_bounded(&S.full[s], ph);
-                    if (!ok) break;
+            bool ok = true;
+            for (int u = first; ok && u < n_units && !*abort_flag; u += step)
+                for (int k0 = 0; ok && k0 < k_blocks; k0 += kPerAcc, ++t) {
+                    const uint32_t acc = (uint32_t)(t & 1), aph = (uint32_t)(t >> 1) & 1u;
+                    ok = pair_wait<kCtas>(&S.acc_empty[acc], aph ^ 1u);
                     tc_fence_after();
-                    const uint32_t a0 = smem_u32(smem + (size_t)s * stage_bytes), b0 = a0 + kTileABytes;
+                    for (int kb = k0; ok && kb < k_blocks && kb - k0 < kPerAcc; ++kb) {
+                        ok = mbar_wait_bounded(&S.full[s], ph);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint32_t a0 = smem_u32(smem + (size_t)s * stage_bytes), b0 = a0 + kTileABytes;
 #pragma unroll
-                    for (int ks = 0; ks < 4; ++ks)
-                        head_mma<kInt8, kCtas>(tmem + acc * kHeadN, head_desc(a0 + ks * 32, false), head_desc(b0 + ks * 32, false), idesc,
-                                        (kb > 0 || ks > 0) ? 1u : 0u);
-                    pair_commit<kCtas>(&S.empty[s]);
-                    issued = true;
-                    if (++s == P.stages) { s = 0; ph ^= 1u; }
+                        for (int ks = 0; ks < 4; ++ks)
+                            head_mma<kInt8, kCtas>(tmem + acc * kHeadN, head_desc(a0 + ks * 32, false), head_desc(b0 + ks * 32, false), idesc,
+                                                   (kb > k0 || ks > 0) ? 1u : 0u);
+                        pair_commit<kCtas>(&S.empty[s]);
+                        issued = true;
+                        if (++s == P.stages) { s = 0; ph ^= 1u; }
+                    }
+                    if (ok) pair_commit<kCtas>(&S.acc_full[acc]);
                 }
-                if (!ok) { give_up(); break; }
-                pair_commit<kCtas>(&S.acc_full[acc]);
-            }
+            if (!ok) give_up();
             head_finish_products(S, issued, kCtas);
         }
     } else {
@@ -409,10 +410,24 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
         const int chunks = (P.n_tile + 31) / 32;
         float* scales = (float*)(smem + kHeadRingBytes) + (warp - 2) * kMaxChunks * 32;
         int t = 0;
-        for (int u = first; u < n_units && !*abort_flag; u += step, ++t) {
+        bool ok = true;
+        // the next accumulator, and its release
+        auto take = [&](uint32_t& address) {
+            const uint32_t acc = (uint32_t)(t & 1), aph = (uint32_t)(t >> 1) & 1u;
+            ok = __all_sync(0xffffffffu, mbar_wait_bounded(&S.acc_full[acc], aph));
+            if (!ok && lane == 0) give_up();
+            tc_fence_after();
+            address = tmem + lane_base + acc * kHeadN;
+        };
+        auto release = [&]() {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) pair_arrive<kCtas>(&S.acc_empty[t & 1], 0);
+            ++t;
+        };
+        for (int u = first; ok && u < n_units && !*abort_flag; u += step) {
             int m0, nt;
             tile(u, m0, nt);
-            const uint32_t acc = (uint32_t)(t & 1), aph = (uint32_t)(t >> 1) & 1u;
             const int row0 = m0 + (int)rank * kHeadM + q * 32, row = row0 + lane, n0 = nt * P.n_tile;
             const bool in = row < m;
             // Int8Logits: the row of the batch that a column of the accumulator is (past the last one: none)
@@ -436,90 +451,116 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
             } else if (in) {
                 label = P.labels[row];
             }
-            if (!__all_sync(0xffffffffu, mbar_wait_bounded(&S.acc_full[acc], aph))) {
-                if (lane == 0) give_up();
-                break;
-            }
-            tc_fence_after();
-            const uint32_t acc_addr = tmem + lane_base + acc * kHeadN;
-            if (row0 < m) {
-                if (kInt8) {
-                    for (int c = part; c < chunks; c += kParts) {
-                        // a CTA's share is a multiple of 16 rows: the 32 columns are two runs of 16 neighbouring rows
-                        const int r0 = row_of(c * 32), r1 = row_of(c * 32 + 16);
-                        if (r0 >= n && r1 >= n) continue;
-                        const float* chunk_scales = scales + (c - part) / kParts * 32;
-                        float v[32];
-                        __syncwarp();
-                        tmem_load32(acc_addr + (uint32_t)(c * 32), v);
-#pragma unroll
-                        for (int i = 0; i < 32; i += 4) {
-                            const float4 sx = *reinterpret_cast<const float4*>(chunk_scales + i);
-                            v[i] = (float)__float_as_int(v[i]) * sx.x * sw;
-                            v[i + 1] = (float)__float_as_int(v[i + 1]) * sx.y * sw;
-                            v[i + 2] = (float)__float_as_int(v[i + 2]) * sx.z * sw;
-                            v[i + 3] = (float)__float_as_int(v[i + 3]) * sx.w * sw;
-                        }
-                        // lanes are neighbouring vocabulary entries: a warp stores 32 neighbours of one row at a time, or,
-                        // bf16 rows that pairs of entries may be stored to, 32 neighbours of two rows
-                        if (P.out_bf16 == 2 && row0 + 32 <= m) {
-                            store_pairs16((__nv_bfloat16*)P.out + (row & ~1), P.out_stride, r0, n - r0, v, lane);
-                            store_pairs16((__nv_bfloat16*)P.out + (row & ~1), P.out_stride, r1, n - r1, v + 16, lane);
-                        } else if (P.out_bf16) {
-                            store_column16((__nv_bfloat16*)P.out + row, P.out_stride, r0, in ? n - r0 : 0, v);
-                            store_column16((__nv_bfloat16*)P.out + row, P.out_stride, r1, in ? n - r1 : 0, v + 16);
-                        } else {
-                            store_column16((float*)P.out + row, P.out_stride, r0, in ? n - r0 : 0, v);
-                            store_column16((float*)P.out + row, P.out_stride, r1, in ? n - r1 : 0, v + 16);
-                        }
-                    }
-                } else {
-                    float ref = -INFINITY, sum = 0.f;
-                    for (int c = part; c < chunks; c += kParts) {
-                        const int col0 = n0 + c * 32;
-                        if (col0 >= n) break;
-                        float z[32];
-                        __syncwarp();
-                        tmem_load32(acc_addr + (uint32_t)(c * 32), z);
-                        if (label >= col0 && label < col0 + 32) {
-#pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                if (label == col0 + i) P.z_label[row] = z[i];
-                        }
-                        if (n - col0 < 32) {
-#pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                if (i >= n - col0) z[i] = -INFINITY;
-                        }
-                        float mx = z[0];
-#pragma unroll
-                        for (int i = 1; i < 32; ++i) mx = fmaxf(mx, z[i]);
-                        // references in the log2 domain: whatever rounding mx * log2(e) suffers, it is the same number
-                        // that is subtracted here and added back at the end
-                        const float now = fmaxf(ref, mx * kLog2e);
-                        const float base = now == -INFINITY ? 0.f : now;
-                        sum *= ex2_approx(ref - base);
-                        const uint64_t sc = pack2(kLog2e, kLog2e), no = pack2(-base, -base);
-                        uint64_t a = pack2(0.f, 0.f), b = pack2(0.f, 0.f);
-#pragma unroll
-                        for (int i = 0; i < 32; i += 4) {
-                            float t0, t1, t2, t3;
-                            unpack2(fma2(pack2(z[i], z[i + 1]), sc, no), t0, t1);
-                            unpack2(fma2(pack2(z[i + 2], z[i + 3]), sc, no), t2, t3);
-                            a = add2(a, pack2(ex2_approx(t0), ex2_approx(t1)));
-                            b = add2(b, pack2(ex2_approx(t2), ex2_approx(t3)));
-                        }
-                        float s0, s1;
-                        unpack2(add2(a, b), s0, s1);
-                        sum += s0 + s1;
-                        ref = now;
-                    }
-                    if (in) P.stats[(size_t)(nt * kParts + part) * P.stats_stride + row] = make_float2(ref, sum);
+            uint32_t acc_addr;
+            if constexpr (kInt8) {
+                take(acc_addr);
+                if (!ok) break;
+                if (row0 < m) {
+                                        for (int c = part; c < chunks; c += kParts) {
+                                            // a CTA's share is a multiple of 16 rows: the 32 columns are two runs of 16 neighbouring rows
+                                            const int r0 = row_of(c * 32), r1 = row_of(c * 32 + 16);
+                                            if (r0 >= n && r1 >= n) continue;
+                                            const float* chunk_scales = scales + (c - part) / kParts * 32;
+                                            float v[32];
+                                            __syncwarp();
+                                            tmem_load32(acc_addr + (uint32_t)(c * 32), v);
+                    #pragma unroll
+                                            for (int i = 0; i < 32; i += 4) {
+                                                const float4 sx = *reinterpret_cast<const float4*>(chunk_scales + i);
+                                                v[i] = (float)__float_as_int(v[i]) * sx.x * sw;
+                                                v[i + 1] = (float)__float_as_int(v[i + 1]) * sx.y * sw;
+                                                v[i + 2] = (float)__float_as_int(v[i + 2]) * sx.z * sw;
+                                                v[i + 3] = (float)__float_as_int(v[i + 3]) * sx.w * sw;
+                                            }
+                                            // lanes are neighbouring vocabulary entries: a warp stores 32 neighbours of one row at a time, or,
+                                            // bf16 rows that pairs of entries may be stored to, 32 neighbours of two rows
+                                            if (P.out_bf16 == 2 && row0 + 32 <= m) {
+                                                store_pairs16((__nv_bfloat16*)P.out + (row & ~1), P.out_stride, r0, n - r0, v, lane);
+                                                store_pairs16((__nv_bfloat16*)P.out + (row & ~1), P.out_stride, r1, n - r1, v + 16, lane);
+                                            } else if (P.out_bf16) {
+                                                store_column16((__nv_bfloat16*)P.out + row, P.out_stride, r0, in ? n - r0 : 0, v);
+                                                store_column16((__nv_bfloat16*)P.out + row, P.out_stride, r1, in ? n - r1 : 0, v + 16);
+                                            } else {
+                                                store_column16((float*)P.out + row, P.out_stride, r0, in ? n - r0 : 0, v);
+                                                store_column16((float*)P.out + row, P.out_stride, r1, in ? n - r1 : 0, v + 16);
+                                            }
+                                        }
                 }
+                release();
+            } else {
+                // The tensor cores cut an accumulator off after every product instead of rounding it, so its error grows with
+                // the length of the sum (d = 2 048: -1.3e-5 on a logit of 6, 9.7e-7 of the loss).  Sums are cut into kPerAcc
+                // blocks, which are added up here, rounded: 512 terms for many rows (2.2e-7 of the loss; 4096 rows 1.35 ->
+                // 1.42 ms), 256 for few (1.1e-7; 64 rows 57 -> 60 us).
+                float z[kMaxChunks][32];
+                for (int k0 = 0; k0 < k_blocks; k0 += kPerAcc) {
+                    take(acc_addr);
+                    if (!ok) break;
+                    if (row0 < m) {
+                        const uint32_t at = acc_addr + (uint32_t)(part * 32);
+                        __syncwarp();
+                        if (k0 == 0) {
+#pragma unroll
+                            for (int j = 0; j < kMaxChunks; ++j) tmem_load32_issue(at + (uint32_t)(j * kParts * 32), z[j]);
+#pragma unroll
+                            for (int j = 0; j < kMaxChunks; ++j) tmem_load_wait(z[j]);
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < kMaxChunks; ++j) {
+                                float v[32];
+                                tmem_load32_issue(at + (uint32_t)(j * kParts * 32), v);
+                                tmem_load_wait(v);
+#pragma unroll
+                                for (int i = 0; i < 32; i += 2) {
+                                    const uint64_t sum2 = add2(pack2(z[j][i], z[j][i + 1]), pack2(v[i], v[i + 1]));
+                                    unpack2(sum2, z[j][i], z[j][i + 1]);
+                                }
+                            }
+                        }
+                    }
+                    release();
+                }
+                if (!ok) break;
+                float ref = -INFINITY, sum = 0.f;
+#pragma unroll
+                for (int j = 0; j < kMaxChunks; ++j) {
+                    const int col0 = n0 + (part + j * kParts) * 32;
+                    if (col0 >= n || row0 >= m) continue;
+                    if (label >= col0 && label < col0 + 32) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (label == col0 + i) P.z_label[row] = z[j][i];
+                    }
+                    if (n - col0 < 32) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (i >= n - col0) z[j][i] = -INFINITY;
+                    }
+                    float mx = z[j][0];
+#pragma unroll
+                    for (int i = 1; i < 32; ++i) mx = fmaxf(mx, z[j][i]);
+                    // references in the log2 domain: whatever rounding mx * log2(e) suffers, it is the same number
+                    // that is subtracted here and added back at the end
+                    const float now = fmaxf(ref, mx * kLog2e);
+                    const float base = now == -INFINITY ? 0.f : now;
+                    sum *= ex2_approx(ref - base);
+                    const uint64_t sc = pack2(kLog2e, kLog2e), no = pack2(-base, -base);
+                    uint64_t a = pack2(0.f, 0.f), b = pack2(0.f, 0.f);
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4) {
+                        float t0, t1, t2, t3;
+                        unpack2(fma2(pack2(z[j][i], z[j][i + 1]), sc, no), t0, t1);
+                        unpack2(fma2(pack2(z[j][i + 2], z[j][i + 3]), sc, no), t2, t3);
+                        a = add2(a, pack2(ex2_approx(t0), ex2_approx(t1)));
+                        b = add2(b, pack2(ex2_approx(t2), ex2_approx(t3)));
+                    }
+                    float s0, s1;
+                    unpack2(add2(a, b), s0, s1);
+                    sum += s0 + s1;
+                    ref = now;
+                }
+                if (in) P.stats[(size_t)(nt * kParts + part) * P.stats_stride + row] = make_float2(ref, sum);
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) pair_arrive<kCtas>(&S.acc_empty[acc], 0);
         }
     }
     head_takedown<kCtas>(tmem, warp);
@@ -587,7 +628,7 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     __shared__ HeadShared S;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t tmem = head_setup<kCtas>(S, kStages, kHeadEpiWarps, warp), rank = pair_rank<kCtas>();
+    const uint32_t tmem = head_setup<kCtas>(S, kStages, warp), rank = pair_rank<kCtas>();
     volatile int* abort_flag = &S.abort;
     auto give_up = [&]() { atomicOr(P.dev_status, DSPARK_DEV_TIMEOUT); *abort_flag = 1; };
 
@@ -1156,11 +1197,11 @@ static bool allow_smem(Kernel kernel, int bytes, std::atomic<unsigned long long>
 
 // launch_pdl with clusters of kCtas CTAs
 template <int kCtas, typename... KArgs, typename... Args>
-static void launch_pairs(void (*kernel)(KArgs...), int ctas, int threads, size_t smem, cudaStream_t stream, Args... args)
+static void launch_pairs(void (*kernel)(KArgs...), int ctas, size_t smem, cudaStream_t stream, Args... args)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)ctas);
-    cfg.blockDim = dim3((unsigned)threads);
+    cfg.blockDim = dim3(kHeadThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
@@ -1184,7 +1225,7 @@ static int head_launch(HeadParams P, const CUtensorMap& a, const CUtensorMap& b,
     const long long units = (long long)((P.m + kCtas * kHeadM - 1) / (kCtas * kHeadM)) * ((P.n + P.n_tile - 1) / P.n_tile);
     const int groups = device_sms() / kCtas;
     KernelTimerScope timer(timer_id, s);
-    launch_pairs<kCtas>(lm_head_kernel<kMode, kCtas>, kCtas * (int)(units < groups ? units : groups), (2 + head_epi_warps(kMode)) * 32, kSmem, s, P, a, b);
+    launch_pairs<kCtas>(lm_head_kernel<kMode, kCtas>, kCtas * (int)(units < groups ? units : groups), kSmem, s, P, a, b);
     return launch_status();
 }
 
@@ -1195,7 +1236,7 @@ static int back_launch(const BackParams& P, const BackMaps& M, cudaStream_t s)
     static std::atomic<unsigned long long> ready{0};
     if (!allow_smem(lm_head_backward_kernel<kCtas>, kSmem, ready)) return launch_status();
     KernelTimerScope timer(DSPARK_K_HEAD_GRAD, s);
-    launch_pairs<kCtas>(lm_head_backward_kernel<kCtas>, device_sms() / kCtas * kCtas, kHeadThreads, kSmem, s, P, M);
+    launch_pairs<kCtas>(lm_head_backward_kernel<kCtas>, device_sms() / kCtas * kCtas, kSmem, s, P, M);
     return launch_status();
 }
 
