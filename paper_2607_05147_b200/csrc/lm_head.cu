@@ -588,7 +588,9 @@ struct BackParams {
     int32_t* dev_status;
     int32_t* sync;                  // [0] next unit, [1 + 3 p + kind] warps done with the units of that kind of piece p; zeros at the start
     __nv_bfloat16* G;               // three buffers [n_pad][piece]
-    const int32_t* labels; const float* lse2; const float* grad; float* label_err;
+    const int32_t* labels; const float* lse2; const float* grad; float* label_err;      // rows in the order of their labels
+    const int32_t* first;           // first row of a vocabulary entry that has rows
+    const __nv_bfloat16* rows; long long rows_stride;
     float* part; long long part_stride;
     __nv_bfloat16* dw; long long dw_stride;
 };
@@ -605,6 +607,25 @@ __device__ __forceinline__ bool wait_for_count(const int32_t* cell, int want)
 }
 __device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
 
+// v += a * 32 bf16
+__device__ __forceinline__ void add_scaled32(float (&v)[32], float a, const uint4 (&h)[4])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t w[4] = {h[i].x, h[i].y, h[i].z, h[i].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[8 * i + 2 * j] = fmaf(a, bf16lo(w[j]), v[8 * i + 2 * j]);
+            v[8 * i + 2 * j + 1] = fmaf(a, bf16hi(w[j]), v[8 * i + 2 * j + 1]);
+        }
+    }
+}
+__device__ __forceinline__ float load_relaxed(const float* p)
+{
+    float v;
+    asm volatile("ld.relaxed.gpu.global.f32 %0, [%1];" : "=f"(v) : "l"(p) : "memory");
+    return v;
+}
 __device__ __forceinline__ void load8(const float* p, float (&v)[8])
 {
     asm volatile("ld.relaxed.gpu.global.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
@@ -833,6 +854,17 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
             int label = -1;
             float lse2 = 0.f, g = 0.f;
             if (kind == kLossGrad && row < live) { label = P.labels[row]; lse2 = P.lse2[row]; g = P.grad[row]; }
+            // GradWeight: the rows whose label is this lane's vocabulary entry, and what the first of them lost
+            int run = 0, run_first = 0;
+            float run_err = 0.f;
+            if (kind == kGradWeight && p * P.piece + row < P.V) {
+                const int v = p * P.piece + row;
+                run_first = P.first[v];
+                if ((unsigned)run_first < (unsigned)live) {
+                    run_err = load_relaxed(P.label_err + run_first);
+                    while (run_first + run < live && P.labels[run_first + run] == v) ++run;
+                }
+            }
             if (any) {
                 if (!__all_sync(0xffffffffu, mbar_wait_bounded(&S.acc_full[acc], aph))) {
                     if (lane == 0) give_up();
@@ -906,8 +938,22 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
                     for (int c = half; c < P.n_tile_d / 32; c += 2) {
                         const int col0 = n0 + c * 32;
                         if (col0 >= P.d) break;
+                        // What the rounding of G lost of the labels' entries, most of a row of G and, with equal weights,
+                        // the same part of each (without this dW was 2.4e-3 off instead of 1.7e-3, its own rounding).
+                        const __nv_bfloat16* h = P.rows + (long long)run_first * P.rows_stride + col0;
+                        uint4 h0[4];
+                        if (run)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) h0[i] = reinterpret_cast<const uint4*>(h)[i];
                         float v[32];
                         load(c, v);
+                        if (run) add_scaled32(v, run_err, h0);
+                        for (int r = 1; r < run; ++r) {
+                            h += P.rows_stride;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) h0[i] = reinterpret_cast<const uint4*>(h)[i];
+                            add_scaled32(v, load_relaxed(P.label_err + run_first + r), h0);
+                        }
                         if (dw_vec && P.d - col0 >= 32) {
                             if (lane < rows) store_row32<true>(out + lane * P.dw_stride + col0, v);
                         } else {
@@ -930,10 +976,10 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
     head_takedown<kCtas>(tmem, warp);
 }
 
-// ---- rows that count, in order ------------------------------------------------------------------------
+// ---- rows that count ------------------------------------------------------------------------
 // A row whose label is negative is ignored: it is left out of the products altogether, so it costs nothing and nothing
-// it holds (padding, NaN) can reach a gradient.  The rows that count are copied next to each other, in order; each CTA
-// counts the labels before its own rows.  The last CTA fills up the last block of 64 rows with zeros (the product
+// it holds (padding, NaN) can reach a gradient.  The rows that count are copied next to each other; each CTA finds the
+// places of its own rows by looking at all labels.  The last CTA fills up the last block of 64 rows with zeros (the product
 // over rows reads it) and leaves the count.
 struct GatherParams {
     const __nv_bfloat16* h; long long h_stride;
@@ -941,6 +987,7 @@ struct GatherParams {
     int N, V, d;
     __nv_bfloat16* rows; long long rows_stride;     // compact copy
     int32_t* live; int32_t* idx; int32_t* label;
+    int32_t* first;                                 // backward: [V]
     float* loss; float* lse;                        // forward: zeros of the ignored rows
     const float* lse_in; const float* grad_in; float* lse2; float* grad;    // backward
     __nv_bfloat16* dh; long long dh_stride;         // backward: zeros of the ignored rows
@@ -949,39 +996,73 @@ struct GatherParams {
 };
 constexpr int kGatherThreads = 256;
 
-// kGatherRows: 8, a row per warp, while counting the labels of the rows before costs nothing; 32 for long inputs
-template <int kGatherRows>
+// kGatherRows: 8, a row per warp, while looking at all labels costs nothing; 32 for long inputs.
+// kSort (gradients): in the order of (label, row) instead of the rows' own, so that the rows of one vocabulary entry lie next
+// to each other from first[entry] on (entries without rows: whatever was there, which the reader checks).
+template <int kGatherRows, bool kSort>
 __global__ void __launch_bounds__(kGatherThreads) lm_head_gather_kernel(const __grid_constant__ GatherParams P)
 {
-    __shared__ int s_count[kGatherThreads / 32];
-    __shared__ int s_slot[kGatherRows];
+    __shared__ int s_slot[kGatherRows], s_label[kGatherRows], s_later[kGatherRows], s_total;
     pdl_wait();
     pdl_trigger();                                          // the contraction may set up its barriers and tensor memory
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int r0 = blockIdx.x * kGatherRows;
     for (int i = blockIdx.x * kGatherThreads + tid; i < P.n_sync; i += gridDim.x * kGatherThreads) P.sync[i] = 0;
-    auto counts = [&](int label) { return label >= 0 && label < P.V; };
-    int before = 0;
-    for (int i = tid; i < r0; i += kGatherThreads) before += counts(P.labels[i]);
-    before = __reduce_add_sync(0xffffffffu, before);
-    if (lane == 0) s_count[warp] = before;
+    const unsigned V = (unsigned)P.V;                       // a label counts when it is below V as an unsigned number
+    if (tid < kGatherRows) {
+        s_label[tid] = r0 + tid < P.N ? P.labels[r0 + tid] : -1;
+        s_slot[tid] = s_later[tid] = 0;
+    }
+    if (tid == 0) s_total = 0;
     __syncthreads();
-    before = 0;
-    for (int w = 0; w < kGatherThreads / 32; ++w) before += s_count[w];
-    const int row = r0 + lane;
-    const int label = lane < kGatherRows && row < P.N ? P.labels[row] : -1;
-    const bool in = counts(label);
-    const unsigned mask = __ballot_sync(0xffffffffu, in);
-    const int slot = before + __popc(mask & ((1u << lane) - 1u));
-    if (warp == 0 && lane < kGatherRows) {
-        s_slot[lane] = in ? slot : -1;
+    // every row's place: the rows that come before it
+    const bool last = blockIdx.x == gridDim.x - 1;
+    int count[kSort ? kGatherRows : 1], total = 0;
+#pragma unroll
+    for (int j = 0; j < (kSort ? kGatherRows : 1); ++j) count[j] = 0;
+    const int end_scan = kSort || last ? P.N : r0;
+    for (int m = tid; m < end_scan; m += kGatherThreads) {
+        const int other = P.labels[m];
+        if ((unsigned)other >= V) continue;
+        ++total;
+        if (kSort) {
+#pragma unroll
+            for (int j = 0; j < kGatherRows; ++j) {
+                const int mine = s_label[j];
+                count[j] += other < mine || (other == mine && m < r0 + j);
+                if (other == mine && m < r0 + j) s_later[j] = 1;           // not the first of its entry (every writer writes 1)
+            }
+        } else {
+            count[0] += m < r0;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < (kSort ? kGatherRows : 1); ++j) {
+        const int sum = __reduce_add_sync(0xffffffffu, count[j]);
+        if (lane == 0 && sum) atomicAdd(&s_slot[j], sum);
+    }
+    total = __reduce_add_sync(0xffffffffu, total);
+    if (lane == 0 && total) atomicAdd(&s_total, total);
+    __syncthreads();
+    if (warp == 0) {
+        const int row = r0 + lane, label = lane < kGatherRows ? s_label[lane] : -1;
+        const bool in = (unsigned)label < V;
+        const unsigned mask = __ballot_sync(0xffffffffu, in);
+        const int slot = kSort ? s_slot[lane < kGatherRows ? lane : 0] : s_slot[0] + __popc(mask & ((1u << lane) - 1u));
+        const bool head = lane < kGatherRows && !s_later[lane < kGatherRows ? lane : 0];
+        __syncwarp();
+        if (lane < kGatherRows) s_slot[lane] = in ? slot : -1;
         if (in) {
             P.idx[slot] = row;
             P.label[slot] = label;
-            if (P.lse2) { P.lse2[slot] = P.lse_in[row] * kLog2e; P.grad[slot] = P.grad_in[row]; }
-        } else if (row < P.N) {
+            if (kSort) {
+                P.lse2[slot] = P.lse_in[row] * kLog2e;
+                P.grad[slot] = P.grad_in[row];
+                if (head) P.first[label] = slot;
+            }
+        } else if (lane < kGatherRows && row < P.N) {
             if (P.loss) { P.loss[row] = 0.f; P.lse[row] = 0.f; }
-            if (label >= P.V) atomicOr(P.dev_status, DSPARK_DEV_BAD_TOKEN);
+            if (label >= 0) atomicOr(P.dev_status, DSPARK_DEV_BAD_TOKEN);
         }
     }
     __syncthreads();
@@ -1000,19 +1081,20 @@ __global__ void __launch_bounds__(kGatherThreads) lm_head_gather_kernel(const __
             for (int i = lane; i < P.d; i += 32) dst[i] = __float2bfloat16_rn(0.f);
         }
     }
-    if (blockIdx.x == gridDim.x - 1) {
-        const int total = before + __popc(mask);
-        if (tid == 0) *P.live = total;
-        const int end = (total + 63) & ~63;
-        for (int r = total + warp; r < end; r += kGatherThreads / 32)
+    if (last) {
+        const int live = s_total;
+        if (tid == 0) *P.live = live;
+        const int end = (live + 63) & ~63;
+        for (int r = live + warp; r < end; r += kGatherThreads / 32)
             for (int i = lane; i < P.d; i += 32) P.rows[(long long)r * P.rows_stride + i] = __float2bfloat16_rn(0.f);
     }
 }
 
+template <bool kSort>
 static void gather_launch(const GatherParams& g, cudaStream_t s)
 {
-    if (g.N <= 16384) launch_pdl(lm_head_gather_kernel<8>, dim3((g.N + 7) / 8), dim3(kGatherThreads), 0, s, g);
-    else launch_pdl(lm_head_gather_kernel<32>, dim3((g.N + 31) / 32), dim3(kGatherThreads), 0, s, g);
+    if (g.N <= 16384) launch_pdl(lm_head_gather_kernel<8, kSort>, dim3((g.N + 7) / 8), dim3(kGatherThreads), 0, s, g);
+    else launch_pdl(lm_head_gather_kernel<32, kSort>, dim3((g.N + 31) / 32), dim3(kGatherThreads), 0, s, g);
 }
 
 // ---- loss of every row from the statistics of the vocabulary tiles --------------------------------------
@@ -1244,7 +1326,7 @@ constexpr int kMaxRows = 1 << 20, kMaxVocab = 1 << 24, kMaxWidth = 1 << 16;
 constexpr long long kPieceBytes = 32ll << 20;
 
 struct LossWs {
-    size_t live, sync, idx, label, z_label, lse2, grad, label_err, rows, stats, G, part, total;
+    size_t live, sync, first, idx, label, z_label, lse2, grad, label_err, rows, stats, G, part, total;
     long long n_pad, d_pitch, part_pitch;
     int ctas, piece, pieces, n_sync, slices, kb_slice, n_tile_d, d_tiles;
 };
@@ -1285,6 +1367,7 @@ static LossWs loss_layout(int N, int V, int d)
     auto take = [&](size_t bytes) { const size_t at = o; o += up(bytes, 256); return at; };
     w.live = take(4);
     w.sync = take(4 * (size_t)w.n_sync);
+    w.first = take(4 * (size_t)V);
     w.idx = take(4 * (size_t)w.n_pad); w.label = take(4 * (size_t)w.n_pad); w.z_label = take(4 * (size_t)w.n_pad);
     w.lse2 = take(4 * (size_t)w.n_pad); w.grad = take(4 * (size_t)w.n_pad); w.label_err = take(4 * (size_t)w.n_pad);
     w.rows = take(2 * (size_t)w.n_pad * (size_t)w.d_pitch);
@@ -1384,7 +1467,7 @@ int dspark_lm_head_loss(const void* hidden, int64_t hidden_row_stride, const voi
     g.loss = out_loss; g.lse = out_lse; g.dev_status = dev_status;
     {
         KernelTimerScope timer(DSPARK_K_HEAD_ROWS, s);
-        gather_launch(g, s);
+        gather_launch<false>(g, s);
     }
     HeadParams P;
     memset(&P, 0, sizeof P);
@@ -1429,11 +1512,11 @@ int dspark_lm_head_loss_backward(const void* hidden, int64_t hidden_row_stride, 
     g.rows = (__nv_bfloat16*)(ws + w.rows); g.rows_stride = w.d_pitch;
     g.live = (int32_t*)(ws + w.live); g.idx = (int32_t*)(ws + w.idx); g.label = (int32_t*)(ws + w.label);
     g.lse_in = lse; g.grad_in = grad_loss; g.lse2 = (float*)(ws + w.lse2); g.grad = (float*)(ws + w.grad);
-    g.sync = (int32_t*)(ws + w.sync); g.n_sync = w.n_sync;
+    g.sync = (int32_t*)(ws + w.sync); g.n_sync = w.n_sync; g.first = (int32_t*)(ws + w.first);
     g.dh = (__nv_bfloat16*)out_grad_hidden; g.dh_stride = grad_hidden_row_stride; g.dev_status = dev_status;
     {
         KernelTimerScope timer(DSPARK_K_HEAD_ROWS, s);
-        gather_launch(g, s);
+        gather_launch<true>(g, s);
     }
     BackMaps M;
     const int box_v = V < kHeadN / w.ctas ? V : kHeadN / w.ctas;
@@ -1456,6 +1539,7 @@ int dspark_lm_head_loss_backward(const void* hidden, int64_t hidden_row_stride, 
     P.live = g.live; P.dev_status = dev_status; P.sync = g.sync;
     P.G = (__nv_bfloat16*)(ws + w.G);
     P.labels = g.label; P.lse2 = g.lse2; P.grad = g.grad; P.label_err = (float*)(ws + w.label_err);
+    P.first = g.first; P.rows = g.rows; P.rows_stride = w.d_pitch;
     P.part = (float*)(ws + w.part); P.part_stride = w.part_pitch;
     P.dw = (__nv_bfloat16*)out_grad_weight; P.dw_stride = grad_weight_row_stride;
     const int rc = w.ctas == 2 ? back_launch<2>(P, M, s) : back_launch<1>(P, M, s);

@@ -127,6 +127,27 @@ def test_every_row_ignored():
         assert (t == 0).all()
 
 
+@pytest.mark.parametrize("kind", ["one label", "two labels", "neighbours", "ends"])
+def test_labels_that_many_rows_share(kind):
+    h, w, labels, gl = make(300, 1500, 200, 19, ignored=0.1)
+    live = labels >= 0
+    some = {"one label": [777], "two labels": [255, 256], "neighbours": list(range(512, 530)), "ends": [0, 1499]}[kind]
+    labels[live] = torch.tensor(some, device="cuda", dtype=torch.int32)[torch.arange(300, device="cuda") % len(some)][live]
+    check(h, w, labels, gl)
+
+
+def test_equal_weights_whose_rounding_is_the_same_for_every_row():
+    # g = 1.00390625 - tiny: every label's entry of G, about -g, loses almost half a step of bf16 on the same side
+    h, w, labels, gl = make(260, 3000, 128, 20, lift=0.0)
+    gl.fill_(1.0 + 2.0 ** -8 - 2.0 ** -12)
+    out, _ = reference(h, w, labels, gl)
+    _, lse, _ = forward(h, w, labels)
+    dh, dw, _ = backward(h, w, labels, lse, gl)
+    # the result's rounding (2^-8 / sqrt 3 as a norm) and the little that the entries beside the labels' add
+    for got, want in ((dh, out["dh"]), (dw, out["dw"])):
+        assert (got.double() - want).norm() <= 0.7 * H * want.norm()
+
+
 def test_what_an_ignored_row_holds_reaches_nothing():
     h, w, labels, gl = make(200, 900, 64, 10, ignored=0.3)
     a = check(h, w, labels, gl)
