@@ -543,9 +543,10 @@ int dspark_lm_head_int8(const int8_t* x_q, int64_t x_row_stride, const float* x_
  *   out_grad_hidden device bf16 [N, >= d], out_grad_weight device bf16 [V, >= d]: any row stride, written (not added to);
  *                  either may be NULL, not both
  *   workspace      dspark_lm_head_loss_workspace_bytes(N, V, d), 256-byte aligned, any content; one call at a time
- * Products are bf16 with fp32 accumulation, softmax statistics fp32 (combined in fp64).  G is rounded to bf16 for its two
- * products (what that loses of the label's entry is added back to grad_hidden in fp32); sums over pieces and slices are
- * fp32 in a fixed order: the same inputs give the same bits.  A row whose loss is not finite sets DSPARK_DEV_BAD_ROW; its
+ * Products are bf16 with fp32 accumulation (the logits' sums in runs of at most 512 terms, added up in fp32), softmax
+ * statistics fp32 (combined in fp64).  G is rounded to bf16 for its two products; what that loses of the labels' entries is
+ * added back to both gradients in fp32, which are then off by about their own rounding to bf16.  Sums over pieces and
+ * slices are fp32 in a fixed order: the same inputs give the same bits.  A row whose loss is not finite sets DSPARK_DEV_BAD_ROW; its
  * loss and gradients are what the arithmetic gives (NaN reaches grad_weight, as in the formula).
  * Limits: N <= 2^20, V <= 2^24, d <= 65 536.  Errors: INVALID_ARG, SHAPE, ALIGNMENT, WORKSPACE, CUDA.
  * Resources (all three contractions): one CTA per SM with 193 KB of shared memory, all 512 tensor-memory columns of the SM;

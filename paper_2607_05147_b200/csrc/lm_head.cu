@@ -573,9 +573,9 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
 // C(p): the tiles of G of piece p; AB(p): the tiles of dH's partial sums over piece p, then those of dW's rows of it.  G of
 // three pieces is kept.  A unit waits (bounded) until what it needs is done: AB(p) for C(p) and, dH adding to what the
 // piece before left, for the dH tiles of piece p-1; C(p) for AB(p-3), whose piece of G it overwrites.  All of that was
-// handed out earlier, by at least a phase, to CTAs that are running: the waits end, and are short.  A separate launch per product and piece
-// (the first form) left SMs idle at the end of each of three launches a piece: 6.9 ms instead of 5.4 ms at 4 096 rows,
-// d 2 048.
+// handed out earlier, by at least a phase, to CTAs that are running: the waits end, and are short.  One launch per product
+// and piece left SMs idle at the end of each of three launches a piece: 4096 rows, d 2048 6.9 ms, 6.0 ms this way (single
+// CTAs), 5.1 ms with pairs.
 struct BackParams {
     int n_pad, V, d;
     int piece, pieces;              // entries of a piece (a multiple of 256), number of pieces
@@ -1424,8 +1424,9 @@ int dspark_lm_head_int8(const int8_t* x_q, int64_t x_row_stride, const float* x_
     memset(&P, 0, sizeof P);
     P.m = V; P.n = rows; P.k = K;
     // Pairs where the products bound the call, single CTAs where the weight's bytes or the stores do (V = 129 280, single /
-    // pair: 256 rows K 1024 43 / 46 us, 512 rows K 1024 74 / 75, 256 rows K 2048 71 / 67, 1482 rows K 4096 597 / 558).
-    const int ctas = rows > kHeadM && (long long)rows * K >= 1ll << 19 ? 2 : 1;
+    // pair, us: 352 rows K 1024 61 / 66, 1024 rows K 1024 142 / 142, 1482 rows K 512 139 / 161; 500 rows K 1536 101 / 94,
+    // 200 rows K 2048 67 / 63, 1482 rows K 4096 597 / 558; up to 128 rows the weight bounds it at any K).
+    const int ctas = rows > kHeadM && K > 1024 ? 2 : 1;
     // row tiles of one size, and no taller a box than there are rows (one row of 32 in a box: 170 us instead of 84 at
     // K = 4 096)
     const int row_tiles = (rows + kHeadN - 1) / kHeadN;
