@@ -456,35 +456,35 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
                 take(acc_addr);
                 if (!ok) break;
                 if (row0 < m) {
-                                        for (int c = part; c < chunks; c += kParts) {
-                                            // a CTA's share is a multiple of 16 rows: the 32 columns are two runs of 16 neighbouring rows
-                                            const int r0 = row_of(c * 32), r1 = row_of(c * 32 + 16);
-                                            if (r0 >= n && r1 >= n) continue;
-                                            const float* chunk_scales = scales + (c - part) / kParts * 32;
-                                            float v[32];
-                                            __syncwarp();
-                                            tmem_load32(acc_addr + (uint32_t)(c * 32), v);
-                    #pragma unroll
-                                            for (int i = 0; i < 32; i += 4) {
-                                                const float4 sx = *reinterpret_cast<const float4*>(chunk_scales + i);
-                                                v[i] = (float)__float_as_int(v[i]) * sx.x * sw;
-                                                v[i + 1] = (float)__float_as_int(v[i + 1]) * sx.y * sw;
-                                                v[i + 2] = (float)__float_as_int(v[i + 2]) * sx.z * sw;
-                                                v[i + 3] = (float)__float_as_int(v[i + 3]) * sx.w * sw;
-                                            }
-                                            // lanes are neighbouring vocabulary entries: a warp stores 32 neighbours of one row at a time, or,
-                                            // bf16 rows that pairs of entries may be stored to, 32 neighbours of two rows
-                                            if (P.out_bf16 == 2 && row0 + 32 <= m) {
-                                                store_pairs16((__nv_bfloat16*)P.out + (row & ~1), P.out_stride, r0, n - r0, v, lane);
-                                                store_pairs16((__nv_bfloat16*)P.out + (row & ~1), P.out_stride, r1, n - r1, v + 16, lane);
-                                            } else if (P.out_bf16) {
-                                                store_column16((__nv_bfloat16*)P.out + row, P.out_stride, r0, in ? n - r0 : 0, v);
-                                                store_column16((__nv_bfloat16*)P.out + row, P.out_stride, r1, in ? n - r1 : 0, v + 16);
-                                            } else {
-                                                store_column16((float*)P.out + row, P.out_stride, r0, in ? n - r0 : 0, v);
-                                                store_column16((float*)P.out + row, P.out_stride, r1, in ? n - r1 : 0, v + 16);
-                                            }
-                                        }
+                    for (int c = part; c < chunks; c += kParts) {
+                        // a CTA's share is a multiple of 16 rows: the 32 columns are two runs of 16 neighbouring rows
+                        const int r0 = row_of(c * 32), r1 = row_of(c * 32 + 16);
+                        if (r0 >= n && r1 >= n) continue;
+                        const float* chunk_scales = scales + (c - part) / kParts * 32;
+                        float v[32];
+                        __syncwarp();
+                        tmem_load32(acc_addr + (uint32_t)(c * 32), v);
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4) {
+                            const float4 sx = *reinterpret_cast<const float4*>(chunk_scales + i);
+                            v[i] = (float)__float_as_int(v[i]) * sx.x * sw;
+                            v[i + 1] = (float)__float_as_int(v[i + 1]) * sx.y * sw;
+                            v[i + 2] = (float)__float_as_int(v[i + 2]) * sx.z * sw;
+                            v[i + 3] = (float)__float_as_int(v[i + 3]) * sx.w * sw;
+                        }
+                        // lanes are neighbouring vocabulary entries: a warp stores 32 neighbours of one row at a time, or,
+                        // bf16 rows that pairs of entries may be stored to, 32 neighbours of two rows
+                        if (P.out_bf16 == 2 && row0 + 32 <= m) {
+                            store_pairs16((__nv_bfloat16*)P.out + (row & ~1), P.out_stride, r0, n - r0, v, lane);
+                            store_pairs16((__nv_bfloat16*)P.out + (row & ~1), P.out_stride, r1, n - r1, v + 16, lane);
+                        } else if (P.out_bf16) {
+                            store_column16((__nv_bfloat16*)P.out + row, P.out_stride, r0, in ? n - r0 : 0, v);
+                            store_column16((__nv_bfloat16*)P.out + row, P.out_stride, r1, in ? n - r1 : 0, v + 16);
+                        } else {
+                            store_column16((float*)P.out + row, P.out_stride, r0, in ? n - r0 : 0, v);
+                            store_column16((float*)P.out + row, P.out_stride, r1, in ? n - r1 : 0, v + 16);
+                        }
+                    }
                 }
                 release();
             } else {

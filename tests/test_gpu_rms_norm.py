@@ -64,6 +64,38 @@ def test_sizes(dtype, n, d, with_residual):
     check(x, w, 1e-6, r, call(x, w, 1e-6, r))
 
 
+# many rows: rings of rows in shared memory, a CTA or a warp per row
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n,d", [(600, 1032), (1500, 4096), (700, 8192), (593, 16384), (650, 10000), (5000, 512), (4800, 1000), (6001, 24), (9000, 264)])
+@pytest.mark.parametrize("with_residual,live", [(True, None), (False, None), (True, 595), (False, 4737)])
+def test_many_rows(dtype, n, d, with_residual, live):
+    g = torch.Generator(device="cuda").manual_seed(n + d)
+    x = torch.randn(n, d, generator=g, device="cuda").to(dtype)
+    x[n // 2] = 0
+    x[n // 3, d - 1] = float("nan")
+    r = (3 * torch.randn(n, d, generator=g, device="cuda")).to(dtype) if with_residual else None
+    w = (1 + 0.3 * torch.randn(d, generator=g, device="cuda")).to(dtype)
+    got = call(x, w, 1e-6, r, n_live=None if live is None else torch.tensor([live], dtype=torch.int32, device="cuda"), pads=(8, 16, 8))
+    rows = n if live is None else min(live, n)
+    assert torch.isnan(got[2][n // 3]) if n // 3 < rows else True
+    # the row with the NaN apart, everything as the formula says
+    keep = torch.arange(n, device="cuda") != n // 3
+    check(x[keep], w, 1e-6, r[keep] if with_residual else None, tuple(t[keep] for t in got), live=rows - (1 if n // 3 < rows else 0))
+
+
+@pytest.mark.parametrize("n,d", [(3000, 2048), (5000, 256)])
+def test_many_rows_in_place(n, d):
+    x = torch.randn(n, d, device="cuda").bfloat16()
+    r = torch.randn(n, d, device="cuda").bfloat16()
+    w = torch.randn(d, device="cuda").bfloat16()
+    rh, rq, rs, ry = reference(x, r, w, 1e-6)
+    q = torch.empty(n, d, dtype=torch.int8, device="cuda")
+    s = torch.empty(n, device="cuda")
+    B.dspark_rms_norm_quant(x, w, 1e-6, residual=r, out_residual=r, out_q=q, out_scale=s, out_norm=x)
+    assert torch.equal(r, rh) and torch.equal(q, rq)
+    assert ((x.double() - ry).abs() <= (2.0 ** -8 + SCALE_TOL) * 1.01 * ry.abs()).all()
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("pad_in,pads,offset", [(8, (8, 16, 24), 0), (1, (0, 0, 0), 0), (0, (1, 0, 0), 0), (0, (0, 3, 0), 0), (0, (0, 0, 5), 0), (8, (8, 8, 8), 1)])
 def test_strides_and_alignment(dtype, pad_in, pads, offset):
