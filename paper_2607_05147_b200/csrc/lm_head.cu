@@ -41,8 +41,8 @@ constexpr int kHeadRingBytes = 4 * (kTileABytes + kHeadN * kRowBytes);   // 192 
 constexpr int kHeadEpiWarps = 8;                   // 16 take issue slots and polls from the issuer: backward 5 % slower, statistics 2 x
 constexpr int kUnitSlots = 4;
 constexpr int kHeadThreads = (2 + kHeadEpiWarps) * 32;
-constexpr int kTurnPitch = 34;                   // bf16: 17 words, so that rows fall into different banks
-constexpr int kTurnBytes = 32 * kTurnPitch * 2;   // one warp's block
+constexpr int kTurnPitch = 17;                   // words of 2 bf16: rows fall into different banks
+constexpr int kTurnBytes = 32 * kTurnPitch * 4;   // one warp's block
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct HeadParams {
@@ -182,17 +182,31 @@ __device__ __forceinline__ void store_row32(__nv_bfloat16* p, const float (&v)[3
     }
 #undef DSPARK_STORE8
 }
-// The same for rows that are not aligned or end inside: the 32 x 32 block of the warp is turned in shared memory (an odd
-// pitch of 17 words), so that 32 lanes store neighbours of one row.  `rows` and `n`: rows and columns that exist.
-__device__ __forceinline__ void store_block32(__nv_bfloat16* p, long long stride, const float (&v)[32], int rows, int n, __nv_bfloat16* block, int lane)
+// The same for rows that are not aligned or end inside: the 32 x 32 block of the warp is turned in shared memory (a pitch of
+// 17 words), so that neighbouring lanes store neighbours of one row: pairs of two rows at a time where pairs are aligned
+// (`pairs`), single elements otherwise.  `rows` and `n`: rows and columns that exist.
+__device__ __forceinline__ void store_block32(__nv_bfloat16* p, long long stride, const float (&v)[32], int rows, int n, bool pairs,
+                                              uint32_t* block, int lane)
 {
     __syncwarp();
 #pragma unroll
-    for (int i = 0; i < 32; ++i) block[lane * kTurnPitch + i] = __float2bfloat16_rn(v[i]);
+    for (int i = 0; i < 16; ++i) block[lane * kTurnPitch + i] = bf16_pair(v[2 * i], v[2 * i + 1]);
     __syncwarp();
-    if (lane < n)
+    if (pairs) {
+        const int c = lane & 15, r0 = lane >> 4;
+        uint32_t* q = reinterpret_cast<uint32_t*>(p + r0 * stride) + c;
+        if (2 * c + 1 < n)
 #pragma unroll 8
-        for (int r = 0; r < rows; ++r) p[r * stride + lane] = block[r * kTurnPitch + lane];
+            for (int r = r0; r < rows; r += 2) {
+                *q = block[r * kTurnPitch + c];
+                q += stride;                                // two rows of bf16: `stride` words
+            }
+        else if (2 * c < n)
+            for (int r = r0; r < rows; r += 2) p[r * stride + 2 * c] = reinterpret_cast<const __nv_bfloat16*>(block + r * kTurnPitch)[2 * c];
+    } else if (lane < n) {
+#pragma unroll 8
+        for (int r = 0; r < rows; ++r) p[r * stride + lane] = reinterpret_cast<const __nv_bfloat16*>(block + r * kTurnPitch)[lane];
+    }
 }
 
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
@@ -833,7 +847,8 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
         // ---------------- epilogue -----------------------------------------------------------------------
         const int q = warp & 3, half = (warp - 2) >> 2;
         const uint32_t lane_base = (uint32_t)(q * 32) << 16;
-        __nv_bfloat16* turn = (__nv_bfloat16*)(smem + kHeadRingBytes + (warp - 2) * kTurnBytes);
+        uint32_t* turn = (uint32_t*)(smem + kHeadRingBytes + (warp - 2) * kTurnBytes);
+        const bool dw_pairs = ((uintptr_t)P.dw & 3u) == 0 && (P.dw_stride & 1) == 0;
         const bool dw_vec = ((uintptr_t)P.dw & 31u) == 0 && (P.dw_stride & 15) == 0;
         int t = 0, slot = 0;
         uint32_t sph = 0;
@@ -957,7 +972,7 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
                         if (dw_vec && P.d - col0 >= 32) {
                             if (lane < rows) store_row32<true>(out + lane * P.dw_stride + col0, v);
                         } else {
-                            store_block32(out + col0, P.dw_stride, v, rows, P.d - col0, turn, lane);
+                            store_block32(out + col0, P.dw_stride, v, rows, P.d - col0, dw_pairs, turn, lane);
                         }
                     }
             }

@@ -116,6 +116,13 @@ def test_row_pitches():
     check(*make(150, 700, 100, 8, pad=1), pads=(4, 8))
 
 
+@pytest.mark.parametrize("d", [64, 33, 34, 500, 511])
+@pytest.mark.parametrize("pad", [0, 1, 2, 6, 16])
+def test_pitches_of_the_weight_gradient(d, pad):
+    # whole sectors, pairs and single elements; the last row of the last tile of 32
+    check(*make(40, 333, d, 21), pads=(pad, pad))
+
+
 def test_every_row_ignored():
     h, w, labels, gl = make(70, 600, 64, 9)
     labels[:] = -1
