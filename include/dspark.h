@@ -544,7 +544,8 @@ int dspark_lm_head_int8(const int8_t* x_q, int64_t x_row_stride, const float* x_
  *                  either may be NULL, not both
  *   workspace      dspark_lm_head_loss_workspace_bytes(N, V, d), 256-byte aligned, any content; one call at a time
  * Products are bf16 with fp32 accumulation (the logits' sums in runs of at most 512 terms, added up in fp32), softmax
- * statistics fp32 (combined in fp64).  G is rounded to bf16 for its two products; what that loses of the labels' entries is
+ * statistics fp32 (combined in fp64).  The label's logit is summed in fp32 on its own and the loss is log(1 + sum over the
+ * other entries of e^(z - z[label])), so a row that is sure of its label keeps the digits of its small loss and gradient.  G is rounded to bf16 for its two products; what that loses of the labels' entries is
  * added back to both gradients in fp32, which are then off by about their own rounding to bf16.  Sums over pieces and
  * slices are fp32 in a fixed order: the same inputs give the same bits.  A row whose loss is not finite sets DSPARK_DEV_BAD_ROW; its
  * loss and gradients are what the arithmetic gives (NaN reaches grad_weight, as in the formula).

@@ -44,6 +44,10 @@ constexpr int kHeadThreads = (2 + kHeadEpiWarps) * 32;
 constexpr int kTurnPitch = 17;                   // words of 2 bf16: rows fall into different banks
 constexpr int kTurnBytes = 32 * kTurnPitch * 4;   // one warp's block
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kHeadParts = kHeadEpiWarps / 4;     // warps per lane quarter
+constexpr int kHeadGroups = kHeadN / 32 / kHeadParts;     // groups of 32 columns of one warp
+// k blocks (of 64) of one accumulator of logits: see add_accumulator()
+template <int kCtas> __host__ __device__ constexpr int logit_blocks() { return kCtas == 2 ? 8 : 4; }
 
 struct HeadParams {
     int m, n, k;                    // extents; the one that counts rows is bounded by *live
@@ -53,8 +57,10 @@ struct HeadParams {
     int32_t* dev_status;
     void* out; long long out_stride; int out_bf16;                  // Int8Logits; out_bf16 2: pairs of entries may be stored
     const float* row_scale; const float* col_scale;
-    float2* stats; long long stats_stride;                          // LossStats: [2 n_tiles][rows] (reference, sum)
+    float2* stats; long long stats_stride;                          // LossStats: [2 n_tiles][rows] (largest logit, sum of e^(z - it))
     const int32_t* labels; float* z_label;
+    const __nv_bfloat16* rows; long long rows_stride;               // LossStats: the operands, for the labels' logits
+    const __nv_bfloat16* w; long long w_stride;
 };
 
 // ---- descriptors ------------------------------------------------------------------------------------
@@ -240,6 +246,68 @@ __device__ __forceinline__ void store_pairs16(__nv_bfloat16* p, long long stride
     }
 }
 
+// Logits of a 128 x 256 tile, one row a lane: z (+)= this warp's groups of columns of an accumulator.
+// The tensor cores cut an accumulator off after every product instead of rounding it, so its error grows with the length of
+// the sum (d = 2 048: -1.3e-5 on a logit of 6, 9.7e-7 of the loss).  Sums are therefore cut into accumulators of 512 terms
+// for many rows (3.0e-7 of the loss, with fp32 products 3.2e-7; 4096 rows 1.35 -> 1.42 ms) or 256 for few (64 rows 57 ->
+// 60 us) that are added up here, rounded.  The gradients need no such care: a probability is only relatively off.
+__device__ __forceinline__ void add_accumulator(float (&z)[kHeadGroups][32], uint32_t address, bool first)
+{
+    __syncwarp();
+    if (first) {
+#pragma unroll
+        for (int j = 0; j < kHeadGroups; ++j) tmem_load32_issue(address + (uint32_t)(j * kHeadParts * 32), z[j]);
+#pragma unroll
+        for (int j = 0; j < kHeadGroups; ++j) tmem_load_wait(z[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < kHeadGroups; ++j) {
+            float v[32];
+            tmem_load32_issue(address + (uint32_t)(j * kHeadParts * 32), v);
+            tmem_load_wait(v);
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) {
+                const uint64_t sum = add2(pack2(z[j][i], z[j][i + 1]), pack2(v[i], v[i + 1]));
+                unpack2(sum, z[j][i], z[j][i + 1]);
+            }
+        }
+    }
+}
+
+// The logit of a row's label, a product of two rows summed by a warp in fp32, rounded.  Where a row is sure of its label,
+// softmax - 1 there and the loss are small differences of this logit and lse, in which the tensor cores' cut-off sums showed
+// (a loss of 5e-3: gradients 2.5 % off).  So the loss is written with this logit and the sum over the other entries, and the
+// gradient takes the same logit, bit for bit.  16 MB more of W for 4096 rows: at most 1 % of a call.
+// kAligned: h in vectors of 8; the sums are the same either way.
+template <bool kAligned>
+__device__ __forceinline__ float label_logit(const __nv_bfloat16* h, const __nv_bfloat16* w, int d, int lane)
+{
+    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int i = lane; i < d / 8; i += 32) {
+        const uint4 b = reinterpret_cast<const uint4*>(w)[i];
+        const uint32_t y[4] = {b.x, b.y, b.z, b.w};
+        uint4 a;
+        if (kAligned) a = reinterpret_cast<const uint4*>(h)[i];
+        else {
+            const unsigned short* e = reinterpret_cast<const unsigned short*>(h) + 8 * i;
+            a = make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16, e[4] | (uint32_t)e[5] << 16, e[6] | (uint32_t)e[7] << 16);
+        }
+        const uint32_t x[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            sum[2 * j] = fmaf(bf16lo(x[j]), bf16lo(y[j]), sum[2 * j]);
+            sum[2 * j + 1] = fmaf(bf16hi(x[j]), bf16hi(y[j]), sum[2 * j + 1]);
+        }
+    }
+    float z = ((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7]));
+    const int i = d / 8 * 8 + lane;
+    if (i < d) z = fmaf(__bfloat162float(h[i]), __bfloat162float(w[i]), z);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+    return z;
+}
+
 // What both kernels set up and take down: barriers, tensor memory.
 struct HeadShared {
     uint64_t full[kHeadMaxStages], empty[kHeadMaxStages], acc_full[2], acc_empty[2], mma_done;
@@ -322,9 +390,7 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
 {
     constexpr bool kInt8 = kMode == kInt8Logits;
     constexpr int kBlockK = kInt8 ? 128 : 64, kM = kCtas * kHeadM;
-    constexpr int kParts = kHeadEpiWarps / 4;       // warps per lane quarter
-    constexpr int kMaxChunks = kHeadN / 32 / kParts;        // groups of 32 columns of one warp
-    constexpr int kPerAcc = kInt8 ? 1 << 20 : kCtas == 2 ? 8 : 4;   // k blocks of one accumulator: integers are exact, see below
+    constexpr int kPerAcc = kInt8 ? 1 << 20 : logit_blocks<kCtas>();       // integers are exact
 
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);   // swizzle atoms: 1 KB
@@ -422,7 +488,7 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
         const int q = warp & 3, part = (warp - 2) >> 2;
         const uint32_t lane_base = (uint32_t)(q * 32) << 16;
         const int chunks = (P.n_tile + 31) / 32;
-        float* scales = (float*)(smem + kHeadRingBytes) + (warp - 2) * kMaxChunks * 32;
+        float* scales = (float*)(smem + kHeadRingBytes) + (warp - 2) * kHeadGroups * 32;
         int t = 0;
         bool ok = true;
         // the next accumulator, and its release
@@ -439,6 +505,12 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
             if (lane == 0) pair_arrive<kCtas>(&S.acc_empty[t & 1], 0);
             ++t;
         };
+        // the labels' logits, while the first tile is being computed: in the gather launch they cost 2 us of 59
+        if (!kInt8)
+            for (int r = (int)blockIdx.x * kHeadEpiWarps + warp - 2; r < m; r += (int)gridDim.x * kHeadEpiWarps) {
+                const float z = label_logit<true>(P.rows + r * P.rows_stride, P.w + P.labels[r] * P.w_stride, P.k, lane);
+                if (lane == 0) P.z_label[r] = z;
+            }
         for (int u = first; ok && u < n_units && !*abort_flag; u += step) {
             int m0, nt;
             tile(u, m0, nt);
@@ -457,8 +529,8 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
                 if (in) sw = P.col_scale[row];
                 __syncwarp();                               // the scales of the tile before have been read
 #pragma unroll
-                for (int j = 0; j < kMaxChunks; ++j) {
-                    const int r = row_of((part + j * kParts) * 32 + lane);
+                for (int j = 0; j < kHeadGroups; ++j) {
+                    const int r = row_of((part + j * kHeadParts) * 32 + lane);
                     scales[j * 32 + lane] = r < n ? P.row_scale[r] : 0.f;
                 }
                 __syncwarp();
@@ -470,11 +542,11 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
                 take(acc_addr);
                 if (!ok) break;
                 if (row0 < m) {
-                    for (int c = part; c < chunks; c += kParts) {
+                    for (int c = part; c < chunks; c += kHeadParts) {
                         // a CTA's share is a multiple of 16 rows: the 32 columns are two runs of 16 neighbouring rows
                         const int r0 = row_of(c * 32), r1 = row_of(c * 32 + 16);
                         if (r0 >= n && r1 >= n) continue;
-                        const float* chunk_scales = scales + (c - part) / kParts * 32;
+                        const float* chunk_scales = scales + (c - part) / kHeadParts * 32;
                         float v[32];
                         __syncwarp();
                         tmem_load32(acc_addr + (uint32_t)(c * 32), v);
@@ -502,78 +574,52 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
                 }
                 release();
             } else {
-                // The tensor cores cut an accumulator off after every product instead of rounding it, so its error grows with
-                // the length of the sum (d = 2 048: -1.3e-5 on a logit of 6, 9.7e-7 of the loss).  Sums are cut into kPerAcc
-                // blocks, which are added up here, rounded: 512 terms for many rows (2.2e-7 of the loss; 4096 rows 1.35 ->
-                // 1.42 ms), 256 for few (1.1e-7; 64 rows 57 -> 60 us).
-                float z[kMaxChunks][32];
+                float z[kHeadGroups][32];
                 for (int k0 = 0; k0 < k_blocks; k0 += kPerAcc) {
                     take(acc_addr);
                     if (!ok) break;
-                    if (row0 < m) {
-                        const uint32_t at = acc_addr + (uint32_t)(part * 32);
-                        __syncwarp();
-                        if (k0 == 0) {
-#pragma unroll
-                            for (int j = 0; j < kMaxChunks; ++j) tmem_load32_issue(at + (uint32_t)(j * kParts * 32), z[j]);
-#pragma unroll
-                            for (int j = 0; j < kMaxChunks; ++j) tmem_load_wait(z[j]);
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < kMaxChunks; ++j) {
-                                float v[32];
-                                tmem_load32_issue(at + (uint32_t)(j * kParts * 32), v);
-                                tmem_load_wait(v);
-#pragma unroll
-                                for (int i = 0; i < 32; i += 2) {
-                                    const uint64_t sum2 = add2(pack2(z[j][i], z[j][i + 1]), pack2(v[i], v[i + 1]));
-                                    unpack2(sum2, z[j][i], z[j][i + 1]);
-                                }
-                            }
-                        }
-                    }
+                    if (row0 < m) add_accumulator(z, acc_addr + (uint32_t)(part * 32), k0 == 0);
                     release();
                 }
                 if (!ok) break;
-                float ref = -INFINITY, sum = 0.f;
+                // The sum of e^(z - top) without the label's term, top the largest of the lane's (up to) 128 logits: what
+                // the loss of a row that is sure of its label consists of is not added to a one.
+                float top = -INFINITY, sum = 0.f;
+                if (row0 < m) {
 #pragma unroll
-                for (int j = 0; j < kMaxChunks; ++j) {
-                    const int col0 = n0 + (part + j * kParts) * 32;
-                    if (col0 >= n || row0 >= m) continue;
-                    if (label >= col0 && label < col0 + 32) {
+                    for (int j = 0; j < kHeadGroups; ++j) {
+                        const int col0 = n0 + (part + j * kHeadParts) * 32;
+                        if (label >= col0 && label < col0 + 32) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (label == col0 + i) P.z_label[row] = z[j][i];
+                            for (int i = 0; i < 32; ++i)
+                                if (label == col0 + i) z[j][i] = -INFINITY;
+                        }
+                        if (n - col0 < 32) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (i >= n - col0) z[j][i] = -INFINITY;
+                        }
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) top = fmaxf(top, z[j][i]);
                     }
-                    if (n - col0 < 32) {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (i >= n - col0) z[j][i] = -INFINITY;
-                    }
-                    float mx = z[j][0];
-#pragma unroll
-                    for (int i = 1; i < 32; ++i) mx = fmaxf(mx, z[j][i]);
-                    // references in the log2 domain: whatever rounding mx * log2(e) suffers, it is the same number
-                    // that is subtracted here and added back at the end
-                    const float now = fmaxf(ref, mx * kLog2e);
-                    const float base = now == -INFINITY ? 0.f : now;
-                    sum *= ex2_approx(ref - base);
+                    const float base = top == -INFINITY ? 0.f : top;
                     const uint64_t sc = pack2(kLog2e, kLog2e), no = pack2(-base, -base);
                     uint64_t a = pack2(0.f, 0.f), b = pack2(0.f, 0.f);
 #pragma unroll
-                    for (int i = 0; i < 32; i += 4) {
-                        float t0, t1, t2, t3;
-                        unpack2(fma2(pack2(z[j][i], z[j][i + 1]), sc, no), t0, t1);
-                        unpack2(fma2(pack2(z[j][i + 2], z[j][i + 3]), sc, no), t2, t3);
-                        a = add2(a, pack2(ex2_approx(t0), ex2_approx(t1)));
-                        b = add2(b, pack2(ex2_approx(t2), ex2_approx(t3)));
-                    }
+                    for (int j = 0; j < kHeadGroups; ++j)
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4) {
+                            float t0, t1, t2, t3;
+                            unpack2(mul2(add2(pack2(z[j][i], z[j][i + 1]), no), sc), t0, t1);
+                            unpack2(mul2(add2(pack2(z[j][i + 2], z[j][i + 3]), no), sc), t2, t3);
+                            a = add2(a, pack2(ex2_approx(t0), ex2_approx(t1)));
+                            b = add2(b, pack2(ex2_approx(t2), ex2_approx(t3)));
+                        }
                     float s0, s1;
                     unpack2(add2(a, b), s0, s1);
-                    sum += s0 + s1;
-                    ref = now;
+                    sum = s0 + s1;
                 }
-                if (in) P.stats[(size_t)(nt * kParts + part) * P.stats_stride + row] = make_float2(ref, sum);
+                if (in) P.stats[(size_t)(nt * kHeadParts + part) * P.stats_stride + row] = make_float2(top, sum);
             }
         }
     }
@@ -602,7 +648,7 @@ struct BackParams {
     int32_t* dev_status;
     int32_t* sync;                  // [0] next unit, [1 + 3 p + kind] warps done with the units of that kind of piece p; zeros at the start
     __nv_bfloat16* G;               // three buffers [n_pad][piece]
-    const int32_t* labels; const float* lse2; const float* grad; float* label_err;      // rows in the order of their labels
+    const int32_t* labels; const float* lse2; const float* grad; const float* at_label; const float* label_err;  // rows in the order of their labels
     const int32_t* first;           // first row of a vocabulary entry that has rows
     const __nv_bfloat16* rows; long long rows_stride;
     float* part; long long part_stride;
@@ -633,12 +679,6 @@ __device__ __forceinline__ void add_scaled32(float (&v)[32], float a, const uint
             v[8 * i + 2 * j + 1] = fmaf(a, bf16hi(w[j]), v[8 * i + 2 * j + 1]);
         }
     }
-}
-__device__ __forceinline__ float load_relaxed(const float* p)
-{
-    float v;
-    asm volatile("ld.relaxed.gpu.global.f32 %0, [%1];" : "=f"(v) : "l"(p) : "memory");
-    return v;
 }
 __device__ __forceinline__ void load8(const float* p, float (&v)[8])
 {
@@ -845,7 +885,7 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
         }
     } else {
         // ---------------- epilogue -----------------------------------------------------------------------
-        const int q = warp & 3, half = (warp - 2) >> 2;
+        const int q = warp & 3, part = (warp - 2) >> 2;
         const uint32_t lane_base = (uint32_t)(q * 32) << 16;
         uint32_t* turn = (uint32_t*)(smem + kHeadRingBytes + (warp - 2) * kTurnBytes);
         const bool dw_pairs = ((uintptr_t)P.dw & 3u) == 0 && (P.dw_stride & 1) == 0;
@@ -867,8 +907,8 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
             const uint32_t acc = (uint32_t)(t & 1), aph = (uint32_t)(t >> 1) & 1u;
             const int row = row0 + lane;
             int label = -1;
-            float lse2 = 0.f, g = 0.f;
-            if (kind == kLossGrad && row < live) { label = P.labels[row]; lse2 = P.lse2[row]; g = P.grad[row]; }
+            float lse2 = 0.f, g = 0.f, at_label = 0.f;
+            if (kind == kLossGrad && row < live) { label = P.labels[row]; lse2 = P.lse2[row]; g = P.grad[row]; at_label = P.at_label[row]; }
             // GradWeight: the rows whose label is this lane's vocabulary entry, and what the first of them lost
             int run = 0, run_first = 0;
             float run_err = 0.f;
@@ -876,7 +916,7 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
                 const int v = p * P.piece + row;
                 run_first = P.first[v];
                 if ((unsigned)run_first < (unsigned)live) {
-                    run_err = load_relaxed(P.label_err + run_first);
+                    run_err = P.label_err[run_first];
                     while (run_first + run < live && P.labels[run_first + run] == v) ++run;
                 }
             }
@@ -903,7 +943,7 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
                 const int v0 = p * P.piece;
                 label -= v0;
                 __nv_bfloat16* out = P.G + ((long long)(p % 3) * P.n_pad + row) * P.piece;
-                for (int c = half; c < kHeadN / 32; c += 2) {
+                for (int c = part; c < kHeadN / 32; c += kHeadParts) {
                     const int col0 = n0 + c * 32;
                     float z[32];
                     load(c, z);
@@ -913,10 +953,7 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
                     if (label >= col0 && label < col0 + 32) {
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
-                            if (label == col0 + i) {
-                                z[i] -= g;
-                                P.label_err[row] = z[i] - __bfloat162float(__float2bfloat16_rn(z[i]));
-                            }
+                            if (label == col0 + i) z[i] = at_label;
                     }
                     if (valid < 32) {
 #pragma unroll
@@ -928,7 +965,7 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
             } else if (kind == kGradHidden) {
                 float* out = P.part + ((long long)u1.z * P.n_pad + row) * P.part_stride;
                 if (row0 < live)
-                    for (int c = half; c < P.n_tile_d / 32; c += 2) {
+                    for (int c = part; c < P.n_tile_d / 32; c += kHeadParts) {
                         const int col0 = n0 + c * 32;
                         if (col0 >= P.d) break;
                         float v[32];
@@ -950,7 +987,7 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
                 const int rows = P.V - first < 32 ? P.V - first : 32;
                 __nv_bfloat16* out = P.dw + (long long)first * P.dw_stride;
                 if (rows > 0)
-                    for (int c = half; c < P.n_tile_d / 32; c += 2) {
+                    for (int c = part; c < P.n_tile_d / 32; c += kHeadParts) {
                         const int col0 = n0 + c * 32;
                         if (col0 >= P.d) break;
                         // What the rounding of G lost of the labels' entries, most of a row of G and, with equal weights,
@@ -967,7 +1004,7 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
                             h += P.rows_stride;
 #pragma unroll
                             for (int i = 0; i < 4; ++i) h0[i] = reinterpret_cast<const uint4*>(h)[i];
-                            add_scaled32(v, load_relaxed(P.label_err + run_first + r), h0);
+                            add_scaled32(v, P.label_err[run_first + r], h0);
                         }
                         if (dw_vec && P.d - col0 >= 32) {
                             if (lane < rows) store_row32<true>(out + lane * P.dw_stride + col0, v);
@@ -1004,7 +1041,9 @@ struct GatherParams {
     int32_t* live; int32_t* idx; int32_t* label;
     int32_t* first;                                 // backward: [V]
     float* loss; float* lse;                        // forward: zeros of the ignored rows
-    const float* lse_in; const float* grad_in; float* lse2; float* grad;    // backward
+    const float* lse_in; const float* grad_in; float* grad;    // backward (lse: the compact rows', times log2(e))
+    const __nv_bfloat16* w; long long w_stride;     // backward
+    float* at_label; float* label_err;              // backward: the label's entry of G, and what is lost when it is rounded to bf16
     __nv_bfloat16* dh; long long dh_stride;         // backward: zeros of the ignored rows
     int32_t* sync; int n_sync;                      // backward: the counters of the units, zeroed
     int32_t* dev_status;
@@ -1071,7 +1110,7 @@ __global__ void __launch_bounds__(kGatherThreads) lm_head_gather_kernel(const __
             P.idx[slot] = row;
             P.label[slot] = label;
             if (kSort) {
-                P.lse2[slot] = P.lse_in[row] * kLog2e;
+                P.lse[slot] = P.lse_in[row] * kLog2e;
                 P.grad[slot] = P.grad_in[row];
                 if (head) P.first[label] = slot;
             }
@@ -1091,6 +1130,17 @@ __global__ void __launch_bounds__(kGatherThreads) lm_head_gather_kernel(const __
             for (int i = lane; i < vectors; i += 32) reinterpret_cast<uint4*>(dst)[i] = reinterpret_cast<const uint4*>(src)[i];
 #pragma unroll 4
             for (int i = vectors * 8 + lane; i < P.d; i += 32) dst[i] = src[i];
+            if (kSort) {
+                // g (softmax - 1), of which the product over rows reads the bf16
+                const __nv_bfloat16* w = P.w + (long long)s_label[r] * P.w_stride;
+                const float z = vectors ? label_logit<true>(src, w, P.d, lane) : label_logit<false>(src, w, P.d, lane);
+                if (lane == 0) {
+                    const float x = z - P.lse_in[r0 + r];
+                    const float e = expm1f(x > 0.f ? 0.f : x) * P.grad_in[r0 + r];
+                    P.at_label[to] = e;
+                    P.label_err[to] = e - __bfloat162float(__float2bfloat16_rn(e));
+                }
+            }
         } else if (P.dh) {
             __nv_bfloat16* dst = P.dh + (long long)(r0 + r) * P.dh_stride;
             for (int i = lane; i < P.d; i += 32) dst[i] = __float2bfloat16_rn(0.f);
@@ -1114,7 +1164,8 @@ static void gather_launch(const GatherParams& g, cudaStream_t s)
 
 // ---- loss of every row from the statistics of the vocabulary tiles --------------------------------------
 // Eight rows per CTA, 128 threads per row, each taking every 128th entry (eight loads in flight): at V = 129 280 a row has
-// 1 010 entries.  lse = ln 2 * (R + log2(sum s_i 2^(r_i - R))), the sum over threads in 64 bits.
+// 1 010 entries.  loss = log(1 + T e^(R - z)), lse = z + loss, with z the label's logit and T = sum s_i e^(r_i - R) over the
+// other entries, R the largest r_i; the sum over threads and the rest in 64 bits.
 struct LossParams {
     const float2* stats; long long stats_stride; int entries;
     const float* z_label; const int32_t* idx; const int32_t* live;
@@ -1143,15 +1194,15 @@ __global__ void __launch_bounds__(kLossThreads) lm_head_loss_kernel(const __grid
 #pragma unroll
         for (int i = 0; i < kLossPer; ++i) now = fmaxf(now, v[i].x);
         const float base = now == -INFINITY ? 0.f : now;
-        sum *= ex2_approx(ref - base);
+        sum *= ex2_approx((ref - base) * kLog2e);
 #pragma unroll
-        for (int i = 0; i < kLossPer; ++i) sum = fmaf(v[i].y, ex2_approx(v[i].x - base), sum);
+        for (int i = 0; i < kLossPer; ++i) sum = fmaf(v[i].y, ex2_approx((v[i].x - base) * kLog2e), sum);
         ref = now;
     }
     float top = ref;
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-    double part = (double)(sum * ex2_approx(ref - (top == -INFINITY ? 0.f : top)));
+    double part = (double)(sum * ex2_approx((ref - (top == -INFINITY ? 0.f : top)) * kLog2e));
     part += __shfl_xor_sync(0xffffffffu, part, 8);
     part += __shfl_xor_sync(0xffffffffu, part, 16);
     if (lane < kLossRows) { s_ref[warp][lane] = top; s_sum[warp][lane] = part; }
@@ -1161,13 +1212,14 @@ __global__ void __launch_bounds__(kLossThreads) lm_head_loss_kernel(const __grid
     for (int w = 0; w < kLossThreads / 32; ++w) top = fmaxf(top, s_ref[w][lane]);
     const float base = top == -INFINITY ? 0.f : top;
     double total = 0.0;
-    for (int w = 0; w < kLossThreads / 32; ++w) total += s_sum[w][lane] * (double)ex2_approx(s_ref[w][lane] - base);
-    const double lse = ((double)base + log2(total)) * 0.69314718055994530942;
+    for (int w = 0; w < kLossThreads / 32; ++w) total += s_sum[w][lane] * (double)ex2_approx((s_ref[w][lane] - base) * kLog2e);
+    // `total` e^base is the sum over the other entries (none of them: 0); z - z is not a number when z is none or not finite
+    const double z = P.z_label[row], shift = total == 0.0 ? 0.0 : base - z;
+    const double loss = (z - z) + (shift > 0.0 ? shift + log(total + exp(-shift)) : log1p(total * exp(shift)));
     const int at = P.idx[row];
-    const float loss = (float)(lse - (double)P.z_label[row]);
-    P.loss[at] = loss;
-    P.lse[at] = (float)lse;
-    if (!(fabsf(loss) < INFINITY)) atomicOr(P.dev_status, DSPARK_DEV_BAD_ROW);
+    P.loss[at] = (float)loss;
+    P.lse[at] = (float)(z + loss);
+    if (!(fabs(loss) < INFINITY)) atomicOr(P.dev_status, DSPARK_DEV_BAD_ROW);
 }
 
 // ---- gradient of the hidden states from the slices' partial sums ---------------------------------------
@@ -1341,7 +1393,7 @@ constexpr int kMaxRows = 1 << 20, kMaxVocab = 1 << 24, kMaxWidth = 1 << 16;
 constexpr long long kPieceBytes = 32ll << 20;
 
 struct LossWs {
-    size_t live, sync, first, idx, label, z_label, lse2, grad, label_err, rows, stats, G, part, total;
+    size_t live, sync, first, idx, label, at_label, lse, grad, label_err, rows, stats, G, part, total;
     long long n_pad, d_pitch, part_pitch;
     int ctas, piece, pieces, n_sync, slices, kb_slice, n_tile_d, d_tiles;
 };
@@ -1383,8 +1435,8 @@ static LossWs loss_layout(int N, int V, int d)
     w.live = take(4);
     w.sync = take(4 * (size_t)w.n_sync);
     w.first = take(4 * (size_t)V);
-    w.idx = take(4 * (size_t)w.n_pad); w.label = take(4 * (size_t)w.n_pad); w.z_label = take(4 * (size_t)w.n_pad);
-    w.lse2 = take(4 * (size_t)w.n_pad); w.grad = take(4 * (size_t)w.n_pad); w.label_err = take(4 * (size_t)w.n_pad);
+    w.idx = take(4 * (size_t)w.n_pad); w.label = take(4 * (size_t)w.n_pad); w.at_label = take(4 * (size_t)w.n_pad);
+    w.lse = take(4 * (size_t)w.n_pad); w.grad = take(4 * (size_t)w.n_pad); w.label_err = take(4 * (size_t)w.n_pad);
     w.rows = take(2 * (size_t)w.n_pad * (size_t)w.d_pitch);
     const size_t common = o;
     // forward: two entries per vocabulary tile and row
@@ -1490,7 +1542,8 @@ int dspark_lm_head_loss(const void* hidden, int64_t hidden_row_stride, const voi
     P.m = N; P.n = V; P.k = d;
     P.n_tile = kHeadN; P.box_n = V < kHeadN / w.ctas ? V : kHeadN / w.ctas;
     P.live = g.live; P.dev_status = dev_status;
-    P.stats = (float2*)(ws + w.stats); P.stats_stride = w.n_pad; P.labels = g.label; P.z_label = (float*)(ws + w.z_label);
+    P.stats = (float2*)(ws + w.stats); P.stats_stride = w.n_pad; P.labels = g.label; P.z_label = (float*)(ws + w.at_label);
+    P.rows = g.rows; P.rows_stride = w.d_pitch; P.w = (const __nv_bfloat16*)weight; P.w_stride = weight_row_stride;
     CUtensorMap a, b;
     if (!operand_map(&a, g.rows, 2, w.n_pad, d, w.d_pitch * 2, 64, kHeadM) || !operand_map(&b, weight, 2, V, d, weight_row_stride * 2, 64, P.box_n))
         return DSPARK_ERR_CUDA;
@@ -1527,7 +1580,9 @@ int dspark_lm_head_loss_backward(const void* hidden, int64_t hidden_row_stride, 
     g.h = (const __nv_bfloat16*)hidden; g.h_stride = hidden_row_stride; g.labels = labels; g.N = N; g.V = V; g.d = d;
     g.rows = (__nv_bfloat16*)(ws + w.rows); g.rows_stride = w.d_pitch;
     g.live = (int32_t*)(ws + w.live); g.idx = (int32_t*)(ws + w.idx); g.label = (int32_t*)(ws + w.label);
-    g.lse_in = lse; g.grad_in = grad_loss; g.lse2 = (float*)(ws + w.lse2); g.grad = (float*)(ws + w.grad);
+    g.lse_in = lse; g.grad_in = grad_loss; g.lse = (float*)(ws + w.lse); g.grad = (float*)(ws + w.grad);
+    g.w = (const __nv_bfloat16*)weight; g.w_stride = weight_row_stride;
+    g.at_label = (float*)(ws + w.at_label); g.label_err = (float*)(ws + w.label_err);
     g.sync = (int32_t*)(ws + w.sync); g.n_sync = w.n_sync; g.first = (int32_t*)(ws + w.first);
     g.dh = (__nv_bfloat16*)out_grad_hidden; g.dh_stride = grad_hidden_row_stride; g.dev_status = dev_status;
     {
@@ -1554,7 +1609,7 @@ int dspark_lm_head_loss_backward(const void* hidden, int64_t hidden_row_stride, 
     P.want_h = out_grad_hidden != nullptr; P.want_w = out_grad_weight != nullptr;
     P.live = g.live; P.dev_status = dev_status; P.sync = g.sync;
     P.G = (__nv_bfloat16*)(ws + w.G);
-    P.labels = g.label; P.lse2 = g.lse2; P.grad = g.grad; P.label_err = (float*)(ws + w.label_err);
+    P.labels = g.label; P.lse2 = g.lse; P.grad = g.grad; P.at_label = g.at_label; P.label_err = g.label_err;
     P.first = g.first; P.rows = g.rows; P.rows_stride = w.d_pitch;
     P.part = (float*)(ws + w.part); P.part_stride = w.part_pitch;
     P.dw = (__nv_bfloat16*)out_grad_weight; P.dw_stride = grad_weight_row_stride;
@@ -1563,7 +1618,7 @@ int dspark_lm_head_loss_backward(const void* hidden, int64_t hidden_row_stride, 
     if (out_grad_hidden) {
         HiddenParams Hp;
         Hp.part = (const float*)(ws + w.part); Hp.part_stride = w.part_pitch; Hp.slices = w.slices; Hp.m = (int)w.n_pad;
-        Hp.label_err = (const float*)(ws + w.label_err); Hp.label = g.label; Hp.idx = g.idx; Hp.live = g.live;
+        Hp.label_err = g.label_err; Hp.label = g.label; Hp.idx = g.idx; Hp.live = g.live;
         Hp.w = (const __nv_bfloat16*)weight; Hp.w_stride = weight_row_stride; Hp.d = d;
         Hp.dh = g.dh; Hp.dh_stride = grad_hidden_row_stride;
         KernelTimerScope timer(DSPARK_K_HEAD_ROWS, s);

@@ -199,6 +199,44 @@ def test_large_logits():
     check((h.float() * 64).bfloat16(), w, labels, gl)
 
 
+@pytest.mark.parametrize("N,pad", [(1, 0), (2, 0), (100, 1), (200, 0)])
+def test_rows_that_are_sure_of_their_label(N, pad):
+    """Losses of 5e-3 at d = 16 384: softmax - 1 at the label is small against what a long sum that is cut off loses.
+
+    A loss is log(1 + e^-z[label] sum e^z), so it is off by what the exponents are (2 dz) and the exponentials (2^-20), all
+    relative to its size; lse is rounded once, and the label's entry e^(z - lse) - 1 sees that and the 11 roundings of lse as
+    above, and the loss's own error.  It is rounded to bf16 in two parts.  Every other entry is a probability, off by its
+    exponent and half a step."""
+    V, d = 2000, 16384
+    g = torch.Generator(device="cuda").manual_seed(77 + N)
+    w = (torch.randn(V, d, generator=g, device="cuda") * (0.2 / d ** 0.5)).bfloat16()
+    labels = torch.randperm(V, generator=g, device="cuda")[:N].int()
+    h = (torch.rand(N, d, generator=g, device="cuda") + 0.5) * w[labels.long()].float().sign()
+    z = (h.double() * w[labels.long()].double()).sum(1, keepdim=True)
+    h = h * (12.9 / z).float()
+    h = torch.cat([h, h[:, :pad]], 1).bfloat16()[:, :d]
+    gl = torch.ones(N, device="cuda")
+    hd, wd, at = h.double(), w.double(), labels.long()[:, None]
+    z = hd @ wd.T
+    lse = torch.logsumexp(z, 1, keepdim=True)
+    want = (z.scatter(1, at, float("-inf")) - lse).exp().sum(1, keepdim=True)       # 1 - softmax at the label
+    loss = -torch.log1p(-want)
+    assert float(loss.min()) > 2e-3 and float(loss.max()) < 2e-2
+    dz = (d / 16 + 8) * 2.0 ** -23 * float((hd.abs() @ wd.abs().T).max())            # of any logit, summed in one piece
+    p = (z - lse).exp().scatter(1, at, 0.0)
+    G = p.scatter(1, at, -want)
+    one = torch.zeros_like(p).scatter_(1, at, 1.0)
+    got = forward(h, w, labels)
+    assert got[2] == 0
+    assert ((got[0].double() - loss[:, 0]).abs() <= (2 * dz + 2.0 ** -19) * loss[:, 0]).all()
+    dh, dw, st = backward(h, w, labels, got[1], gl)
+    assert st == 0
+    rel = H + 2 * dz + 11 * 2.0 ** -24 * float(lse.max()) + 2.0 ** -20
+    off = rel * p + (11 * 2.0 ** -24 * lse.max() + (2 * dz + 2.0 ** -19 + H * H) * want) * one
+    assert ((dh.double() - G @ wd).abs() <= off @ wd.abs() + H * (G @ wd).abs() + 2.0 ** -20 * (G.abs() @ wd.abs())).all()
+    assert ((dw.double() - G.T @ hd).abs() <= off.T @ hd.abs() + H * (G.T @ hd).abs() + 2.0 ** -20 * (G.abs().T @ hd.abs())).all()
+
+
 def test_equal_logits():
     h = torch.zeros(30, 40, dtype=torch.bfloat16, device="cuda")
     w = torch.randn(1000, 40, device="cuda").bfloat16()
