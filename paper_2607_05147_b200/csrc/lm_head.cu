@@ -1050,6 +1050,21 @@ struct GatherParams {
 };
 constexpr int kGatherThreads = 256;
 
+// One row by a warp, kFlight elements of each lane in flight.
+template <int kFlight, typename T>
+__device__ __forceinline__ void copy_row(T* dst, const T* src, int n, int lane)
+{
+    for (int i = lane; i < n; i += 32 * kFlight) {
+        T v[kFlight];
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u)
+            if (i + 32 * u < n) v[u] = src[i + 32 * u];
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u)
+            if (i + 32 * u < n) dst[i + 32 * u] = v[u];
+    }
+}
+
 // kGatherRows: 8, a row per warp, while looking at all labels costs nothing; 32 for long inputs.
 // kSort (gradients): in the order of (label, row) instead of the rows' own, so that the rows of one vocabulary entry lie next
 // to each other from first[entry] on (entries without rows: whatever was there, which the reader checks).
@@ -1063,20 +1078,34 @@ __global__ void __launch_bounds__(kGatherThreads) lm_head_gather_kernel(const __
     const int r0 = blockIdx.x * kGatherRows;
     for (int i = blockIdx.x * kGatherThreads + tid; i < P.n_sync; i += gridDim.x * kGatherThreads) P.sync[i] = 0;
     const unsigned V = (unsigned)P.V;                       // a label counts when it is below V as an unsigned number
+    const bool last = blockIdx.x == gridDim.x - 1;
+    const int end_scan = kSort || last ? P.N : r0;
+    int other = tid < end_scan ? P.labels[tid] : -1;        // of the scan below, asked for together with the CTA's own
     if (tid < kGatherRows) {
         s_label[tid] = r0 + tid < P.N ? P.labels[r0 + tid] : -1;
         s_slot[tid] = s_later[tid] = 0;
     }
     if (tid == 0) s_total = 0;
     __syncthreads();
+    const int vectors = ((uintptr_t)P.h & 15u) == 0 && P.h_stride % 8 == 0 ? P.d / 8 : 0;
+    float at_label[kGatherRows / (kGatherThreads / 32)];    // g (softmax - 1) of the warp's rows
+    if (kSort)
+#pragma unroll
+        for (int j = 0; j < kGatherRows / (kGatherThreads / 32); ++j) {
+            const int r = warp + j * (kGatherThreads / 32), label = s_label[r];
+            if ((unsigned)label >= V) continue;
+            const float lse = P.lse_in[r0 + r], g = P.grad_in[r0 + r];
+            const __nv_bfloat16* h = P.h + (long long)(r0 + r) * P.h_stride;
+            const __nv_bfloat16* w = P.w + (long long)label * P.w_stride;
+            const float x = (vectors ? label_logit<true>(h, w, P.d, lane) : label_logit<false>(h, w, P.d, lane)) - lse;
+            at_label[j] = expm1f(x > 0.f ? 0.f : x) * g;
+        }
     // every row's place: the rows that come before it
-    const bool last = blockIdx.x == gridDim.x - 1;
     int count[kSort ? kGatherRows : 1], total = 0;
 #pragma unroll
     for (int j = 0; j < (kSort ? kGatherRows : 1); ++j) count[j] = 0;
-    const int end_scan = kSort || last ? P.N : r0;
     for (int m = tid; m < end_scan; m += kGatherThreads) {
-        const int other = P.labels[m];
+        if (m != tid) other = P.labels[m];
         if ((unsigned)other >= V) continue;
         ++total;
         if (kSort) {
@@ -1120,26 +1149,19 @@ __global__ void __launch_bounds__(kGatherThreads) lm_head_gather_kernel(const __
         }
     }
     __syncthreads();
-    const int vectors = ((uintptr_t)P.h & 15u) == 0 && P.h_stride % 8 == 0 ? P.d / 8 : 0;
-    for (int r = warp; r < kGatherRows && r0 + r < P.N; r += kGatherThreads / 32) {
+#pragma unroll
+    for (int j = 0; j < kGatherRows / (kGatherThreads / 32); ++j) {
+        const int r = warp + j * (kGatherThreads / 32);
+        if (r0 + r >= P.N) break;
         const int to = s_slot[r];
         const __nv_bfloat16* src = P.h + (long long)(r0 + r) * P.h_stride;
         if (to >= 0) {
             __nv_bfloat16* dst = P.rows + (long long)to * P.rows_stride;
-#pragma unroll 4
-            for (int i = lane; i < vectors; i += 32) reinterpret_cast<uint4*>(dst)[i] = reinterpret_cast<const uint4*>(src)[i];
-#pragma unroll 4
-            for (int i = vectors * 8 + lane; i < P.d; i += 32) dst[i] = src[i];
-            if (kSort) {
-                // g (softmax - 1), of which the product over rows reads the bf16
-                const __nv_bfloat16* w = P.w + (long long)s_label[r] * P.w_stride;
-                const float z = vectors ? label_logit<true>(src, w, P.d, lane) : label_logit<false>(src, w, P.d, lane);
-                if (lane == 0) {
-                    const float x = z - P.lse_in[r0 + r];
-                    const float e = expm1f(x > 0.f ? 0.f : x) * P.grad_in[r0 + r];
-                    P.at_label[to] = e;
-                    P.label_err[to] = e - __bfloat162float(__float2bfloat16_rn(e));
-                }
+            copy_row<4>(reinterpret_cast<uint4*>(dst), reinterpret_cast<const uint4*>(src), vectors, lane);
+            copy_row<16>(dst + vectors * 8, src + vectors * 8, P.d - vectors * 8, lane);
+            if (kSort && lane == 0) {
+                P.at_label[to] = at_label[j];               // the products read the bf16 of it
+                P.label_err[to] = at_label[j] - __bfloat162float(__float2bfloat16_rn(at_label[j]));
             }
         } else if (P.dh) {
             __nv_bfloat16* dst = P.dh + (long long)(r0 + r) * P.dh_stride;
@@ -1182,6 +1204,8 @@ __global__ void __launch_bounds__(kLossThreads) lm_head_loss_kernel(const __grid
     const int row = blockIdx.x * kLossRows + (lane & 7), live = *P.live;
     if (blockIdx.x * kLossRows >= live) return;
     const int first = (int)threadIdx.x >> 3;
+    const int at = row < live ? P.idx[row] : 0;
+    const double z = row < live ? P.z_label[row] : 0.f;
     float ref = -INFINITY, sum = 0.f;
     for (int e0 = first; e0 < P.entries; e0 += 128 * kLossPer) {
         float2 v[kLossPer];
@@ -1214,9 +1238,8 @@ __global__ void __launch_bounds__(kLossThreads) lm_head_loss_kernel(const __grid
     double total = 0.0;
     for (int w = 0; w < kLossThreads / 32; ++w) total += s_sum[w][lane] * (double)ex2_approx((s_ref[w][lane] - base) * kLog2e);
     // `total` e^base is the sum over the other entries (none of them: 0); z - z is not a number when z is none or not finite
-    const double z = P.z_label[row], shift = total == 0.0 ? 0.0 : base - z;
+    const double shift = total == 0.0 ? 0.0 : base - z;
     const double loss = (z - z) + (shift > 0.0 ? shift + log(total + exp(-shift)) : log1p(total * exp(shift)));
-    const int at = P.idx[row];
     P.loss[at] = (float)loss;
     P.lse[at] = (float)(z + loss);
     if (!(fabs(loss) < INFINITY)) atomicOr(P.dev_status, DSPARK_DEV_BAD_ROW);
@@ -1242,18 +1265,21 @@ __global__ void __launch_bounds__(kHiddenThreads) lm_head_grad_hidden_kernel(con
     if (c >= P.d) return;
     const float* part = P.part + (long long)row * P.part_stride + c;       // the pitch is a multiple of 8
     const long long step = (long long)P.m * P.part_stride;
+    const float err = P.label_err[row];
+    const __nv_bfloat16* w = P.w + (long long)P.label[row] * P.w_stride + c;
+    __nv_bfloat16* out = P.dh + (long long)P.idx[row] * P.dh_stride + c;
+    float at_label[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) at_label[i] = c + i < P.d ? __bfloat162float(w[i]) : 0.f;
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 16
     for (int s = 0; s < P.slices; ++s) {
         const float4 v = *reinterpret_cast<const float4*>(part + s * step);
         sum[0] += v.x; sum[1] += v.y; sum[2] += v.z; sum[3] += v.w;
     }
-    const float err = P.label_err[row];
-    const __nv_bfloat16* w = P.w + (long long)P.label[row] * P.w_stride + c;
-    __nv_bfloat16* out = P.dh + (long long)P.idx[row] * P.dh_stride + c;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        if (c + i < P.d) out[i] = __float2bfloat16_rn(fmaf(err, __bfloat162float(w[i]), sum[i]));
+        if (c + i < P.d) out[i] = __float2bfloat16_rn(fmaf(err, at_label[i], sum[i]));
 }
 
 // ---- int8 weights ------------------------------------------------------------------------------------------
