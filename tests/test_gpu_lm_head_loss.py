@@ -237,6 +237,27 @@ def test_rows_that_are_sure_of_their_label(N, pad):
     assert ((dw.double() - G.T @ hd).abs() <= off.T @ hd.abs() + H * (G.T @ hd).abs() + 2.0 ** -20 * (G.abs().T @ hd.abs())).all()
 
 
+@pytest.mark.parametrize("N", [1, 130])
+@pytest.mark.parametrize("size", [0.5, -200.0, 200.0])
+def test_a_vocabulary_of_one_entry(N, size):
+    # nothing but the label: the loss is the logarithm of one, whatever the logit
+    d = 64
+    h = torch.full((N, d), size, device="cuda").bfloat16()
+    w = torch.full((1, d), 0.5, device="cuda").bfloat16()
+    labels = torch.zeros(N, dtype=torch.int32, device="cuda")
+    loss, lse, st = forward(h, w, labels)
+    assert st == 0 and (loss == 0).all() and (lse == d * 0.5 * size).all()
+    dh, dw, st = backward(h, w, labels, lse, torch.ones(N, device="cuda"))
+    assert st == 0 and (dh == 0).all() and (dw == 0).all()
+
+
+@pytest.mark.parametrize("N", [3, 200])
+def test_labels_far_below_the_largest_logit(N):
+    # losses of several hundred, and a label whose own logit is far below what e^x holds
+    h, w, labels, gl = make(N, 700, 128, 21, lift=-60.0)
+    check((h.float() * 16).bfloat16(), w, labels, gl)
+
+
 def test_equal_logits():
     h = torch.zeros(30, 40, dtype=torch.bfloat16, device="cuda")
     w = torch.randn(1000, 40, device="cuda").bfloat16()
