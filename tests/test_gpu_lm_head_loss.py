@@ -143,6 +143,19 @@ def test_labels_that_many_rows_share(kind):
     check(h, w, labels, gl)
 
 
+@pytest.mark.parametrize("V,d", [(900, 100), (300, 257), (5000, 64)])
+def test_runs_of_every_length(V, d):
+    # neighbouring entries that are the label of 1, 2, ... 40 rows: runs a lane adds up alone (up to 16) and ones that the
+    # warp shares, of whole and of broken groups of eight rows, at the edge of a tile of 128 entries
+    first = 110
+    labels = torch.repeat_interleave(torch.arange(first, first + 40), torch.arange(1, 41))
+    N = labels.numel()
+    h, w, _, gl = make(N, V, d, 22)
+    labels = labels[torch.randperm(N, generator=torch.Generator().manual_seed(3))].int().cuda()
+    gl.fill_(1.0 + 2.0 ** -8 - 2.0 ** -12)              # every label's entry of G rounded to the same side
+    check(h, w, labels, gl, pads=(0, 16 - d % 16))
+
+
 def test_equal_weights_whose_rounding_is_the_same_for_every_row():
     # g = 1.00390625 - tiny: every label's entry of G, about -g, loses almost half a step of bf16 on the same side
     h, w, labels, gl = make(260, 3000, 128, 20, lift=0.0)
