@@ -113,6 +113,15 @@ __device__ __forceinline__ void pair_arrive(uint64_t* bar, uint32_t rank)
     if (kCtas == 1) mbar_arrive(bar);
     else asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(pair_address(bar, rank)) : "memory");
 }
+// The same where only the end of reads is announced (an accumulator or a unit's slot may be written again): without the
+// release at cluster scope, which waits for the thread's stores to global memory, 3 us after the logits of a tile (int8,
+// 1024 rows K 1024 142 -> 129 us).  What has been read is in registers by then: tcgen05.wait::ld, or a use of it.
+template <int kCtas>
+__device__ __forceinline__ void pair_arrive_read(uint64_t* bar, uint32_t rank)
+{
+    if (kCtas == 1) mbar_arrive(bar);
+    else asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(pair_address(bar, rank)) : "memory");
+}
 // bounded wait on a barrier of this CTA that the other CTA may arrive on
 template <int kCtas>
 __device__ __forceinline__ bool pair_wait(uint64_t* bar, uint32_t parity)
@@ -502,7 +511,7 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
         auto release = [&]() {
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) pair_arrive<kCtas>(&S.acc_empty[t & 1], 0);
+            if (lane == 0) pair_arrive_read<kCtas>(&S.acc_empty[t & 1], 0);
             ++t;
         };
         // the labels' logits, while the first tile is being computed: in the gather launch they cost 2 us of 59
@@ -929,7 +938,7 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
             }
             const int4 u0 = S.unit[slot][0], u1 = S.unit[slot][1];
             __syncwarp();
-            if (lane == 0) pair_arrive<kCtas>(&S.unit_empty[slot], 0);
+            if (lane == 0 && u0.x >= 0 && u1.x >= 0) pair_arrive_read<kCtas>(&S.unit_empty[slot], 0);      // always: both have been read
             if (++slot == kUnitSlots) { slot = 0; sph ^= 1u; }
             const int kind = u0.x, row0 = u0.y + (int)rank * kHeadM + q * 32, n0 = u0.z, p = u1.y;
             const bool any = u0.w < u1.x;
@@ -1061,7 +1070,7 @@ lm_head_backward_kernel(const __grid_constant__ BackParams P, const __grid_const
             if (kind != kGradWeight) fence_proxy_async_all();
             __syncwarp();
             if (lane == 0) {
-                if (any) pair_arrive<kCtas>(&S.acc_empty[acc], 0);
+                if (any) pair_arrive_read<kCtas>(&S.acc_empty[acc], 0);
                 // Nobody in this launch reads dW: what is counted for it is that G has been read.  (The fence waits for the
                 // stores: a microsecond or two, as long as a short unit's products take.)
                 if (kind != kGradWeight) __threadfence();
@@ -1560,10 +1569,12 @@ int dspark_lm_head_int8(const int8_t* x_q, int64_t x_row_stride, const float* x_
     HeadParams P;
     memset(&P, 0, sizeof P);
     P.m = V; P.n = rows; P.k = K;
-    // Pairs where the products bound the call, single CTAs where the weight's bytes or the stores do (V = 129 280, single /
-    // pair, us: 352 rows K 1024 61 / 66, 1024 rows K 1024 142 / 142, 1482 rows K 512 139 / 161; 500 rows K 1536 101 / 94,
-    // 200 rows K 2048 67 / 63, 1482 rows K 4096 597 / 558; up to 128 rows the weight bounds it at any K).
-    const int ctas = rows > kHeadM && K > 1024 ? 2 : 1;
+    // Pairs where the copies from the L2 bound the call, single CTAs where the weight's bytes or the stores do, or the call is
+    // too short for the 3 us that a launch of pairs takes longer.  Single / pair, us: V = 129 280, K 512 256 rows 33 / 32,
+    // 1482 rows 136 / 137; K 768 256 rows 39 / 36, 1482 rows 168 / 164; K 1024 129 rows 35 / 35, 256 rows 46 / 39, 352 rows
+    // (pairs' tiles are multiples of 32) 60 / 62, 500 rows 75 / 69, 1482 rows 201 / 185; K 4096 1482 rows 732 / 591.
+    // V = 32 000, K 1024 256 rows 18 / 20, 500 rows 26 / 23; K 1536 129 rows 18 / 17; V = 16 000, K 1024 512 rows 16 / 16.
+    const int ctas = rows > kHeadM && (K > 1024 || (K >= 768 && (double)rows * V * K > 1.2e10)) ? 2 : 1;
     // row tiles of one size, and no taller a box than there are rows (one row of 32 in a box: 170 us instead of 84 at
     // K = 4 096)
     const int row_tiles = (rows + kHeadN - 1) / kHeadN;

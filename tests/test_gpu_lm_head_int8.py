@@ -44,6 +44,12 @@ def test_sizes(dtype, n, V, K):
     check(*operands(n, V, K, n + V + K), dtype, out_pad=3)
 
 
+@pytest.mark.parametrize("n,V,K", [(700, 20001, 900), (1482, 9000, 1001), (300, 60000, 768), (130, 129280, 767)])
+def test_pairs_by_the_size_of_the_product(n, V, K):
+    # on either side of the rule that gives rows of up to 1 024 entries to pairs of CTAs
+    check(*operands(n, V, K, n + V + K), torch.bfloat16, out_pad=1)
+
+
 @pytest.mark.parametrize("live", [0, 1, 31, 256, 257, 300, 1000])
 def test_rows_behind_the_last_one_are_left(live):
     check(*operands(300, 700, 200, 3), torch.bfloat16, live=live)
