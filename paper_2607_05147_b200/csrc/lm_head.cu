@@ -260,7 +260,8 @@ __device__ __forceinline__ void store_pairs16(__nv_bfloat16* p, long long stride
 // the sum (d = 2 048: -1.3e-5 on a logit of 6, 9.7e-7 of the loss).  Sums are therefore cut into accumulators of 512 terms
 // for many rows (3.0e-7 of the loss, with fp32 products 3.2e-7; 4096 rows 1.35 -> 1.42 ms) or 256 for few (64 rows 57 ->
 // 60 us) that are added up here, rounded.  The gradients need no such care: a probability is only relatively off.
-__device__ __forceinline__ void add_accumulator(float (&z)[kHeadGroups][32], uint32_t address, bool first)
+// `groups`: how many of the groups the tile has.
+__device__ __forceinline__ void add_accumulator(float (&z)[kHeadGroups][32], uint32_t address, bool first, int groups)
 {
     __syncwarp();
     if (first) {
@@ -271,6 +272,7 @@ __device__ __forceinline__ void add_accumulator(float (&z)[kHeadGroups][32], uin
     } else {
 #pragma unroll
         for (int j = 0; j < kHeadGroups; ++j) {
+            if (j >= groups) break;
             float v[32];
             tmem_load32_issue(address + (uint32_t)(j * kHeadParts * 32), v);
             tmem_load_wait(v);
@@ -584,10 +586,11 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
                 release();
             } else {
                 float z[kHeadGroups][32];
+                const int groups = (chunks - part + kHeadParts - 1) / kHeadParts, end = n < n0 + P.n_tile ? n : n0 + P.n_tile;
                 for (int k0 = 0; k0 < k_blocks; k0 += kPerAcc) {
                     take(acc_addr);
                     if (!ok) break;
-                    if (row0 < m) add_accumulator(z, acc_addr + (uint32_t)(part * 32), k0 == 0);
+                    if (row0 < m) add_accumulator(z, acc_addr + (uint32_t)(part * 32), k0 == 0, groups);
                     release();
                 }
                 if (!ok) break;
@@ -603,10 +606,10 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
                             for (int i = 0; i < 32; ++i)
                                 if (label == col0 + i) z[j][i] = -INFINITY;
                         }
-                        if (n - col0 < 32) {
+                        if (end - col0 < 32) {
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
-                                if (i >= n - col0) z[j][i] = -INFINITY;
+                                if (i >= end - col0) z[j][i] = -INFINITY;
                         }
 #pragma unroll
                         for (int i = 0; i < 32; ++i) top = fmaxf(top, z[j][i]);
@@ -615,7 +618,8 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
                     const uint64_t sc = pack2(kLog2e, kLog2e), no = pack2(-base, -base);
                     uint64_t a = pack2(0.f, 0.f), b = pack2(0.f, 0.f);
 #pragma unroll
-                    for (int j = 0; j < kHeadGroups; ++j)
+                    for (int j = 0; j < kHeadGroups; ++j) {
+                        if (j >= groups) break;
 #pragma unroll
                         for (int i = 0; i < 32; i += 4) {
                             float t0, t1, t2, t3;
@@ -624,6 +628,7 @@ lm_head_kernel(const __grid_constant__ HeadParams P, const __grid_constant__ CUt
                             a = add2(a, pack2(ex2_approx(t0), ex2_approx(t1)));
                             b = add2(b, pack2(ex2_approx(t2), ex2_approx(t3)));
                         }
+                    }
                     float s0, s1;
                     unpack2(add2(a, b), s0, s1);
                     sum = s0 + s1;
@@ -1474,13 +1479,21 @@ constexpr long long kPieceBytes = 32ll << 20;
 struct LossWs {
     size_t live, sync, first, idx, label, at_label, lse, grad, label_err, rows, stats, G, part, total;
     long long n_pad, d_pitch, part_pitch;
-    int ctas, piece, pieces, n_sync, slices, kb_slice, n_tile_d, d_tiles;
+    int ctas, n_tile, piece, pieces, n_sync, slices, kb_slice, n_tile_d, d_tiles;
 };
 static LossWs loss_layout(int N, int V, int d)
 {
     LossWs w;
     w.ctas = N > kHeadM ? 2 : 1;                            // one row tile of 128 rows: the second CTA of a pair would hold none
     w.n_pad = (long long)up((size_t)N, w.ctas * kHeadM);
+    // Vocabulary entries of a tile of the statistics: for up to 128 rows narrower than 256 where few rounds of tiles over the
+    // SMs leave many of them idle in the last one, by at least 1/16.  256 / this rule, us: 64 rows V 129 280 d 1024 57.8 /
+    // 55.7, V 151 936 68.8 / 65.7, V 50 257 d 768 27.2 / 25.7, V 10 007 d 500 14.3 / 13.0.  (Pairs read B once for both rows
+    // of tiles and lose by it: 600 rows V 40 000 d 300 32.8 / 43.6.)
+    auto rounds = [&](int tile) { return ((V + tile - 1) / tile + 147) / 148 * tile; };
+    w.n_tile = kHeadN;
+    for (int tile = kHeadN - 32; w.ctas == 1 && tile >= 128; tile -= 32)
+        if (rounds(tile) * 16ll <= rounds(w.n_tile) * 15ll) w.n_tile = tile;
     w.d_pitch = (long long)up((size_t)d, 64);               // whole blocks of columns (block_map)
     w.part_pitch = (long long)up((size_t)d, 8);
     w.n_tile_d = d >= kHeadN ? kHeadN : (int)up((size_t)d, 64 * w.ctas);
@@ -1519,7 +1532,7 @@ static LossWs loss_layout(int N, int V, int d)
     w.rows = take(2 * (size_t)w.n_pad * (size_t)w.d_pitch);
     const size_t common = o;
     // forward: two entries per vocabulary tile and row
-    w.stats = take(2 * up((size_t)V, kHeadN) / kHeadN * (size_t)w.n_pad * sizeof(float2));
+    w.stats = take((size_t)kHeadParts * up((size_t)V, w.n_tile) / w.n_tile * (size_t)w.n_pad * sizeof(float2));
     const size_t forward = o;
     // backward: three pieces of G, the slices' sums
     o = common;
@@ -1621,7 +1634,7 @@ int dspark_lm_head_loss(const void* hidden, int64_t hidden_row_stride, const voi
     HeadParams P;
     memset(&P, 0, sizeof P);
     P.m = N; P.n = V; P.k = d;
-    P.n_tile = kHeadN; P.box_n = V < kHeadN / w.ctas ? V : kHeadN / w.ctas;
+    P.n_tile = w.n_tile; P.box_n = V < w.n_tile / w.ctas ? V : w.n_tile / w.ctas;
     P.live = g.live; P.dev_status = dev_status;
     P.stats = (float2*)(ws + w.stats); P.stats_stride = w.n_pad; P.labels = g.label; P.z_label = (float*)(ws + w.at_label);
     P.rows = g.rows; P.rows_stride = w.d_pitch; P.w = (const __nv_bfloat16*)weight; P.w_stride = weight_row_stride;
@@ -1631,7 +1644,7 @@ int dspark_lm_head_loss(const void* hidden, int64_t hidden_row_stride, const voi
     const int rc = w.ctas == 2 ? head_launch<kLossStats, 2>(P, a, b, s, DSPARK_K_HEAD_LOSS) : head_launch<kLossStats, 1>(P, a, b, s, DSPARK_K_HEAD_LOSS);
     if (rc != DSPARK_OK) return rc;
     LossParams L;
-    L.stats = P.stats; L.stats_stride = w.n_pad; L.entries = 2 * ((V + kHeadN - 1) / kHeadN);
+    L.stats = P.stats; L.stats_stride = w.n_pad; L.entries = kHeadParts * ((V + w.n_tile - 1) / w.n_tile);
     L.z_label = P.z_label; L.idx = g.idx; L.live = g.live; L.loss = out_loss; L.lse = out_lse; L.dev_status = dev_status;
     {
         KernelTimerScope timer(DSPARK_K_HEAD_ROWS, s);

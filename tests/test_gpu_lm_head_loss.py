@@ -123,6 +123,12 @@ def test_pitches_of_the_weight_gradient(d, pad):
     check(*make(40, 333, d, 21), pads=(pad, pad))
 
 
+@pytest.mark.parametrize("V", [18944, 28417, 33153, 40001, 76000])
+def test_narrower_tiles_of_the_statistics(V):
+    # vocabularies for which few rows take tiles of 128 (all whole), 224, 256, 160 (one entry in the last) and 192 entries
+    check(*make(90, V, 72, 23, ignored=0.1))
+
+
 def test_every_row_ignored():
     h, w, labels, gl = make(70, 600, 64, 9)
     labels[:] = -1
