@@ -1243,8 +1243,8 @@ static void gather_launch(const GatherParams& g, cudaStream_t s)
 }
 
 // ---- loss of every row from the statistics of the vocabulary tiles --------------------------------------
-// Eight rows per CTA, 128 threads per row, each taking every 128th entry (eight loads in flight): at V = 129 280 a row has
-// 1 010 entries.  loss = log(1 + T e^(R - z)), lse = z + loss, with z the label's logit and T = sum s_i e^(r_i - R) over the
+// Eight rows per CTA, 128 threads per row, each taking every 128th entry (eight loads in flight; ten: no faster): at
+// V = 129 280 a row has 1 010 to 1 156 entries.  loss = log(1 + T e^(R - z)), lse = z + loss, with z the label's logit and T = sum s_i e^(r_i - R) over the
 // other entries, R the largest r_i; the sum over threads and the rest in 64 bits.
 struct LossParams {
     const float2* stats; long long stats_stride; int entries;
