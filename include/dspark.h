@@ -550,7 +550,7 @@ int dspark_lm_head_int8(const int8_t* x_q, int64_t x_row_stride, const float* x_
  * slices are fp32 in a fixed order: the same inputs give the same bits.  A row whose loss is not finite sets DSPARK_DEV_BAD_ROW; its
  * loss and gradients are what the arithmetic gives (NaN reaches grad_weight, as in the formula).
  * Limits: N <= 2^20, V <= 2^24, d <= 65 536.  Errors: INVALID_ARG, SHAPE, ALIGNMENT, WORKSPACE, CUDA.
- * Resources (all three contractions): one CTA per SM with 193 KB of shared memory, all 512 tensor-memory columns of the SM;
+ * Resources (all three contractions): one CTA per SM with 193 to 210 KB of shared memory, all 512 tensor-memory columns of the SM;
  * a wait that ran out sets DSPARK_DEV_TIMEOUT in *dev_status and the outputs are unspecified.
  */
 size_t dspark_lm_head_loss_workspace_bytes(int N, int V, int d);
