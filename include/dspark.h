@@ -542,7 +542,8 @@ int dspark_lm_head_int8(const int8_t* x_q, int64_t x_row_stride, const float* x_
  *   grad_loss      device fp32 [N]: dL / dloss[n] -- the weights of a mean or of the block's positions
  *   out_grad_hidden device bf16 [N, >= d], out_grad_weight device bf16 [V, >= d]: any row stride, written (not added to);
  *                  either may be NULL, not both
- *   workspace      dspark_lm_head_loss_workspace_bytes(N, V, d), 256-byte aligned, any content; one call at a time
+ *   workspace      dspark_lm_head_loss_workspace_bytes(N, V, d), 256-byte aligned, any content; one call at a time.  The
+ *                  size never falls as N rises: a workspace for the largest batch does for every smaller one
  * Products are bf16 with fp32 accumulation (the logits' sums in runs of at most 512 terms, added up in fp32), softmax
  * statistics fp32 (combined in fp64).  The label's logit is summed in fp32 on its own and the loss is log(1 + sum over the
  * other entries of e^(z - z[label])), so a row that is sure of its label keeps the digits of its small loss and gradient.  G is rounded to bf16 for its two products; what that loses of the labels' entries is

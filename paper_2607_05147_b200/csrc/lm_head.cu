@@ -1606,7 +1606,14 @@ int dspark_lm_head_int8(const int8_t* x_q, int64_t x_row_stride, const float* x_
 size_t dspark_lm_head_loss_workspace_bytes(int N, int V, int d)
 {
     if (N < 1 || V < 1 || d < 1 || N > kMaxRows || V > kMaxVocab || d > kMaxWidth) return 0;
-    return loss_layout(N, V, d).total;
+    // The layout of fewer rows may be larger (longer pieces, more slices of dH's sums), so the answer is the largest over all
+    // row counts up to N.  A layout depends on the rows only through n_pad, and through one row tile or pairs of them.
+    size_t most = loss_layout(N, V, d).total;
+    for (int n = kHeadM; n < N; n += n == kHeadM ? kHeadM : 2 * kHeadM) {
+        const size_t bytes = loss_layout(n, V, d).total;
+        if (bytes > most) most = bytes;
+    }
+    return most;
 }
 
 int dspark_lm_head_loss(const void* hidden, int64_t hidden_row_stride, const void* weight, int64_t weight_row_stride,
