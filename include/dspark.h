@@ -527,7 +527,7 @@ int dspark_lm_head_int8(const int8_t* x_q, int64_t x_row_stride, const float* x_
                         const float* w_scale, int rows, int V, int K, const int32_t* n_live, void* out_logits, int out_dtype,
                         int64_t out_row_stride, int32_t* dev_status, void* stream);
 
-/* dspark_lm_head_loss, dspark_lm_head_loss_backward -- softmax cross entropy of hidden states against the vocabulary, in
+/* dspark_lm_head_loss, dspark_lm_head_loss_backward, dspark_lm_head_loss_backward_from_loss -- softmax cross entropy of hidden states against the vocabulary, in
  * pieces of the vocabulary, without keeping the logits:
  *     z = hidden weight^T,   lse[n] = log sum_v exp z[n, v],   loss[n] = lse[n] - z[n, labels[n]],
  *     G[n, v] = grad_loss[n] (exp(z[n, v] - lse[n]) - [v = labels[n]]),
@@ -538,7 +538,7 @@ int dspark_lm_head_int8(const int8_t* x_q, int64_t x_row_stride, const float* x_
  *                  row holds (padding, NaN) reaches grad_weight; it costs no work.  A label >= V is ignored the same way
  *                  and sets DSPARK_DEV_BAD_TOKEN.
  *   out_loss, out_lse   device fp32 [N]
- *   lse            device fp32 [N]: what the forward call left (entries of ignored rows are not used)
+ *   lse, loss      device fp32 [N]: what the forward call left in out_lse and out_loss (entries of ignored rows are not used)
  *   grad_loss      device fp32 [N]: dL / dloss[n] -- the weights of a mean or of the block's positions
  *   out_grad_hidden device bf16 [N, >= d], out_grad_weight device bf16 [V, >= d]: any row stride, written (not added to);
  *                  either may be NULL, not both
@@ -546,8 +546,12 @@ int dspark_lm_head_int8(const int8_t* x_q, int64_t x_row_stride, const float* x_
  *                  size never falls as N rises: a workspace for the largest batch does for every smaller one
  * Products are bf16 with fp32 accumulation (the logits' sums in runs of at most 512 terms, added up in fp32), softmax
  * statistics fp32 (combined in fp64).  The label's logit is summed in fp32 on its own and the loss is log(1 + sum over the
- * other entries of e^(z - z[label])), so a row that is sure of its label keeps the digits of its small loss and gradient.  G is rounded to bf16 for its two products; what that loses of the labels' entries is
- * added back to both gradients in fp32, which are then off by about their own rounding to bf16.  Sums over pieces and
+ * other entries of e^(z - z[label])), so a row that is sure of its label keeps the digits of its small loss.  Its gradient
+ * keeps them where the backward call is given the loss (_from_loss: the label's entry of G is grad_loss expm1(-loss));
+ * from lse alone that entry is grad_loss expm1(z[label] - lse), off by what fp32 holds of lse, about
+ * 2^-24 |lse| grad_loss (1e-6 at lse = 20), however small the loss.  G is rounded to bf16 for its two products; what that
+ * loses of the labels' entries is added back to both gradients in fp32, which are then off by about their own rounding to
+ * bf16.  Sums over pieces and
  * slices are fp32 in a fixed order: the same inputs give the same bits.  A row whose loss is not finite sets DSPARK_DEV_BAD_ROW; its
  * loss and gradients are what the arithmetic gives (NaN reaches grad_weight, as in the formula).
  * Limits: N <= 2^20, V <= 2^24, d <= 65 536.  Errors: INVALID_ARG, SHAPE, ALIGNMENT, WORKSPACE, CUDA.
@@ -563,6 +567,11 @@ int dspark_lm_head_loss_backward(const void* hidden, int64_t hidden_row_stride, 
                                  void* out_grad_hidden, int64_t grad_hidden_row_stride, void* out_grad_weight,
                                  int64_t grad_weight_row_stride, int32_t* dev_status, void* workspace, size_t workspace_bytes,
                                  void* stream);
+int dspark_lm_head_loss_backward_from_loss(const void* hidden, int64_t hidden_row_stride, const void* weight, int64_t weight_row_stride,
+                                           const int32_t* labels, const float* lse, const float* loss, const float* grad_loss, int N,
+                                           int V, int d, void* out_grad_hidden, int64_t grad_hidden_row_stride, void* out_grad_weight,
+                                           int64_t grad_weight_row_stride, int32_t* dev_status, void* workspace,
+                                           size_t workspace_bytes, void* stream);
 
 /* The two uniforms of (seed, request, position) exactly as the verifier draws them
  * (host computation; for tests and for replaying a step). */

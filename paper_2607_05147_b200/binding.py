@@ -39,6 +39,7 @@ EXPORTS = [
     "dspark_sts_workspace_bytes", "dspark_sts_calibrate", "dspark_sts_apply",
     "dspark_rms_norm_quant", "dspark_lm_head_quantize", "dspark_lm_head_int8",
     "dspark_lm_head_loss_workspace_bytes", "dspark_lm_head_loss", "dspark_lm_head_loss_backward",
+    "dspark_lm_head_loss_backward_from_loss",
     "dspark_ktimer_create", "dspark_ktimer_destroy", "dspark_ktimer_attach", "dspark_ktimer_reset",
     "dspark_ktimer_read", "dspark_set_stream_path", "dspark_set_wait_poll_limit", "dspark_status_string", "dspark_kernel_name",
     "dspark_version",
@@ -115,6 +116,7 @@ def lib() -> C.CDLL:
         L.dspark_lm_head_loss_workspace_bytes.argtypes = [i32, i32, i32]
         L.dspark_lm_head_loss_workspace_bytes.restype = sz
         L.dspark_lm_head_loss.argtypes = [vp, i64, vp, i64, vp, i32, i32, i32, vp, vp, vp, vp, sz, vp]
+        L.dspark_lm_head_loss_backward_from_loss.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, i32, i32, i32, vp, i64, vp, i64, vp, vp, sz, vp]
         L.dspark_lm_head_loss_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, i32, i32, i32, vp, i64, vp, i64, vp, vp, sz, vp]
         L.dspark_uniforms.argtypes = [u64, C.c_uint32, C.c_uint32, C.POINTER(C.c_float), C.POINTER(C.c_float)]
         L.dspark_uniforms.restype = None
@@ -745,16 +747,23 @@ def dspark_lm_head_loss(hidden: torch.Tensor, weight: torch.Tensor, labels: torc
 
 
 def dspark_lm_head_loss_backward(hidden: torch.Tensor, weight: torch.Tensor, labels: torch.Tensor, lse: torch.Tensor,
-                                 grad_loss: torch.Tensor, *, out_grad_hidden: Optional[torch.Tensor] = None,
-                                 out_grad_weight: Optional[torch.Tensor] = None, dev_status: torch.Tensor,
-                                 workspace: torch.Tensor) -> None:
-    """Gradients of sum_n grad_loss[n] * loss[n]; lse: what dspark_lm_head_loss left for the same rows."""
+                                 grad_loss: torch.Tensor, *, loss: Optional[torch.Tensor] = None,
+                                 out_grad_hidden: Optional[torch.Tensor] = None, out_grad_weight: Optional[torch.Tensor] = None,
+                                 dev_status: torch.Tensor, workspace: torch.Tensor) -> None:
+    """Gradients of sum_n grad_loss[n] * loss[n]; lse: what dspark_lm_head_loss left for the same rows.
+
+    loss: what the same call left in out_loss.  With it (dspark_lm_head_loss_backward_from_loss) the gradient of a row that
+    is sure of its label keeps the digits of its small loss; lse alone holds 1 - softmax to about 2^-24 |lse|."""
     head, N, V, d, dev = _loss_args(hidden, weight, labels)
     hp, hs = _rows(out_grad_hidden, "out_grad_hidden", torch.bfloat16, N, d, dev)
     wp, ws = _rows(out_grad_weight, "out_grad_weight", torch.bfloat16, V, d, dev)
-    rc = lib().dspark_lm_head_loss_backward(*head, _vec(_need(lse, "lse"), "lse", torch.float32, N, dev),
-                                            _vec(_need(grad_loss, "grad_loss"), "grad_loss", torch.float32, N, dev), N, V, d, hp, hs, wp, ws,
-                                            *_loss_scratch(dev_status, workspace, dev))
+    lp = _vec(_need(lse, "lse"), "lse", torch.float32, N, dev)
+    gp = _vec(_need(grad_loss, "grad_loss"), "grad_loss", torch.float32, N, dev)
+    tail = (gp, N, V, d, hp, hs, wp, ws, *_loss_scratch(dev_status, workspace, dev))
+    if loss is None:
+        rc = lib().dspark_lm_head_loss_backward(*head, lp, *tail)
+    else:
+        rc = lib().dspark_lm_head_loss_backward_from_loss(*head, lp, _vec(loss, "loss", torch.float32, N, dev), *tail)
     _check(rc, "dspark_lm_head_loss_backward")
 
 

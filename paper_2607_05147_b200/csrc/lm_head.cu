@@ -1100,6 +1100,7 @@ struct GatherParams {
     int32_t* first;                                 // backward: [V]
     float* loss; float* lse;                        // forward: zeros of the ignored rows
     const float* lse_in; const float* grad_in; float* grad;    // backward (lse: the compact rows', times log2(e))
+    const float* loss_in;                           // backward: the rows' losses, or NULL
     const __nv_bfloat16* w; long long w_stride;     // backward
     float* at_label; float* label_err;              // backward: the label's entry of G, and what is lost when it is rounded to bf16
     __nv_bfloat16* dh; long long dh_stride;         // backward: zeros of the ignored rows
@@ -1152,10 +1153,16 @@ __global__ void __launch_bounds__(kGatherThreads) lm_head_gather_kernel(const __
         for (int j = 0; j < kGatherRows / (kGatherThreads / 32); ++j) {
             const int r = warp + j * (kGatherThreads / 32), label = s_label[r];
             if ((unsigned)label >= V) continue;
-            const float lse = P.lse_in[r0 + r], g = P.grad_in[r0 + r];
-            const __nv_bfloat16* h = P.h + (long long)(r0 + r) * P.h_stride;
-            const __nv_bfloat16* w = P.w + (long long)label * P.w_stride;
-            const float x = (vectors ? label_logit<true>(h, w, P.d, lane) : label_logit<false>(h, w, P.d, lane)) - lse;
+            const float g = P.grad_in[r0 + r];
+            float x;                                        // the logarithm of the label's probability
+            if (P.loss_in) {
+                x = -P.loss_in[r0 + r];
+            } else {
+                // lse holds it to half a unit of its own last place and no better (losses of 1e-5 at a logit of 13: 4.6 % off)
+                const __nv_bfloat16* h = P.h + (long long)(r0 + r) * P.h_stride;
+                const __nv_bfloat16* w = P.w + (long long)label * P.w_stride;
+                x = (vectors ? label_logit<true>(h, w, P.d, lane) : label_logit<false>(h, w, P.d, lane)) - P.lse_in[r0 + r];
+            }
             at_label[j] = expm1f(x > 0.f ? 0.f : x) * g;
         }
     // every row's place: the rows that come before it
@@ -1552,6 +1559,74 @@ static int loss_check(const void* hidden, int64_t h_stride, const void* weight, 
     return DSPARK_OK;
 }
 
+// Both backward calls; loss NULL: the label's entry of G from lse.
+static int loss_backward(const void* hidden, int64_t hidden_row_stride, const void* weight, int64_t weight_row_stride,
+                         const int32_t* labels, const float* lse, const float* loss, const float* grad_loss, int N, int V, int d,
+                         void* out_grad_hidden, int64_t grad_hidden_row_stride, void* out_grad_weight,
+                         int64_t grad_weight_row_stride, int32_t* dev_status, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!lse || !grad_loss || (!out_grad_hidden && !out_grad_weight) || N < 1 || V < 1 || d < 1) return DSPARK_ERR_INVALID_ARG;
+    if ((out_grad_hidden && grad_hidden_row_stride < d) || (out_grad_weight && grad_weight_row_stride < d)) return DSPARK_ERR_INVALID_ARG;
+    if (N > kMaxRows || V > kMaxVocab || d > kMaxWidth) return DSPARK_ERR_SHAPE;
+    const LossWs w = loss_layout(N, V, d);
+    const int rc0 = loss_check(hidden, hidden_row_stride, weight, weight_row_stride, labels, N, V, d, dev_status, workspace, workspace_bytes, w);
+    if (rc0 != DSPARK_OK) return rc0;
+    if ((((uintptr_t)lse | (uintptr_t)loss | (uintptr_t)grad_loss) & 3u) || (((uintptr_t)out_grad_hidden | (uintptr_t)out_grad_weight) & 1u))
+        return DSPARK_ERR_ALIGNMENT;
+    unsigned char* ws = (unsigned char*)workspace;
+    cudaStream_t s = (cudaStream_t)stream;
+    GatherParams g;
+    memset(&g, 0, sizeof g);
+    g.h = (const __nv_bfloat16*)hidden; g.h_stride = hidden_row_stride; g.labels = labels; g.N = N; g.V = V; g.d = d;
+    g.rows = (__nv_bfloat16*)(ws + w.rows); g.rows_stride = w.d_pitch;
+    g.live = (int32_t*)(ws + w.live); g.idx = (int32_t*)(ws + w.idx); g.label = (int32_t*)(ws + w.label);
+    g.lse_in = lse; g.loss_in = loss; g.grad_in = grad_loss; g.lse = (float*)(ws + w.lse); g.grad = (float*)(ws + w.grad);
+    g.w = (const __nv_bfloat16*)weight; g.w_stride = weight_row_stride;
+    g.at_label = (float*)(ws + w.at_label); g.label_err = (float*)(ws + w.label_err);
+    g.sync = (int32_t*)(ws + w.sync); g.n_sync = w.n_sync; g.first = (int32_t*)(ws + w.first);
+    g.dh = (__nv_bfloat16*)out_grad_hidden; g.dh_stride = grad_hidden_row_stride; g.dev_status = dev_status;
+    {
+        KernelTimerScope timer(DSPARK_K_HEAD_ROWS, s);
+        gather_launch<true>(g, s);
+    }
+    BackMaps M;
+    const int box_v = V < kHeadN / w.ctas ? V : kHeadN / w.ctas;
+    const long long g_pitch = (long long)w.piece * 2;
+    if (!operand_map(&M.rows_k, g.rows, 2, w.n_pad, d, w.d_pitch * 2, 64, kHeadM) ||
+        !operand_map(&M.w_k, weight, 2, V, d, weight_row_stride * 2, 64, box_v) ||
+        !operand_map(&M.g_k, ws + w.G, 2, 3 * w.n_pad, w.piece, g_pitch, 64, kHeadM) ||
+        !(d % 64 == 0 ? block_map(&M.w_mn, weight, V, d, weight_row_stride * 2, 64, w.n_tile_d / w.ctas / 64)
+                      : operand_map(&M.w_mn, weight, 2, V, d, weight_row_stride * 2, 64, 64)) ||
+        !block_map(&M.g_mn, ws + w.G, 3 * w.n_pad, w.piece, g_pitch, 64, kHeadM / 64) ||
+        !block_map(&M.rows_mn, g.rows, w.n_pad, d, w.d_pitch * 2, 64, w.n_tile_d / w.ctas / 64))
+        return DSPARK_ERR_CUDA;
+    BackParams P;
+    memset(&P, 0, sizeof P);
+    P.n_pad = (int)w.n_pad; P.V = V; P.d = d;
+    P.piece = w.piece; P.pieces = w.pieces; P.n_tile_d = w.n_tile_d; P.d_tiles = w.d_tiles;
+    P.slices = w.slices; P.kb_slice = w.kb_slice;
+    P.box_v = box_v; P.w_blocks = d % 64 == 0;
+    P.want_h = out_grad_hidden != nullptr; P.want_w = out_grad_weight != nullptr;
+    P.live = g.live; P.dev_status = dev_status; P.sync = g.sync;
+    P.G = (__nv_bfloat16*)(ws + w.G);
+    P.labels = g.label; P.lse2 = g.lse; P.grad = g.grad; P.at_label = g.at_label; P.label_err = g.label_err;
+    P.first = g.first; P.rows = g.rows; P.rows_stride = w.d_pitch;
+    P.part = (float*)(ws + w.part); P.part_stride = w.part_pitch;
+    P.dw = (__nv_bfloat16*)out_grad_weight; P.dw_stride = grad_weight_row_stride;
+    const int rc = w.ctas == 2 ? back_launch<2>(P, M, s) : back_launch<1>(P, M, s);
+    if (rc != DSPARK_OK) return rc;
+    if (out_grad_hidden) {
+        HiddenParams Hp;
+        Hp.part = (const float*)(ws + w.part); Hp.part_stride = w.part_pitch; Hp.slices = w.slices; Hp.m = (int)w.n_pad;
+        Hp.label_err = g.label_err; Hp.label = g.label; Hp.idx = g.idx; Hp.live = g.live;
+        Hp.w = (const __nv_bfloat16*)weight; Hp.w_stride = weight_row_stride; Hp.d = d;
+        Hp.dh = g.dh; Hp.dh_stride = grad_hidden_row_stride;
+        KernelTimerScope timer(DSPARK_K_HEAD_ROWS, s);
+        launch_pdl(lm_head_grad_hidden_kernel, dim3(N, (d + 4 * kHiddenThreads - 1) / (4 * kHiddenThreads)), dim3(kHiddenThreads), 0, s, Hp);
+    }
+    return launch_status();
+}
+
 }  // namespace dspark
 
 using namespace dspark;
@@ -1666,66 +1741,19 @@ int dspark_lm_head_loss_backward(const void* hidden, int64_t hidden_row_stride, 
                                  int64_t grad_weight_row_stride, int32_t* dev_status, void* workspace, size_t workspace_bytes,
                                  void* stream)
 {
-    if (!lse || !grad_loss || (!out_grad_hidden && !out_grad_weight) || N < 1 || V < 1 || d < 1) return DSPARK_ERR_INVALID_ARG;
-    if ((out_grad_hidden && grad_hidden_row_stride < d) || (out_grad_weight && grad_weight_row_stride < d)) return DSPARK_ERR_INVALID_ARG;
-    if (N > kMaxRows || V > kMaxVocab || d > kMaxWidth) return DSPARK_ERR_SHAPE;
-    const LossWs w = loss_layout(N, V, d);
-    const int rc0 = loss_check(hidden, hidden_row_stride, weight, weight_row_stride, labels, N, V, d, dev_status, workspace, workspace_bytes, w);
-    if (rc0 != DSPARK_OK) return rc0;
-    if ((((uintptr_t)lse | (uintptr_t)grad_loss) & 3u) || (((uintptr_t)out_grad_hidden | (uintptr_t)out_grad_weight) & 1u))
-        return DSPARK_ERR_ALIGNMENT;
-    unsigned char* ws = (unsigned char*)workspace;
-    cudaStream_t s = (cudaStream_t)stream;
-    GatherParams g;
-    memset(&g, 0, sizeof g);
-    g.h = (const __nv_bfloat16*)hidden; g.h_stride = hidden_row_stride; g.labels = labels; g.N = N; g.V = V; g.d = d;
-    g.rows = (__nv_bfloat16*)(ws + w.rows); g.rows_stride = w.d_pitch;
-    g.live = (int32_t*)(ws + w.live); g.idx = (int32_t*)(ws + w.idx); g.label = (int32_t*)(ws + w.label);
-    g.lse_in = lse; g.grad_in = grad_loss; g.lse = (float*)(ws + w.lse); g.grad = (float*)(ws + w.grad);
-    g.w = (const __nv_bfloat16*)weight; g.w_stride = weight_row_stride;
-    g.at_label = (float*)(ws + w.at_label); g.label_err = (float*)(ws + w.label_err);
-    g.sync = (int32_t*)(ws + w.sync); g.n_sync = w.n_sync; g.first = (int32_t*)(ws + w.first);
-    g.dh = (__nv_bfloat16*)out_grad_hidden; g.dh_stride = grad_hidden_row_stride; g.dev_status = dev_status;
-    {
-        KernelTimerScope timer(DSPARK_K_HEAD_ROWS, s);
-        gather_launch<true>(g, s);
-    }
-    BackMaps M;
-    const int box_v = V < kHeadN / w.ctas ? V : kHeadN / w.ctas;
-    const long long g_pitch = (long long)w.piece * 2;
-    if (!operand_map(&M.rows_k, g.rows, 2, w.n_pad, d, w.d_pitch * 2, 64, kHeadM) ||
-        !operand_map(&M.w_k, weight, 2, V, d, weight_row_stride * 2, 64, box_v) ||
-        !operand_map(&M.g_k, ws + w.G, 2, 3 * w.n_pad, w.piece, g_pitch, 64, kHeadM) ||
-        !(d % 64 == 0 ? block_map(&M.w_mn, weight, V, d, weight_row_stride * 2, 64, w.n_tile_d / w.ctas / 64)
-                      : operand_map(&M.w_mn, weight, 2, V, d, weight_row_stride * 2, 64, 64)) ||
-        !block_map(&M.g_mn, ws + w.G, 3 * w.n_pad, w.piece, g_pitch, 64, kHeadM / 64) ||
-        !block_map(&M.rows_mn, g.rows, w.n_pad, d, w.d_pitch * 2, 64, w.n_tile_d / w.ctas / 64))
-        return DSPARK_ERR_CUDA;
-    BackParams P;
-    memset(&P, 0, sizeof P);
-    P.n_pad = (int)w.n_pad; P.V = V; P.d = d;
-    P.piece = w.piece; P.pieces = w.pieces; P.n_tile_d = w.n_tile_d; P.d_tiles = w.d_tiles;
-    P.slices = w.slices; P.kb_slice = w.kb_slice;
-    P.box_v = box_v; P.w_blocks = d % 64 == 0;
-    P.want_h = out_grad_hidden != nullptr; P.want_w = out_grad_weight != nullptr;
-    P.live = g.live; P.dev_status = dev_status; P.sync = g.sync;
-    P.G = (__nv_bfloat16*)(ws + w.G);
-    P.labels = g.label; P.lse2 = g.lse; P.grad = g.grad; P.at_label = g.at_label; P.label_err = g.label_err;
-    P.first = g.first; P.rows = g.rows; P.rows_stride = w.d_pitch;
-    P.part = (float*)(ws + w.part); P.part_stride = w.part_pitch;
-    P.dw = (__nv_bfloat16*)out_grad_weight; P.dw_stride = grad_weight_row_stride;
-    const int rc = w.ctas == 2 ? back_launch<2>(P, M, s) : back_launch<1>(P, M, s);
-    if (rc != DSPARK_OK) return rc;
-    if (out_grad_hidden) {
-        HiddenParams Hp;
-        Hp.part = (const float*)(ws + w.part); Hp.part_stride = w.part_pitch; Hp.slices = w.slices; Hp.m = (int)w.n_pad;
-        Hp.label_err = g.label_err; Hp.label = g.label; Hp.idx = g.idx; Hp.live = g.live;
-        Hp.w = (const __nv_bfloat16*)weight; Hp.w_stride = weight_row_stride; Hp.d = d;
-        Hp.dh = g.dh; Hp.dh_stride = grad_hidden_row_stride;
-        KernelTimerScope timer(DSPARK_K_HEAD_ROWS, s);
-        launch_pdl(lm_head_grad_hidden_kernel, dim3(N, (d + 4 * kHiddenThreads - 1) / (4 * kHiddenThreads)), dim3(kHiddenThreads), 0, s, Hp);
-    }
-    return launch_status();
+    return loss_backward(hidden, hidden_row_stride, weight, weight_row_stride, labels, lse, nullptr, grad_loss, N, V, d, out_grad_hidden,
+                         grad_hidden_row_stride, out_grad_weight, grad_weight_row_stride, dev_status, workspace, workspace_bytes, stream);
+}
+
+int dspark_lm_head_loss_backward_from_loss(const void* hidden, int64_t hidden_row_stride, const void* weight, int64_t weight_row_stride,
+                                           const int32_t* labels, const float* lse, const float* loss, const float* grad_loss, int N,
+                                           int V, int d, void* out_grad_hidden, int64_t grad_hidden_row_stride, void* out_grad_weight,
+                                           int64_t grad_weight_row_stride, int32_t* dev_status, void* workspace,
+                                           size_t workspace_bytes, void* stream)
+{
+    if (!loss) return DSPARK_ERR_INVALID_ARG;
+    return loss_backward(hidden, hidden_row_stride, weight, weight_row_stride, labels, lse, loss, grad_loss, N, V, d, out_grad_hidden,
+                         grad_hidden_row_stride, out_grad_weight, grad_weight_row_stride, dev_status, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"
