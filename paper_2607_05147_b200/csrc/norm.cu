@@ -40,6 +40,7 @@ constexpr int kNormVec = 16;                    // bytes of one vector of x
 constexpr int kNormMaxThreads = 1024;
 constexpr int kNormMaxD = 16384;
 constexpr int kNormMaxStages = 8;
+constexpr float kNormSmall = 1e-33f, kNormMark = -1.f;   // small_row()
 constexpr int kNormStreamRows = 592;             // four rows an SM: below, a row per CTA starts sooner than a ring fills
 
 template <typename T> struct Elem;
@@ -176,18 +177,16 @@ struct NormRow {
     __device__ __forceinline__ void finish(const NormParams& P, long long row, const Weight (&weight)[kVpt], float sum, Prod top, int width, int me)
     {
         const bool bad = !(sum < INFINITY);                 // NaN or infinity in the row, or beyond fp32's range
-        float topf = (float)top, rstd = rsqrtf(sum / (float)P.d + P.eps);
+        const float topf = (float)top, rstd = rsqrtf(sum / (float)P.d + P.eps);
         if (me == 0) P.scale[row] = bad ? NAN : (top == 0 ? 0.f : topf * rstd * (1.f / 127.f));
         const bool zero = bad || top == 0;
-        if (topf < 1e-33f) {                                // next to the smallest fp32 numbers: brought up by 2^64
+        // fp32: or the compiler keeps the 64-bit products of the statistics for the few elements next to a half, two registers
+        // each (rows of 1001 elements 158 -> 293 us)
+        if (sizeof(T) == 4)
 #pragma unroll
             for (int v = 0; v < kVpt; ++v)
 #pragma unroll
-                for (int e = 0; e < kPer; ++e) h[v][e] *= 0x1p64f;
-            topf *= 0x1p64f;
-            top *= (Prod)0x1p64;
-            rstd *= 0x1p-64f;
-        }
+                for (int e = 0; e < kPer; ++e) asm volatile("" : "+f"(h[v][e]));
         const float inv = zero ? 0.f : 127.f / topf;
         constexpr float limit = 0.49996f;
         constexpr float kMagic = 12582912.f;                // 1.5 * 2^23: the integer ends up in the low bits
@@ -267,6 +266,77 @@ __device__ __forceinline__ void group_reduce(float& sum, Prod& top, float* s_sum
     }
 }
 
+// Rows at the bottom of fp32's range, in 64 bits: where the largest product is below kNormSmall, products next to a half and
+// the maximum itself may be subnormal in fp32 and have lost the digits that decide an integer.  64 bits hold every product of
+// two elements.  Rows of nothing but zeros (padding) are found first, in vectors.  The row is read again: h from out_residual
+// where it was stored (which may be x itself), else x + residual.  It comes last in a kernel, when nothing else is kept in
+// registers: the ring marks such rows in out_scale and does them after its last row (called from its loop, it cost fp32 rows
+// 13 to 30 %).
+template <bool kWarp>
+__device__ __forceinline__ void group_reduce64(double& sum, double& top)
+{
+    sum = warp_sum_f64(sum);
+    top = warp_max_any(top);
+    if (!kWarp) {
+        __shared__ double s_sum[kNormMaxThreads / 32], s_top[kNormMaxThreads / 32];
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = (int)blockDim.x >> 5;
+        if (lane == 0) { s_sum[warp] = sum; s_top[warp] = top; }
+        __syncthreads();
+        sum = warp_sum_f64(lane < n_warps ? s_sum[lane] : 0.0);
+        top = warp_max_any(lane < n_warps ? s_top[lane] : 0.0);
+    }
+}
+template <typename T, bool kVec, bool kWarp>
+__device__ __forceinline__ void small_row(const NormParams& P, long long row)
+{
+    typedef Elem<T> E;
+    const int width = kWarp ? 32 : (int)blockDim.x, me = kWarp ? (int)threadIdx.x & 31 : (int)threadIdx.x;
+    // out_residual was written by the whole group; the sums of the row before have been read
+    if (kWarp) __syncwarp(); else __syncthreads();
+    const T* x = (const T*)(P.h_out ? P.h_out : P.x) + row * (P.h_out ? P.h_stride : P.x_stride);
+    const T* res = P.res && !P.h_out ? (const T*)P.res + row * P.res_stride : nullptr;
+    auto load = [&](int i) { return res ? E::round(E::load(x, i) + E::load(res, i)) : E::load(x, i); };
+    int8_t* q = P.q + row * P.q_stride;
+    T* y = P.y ? (T*)P.y + row * P.y_stride : nullptr;
+    if constexpr (kVec) {
+        constexpr int kPer = E::kPer;
+        bool some = false;
+#pragma unroll 4
+        for (int at = me; at * kPer < P.d; at += width) {
+            float h[kPer], r[kPer];
+            E::unpack(reinterpret_cast<const uint4*>(x)[at], h);
+            E::unpack(res ? reinterpret_cast<const uint4*>(res)[at] : make_uint4(0, 0, 0, 0), r);
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) some = some || h[e] + r[e] != 0.f;      // a sum of two numbers is not rounded to zero
+        }
+        if (!(kWarp ? __any_sync(0xffffffffu, some) : __syncthreads_or(some))) {
+            if (me == 0) P.scale[row] = 0.f;
+            for (int at = me; at * kPer < P.d; at += width) {
+                if (kPer == 8) *reinterpret_cast<uint2*>(q + (long long)at * 8) = make_uint2(0, 0);
+                else *reinterpret_cast<uint32_t*>(q + (long long)at * 4) = 0;
+                if (y) reinterpret_cast<uint4*>(y)[at] = make_uint4(0, 0, 0, 0);
+            }
+            return;
+        }
+    }
+    double sum = 0.0, top = 0.0;
+#pragma unroll 1
+    for (int i = me; i < P.d; i += width) {
+        const double h = load(i);
+        sum = fma(h, h, sum);
+        top = max_abs_nan(top, h * (double)E::load(P.w, i));
+    }
+    group_reduce64<kWarp>(sum, top);
+    const double rstd = 1.0 / sqrt(sum / P.d + (double)P.eps);
+    if (me == 0) P.scale[row] = top == 0.0 ? 0.f : (float)(top * rstd / 127.0);
+#pragma unroll 1
+    for (int i = me; i < P.d; i += width) {
+        const double t = (double)load(i) * (double)E::load(P.w, i);
+        q[i] = top == 0.0 ? 0 : (int8_t)rint(t * 127.0 / top);
+        if (y) E::store(y, i, top == 0.0 ? 0.f : (float)(t * rstd));
+    }
+}
+
 // One row per group, loaded straight into registers: few rows, or rows that break the 16-byte rule.
 // kWarp: a warp per row, several rows per CTA; otherwise a CTA per row.
 template <typename T, int kVpt, bool kVec, bool kWarp, int kThreads>
@@ -322,7 +392,8 @@ __global__ void __launch_bounds__(kThreads) rms_norm_quant_kernel(const __grid_c
     Prod top;
     r.statistics(w, sum, top);
     group_reduce<kWarp>(sum, top, s_sum, s_top);
-    r.finish(P, row, w, sum, top, width, me);
+    if (sum < INFINITY && top < (Prod)kNormSmall) small_row<T, kVec, kWarp>(P, row);
+    else r.finish(P, row, w, sum, top, width, me);
 }
 
 // Many rows: persistent groups walk the rows, each with a ring of `stages` rows of x and the residual in shared memory that
@@ -375,7 +446,9 @@ __global__ void __launch_bounds__(kThreads, kCtas) rms_norm_quant_stream_kernel(
     }
     int s = 0, turn = 0;
     uint32_t ph = 0;
-    for (long long row = first; row < live; row += step) {
+    bool small = false;                                     // the same in the whole group
+    long long row = first;
+    for (; row < live; row += step) {
         // The copy is this group's own and lands; a wait that ran out all the same gives the row up as one that cannot be
         // normalised, and its stage is not filled again.
         const bool ok = mbar_wait_bounded(&full[group][s], ph);
@@ -399,9 +472,19 @@ __global__ void __launch_bounds__(kThreads, kCtas) rms_norm_quant_stream_kernel(
         group_reduce<kWarp>(sum, top, s_sum[turn & 1], s_top[turn & 1]);
         if (kWarp) __syncwarp();
         if (me == 0 && ok && row + stages * step < live) request(row + stages * step, s);
-        r.finish(P, row, w, sum, top, width, me);
+        if (sum < INFINITY && top < (Prod)kNormSmall) {
+            small = true;
+            if (me == 0) P.scale[row] = kNormMark;
+        } else {
+            r.finish(P, row, w, sum, top, width, me);
+        }
         if (++s == stages) { s = 0; ph ^= 1u; }
         ++turn;
+    }
+    if (small) {
+        if (kWarp) __syncwarp(); else __syncthreads();      // the marks are written
+        for (row -= step; row >= 0; row -= step)
+            if (*(volatile const float*)(P.scale + row) == kNormMark) small_row<T, true, kWarp>(P, row);
     }
 }
 
