@@ -495,9 +495,9 @@ int dspark_sts_apply(const float* conf, int N, int gamma, const float* T, float*
  *   out_residual       device [rows, >= d] of `dtype` or NULL: h; may be `residual` or `x` itself (same stride)
  *   out_q, out_scale   device int8 [rows, >= d], device fp32 [rows]
  *   out_norm           device [rows, >= d] of `dtype` or NULL: y (what the confidence head reads); may be x itself
- *   A row of zeros gives q = 0 and scale 0.  A row that holds NaN or an infinity, or whose sum of squares or a product
- *   h * weight passes the range of fp32, gives q = 0 and a scale of NaN: its logits are then NaN and a verifier reports
- *   DSPARK_DEV_BAD_ROW.  Outputs must not overlap otherwise.  No workspace.
+ *   A row of zeros gives q = 0, scale 0 and y = 0, with an eps of 0 too.  A row that holds NaN or an infinity, or whose sum
+ *   of squares or a product h * weight passes the range of fp32, gives q = 0 and a scale of NaN: its logits are then NaN and
+ *   a verifier reports DSPARK_DEV_BAD_ROW.  Outputs must not overlap otherwise.  No workspace.
  * Limits: d <= 16 384.  Errors: INVALID_ARG, SHAPE, ALIGNMENT (a pointer not aligned to its element), CUDA.
  */
 int dspark_rms_norm_quant(const void* x, int64_t x_row_stride, const void* residual, int64_t residual_row_stride,

@@ -40,7 +40,7 @@ constexpr int kNormVec = 16;                    // bytes of one vector of x
 constexpr int kNormMaxThreads = 1024;
 constexpr int kNormMaxD = 16384;
 constexpr int kNormMaxStages = 8;
-constexpr float kNormSmall = 1e-33f, kNormMark = -1.f;   // small_row()
+constexpr float kNormSmall = 1e-33f, kNormLargeRstd = 0x1p59f, kNormMark = -1.f;   // small_row()
 constexpr int kNormStreamRows = 592;             // four rows an SM: below, a row per CTA starts sooner than a ring fills
 
 template <typename T> struct Elem;
@@ -174,10 +174,10 @@ struct NormRow {
         // an infinite or NaN maximum (of the row or of the weights) travels in the sum
         if (!(top <= (Prod)3.4e38)) sum = NAN;
     }
-    __device__ __forceinline__ void finish(const NormParams& P, long long row, const Weight (&weight)[kVpt], float sum, Prod top, int width, int me)
+    __device__ __forceinline__ void finish(const NormParams& P, long long row, const Weight (&weight)[kVpt], float sum, float rstd, Prod top, int width, int me)
     {
         const bool bad = !(sum < INFINITY);                 // NaN or infinity in the row, or beyond fp32's range
-        const float topf = (float)top, rstd = rsqrtf(sum / (float)P.d + P.eps);
+        const float topf = (float)top;
         if (me == 0) P.scale[row] = bad ? NAN : (top == 0 ? 0.f : topf * rstd * (1.f / 127.f));
         const bool zero = bad || top == 0;
         // fp32: or the compiler keeps the 64-bit products of the statistics for the few elements next to a half, two registers
@@ -266,12 +266,18 @@ __device__ __forceinline__ void group_reduce(float& sum, Prod& top, float* s_sum
     }
 }
 
-// Rows at the bottom of fp32's range, in 64 bits: where the largest product is below kNormSmall, products next to a half and
-// the maximum itself may be subnormal in fp32 and have lost the digits that decide an integer.  64 bits hold every product of
-// two elements.  Rows of nothing but zeros (padding) are found first, in vectors.  The row is read again: h from out_residual
-// where it was stored (which may be x itself), else x + residual.  It comes last in a kernel, when nothing else is kept in
-// registers: the ring marks such rows in out_scale and does them after its last row (called from its loop, it cost fp32 rows
-// 13 to 30 %).
+// Rows at the bottom of fp32's range, in 64 bits.  Where the largest product is below kNormSmall, products next to a half and
+// the maximum itself may be subnormal in fp32 and have lost the digits that decide an integer; where the mean of the squares
+// and eps together are below 2^-118 (rstd above kNormLargeRstd), squares that underflow (off by 2^-150 each) show in the root.
+// 64 bits hold every product of two elements.  Rows of nothing but zeros (padding) are found first, in vectors.  The row is
+// read again: h from out_residual where it was stored (which may be x itself), else x + residual.  It comes last in a kernel,
+// when nothing else is kept in registers: the ring marks such rows in out_scale and does them after its last row (called from
+// its loop, it cost fp32 rows 13 to 30 %).
+template <typename Prod>
+__device__ __forceinline__ bool is_small(float sum, float rstd, Prod top)
+{
+    return sum < INFINITY && (top < (Prod)kNormSmall || rstd > kNormLargeRstd);
+}
 template <bool kWarp>
 __device__ __forceinline__ void group_reduce64(double& sum, double& top)
 {
@@ -392,8 +398,9 @@ __global__ void __launch_bounds__(kThreads) rms_norm_quant_kernel(const __grid_c
     Prod top;
     r.statistics(w, sum, top);
     group_reduce<kWarp>(sum, top, s_sum, s_top);
-    if (sum < INFINITY && top < (Prod)kNormSmall) small_row<T, kVec, kWarp>(P, row);
-    else r.finish(P, row, w, sum, top, width, me);
+    const float rstd = rsqrtf(sum / (float)P.d + P.eps);
+    if (is_small(sum, rstd, top)) small_row<T, kVec, kWarp>(P, row);
+    else r.finish(P, row, w, sum, rstd, top, width, me);
 }
 
 // Many rows: persistent groups walk the rows, each with a ring of `stages` rows of x and the residual in shared memory that
@@ -472,11 +479,12 @@ __global__ void __launch_bounds__(kThreads, kCtas) rms_norm_quant_stream_kernel(
         group_reduce<kWarp>(sum, top, s_sum[turn & 1], s_top[turn & 1]);
         if (kWarp) __syncwarp();
         if (me == 0 && ok && row + stages * step < live) request(row + stages * step, s);
-        if (sum < INFINITY && top < (Prod)kNormSmall) {
+        const float rstd = rsqrtf(sum / (float)P.d + P.eps);
+        if (is_small(sum, rstd, top)) {
             small = true;
             if (me == 0) P.scale[row] = kNormMark;
         } else {
-            r.finish(P, row, w, sum, top, width, me);
+            r.finish(P, row, w, sum, rstd, top, width, me);
         }
         if (++s == stages) { s = 0; ph ^= 1u; }
         ++turn;
