@@ -611,7 +611,10 @@ int dspark_set_stream_path(int path);
  * order of a second); a wait gives up after polls - 1 unsuccessful polls, so 1 makes every such wait run
  * out at once.  That is how the tests reach the give-up path without hanging anything: a kernel that gives
  * up still waits, with the long default bound, for the bulk copies it has already issued before it leaves,
- * and its outputs are unspecified.  Per device (the current one), synchronous; the paper has no counterpart. */
+ * and its outputs are unspecified.  dspark_rms_norm_quant's waits for rows copied ahead (many rows) have the same
+ * limit (a captured graph: the one at its capture); a thread whose wait runs out reads its rows from memory instead, so
+ * that its outputs are the same as ever.
+ * Per device (the current one), synchronous; the paper has no counterpart. */
 int dspark_set_wait_poll_limit(unsigned int polls);
 
 const char* dspark_status_string(int status);

@@ -409,7 +409,7 @@ __global__ void __launch_bounds__(kThreads) rms_norm_quant_kernel(const __grid_c
 // kCtas: CTAs an SM that the registers have to allow.  Occupancy is what hides the chain of a row (shared memory,
 // reduction, barrier, store).
 template <typename T, int kVpt, bool kWarp, int kThreads, int kCtas>
-__global__ void __launch_bounds__(kThreads, kCtas) rms_norm_quant_stream_kernel(const __grid_constant__ NormParams P, int stages)
+__global__ void __launch_bounds__(kThreads, kCtas) rms_norm_quant_stream_kernel(const __grid_constant__ NormParams P, int stages, uint32_t poll_limit)
 {
     typedef Elem<T> E;
     typedef typename E::Product Prod;
@@ -432,11 +432,12 @@ __global__ void __launch_bounds__(kThreads, kCtas) rms_norm_quant_stream_kernel(
     }
     __syncthreads();
     pdl_wait();
-    long long live = P.rows;
-    if (P.n_live) { const int n = *P.n_live; live = n < P.rows ? n : P.rows; }
-    const long long first = (long long)blockIdx.x * kGroups + group, step = (long long)gridDim.x * kGroups;
+    // 32 bits hold a row's number and `stages` steps beyond the last one
+    uint32_t live = (uint32_t)P.rows;
+    if (P.n_live) { const int n = *P.n_live; live = (uint32_t)(n < 0 ? 0 : n < P.rows ? n : P.rows); }
+    const uint32_t first = blockIdx.x * kGroups + group, step = gridDim.x * kGroups;
     const uint64_t pol = l2_policy_evict_first();
-    auto request = [&](long long row, int s) {
+    auto request = [&](uint32_t row, int s) {
         mbar_arrive_expect_tx(&full[group][s], stage_bytes);
         bulk_g2s_hint(ring + s * stage_bytes, (const T*)P.x + row * P.x_stride, row_bytes, &full[group][s], pol);
         if (P.res) bulk_g2s_hint(ring + s * stage_bytes + row_bytes, (const T*)P.res + row * P.res_stride, row_bytes, &full[group][s], pol);
@@ -453,13 +454,29 @@ __global__ void __launch_bounds__(kThreads, kCtas) rms_norm_quant_stream_kernel(
     }
     int s = 0, turn = 0;
     uint32_t ph = 0;
+    bool direct = false;                                    // each thread's own
     bool small = false;                                     // the same in the whole group
-    long long row = first;
+    uint32_t row = first;
     for (; row < live; row += step) {
-        // The copy is this group's own and lands; a wait that ran out all the same gives the row up as one that cannot be
-        // normalised, and its stage is not filled again.
-        const bool ok = mbar_wait_bounded(&full[group][s], ph);
-        const unsigned char* stage = ring + s * stage_bytes;
+        unsigned char* stage = ring + s * stage_bytes;
+        // The copy is this group's own and lands.  A thread whose wait ran out all the same fetches its part of this row and of
+        // all that follow itself, from where nobody else writes to where nobody else reads: a barrier that is behind by a phase
+        // would pass for the one awaited.  The group's first thread, which asks for the copies, then lets those on their way
+        // land (with the long bound) and asks for no more; waits of the others run out in turn.
+        if (!direct && !mbar_wait_bounded(&full[group][s], ph, poll_limit)) {
+            direct = true;
+            if (me == 0)
+                for (int i = 0; i < stages && row + i * step < live; ++i)
+                    mbar_wait_bounded(&full[group][s + i < stages ? s + i : s + i - stages], s + i < stages ? ph : ph ^ 1u);
+        }
+        if (direct) {
+#pragma unroll 1
+            for (int at = me; at * kPer < P.d; at += width) {
+                reinterpret_cast<uint4*>(stage)[at] = reinterpret_cast<const uint4*>((const T*)P.x + row * P.x_stride)[at];
+                if (P.res) reinterpret_cast<uint4*>(stage + row_bytes)[at] = reinterpret_cast<const uint4*>((const T*)P.res + row * P.res_stride)[at];
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
         uint4 xv[kVpt], rv[kVpt];
 #pragma unroll
         for (int v = 0; v < kVpt; ++v) {
@@ -475,10 +492,9 @@ __global__ void __launch_bounds__(kThreads, kCtas) rms_norm_quant_stream_kernel(
         float sum;
         Prod top;
         r.statistics(w, sum, top);
-        if (!ok) sum = NAN;
         group_reduce<kWarp>(sum, top, s_sum[turn & 1], s_top[turn & 1]);
         if (kWarp) __syncwarp();
-        if (me == 0 && ok && row + stages * step < live) request(row + stages * step, s);
+        if (me == 0 && !direct && row + stages * step < live) request(row + stages * step, s);
         const float rstd = rsqrtf(sum / (float)P.d + P.eps);
         if (is_small(sum, rstd, top)) {
             small = true;
@@ -491,9 +507,22 @@ __global__ void __launch_bounds__(kThreads, kCtas) rms_norm_quant_stream_kernel(
     }
     if (small) {
         if (kWarp) __syncwarp(); else __syncthreads();      // the marks are written
-        for (row -= step; row >= 0; row -= step)
+        while (row >= step) {                               // the first row is below `step`
+            row -= step;
             if (*(volatile const float*)(P.scale + row) == kNormMark) small_row<T, true, kWarp>(P, row);
+        }
     }
+}
+
+// Polls of a wait for a row's copy, by device, 0 standing for kWaitPollLimit (dspark_set_wait_poll_limit); a kernel argument,
+// since a register for it would be spilled.  The wait for copies before they are given up keeps the long bound.
+static std::atomic<uint32_t> g_norm_poll_limit[64];
+int norm_set_poll_limit(uint32_t polls)
+{
+    int dev = 0;
+    cudaGetDevice(&dev);
+    g_norm_poll_limit[dev & 63].store(polls ^ kWaitPollLimit, std::memory_order_relaxed);
+    return launch_status();
 }
 
 template <typename T, int kVpt, bool kWarp, int kThreads, int kCtas>
@@ -521,7 +550,7 @@ static bool norm_stream(const NormParams& P, int threads, cudaStream_t s)
     }
     const long long want = ((long long)P.rows + groups - 1) / groups, cap = (long long)sms * ctas;
     launch_pdl(rms_norm_quant_stream_kernel<T, kVpt, kWarp, kThreads, kCtas>, dim3((unsigned)(want < cap ? want : cap)), dim3(threads),
-               (size_t)stages * stage, s, P, stages);
+               (size_t)stages * stage, s, P, stages, g_norm_poll_limit[dev & 63].load(std::memory_order_relaxed) ^ kWaitPollLimit);
     return true;
 }
 

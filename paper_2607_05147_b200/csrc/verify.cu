@@ -1342,7 +1342,8 @@ size_t dspark_verify_workspace_bytes(int R, int n_rows, int V)
 int dspark_set_wait_poll_limit(unsigned int polls)
 {
     const uint32_t v = polls ? polls - 1u : kWaitPollLimit;     // 1: no poll at all, the wait gives up at once
-    return cudaMemcpyToSymbol(g_entry_poll_limit, &v, sizeof(v)) == cudaSuccess ? DSPARK_OK : launch_status();
+    if (cudaMemcpyToSymbol(g_entry_poll_limit, &v, sizeof(v)) != cudaSuccess) return launch_status();
+    return norm_set_poll_limit(v);
 }
 
 int dspark_set_stream_path(int path)
