@@ -1369,9 +1369,10 @@ __global__ void __launch_bounds__(256) lm_head_quantize_kernel(const __nv_bfloat
     top = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = fmaxf(top, s_top[i]);
+    const float down = top > 1e36f ? 0x1p-16f : 1.f;        // or 127 w passes the range
     for (int i = tid; i < K; i += 256) {
         // 127 w has 15 significant bits: the correctly rounded quotient keeps a half a half
-        const float v = (bad || top == 0.f) ? 0.f : rintf(__fdiv_rn(127.f * __bfloat162float(w[i]), top));
+        const float v = (bad || top == 0.f) ? 0.f : rintf(__fdiv_rn(127.f * (__bfloat162float(w[i]) * down), top * down));
         out[i] = (int8_t)v;
     }
     if (tid == 0) scale[blockIdx.x] = bad ? NAN : top / 127.f;
