@@ -1307,7 +1307,7 @@ __global__ void __launch_bounds__(kLossThreads) lm_head_loss_kernel(const __grid
     const double loss = (z - z) + (shift > 0.0 ? shift + log(total + exp(-shift)) : log1p(total * exp(shift)));
     P.loss[at] = (float)loss;
     P.lse[at] = (float)(z + loss);
-    if (!(fabs(loss) < INFINITY)) atomicOr(P.dev_status, DSPARK_DEV_BAD_ROW);
+    if (!(fabsf((float)loss) < INFINITY)) atomicOr(P.dev_status, DSPARK_DEV_BAD_ROW);      // as it is stored
 }
 
 // ---- gradient of the hidden states from the slices' partial sums ---------------------------------------
