@@ -1369,10 +1369,11 @@ __global__ void __launch_bounds__(256) lm_head_quantize_kernel(const __nv_bfloat
     top = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = fmaxf(top, s_top[i]);
-    const float down = top > 1e36f ? 0x1p-16f : 1.f;        // or 127 w passes the range
+    // above, 127 w passes the range: 127 and the maximum 2^16 smaller there
+    const float up = top > 1e36f ? 127.f * 0x1p-16f : 127.f, by = top > 1e36f ? top * 0x1p-16f : top;
     for (int i = tid; i < K; i += 256) {
         // 127 w has 15 significant bits: the correctly rounded quotient keeps a half a half
-        const float v = (bad || top == 0.f) ? 0.f : rintf(__fdiv_rn(127.f * (__bfloat162float(w[i]) * down), top * down));
+        const float v = (bad || top == 0.f) ? 0.f : rintf(__fdiv_rn(up * __bfloat162float(w[i]), by));
         out[i] = (int8_t)v;
     }
     if (tid == 0) scale[blockIdx.x] = bad ? NAN : top / 127.f;
@@ -1481,6 +1482,8 @@ static int back_launch(const BackParams& P, const BackMaps& M, cudaStream_t s)
     return launch_status();
 }
 
+// A B200's.  Not asked of the device: the size of the workspace is known without one, and the same everywhere.
+constexpr int kSms = 148;
 constexpr int kMaxRows = 1 << 20, kMaxVocab = 1 << 24, kMaxWidth = 1 << 16;
 constexpr long long kPieceBytes = 32ll << 20;
 
@@ -1498,7 +1501,7 @@ static LossWs loss_layout(int N, int V, int d)
     // SMs leave many of them idle in the last one, by at least 1/16.  256 / this rule, us: 64 rows V 129 280 d 1024 57.8 /
     // 55.7, V 151 936 68.8 / 65.7, V 50 257 d 768 27.2 / 25.7, V 10 007 d 500 14.3 / 13.0.  (Pairs read B once for both rows
     // of tiles and lose by it: 600 rows V 40 000 d 300 32.8 / 43.6.)
-    auto rounds = [&](int tile) { return ((V + tile - 1) / tile + 147) / 148 * tile; };
+    auto rounds = [&](int tile) { return ((V + tile - 1) / tile + kSms - 1) / kSms * tile; };
     w.n_tile = kHeadN;
     for (int tile = kHeadN - 32; w.ctas == 1 && tile >= 128; tile -= 32)
         if (rounds(tile) * 16ll <= rounds(w.n_tile) * 15ll) w.n_tile = tile;
@@ -1523,7 +1526,7 @@ static LossWs loss_layout(int N, int V, int d)
     // k blocks of the units of one piece, over the SMs: a slice of dH's sum over the piece is at most half of an SM's share
     const long long m_tiles = w.n_pad / (w.ctas * kHeadM), blocks = piece / 64;
     const long long work = 2 * m_tiles * w.d_tiles * blocks + m_tiles * (piece / kHeadN) * ((d + 63) / 64);
-    long long most = work / (2 * 148 / w.ctas);
+    long long most = work / (2 * kSms / w.ctas);
     if (most < 8) most = 8;
     long long slices = (blocks + most - 1) / most;
     if (slices > 64) slices = 64;
@@ -1662,7 +1665,12 @@ int dspark_lm_head_int8(const int8_t* x_q, int64_t x_row_stride, const float* x_
     // too short for the 3 us that a launch of pairs takes longer.  Single / pair, us: V = 129 280, K 512 256 rows 33 / 32,
     // 1482 rows 136 / 137; K 768 256 rows 39 / 36, 1482 rows 168 / 164; K 1024 129 rows 35 / 35, 256 rows 46 / 39, 352 rows
     // (pairs' tiles are multiples of 32) 60 / 62, 500 rows 75 / 69, 1482 rows 201 / 185; K 4096 1482 rows 732 / 591.
-    // V = 32 000, K 1024 256 rows 18 / 20, 500 rows 26 / 23; K 1536 129 rows 18 / 17; V = 16 000, K 1024 512 rows 16 / 16.
+    // V = 32 000, K 1024 256 rows 18 / 20, 500 rows 26 / 23; K 1040 200 rows 25.5 / 19.8; K 1536 129 rows 18 / 17, 512 rows
+    // 28.3 / 26.6; V = 16 000, K 1024 512 rows 16 / 16, K 2048 256 rows 13.5 / 13.1.  V is not asked for beyond K 1024: where
+    // there are few tiles an SM, pairs lose up to 2 us -- K 1536 V 1000 200 rows 8.2 / 9.3, K 2048 V 10 007 200 rows
+    // 11.4 / 12.3, 512 rows 19.8 / 18.5, K 4096 V 1000 129 rows 13.3 / 15.4, V 10 007 129 rows 14.7 / 16.0.
+    // Both choices go by the rows there is room for, since the count is on the device: 576 rows of which 1 counts, K 1024
+    // 32.5 us (a call for 1 row 29.2), K 4096 97 (83); 192 of 576 as a call for 192.
     const int ctas = rows > kHeadM && (K > 1024 || (K >= 768 && (double)rows * V * K > 1.2e10)) ? 2 : 1;
     // row tiles of one size, and no taller a box than there are rows (one row of 32 in a box: 170 us instead of 84 at
     // K = 4 096)

@@ -41,7 +41,8 @@ constexpr int kNormMaxThreads = 1024;
 constexpr int kNormMaxD = 16384;
 constexpr int kNormMaxStages = 8;
 constexpr float kNormSmall = 1e-33f, kNormLargeRstd = 0x1p59f, kNormMark = -1.f;   // small_row()
-constexpr int kNormStreamRows = 592;             // four rows an SM: below, a row per CTA starts sooner than a ring fills
+constexpr int kNormSms = 148;                   // a B200's: what the thresholds below were measured on
+constexpr int kNormStreamRows = 4 * kNormSms;   // below, a row per CTA starts sooner than a ring fills
 
 template <typename T> struct Elem;
 template <> struct Elem<float> {
@@ -560,7 +561,7 @@ static void norm_launch(const NormParams& P, cudaStream_t s)
     constexpr int kPer = Elem<T>::kPer;
     const int vectors = (P.d + kPer - 1) / kPer;
     // a warp per row; rows of more than 256 elements only where there are enough of them to fill the SMs with warps
-    if (P.d <= 256 || (P.d <= 1024 && P.rows >= 8 * 148)) {
+    if (P.d <= 256 || (P.d <= 1024 && P.rows >= 8 * kNormSms)) {
         const int per = (vectors + 31) / 32;
         if constexpr (kVec) {
             if (P.rows >= kNormStreamRows * 8) {
@@ -572,7 +573,7 @@ static void norm_launch(const NormParams& P, cudaStream_t s)
                 if (done) return;
             }
         }
-        const int warps = P.rows >= 8 * 148 ? 8 : 1;
+        const int warps = P.rows >= 8 * kNormSms ? 8 : 1;
         const dim3 grid((unsigned)((P.rows + warps - 1) / warps)), block(warps * 32);
         if (per <= 1) launch_pdl(rms_norm_quant_kernel<T, 1, kVec, true, 256>, grid, block, 0, s, P);
         else if (per <= 2) launch_pdl(rms_norm_quant_kernel<T, 2, kVec, true, 256>, grid, block, 0, s, P);
