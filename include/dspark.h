@@ -44,7 +44,7 @@ typedef enum {
     DSPARK_ERR_STATIC_LIMIT = 7
 } dspark_status_t;
 
-typedef enum { DSPARK_F32 = 0, DSPARK_BF16 = 1 } dspark_dtype_t;
+typedef enum { DSPARK_F32 = 0, DSPARK_BF16 = 1, DSPARK_I8 = 2, DSPARK_E4M3 = 3 } dspark_dtype_t;   /* the last two: caches only */
 
 typedef enum {
     DSPARK_SCHED_EARLY_STOP = 0, /* Algorithm 1 as printed: stop at the first non-improving admission */
@@ -61,6 +61,8 @@ typedef enum {
 #define DSPARK_DEV_BUDGET_LT_R 32  /* token budget below the number of requests: every l*_r = 0 */
 #define DSPARK_DEV_ALL_NEG_INF 64  /* greedy: a row without any element above -inf (index 0 reported) */
 #define DSPARK_DEV_BAD_TEMPERATURE 128 /* a per-request temperature that is not a positive finite number */
+#define DSPARK_DEV_BAD_PAGE 256    /* a page number outside the cache, or a request longer than its row of the block table */
+#define DSPARK_DEV_BAD_TREE 512    /* a parent that is not an earlier node, or a path that is not one of ascending nodes */
 
 /* ------------------------------------------------------------------------------------
  * Engine throughput profile SPS(B), steps per second at B batch tokens: a table the engine measures
@@ -577,6 +579,123 @@ int dspark_lm_head_loss_backward_from_loss(const void* hidden, int64_t hidden_ro
                                            int64_t grad_weight_row_stride, int32_t* dev_status, void* workspace,
                                            size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------------------
+ * A step with trees of drafted tokens over a paged cache (Section 2.1 verifies one drafted chain; a tree offers several
+ * tokens for a position).  The paper states no kernel for any of it.
+ *
+ * Ragged batch: request r owns the rows [row_offsets[r], row_offsets[r+1]), one for each node of its tree, in every array of
+ * the step; n_rows is the host-known capacity.  Node 0 is the root (the last token that is certain), every other node's parent
+ * is an earlier node; a chain is parents[i] = i - 1.  first[r] tokens are in the cache before the step; the K and V rows of
+ * node i are at position first[r] + i.  A request without rows is nothing to do.  A request whose first[r] is negative or
+ * whose rows pass the end of its row of the block table (DSPARK_DEV_BAD_PAGE), or whose offsets are not ascending within
+ * [0, n_rows] (DSPARK_DEV_BAD_OFFSETS), is left alone: its outputs stay as they were; the others are unaffected, but for rows
+ * that such offsets give to two requests.
+ *
+ * The cache: position t of request r is token t % page_size of page block_table[r * block_table_stride + t / page_size].
+ *   k, v               device, element (layer, page, token, head, i) at
+ *                      layer * layer_stride + page * page_stride + token * token_stride + head * head_stride + i elements;
+ *                      both have these strides.  16-byte aligned, strides multiples of 16 bytes
+ *   dtype              DSPARK_BF16, or DSPARK_I8 / DSPARK_E4M3 with one scale per token and head: value = scale * stored
+ *   k_scale, v_scale   device fp32 [n_layers][n_pages][kv_heads][page_size] (NULL with DSPARK_BF16), 4-byte aligned
+ *   page_size          a power of two from 8 to 128, or any number above 128
+ *   head_dim           a multiple of 16, at most 256 (dspark_tree_attention: at most 128)
+ *   block_table        device int32, block_table_stride entries a request, max_pages of them valid
+ * A page number outside [0, n_pages) sets DSPARK_DEV_BAD_PAGE: nothing is written there, and its tokens read as zeros.
+ * Limits: kv_heads <= 1 024, n_layers <= 1 024, n_pages <= 2^28, page_size <= 2^20, positions below 2^31, 1 <= R <= 2^20,
+ * n_rows <= 2^24.
+ */
+typedef struct {
+    void* k; void* v;
+    float* k_scale; float* v_scale;
+    int32_t dtype, n_layers, n_pages, page_size, kv_heads, head_dim;
+    int64_t layer_stride, page_stride, token_stride, head_stride;
+    const int32_t* block_table;
+    int64_t block_table_stride;
+    int32_t max_pages;
+} dspark_kv_cache_t;
+
+/* dspark_kv_write -- K and V rows of a step into one layer of the cache, quantised as they are written:
+ *     DSPARK_I8:    scale = max|x| / 127,  stored = rint(127 x / max|x|)          (a half to the even integer)
+ *     DSPARK_E4M3:  scale = max|x| / 448,  stored = 448 x / max|x| rounded to e4m3 (ties to even)
+ *   per row and head, the integer or value that of the exact quotient.  A head of zeros gives scale 0; one with NaN or an
+ *   infinity stores zeros and a scale of NaN.  k, v: device bf16 [n_rows][kv_heads][head_dim], row and head strides in
+ *   elements (both arrays have them), 16-byte aligned, strides multiples of 8.  No two rows may share a position.
+ * dspark_kv_read -- the rows at the same positions back: out = scale * stored, rounded once to out_dtype (DSPARK_BF16 /
+ *   DSPARK_F32), strides multiples of 16 bytes; out_k or out_v may be NULL, not both.
+ * Errors: INVALID_ARG, SHAPE (the limits above), ALIGNMENT, CUDA.  No workspace.
+ */
+int dspark_kv_write(const dspark_kv_cache_t* cache, int layer, const void* k, const void* v, int64_t row_stride,
+                    int64_t head_stride, const int32_t* first, const int32_t* row_offsets, int R, int n_rows,
+                    int32_t* dev_status, void* stream);
+int dspark_kv_read(const dspark_kv_cache_t* cache, int layer, const int32_t* first, const int32_t* row_offsets, int R,
+                   int n_rows, void* out_k, void* out_v, int out_dtype, int64_t out_row_stride, int64_t out_head_stride,
+                   int32_t* dev_status, void* stream);
+
+/* dspark_kv_commit -- after a tree has been verified: the accepted nodes' K and V (and scales) of all layers are moved
+ * together behind the root, position first[r] + path[i] to first[r] + 1 + i, so that the cache holds the accepted tokens
+ * in order.
+ *   accepted_len   device int32 [R]: accepted nodes without the root, n_r
+ *   path           device int32 [n_rows]: path[row_offsets[r] + i], i < n_r, the nodes in ascending order (dspark_verify_tree)
+ *   out_first      device int32 [R] or NULL, not first itself: first[r] + 1 + n_r, what `first` is in the next step.  A
+ *                  request that is left alone, or whose path is not ascending within its nodes (DSPARK_DEV_BAD_TREE: nothing
+ *                  is moved), gets first[r]; a request without rows too
+ * Errors: INVALID_ARG, SHAPE, ALIGNMENT, CUDA.  No workspace.
+ */
+int dspark_kv_commit(const dspark_kv_cache_t* cache, const int32_t* first, const int32_t* row_offsets, int R, int n_rows,
+                     const int32_t* accepted_len, const int32_t* path, int32_t* out_first, int32_t* dev_status, void* stream);
+
+/* dspark_tree_attention -- attention of the step's nodes over one layer of the cache:
+ *     out[i, h] = sum_t w_t v[t, h / group],  w = softmax over the positions t that node i sees of scale * q[i, h] . k[t, h / group],
+ *   the positions before first[r], node i itself and its ancestors (at first[r] + j).  What is stored for other nodes (NaN,
+ *   infinities) does not reach the row.  The nodes' own K and V have been written before (dspark_kv_write).
+ *   q, out      device bf16 [n_rows][q_heads][head_dim], own row and head strides in elements, multiples of 8; 16-byte aligned;
+ *               q_heads = group * kv_heads with group <= 128.  out may be q itself with the same strides
+ *   parents     device int32 [n_rows], the parent's index within the request (the root's entry is not read); NULL: chains,
+ *               node i sees the nodes up to i.  A parent that is not an earlier node sets DSPARK_DEV_BAD_TREE and ends the
+ *               ancestors there
+ *   scale       finite
+ *   out_lse     device fp32 [n_rows][q_heads] or NULL: log of the sum of e^(scale * q . k) over the positions seen
+ *   workspace   dspark_tree_attention_workspace_bytes(...), 256-byte aligned, any content; one call at a time
+ * The products are bf16 (an 8-bit cache: 16-bit operands that hold its values exactly) with fp32 accumulation; softmax
+ * statistics are fp32; the weights are rounded to 16 bits for their product with v.  The same inputs give the same bits.
+ * Errors: INVALID_ARG, SHAPE, ALIGNMENT, WORKSPACE, CUDA.
+ */
+size_t dspark_tree_attention_workspace_bytes(int n_rows, int q_heads, int kv_heads, int head_dim);
+int dspark_tree_attention(const dspark_kv_cache_t* cache, int layer, const void* q, int64_t q_row_stride, int64_t q_head_stride,
+                          int q_heads, const int32_t* first, const int32_t* row_offsets, const int32_t* parents, int R,
+                          int n_rows, float scale, void* out, int64_t out_row_stride, int64_t out_head_stride,
+                          float* out_lse, int32_t* dev_status, void* workspace, size_t workspace_bytes, void* stream);
+
+/* dspark_verify_tree -- lossless verification of a tree of drafted tokens from given random numbers.  Row u of target_probs
+ * is p(. | node u), row u of draft_probs the distribution q(. | node u) that the tokens of u's children were drawn from,
+ * independently.  The walk starts at the root with A = 0 and Z = 1; the children of the node u it stands at are looked at in
+ * ascending order: with r(v) = max(p_u(v) - A q_u(v), 0), child c with token x is accepted iff
+ *     u_accept[c] * q_u(x) * Z < r(x),
+ * and the walk goes on there with A = 0, Z = 1; otherwise A += Z and Z = sum_v r(v) for the new A.  Where no child is left,
+ * the last token is drawn from r: the smallest v whose running sum exceeds u_sample[r] times the total.  (r / Z is what
+ * repeated acceptance with probability min(1, p / q) and residual norm(max(0, p - q)) leaves; a chain is the verifier's rule.)
+ *   draft_probs NULL: the tokens were chosen, not drawn: q_u is one at the token, so that x is accepted iff
+ *   u_accept[c] * Z < r(x), else r(x) = 0 and Z is less by what it was.
+ *   target_probs, draft_probs   device fp32 [n_rows, >= V], row strides in elements; rows sum to one.  Negative differences
+ *                  count as zero; where a residual has no mass left (r = 0 everywhere), the last token is drawn from p_u
+ *   tokens         device int32 [n_rows]: a node's token (the root's is not read);  parents  device int32 [n_rows]
+ *   u_accept       device fp32 [n_rows], u_sample  device fp32 [R]: numbers in [0, 1); the root's u_accept is not read
+ *   accepted_len   device int32 [R]: accepted nodes without the root, n_r
+ *   out_tokens     device int32 [n_rows]: the accepted nodes' tokens, then the drawn one at n_r, -1 behind
+ *   out_path       device int32 [n_rows] or NULL: the accepted nodes, -1 from n_r on
+ * Sums and tests are fp64.  A request with a node whose parent is not an earlier one (DSPARK_DEV_BAD_TREE), a token outside
+ * [0, V) (DSPARK_DEV_BAD_TOKEN), more than DSPARK_TREE_MAX_NODES nodes or no row at all (DSPARK_DEV_BAD_OFFSETS), or NaN, an
+ * infinity or no mass in what it looks at (DSPARK_DEV_BAD_ROW) is voided: accepted_len 0, its tokens and path -1.  (With
+ * offsets that are not ascending within [0, n_rows], only accepted_len is written.)
+ * Reads one entry of p and q for every node, and the rows of a node when one of its children has been rejected or the walk
+ * ends there.  Limits: V <= 2^24, 1 <= R <= 2^20, n_rows <= 2^24.  Errors: INVALID_ARG, SHAPE, ALIGNMENT, CUDA.  No workspace.
+ */
+#define DSPARK_TREE_MAX_NODES 1024
+int dspark_verify_tree(const float* target_probs, int64_t target_row_stride, const float* draft_probs, int64_t draft_row_stride,
+                       int V, const int32_t* tokens, const int32_t* parents, const int32_t* row_offsets, int R, int n_rows,
+                       const float* u_accept, const float* u_sample, int32_t* accepted_len, int32_t* out_tokens,
+                       int32_t* out_path, int32_t* dev_status, void* stream);
+
 /* The two uniforms of (seed, request, position) exactly as the verifier draws them
  * (host computation; for tests and for replaying a step). */
 void dspark_uniforms(uint64_t seed, uint32_t request, uint32_t position,
@@ -595,7 +714,8 @@ enum {
     DSPARK_K_RESIDUAL = 4, DSPARK_K_FINALIZE = 5, DSPARK_K_GREEDY_STREAM = 6, DSPARK_K_GREEDY_DECIDE = 7,
     DSPARK_K_ROW_SCALE = 8, DSPARK_K_MARKOV_GEMM = 9, DSPARK_K_MARKOV_DRAW = 10, DSPARK_K_TRUNCATE = 11,
     DSPARK_K_RMS_NORM = 12, DSPARK_K_HEAD_INT8 = 13, DSPARK_K_HEAD_ROWS = 14, DSPARK_K_HEAD_LOSS = 15,
-    DSPARK_K_HEAD_GRAD = 16, DSPARK_K_COUNT = 17
+    DSPARK_K_HEAD_GRAD = 16, DSPARK_K_KV_WRITE = 17, DSPARK_K_KV_READ = 18, DSPARK_K_KV_COMMIT = 19,
+    DSPARK_K_TREE_ATTENTION = 20, DSPARK_K_TREE_COMBINE = 21, DSPARK_K_VERIFY_TREE = 22, DSPARK_K_COUNT = 23
 };
 int dspark_ktimer_create(int capacity, dspark_ktimer_t** out);
 int dspark_ktimer_destroy(dspark_ktimer_t* t);

@@ -17,13 +17,15 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libdspark.so")
 _lib: Optional[C.CDLL] = None
 
-DSPARK_F32, DSPARK_BF16 = 0, 1
+DSPARK_F32, DSPARK_BF16, DSPARK_I8, DSPARK_E4M3 = 0, 1, 2, 3
 DSPARK_SCHED_EARLY_STOP, DSPARK_SCHED_GLOBAL, DSPARK_SCHED_TOPK = 0, 1, 2
 DEV_BAD_OFFSETS, DEV_BAD_TOKEN, DEV_BAD_ROW, DEV_TIMEOUT = 1, 2, 4, 8
 DEV_CONF_CLAMPED, DEV_BUDGET_LT_R, DEV_ALL_NEG_INF, DEV_BAD_TEMPERATURE = 16, 32, 64, 128
+DEV_BAD_PAGE, DEV_BAD_TREE = 256, 512
+TREE_MAX_NODES = 1024
 (K_SCHEDULE, K_OFFSETS, K_STREAM, K_DECIDE, K_RESIDUAL, K_FINALIZE, K_GREEDY_STREAM, K_GREEDY_DECIDE,
  K_ROW_SCALE, K_MARKOV_GEMM, K_MARKOV_DRAW, K_TRUNCATE, K_RMS_NORM, K_HEAD_INT8, K_HEAD_ROWS, K_HEAD_LOSS, K_HEAD_GRAD,
- K_COUNT) = range(18)
+ K_KV_WRITE, K_KV_READ, K_KV_COMMIT, K_TREE_ATTENTION, K_TREE_COMBINE, K_VERIFY_TREE, K_COUNT) = range(24)
 
 EXPORTS = [
     "dspark_profile_create", "dspark_profile_destroy", "dspark_profile_table",
@@ -40,6 +42,8 @@ EXPORTS = [
     "dspark_rms_norm_quant", "dspark_lm_head_quantize", "dspark_lm_head_int8",
     "dspark_lm_head_loss_workspace_bytes", "dspark_lm_head_loss", "dspark_lm_head_loss_backward",
     "dspark_lm_head_loss_backward_from_loss",
+    "dspark_kv_write", "dspark_kv_read", "dspark_kv_commit", "dspark_tree_attention_workspace_bytes", "dspark_tree_attention",
+    "dspark_verify_tree",
     "dspark_ktimer_create", "dspark_ktimer_destroy", "dspark_ktimer_attach", "dspark_ktimer_reset",
     "dspark_ktimer_read", "dspark_set_stream_path", "dspark_set_wait_poll_limit", "dspark_status_string", "dspark_kernel_name",
     "dspark_version",
@@ -53,6 +57,14 @@ class DsparkError(RuntimeError):
 class SchedInfo(C.Structure):
     _fields_ = [("B", C.c_int32), ("n_admitted", C.c_int32), ("status", C.c_int32),
                 ("n_candidates", C.c_int32), ("tau", C.c_double), ("theta", C.c_double)]
+
+
+class KvCacheStruct(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("dtype", C.c_int32), ("n_layers", C.c_int32), ("n_pages", C.c_int32), ("page_size", C.c_int32),
+                ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("layer_stride", C.c_int64), ("page_stride", C.c_int64),
+                ("token_stride", C.c_int64), ("head_stride", C.c_int64), ("block_table", C.c_void_p),
+                ("block_table_stride", C.c_int64), ("max_pages", C.c_int32)]
 
 
 def lib() -> C.CDLL:
@@ -118,6 +130,14 @@ def lib() -> C.CDLL:
         L.dspark_lm_head_loss.argtypes = [vp, i64, vp, i64, vp, i32, i32, i32, vp, vp, vp, vp, sz, vp]
         L.dspark_lm_head_loss_backward_from_loss.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, i32, i32, i32, vp, i64, vp, i64, vp, vp, sz, vp]
         L.dspark_lm_head_loss_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, i32, i32, i32, vp, i64, vp, i64, vp, vp, sz, vp]
+        kv = C.POINTER(KvCacheStruct)
+        L.dspark_kv_write.argtypes = [kv, i32, vp, vp, i64, i64, vp, vp, i32, i32, vp, vp]
+        L.dspark_kv_read.argtypes = [kv, i32, vp, vp, i32, i32, vp, vp, i32, i64, i64, vp, vp]
+        L.dspark_kv_commit.argtypes = [kv, vp, vp, i32, i32, vp, vp, vp, vp, vp]
+        L.dspark_tree_attention_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        L.dspark_tree_attention_workspace_bytes.restype = sz
+        L.dspark_tree_attention.argtypes = [kv, i32, vp, i64, i64, i32, vp, vp, vp, i32, i32, C.c_float, vp, i64, i64, vp, vp, vp, sz, vp]
+        L.dspark_verify_tree.argtypes = [vp, i64, vp, i64, i32, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp]
         L.dspark_uniforms.argtypes = [u64, C.c_uint32, C.c_uint32, C.POINTER(C.c_float), C.POINTER(C.c_float)]
         L.dspark_uniforms.restype = None
         L.dspark_ktimer_create.argtypes = [i32, C.POINTER(vp)]
@@ -771,6 +791,189 @@ def dspark_lm_head_loss_backward(hidden: torch.Tensor, weight: torch.Tensor, lab
     else:
         rc = lib().dspark_lm_head_loss_backward_from_loss(*head, lp, _vec(loss, "loss", torch.float32, N, dev), *tail)
     _check(rc, "dspark_lm_head_loss_backward")
+
+
+# -------------------------------------------------------------- trees over a paged cache ----
+_CACHE_CODES = {torch.bfloat16: DSPARK_BF16, torch.int8: DSPARK_I8, torch.float8_e4m3fn: DSPARK_E4M3}
+
+
+class KvCache:
+    """A paged cache of K and V rows as the step's calls take it: the tensors, checked once.
+
+    k, v: CUDA tensors [n_pages, page_size, kv_heads, head_dim], or [n_layers, ...] for several layers, of bfloat16, int8 or
+    float8_e4m3fn; any strides that both share (unit inner stride).  k_scale, v_scale: fp32 [(n_layers,) n_pages, kv_heads,
+    page_size], contiguous, with the 8-bit types.  block_table: int32 [R, max_pages]; another one can be set (`set_block_table`).
+    """
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, block_table: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+                 v_scale: Optional[torch.Tensor] = None):
+        dev = _device_of(_need(k, "k"), "k")
+        if k.dtype not in _CACHE_CODES:
+            raise DsparkError("k must be bfloat16, int8 or float8_e4m3fn")
+        _here(_need(v, "v"), "v", k.dtype, dev)
+        if k.dim() not in (4, 5) or k.shape != v.shape or k.numel() == 0:
+            raise DsparkError("k and v must be [n_pages, page_size, kv_heads, head_dim] (or [n_layers, ...]) of one shape")
+        many = k.dim() == 5
+        shape = tuple(k.shape) if many else (1, *k.shape)
+
+        def steps(t):
+            s = list(t.stride()) if many else [0, *t.stride()]
+            for i, n in enumerate(shape):                   # the stride of a single entry carries no meaning
+                if n == 1 and i < 4:
+                    s[i] = 0
+            return s
+        s = steps(k)
+        if s != steps(v) or (s[4] != 1 and shape[4] > 1):
+            raise DsparkError("k and v must have the same strides, unit in the last dimension")
+        c = KvCacheStruct()
+        if k.dtype is not torch.bfloat16:
+            want = (shape[0], shape[1], shape[3], shape[2])
+            for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+                _here(_need(t, name), name, torch.float32, dev)
+                if (tuple(t.shape) if many else (1, *t.shape)) != want or not t.is_contiguous():
+                    raise DsparkError(f"{name} must be contiguous, [n_pages, kv_heads, page_size] in each layer")
+            c.k_scale, c.v_scale = k_scale.data_ptr(), v_scale.data_ptr()
+        c.k, c.v, c.dtype = k.data_ptr(), v.data_ptr(), _CACHE_CODES[k.dtype]
+        c.n_layers, c.n_pages, c.page_size, c.kv_heads, c.head_dim = shape
+        c.layer_stride, c.page_stride, c.token_stride, c.head_stride = s[:4]
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.struct, self.ref, self.device, self.kv_heads, self.head_dim = c, C.byref(c), dev, shape[3], shape[4]
+        self.set_block_table(block_table)
+
+    def set_block_table(self, block_table: torch.Tensor) -> None:
+        t = _need(block_table, "block_table")
+        _here(t, "block_table", torch.int32, self.device)
+        if t.dim() != 2 or t.numel() == 0 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+            raise DsparkError("block_table must be [R, max_pages] with unit inner stride")
+        self.block_table, self.requests = t, t.shape[0]
+        self.struct.block_table, self.struct.max_pages = t.data_ptr(), t.shape[1]
+        self.struct.block_table_stride = t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _heads(t, name: str, dtype, rows: int, heads: int, d: int, dev: int):
+    """(address, row stride, head stride) of [rows, heads, d] with unit inner stride."""
+    _here(t, name, dtype, dev)
+    shape, s = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] < rows or shape[1] != heads or shape[2] != d:
+        raise DsparkError(f"{name} must be [{rows}, {heads}, {d}], got {list(shape)}")
+    if s[2] != 1:
+        raise DsparkError(f"{name} must have unit inner stride")
+    return t.data_ptr(), s[0] if shape[0] > 1 else 0, s[1] if heads > 1 else 0
+
+
+def _step(cache: KvCache, first, row_offsets):
+    """The step's arrays: (first, row_offsets) addresses, R; the cache's device is the current one."""
+    dev = cache.device
+    if dev != torch.cuda.current_device():
+        raise DsparkError("the cache must be on the current device")
+    R = _need(row_offsets, "row_offsets").numel() - 1
+    if R < 1 or R > cache.requests:
+        raise DsparkError("row_offsets needs R + 1 entries, the block table R rows")
+    return dev, R, _vec(_need(first, "first"), "first", torch.int32, R, dev), _vec(row_offsets, "row_offsets", torch.int32, R + 1, dev)
+
+
+def _layer(cache: KvCache, layer: int) -> int:
+    if not 0 <= layer < cache.struct.n_layers:
+        raise DsparkError(f"layer {layer} is outside the cache's {cache.struct.n_layers}")
+    return layer
+
+
+def dspark_kv_write(cache: KvCache, k: torch.Tensor, v: torch.Tensor, first: torch.Tensor, row_offsets: torch.Tensor, *,
+                    layer: int = 0, dev_status: torch.Tensor) -> None:
+    """K and V rows [n_rows, kv_heads, head_dim] of a step into the cache, quantised where it holds 8 bits."""
+    dev, R, fp, op = _step(cache, first, row_offsets)
+    n = _need(k, "k").shape[0]
+    kp, row, head = _heads(k, "k", torch.bfloat16, n, cache.kv_heads, cache.head_dim, dev)
+    vp, vrow, vhead = _heads(_need(v, "v"), "v", torch.bfloat16, n, cache.kv_heads, cache.head_dim, dev)
+    if v.shape[0] != n or (vrow, vhead) != (row, head):
+        raise DsparkError("k and v must have the same rows and strides")
+    rc = lib().dspark_kv_write(cache.ref, _layer(cache, layer), kp, vp, row, head, fp, op, R, n,
+                               _vec(_need(dev_status, "dev_status"), "dev_status", torch.int32, 1, dev), _stream())
+    if rc:
+        _check(rc, "dspark_kv_write")
+
+
+def dspark_kv_read(cache: KvCache, first: torch.Tensor, row_offsets: torch.Tensor, *, out_k: Optional[torch.Tensor] = None,
+                   out_v: Optional[torch.Tensor] = None, layer: int = 0, dev_status: torch.Tensor) -> None:
+    """The rows at the step's positions back from the cache, as bfloat16 or float32 values."""
+    dev, R, fp, op = _step(cache, first, row_offsets)
+    some = out_k if out_k is not None else _need(out_v, "out_k or out_v")
+    dtype, n = some.dtype, some.shape[0]
+    if dtype is not torch.bfloat16 and dtype is not torch.float32:
+        raise DsparkError("out_k and out_v must be float32 or bfloat16")
+    kp, row, head = _heads(some, "out_k" if out_k is not None else "out_v", dtype, n, cache.kv_heads, cache.head_dim, dev)
+    vp = None
+    if out_k is None:
+        kp, vp = None, kp
+    elif out_v is not None:
+        vp, vrow, vhead = _heads(out_v, "out_v", dtype, n, cache.kv_heads, cache.head_dim, dev)
+        if out_v.shape[0] != n or (vrow, vhead) != (row, head):
+            raise DsparkError("out_k and out_v must have the same rows and strides")
+    rc = lib().dspark_kv_read(cache.ref, _layer(cache, layer), fp, op, R, n, kp, vp, DSPARK_F32 if dtype is torch.float32 else DSPARK_BF16,
+                              row, head, _vec(_need(dev_status, "dev_status"), "dev_status", torch.int32, 1, dev), _stream())
+    if rc:
+        _check(rc, "dspark_kv_read")
+
+
+def dspark_kv_commit(cache: KvCache, first: torch.Tensor, row_offsets: torch.Tensor, accepted_len: torch.Tensor, path: torch.Tensor, *,
+                     out_first: Optional[torch.Tensor] = None, dev_status: torch.Tensor) -> None:
+    """Moves the accepted nodes' rows of all layers together behind the root; out_first: the next step's `first`."""
+    dev, R, fp, op = _step(cache, first, row_offsets)
+    n = _need(path, "path").numel()
+    rc = lib().dspark_kv_commit(cache.ref, fp, op, R, n, _vec(_need(accepted_len, "accepted_len"), "accepted_len", torch.int32, R, dev),
+                                _vec(path, "path", torch.int32, n, dev), _vec(out_first, "out_first", torch.int32, R, dev),
+                                _vec(_need(dev_status, "dev_status"), "dev_status", torch.int32, 1, dev), _stream())
+    if rc:
+        _check(rc, "dspark_kv_commit")
+
+
+def dspark_tree_attention_workspace_bytes(n_rows: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
+    return int(lib().dspark_tree_attention_workspace_bytes(n_rows, q_heads, kv_heads, head_dim))
+
+
+def dspark_tree_attention(q: torch.Tensor, cache: KvCache, first: torch.Tensor, row_offsets: torch.Tensor, *,
+                          parents: Optional[torch.Tensor] = None, scale: float, out: torch.Tensor,
+                          out_lse: Optional[torch.Tensor] = None, layer: int = 0, dev_status: torch.Tensor,
+                          workspace: torch.Tensor) -> None:
+    """Attention of the step's nodes [n_rows, q_heads, head_dim] over the cache; parents None: chains."""
+    dev, R, fp, op = _step(cache, first, row_offsets)
+    if _need(q, "q").dim() != 3:
+        raise DsparkError("q must be [n_rows, q_heads, head_dim]")
+    n, hq, d = q.shape
+    if d != cache.head_dim or hq % cache.kv_heads:
+        raise DsparkError("q must have the cache's head_dim and a multiple of its heads")
+    qp, qr, qh = _heads(q, "q", torch.bfloat16, n, hq, d, dev)
+    yp, yr, yh = _heads(_need(out, "out"), "out", torch.bfloat16, n, hq, d, dev)
+    _need(workspace, "workspace")
+    rc = lib().dspark_tree_attention(cache.ref, _layer(cache, layer), qp, qr, qh, hq, fp, op, _vec(parents, "parents", torch.int32, n, dev),
+                                     R, n, scale, yp, yr, yh, _vec(out_lse, "out_lse", torch.float32, n * hq, dev),
+                                     _vec(_need(dev_status, "dev_status"), "dev_status", torch.int32, 1, dev),
+                                     _vec(workspace, "workspace", workspace.dtype, 0, dev), workspace.numel() * workspace.element_size(),
+                                     _stream())
+    if rc:
+        _check(rc, "dspark_tree_attention")
+
+
+def dspark_verify_tree(target_probs: torch.Tensor, draft_probs: Optional[torch.Tensor], tokens: torch.Tensor, parents: torch.Tensor,
+                       row_offsets: torch.Tensor, u_accept: torch.Tensor, u_sample: torch.Tensor, *, accepted_len: torch.Tensor,
+                       out_tokens: torch.Tensor, out_path: Optional[torch.Tensor] = None, dev_status: torch.Tensor) -> None:
+    """Lossless verification of drafted trees; draft_probs None: the drafted tokens were chosen, not drawn."""
+    n, V = _matrix(target_probs, "target_probs")
+    dev = _device_of(target_probs, "target_probs")
+    R = _need(row_offsets, "row_offsets").numel() - 1
+    pp, ps = _rows(target_probs, "target_probs", torch.float32, n, V, dev)
+    qp, qs = _rows(draft_probs, "draft_probs", torch.float32, n, V, dev)
+    rc = lib().dspark_verify_tree(pp, ps, qp, qs, V, _vec(_need(tokens, "tokens"), "tokens", torch.int32, n, dev),
+                                  _vec(_need(parents, "parents"), "parents", torch.int32, n, dev),
+                                  _vec(row_offsets, "row_offsets", torch.int32, 2, dev), R, n,
+                                  _vec(_need(u_accept, "u_accept"), "u_accept", torch.float32, n, dev),
+                                  _vec(_need(u_sample, "u_sample"), "u_sample", torch.float32, R, dev),
+                                  _vec(_need(accepted_len, "accepted_len"), "accepted_len", torch.int32, R, dev),
+                                  _vec(_need(out_tokens, "out_tokens"), "out_tokens", torch.int32, n, dev),
+                                  _vec(out_path, "out_path", torch.int32, n, dev),
+                                  _vec(_need(dev_status, "dev_status"), "dev_status", torch.int32, 1, dev), _stream())
+    if rc:
+        _check(rc, "dspark_verify_tree")
 
 
 def dspark_uniforms(seed: int, request: int, position: int):

@@ -187,7 +187,8 @@ const char* dspark_kernel_name(int id)
     static const char* names[DSPARK_K_COUNT] = {
         "schedule", "build_offsets", "stream_stats", "decide", "residual_stream", "finalize",
         "greedy_stream", "greedy_decide", "row_scale", "markov_gemm", "markov_draw", "truncate",
-        "rms_norm", "lm_head_int8", "lm_head_rows", "lm_head_loss", "lm_head_grad"};
+        "rms_norm", "lm_head_int8", "lm_head_rows", "lm_head_loss", "lm_head_grad",
+        "kv_write", "kv_read", "kv_commit", "tree_attention", "tree_combine", "verify_tree"};
     return (id >= 0 && id < DSPARK_K_COUNT) ? names[id] : "?";
 }
 
