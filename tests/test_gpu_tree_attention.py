@@ -165,6 +165,36 @@ def test_a_prefix_position_with_nan_reaches_every_row():
     assert torch.isnan(got[..., 9]).all() and torch.isfinite(got[..., :9]).all()
 
 
+def test_nan_codes_of_other_nodes():
+    # 0x7f and 0xff are e4m3's NaN: dspark_kv_write stores none, another writer may
+    first, nodes = [60, 127], [20, 10]
+    parents = T.random_parents(nodes, 3, "star")
+    cache, q = step(first, nodes, 16, 2, 4, 64, "e4m3", seed=10)
+    clean = check(cache, q, first, nodes, parents, 0.2)
+    pg, at = cache.slots(0, [67, 68])
+    cache.v.view(torch.uint8)[0, pg, at, :, 3] = 0x7f
+    cache.k.view(torch.uint8)[0, pg[:1], at[:1], :, 5] = 0xff
+    got, _, st = T.run_attention(cache, q, T.i32(first), T.offsets(nodes), T.i32(parents), 0.2)
+    others = torch.ones(30, dtype=torch.bool, device="cuda")
+    others[7:9] = False
+    assert st == 0 and torch.equal(got[others], clean[others])
+    assert torch.isnan(got[7]).all() and torch.isnan(got[8, :, 3]).all() and torch.equal(got[8, :, 4:], clean[8, :, 4:])
+
+
+def test_large_scales_of_other_nodes():
+    # what a node that a row does not see has stored is not in that row's arithmetic, whatever its size
+    first, nodes = [60], [20]
+    parents = T.random_parents(nodes, 3, "star")
+    cache, q = step(first, nodes, 16, 2, 4, 64, "int8", seed=10)
+    clean = check(cache, q, first, nodes, parents, 0.2)
+    pg, at = cache.slots(0, [67, 68])
+    cache.vs[0, pg, :, at] = 1e30
+    got, _, _ = T.run_attention(cache, q, T.i32(first), T.offsets(nodes), T.i32(parents), 0.2)
+    others = torch.ones(20, dtype=torch.bool, device="cuda")
+    others[7:9] = False
+    assert torch.equal(got[others], clean[others]) and torch.isfinite(got).all()
+
+
 def test_rows_strides_outputs_in_place_and_rows_behind_the_last_request():
     first, nodes, d = [50, 10], [6, 3], 64
     cache, q0 = step(first, nodes, 16, 2, 4, d, "bf16", seed=12)

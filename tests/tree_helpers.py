@@ -158,7 +158,12 @@ def attention(cache, q, first, off, parents, scale, layer=0):
     bound: how far bf16 arithmetic may be off, element by element.  With a = sum w |v|: every weight is rounded to 16 bits
     (2^-8 a), the result to bf16 (2^-8 |out|); scores are fp32 sums of d products, off by at most d 2^-23 of the sum of their
     magnitudes (the tensor cores cut instead of rounding), which moves every weight by twice that; exponentials, the sum of
-    the weights and its division: 2^-20 for lengths below 2^17 in runs of 128 added up in fp32."""
+    the weights and its division: 2^-20 for lengths below 2^17 in runs of 128 added up in fp32.
+
+    8-bit caches: the weights times V's scales are fp16 numbers whose smallest step is 2^-24, half of it lost at most.  They
+    are stored with the largest weight of a cache tile times a power of two above its largest scale at 2^7 or more: a position
+    is off by at most 2^-25 / 2^7 of that product, which is at most twice the largest weight times the largest scale of the
+    positions seen, times the largest stored value (127 or 448)."""
     rows, hq, d = q.shape
     h = cache.heads
     g = hq // h
@@ -179,7 +184,12 @@ def attention(cache, q, first, off, parents, scale, layer=0):
             a = torch.einsum("hgl,lhd->hgd", w, v.abs())
             off_by = (d * 2.0 ** -23 * size + 2.0 ** -20)
             out[row], lse[row] = o.reshape(hq, d), torch.logsumexp(z, -1).reshape(hq)
-            bound[row] = (2.0 ** -8 * (a + o.abs()) * 1.01 + 2 * off_by[..., None] * a + 1e-37).reshape(hq, d)
+            tiny = torch.zeros(h, 1, 1, dtype=torch.float64, device="cuda")
+            if cache.kind != "bf16":
+                pg, at = cache.slots(r, pos)
+                scale_top = cache.vs[layer, pg, :, at].double().amax(0)
+                tiny = (len(pos) * 2.0 ** -32 * 2 * (127 if cache.kind == "int8" else 448) * scale_top)[:, None, None] * w.amax(-1, keepdim=True)
+            bound[row] = (tiny + 2.0 ** -8 * (a + o.abs()) * 1.01 + 2 * off_by[..., None] * a + 1e-37).reshape(hq, d)
             lse_bound[row] = off_by.reshape(hq) + 2.0 ** -22 * (1 + lse[row].abs())
     return out, bound, lse, lse_bound
 
