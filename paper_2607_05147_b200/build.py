@@ -13,7 +13,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libdspark.so")
 SOURCES = ["api.cu", "schedule.cu", "verify.cu", "markov.cu", "sts.cu", "truncate.cu", "truncate_f32.cu",
-           "norm.cu", "lm_head.cu", "kv_cache.cu", "tree_attention.cu", "verify_tree.cu"]
+           "norm.cu", "lm_head.cu", "kv_cache.cu", "tree_attention.cu",
+           "tree_attention_few.cu", "verify_tree.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC,-ffp-contract=off,-fvisibility=default"]
 

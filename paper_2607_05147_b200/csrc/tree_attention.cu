@@ -20,193 +20,10 @@
 //     multiply the scores and those of V the weights, so that neither is rounded into the operands.
 //
 // Bound by the cache's bytes where a K/V head has up to about 128 rows (bf16), by the exponentials and the products beyond.
-#include <cuda_bf16.h>
-#include <math.h>
-
-#include "kv_cache.cuh"
-#include "tcgen05.cuh"
+#include "tree_attention.cuh"
 
 namespace dspark {
 
-constexpr int kAttnMaxDim = 128;
-constexpr int kAttnSms = 148;                    // a B200's: the workspace's size is known without the device
-constexpr int kAttnTile = 128;                   // rows of a row tile, positions of a cache tile
-constexpr int kChunkBytes = kAttnTile * 128;     // 64 columns of 16 bits of a tile: 128 rows of 128 bytes, swizzled
-constexpr int kAttnMaxSlots = 12, kAttnMaxRaw = 8, kAttnScaleTiles = 4;
-constexpr int kAttnRingBytes = 7 * 2 * kChunkBytes;           // 224 KB: Q and the ring
-constexpr int kAttnNarrowBytes = 208 * 1024;                  // with 8-bit caches (4 KB of scales beside it)
-constexpr float kAttnLog2e = 1.4426950408889634f;
-constexpr float kAttnLazy = 8.f;                 // O is scaled when the maximum rises by more than 2^8
-constexpr float kAttnNarrowOffset = 7.f;         // fp16 weights: up to 2^(7 + 8) of 65 504, down to 2^-31 of the largest
-constexpr int kSoftmaxWarps = 8;
-constexpr int kAttnUnitFlags = 8;               // units of one CTA that are under way at a time: at most four
-
-enum AttnKind { kAttnWide = 0, kAttnI8 = 1, kAttnE4M3 = 2 };
-
-struct AttnParams {
-    KvView c;
-    const unsigned char* q; long long q_row, q_head;          // bytes
-    unsigned char* out; long long out_row, out_head;
-    float* out_lse;
-    const int32_t* first; const int32_t* row_offsets; const int32_t* parents;
-    int R, n_rows, q_heads, group;
-    float score_factor;                          // |scale| log2(e)
-    uint32_t q_sign;                             // sign bits of a pair to flip where scale is negative
-    int q_tiles;                                 // row tiles of a unit: 1 or 2
-    int chunks;                                  // of 64 columns: 1 or 2
-    int slots, raw_slots;                        // 16-bit tiles of the ring, 8-bit tiles
-    int tile_tokens, page_tiles, page_boxes;     // positions of a box; cache tiles of a page (pages above 128) ; boxes of a tile
-    int part_rows;                               // rows of a partial result
-    int32_t* dev_status;
-    int4* cuts;                                  // workspace: [kAttnSms] (1 + head, last CTA, first row, nodes); 0: none
-    float* parts;                                // [2 kAttnSms][part_rows][d]
-    float2* part_stats;                          // [2 kAttnSms][part_rows]
-};
-
-// ---- the work list ---------------------------------------------------------------------------------------
-// cache tiles that hold positions 0 .. length - 1
-__device__ __forceinline__ int attn_tiles(const AttnParams& P, int length)
-{
-    if (P.c.page_size <= kAttnTile) return (length + kAttnTile - 1) / kAttnTile;
-    const int pages = length / P.c.page_size;
-    return pages * P.page_tiles + (length - pages * P.c.page_size + kAttnTile - 1) / kAttnTile;
-}
-// first position of a cache tile and the positions that belong to it
-__device__ __forceinline__ void attn_tile_at(const AttnParams& P, int j, int& start, int& len)
-{
-    if (P.c.page_size <= kAttnTile) { start = j * kAttnTile; len = kAttnTile; return; }
-    const int page = j / P.page_tiles, at = (j - page * P.page_tiles) * kAttnTile;
-    start = page * P.c.page_size + at;
-    len = min(kAttnTile, P.c.page_size - at);
-}
-
-struct AttnUnit {
-    int r, head, row_tile;                       // row_tile: of q_tiles tiles
-    int row0, n, first;                          // the request
-    int node0, length;                           // first node of the unit; positions that any of its nodes may see
-    int tiles, j0, j1;                           // cache tiles of the unit; those of this CTA
-    bool pair;                                   // the second row tile has nodes
-};
-// The units of one CTA, in order.
-struct AttnIter {
-    int r, head, row_tile, j;
-    long long left;
-    int row0, n, first;                          // of request r
-    __device__ __forceinline__ void request(const AttnParams& P)
-    {
-        for (; r < P.R; ++r) {
-            const KvRequest q = kv_request(P.first, P.row_offsets, r, P.n_rows, kv_capacity(P.c));
-            if (q.n > 0) { row0 = q.row0; n = q.n; first = q.first; return; }
-        }
-        left = 0;
-    }
-    __device__ __forceinline__ bool next(const AttnParams& P, AttnUnit& u)
-    {
-        if (left <= 0) return false;
-        const int tile_nodes = kAttnTile / P.group, nodes = tile_nodes * P.q_tiles;
-        u.r = r; u.head = head; u.row_tile = row_tile;
-        u.row0 = row0; u.n = n; u.first = first;
-        u.node0 = row_tile * nodes;
-        u.length = first + min(n, u.node0 + nodes);
-        u.tiles = attn_tiles(P, u.length);
-        u.pair = P.q_tiles == 2 && n > u.node0 + tile_nodes;
-        u.j0 = j;
-        u.j1 = (int)min((long long)u.tiles, j + left);
-        left -= u.j1 - u.j0;
-        j = 0;
-        if (u.node0 + nodes < n) ++row_tile;
-        else {
-            row_tile = 0;
-            if (++head == P.c.kv_heads) { head = 0; ++r; if (left > 0) request(P); }
-        }
-        return true;
-    }
-};
-// cache tiles of one K/V head of a request
-__device__ __forceinline__ long long attn_head_tiles(const AttnParams& P, int first, int n)
-{
-    const int nodes = kAttnTile / P.group * P.q_tiles;
-    long long sum = 0;
-    for (int at = 0; at < n; at += nodes) sum += attn_tiles(P, first + min(n, at + nodes));
-    return sum;
-}
-
-// ---- PTX -------------------------------------------------------------------------------------------------
-__device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, int x, int y, int z, int w, uint64_t* bar)
-{
-    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
-                 ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
-                 : "memory");
-}
-__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-// 128-byte swizzle, descriptor version 1; groups of 8 rows (k-major) or of 8 k (mn-major) are 1 024 bytes apart.  mn-major:
-// the next 64 mn elements are a chunk further.
-__device__ __forceinline__ uint64_t attn_desc(uint32_t addr, bool mn_major)
-{
-    const uint64_t lead = mn_major ? (uint64_t)(kChunkBytes >> 4) : 1ull;
-    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (lead << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
-}
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
-{
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
-}
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
-{
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
-}
-__device__ __forceinline__ void tmem_load16(uint32_t taddr, float (&v)[16])
-{
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
-                 "tcgen05.wait::ld.sync.aligned;"
-                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
-                   "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
-                 : "r"(taddr) : "memory");
-}
-__device__ __forceinline__ void tmem_store16(uint32_t taddr, const uint32_t (&v)[16])
-{
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
-                 ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
-                   "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
-}
-__device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-template <bool kHalf>
-__device__ __forceinline__ uint32_t pack16(float lo, float hi)
-{
-    uint32_t r;
-    if (kHalf) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-// the largest of those of four scales that are finite and asked for
-__device__ __forceinline__ float attn_finite_max(float4 x, uint32_t of, float top)
-{
-    if ((of & 1u) && x.x < INFINITY) top = fmaxf(top, x.x);
-    if ((of & 2u) && x.y < INFINITY) top = fmaxf(top, x.y);
-    if ((of & 4u) && x.z < INFINITY) top = fmaxf(top, x.z);
-    if ((of & 8u) && x.w < INFINITY) top = fmaxf(top, x.w);
-    return top;
-}
-// e with 2^e > x, of a size that keeps the softmax's sum in range
-__device__ __forceinline__ float attn_exponent(float x) { return fmaxf((float)((int)(__float_as_uint(x) >> 23) - 126), -60.f); }
-// four 8-bit values as fp16, exactly
-template <int kKind>
-__device__ __forceinline__ uint2 widen4(uint32_t w)
-{
-    uint2 r;
-    if (kKind == kAttnI8) {
-        // 0x6400 + b is 1024 + b: with b = value + 128, 1152 is taken off
-        const uint32_t x = w ^ 0x80808080u;
-        const uint32_t a = __byte_perm(x, 0x64646464u, 0x4140), b = __byte_perm(x, 0x64646464u, 0x4342);
-        asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r.x) : "r"(a), "r"(0x64806480u));
-        asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r.y) : "r"(b), "r"(0x64806480u));
-    } else {
-        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r.x) : "h"((uint16_t)w));
-        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r.y) : "h"((uint16_t)(w >> 16)));
-    }
-    return r;
-}
 // ---- the kernel ------------------------------------------------------------------------------------------
 struct AttnShared {
     uint64_t full[kAttnMaxSlots], empty[kAttnMaxSlots];       // 16-bit tiles
@@ -214,8 +31,7 @@ struct AttnShared {
     uint64_t q_full, s_full[2], p_full[2], o_full[2], merge_ready, merge_done, mma_done;
     uint32_t tmem_base;
     int abort, bad_value[kAttnUnitFlags];
-    int start_r;
-    long long start_left, scan[16], start_at;
+    AttnList list;
     float2 second[kAttnTile];                    // (reference, sum) of the second group
 };
 template <int kKind>
@@ -256,133 +72,17 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
     }
     pdl_wait();
 
-    // This CTA's run of the work list: every thread sums the tiles of its requests, a scan places them.
-    const long long capacity = kv_capacity(P.c);
-    const int per = (P.R + kThreads - 1) / kThreads, r_lo = tid * per, r_hi = min(P.R, r_lo + per);
-    long long mine = 0;
-    int status = 0;
-    for (int r = r_lo; r < r_hi; ++r) {
-        const KvRequest q = kv_request(P.first, P.row_offsets, r, P.n_rows, capacity);
-        status |= q.status;
-        if (q.n > 0) mine += attn_head_tiles(P, q.first, q.n) * P.c.kv_heads;
-    }
-    if (status && blockIdx.x == 0) atomicOr(P.dev_status, status);
-    long long upto = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long y = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += y;
-    }
-    if (lane == 31) S.scan[warp] = upto;
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-    long long total = 0, before = 0;
-#pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) {
-        if (w == warp) before = total;
-        total += S.scan[w];
-    }
-    before += upto - mine;
-    const long long ctas = min((long long)gridDim.x, total);
-    const bool busy = (long long)blockIdx.x < ctas;
-    const long long x0 = busy ? total * blockIdx.x / ctas : 0, x1 = busy ? total * (blockIdx.x + 1) / ctas : 0;
-    if (busy && before <= x0 && x0 < before + mine) {
-        long long at = before;
-        int r = r_lo;
-        for (;; ++r) {
-            const KvRequest q = kv_request(P.first, P.row_offsets, r, P.n_rows, capacity);
-            const long long here = q.n > 0 ? attn_head_tiles(P, q.first, q.n) * P.c.kv_heads : 0;
-            if (x0 < at + here) break;
-            at += here;
-        }
-        S.start_r = r;
-        S.start_at = x0 - at;
-    }
-    __syncthreads();
+    AttnIter it = attn_begin<kThreads>(P, S.list);
     const uint32_t tmem = S.tmem_base;
     pdl_trigger();                               // the joining kernel only waits
     volatile int* abort_flag = &S.abort;
     auto give_up = [&]() { atomicOr(P.dev_status, DSPARK_DEV_TIMEOUT); *abort_flag = 1; };
-
-    AttnIter it;
-    it.left = x1 - x0;
-    int4 cut = make_int4(0, 0, 0, 0);
-    if (busy) {
-        it.r = S.start_r;
-        it.request(P);
-        long long at = S.start_at;
-        const long long head_tiles = attn_head_tiles(P, it.first, it.n);
-        it.head = (int)(at / head_tiles);
-        at -= it.head * head_tiles;
-        it.row_tile = 0;
-        const int nodes = kAttnTile / P.group * P.q_tiles;
-        int tiles;
-        for (;;) {
-            tiles = attn_tiles(P, it.first + min(it.n, (it.row_tile + 1) * nodes));
-            if (at < tiles) break;
-            at -= tiles;
-            ++it.row_tile;
-        }
-        it.j = (int)at;
-        // A unit that this CTA's start divides first: CTA blockIdx.x - 1 has its beginning, the others up to `last` go on with it
-        // from their starts.
-        const long long unit = x0 - at;
-        if (tid == 0 && at > 0 && total * ((long long)blockIdx.x - 1) / ctas <= unit) {
-            const long long end = unit + tiles - 1;
-            long long last = end * ctas / total;
-            while (total * (last + 1) / ctas <= end) ++last;
-            const int node0 = it.row_tile * nodes;
-            cut = make_int4(1 + it.head, (int)last, it.row0 + node0, min(it.n - node0, nodes));
-        }
-    }
-    if (tid == 0) P.cuts[blockIdx.x] = cut;
-    const int tile_nodes = kAttnTile / P.group;
+    const int tile_nodes = P.tile_nodes;
     AttnUnit u;
 
     if (warp == kProducer) {
-        // ---------------- K and V tiles ---------------------------------------------------------------------
-        const int slots = kNarrow ? P.raw_slots : P.slots, row_bytes = kNarrow ? d : 128, copies = kNarrow ? 1 : P.chunks;
-        const int slot_bytes = kNarrow ? kAttnTile * d : tile_bytes;
-        unsigned char* base = kNarrow ? raw : ring;
-        uint64_t* full = kNarrow ? S.raw_full : S.full;
-        uint64_t* empty = kNarrow ? S.raw_empty : S.empty;
-        const int box = lane / copies, chunk = lane - box * copies;          // a lane brings one box
-        int s = 0;
-        uint32_t ph = 0;
-        bool ok = true, bad_page = false;
-        while (ok && !*abort_flag && it.next(P, u)) {
-            const int32_t* table = P.c.block_table + u.r * P.c.table_stride;
-            for (int j = u.j0; ok && j < u.j1; ++j) {
-                int start, len;
-                attn_tile_at(P, j, start, len);
-                const int boxes = P.page_boxes == 1 ? 1 : (min(kAttnTile, u.length - start) + P.tile_tokens - 1) / P.tile_tokens;
-                const int page_of = start / P.c.page_size, y = P.page_boxes == 1 ? start - page_of * P.c.page_size : 0;
-                int page = 0;
-                if (box < boxes) {
-                    page = table[page_of + box];
-                    if (page < 0 || page >= P.c.n_pages) { page = P.c.n_pages; bad_page = true; }     // outside the map: zeros
-                }
-                for (int kv = 0; kv < 2; ++kv) {
-                    ok = __all_sync(0xffffffffu, mbar_wait_bounded(&empty[s], ph ^ 1u));
-                    if (!ok) break;
-                    if (lane == 0) mbar_arrive_expect_tx(&full[s], (uint32_t)(boxes * copies * P.tile_tokens * row_bytes));
-                    __syncwarp();
-                    if (box < boxes)
-                        tma_load_4d(base + (size_t)s * slot_bytes + chunk * kChunkBytes + box * P.tile_tokens * row_bytes, kv ? &map_v : &map_k,
-                                    chunk * 64, y, u.head, page, &full[s]);
-                    if (++s == slots) { s = 0; ph ^= 1u; }
-                }
-            }
-        }
-        if (bad_page) atomicOr(P.dev_status, DSPARK_DEV_BAD_PAGE);
-        if (!ok && lane == 0) give_up();
-        // Leave only after every copy has landed: its slot has been announced as free, or, where somebody gave up, is full.
-        for (int i = 0; i < slots; ++i) {
-            if (!*abort_flag) mbar_wait_bounded(&empty[s], ph ^ 1u);
-            else mbar_wait_bounded(&full[s], ph ^ 1u, 1u << 16);
-            if (++s == slots) { s = 0; ph ^= 1u; }
-        }
+        attn_produce<kNarrow>(P, it, map_k, map_v, kNarrow ? raw : ring, kNarrow ? S.raw_full : S.full, kNarrow ? S.raw_empty : S.empty,
+                              kNarrow ? P.raw_slots : P.slots, abort_flag);
     } else if (warp == kIssuer) {
         // ---------------- products --------------------------------------------------------------------------
         if (lane == 0) {
@@ -655,23 +355,8 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                     const uint32_t i = seq + 2 * jj + 1, s = i % P.slots;
                     if (!wait(&S.full[s], i / P.slots & 1u)) break;
                     if (start + row >= u.first || row >= valid) {
-                        unsigned char* v = ring + (size_t)s * tile_bytes + row * 128;
-                        for (int c = 0; c < 8 * P.chunks; ++c) {
-                            uint4* p = reinterpret_cast<uint4*>(v + (c >> 3) * kChunkBytes + (((c & 7) ^ (row & 7)) << 4));
-                            if (row >= valid) { *p = make_uint4(0, 0, 0, 0); continue; }
-                            uint4 x = *p;
-                            uint32_t w[4] = {x.x, x.y, x.z, x.w};
-                            bool bad = false;
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                if ((w[k] & 0x7f80u) == 0x7f80u) { w[k] &= 0xffff0000u; bad = true; }
-                                if ((w[k] & 0x7f800000u) == 0x7f800000u) { w[k] &= 0xffffu; bad = true; }
-                            }
-                            if (bad) {
-                                *p = make_uint4(w[0], w[1], w[2], w[3]);
-                                S.bad_value[units % kAttnUnitFlags] = 1;
-                            }
-                        }
+                        if (attn_clean_values(ring + (size_t)s * tile_bytes + row * 128, row, P.chunks, row < valid))
+                            S.bad_value[units % kAttnUnitFlags] = 1;
                     }
                     fence_async_smem();
                 }
@@ -728,30 +413,9 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
 #pragma unroll
                             for (int i = 0; i < 16; ++i) o[i] = o[i] * f0 + o1[i] * f1;
                         }
-                        if (bad_value && live) {
-                            int a = node;
-                            for (;;) {           // values that were left out of the product, where this row sees them
-                                const int position = done.first + a;
-                                const int page_of = position / P.c.page_size, token = position - page_of * P.c.page_size;
-                                const int j = P.c.page_size <= kAttnTile ? position / kAttnTile : page_of * P.page_tiles + token / kAttnTile;
-                                const int page = P.c.block_table[done.r * P.c.table_stride + page_of];
-                                if (j >= done.j0 && j < done.j1 && page >= 0 && page < P.c.n_pages) {
-                                    const unsigned char* v = P.c.v + page * P.c.page_stride + token * P.c.token_stride + done.head * P.c.head_stride;
+                        if (bad_value && live)   // values that were left out of the product, where this row sees them
 #pragma unroll
-                                    for (int i = 0; i < 16; ++i) {
-                                        if (kNarrow) { if ((v[c + i] & 0x7fu) == 0x7fu) o[i] = NAN; }
-                                        else {
-                                            const uint32_t x = reinterpret_cast<const uint16_t*>(v)[c + i];
-                                            if ((x & 0x7f80u) == 0x7f80u) o[i] += __uint_as_float(x << 16);
-                                        }
-                                    }
-                                }
-                                if (a == 0) break;
-                                const int p = P.parents ? P.parents[done.row0 + a] : a - 1;
-                                if (p < 0 || p >= a) break;
-                                a = p;
-                            }
-                        }
+                            for (int i = 0; i < 16; ++i) o[i] += attn_bad_values<kNarrow>(P, done, node, c + i);
                         if (live && whole) {
                             uint32_t w[8];
 #pragma unroll
@@ -781,81 +445,28 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
         // ---------------- 8-bit tiles to 16 bits --------------------------------------------------------------
         if constexpr (kNarrow) {
             const int ct = tid - (kSoftmaxWarps + 2) * 32;                  // 0 .. 127
-            const int pieces = d / 16, inverse = (65536 + pieces - 1) / pieces;   // 16-byte pieces of a position
-            int s = 0, rs = 0, tile_no = 0, unit_next = 0;
-            uint32_t ph = 0, rph = 0;
-            bool ok = true;
-            auto wait = [&](uint64_t* bar, uint32_t p) { ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, p)); return ok; };
             // scales of position ct of a tile
-            auto load_scales = [&](const AttnUnit& w, int j, float& k, float& v) {
+            float k_now = 0.f, v_now = 0.f;
+            auto load_scales = [&](const AttnUnit& w, int j) {
                 int start, len;
                 attn_tile_at(P, j, start, len);
-                k = v = 0.f;
+                k_now = v_now = 0.f;
                 if (ct >= min(len, w.length - start)) return;
                 const int position = start + ct, page_of = position / P.c.page_size, token = position - page_of * P.c.page_size;
                 const int page = P.c.block_table[w.r * P.c.table_stride + page_of];
                 if (page < 0 || page >= P.c.n_pages) return;
                 const long long at = ((long long)page * P.c.kv_heads + w.head) * P.c.page_size + token;
-                k = P.c.k_scale[at];
-                v = P.c.v_scale[at];
+                k_now = P.c.k_scale[at];
+                v_now = P.c.v_scale[at];
             };
-            bool have = it.next(P, u);
-            int j = u.j0;
-            float ks = 0.f, vs = 0.f;
-            if (have) load_scales(u, j, ks, vs);
-            while (ok && have && !*abort_flag) {
-                int start, len;
-                attn_tile_at(P, j, start, len);
-                const int valid = min(len, u.length - start);
-                const int tree = u.first - start;                           // positions from here on are nodes
-                const float k_now = ks * P.score_factor, v_now = vs;
-                const int unit_no = unit_next;
-                if (++j == u.j1) { have = it.next(P, u); j = u.j0; ++unit_next; }
-                if (have) load_scales(u, j, ks, vs);
-                for (int kv = 0; kv < 2; ++kv) {
-                    if (!wait(&S.raw_full[rs], rph) || !wait(&S.empty[s], ph ^ 1u)) break;
-                    if (kv == 0) {
-                        // free: the scores of tile_no - 2 are not computed before the weights of tile_no - 4 are there
-                        scales.k[tile_no % kAttnScaleTiles][ct] = k_now;
-                        scales.v[tile_no % kAttnScaleTiles][ct] = v_now;
-                    }
-                    const unsigned char* src = raw + (size_t)rs * kAttnTile * d;
-                    unsigned char* dst = ring + (size_t)s * tile_bytes;
-#pragma unroll 4
-                    for (int i = 0; i < pieces; ++i) {
-                        const int x = i * 128 + ct, token = x * inverse >> 16, piece = x - token * pieces;
-                        const uint4 w = *reinterpret_cast<const uint4*>(src + x * 16);
-                        uint2 a = widen4<kKind>(w.x), b = widen4<kKind>(w.y), c = widen4<kKind>(w.z), e = widen4<kKind>(w.w);
-                        if (token >= valid) a = b = c = e = make_uint2(0, 0);
-                        if (kKind == kAttnE4M3 && kv && token >= tree) {
-                            // a NaN among the nodes' values of V: as with 16 bits, zero here and back in the rows that see it
-                            uint32_t h[8] = {a.x, a.y, b.x, b.y, c.x, c.y, e.x, e.y};
-                            bool bad = false;
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) {
-                                if ((h[k] & 0x7c00u) == 0x7c00u) { h[k] &= 0xffff0000u; bad = true; }
-                                if ((h[k] & 0x7c000000u) == 0x7c000000u) { h[k] &= 0xffffu; bad = true; }
-                            }
-                            if (bad) {
-                                a = make_uint2(h[0], h[1]); b = make_uint2(h[2], h[3]); c = make_uint2(h[4], h[5]); e = make_uint2(h[6], h[7]);
-                                S.bad_value[unit_no % kAttnUnitFlags] = 1;
-                            }
-                        }
-                        unsigned char* line = dst + (piece >> 2) * kChunkBytes + token * 128;
-                        const int at = (piece & 3) * 2, turn = (piece >> 2) & 1;       // the two halves of eight lanes store in turn
-                        const uint4 lo = make_uint4(a.x, a.y, b.x, b.y), hi = make_uint4(c.x, c.y, e.x, e.y);
-                        *reinterpret_cast<uint4*>(line + (((at + turn) ^ (token & 7)) << 4)) = turn ? hi : lo;
-                        *reinterpret_cast<uint4*>(line + (((at + 1 - turn) ^ (token & 7)) << 4)) = turn ? lo : hi;
-                    }
-                    fence_async_smem();
-                    __syncwarp();
-                    if (lane == 0) { mbar_arrive(&S.raw_empty[rs]); mbar_arrive(&S.full[s]); }
-                    if (++rs == P.raw_slots) { rs = 0; rph ^= 1u; }
-                    if (++s == P.slots) { s = 0; ph ^= 1u; }
-                }
-                ++tile_no;
-            }
-            if (!ok && lane == 0) give_up();
+            auto store_scales = [&](int number) {
+                // free: the scores of tile number - 2 are not computed before the weights of tile number - 4 are there
+                scales.k[number % kAttnScaleTiles][ct] = k_now * P.score_factor;
+                scales.v[number % kAttnScaleTiles][ct] = v_now;
+            };
+            if (!attn_widen<kKind, 128>(P, it, ct, raw, ring, tile_bytes, S.raw_full, S.raw_empty, S.full, S.empty, S.bad_value, abort_flag, load_scales,
+                                        store_scales) && lane == 0)
+                give_up();
         }
     }
     tc_fence_before();
@@ -901,7 +512,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const __grid_co
         if (lane == 0) { s_cuts = n; s_start[n] = rows; }
     }
     __syncthreads();
-    const int cuts = s_cuts, d = P.c.head_dim, tile_rows = kAttnTile / P.group * P.group;
+    const int cuts = s_cuts, d = P.c.head_dim, tile_rows = P.tile_nodes * P.group;
     const int rows = s_start[cuts];
     int at = 0;
     for (int w = blockIdx.x * (kJoinThreads / 32) + (tid >> 5); w < rows; w += gridDim.x * (kJoinThreads / 32)) {
@@ -994,13 +605,7 @@ static int attn_launch(AttnParams& P, const CUtensorMap& k, const CUtensorMap& v
     constexpr bool kNarrow = kKind != kAttnWide;
     constexpr int kSmem = (kNarrow ? kAttnNarrowBytes : kAttnRingBytes) + 1024;
     static std::atomic<unsigned long long> ready{0};
-    int dev = 0;
-    cudaGetDevice(&dev);
-    const unsigned long long bit = 1ull << (dev & 63);
-    if (!(ready.load(std::memory_order_relaxed) & bit)) {
-        if (cudaFuncSetAttribute(attn_kernel<kKind>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return launch_status();
-        ready.fetch_or(bit, std::memory_order_relaxed);
-    }
+    if (!attn_allow_smem(attn_kernel<kKind>, kSmem, ready)) return launch_status();
     const int tile = P.chunks * kChunkBytes;
     if (kNarrow) {
         // four 16-bit tiles beside one of Q, three beside two; the rest for 8-bit ones
@@ -1061,8 +666,13 @@ int dspark_tree_attention(const dspark_kv_cache_t* cache, int layer, const void*
     P.score_factor = fabsf(scale) * kAttnLog2e;
     P.q_sign = scale < 0.f ? 0x80008000u : 0u;
     P.dev_status = dev_status;
-    // two row tiles a unit where the requests have more rows than one holds on average: their cache tiles are then read once
-    P.q_tiles = (long long)n_rows * P.group > (long long)kAttnTile * R ? 2 : 1;
+    // rows of a request with one K/V head on average
+    const long long rows = (long long)((n_rows + R - 1) / R) * P.group;
+    const bool few = rows <= 64;
+    // two row tiles a unit where one does not hold a request's rows: their cache tiles are then read once
+    P.q_tiles = rows > kAttnTile ? 2 : 1;
+    P.tile_nodes = (few ? (rows <= 16 ? 16 : rows <= 32 ? 32 : 64) : kAttnTile) / P.group;
+    P.unit_nodes = P.tile_nodes * P.q_tiles;
     P.chunks = d > 64 ? 2 : 1;
     P.tile_tokens = cache->page_size < kAttnTile ? cache->page_size : kAttnTile;
     P.page_boxes = kAttnTile / P.tile_tokens;
@@ -1077,7 +687,8 @@ int dspark_tree_attention(const dspark_kv_cache_t* cache, int layer, const void*
     cudaStream_t s = (cudaStream_t)stream;
     const int sms = attn_sms();
     int rc;
-    if (cache->dtype == DSPARK_BF16) rc = attn_launch<kAttnWide>(P, map_k, map_v, sms, s);
+    if (few) rc = attn_few_launch(P, (int)rows, map_k, map_v, sms, s);
+    else if (cache->dtype == DSPARK_BF16) rc = attn_launch<kAttnWide>(P, map_k, map_v, sms, s);
     else if (cache->dtype == DSPARK_I8) rc = attn_launch<kAttnI8>(P, map_k, map_v, sms, s);
     else rc = attn_launch<kAttnE4M3>(P, map_k, map_v, sms, s);
     if (rc) return rc;
