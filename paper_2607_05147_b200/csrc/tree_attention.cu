@@ -50,7 +50,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);   // swizzle atoms: 1 KB
     __shared__ AttnShared S;
     __shared__ __align__(16) AttnScales<kKind> scales;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;    // warp: uniform, and known to be
     const int d = P.c.head_dim, tile_bytes = P.chunks * kChunkBytes;
     unsigned char* sQ = smem;
     unsigned char* ring = smem + P.q_tiles * tile_bytes;
@@ -85,60 +85,71 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                               kNarrow ? P.raw_slots : P.slots, abort_flag);
     } else if (warp == kIssuer) {
         // ---------------- products --------------------------------------------------------------------------
-        if (lane == 0) {
-            const uint32_t type = kNarrow ? 0u : 1u;                        // fp16 or bf16 operands, fp32 sums
-            const uint32_t common = (1u << 4) | (type << 7) | (type << 10) | ((uint32_t)(kAttnTile >> 4) << 24);
-            const uint32_t idesc_s = common | ((uint32_t)(kAttnTile >> 3) << 17);
-            const uint32_t idesc_o = common | ((uint32_t)(d >> 3) << 17) | (1u << 16);
-            const uint32_t q0 = smem_u32(sQ), r0 = smem_u32(ring);
-            uint32_t units = 0, items[2] = {0, 0};
-            bool ok = true, issued = false;
-            // K and V tiles alternate in the ring; the places of the next of each
-            int ks = 0, vs = 1;
-            uint32_t kph = 0, vph = 0;
-            auto advance = [&](int& s, uint32_t& ph) { s += 2; if (s >= P.slots) { s -= P.slots; ph ^= 1u; } };
-            while (ok && !*abort_flag && it.next(P, u)) {
-                const int n = (u.j1 - u.j0) << (u.pair ? 1 : 0);
-                auto scores = [&](int t) {
-                    if (!mbar_wait_bounded(&S.full[ks], kph)) return false;
-                    tc_fence_after();
-                    const uint32_t a = q0 + (u.pair && t ? tile_bytes : 0), b = r0 + ks * tile_bytes;
-                    for (int k = 0; k < d / 16; ++k) {
-                        const uint32_t at = (uint32_t)((k >> 2) * kChunkBytes + (k & 3) * 32);
-                        mma_ss(tmem + t * 128, attn_desc(a + at, false), attn_desc(b + at, false), idesc_s, k > 0);
-                    }
-                    umma_commit(&S.s_full[t]);
-                    if (!u.pair || t) { umma_commit(&S.empty[ks]); advance(ks, kph); }
-                    issued = true;
-                    return true;
-                };
-                ok = mbar_wait_bounded(&S.q_full, units & 1u);
-                ++units;
-                if (!ok) break;
+        const uint32_t type = kNarrow ? 0u : 1u;                            // fp16 or bf16 operands, fp32 sums
+        const uint32_t common = (1u << 4) | (type << 7) | (type << 10) | ((uint32_t)(kAttnTile >> 4) << 24);
+        const uint32_t idesc_s = common | ((uint32_t)(kAttnTile >> 3) << 17);
+        const uint32_t idesc_o = common | ((uint32_t)(d >> 3) << 17) | (1u << 16);
+        const uint32_t q0 = desc_k_major(smem_u32(sQ)), k0 = desc_k_major(smem_u32(ring)), v0 = desc_mn_major(smem_u32(ring));
+        const uint32_t tile_step = (uint32_t)tile_bytes >> 4;
+        const int steps = d / 16;
+        uint32_t units = 0, items[2] = {0, 0};
+        bool ok = true, issued = false;
+        // K and V tiles alternate in the ring; the places of the next of each
+        uint32_t ks = 0, vs = 1, kph = 0, vph = 0;
+        auto advance = [&](uint32_t& s, uint32_t& ph) { s += 2; if (s >= (uint32_t)P.slots) { s -= P.slots; ph ^= 1u; } };
+        auto wait = [&](uint64_t* bar, uint32_t ph) { ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, ph)); return ok; };
+        while (ok && !__any_sync(0xffffffffu, *abort_flag) && it.next(P, u)) {
+            const int n = (u.j1 - u.j0) << (u.pair ? 1 : 0);
+            const bool pair = u.pair;
+            auto scores = [&](uint32_t t) {
+                if (!wait(&S.full[ks], kph)) return;
                 tc_fence_after();
-                ok = scores(0);
-                if (ok && n > 1) ok = scores(1);
-                for (int i = 0; ok && i < n; ++i) {
-                    const int t = i & 1;
-                    ok = mbar_wait_bounded(&S.p_full[t], items[t] & 1u) && mbar_wait_bounded(&S.full[vs], vph);
-                    ++items[t];
-                    if (!ok) break;
-                    tc_fence_after();
-                    const uint32_t b = r0 + vs * tile_bytes;
+                const uint32_t a = q0 + (pair && t ? tile_step : 0u), b = k0 + ks * tile_step;
+                const bool last = !pair || t;
+                if (elect_one()) {
+#pragma unroll
+                    for (int k = 0; k < kAttnMaxDim / 16; ++k)
+                        if (k < steps) {
+                            const uint32_t at = (uint32_t)((k >> 2) * (kChunkBytes >> 4) + (k & 3) * 2);
+                            mma_ss(tmem + t * 128, a + at, b + at, idesc_s, k > 0);
+                        }
+                    umma_commit(&S.s_full[t]);
+                    if (last) umma_commit(&S.empty[ks]);
+                }
+                __syncwarp();
+                if (last) advance(ks, kph);
+                issued = true;
+            };
+            if (!wait(&S.q_full, units & 1u)) break;
+            ++units;
+            tc_fence_after();
+            scores(0);
+            if (n > 1) scores(1);
+            for (int i = 0; ok && i < n; ++i) {
+                const uint32_t t = (uint32_t)(i & 1);
+                if (!wait(&S.p_full[t], (t ? items[1] : items[0]) & 1u) || !wait(&S.full[vs], vph)) break;
+                if (t) ++items[1]; else ++items[0];
+                tc_fence_after();
+                const uint32_t b = v0 + vs * tile_step;
+                const bool last = !pair || t;
+                if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < kAttnTile / 16; ++k)
-                        mma_ts(tmem + 256 + t * 128, tmem + t * 128 + k * 8, attn_desc(b + k * 2048, true), idesc_o, i > 1 || k > 0);
-                    if (!u.pair || t) { umma_commit(&S.empty[vs]); advance(vs, vph); }
-                    if (u.pair) { if (i + 2 >= n) umma_commit(&S.o_full[t]); }
+                        mma_ts(tmem + 256 + t * 128, tmem + t * 128 + k * 8, b + k * 128, idesc_o, i > 1 || k > 0);
+                    if (last) umma_commit(&S.empty[vs]);
+                    if (pair) { if (i + 2 >= n) umma_commit(&S.o_full[t]); }
                     else if (i + 1 == n) { umma_commit(&S.o_full[0]); umma_commit(&S.o_full[1]); }   // the groups share Q
-                    if (i + 2 < n) ok = scores(t);
                 }
+                __syncwarp();
+                if (last) advance(vs, vph);
+                if (i + 2 < n) scores(t);
             }
-            if (!ok) give_up();
-            if (issued) {
-                umma_commit(&S.mma_done);
-                mbar_wait_bounded(&S.mma_done, 0u);
-            }
+        }
+        if (!ok && lane == 0) give_up();
+        if (issued) {
+            if (elect_one()) umma_commit(&S.mma_done);
+            __syncwarp();
+            mbar_wait_bounded(&S.mma_done, 0u);
         }
         __syncwarp();
     } else if (warp < kSoftmaxWarps) {

@@ -148,7 +148,14 @@ __device__ __forceinline__ AttnIter attn_begin(const AttnParams& P, AttnList& S)
     before += upto - mine;
     const long long ctas = min((long long)gridDim.x, total);
     const bool busy = (long long)blockIdx.x < ctas;
-    const long long x0 = busy ? total * blockIdx.x / ctas : 0, x1 = busy ? total * (blockIdx.x + 1) / ctas : 0;
+    // the first `more` CTAs have one tile more than the others
+    long long each = 0, more = 0;
+    if (busy) {
+        if (total >> 32) { each = total / ctas; more = total - each * ctas; }
+        else { each = (uint32_t)total / (uint32_t)ctas; more = (uint32_t)total % (uint32_t)ctas; }     // four times as fast
+    }
+    auto run_start = [&](long long cta) { return each * cta + min(cta, more); };
+    const long long x0 = run_start(blockIdx.x), x1 = busy ? run_start(blockIdx.x + 1) : x0;
     if (busy && before <= x0 && x0 < before + mine) {
         long long at = before;
         int r = r_lo;
@@ -170,7 +177,7 @@ __device__ __forceinline__ AttnIter attn_begin(const AttnParams& P, AttnList& S)
         it.request(P);
         long long at = S.start_at;
         const long long head_tiles = attn_head_tiles(P, it.first, it.n);
-        it.head = (int)(at / head_tiles);
+        it.head = (at | head_tiles) >> 32 ? (int)(at / head_tiles) : (int)((uint32_t)at / (uint32_t)head_tiles);
         at -= it.head * head_tiles;
         it.row_tile = 0;
         const int nodes = P.unit_nodes;
@@ -185,12 +192,11 @@ __device__ __forceinline__ AttnIter attn_begin(const AttnParams& P, AttnList& S)
         // A unit that this CTA's start divides first: CTA blockIdx.x - 1 has its beginning, the others up to `last` go on with it
         // from their starts.
         const long long unit = x0 - at;
-        if (tid == 0 && at > 0 && total * ((long long)blockIdx.x - 1) / ctas <= unit) {
-            const long long end = unit + tiles - 1;
-            long long last = end * ctas / total;
-            while (total * (last + 1) / ctas <= end) ++last;
+        if (tid == 0 && at > 0 && run_start((long long)blockIdx.x - 1) <= unit) {
+            int last = blockIdx.x;
+            while (run_start(last + 1) < unit + tiles) ++last;
             const int node0 = it.row_tile * nodes;
-            cut = make_int4(1 + it.head, (int)last, it.row0 + node0, min(it.n - node0, nodes));
+            cut = make_int4(1 + it.head, last, it.row0 + node0, min(it.n - node0, nodes));
         }
     }
     if (tid == 0) P.cuts[blockIdx.x] = cut;
@@ -205,22 +211,30 @@ __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, i
                  : "memory");
 }
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-// 128-byte swizzle, descriptor version 1; groups of 8 rows (k-major) or of 8 k (mn-major) are 1 024 bytes apart.  mn-major:
-// the next 64 mn elements are a chunk further.
-__device__ __forceinline__ uint64_t attn_desc(uint32_t addr, bool mn_major)
+// Operands in shared memory: 128-byte swizzle, descriptor version 1; groups of 8 rows (k-major) or of 8 k (mn-major) are 1 024
+// bytes apart; mn-major: the next 64 mn elements are a chunk further.  The upper half of such a descriptor is a constant, a step
+// along k an addition to the lower one: 16 products were issued in 1 700 clocks where each built its descriptors from scratch.
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_k_major(uint32_t addr) { return (addr >> 4) | (1u << 16); }
+__device__ __forceinline__ uint32_t desc_mn_major(uint32_t addr) { return (addr >> 4) | ((uint32_t)(kChunkBytes >> 4) << 16); }
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate)
 {
-    const uint64_t lead = mn_major ? (uint64_t)(kChunkBytes >> 4) : 1ull;
-    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (lead << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 x, {%1, %5};\n\tmov.b64 y, {%2, %5};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "r"(kDescHigh) : "memory");
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 y;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 y, {%2, %5};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "r"(kDescHigh) : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+// one lane of a whole warp
+__device__ __forceinline__ bool elect_one()
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
 }
 __device__ __forceinline__ void tmem_load16(uint32_t taddr, float (&v)[16])
 {

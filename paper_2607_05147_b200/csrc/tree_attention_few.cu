@@ -57,23 +57,24 @@ template <int kCols> __device__ __forceinline__ void tmem_read(uint32_t addr, fl
     else { tmem_load32_issue(addr, v); tmem_load_wait(v); }
 }
 
-// 16 warps of threads widen 8-bit tiles where registers allow it (a block's warps share 64 K of them)
-template <int kKind, int kN> constexpr int kFewConverters = kKind == kAttnWide ? 0 : kN == 64 ? 4 : 8;
-template <int kKind, int kN> constexpr int kFewThreads = (kSoftmaxWarps + 2 + kFewConverters<kKind, kN>) * 32;
+template <int kKind> constexpr int kFewConverters = kKind == kAttnWide ? 0 : 4;
+template <int kKind> constexpr int kFewThreads = (kSoftmaxWarps + 2 + kFewConverters<kKind>) * 32;
 
 template <int kKind, int kN>
-__global__ void __launch_bounds__(kFewThreads<kKind, kN>, 1)
+__global__ void __launch_bounds__(kFewThreads<kKind>, 1)
 attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v)
 {
     constexpr bool kNarrow = kKind != kAttnWide;
-    constexpr int kThreads = kFewThreads<kKind, kN>, kProducer = kSoftmaxWarps, kIssuer = kSoftmaxWarps + 1;
-    constexpr int kWarps = kFewConverters<kKind, kN>, kCols = kN < 32 ? kN : 32;
+    constexpr int kThreads = kFewThreads<kKind>, kProducer = kSoftmaxWarps, kIssuer = kSoftmaxWarps + 1;
+    constexpr int kWarps = kFewConverters<kKind>, kCols = kN < 32 || (kNarrow && kN == 64) ? 16 : 32;
+    constexpr bool kKeep = kN <= 32; // a tile's scores stay in registers between the vote and the exponentials
+    constexpr int kParts = kKeep ? kN / kCols : 1;
     constexpr uint32_t kO = 128;                 // columns of tensor memory: S^T at 0 and 64, O^T at 128 and 192
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);   // swizzle atoms: 1 KB
     __shared__ FewShared S;
     __shared__ __align__(16) FewTables<kN> T;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;    // warp: uniform, and known to be
     const int d = P.c.head_dim, tile_bytes = P.chunks * kChunkBytes;
     unsigned char* sP = smem;
     unsigned char* sQ = sP + 2 * kFewPBytes;     // per 64 components: kN lines of 128 bytes
@@ -107,86 +108,97 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                               kNarrow ? P.raw_slots : P.slots, abort_flag);
     } else if (warp == kIssuer) {
         // ---------------- products --------------------------------------------------------------------------
-        if (lane == 0) {
-            const uint32_t type = kNarrow ? 0u : 1u;                        // fp16 or bf16 operands, fp32 sums
-            const uint32_t idesc_s = (1u << 4) | (type << 7) | (type << 10) | ((uint32_t)(kN >> 3) << 17) | ((uint32_t)(kAttnTile >> 4) << 24);
-            const uint32_t idesc_o = idesc_s | (1u << 15) | (1u << 16);
-            const uint32_t q0 = smem_u32(sQ), p0 = smem_u32(sP), r0 = smem_u32(ring);
-            uint32_t units = 0, items[2] = {0, 0};
-            bool ok = true, issued = false;
-            // K and V tiles alternate in the ring; the places of the next of each
-            int ks = 0, vs = 1;
-            uint32_t kph = 0, vph = 0;
-            auto advance = [&](int& s, uint32_t& ph) { s += 2; if (s >= P.slots) { s -= P.slots; ph ^= 1u; } };
-            while (ok && !*abort_flag && it.next(P, u)) {
-                const int n = u.j1 - u.j0;
-                auto scores = [&](int t) {
-                    if (!mbar_wait_bounded(&S.full[ks], kph)) return false;
-                    tc_fence_after();
-                    const uint32_t a = r0 + ks * tile_bytes;
-                    for (int k = 0; k < d / 16; ++k)
-                        mma_ss(tmem + t * 64, attn_desc(a + (k >> 2) * kChunkBytes + (k & 3) * 32, false),
-                               attn_desc(q0 + (k >> 2) * (kN * 128) + (k & 3) * 32, false), idesc_s, k > 0);
+        const uint32_t type = kNarrow ? 0u : 1u;                            // fp16 or bf16 operands, fp32 sums
+        const uint32_t idesc_s = (1u << 4) | (type << 7) | (type << 10) | ((uint32_t)(kN >> 3) << 17) | ((uint32_t)(kAttnTile >> 4) << 24);
+        const uint32_t idesc_o = idesc_s | (1u << 15) | (1u << 16);
+        const uint32_t q0 = desc_k_major(smem_u32(sQ)), p0 = desc_mn_major(smem_u32(sP));
+        const uint32_t k0 = desc_k_major(smem_u32(ring)), v0 = desc_mn_major(smem_u32(ring)), tile_step = (uint32_t)tile_bytes >> 4;
+        const int steps = d / 16;
+        uint32_t units = 0, items[2] = {0, 0};
+        bool ok = true, issued = false;
+        // K and V tiles alternate in the ring; the places of the next of each
+        uint32_t ks = 0, vs = 1, kph = 0, vph = 0;
+        auto advance = [&](uint32_t& s, uint32_t& ph) { s += 2; if (s >= (uint32_t)P.slots) { s -= P.slots; ph ^= 1u; } };
+        auto wait = [&](uint64_t* bar, uint32_t ph) { ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, ph)); return ok; };
+        while (ok && !__any_sync(0xffffffffu, *abort_flag) && it.next(P, u)) {
+            const int n = u.j1 - u.j0;
+            const uint32_t turn = units & 1u;                               // the group that has the even tiles
+            auto scores = [&](uint32_t t) {
+                if (!wait(&S.full[ks], kph)) return;
+                tc_fence_after();
+                const uint32_t a = k0 + ks * tile_step;
+                if (elect_one()) {
+#pragma unroll
+                    for (int k = 0; k < kAttnMaxDim / 16; ++k)
+                        if (k < steps)
+                            mma_ss(tmem + t * 64, a + (k >> 2) * (kChunkBytes >> 4) + (k & 3) * 2, q0 + (k >> 2) * (kN * 8) + (k & 3) * 2, idesc_s, k > 0);
                     umma_commit(&S.s_full[t]);
                     umma_commit(&S.empty[ks]);
-                    advance(ks, kph);
-                    issued = true;
-                    return true;
-                };
-                ok = mbar_wait_bounded(&S.q_full, units & 1u);
-                ++units;
-                if (!ok) break;
-                tc_fence_after();
-                ok = scores(0);
-                if (ok && n > 1) ok = scores(1);
-                for (int i = 0; ok && i < n; ++i) {
-                    const int t = i & 1;
-                    ok = mbar_wait_bounded(&S.p_full[t], items[t] & 1u) && mbar_wait_bounded(&S.full[vs], vph);
-                    ++items[t];
-                    if (!ok) break;
-                    tc_fence_after();
-                    const uint32_t a = r0 + vs * tile_bytes, b = p0 + t * kFewPBytes;
-#pragma unroll
-                    for (int k = 0; k < kAttnTile / 16; ++k)
-                        mma_ss(tmem + kO + t * 64, attn_desc(a + k * 2048, true), attn_desc(b + k * 2048, true), idesc_o, i > 1 || k > 0);
-                    umma_commit(&S.empty[vs]);
-                    advance(vs, vph);
-                    if (i + 1 == n) { umma_commit(&S.o_full[0]); umma_commit(&S.o_full[1]); }       // the groups share Q
-                    if (i + 2 < n) ok = scores(t);
                 }
+                __syncwarp();
+                advance(ks, kph);
+                issued = true;
+            };
+            if (!wait(&S.q_full, units & 1u)) break;
+            ++units;
+            tc_fence_after();
+            scores(turn);
+            if (n > 1) scores(turn ^ 1u);
+            for (int i = 0; ok && i < n; ++i) {
+                const uint32_t t = turn ^ (uint32_t)(i & 1);
+                if (!wait(&S.p_full[t], (t ? items[1] : items[0]) & 1u) || !wait(&S.full[vs], vph)) break;
+                if (t) ++items[1]; else ++items[0];
+                tc_fence_after();
+                const uint32_t a = v0 + vs * tile_step, b = p0 + t * (kFewPBytes >> 4);
+                if (elect_one()) {
+#pragma unroll
+                    for (int k = 0; k < kAttnTile / 16; ++k) mma_ss(tmem + kO + t * 64, a + k * 128, b + k * 128, idesc_o, i > 1 || k > 0);
+                    umma_commit(&S.empty[vs]);
+                    if (i + 1 == n) { umma_commit(&S.o_full[0]); umma_commit(&S.o_full[1]); }       // the groups share Q
+                }
+                __syncwarp();
+                advance(vs, vph);
+                if (i + 2 < n) scores(t);
             }
-            if (!ok) give_up();
-            if (issued) {
-                umma_commit(&S.mma_done);
-                mbar_wait_bounded(&S.mma_done, 0u);
-            }
+        }
+        if (!ok && lane == 0) give_up();
+        if (issued) {
+            if (elect_one()) umma_commit(&S.mma_done);
+            __syncwarp();
+            mbar_wait_bounded(&S.mma_done, 0u);
         }
         __syncwarp();
     } else if (warp < kSoftmaxWarps) {
         // ---------------- softmax ---------------------------------------------------------------------------
-        // A wait that runs out makes `ok` false in its warp; the threads of a group leave together, at the next vote.
+        // The group that has a unit's odd tiles brings the next unit's Q and has that one's even tiles, so that it begins with it
+        // while the other group writes the results.  A wait that runs out makes `ok` false in its warp; the threads of a group leave
+        // together, at the next vote.
         const int t = warp >> 2, pos = tid & 127;                           // group; position in a tile, later component
         const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t tS = tmem + lane_base + t * 64, tO = tmem + lane_base + kO;
+        const uint32_t tS = tmem + lane_base + t * 64, tO = tmem + lane_base + kO + t * 64, tOther = tmem + lane_base + kO + (t ^ 1) * 64;
         unsigned char* p_line = sP + t * kFewPBytes + pos * 128;
         uint32_t units = 0, items = 0, merges = 0, seq = 0;                 // seq: tiles of the ring used by earlier units
         bool ok = true, merged = false;
         auto wait = [&](uint64_t* bar, uint32_t ph) { ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, ph)); };
         auto arrive = [&](uint64_t* bar) { __syncwarp(); if (lane == 0) mbar_arrive(bar); };
-        // Q of a unit, by the second group: 128 / kN threads a row.  With an 8-bit cache as fp16, scaled by a power of two so that
-        // no value passes the range and what is lost is below 2^-37 of the row's largest.
-        auto load_q = [&](const AttnUnit& w) {
-            constexpr int kPer = 128 / kN, kMost = (kAttnMaxDim / 8 + kPer - 1) / kPer;
+        // Q of a unit: 128 / kN threads a row, asked for and later stored.
+        constexpr int kPer = 128 / kN, kMost = (kAttnMaxDim / 8 + kPer - 1) / kPer;
+        uint4 x[kMost];
+        auto fetch_q = [&](const AttnUnit& w) {
             const int row = pos / kPer, sub = pos % kPer, node = w.node0 + row / P.group, pieces = d / 8;
             const bool live = row < P.tile_nodes * P.group && node < w.n;
             const uint4* src = reinterpret_cast<const uint4*>(P.q + (long long)(w.row0 + node) * P.q_row +
                                                               (long long)(w.head * P.group + row % P.group) * P.q_head);
-            uint4 x[kMost];
 #pragma unroll
             for (int i = 0; i < kMost; ++i) {
                 x[i] = make_uint4(0, 0, 0, 0);
                 if (live && i * kPer + sub < pieces) x[i] = src[i * kPer + sub];
             }
+        };
+        // With an 8-bit cache as fp16, scaled by a power of two so that no value passes the range and what is lost is below 2^-37
+        // of the row's largest.
+        auto store_q = [&]() {
+            const int row = pos / kPer, sub = pos % kPer, pieces = d / 8;
             if constexpr (kNarrow) {
                 float top = 0.f;
 #pragma unroll
@@ -212,9 +224,8 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
 #pragma unroll
             for (int i = 0; i < kMost; ++i) {
                 const int c = i * kPer + sub;
-                if (c >= pieces) continue;
                 x[i].x ^= P.q_sign; x[i].y ^= P.q_sign; x[i].z ^= P.q_sign; x[i].w ^= P.q_sign;
-                *reinterpret_cast<uint4*>(sQ + (c >> 3) * (kN * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = x[i];
+                if (c < pieces) *reinterpret_cast<uint4*>(sQ + (c >> 3) * (kN * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = x[i];
             }
             fence_async_smem();
             arrive(&S.q_full);
@@ -243,8 +254,18 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
             return s;
         };
         bool have = it.next(P, u);
-        if (have && t == 1) load_q(u);
+        Ahead ahead = {-1, 0};
+        float2 scale_next = make_float2(0.f, 0.f);
+        auto first_scales = [&](int at) {
+            scale_next = scales_of(u, page_of(u, at));
+            ahead = page_of(u, at + 2);
+        };
+        if (have) {
+            if (t == 1) { fetch_q(u); store_q(); }
+            first_scales(t);
+        }
         while (have) {
+            const int turn = t ^ (int)(units & 1u);                         // 0: this group has the even tiles
             if (pos < kN) T.less[t][pos] = kFewUnset;
             if (tid == 0) S.bad_value[(units + kAttnUnitFlags / 2) % kAttnUnitFlags] = 0;
             if (group_any(t, !ok || *abort_flag)) { ok = false; break; }
@@ -253,10 +274,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
             for (int c = 0; c < kN / 2; ++c) sums[c] = pack2(0.f, 0.f);
             const int count = u.j1 - u.j0;
             bool any = false, left = false;
-            Ahead ahead = page_of(u, t);
-            float2 scale_next = scales_of(u, ahead);
-            ahead = page_of(u, t + 2);
-            for (int jj = t; jj < count; jj += 2) {
+            for (int jj = turn; jj < count; jj += 2) {
                 int start, len;
                 attn_tile_at(P, u.j0 + jj, start, len);
                 const int valid = min(len, u.length - start);               // positions of this tile that exist
@@ -288,7 +306,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                             }
                         }
                         group_sync(t);
-                        if (node >= 0) seen = T.seen[t][pos];
+                        if (node >= 0 && pos < valid) seen = T.seen[t][pos];
                     }
                 }
                 const float2 scale = scale_next;
@@ -302,44 +320,45 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                 ++items;
                 tc_fence_after();
                 const uint64_t k2 = pack2(k_scale, k_scale);
-                // score * factor - reference, of two rows
-                auto relative = [&](float a, float b, int c) {
-                    uint64_t k = k2;
-                    if constexpr (kNarrow) k = mul2(k, *reinterpret_cast<const uint64_t*>(&T.q[c]));
-                    return fma2(pack2(a, b), k, *reinterpret_cast<const uint64_t*>(&T.less[t][c]));
-                };
-                float top = -INFINITY;
-#pragma unroll
-                for (int c0 = 0; c0 < kN; c0 += kCols) {
-                    float s[kCols], tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                    tmem_read(tS + c0, s);
+                // y = score * factor - reference for the columns from c0 on, in place; -infinity where the position is not seen
+                auto relative = [&](float (&s)[kCols], int c0) {
 #pragma unroll
                     for (int c = 0; c < kCols; c += 2) {
-                        float y0, y1;
-                        unpack2(relative(s[c], s[c + 1], c0 + c), y0, y1);
+                        uint64_t k = k2;
+                        if constexpr (kNarrow) k = mul2(k, *reinterpret_cast<const uint64_t*>(&T.q[c0 + c]));
+                        unpack2(fma2(pack2(s[c], s[c + 1]), k, *reinterpret_cast<const uint64_t*>(&T.less[t][c0 + c])), s[c], s[c + 1]);
                         if (masked) {
-                            y0 = (seen >> (c0 + c) & 1) ? y0 : -INFINITY;
-                            y1 = (seen >> (c0 + c + 1) & 1) ? y1 : -INFINITY;
+                            s[c] = (seen >> (c0 + c) & 1) ? s[c] : -INFINITY;
+                            s[c + 1] = (seen >> (c0 + c + 1) & 1) ? s[c + 1] : -INFINITY;
                         }
-                        tops[c / 2 % 4] = fmaxf(tops[c / 2 % 4], fmaxf(y0, y1));
                     }
-                    top = fmaxf(top, fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
+                };
+                float y[kParts][kCols];
+                float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int h = 0; h < kN / kCols; ++h) {
+                    float (&s)[kCols] = y[kKeep ? h : 0];
+                    tmem_read(tS + h * kCols, s);
+                    relative(s, h * kCols);
+#pragma unroll
+                    for (int c = 0; c < kCols; c += 2) tops[c / 2 % 4] = fmaxf(tops[c / 2 % 4], fmaxf(s[c], s[c + 1]));
                 }
+                const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
                 if (group_any(t, !ok || top + above > kAttnLazy)) {
                     // references: the largest score of each row in this tile, where it is that much above
                     if (group_any(t, !ok)) { left = true; break; }
+#pragma unroll 1
+                    for (int c0 = 0; c0 < kN; c0 += 16) {
+                        float s[16], mine = -INFINITY;
+                        tmem_load16(tS + c0, s);
 #pragma unroll
-                    for (int c0 = 0; c0 < kN; c0 += kCols) {
-                        float s[kCols], mine = -INFINITY;
-                        tmem_read(tS + c0, s);
-#pragma unroll
-                        for (int c = 0; c < kCols; ++c) {
-                            float x = s[c] * (kNarrow ? k_scale * T.q[c0 + c] : k_scale) + above;
-                            if (masked) x = (seen >> (c0 + c) & 1) ? x : -INFINITY;
-                            x = warp_max_f32(x);
-                            if (lane == c) mine = x;
+                        for (int c = 0; c < 16; ++c) {
+                            float z = s[c] * (kNarrow ? k_scale * T.q[c0 + c] : k_scale) + above;
+                            if (masked) z = (seen >> (c0 + c) & 1) ? z : -INFINITY;
+                            z = warp_max_f32(z);
+                            if (lane == c) mine = z;
                         }
-                        if (lane < kCols) T.top[t][warp & 3][c0 + lane] = mine;
+                        if (lane < 16) T.top[t][warp & 3][c0 + lane] = mine;
                     }
                     group_sync(t);
                     if (pos < kN) {
@@ -352,48 +371,52 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                     group_sync(t);
 #pragma unroll
                     for (int c = 0; c < kN / 2; ++c) sums[c] = mul2(sums[c], *reinterpret_cast<const uint64_t*>(&T.scale[t][2 * c]));
-                    if (any)
-#pragma unroll
+                    if (any) {
+#pragma unroll 1
                         for (int c0 = 0; c0 < kN; c0 += 16) {
                             float o[16];
                             uint32_t w[16];
-                            tmem_load16(tO + t * 64 + c0, o);
+                            tmem_load16(tO + c0, o);
 #pragma unroll
                             for (int c = 0; c < 16; ++c) w[c] = __float_as_uint(o[c] * T.scale[t][c0 + c]);
-                            tmem_store16(tO + t * 64 + c0, w);
+                            tmem_store16(tO + c0, w);
                         }
-                    tmem_store_wait();
+                        tmem_store_wait();
+                    }
+                    if (kKeep)
+#pragma unroll
+                        for (int h = 0; h < kN / kCols; ++h) {
+                            tmem_read(tS + h * kCols, y[kKeep ? h : 0]);
+                            relative(y[kKeep ? h : 0], h * kCols);
+                        }
                 }
                 any = true;
 #pragma unroll
-                for (int c0 = 0; c0 < kN; c0 += kCols) {
-                    float s[kCols];
-                    tmem_read(tS + c0, s);
+                for (int h = 0; h < kN / kCols; ++h) {
+                    float (&s)[kCols] = y[kKeep ? h : 0];
+                    if (!kKeep) {
+                        tmem_read(tS + h * kCols, s);
+                        relative(s, h * kCols);
+                    }
                     uint32_t w[kCols / 2];
 #pragma unroll
                     for (int c = 0; c < kCols; c += 2) {
-                        float e0, e1;
-                        unpack2(relative(s[c], s[c + 1], c0 + c), e0, e1);
-                        if (masked) {
-                            e0 = (seen >> (c0 + c) & 1) ? e0 : -INFINITY;
-                            e1 = (seen >> (c0 + c + 1) & 1) ? e1 : -INFINITY;
-                        }
-                        e0 = ex2_approx(e0);
-                        e1 = ex2_approx(e1);
+                        float e0 = ex2_approx(s[c]), e1 = ex2_approx(s[c + 1]);
                         const uint64_t e = pack2(e0, e1);
-                        sums[(c0 + c) / 2] = add2(sums[(c0 + c) / 2], e);
+                        sums[(h * kCols + c) / 2] = add2(sums[(h * kCols + c) / 2], e);
                         if constexpr (kNarrow) {
                             unpack2(mul2(e, pack2(scale.y, scale.y)), e0, e1);
                             if (masked) {
-                                e0 = (seen >> (c0 + c) & 1) ? e0 : 0.f;
-                                e1 = (seen >> (c0 + c + 1) & 1) ? e1 : 0.f;
+                                e0 = (seen >> (h * kCols + c) & 1) ? e0 : 0.f;
+                                e1 = (seen >> (h * kCols + c + 1) & 1) ? e1 : 0.f;
                             }
                         }
                         w[c / 2] = pack16<kNarrow>(e0, e1);
                     }
 #pragma unroll
                     for (int c = 0; c < kCols / 8; ++c)
-                        *reinterpret_cast<uint4*>(p_line + (((c0 / 8 + c) ^ (pos & 7)) << 4)) = make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+                        *reinterpret_cast<uint4*>(p_line + (((h * kCols / 8 + c) ^ (pos & 7)) << 4)) =
+                            make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
                 }
                 if (!kNarrow && masked) {
                     // V of positions that no row sees, or that hold NaN or infinities that only some see, must not meet a
@@ -405,7 +428,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                             S.bad_value[units % kAttnUnitFlags] = 1;
                 }
                 fence_async_smem();
-                if (merged) {                    // the second group's O^T of the unit before has been read
+                if (merged) {                    // this group's O^T of the unit before has been read
                     wait(&S.merge_done, (merges - 1) & 1u);
                     merged = false;
                 }
@@ -413,15 +436,15 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                 arrive(&S.p_full[t]);
             }
             if (left) { ok = false; break; }                                // all of the group
-            wait(&S.o_full[t], units & 1u);
-            tc_fence_after();
-            // Everything of this unit has been multiplied: Q of the next one takes the place of this one's.
+            // The next unit's Q and scales, asked for while the products of this one are finished.
             const AttnUnit done = u;
             have = it.next(P, u);
-            if (have && t == 1) load_q(u);
+            if (have) {
+                if (turn == 1) fetch_q(u);
+                first_scales(turn ^ 1);
+            }
             const bool join = count > 1;
-            if (t == 1 && merged) { wait(&S.merge_done, (merges - 1) & 1u); merged = false; }
-            if (t == 0 || join) {
+            if (turn == 0 || join) {
                 // sums over the positions of this warp: half of the rows pass to the other half of the lanes, five times
                 float v[kN];
 #pragma unroll
@@ -447,22 +470,28 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                 for (int i = 0; i < kSteps; ++i) row += (lane >> (4 - i) & 1) * (kN >> (i + 1));
                 if (kN >= 32 || (lane & 1) == 0)
 #pragma unroll
-                    for (int c = 0; c < kLeft; ++c) T.sum[t][warp & 3][row + c] = v[c];
+                    for (int c = 0; c < kLeft; ++c) T.sum[turn][warp & 3][row + c] = v[c];
             }
-            if (t == 1 && join) {
-                if (pos < kN) T.last[pos] = -T.less[1][pos];
-                tc_fence_before();
-                arrive(&S.merge_ready);
-                ++merges;
-                merged = true;
-            } else if (t == 0) {
+            wait(&S.o_full[t], units & 1u);
+            tc_fence_after();
+            // Everything of this unit has been multiplied: Q of the next one takes the place of this one's.
+            if (turn == 1) {
+                if (have) store_q();
+                if (join) {
+                    if (pos < kN) T.last[pos] = -T.less[t][pos];
+                    tc_fence_before();
+                    arrive(&S.merge_ready);
+                    ++merges;
+                    merged = true;
+                }
+            } else {
                 if (join) { wait(&S.merge_ready, merges & 1u); ++merges; tc_fence_after(); }
-                if (group_any(0, !ok)) { ok = false; break; }
+                if (group_any(t, !ok)) { ok = false; break; }
                 const bool whole = done.j0 == 0 && done.j1 == done.tiles;
                 const long long part = (long long)(2 * blockIdx.x + (done.j0 > 0 ? 0 : 1)) * P.part_rows;
                 const int rows = min(P.tile_nodes, done.n - done.node0) * P.group;
                 if (pos < rows) {
-                    float base = -T.less[0][pos], f0 = 1.f, f1 = 0.f;
+                    float base = -T.less[t][pos], f0 = 1.f, f1 = 0.f;
                     float sum = (T.sum[0][0][pos] + T.sum[0][1][pos]) + (T.sum[0][2][pos] + T.sum[0][3][pos]);
                     if (join) {
                         const float base1 = T.last[pos], both = fmaxf(base, base1);
@@ -480,40 +509,53 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                                 (base + log2f(sum)) * 0.6931471805599453f;
                     } else
                         P.part_stats[part + pos] = make_float2(base, sum);
-                    T.scale[0][pos] = f0;
-                    T.top[0][0][pos] = f1;
+                    T.scale[t][pos] = f0;
+                    T.top[t][0][pos] = f1;
                 }
-                group_sync(0);
-                const bool bad_value = kKind != kAttnI8 && *(volatile int*)&S.bad_value[units % kAttnUnitFlags] != 0;
-                int node = done.node0, in_group = 0;                        // of the row
-                for (int c0 = 0; c0 < rows; c0 += 16) {
-                    float o[16];
-                    __syncwarp();
-                    tmem_load16(tO + c0, o);
+                group_sync(t);
+                float o[kN];
+#pragma unroll
+                for (int h = 0; h < kN; h += 16) {
+                    float a[16];
+                    tmem_load16(tO + h, a);
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) o[h + c] = a[c] * T.scale[t][h + c];
                     if (join) {
-                        float o1[16];
-                        tmem_load16(tO + 64 + c0, o1);
+                        tmem_load16(tOther + h, a);
 #pragma unroll
-                        for (int c = 0; c < 16; ++c) o[c] = o[c] * T.scale[0][c0 + c] + o1[c] * T.top[0][0][c0 + c];
-                    } else
-#pragma unroll
-                        for (int c = 0; c < 16; ++c) o[c] *= T.scale[0][c0 + c];
-#pragma unroll
-                    for (int c = 0; c < 16; ++c) {
-                        if (c0 + c < rows && pos < d) {
-                            float x = o[c];
-                            if (bad_value) x += attn_bad_values<kNarrow>(P, done, node, pos);
-                            if (whole)
-                                *reinterpret_cast<uint16_t*>(P.out + (long long)(done.row0 + node) * P.out_row +
-                                                             (long long)(done.head * P.group + in_group) * P.out_head + pos * 2) = (uint16_t)pack16<false>(x, 0.f);
-                            else
-                                P.parts[(part + c0 + c) * d + pos] = x;
-                        }
-                        if (++in_group == P.group) { in_group = 0; ++node; }
+                        for (int c = 0; c < 16; ++c) o[h + c] = fmaf(a[c], T.top[t][0][h + c], o[h + c]);
                     }
                 }
-                __syncwarp();
                 if (join) { tc_fence_before(); arrive(&S.merge_done); }
+                if (pos < d) {
+                    if (whole) {
+                        unsigned char* to = P.out + (long long)(done.row0 + done.node0) * P.out_row + (long long)(done.head * P.group) * P.out_head + pos * 2;
+                        const long long next_node = P.out_row - (P.group - 1) * P.out_head;
+                        int in_group = 0;
+#pragma unroll
+                        for (int c = 0; c < kN; ++c) {
+                            if (c < rows) *reinterpret_cast<uint16_t*>(to) = (uint16_t)pack16<false>(o[c], 0.f);
+                            if (++in_group == P.group) { in_group = 0; to += next_node; } else to += P.out_head;
+                        }
+                    } else {
+                        float* to = P.parts + part * d + pos;
+#pragma unroll
+                        for (int c = 0; c < kN; ++c)
+                            if (c < rows) to[c * d] = o[c];
+                    }
+                    if (kKind != kAttnI8 && *(volatile int*)&S.bad_value[units % kAttnUnitFlags] != 0)
+                        for (int c = 0; c < rows; ++c) {                    // values that were left out, where the row sees them
+                            const int node = done.node0 + c / P.group;
+                            const float bad = attn_bad_values<kNarrow>(P, done, node, pos);
+                            unsigned char* to = P.out + (long long)(done.row0 + node) * P.out_row + (long long)(done.head * P.group + c % P.group) * P.out_head + pos * 2;
+                            if (bad == 0.f) continue;
+                            if (!whole) P.parts[(part + c) * d + pos] += bad;
+                            else {
+                                const float now = __uint_as_float((uint32_t)*reinterpret_cast<uint16_t*>(to) << 16) + bad;
+                                *reinterpret_cast<uint16_t*>(to) = (uint16_t)pack16<false>(now, 0.f);
+                            }
+                        }
+                }
             }
             seq += 2 * count;
             ++units;
@@ -554,7 +596,7 @@ static int few_launch(AttnParams& P, const CUtensorMap& k, const CUtensorMap& v,
         P.raw_slots = 0;
     }
     KernelTimerScope timer(DSPARK_K_TREE_ATTENTION, s);
-    launch_pdl(attn_few_kernel<kKind, kN>, dim3((unsigned)sms), dim3(kFewThreads<kKind, kN>), kSmem, s, P, k, v);
+    launch_pdl(attn_few_kernel<kKind, kN>, dim3((unsigned)sms), dim3(kFewThreads<kKind>), kSmem, s, P, k, v);
     return launch_status();
 }
 template <int kKind>
