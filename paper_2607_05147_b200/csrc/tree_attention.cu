@@ -183,8 +183,8 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
 #pragma unroll
                         for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(bf16lo(w4[i])), fabsf(bf16hi(w4[i]))));
                     }
-                    // 2^e with the largest value below 2^14: exponent field of top to that of 2^13, within the powers of fp32
-                    const int e = min(253, max(1, 254 + 13 - (int)(__float_as_uint(top) >> 23)));
+                    // 2^e with the largest value below 2^14: exponent field of top to that of 2^13; at most 2^60
+                    const int e = min(127 + 60, max(1, 254 + 13 - (int)(__float_as_uint(top) >> 23)));
                     up = __uint_as_float((uint32_t)e << 23);
                     scales.q[tile][row] = __uint_as_float((uint32_t)(254 - e) << 23);   // the inverse power
                 }
@@ -674,7 +674,7 @@ int dspark_tree_attention(const dspark_kv_cache_t* cache, int layer, const void*
     P.out_lse = out_lse;
     P.first = first; P.row_offsets = row_offsets; P.parents = parents;
     P.R = R; P.n_rows = n_rows; P.q_heads = q_heads;
-    P.score_factor = fabsf(scale) * kAttnLog2e;
+    P.score_factor = fmaxf(fabsf(scale) * kAttnLog2e, kAttnLeastFactor);
     P.q_sign = scale < 0.f ? 0x80008000u : 0u;
     P.dev_status = dev_status;
     // rows of a request with one K/V head on average

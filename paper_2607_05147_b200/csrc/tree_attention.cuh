@@ -18,6 +18,7 @@ constexpr int kAttnNarrowBytes = 208 * 1024;                  // with 8-bit cach
 constexpr float kAttnLog2e = 1.4426950408889634f;
 constexpr float kAttnLazy = 8.f;                 // O is scaled when the maximum rises by more than 2^8
 constexpr float kAttnNarrowOffset = 7.f;         // fp16 weights: up to 2^(7 + 8) of 65 504, down to 2^-31 of the largest
+constexpr float kAttnLeastFactor = 1e-20f;       // of a score: -infinity times it is -infinity, a score times it next to nothing
 constexpr int kSoftmaxWarps = 8;
 constexpr int kAttnUnitFlags = 8;               // units of one CTA that are under way at a time: at most four
 

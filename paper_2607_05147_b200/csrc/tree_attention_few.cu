@@ -28,7 +28,7 @@ constexpr float kFewUnset = 1e38f;               // less a reference that every 
 
 struct FewShared {
     uint64_t full[kAttnMaxSlots], empty[kAttnMaxSlots], raw_full[kAttnMaxRaw], raw_empty[kAttnMaxRaw];
-    uint64_t q_full, s_full[2], p_full[2], o_full[2], merge_ready, merge_done, mma_done;
+    uint64_t q_full, q_empty, s_full[2], p_full[2], o_done[2], merge_ready, merge_done, mma_done[2];
     uint32_t tmem_base;
     int abort, bad_value[kAttnUnitFlags];
     AttnList list;
@@ -38,7 +38,7 @@ struct FewTables {
     float less[2][kN];                           // less the references, in units of log2, of each group
     float last[kN];                              // those of the second group at the end of a unit
     float scale[2][kN];                          // what O^T and the sums are multiplied by when they change; joining: weights
-    float q[kN];                                 // 8-bit caches: what a row of Q was divided by
+    float q[2][kN];                              // 8-bit caches: what a row of Q was divided by, of this unit and the next
     float top[2][4][kN], sum[2][4][kN];          // a warp's maxima; its sums at the end
     unsigned long long seen[2][kAttnTile];       // rows that see a position (tiles with nodes)
 };
@@ -58,14 +58,14 @@ template <int kCols> __device__ __forceinline__ void tmem_read(uint32_t addr, fl
 }
 
 template <int kKind> constexpr int kFewConverters = kKind == kAttnWide ? 0 : 4;
-template <int kKind> constexpr int kFewThreads = (kSoftmaxWarps + 2 + kFewConverters<kKind>) * 32;
+template <int kKind> constexpr int kFewThreads = (kSoftmaxWarps + 3 + kFewConverters<kKind>) * 32;
 
 template <int kKind, int kN>
 __global__ void __launch_bounds__(kFewThreads<kKind>, 1)
 attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v)
 {
     constexpr bool kNarrow = kKind != kAttnWide;
-    constexpr int kThreads = kFewThreads<kKind>, kProducer = kSoftmaxWarps, kIssuer = kSoftmaxWarps + 1;
+    constexpr int kThreads = kFewThreads<kKind>, kProducer = kSoftmaxWarps, kIssuer = kSoftmaxWarps + 1, kIssuerO = kSoftmaxWarps + 2;
     constexpr int kWarps = kFewConverters<kKind>, kCols = kN < 32 || (kNarrow && kN == 64) ? 16 : 32;
     constexpr bool kKeep = kN <= 32; // a tile's scores stay in registers between the vote and the exponentials
     constexpr int kParts = kKeep ? kN / kCols : 1;
@@ -84,10 +84,10 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
     if (tid == 0) {
         for (int s = 0; s < P.slots; ++s) { mbar_init(&S.full[s], kNarrow ? kWarps : 1); mbar_init(&S.empty[s], 1); }
         for (int s = 0; s < P.raw_slots; ++s) { mbar_init(&S.raw_full[s], 1); mbar_init(&S.raw_empty[s], kNarrow ? kWarps : 1); }
-        mbar_init(&S.q_full, 4);
-        for (int t = 0; t < 2; ++t) { mbar_init(&S.s_full[t], 1); mbar_init(&S.p_full[t], 4); mbar_init(&S.o_full[t], 1); }
+        mbar_init(&S.q_full, 4); mbar_init(&S.q_empty, 1);
+        for (int t = 0; t < 2; ++t) { mbar_init(&S.s_full[t], 1); mbar_init(&S.p_full[t], 4); mbar_init(&S.o_done[t], 1); mbar_init(&S.mma_done[t], 1); }
         for (int i = 0; i < kAttnUnitFlags; ++i) S.bad_value[i] = 0;
-        mbar_init(&S.merge_ready, 4); mbar_init(&S.merge_done, 4); mbar_init(&S.mma_done, 1);
+        mbar_init(&S.merge_ready, 4); mbar_init(&S.merge_done, 4);
         S.abort = 0;
         mbar_fence_init();
     }
@@ -106,66 +106,60 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
     if (warp == kProducer) {
         attn_produce<kNarrow>(P, it, map_k, map_v, kNarrow ? raw : ring, kNarrow ? S.raw_full : S.full, kNarrow ? S.raw_empty : S.empty,
                               kNarrow ? P.raw_slots : P.slots, abort_flag);
-    } else if (warp == kIssuer) {
+    } else if (warp == kIssuer || warp == kIssuerO) {
         // ---------------- products --------------------------------------------------------------------------
+        // One warp issues S^T = K Q^T, another O^T += V^T P^T: what a single one has to wait for and to issue for a tile takes it
+        // longer than the tile's bytes take to arrive.  K and V tiles alternate in the ring.
+        const bool second = warp == kIssuerO;
         const uint32_t type = kNarrow ? 0u : 1u;                            // fp16 or bf16 operands, fp32 sums
         const uint32_t idesc_s = (1u << 4) | (type << 7) | (type << 10) | ((uint32_t)(kN >> 3) << 17) | ((uint32_t)(kAttnTile >> 4) << 24);
         const uint32_t idesc_o = idesc_s | (1u << 15) | (1u << 16);
-        const uint32_t q0 = desc_k_major(smem_u32(sQ)), p0 = desc_mn_major(smem_u32(sP));
-        const uint32_t k0 = desc_k_major(smem_u32(ring)), v0 = desc_mn_major(smem_u32(ring)), tile_step = (uint32_t)tile_bytes >> 4;
-        const int steps = d / 16;
-        uint32_t units = 0, items[2] = {0, 0};
-        bool ok = true, issued = false;
-        // K and V tiles alternate in the ring; the places of the next of each
-        uint32_t ks = 0, vs = 1, kph = 0, vph = 0;
-        auto advance = [&](uint32_t& s, uint32_t& ph) { s += 2; if (s >= (uint32_t)P.slots) { s -= P.slots; ph ^= 1u; } };
-        auto wait = [&](uint64_t* bar, uint32_t ph) { ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, ph)); return ok; };
+        const uint32_t tile_step = (uint32_t)tile_bytes >> 4;
+        uint32_t units = 0, items[2] = {0, 0}, s = second ? 1 : 0, ph = 0;
+        bool ok = true;
+        auto wait = [&](uint64_t* bar, uint32_t p) { ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, p)); return ok; };
         while (ok && !__any_sync(0xffffffffu, *abort_flag) && it.next(P, u)) {
             const int n = u.j1 - u.j0;
             const uint32_t turn = units & 1u;                               // the group that has the even tiles
-            auto scores = [&](uint32_t t) {
-                if (!wait(&S.full[ks], kph)) return;
-                tc_fence_after();
-                const uint32_t a = k0 + ks * tile_step;
-                if (elect_one()) {
-#pragma unroll
-                    for (int k = 0; k < kAttnMaxDim / 16; ++k)
-                        if (k < steps)
-                            mma_ss(tmem + t * 64, a + (k >> 2) * (kChunkBytes >> 4) + (k & 3) * 2, q0 + (k >> 2) * (kN * 8) + (k & 3) * 2, idesc_s, k > 0);
-                    umma_commit(&S.s_full[t]);
-                    umma_commit(&S.empty[ks]);
-                }
-                __syncwarp();
-                advance(ks, kph);
-                issued = true;
-            };
-            if (!wait(&S.q_full, units & 1u)) break;
+            if (!second && !wait(&S.q_full, units & 1u)) break;
             ++units;
-            tc_fence_after();
-            scores(turn);
-            if (n > 1) scores(turn ^ 1u);
-            for (int i = 0; ok && i < n; ++i) {
-                const uint32_t t = turn ^ (uint32_t)(i & 1);
-                if (!wait(&S.p_full[t], (t ? items[1] : items[0]) & 1u) || !wait(&S.full[vs], vph)) break;
-                if (t) ++items[1]; else ++items[0];
-                tc_fence_after();
-                const uint32_t a = v0 + vs * tile_step, b = p0 + t * (kFewPBytes >> 4);
-                if (elect_one()) {
+            for (int i = 0; i < n; ++i) {
+                const uint32_t t = turn ^ (uint32_t)(i & 1), item = t ? items[1]++ : items[0]++;
+                if (second) {
+                    if (!wait(&S.full[s], ph) || !wait(&S.p_full[t], item & 1u)) break;
+                    tc_fence_after();
+                    const uint32_t a = desc_mn_major(smem_u32(ring)) + s * tile_step, b = desc_mn_major(smem_u32(sP)) + t * (kFewPBytes >> 4);
+                    if (elect_one()) {
 #pragma unroll
-                    for (int k = 0; k < kAttnTile / 16; ++k) mma_ss(tmem + kO + t * 64, a + k * 128, b + k * 128, idesc_o, i > 1 || k > 0);
-                    umma_commit(&S.empty[vs]);
-                    if (i + 1 == n) { umma_commit(&S.o_full[0]); umma_commit(&S.o_full[1]); }       // the groups share Q
+                        for (int k = 0; k < kAttnTile / 16; ++k) mma_ss(tmem + kO + t * 64, a + k * 128, b + k * 128, idesc_o, i > 1 || k > 0);
+                        umma_commit(&S.empty[s]);
+                        umma_commit(&S.o_done[t]);
+                    }
+                } else {
+                    // the scores that were here before have been read
+                    if ((item && !wait(&S.p_full[t], (item - 1) & 1u)) || !wait(&S.full[s], ph)) break;
+                    tc_fence_after();
+                    const uint32_t a = desc_k_major(smem_u32(ring)) + s * tile_step, b = desc_k_major(smem_u32(sQ));
+                    if (elect_one()) {
+#pragma unroll
+                        for (int k = 0; k < kAttnMaxDim / 16; ++k)
+                            if (k < d / 16)
+                                mma_ss(tmem + t * 64, a + (k >> 2) * (kChunkBytes >> 4) + (k & 3) * 2, b + (k >> 2) * (kN * 8) + (k & 3) * 2, idesc_s, k > 0);
+                        umma_commit(&S.s_full[t]);
+                        umma_commit(&S.empty[s]);
+                        if (i + 1 == n) umma_commit(&S.q_empty);
+                    }
                 }
                 __syncwarp();
-                advance(vs, vph);
-                if (i + 2 < n) scores(t);
+                s += 2;
+                if (s >= (uint32_t)P.slots) { s -= P.slots; ph ^= 1u; }
             }
         }
         if (!ok && lane == 0) give_up();
-        if (issued) {
-            if (elect_one()) umma_commit(&S.mma_done);
+        if (units) {                             // tensor memory is returned only after the last product
+            if (elect_one()) umma_commit(&S.mma_done[second]);
             __syncwarp();
-            mbar_wait_bounded(&S.mma_done, 0u);
+            mbar_wait_bounded(&S.mma_done[second], 0u);
         }
         __syncwarp();
     } else if (warp < kSoftmaxWarps) {
@@ -197,7 +191,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
         };
         // With an 8-bit cache as fp16, scaled by a power of two so that no value passes the range and what is lost is below 2^-37
         // of the row's largest.
-        auto store_q = [&]() {
+        auto store_q = [&](uint32_t unit) {
             const int row = pos / kPer, sub = pos % kPer, pieces = d / 8;
             if constexpr (kNarrow) {
                 float top = 0.f;
@@ -209,10 +203,10 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                 }
 #pragma unroll
                 for (int o = kPer / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                // 2^e with the largest value below 2^14: exponent field of top to that of 2^13, within the powers of fp32
-                const int e = min(253, max(1, 254 + 13 - (int)(__float_as_uint(top) >> 23)));
+                // 2^e with the largest value below 2^14: exponent field of top to that of 2^13; at most 2^60
+                const int e = min(127 + 60, max(1, 254 + 13 - (int)(__float_as_uint(top) >> 23)));
                 const float up = __uint_as_float((uint32_t)e << 23);
-                if (sub == 0) T.q[row] = __uint_as_float((uint32_t)(254 - e) << 23);
+                if (sub == 0) T.q[unit & 1u][row] = __uint_as_float((uint32_t)(254 - e) << 23);
 #pragma unroll
                 for (int i = 0; i < kMost; ++i) {
                     x[i].x = pack16<true>(bf16lo(x[i].x) * up, bf16hi(x[i].x) * up);
@@ -261,7 +255,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
             ahead = page_of(u, at + 2);
         };
         if (have) {
-            if (t == 1) { fetch_q(u); store_q(); }
+            if (t == 1) { fetch_q(u); store_q(0); }
             first_scales(t);
         }
         while (have) {
@@ -312,25 +306,42 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                 const float2 scale = scale_next;
                 scale_next = scales_of(u, ahead);
                 ahead = page_of(u, jj + 4);
-                const float k_scale = kNarrow ? scale.x * P.score_factor : P.score_factor;
+                float k_scale = P.score_factor, v_scale = scale.y;
                 // an 8-bit V: 2^exponent > its scale; what a weight may be above its reference depends on it
                 float above = 0.f;
-                if constexpr (kNarrow) above = attn_exponent(scale.y < INFINITY ? fmaxf(scale.y, 0.f) : 0.f) - kAttnNarrowOffset;
+                if constexpr (kNarrow) {
+                    k_scale *= scale.x;
+                    if (k_scale < kAttnLeastFactor) k_scale = kAttnLeastFactor;
+                    above = attn_exponent(scale.y < INFINITY ? fmaxf(scale.y, 0.f) : 0.f) - kAttnNarrowOffset;
+                }
+                if (items) wait(&S.o_done[t], (items - 1) & 1u);            // P and O^T of the tile before
                 wait(&S.s_full[t], items & 1u);
                 ++items;
                 tc_fence_after();
+                if (masked) {
+                    // scores of rows that do not see the position: -infinity, in place.  Where a scale is no number the position
+                    // is NaN for the rows that see it, and the scales are not used.
+                    const bool bad = kNarrow && !(fabsf(scale.x) < INFINITY && fabsf(scale.y) < INFINITY);
+#pragma unroll 1
+                    for (int c0 = 0; c0 < kN; c0 += 16) {
+                        float s[16];
+                        uint32_t w[16];
+                        tmem_load16(tS + c0, s);
+#pragma unroll
+                        for (int c = 0; c < 16; ++c) w[c] = __float_as_uint(!(seen >> (c0 + c) & 1) ? -INFINITY : bad ? NAN : s[c]);
+                        tmem_store16(tS + c0, w);
+                    }
+                    tmem_store_wait();
+                    if (bad) { k_scale = 1.f; v_scale = 0.f; above = -kAttnNarrowOffset; }
+                }
                 const uint64_t k2 = pack2(k_scale, k_scale);
-                // y = score * factor - reference for the columns from c0 on, in place; -infinity where the position is not seen
+                // y = score * factor - reference for the columns from c0 on, in place
                 auto relative = [&](float (&s)[kCols], int c0) {
 #pragma unroll
                     for (int c = 0; c < kCols; c += 2) {
                         uint64_t k = k2;
-                        if constexpr (kNarrow) k = mul2(k, *reinterpret_cast<const uint64_t*>(&T.q[c0 + c]));
+                        if constexpr (kNarrow) k = mul2(k, *reinterpret_cast<const uint64_t*>(&T.q[units & 1u][c0 + c]));
                         unpack2(fma2(pack2(s[c], s[c + 1]), k, *reinterpret_cast<const uint64_t*>(&T.less[t][c0 + c])), s[c], s[c + 1]);
-                        if (masked) {
-                            s[c] = (seen >> (c0 + c) & 1) ? s[c] : -INFINITY;
-                            s[c + 1] = (seen >> (c0 + c + 1) & 1) ? s[c + 1] : -INFINITY;
-                        }
                     }
                 };
                 float y[kParts][kCols];
@@ -353,8 +364,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                         tmem_load16(tS + c0, s);
 #pragma unroll
                         for (int c = 0; c < 16; ++c) {
-                            float z = s[c] * (kNarrow ? k_scale * T.q[c0 + c] : k_scale) + above;
-                            if (masked) z = (seen >> (c0 + c) & 1) ? z : -INFINITY;
+                            float z = s[c] * (kNarrow ? k_scale * T.q[units & 1u][c0 + c] : k_scale) + above;
                             z = warp_max_f32(z);
                             if (lane == c) mine = z;
                         }
@@ -405,11 +415,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                         const uint64_t e = pack2(e0, e1);
                         sums[(h * kCols + c) / 2] = add2(sums[(h * kCols + c) / 2], e);
                         if constexpr (kNarrow) {
-                            unpack2(mul2(e, pack2(scale.y, scale.y)), e0, e1);
-                            if (masked) {
-                                e0 = (seen >> (h * kCols + c) & 1) ? e0 : 0.f;
-                                e1 = (seen >> (h * kCols + c + 1) & 1) ? e1 : 0.f;
-                            }
+                            unpack2(mul2(e, pack2(v_scale, v_scale)), e0, e1);
                         }
                         w[c / 2] = pack16<kNarrow>(e0, e1);
                     }
@@ -470,13 +476,15 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                 for (int i = 0; i < kSteps; ++i) row += (lane >> (4 - i) & 1) * (kN >> (i + 1));
                 if (kN >= 32 || (lane & 1) == 0)
 #pragma unroll
-                    for (int c = 0; c < kLeft; ++c) T.sum[turn][warp & 3][row + c] = v[c];
+                    for (int c = 0; c < kLeft; ++c) T.sum[t][warp & 3][row + c] = v[c];
             }
-            wait(&S.o_full[t], units & 1u);
+            if (turn == 0 || join) wait(&S.o_done[t], (items - 1) & 1u);
             tc_fence_after();
-            // Everything of this unit has been multiplied: Q of the next one takes the place of this one's.
             if (turn == 1) {
-                if (have) store_q();
+                if (have) {                      // Q takes the place of this unit's, which has been multiplied
+                    wait(&S.q_empty, units & 1u);
+                    store_q(units + 1);
+                }
                 if (join) {
                     if (pos < kN) T.last[pos] = -T.less[t][pos];
                     tc_fence_before();
@@ -492,12 +500,13 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                 const int rows = min(P.tile_nodes, done.n - done.node0) * P.group;
                 if (pos < rows) {
                     float base = -T.less[t][pos], f0 = 1.f, f1 = 0.f;
-                    float sum = (T.sum[0][0][pos] + T.sum[0][1][pos]) + (T.sum[0][2][pos] + T.sum[0][3][pos]);
+                    float sum = (T.sum[t][0][pos] + T.sum[t][1][pos]) + (T.sum[t][2][pos] + T.sum[t][3][pos]);
                     if (join) {
                         const float base1 = T.last[pos], both = fmaxf(base, base1);
                         f0 = ex2_approx(base - both);
                         f1 = ex2_approx(base1 - both);
-                        sum = sum * f0 + ((T.sum[1][0][pos] + T.sum[1][1][pos]) + (T.sum[1][2][pos] + T.sum[1][3][pos])) * f1;
+                        const float (&other)[4][kN] = T.sum[t ^ 1];
+                        sum = sum * f0 + ((other[0][pos] + other[1][pos]) + (other[2][pos] + other[3][pos])) * f1;
                         base = both;
                     }
                     if (whole) {
@@ -513,49 +522,46 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                     T.top[t][0][pos] = f1;
                 }
                 group_sync(t);
-                float o[kN];
+                unsigned char* to = P.out + (long long)(done.row0 + done.node0) * P.out_row + (long long)(done.head * P.group) * P.out_head + pos * 2;
+                const long long next_node = P.out_row - (P.group - 1) * P.out_head;
+                float* to_part = P.parts + part * d + pos;
+                int in_group = 0;
+#pragma unroll 1
+                for (int h = 0; h < rows; h += 16) {
+                    float o[16];
+                    tmem_load16(tO + h, o);
 #pragma unroll
-                for (int h = 0; h < kN; h += 16) {
-                    float a[16];
-                    tmem_load16(tO + h, a);
-#pragma unroll
-                    for (int c = 0; c < 16; ++c) o[h + c] = a[c] * T.scale[t][h + c];
+                    for (int c = 0; c < 16; ++c) o[c] *= T.scale[t][h + c];
                     if (join) {
+                        float a[16];
                         tmem_load16(tOther + h, a);
 #pragma unroll
-                        for (int c = 0; c < 16; ++c) o[h + c] = fmaf(a[c], T.top[t][0][h + c], o[h + c]);
+                        for (int c = 0; c < 16; ++c) o[c] = fmaf(a[c], T.top[t][0][h + c], o[c]);
                     }
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) {
+                        if (h + c < rows && pos < d) {
+                            if (whole) *reinterpret_cast<uint16_t*>(to) = (uint16_t)pack16<false>(o[c], 0.f);
+                            else to_part[(h + c) * d] = o[c];
+                        }
+                        to += P.out_head;
+                        if (++in_group == P.group) { in_group = 0; to += next_node - P.out_head; }
+                    }
+                    __syncwarp();
                 }
                 if (join) { tc_fence_before(); arrive(&S.merge_done); }
-                if (pos < d) {
-                    if (whole) {
-                        unsigned char* to = P.out + (long long)(done.row0 + done.node0) * P.out_row + (long long)(done.head * P.group) * P.out_head + pos * 2;
-                        const long long next_node = P.out_row - (P.group - 1) * P.out_head;
-                        int in_group = 0;
-#pragma unroll
-                        for (int c = 0; c < kN; ++c) {
-                            if (c < rows) *reinterpret_cast<uint16_t*>(to) = (uint16_t)pack16<false>(o[c], 0.f);
-                            if (++in_group == P.group) { in_group = 0; to += next_node; } else to += P.out_head;
+                if (kKind != kAttnI8 && pos < d && *(volatile int*)&S.bad_value[units % kAttnUnitFlags] != 0)
+                    for (int c = 0; c < rows; ++c) {     // values that were left out, where the row sees them
+                        const int node = done.node0 + c / P.group;
+                        const float bad = attn_bad_values<kNarrow>(P, done, node, pos);
+                        if (bad == 0.f) continue;
+                        if (!whole) P.parts[(part + c) * d + pos] += bad;
+                        else {
+                            uint16_t* at = reinterpret_cast<uint16_t*>(P.out + (long long)(done.row0 + node) * P.out_row +
+                                                                       (long long)(done.head * P.group + c % P.group) * P.out_head) + pos;
+                            *at = (uint16_t)pack16<false>(__uint_as_float((uint32_t)*at << 16) + bad, 0.f);
                         }
-                    } else {
-                        float* to = P.parts + part * d + pos;
-#pragma unroll
-                        for (int c = 0; c < kN; ++c)
-                            if (c < rows) to[c * d] = o[c];
                     }
-                    if (kKind != kAttnI8 && *(volatile int*)&S.bad_value[units % kAttnUnitFlags] != 0)
-                        for (int c = 0; c < rows; ++c) {                    // values that were left out, where the row sees them
-                            const int node = done.node0 + c / P.group;
-                            const float bad = attn_bad_values<kNarrow>(P, done, node, pos);
-                            unsigned char* to = P.out + (long long)(done.row0 + node) * P.out_row + (long long)(done.head * P.group + c % P.group) * P.out_head + pos * 2;
-                            if (bad == 0.f) continue;
-                            if (!whole) P.parts[(part + c) * d + pos] += bad;
-                            else {
-                                const float now = __uint_as_float((uint32_t)*reinterpret_cast<uint16_t*>(to) << 16) + bad;
-                                *reinterpret_cast<uint16_t*>(to) = (uint16_t)pack16<false>(now, 0.f);
-                            }
-                        }
-                }
             }
             seq += 2 * count;
             ++units;
@@ -563,7 +569,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
         if (!ok && lane == 0) give_up();
     } else {
         if constexpr (kNarrow)
-            if (!attn_widen<kKind, kWarps * 32>(P, it, tid - (kSoftmaxWarps + 2) * 32, raw, ring, tile_bytes, S.raw_full, S.raw_empty, S.full, S.empty,
+            if (!attn_widen<kKind, kWarps * 32>(P, it, tid - (kSoftmaxWarps + 3) * 32, raw, ring, tile_bytes, S.raw_full, S.raw_empty, S.full, S.empty,
                                                 S.bad_value, abort_flag, [](const AttnUnit&, int) {}, [](int) {}) &&
                 lane == 0)
                 give_up();
