@@ -54,10 +54,11 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
     const int d = P.c.head_dim, tile_bytes = P.chunks * kChunkBytes;
     unsigned char* sQ = smem;
     unsigned char* ring = smem + P.q_tiles * tile_bytes;
-    unsigned char* raw = ring + P.slots * tile_bytes;
+    const int slots = P.k_slots + P.v_slots;
+    unsigned char* raw = ring + slots * tile_bytes;
 
     if (tid == 0) {
-        for (int s = 0; s < P.slots; ++s) { mbar_init(&S.full[s], kNarrow ? 4 : 1); mbar_init(&S.empty[s], 1); }
+        for (int s = 0; s < slots; ++s) { mbar_init(&S.full[s], kNarrow ? 4 : 1); mbar_init(&S.empty[s], 1); }
         for (int s = 0; s < P.raw_slots; ++s) { mbar_init(&S.raw_full[s], 1); mbar_init(&S.raw_empty[s], 4); }
         mbar_init(&S.q_full, kSoftmaxWarps);
         for (int t = 0; t < 2; ++t) { mbar_init(&S.s_full[t], 1); mbar_init(&S.p_full[t], 4); mbar_init(&S.o_full[t], 1); }
@@ -82,7 +83,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
 
     if (warp == kProducer) {
         attn_produce<kNarrow>(P, it, map_k, map_v, kNarrow ? raw : ring, kNarrow ? S.raw_full : S.full, kNarrow ? S.raw_empty : S.empty,
-                              kNarrow ? P.raw_slots : P.slots, abort_flag);
+                              abort_flag);
     } else if (warp == kIssuer) {
         // ---------------- products --------------------------------------------------------------------------
         const uint32_t type = kNarrow ? 0u : 1u;                            // fp16 or bf16 operands, fp32 sums
@@ -94,15 +95,14 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
         const int steps = d / 16;
         uint32_t units = 0, items[2] = {0, 0};
         bool ok = true, issued = false;
-        // K and V tiles alternate in the ring; the places of the next of each
-        uint32_t ks = 0, vs = 1, kph = 0, vph = 0;
-        auto advance = [&](uint32_t& s, uint32_t& ph) { s += 2; if (s >= (uint32_t)P.slots) { s -= P.slots; ph ^= 1u; } };
+        RingPlace k_at, v_at;
         auto wait = [&](uint64_t* bar, uint32_t ph) { ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, ph)); return ok; };
         while (ok && !__any_sync(0xffffffffu, *abort_flag) && it.next(P, u)) {
             const int n = (u.j1 - u.j0) << (u.pair ? 1 : 0);
             const bool pair = u.pair;
             auto scores = [&](uint32_t t) {
-                if (!wait(&S.full[ks], kph)) return;
+                const uint32_t ks = (uint32_t)k_at.s;
+                if (!wait(&S.full[ks], k_at.ph)) return;
                 tc_fence_after();
                 const uint32_t a = q0 + (pair && t ? tile_step : 0u), b = k0 + ks * tile_step;
                 const bool last = !pair || t;
@@ -117,7 +117,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                     if (last) umma_commit(&S.empty[ks]);
                 }
                 __syncwarp();
-                if (last) advance(ks, kph);
+                if (last) k_at.next(P.k_slots);
                 issued = true;
             };
             if (!wait(&S.q_full, units & 1u)) break;
@@ -127,7 +127,8 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
             if (n > 1) scores(1);
             for (int i = 0; ok && i < n; ++i) {
                 const uint32_t t = (uint32_t)(i & 1);
-                if (!wait(&S.p_full[t], (t ? items[1] : items[0]) & 1u) || !wait(&S.full[vs], vph)) break;
+                const uint32_t vs = (uint32_t)(P.k_slots + v_at.s);
+                if (!wait(&S.p_full[t], (t ? items[1] : items[0]) & 1u) || !wait(&S.full[vs], v_at.ph)) break;
                 if (t) ++items[1]; else ++items[0];
                 tc_fence_after();
                 const uint32_t b = v0 + vs * tile_step;
@@ -141,7 +142,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                     else if (i + 1 == n) { umma_commit(&S.o_full[0]); umma_commit(&S.o_full[1]); }   // the groups share Q
                 }
                 __syncwarp();
-                if (last) advance(vs, vph);
+                if (last) v_at.next(P.v_slots);
                 if (i + 2 < n) scores(t);
             }
         }
@@ -158,7 +159,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
         const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t tS = tmem + lane_base + t * 128, tO = tmem + lane_base + 256 + t * 128;
         uint32_t units = 0, items = 0, merges = 0;
-        uint32_t seq = 0;                        // tiles of the ring used by earlier units
+        uint32_t seq = 0;                        // cache tiles of earlier units
         bool ok = true, merged = false;
         auto wait = [&](uint64_t* bar, uint32_t ph) {
             ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, ph));
@@ -260,7 +261,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                 float v_exp = 0.f;
                 if constexpr (kNarrow) {
                     // the scales of this tile have been stored before its K tile was announced
-                    const int at = (int)((seq / 2 + jj) % kAttnScaleTiles);
+                    const int at = (int)((seq + jj) % kAttnScaleTiles);
                     fk = scales.k[at];
                     fv = scales.v[at];
                     if (!any) factor = scales.q[tile][row];                 // stored before Q was announced
@@ -363,8 +364,8 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                 if (!kNarrow && masked && (!u.pair || t == 0)) {
                     // V of positions that no row sees, or that hold NaN or infinities that only some see, must not meet a
                     // weight of zero in the product: zeros here, the latter added to the rows that see them at the end
-                    const uint32_t i = seq + 2 * jj + 1, s = i % P.slots;
-                    if (!wait(&S.full[s], i / P.slots & 1u)) break;
+                    const uint32_t i = seq + jj, s = P.k_slots + i % P.v_slots;
+                    if (!wait(&S.full[s], i / P.v_slots & 1u)) break;
                     if (start + row >= u.first || row >= valid) {
                         if (attn_clean_values(ring + (size_t)s * tile_bytes + row * 128, row, P.chunks, row < valid))
                             S.bad_value[units % kAttnUnitFlags] = 1;
@@ -448,7 +449,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                 __syncwarp();
                 if (join) { tc_fence_before(); arrive(&S.merge_done); }
             }
-            seq += 2 * done_count;
+            seq += done_count;
             ++units;
         }
         if (!ok && lane == 0) give_up();
@@ -618,16 +619,13 @@ static int attn_launch(AttnParams& P, const CUtensorMap& k, const CUtensorMap& v
     static std::atomic<unsigned long long> ready{0};
     if (!attn_allow_smem(attn_kernel<kKind>, kSmem, ready)) return launch_status();
     const int tile = P.chunks * kChunkBytes;
-    if (kNarrow) {
-        // four 16-bit tiles beside one of Q, three beside two; the rest for 8-bit ones
-        P.slots = P.q_tiles == 1 ? 4 : 3;
-        P.raw_slots = (kAttnNarrowBytes - (P.q_tiles + P.slots) * tile) / (kAttnTile * P.c.head_dim);
-        if (P.raw_slots > kAttnMaxRaw) P.raw_slots = kAttnMaxRaw;
-    } else {
-        P.slots = kAttnRingBytes / tile - P.q_tiles;
-        if (P.slots > kAttnMaxSlots) P.slots = kAttnMaxSlots;
-        P.raw_slots = 0;
-    }
+    // 8-bit: four 16-bit tiles beside one of Q, three beside two; the rest for 8-bit ones
+    int slots = kNarrow ? (P.q_tiles == 1 ? 4 : 3) : kAttnRingBytes / tile - P.q_tiles;
+    if (slots > kAttnMaxSlots) slots = kAttnMaxSlots;
+    P.k_slots = slots / 2;
+    P.v_slots = slots - P.k_slots;
+    P.raw_slots = kNarrow ? (kAttnNarrowBytes - (P.q_tiles + slots) * tile) / (kAttnTile * P.c.head_dim) : 0;
+    if (P.raw_slots > kAttnMaxRaw) P.raw_slots = kAttnMaxRaw;
     KernelTimerScope timer(DSPARK_K_TREE_ATTENTION, s);
     launch_pdl(attn_kernel<kKind>, dim3((unsigned)sms), dim3(kAttnThreads<kKind>), kSmem, s, P, k, v);
     return launch_status();

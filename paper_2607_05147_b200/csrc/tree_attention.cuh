@@ -36,7 +36,7 @@ struct AttnParams {
     int tile_nodes, unit_nodes;                  // nodes of a row tile, of a unit
     int q_tiles;                                 // row tiles of a unit: 1 or 2
     int chunks;                                  // of 64 columns: 1 or 2
-    int slots, raw_slots;                        // 16-bit tiles of the ring, 8-bit tiles
+    int k_slots, v_slots, raw_slots;             // rings: 16-bit tiles of K, of V (behind those of K), 8-bit tiles of both in turn
     int tile_tokens, page_tiles, page_boxes;     // positions of a box; cache tiles of a page (pages above 128) ; boxes of a tile
     int part_rows;                               // rows of a partial result
     int32_t* dev_status;
@@ -290,16 +290,24 @@ __device__ __forceinline__ uint2 widen4(uint32_t w)
 }
 
 // ---- roles that both kernels have ------------------------------------------------------------------------
-// The producer warp: K and V tiles into a ring, K before V, a lane a box.
+// A place in a ring and the parity of its round.  K and V have a ring each: a warp that waits for the tiles of one of them only
+// must meet every round of a slot, or a slot that is two rounds on looks like one that is not there yet.
+struct RingPlace {
+    int s = 0;
+    uint32_t ph = 0;
+    __device__ __forceinline__ void next(int slots) { if (++s == slots) { s = 0; ph ^= 1u; } }
+};
+
+// The producer warp: K and V tiles, K before V, a lane a box; 16-bit ones into their rings, 8-bit ones into one.
 template <bool kNarrow>
 __device__ __forceinline__ void attn_produce(const AttnParams& P, AttnIter it, const CUtensorMap& map_k, const CUtensorMap& map_v, unsigned char* ring,
-                                             uint64_t* full, uint64_t* empty, int slots, volatile int* abort_flag)
+                                             uint64_t* full, uint64_t* empty, volatile int* abort_flag)
 {
     const int lane = threadIdx.x & 31, d = P.c.head_dim;
     const int row_bytes = kNarrow ? d : 128, copies = kNarrow ? 1 : P.chunks, slot_bytes = kNarrow ? kAttnTile * d : P.chunks * kChunkBytes;
     const int box = lane / copies, chunk = lane - box * copies;
-    int s = 0;
-    uint32_t ph = 0;
+    const int slots[2] = {kNarrow ? P.raw_slots : P.k_slots, kNarrow ? P.raw_slots : P.v_slots};
+    RingPlace at[2];                             // 8-bit tiles: the first for both
     bool ok = true, bad_page = false;
     AttnUnit u;
     while (ok && !*abort_flag && it.next(P, u)) {
@@ -314,26 +322,31 @@ __device__ __forceinline__ void attn_produce(const AttnParams& P, AttnIter it, c
                 page = table[page_of + box];
                 if (page < 0 || page >= P.c.n_pages) { page = P.c.n_pages; bad_page = true; }     // outside the map: zeros
             }
+#pragma unroll
             for (int kv = 0; kv < 2; ++kv) {
-                ok = __all_sync(0xffffffffu, mbar_wait_bounded(&empty[s], ph ^ 1u));
+                RingPlace& place = at[kNarrow ? 0 : kv];
+                const int s = place.s + (!kNarrow && kv ? P.k_slots : 0);
+                ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(&empty[s], place.ph ^ 1u));
                 if (!ok) break;
                 if (lane == 0) mbar_arrive_expect_tx(&full[s], (uint32_t)(boxes * copies * P.tile_tokens * row_bytes));
                 __syncwarp();
                 if (box < boxes)
                     tma_load_4d(ring + (size_t)s * slot_bytes + chunk * kChunkBytes + box * P.tile_tokens * row_bytes, kv ? &map_v : &map_k,
                                 chunk * 64, y, u.head, page, &full[s]);
-                if (++s == slots) { s = 0; ph ^= 1u; }
+                place.next(slots[kv]);
             }
         }
     }
     if (bad_page) atomicOr(P.dev_status, DSPARK_DEV_BAD_PAGE);
     if (!ok && lane == 0) { atomicOr(P.dev_status, DSPARK_DEV_TIMEOUT); *abort_flag = 1; }
     // Leave only after every copy has landed: its slot has been announced as free, or, where somebody gave up, is full.
-    for (int i = 0; i < slots; ++i) {
-        if (!*abort_flag) mbar_wait_bounded(&empty[s], ph ^ 1u);
-        else mbar_wait_bounded(&full[s], ph ^ 1u, 1u << 16);
-        if (++s == slots) { s = 0; ph ^= 1u; }
-    }
+    for (int kv = 0; kv < (kNarrow ? 1 : 2); ++kv)
+        for (int i = 0; i < slots[kv]; ++i) {
+            const int s = at[kv].s + (kv ? P.k_slots : 0);
+            if (!*abort_flag) mbar_wait_bounded(&empty[s], at[kv].ph ^ 1u);
+            else mbar_wait_bounded(&full[s], at[kv].ph ^ 1u, 1u << 16);
+            at[kv].next(slots[kv]);
+        }
 }
 
 // kThreads threads: 8-bit tiles of one ring as fp16 tiles of another, as the products read them.  tile(unit, j) is called before
@@ -344,10 +357,29 @@ __device__ __forceinline__ bool attn_widen(const AttnParams& P, AttnIter it, int
                                            volatile int* abort_flag, Tile tile, Ready ready)
 {
     constexpr int kMost = kAttnTile * kAttnMaxDim / 16 / kThreads;          // 16-byte pieces of one thread
-    const int lane = threadIdx.x & 31, d = P.c.head_dim;
-    const int pieces = d / 16, inverse = (65536 + pieces - 1) / pieces, all = kAttnTile * pieces;
-    int s = 0, rs = 0, number = 0, unit = 0;
-    uint32_t ph = 0, rph = 0;
+    const int lane = threadIdx.x & 31, d = P.c.head_dim, pieces = d / 16;
+    int number = 0, unit = 0;
+    RingPlace at[2], from_raw;
+    // Where a thread's pieces come from and go to.  Eight lanes store to eight different places of a line of 128 bytes: the pieces of
+    // two neighbouring positions, which the swizzle parts by an odd number of places; with 128 components one position's lie in
+    // the other chunk, so that the loads' banks differ too.
+    int from[kMost], to[kMost], token[kMost];
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+        const int x = i * kThreads + ct;
+        int piece;
+        if (pieces == 8) {
+            const int odd = x >> 2 & 1;
+            token[i] = (x >> 4) * 2 + odd;
+            piece = ((x >> 3 & 1) ^ odd) * 4 + (x & 3);
+        } else {
+            token[i] = x / pieces;
+            piece = x - token[i] * pieces;
+        }
+        from[i] = token[i] * d + piece * 16;
+        to[i] = (piece >> 2) * kChunkBytes + token[i] * 128 + ((((piece & 3) * 2) ^ (token[i] & 7)) << 4);
+        if (x >= kAttnTile * pieces) token[i] = -1;
+    }
     AttnUnit u;
     while (!*abort_flag && it.next(P, u)) {
         for (int j = u.j0; j < u.j1; ++j, ++number) {
@@ -356,21 +388,22 @@ __device__ __forceinline__ bool attn_widen(const AttnParams& P, AttnIter it, int
             const int valid = min(len, u.length - start), tree = u.first - start;   // positions from `tree` on are nodes
             tile(u, j);
             for (int kv = 0; kv < 2; ++kv) {
-                if (!__all_sync(0xffffffffu, mbar_wait_bounded(&raw_full[rs], rph) && mbar_wait_bounded(&empty[s], ph ^ 1u))) return false;
+                RingPlace& place = at[kv];
+                const int s = place.s + (kv ? P.k_slots : 0), rs = from_raw.s;
+                if (!__all_sync(0xffffffffu, mbar_wait_bounded(&raw_full[rs], from_raw.ph) && mbar_wait_bounded(&empty[s], place.ph ^ 1u))) return false;
                 if (kv == 0) ready(number);
                 const unsigned char* src = raw + (size_t)rs * kAttnTile * d;
                 unsigned char* dst = ring + (size_t)s * tile_bytes;
                 uint4 w[kMost];
 #pragma unroll
                 for (int i = 0; i < kMost; ++i)
-                    if (i * kThreads + ct < all) w[i] = *reinterpret_cast<const uint4*>(src + (i * kThreads + ct) * 16);
+                    if (token[i] >= 0) w[i] = *reinterpret_cast<const uint4*>(src + from[i]);
 #pragma unroll
                 for (int i = 0; i < kMost; ++i) {
-                    const int x = i * kThreads + ct, token = x * inverse >> 16, piece = x - token * pieces;   // x < 1024: exact
-                    if (x >= all) break;
+                    if (token[i] < 0) continue;
                     uint2 a = widen4<kKind>(w[i].x), b = widen4<kKind>(w[i].y), c = widen4<kKind>(w[i].z), e = widen4<kKind>(w[i].w);
-                    if (token >= valid) a = b = c = e = make_uint2(0, 0);
-                    if (kKind == kAttnE4M3 && kv && token >= tree) {
+                    if (valid < kAttnTile && token[i] >= valid) a = b = c = e = make_uint2(0, 0);
+                    if (kKind == kAttnE4M3 && kv && token[i] >= tree) {
                         // a NaN among the nodes' values of V: zero here and back in the rows that see it (attn_bad_values)
                         uint32_t h[8] = {a.x, a.y, b.x, b.y, c.x, c.y, e.x, e.y};
                         bool bad = false;
@@ -384,17 +417,14 @@ __device__ __forceinline__ bool attn_widen(const AttnParams& P, AttnIter it, int
                             bad_value[unit % kAttnUnitFlags] = 1;
                         }
                     }
-                    unsigned char* line = dst + (piece >> 2) * kChunkBytes + token * 128;
-                    const int at = (piece & 3) * 2, turn = (piece >> 2) & 1;       // the two halves of eight lanes store in turn
-                    const uint4 lo = make_uint4(a.x, a.y, b.x, b.y), hi = make_uint4(c.x, c.y, e.x, e.y);
-                    *reinterpret_cast<uint4*>(line + (((at + turn) ^ (token & 7)) << 4)) = turn ? hi : lo;
-                    *reinterpret_cast<uint4*>(line + (((at + 1 - turn) ^ (token & 7)) << 4)) = turn ? lo : hi;
+                    *reinterpret_cast<uint4*>(dst + to[i]) = make_uint4(a.x, a.y, b.x, b.y);
+                    *reinterpret_cast<uint4*>(dst + (to[i] ^ 16)) = make_uint4(c.x, c.y, e.x, e.y);
                 }
                 fence_async_smem();
                 __syncwarp();
                 if (lane == 0) { mbar_arrive(&raw_empty[rs]); mbar_arrive(&full[s]); }
-                if (++rs == P.raw_slots) { rs = 0; rph ^= 1u; }
-                if (++s == P.slots) { s = 0; ph ^= 1u; }
+                from_raw.next(P.raw_slots);
+                place.next(kv ? P.v_slots : P.k_slots);
             }
         }
         ++unit;
