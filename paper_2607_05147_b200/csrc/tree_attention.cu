@@ -35,10 +35,14 @@ struct AttnShared {
     float2 second[kAttnTile];                    // (reference, sum) of the second group
 };
 template <int kKind>
-struct AttnScales { float k[kAttnScaleTiles][kAttnTile], v[kAttnScaleTiles][kAttnTile], q[2][kAttnTile]; };   // q: per row
+struct AttnScales {                              // q: per row; bad: a bit for a node's position with a scale that is no number
+    float k[kAttnScaleTiles][kAttnTile], v[kAttnScaleTiles][kAttnTile], q[2][kAttnTile];
+    uint32_t bad[kAttnScaleTiles][4];
+};
 template <> struct AttnScales<kAttnWide> {};
 
-template <int kKind> constexpr int kAttnThreads = (kSoftmaxWarps + 2 + (kKind == kAttnWide ? 0 : 4)) * 32;
+constexpr int kAttnConverters = 8;
+template <int kKind> constexpr int kAttnThreads = (kSoftmaxWarps + 2 + (kKind == kAttnWide ? 0 : kAttnConverters)) * 32;
 
 template <int kKind>
 __global__ void __launch_bounds__(kAttnThreads<kKind>, 1)
@@ -58,8 +62,8 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
     unsigned char* raw = ring + slots * tile_bytes;
 
     if (tid == 0) {
-        for (int s = 0; s < slots; ++s) { mbar_init(&S.full[s], kNarrow ? 4 : 1); mbar_init(&S.empty[s], 1); }
-        for (int s = 0; s < P.raw_slots; ++s) { mbar_init(&S.raw_full[s], 1); mbar_init(&S.raw_empty[s], 4); }
+        for (int s = 0; s < slots; ++s) { mbar_init(&S.full[s], kNarrow ? kAttnConverters : 1); mbar_init(&S.empty[s], 1); }
+        for (int s = 0; s < P.raw_slots; ++s) { mbar_init(&S.raw_full[s], 1); mbar_init(&S.raw_empty[s], kAttnConverters); }
         mbar_init(&S.q_full, kSoftmaxWarps);
         for (int t = 0; t < 2; ++t) { mbar_init(&S.s_full[t], 1); mbar_init(&S.p_full[t], 4); mbar_init(&S.o_full[t], 1); }
         for (int i = 0; i < kAttnUnitFlags; ++i) S.bad_value[i] = 0;
@@ -219,7 +223,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
             const bool warp_live = __any_sync(0xffffffffu, live);
             float factor = P.score_factor;       // 8-bit caches: what the row of Q was scaled by (K's scales hold score_factor)
             if (tid == 0) S.bad_value[(units + kAttnUnitFlags / 2) % kAttnUnitFlags] = 0;
-            float ref = -INFINITY, sum = 0.f;    // O and the sum are relative to 2^ref
+            float ref = kAttnUnset, sum = 0.f;   // O and the sum are relative to 2^ref, a whole number
             bool any = false;                    // O holds something
             const int step = u.pair ? 1 : 2;
             const int count = u.j1 - u.j0;
@@ -258,104 +262,123 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                 tc_fence_after();
                 const float* fk = nullptr;
                 const float* fv = nullptr;
-                float v_exp = 0.f;
+                float above = 0.f;               // what a weight may be above its reference is less by this
+                const uint32_t* bad = nullptr;
                 if constexpr (kNarrow) {
                     // the scales of this tile have been stored before its K tile was announced
                     const int at = (int)((seq + jj) % kAttnScaleTiles);
                     fk = scales.k[at];
                     fv = scales.v[at];
+                    bad = scales.bad[at];
                     if (!any) factor = scales.q[tile][row];                 // stored before Q was announced
-                    if (!masked) v_exp = attn_exponent(warp_max_f32(attn_finite_max(reinterpret_cast<const float4*>(fv)[lane], ~0u, 0.f)));
+                    if (!masked) above = attn_exponent(warp_max_f32(attn_finite_max(reinterpret_cast<const float4*>(fv)[lane], ~0u, 0.f)));
                     else {                       // of the positions that this row sees
                         float top = 0.f;
 #pragma unroll
                         for (int w = 0; w < 4; ++w)
-#pragma unroll
+#pragma unroll 1
                             for (int i = 0; i < 32; i += 4) top = attn_finite_max(*reinterpret_cast<const float4*>(fv + w * 32 + i), seen[w] >> i, top);
-                        v_exp = attn_exponent(top);
+                        above = attn_exponent(top);
                     }
+                    above -= kAttnNarrowOffset;
                 }
+                __syncwarp();
                 if (warp_live) {
-                    // the largest score, in units of log2
-                    float top = -INFINITY;
+                    if (masked)                  // scores of positions that the row does not see: -infinity, in place
 #pragma unroll
-                    for (int c = 0; c < 4; c += 2) {
-                        float a[2][32];
-                        tmem_load32_issue(tS + c * 32, a[0]);
-                        tmem_load32_issue(tS + c * 32 + 32, a[1]);
-                        tmem_load_wait(a[0]);
-                        tmem_load_wait(a[1]);
+                        for (int w = 0; w < 4; ++w)
+#pragma unroll 1
+                            for (int c = 0; c < 32; c += 16) {
+                                float s[16];
+                                uint32_t x[16];
+                                tmem_load16(tS + w * 32 + c, s);
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            if constexpr (kNarrow) {
-#pragma unroll
-                                for (int i = 0; i < 32; i += 4) {
-                                    const float4 f = *reinterpret_cast<const float4*>(fk + (c + h) * 32 + i);
-                                    a[h][i] *= f.x; a[h][i + 1] *= f.y; a[h][i + 2] *= f.z; a[h][i + 3] *= f.w;
+                                for (int i = 0; i < 16; ++i) {
+                                    x[i] = __float_as_uint((seen[w] >> (c + i) & 1u) ? s[i] : -INFINITY);
+                                    if (kNarrow) x[i] = (seen[w] & bad[w]) >> (c + i) & 1u ? 0x7fffffffu : x[i];    // NaN
                                 }
+                                tmem_store16(tS + w * 32 + c, x);
+                                tmem_store_wait();
                             }
-                            if (masked) {
-#pragma unroll
-                                for (int i = 0; i < 32; ++i) top = fmaxf(top, (seen[c + h] >> i & 1u) ? a[h][i] : -INFINITY);
-                            } else {
-#pragma unroll
-                                for (int i = 0; i < 32; i += 2) top = fmaxf(top, fmaxf(a[h][i], a[h][i + 1]));
-                            }
-                        }
-                    }
-                    top = top * factor + (kNarrow ? v_exp - kAttnNarrowOffset : 0.f);
-                    const bool raise = top > ref + kAttnLazy || (ref == -INFINITY && top > -INFINITY);
-                    if (__any_sync(0xffffffffu, raise)) {
-                        const float f = !raise ? 1.f : ref == -INFINITY ? 0.f : ex2_approx(ref - top);
-                        if (raise) { sum *= f; ref = top; }
-                        if (any)
-                            for (int c = 0; c < d; c += 16) {
-                                float o[16];
-                                uint32_t w[16];
-                                tmem_load16(tO + c, o);
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(o[i] * f);
-                                tmem_store16(tO + c, w);
-                            }
-                    }
-                    any = true;
-                    const float base = ref == -INFINITY ? 0.f : ref;
-                    const uint64_t f2 = pack2(factor, factor), b2 = pack2(-base, -base);
+                    const uint64_t f2 = pack2(factor, factor);
                     uint64_t s2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
-                    float a[2][32];
-                    tmem_load32_issue(tS, a[0]);
-#pragma unroll
+                    // 32 positions at a time: the loop is not unrolled, so that the code stays near
+#pragma unroll 1
                     for (int c = 0; c < 4; ++c) {
-                        float (&x)[32] = a[c & 1];
-                        tmem_load_wait(x);
-                        if (c < 3) tmem_load32_issue(tS + c * 32 + 32, a[(c + 1) & 1]);
+                        float x[32];
+                        auto relative = [&](float less) {                   // score * factor - reference
+                            const uint64_t b2 = pack2(less, less);
+                            tmem_load32_issue(tS + c * 32, x);
+                            tmem_load_wait(x);
+#pragma unroll
+                            for (int i = 0; i < 32; i += 4) {
+                                uint64_t y0 = pack2(x[i], x[i + 1]), y1 = pack2(x[i + 2], x[i + 3]);
+                                if constexpr (kNarrow) {
+                                    const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(fk + c * 32 + i);
+                                    y0 = mul2(y0, f.x);
+                                    y1 = mul2(y1, f.y);
+                                }
+                                unpack2(fma2(y0, f2, b2), x[i], x[i + 1]);
+                                unpack2(fma2(y1, f2, b2), x[i + 2], x[i + 3]);
+                            }
+                            float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                            for (int i = 0; i < 32; i += 2) top[i / 2 & 3] = fmaxf(top[i / 2 & 3], fmaxf(x[i], x[i + 1]));
+                            return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) + above;
+                        };
+                        if (__any_sync(0xffffffffu, relative(-ref) > kAttnLazy)) {
+                            // A new reference for the rows that need one.  It is a whole number, so that what has been stored of this
+                            // tile's weights can be scaled exactly.
+                            const float top = relative(0.f);
+                            const bool raise = top > ref + kAttnLazy;
+                            const float now = raise ? ceilf(top) : ref, f = raise ? ex2_approx(fmaxf(ref - now, -200.f)) : 1.f;
+                            const uint64_t ff = pack2(f, f);
+                            ref = now;
+                            sum *= f;
+                            s2[0] = mul2(s2[0], ff);
+                            s2[1] = mul2(s2[1], ff);
+                            if (any)
+#pragma unroll 1
+                                for (int i = 0; i < d; i += 16) {
+                                    float o[16];
+                                    uint32_t w[16];
+                                    tmem_load16(tO + i, o);
+#pragma unroll
+                                    for (int k = 0; k < 16; ++k) w[k] = __float_as_uint(o[k] * f);
+                                    tmem_store16(tO + i, w);
+                                }
+#pragma unroll 1
+                            for (int i = 0; i < c; ++i) {
+                                float p[16];
+                                uint32_t w[16];
+                                tmem_load16(tS + i * 16, p);
+#pragma unroll
+                                for (int k = 0; k < 16; ++k) w[k] = scale16<kNarrow>(__float_as_uint(p[k]), f);
+                                tmem_store16(tS + i * 16, w);
+                            }
+                            tmem_store_wait();
+                            relative(-ref);
+                        }
                         uint32_t w[16];
 #pragma unroll
-                        for (int i = 0; i < 32; i += 2) {
-                            uint64_t y = pack2(x[i], x[i + 1]);
-                            if constexpr (kNarrow) y = mul2(y, *reinterpret_cast<const uint64_t*>(fk + c * 32 + i));
-                            y = fma2(y, f2, b2);
-                            float e0, e1;
-                            unpack2(y, e0, e1);
-                            if (masked) {
-                                e0 = (seen[c] >> i & 1u) ? e0 : -INFINITY;
-                                e1 = (seen[c] >> (i + 1) & 1u) ? e1 : -INFINITY;
-                            }
-                            e0 = ex2_approx(e0);
-                            e1 = ex2_approx(e1);
-                            const uint64_t e = pack2(e0, e1);
-                            s2[(i >> 1) & 1] = add2(s2[(i >> 1) & 1], e);
+                        for (int i = 0; i < 32; i += 4) {
+                            float e[4];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) e[k] = ex2_approx(x[i + k]);
+                            uint64_t e0 = pack2(e[0], e[1]), e1 = pack2(e[2], e[3]);
+                            s2[0] = add2(s2[0], e0);
+                            s2[1] = add2(s2[1], e1);
                             if constexpr (kNarrow) {
-                                unpack2(mul2(e, *reinterpret_cast<const uint64_t*>(fv + c * 32 + i)), e0, e1);
-                                if (masked) {
-                                    e0 = (seen[c] >> i & 1u) ? e0 : 0.f;
-                                    e1 = (seen[c] >> (i + 1) & 1u) ? e1 : 0.f;
-                                }
+                                const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(fv + c * 32 + i);
+                                unpack2(mul2(e0, f.x), e[0], e[1]);
+                                unpack2(mul2(e1, f.y), e[2], e[3]);
                             }
-                            w[i >> 1] = pack16<kNarrow>(e0, e1);
+                            w[i >> 1] = pack16<kNarrow>(e[0], e[1]);
+                            w[(i >> 1) + 1] = pack16<kNarrow>(e[2], e[3]);
                         }
                         tmem_store16(tS + c * 16, w);
                     }
+                    any = true;
                     float s0, s1;
                     unpack2(add2(s2[0], s2[1]), s0, s1);
                     sum += s0 + s1;
@@ -395,16 +418,15 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                 ++merges;
                 merged = true;
             } else if (done.pair || t == 0) {
-                float ref1 = -INFINITY, f0 = 1.f, f1 = 0.f;
+                float f0 = 1.f, f1 = 0.f;
                 if (join) {
                     if (!wait(&S.merge_ready, merges & 1u)) break;
                     ++merges;
                     tc_fence_after();
                     const float2 o = S.second[row];
-                    ref1 = o.x;
-                    const float top = fmaxf(ref, ref1), base = top == -INFINITY ? 0.f : top;
-                    f0 = ex2_approx(ref - base);
-                    f1 = ex2_approx(ref1 - base);
+                    const float top = fmaxf(ref, o.x);
+                    f0 = ex2_approx(ref - top);
+                    f1 = ex2_approx(o.x - top);
                     sum = sum * f0 + o.y * f1;
                     ref = top;
                 }
@@ -456,14 +478,16 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
     } else {
         // ---------------- 8-bit tiles to 16 bits --------------------------------------------------------------
         if constexpr (kNarrow) {
-            const int ct = tid - (kSoftmaxWarps + 2) * 32;                  // 0 .. 127
+            const int ct = tid - (kSoftmaxWarps + 2) * 32;
             // scales of position ct of a tile
             float k_now = 0.f, v_now = 0.f;
+            bool node = false;
             auto load_scales = [&](const AttnUnit& w, int j) {
                 int start, len;
                 attn_tile_at(P, j, start, len);
                 k_now = v_now = 0.f;
-                if (ct >= min(len, w.length - start)) return;
+                node = start + ct >= w.first;
+                if (ct >= min(kAttnTile, min(len, w.length - start))) return;
                 const int position = start + ct, page_of = position / P.c.page_size, token = position - page_of * P.c.page_size;
                 const int page = P.c.block_table[w.r * P.c.table_stride + page_of];
                 if (page < 0 || page >= P.c.n_pages) return;
@@ -473,10 +497,16 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
             };
             auto store_scales = [&](int number) {
                 // free: the scores of tile number - 2 are not computed before the weights of tile number - 4 are there
-                scales.k[number % kAttnScaleTiles][ct] = k_now * P.score_factor;
-                scales.v[number % kAttnScaleTiles][ct] = v_now;
+                if (ct >= kAttnTile) return;
+                const int at = number % kAttnScaleTiles;
+                const bool bad = node && !(fabsf(k_now) < INFINITY && fabsf(v_now) < INFINITY);
+                const float k = k_now * P.score_factor;
+                scales.k[at][ct] = bad ? 1.f : k < kAttnLeastFactor ? kAttnLeastFactor : k;
+                scales.v[at][ct] = bad ? 0.f : v_now;
+                const uint32_t bits = __ballot_sync(0xffffffffu, bad);
+                if (lane == 0) scales.bad[at][ct >> 5] = bits;
             };
-            if (!attn_widen<kKind, 128>(P, it, ct, raw, ring, tile_bytes, S.raw_full, S.raw_empty, S.full, S.empty, S.bad_value, abort_flag, load_scales,
+            if (!attn_widen<kKind, kAttnConverters * 32>(P, it, ct, raw, ring, tile_bytes, S.raw_full, S.raw_empty, S.full, S.empty, S.bad_value, abort_flag, load_scales,
                                         store_scales) && lane == 0)
                 give_up();
         }

@@ -18,6 +18,7 @@ constexpr int kAttnNarrowBytes = 208 * 1024;                  // with 8-bit cach
 constexpr float kAttnLog2e = 1.4426950408889634f;
 constexpr float kAttnLazy = 8.f;                 // O is scaled when the maximum rises by more than 2^8
 constexpr float kAttnNarrowOffset = 7.f;         // fp16 weights: up to 2^(7 + 8) of 65 504, down to 2^-31 of the largest
+constexpr float kAttnUnset = -1e38f;              // a reference that every score is above
 constexpr float kAttnLeastFactor = 1e-20f;       // of a score: -infinity times it is -infinity, a score times it next to nothing
 constexpr int kSoftmaxWarps = 8;
 constexpr int kAttnUnitFlags = 8;               // units of one CTA that are under way at a time: at most four
@@ -259,6 +260,15 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi)
     if (kHalf) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
+}
+// a pair of 16-bit floats times a power of two
+template <bool kHalf>
+__device__ __forceinline__ uint32_t scale16(uint32_t w, float f)
+{
+    if (!kHalf) return pack16<false>(bf16lo(w) * f, bf16hi(w) * f);
+    float a, b;
+    asm("{\n\t.reg .b16 x, y;\n\tmov.b32 {x, y}, %2;\n\tcvt.f32.f16 %0, x;\n\tcvt.f32.f16 %1, y;\n\t}" : "=f"(a), "=f"(b) : "r"(w));
+    return pack16<true>(a * f, b * f);
 }
 // the largest of those of four scales that are finite and asked for
 __device__ __forceinline__ float attn_finite_max(float4 x, uint32_t of, float top)
