@@ -33,6 +33,7 @@ struct AttnShared {
     int abort, bad_value[kAttnUnitFlags];
     AttnList list;
     float2 second[kAttnTile];                    // (reference, sum) of the second group
+    float of_half[2][2][kAttnTile];              // what the two threads of a row tell one another: largest scores, sums
 };
 template <int kKind>
 struct AttnScales {                              // q: per row; bad: a bit for a node's position with a scale that is no number
@@ -41,15 +42,17 @@ struct AttnScales {                              // q: per row; bad: a bit for a
 };
 template <> struct AttnScales<kAttnWide> {};
 
-constexpr int kAttnConverters = 8;
-template <int kKind> constexpr int kAttnThreads = (kSoftmaxWarps + 2 + (kKind == kAttnWide ? 0 : kAttnConverters)) * 32;
+constexpr int kRowWarps = 16;                    // of the softmax: two groups of four warps a half
+constexpr int kAttnConverters = 4;
+template <int kKind> constexpr int kAttnCols = kKind == kAttnWide ? 32 : 16;    // scores in registers at a time
+template <int kKind> constexpr int kAttnThreads = (kRowWarps + 2 + (kKind == kAttnWide ? 0 : kAttnConverters)) * 32;
 
 template <int kKind>
 __global__ void __launch_bounds__(kAttnThreads<kKind>, 1)
 attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v)
 {
     constexpr bool kNarrow = kKind != kAttnWide;
-    constexpr int kThreads = kAttnThreads<kKind>, kProducer = kSoftmaxWarps, kIssuer = kSoftmaxWarps + 1;
+    constexpr int kThreads = kAttnThreads<kKind>, kProducer = kRowWarps, kIssuer = kRowWarps + 1;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);   // swizzle atoms: 1 KB
     __shared__ AttnShared S;
@@ -63,11 +66,11 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
 
     if (tid == 0) {
         for (int s = 0; s < slots; ++s) { mbar_init(&S.full[s], kNarrow ? kAttnConverters : 1); mbar_init(&S.empty[s], 1); }
-        for (int s = 0; s < P.raw_slots; ++s) { mbar_init(&S.raw_full[s], 1); mbar_init(&S.raw_empty[s], kAttnConverters); }
-        mbar_init(&S.q_full, kSoftmaxWarps);
-        for (int t = 0; t < 2; ++t) { mbar_init(&S.s_full[t], 1); mbar_init(&S.p_full[t], 4); mbar_init(&S.o_full[t], 1); }
+        for (int s = 0; s < P.raw_k + P.raw_v; ++s) { mbar_init(&S.raw_full[s], 1); mbar_init(&S.raw_empty[s], kAttnConverters); }
+        mbar_init(&S.q_full, kRowWarps / 2);
+        for (int t = 0; t < 2; ++t) { mbar_init(&S.s_full[t], 1); mbar_init(&S.p_full[t], kRowWarps / 2); mbar_init(&S.o_full[t], 1); }
         for (int i = 0; i < kAttnUnitFlags; ++i) S.bad_value[i] = 0;
-        mbar_init(&S.merge_ready, 4); mbar_init(&S.merge_done, 4); mbar_init(&S.mma_done, 1);
+        mbar_init(&S.merge_ready, kRowWarps / 2); mbar_init(&S.merge_done, kRowWarps / 2); mbar_init(&S.mma_done, 1);
         S.abort = 0;
         mbar_fence_init();
     }
@@ -140,7 +143,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                 if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < kAttnTile / 16; ++k)
-                        mma_ts(tmem + 256 + t * 128, tmem + t * 128 + k * 8, b + k * 128, idesc_o, i > 1 || k > 0);
+                        mma_ts(tmem + 256 + t * 128, tmem + t * 128 + (k >> 2) * 64 + (k & 3) * 8, b + k * 128, idesc_o, i > 1 || k > 0);
                     if (last) umma_commit(&S.empty[vs]);
                     if (pair) { if (i + 2 >= n) umma_commit(&S.o_full[t]); }
                     else if (i + 1 == n) { umma_commit(&S.o_full[0]); umma_commit(&S.o_full[1]); }   // the groups share Q
@@ -157,19 +160,22 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
             mbar_wait_bounded(&S.mma_done, 0u);
         }
         __syncwarp();
-    } else if (warp < kSoftmaxWarps) {
+    } else if (warp < kRowWarps) {
         // ---------------- softmax ---------------------------------------------------------------------------
-        const int t = warp >> 2, row = tid & 127;                           // group; row of the tile
+        // A row belongs to a thread in each of two warps, which have 64 of a tile's positions each and later half of the row's
+        // components.  They share the row's reference; the two warps vote on it.  A wait that runs out makes `ok` false in its
+        // warp; the two leave together, at the next vote.
+        const int t = warp >> 3, half = warp >> 2 & 1, row = tid & 127;     // group; half; row of the tile
+        const int pair_id = t * 4 + (warp & 3);
         const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t tS = tmem + lane_base + t * 128, tO = tmem + lane_base + 256 + t * 128;
+        const uint32_t tS = tmem + lane_base + t * 128 + half * 64, tO = tmem + lane_base + 256 + t * 128;
+        const int o_begin = half ? (d + 31) / 32 * 16 : 0, o_end = half ? d : (d + 31) / 32 * 16;          // components
         uint32_t units = 0, items = 0, merges = 0;
         uint32_t seq = 0;                        // cache tiles of earlier units
         bool ok = true, merged = false;
-        auto wait = [&](uint64_t* bar, uint32_t ph) {
-            ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, ph));
-            return ok;
-        };
+        auto wait = [&](uint64_t* bar, uint32_t ph) { ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, ph)); };
         auto arrive = [&](uint64_t* bar) { __syncwarp(); if (lane == 0) mbar_arrive(bar); };
+        auto vote = [&](bool x) { return barrier_any<64>(pair_id + 1, x); };
         // Row `row` of row tile `tile` of a unit into shared memory; in 8-bit mode as fp16, scaled by a power of two so that no
         // value passes the range and what is lost is below 2^-37 of the row's largest.
         auto load_q = [&](const AttnUnit& w, int tile) {
@@ -211,23 +217,25 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
         bool have = it.next(P, u);
         // Q of the first unit; afterwards each unit's is loaded at the end of the one before
         auto prepare_q = [&](const AttnUnit& w) {
+            if (half) return;
             if (w.pair) load_q(w, t);
             else if (t == 1) load_q(w, 0);
             arrive(&S.q_full);
         };
         if (have) prepare_q(u);
-        while (ok && have && !*abort_flag) {
+        while (have) {
+            if (vote(!ok || *abort_flag)) { ok = false; break; }
             const int tile = u.pair ? t : 0;
             const int node = u.node0 + tile * tile_nodes + row / P.group;
             const bool live = row < tile_nodes * P.group && node < u.n;
-            const bool warp_live = __any_sync(0xffffffffu, live);
+            const bool warp_live = __any_sync(0xffffffffu, live);           // the same in both warps
             float factor = P.score_factor;       // 8-bit caches: what the row of Q was scaled by (K's scales hold score_factor)
             if (tid == 0) S.bad_value[(units + kAttnUnitFlags / 2) % kAttnUnitFlags] = 0;
-            float ref = kAttnUnset, sum = 0.f;   // O and the sum are relative to 2^ref, a whole number
-            bool any = false;                    // O holds something
+            float ref = kAttnUnset, sum = 0.f;   // O and the sum are relative to 2^ref
+            bool any = false, left = false;      // any: O holds something
             const int step = u.pair ? 1 : 2;
             const int count = u.j1 - u.j0;
-            for (int jj = u.pair ? 0 : t; ok && jj < count; jj += step) {
+            for (int jj = u.pair ? 0 : t; jj < count; jj += step) {
                 int start, len;
                 attn_tile_at(P, u.j0 + jj, start, len);
                 const int valid = min(len, u.length - start);               // positions of this tile that exist
@@ -257,128 +265,121 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                         }
                     }
                 }
-                if (!wait(&S.s_full[t], items & 1u)) break;
+                wait(&S.s_full[t], items & 1u);
                 ++items;
                 tc_fence_after();
                 const float* fk = nullptr;
                 const float* fv = nullptr;
                 float above = 0.f;               // what a weight may be above its reference is less by this
-                const uint32_t* bad = nullptr;
                 if constexpr (kNarrow) {
+                    if (warp_live) {
                     // the scales of this tile have been stored before its K tile was announced
                     const int at = (int)((seq + jj) % kAttnScaleTiles);
-                    fk = scales.k[at];
-                    fv = scales.v[at];
-                    bad = scales.bad[at];
+                    const float* all = scales.v[at];
+                    fk = scales.k[at] + half * 64;
+                    fv = scales.v[at] + half * 64;
                     if (!any) factor = scales.q[tile][row];                 // stored before Q was announced
-                    if (!masked) above = attn_exponent(warp_max_f32(attn_finite_max(reinterpret_cast<const float4*>(fv)[lane], ~0u, 0.f)));
+                    if (!masked) above = attn_exponent(warp_max_f32(attn_finite_max(reinterpret_cast<const float4*>(all)[lane], ~0u, 0.f)));
                     else {                       // of the positions that this row sees
                         float top = 0.f;
 #pragma unroll
                         for (int w = 0; w < 4; ++w)
 #pragma unroll 1
-                            for (int i = 0; i < 32; i += 4) top = attn_finite_max(*reinterpret_cast<const float4*>(fv + w * 32 + i), seen[w] >> i, top);
+                            for (int i = 0; i < 32; i += 4) top = attn_finite_max(*reinterpret_cast<const float4*>(all + w * 32 + i), seen[w] >> i, top);
                         above = attn_exponent(top);
                     }
                     above -= kAttnNarrowOffset;
+                    if (masked) {
+                        // scores of positions that the row does not see: -infinity, in place; NaN where a scale is no number
+                        __syncwarp();
+#pragma unroll
+                        for (int w = 0; w < 2; ++w) {
+                            const uint32_t on = half ? seen[2 + w] : seen[w], bad = on & scales.bad[at][half * 2 + w];
+                            attn_hide(tS + w * 32, on, bad);
+                        }
+                    }
+                    }
+                } else if (masked && warp_live) {
+                    __syncwarp();
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) attn_hide(tS + w * 32, half ? seen[2 + w] : seen[w], 0u);
                 }
-                __syncwarp();
                 if (warp_live) {
-                    if (masked)                  // scores of positions that the row does not see: -infinity, in place
+                    // 32 scores: from tensor memory, with an 8-bit cache times K's scales
+                    auto scores = [&](int c, float (&x)[kAttnCols<kKind>]) {
+                        attn_read<kAttnCols<kKind>>(tS + c, x);
+                        if constexpr (kNarrow) {
 #pragma unroll
-                        for (int w = 0; w < 4; ++w)
-#pragma unroll 1
-                            for (int c = 0; c < 32; c += 16) {
-                                float s[16];
-                                uint32_t x[16];
-                                tmem_load16(tS + w * 32 + c, s);
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) {
-                                    x[i] = __float_as_uint((seen[w] >> (c + i) & 1u) ? s[i] : -INFINITY);
-                                    if (kNarrow) x[i] = (seen[w] & bad[w]) >> (c + i) & 1u ? 0x7fffffffu : x[i];    // NaN
-                                }
-                                tmem_store16(tS + w * 32 + c, x);
-                                tmem_store_wait();
+                            for (int i = 0; i < kAttnCols<kKind>; i += 4) {
+                                const ulonglong2 k = *reinterpret_cast<const ulonglong2*>(fk + c + i);
+                                unpack2(mul2(pack2(x[i], x[i + 1]), k.x), x[i], x[i + 1]);
+                                unpack2(mul2(pack2(x[i + 2], x[i + 3]), k.y), x[i + 2], x[i + 3]);
                             }
-                    const uint64_t f2 = pack2(factor, factor);
-                    uint64_t s2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
-                    // 32 positions at a time: the loop is not unrolled, so that the code stays near
+                        }
+                    };
+                    float top = -INFINITY;
 #pragma unroll 1
-                    for (int c = 0; c < 4; ++c) {
-                        float x[32];
-                        auto relative = [&](float less) {                   // score * factor - reference
-                            const uint64_t b2 = pack2(less, less);
-                            tmem_load32_issue(tS + c * 32, x);
-                            tmem_load_wait(x);
+                    for (int c = 0; c < 64; c += kAttnCols<kKind>) {
+                        float x[kAttnCols<kKind>];
+                        scores(c, x);
+                        float a = -INFINITY, b = -INFINITY;
 #pragma unroll
-                            for (int i = 0; i < 32; i += 4) {
-                                uint64_t y0 = pack2(x[i], x[i + 1]), y1 = pack2(x[i + 2], x[i + 3]);
-                                if constexpr (kNarrow) {
-                                    const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(fk + c * 32 + i);
-                                    y0 = mul2(y0, f.x);
-                                    y1 = mul2(y1, f.y);
-                                }
-                                unpack2(fma2(y0, f2, b2), x[i], x[i + 1]);
-                                unpack2(fma2(y1, f2, b2), x[i + 2], x[i + 3]);
-                            }
-                            float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                            for (int i = 0; i < 32; i += 2) top[i / 2 & 3] = fmaxf(top[i / 2 & 3], fmaxf(x[i], x[i + 1]));
-                            return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) + above;
-                        };
-                        if (__any_sync(0xffffffffu, relative(-ref) > kAttnLazy)) {
-                            // A new reference for the rows that need one.  It is a whole number, so that what has been stored of this
-                            // tile's weights can be scaled exactly.
-                            const float top = relative(0.f);
-                            const bool raise = top > ref + kAttnLazy;
-                            const float now = raise ? ceilf(top) : ref, f = raise ? ex2_approx(fmaxf(ref - now, -200.f)) : 1.f;
-                            const uint64_t ff = pack2(f, f);
-                            ref = now;
-                            sum *= f;
-                            s2[0] = mul2(s2[0], ff);
-                            s2[1] = mul2(s2[1], ff);
-                            if (any)
+                        for (int i = 0; i < kAttnCols<kKind>; i += 4) { a = max3(a, x[i], x[i + 1]); b = max3(b, x[i + 2], x[i + 3]); }
+                        top = max3(top, a, b);
+                    }
+                    top = fmaf(top, factor, above);
+                    if (vote(!ok || top > ref + kAttnLazy)) {
+                        // a new reference for the rows that need one: the larger of the two halves' largest scores
+                        S.of_half[t][half][row] = top;
+                        if (vote(!ok)) { left = true; break; }
+                        const float both = fmaxf(top, S.of_half[t][half ^ 1][row]);
+                        const bool raise = both > ref + kAttnLazy;
+                        const float by = raise ? ex2_approx(ref - both) : 1.f;
+                        if (raise) ref = both;
+                        sum *= by;
+                        if (any) {
 #pragma unroll 1
-                                for (int i = 0; i < d; i += 16) {
-                                    float o[16];
-                                    uint32_t w[16];
-                                    tmem_load16(tO + i, o);
-#pragma unroll
-                                    for (int k = 0; k < 16; ++k) w[k] = __float_as_uint(o[k] * f);
-                                    tmem_store16(tO + i, w);
-                                }
-#pragma unroll 1
-                            for (int i = 0; i < c; ++i) {
-                                float p[16];
+                            for (int c = o_begin; c < o_end; c += 16) {
+                                float o[16];
                                 uint32_t w[16];
-                                tmem_load16(tS + i * 16, p);
+                                tmem_load16(tO + c, o);
 #pragma unroll
-                                for (int k = 0; k < 16; ++k) w[k] = scale16<kNarrow>(__float_as_uint(p[k]), f);
-                                tmem_store16(tS + i * 16, w);
+                                for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(o[i] * by);
+                                tmem_store16(tO + c, w);
                             }
                             tmem_store_wait();
-                            relative(-ref);
                         }
-                        uint32_t w[16];
+                        __syncwarp();
+                    }
+                    any = true;
+                    const uint64_t f2 = pack2(factor, factor), b2 = pack2(-ref, -ref);
+                    uint64_t s2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
+                    // the loops are not unrolled, so that the code stays near
+#pragma unroll 1
+                    for (int c = 0; c < 64; c += kAttnCols<kKind>) {
+                        float x[kAttnCols<kKind>];
+                        uint32_t w[kAttnCols<kKind> / 2];
+                        scores(c, x);
 #pragma unroll
-                        for (int i = 0; i < 32; i += 4) {
+                        for (int i = 0; i < kAttnCols<kKind>; i += 4) {
                             float e[4];
+                            unpack2(fma2(pack2(x[i], x[i + 1]), f2, b2), e[0], e[1]);
+                            unpack2(fma2(pack2(x[i + 2], x[i + 3]), f2, b2), e[2], e[3]);
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) e[k] = ex2_approx(x[i + k]);
-                            uint64_t e0 = pack2(e[0], e[1]), e1 = pack2(e[2], e[3]);
+                            for (int k = 0; k < 4; ++k) e[k] = ex2_approx(e[k]);
+                            const uint64_t e0 = pack2(e[0], e[1]), e1 = pack2(e[2], e[3]);
                             s2[0] = add2(s2[0], e0);
                             s2[1] = add2(s2[1], e1);
                             if constexpr (kNarrow) {
-                                const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(fv + c * 32 + i);
-                                unpack2(mul2(e0, f.x), e[0], e[1]);
-                                unpack2(mul2(e1, f.y), e[2], e[3]);
+                                const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(fv + c + i);
+                                unpack2(mul2(e0, v.x), e[0], e[1]);
+                                unpack2(mul2(e1, v.y), e[2], e[3]);
                             }
                             w[i >> 1] = pack16<kNarrow>(e[0], e[1]);
                             w[(i >> 1) + 1] = pack16<kNarrow>(e[2], e[3]);
                         }
-                        tmem_store16(tS + c * 16, w);
+                        attn_write<kAttnCols<kKind> / 2>(tS + c / 2, w);
                     }
-                    any = true;
                     float s0, s1;
                     unpack2(add2(s2[0], s2[1]), s0, s1);
                     sum += s0 + s1;
@@ -388,31 +389,34 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                     // V of positions that no row sees, or that hold NaN or infinities that only some see, must not meet a
                     // weight of zero in the product: zeros here, the latter added to the rows that see them at the end
                     const uint32_t i = seq + jj, s = P.k_slots + i % P.v_slots;
-                    if (!wait(&S.full[s], i / P.v_slots & 1u)) break;
-                    if (start + row >= u.first || row >= valid) {
+                    wait(&S.full[s], i / P.v_slots & 1u);
+                    if ((row & 1) == half && (start + row >= u.first || row >= valid)) {
                         if (attn_clean_values(ring + (size_t)s * tile_bytes + row * 128, row, P.chunks, row < valid))
                             S.bad_value[units % kAttnUnitFlags] = 1;
                     }
                     fence_async_smem();
                 }
                 if (merged) {                    // the second group's O of the unit before has been read
-                    if (!wait(&S.merge_done, (merges - 1) & 1u)) break;
+                    wait(&S.merge_done, (merges - 1) & 1u);
                     merged = false;
                 }
                 tc_fence_before();
                 arrive(&S.p_full[t]);
             }
-            if (!ok || !wait(&S.o_full[t], units & 1u)) break;
+            if (left) { ok = false; break; }                                // both warps
+            wait(&S.o_full[t], units & 1u);
             tc_fence_after();
             // Everything of this unit has been multiplied: Q of the next one takes the place of this one's.
-            AttnUnit done = u;
+            const AttnUnit done = u;
             have = it.next(P, u);
-            const int done_count = count;
             if (have) prepare_q(u);
-            const bool join = !done.pair && done_count > 1;
+            const bool join = !done.pair && count > 1;
+            if (merged) { wait(&S.merge_done, (merges - 1) & 1u); merged = false; }
+            S.of_half[t][half][row] = sum;
+            if (vote(!ok)) { ok = false; break; }
+            sum += S.of_half[t][half ^ 1][row];
             if (join && t == 1) {
-                if (merged) { if (!wait(&S.merge_done, (merges - 1) & 1u)) break; merged = false; }
-                S.second[row] = make_float2(ref, sum);
+                if (!half) S.second[row] = make_float2(ref, sum);
                 tc_fence_before();
                 arrive(&S.merge_ready);
                 ++merges;
@@ -420,8 +424,9 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
             } else if (done.pair || t == 0) {
                 float f0 = 1.f, f1 = 0.f;
                 if (join) {
-                    if (!wait(&S.merge_ready, merges & 1u)) break;
+                    wait(&S.merge_ready, merges & 1u);
                     ++merges;
+                    if (vote(!ok)) { ok = false; break; }
                     tc_fence_after();
                     const float2 o = S.second[row];
                     const float top = fmaxf(ref, o.x);
@@ -437,7 +442,8 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                 const long long out_row = done.row0 + node;
                 const float inverse = 1.f / sum;
                 if (warp_live) {
-                    for (int c = 0; c < d; c += 16) {
+#pragma unroll 1
+                    for (int c = o_begin; c < o_end; c += 16) {
                         float o[16];
                         __syncwarp();
                         tmem_load16(tO + c, o);
@@ -463,7 +469,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                             for (int i = 0; i < 4; ++i) dst[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
                         }
                     }
-                    if (live) {
+                    if (live && !half) {
                         if (!whole) P.part_stats[part] = make_float2(ref, sum);
                         else if (P.out_lse) P.out_lse[out_row * P.q_heads + head] = (ref + log2f(sum)) * 0.6931471805599453f;
                     }
@@ -471,14 +477,14 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                 __syncwarp();
                 if (join) { tc_fence_before(); arrive(&S.merge_done); }
             }
-            seq += done_count;
+            seq += count;
             ++units;
         }
         if (!ok && lane == 0) give_up();
     } else {
         // ---------------- 8-bit tiles to 16 bits --------------------------------------------------------------
         if constexpr (kNarrow) {
-            const int ct = tid - (kSoftmaxWarps + 2) * 32;
+            const int ct = tid - (kRowWarps + 2) * 32;
             // scales of position ct of a tile
             float k_now = 0.f, v_now = 0.f;
             bool node = false;
@@ -506,7 +512,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                 const uint32_t bits = __ballot_sync(0xffffffffu, bad);
                 if (lane == 0) scales.bad[at][ct >> 5] = bits;
             };
-            if (!attn_widen<kKind, kAttnConverters * 32>(P, it, ct, raw, ring, tile_bytes, S.raw_full, S.raw_empty, S.full, S.empty, S.bad_value, abort_flag, load_scales,
+            if (!attn_widen<kKind, kAttnConverters * 32>(P, it, ct, 0, 1, raw, ring, tile_bytes, S.raw_full, S.raw_empty, S.full, S.empty, S.bad_value, abort_flag, load_scales,
                                         store_scales) && lane == 0)
                 give_up();
         }
@@ -654,8 +660,9 @@ static int attn_launch(AttnParams& P, const CUtensorMap& k, const CUtensorMap& v
     if (slots > kAttnMaxSlots) slots = kAttnMaxSlots;
     P.k_slots = slots / 2;
     P.v_slots = slots - P.k_slots;
-    P.raw_slots = kNarrow ? (kAttnNarrowBytes - (P.q_tiles + slots) * tile) / (kAttnTile * P.c.head_dim) : 0;
-    if (P.raw_slots > kAttnMaxRaw) P.raw_slots = kAttnMaxRaw;
+    const int raw = (kAttnNarrowBytes - (P.q_tiles + slots) * tile) / (kAttnTile * P.c.head_dim), most = raw < kAttnMaxRaw ? raw : kAttnMaxRaw;
+    P.raw_k = kNarrow ? most / 2 : 0;
+    P.raw_v = kNarrow ? most - P.raw_k : 0;
     KernelTimerScope timer(DSPARK_K_TREE_ATTENTION, s);
     launch_pdl(attn_kernel<kKind>, dim3((unsigned)sms), dim3(kAttnThreads<kKind>), kSmem, s, P, k, v);
     return launch_status();

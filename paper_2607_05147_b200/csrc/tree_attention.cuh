@@ -13,14 +13,13 @@ constexpr int kAttnSms = 148;                    // a B200's: the workspace's si
 constexpr int kAttnTile = 128;                   // rows of a row tile, positions of a cache tile
 constexpr int kChunkBytes = kAttnTile * 128;     // 64 columns of 16 bits of a tile: 128 rows of 128 bytes, swizzled
 constexpr int kAttnMaxSlots = 12, kAttnMaxRaw = 8, kAttnScaleTiles = 4;
-constexpr int kAttnRingBytes = 7 * 2 * kChunkBytes;           // 224 KB: Q and the ring
+constexpr int kAttnRingBytes = 6 * 2 * kChunkBytes;           // 192 KB: Q and the rings
 constexpr int kAttnNarrowBytes = 208 * 1024;                  // with 8-bit caches (4 KB of scales beside it)
 constexpr float kAttnLog2e = 1.4426950408889634f;
 constexpr float kAttnLazy = 8.f;                 // O is scaled when the maximum rises by more than 2^8
 constexpr float kAttnNarrowOffset = 7.f;         // fp16 weights: up to 2^(7 + 8) of 65 504, down to 2^-31 of the largest
 constexpr float kAttnUnset = -1e38f;              // a reference that every score is above
 constexpr float kAttnLeastFactor = 1e-20f;       // of a score: -infinity times it is -infinity, a score times it next to nothing
-constexpr int kSoftmaxWarps = 8;
 constexpr int kAttnUnitFlags = 8;               // units of one CTA that are under way at a time: at most four
 
 enum AttnKind { kAttnWide = 0, kAttnI8 = 1, kAttnE4M3 = 2 };
@@ -37,7 +36,8 @@ struct AttnParams {
     int tile_nodes, unit_nodes;                  // nodes of a row tile, of a unit
     int q_tiles;                                 // row tiles of a unit: 1 or 2
     int chunks;                                  // of 64 columns: 1 or 2
-    int k_slots, v_slots, raw_slots;             // rings: 16-bit tiles of K, of V (behind those of K), 8-bit tiles of both in turn
+    int k_slots, v_slots;                        // rings: 16-bit tiles of K, of V (behind those of K)
+    int raw_k, raw_v;                            // 8-bit tiles, the same way
     int tile_tokens, page_tiles, page_boxes;     // positions of a box; cache tiles of a page (pages above 128) ; boxes of a tile
     int part_rows;                               // rows of a partial result
     int32_t* dev_status;
@@ -115,7 +115,7 @@ __device__ __forceinline__ long long attn_head_tiles(const AttnParams& P, int fi
 
 // This CTA's run of the list, and the unit that it divides first (for the joining kernel).  All threads of the CTA; meets them
 // twice, so that what was set up before is seen by all.
-struct AttnList { long long scan[24], start_at; int start_r; };
+struct AttnList { long long scan[32], start_at; int start_r; };
 template <int kThreads>
 __device__ __forceinline__ AttnIter attn_begin(const AttnParams& P, AttnList& S)
 {
@@ -252,6 +252,23 @@ __device__ __forceinline__ void tmem_store16(uint32_t taddr, const uint32_t (&v)
                  ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
                    "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
 }
+template <int kCols>
+__device__ __forceinline__ void attn_read(uint32_t addr, float (&v)[kCols])
+{
+    if constexpr (kCols == 8)
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n\ttcgen05.wait::ld.sync.aligned;"
+                     : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]) : "r"(addr) : "memory");
+    else if constexpr (kCols == 16) tmem_load16(addr, v);
+    else { tmem_load32_issue(addr, v); tmem_load_wait(v); }
+}
+template <int kCols>
+__device__ __forceinline__ void attn_write(uint32_t addr, const uint32_t (&v)[kCols])
+{
+    if constexpr (kCols == 8)
+        asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                     ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+    else tmem_store16(addr, v);
+}
 __device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 template <bool kHalf>
 __device__ __forceinline__ uint32_t pack16(float lo, float hi)
@@ -261,14 +278,34 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi)
     else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-// a pair of 16-bit floats times a power of two
-template <bool kHalf>
-__device__ __forceinline__ uint32_t scale16(uint32_t w, float f)
+// 32 columns of scores: -infinity where `on` has no bit, NaN where `bad` has one
+__device__ __forceinline__ void attn_hide(uint32_t addr, uint32_t on, uint32_t bad)
 {
-    if (!kHalf) return pack16<false>(bf16lo(w) * f, bf16hi(w) * f);
-    float a, b;
-    asm("{\n\t.reg .b16 x, y;\n\tmov.b32 {x, y}, %2;\n\tcvt.f32.f16 %0, x;\n\tcvt.f32.f16 %1, y;\n\t}" : "=f"(a), "=f"(b) : "r"(w));
-    return pack16<true>(a * f, b * f);
+#pragma unroll 1
+    for (int c = 0; c < 32; c += 16) {
+        float s[16];
+        uint32_t x[16];
+        tmem_load16(addr + c, s);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = !(on >> (c + i) & 1u) ? 0xff800000u : (bad >> (c + i) & 1u) ? 0x7fffffffu : __float_as_uint(s[i]);
+        tmem_store16(addr + c, x);
+    }
+    tmem_store_wait();
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// whether one of the kThreads threads that meet at barrier `id` says so
+template <int kThreads>
+__device__ __forceinline__ bool barrier_any(int id, bool x)
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"((uint32_t)x), "r"(id), "n"(kThreads) : "memory");
+    return r != 0;
 }
 // the largest of those of four scales that are finite and asked for
 __device__ __forceinline__ float attn_finite_max(float4 x, uint32_t of, float top)
@@ -308,7 +345,7 @@ struct RingPlace {
     __device__ __forceinline__ void next(int slots) { if (++s == slots) { s = 0; ph ^= 1u; } }
 };
 
-// The producer warp: K and V tiles, K before V, a lane a box; 16-bit ones into their rings, 8-bit ones into one.
+// The producer warp: K and V tiles into their rings, K before V, a lane a box.
 template <bool kNarrow>
 __device__ __forceinline__ void attn_produce(const AttnParams& P, AttnIter it, const CUtensorMap& map_k, const CUtensorMap& map_v, unsigned char* ring,
                                              uint64_t* full, uint64_t* empty, volatile int* abort_flag)
@@ -316,8 +353,8 @@ __device__ __forceinline__ void attn_produce(const AttnParams& P, AttnIter it, c
     const int lane = threadIdx.x & 31, d = P.c.head_dim;
     const int row_bytes = kNarrow ? d : 128, copies = kNarrow ? 1 : P.chunks, slot_bytes = kNarrow ? kAttnTile * d : P.chunks * kChunkBytes;
     const int box = lane / copies, chunk = lane - box * copies;
-    const int slots[2] = {kNarrow ? P.raw_slots : P.k_slots, kNarrow ? P.raw_slots : P.v_slots};
-    RingPlace at[2];                             // 8-bit tiles: the first for both
+    const int k_slots = kNarrow ? P.raw_k : P.k_slots, v_slots = kNarrow ? P.raw_v : P.v_slots;
+    RingPlace at[2];
     bool ok = true, bad_page = false;
     AttnUnit u;
     while (ok && !*abort_flag && it.next(P, u)) {
@@ -334,8 +371,8 @@ __device__ __forceinline__ void attn_produce(const AttnParams& P, AttnIter it, c
             }
 #pragma unroll
             for (int kv = 0; kv < 2; ++kv) {
-                RingPlace& place = at[kNarrow ? 0 : kv];
-                const int s = place.s + (!kNarrow && kv ? P.k_slots : 0);
+                RingPlace& place = at[kv];
+                const int s = place.s + (kv ? k_slots : 0);
                 ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(&empty[s], place.ph ^ 1u));
                 if (!ok) break;
                 if (lane == 0) mbar_arrive_expect_tx(&full[s], (uint32_t)(boxes * copies * P.tile_tokens * row_bytes));
@@ -343,53 +380,82 @@ __device__ __forceinline__ void attn_produce(const AttnParams& P, AttnIter it, c
                 if (box < boxes)
                     tma_load_4d(ring + (size_t)s * slot_bytes + chunk * kChunkBytes + box * P.tile_tokens * row_bytes, kv ? &map_v : &map_k,
                                 chunk * 64, y, u.head, page, &full[s]);
-                place.next(slots[kv]);
+                place.next(kv ? v_slots : k_slots);
             }
         }
     }
     if (bad_page) atomicOr(P.dev_status, DSPARK_DEV_BAD_PAGE);
     if (!ok && lane == 0) { atomicOr(P.dev_status, DSPARK_DEV_TIMEOUT); *abort_flag = 1; }
     // Leave only after every copy has landed: its slot has been announced as free, or, where somebody gave up, is full.
-    for (int kv = 0; kv < (kNarrow ? 1 : 2); ++kv)
-        for (int i = 0; i < slots[kv]; ++i) {
-            const int s = at[kv].s + (kv ? P.k_slots : 0);
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv)
+        for (int i = 0; i < (kv ? v_slots : k_slots); ++i) {
+            const int s = at[kv].s + (kv ? k_slots : 0);
             if (!*abort_flag) mbar_wait_bounded(&empty[s], at[kv].ph ^ 1u);
             else mbar_wait_bounded(&full[s], at[kv].ph ^ 1u, 1u << 16);
-            at[kv].next(slots[kv]);
+            at[kv].next(kv ? v_slots : k_slots);
         }
 }
 
-// kThreads threads: 8-bit tiles of one ring as fp16 tiles of another, as the products read them.  tile(unit, j) is called before
-// the waits for a tile's K, ready(number) between them and the work.  False: a wait ran out.
-template <int kKind, int kThreads, typename Tile, typename Ready>
-__device__ __forceinline__ bool attn_widen(const AttnParams& P, AttnIter it, int ct, const unsigned char* raw, unsigned char* ring, int tile_bytes,
-                                           uint64_t* raw_full, uint64_t* raw_empty, uint64_t* full, uint64_t* empty, volatile int* bad_value,
-                                           volatile int* abort_flag, Tile tile, Ready ready)
+// Where 16 bytes x of an 8-bit tile come from and go to (and the next 16 beside).  Eight lanes store to eight different places of a
+// line of 128 bytes: the pieces of two neighbouring positions, which the swizzle parts by an odd number of places; with 128
+// components one position's lie in the other chunk, so that the loads' banks differ too.
+__device__ __forceinline__ void widen_place(int x, int d, int& token, int& from, int& to)
 {
-    constexpr int kMost = kAttnTile * kAttnMaxDim / 16 / kThreads;          // 16-byte pieces of one thread
-    const int lane = threadIdx.x & 31, d = P.c.head_dim, pieces = d / 16;
-    int number = 0, unit = 0;
-    RingPlace at[2], from_raw;
-    // Where a thread's pieces come from and go to.  Eight lanes store to eight different places of a line of 128 bytes: the pieces of
-    // two neighbouring positions, which the swizzle parts by an odd number of places; with 128 components one position's lie in
-    // the other chunk, so that the loads' banks differ too.
-    int from[kMost], to[kMost], token[kMost];
-#pragma unroll
-    for (int i = 0; i < kMost; ++i) {
-        const int x = i * kThreads + ct;
-        int piece;
-        if (pieces == 8) {
-            const int odd = x >> 2 & 1;
-            token[i] = (x >> 4) * 2 + odd;
-            piece = ((x >> 3 & 1) ^ odd) * 4 + (x & 3);
-        } else {
-            token[i] = x / pieces;
-            piece = x - token[i] * pieces;
-        }
-        from[i] = token[i] * d + piece * 16;
-        to[i] = (piece >> 2) * kChunkBytes + token[i] * 128 + ((((piece & 3) * 2) ^ (token[i] & 7)) << 4);
-        if (x >= kAttnTile * pieces) token[i] = -1;
+    const int pieces = d / 16;
+    int piece;
+    if (pieces == 8) {
+        const int odd = x >> 2 & 1;
+        token = (x >> 4) * 2 + odd;
+        piece = ((x >> 3 & 1) ^ odd) * 4 + (x & 3);
+    } else {
+        token = x / pieces;
+        piece = x - token * pieces;
     }
+    from = token * d + piece * 16;
+    to = (piece >> 2) * kChunkBytes + token * 128 + ((((piece & 3) * 2) ^ (token & 7)) << 4);
+}
+template <int kKind>
+__device__ __forceinline__ void widen16(uint4 w, unsigned char* dst, int to)
+{
+    const uint2 a = widen4<kKind>(w.x), b = widen4<kKind>(w.y), c = widen4<kKind>(w.z), e = widen4<kKind>(w.w);
+    *reinterpret_cast<uint4*>(dst + to) = make_uint4(a.x, a.y, b.x, b.y);
+    *reinterpret_cast<uint4*>(dst + (to ^ 16)) = make_uint4(c.x, c.y, e.x, e.y);
+}
+// A tile by kThreads threads; of 64 or 128 components (kDim) a thread's pieces are a fixed number of positions apart.
+template <int kKind, int kThreads, int kDim>
+__device__ __forceinline__ void widen_tile(const unsigned char* src, unsigned char* dst, int ct, int from0, int to0, int d)
+{
+    if constexpr (kDim > 0) {
+        constexpr int kPieces = kAttnTile * kDim / 16 / kThreads, kApart = kThreads * 16 / kDim, kBatch = kPieces < 4 ? kPieces : 4;
+#pragma unroll
+        for (int i0 = 0; i0 < kPieces; i0 += kBatch) {
+            uint4 w[kBatch];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) w[i] = *reinterpret_cast<const uint4*>(src + from0 + (i0 + i) * kApart * kDim);
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) widen16<kKind>(w[i], dst, to0 + (i0 + i) * kApart * 128);
+        }
+    } else {
+#pragma unroll 2
+        for (int x = ct; x < kAttnTile * d / 16; x += kThreads) {
+            int token, from, to;
+            widen_place(x, d, token, from, to);
+            widen16<kKind>(*reinterpret_cast<const uint4*>(src + from), dst, to);
+        }
+    }
+}
+// kThreads threads: 8-bit tiles as fp16 tiles, as the products read them; K and V (kv 0 and 1), or one of them.  tile(unit, j) is
+// called before the waits for a tile's K, ready(number) between them and the work.  False: a wait ran out.
+template <int kKind, int kThreads, typename Tile, typename Ready>
+__device__ __forceinline__ bool attn_widen(const AttnParams& P, AttnIter it, int ct, int kv_first, int kv_last, const unsigned char* raw,
+                                           unsigned char* ring, int tile_bytes, uint64_t* raw_full, uint64_t* raw_empty, uint64_t* full,
+                                           uint64_t* empty, volatile int* bad_value, volatile int* abort_flag, Tile tile, Ready ready)
+{
+    const int lane = threadIdx.x & 31, d = P.c.head_dim;
+    int number = 0, unit = 0, token0, from0, to0;
+    widen_place(ct, d, token0, from0, to0);
+    RingPlace at[2], from_raw[2];
     AttnUnit u;
     while (!*abort_flag && it.next(P, u)) {
         for (int j = u.j0; j < u.j1; ++j, ++number) {
@@ -397,44 +463,46 @@ __device__ __forceinline__ bool attn_widen(const AttnParams& P, AttnIter it, int
             attn_tile_at(P, j, start, len);
             const int valid = min(len, u.length - start), tree = u.first - start;   // positions from `tree` on are nodes
             tile(u, j);
-            for (int kv = 0; kv < 2; ++kv) {
-                RingPlace& place = at[kv];
-                const int s = place.s + (kv ? P.k_slots : 0), rs = from_raw.s;
-                if (!__all_sync(0xffffffffu, mbar_wait_bounded(&raw_full[rs], from_raw.ph) && mbar_wait_bounded(&empty[s], place.ph ^ 1u))) return false;
+            for (int kv = kv_first; kv <= kv_last; ++kv) {
+                const int s = kv ? P.k_slots + at[1].s : at[0].s, rs = kv ? P.raw_k + from_raw[1].s : from_raw[0].s;
+                const uint32_t ph = kv ? at[1].ph : at[0].ph, rph = kv ? from_raw[1].ph : from_raw[0].ph;
+                if (!__all_sync(0xffffffffu, mbar_wait_bounded(&empty[s], ph ^ 1u) && mbar_wait_bounded(&raw_full[rs], rph))) return false;
                 if (kv == 0) ready(number);
                 const unsigned char* src = raw + (size_t)rs * kAttnTile * d;
                 unsigned char* dst = ring + (size_t)s * tile_bytes;
-                uint4 w[kMost];
+                if (d == 128) widen_tile<kKind, kThreads, 128>(src, dst, ct, from0, to0, d);
+                else if (d == 64) widen_tile<kKind, kThreads, 64>(src, dst, ct, from0, to0, d);
+                else widen_tile<kKind, kThreads, 0>(src, dst, ct, from0, to0, d);
+                if (valid < kAttnTile || (kKind == kAttnE4M3 && kv && tree < kAttnTile)) {
+                    // positions that do not exist: zeros; a NaN among the nodes' values of V: zero here and back in the rows that see
+                    // it (attn_bad_values).  Every thread looks at what it has written.
+#pragma unroll 1
+                    for (int x = ct; x < kAttnTile * d / 16; x += kThreads) {
+                        int token, from, to;
+                        widen_place(x, d, token, from, to);
+#pragma unroll 1
+                        for (int k = 0; k < 2; ++k) {
+                            uint4* p = reinterpret_cast<uint4*>(dst + (to ^ (k * 16)));
+                            if (token >= valid) *p = make_uint4(0, 0, 0, 0);
+                            else if (kKind == kAttnE4M3 && kv && token >= tree) {
+                                uint4 y = *p;
+                                uint32_t* h[4] = {&y.x, &y.y, &y.z, &y.w};
+                                bool bad = false;
 #pragma unroll
-                for (int i = 0; i < kMost; ++i)
-                    if (token[i] >= 0) w[i] = *reinterpret_cast<const uint4*>(src + from[i]);
-#pragma unroll
-                for (int i = 0; i < kMost; ++i) {
-                    if (token[i] < 0) continue;
-                    uint2 a = widen4<kKind>(w[i].x), b = widen4<kKind>(w[i].y), c = widen4<kKind>(w[i].z), e = widen4<kKind>(w[i].w);
-                    if (valid < kAttnTile && token[i] >= valid) a = b = c = e = make_uint2(0, 0);
-                    if (kKind == kAttnE4M3 && kv && token[i] >= tree) {
-                        // a NaN among the nodes' values of V: zero here and back in the rows that see it (attn_bad_values)
-                        uint32_t h[8] = {a.x, a.y, b.x, b.y, c.x, c.y, e.x, e.y};
-                        bool bad = false;
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            if ((h[k] & 0x7c00u) == 0x7c00u) { h[k] &= 0xffff0000u; bad = true; }
-                            if ((h[k] & 0x7c000000u) == 0x7c000000u) { h[k] &= 0xffffu; bad = true; }
-                        }
-                        if (bad) {
-                            a = make_uint2(h[0], h[1]); b = make_uint2(h[2], h[3]); c = make_uint2(h[4], h[5]); e = make_uint2(h[6], h[7]);
-                            bad_value[unit % kAttnUnitFlags] = 1;
+                                for (int i = 0; i < 4; ++i) {
+                                    if ((*h[i] & 0x7c00u) == 0x7c00u) { *h[i] &= 0xffff0000u; bad = true; }
+                                    if ((*h[i] & 0x7c000000u) == 0x7c000000u) { *h[i] &= 0xffffu; bad = true; }
+                                }
+                                if (bad) { *p = y; bad_value[unit % kAttnUnitFlags] = 1; }
+                            }
                         }
                     }
-                    *reinterpret_cast<uint4*>(dst + to[i]) = make_uint4(a.x, a.y, b.x, b.y);
-                    *reinterpret_cast<uint4*>(dst + (to[i] ^ 16)) = make_uint4(c.x, c.y, e.x, e.y);
                 }
                 fence_async_smem();
                 __syncwarp();
                 if (lane == 0) { mbar_arrive(&raw_empty[rs]); mbar_arrive(&full[s]); }
-                from_raw.next(P.raw_slots);
-                place.next(kv ? P.v_slots : P.k_slots);
+                if (kv) { at[1].next(P.v_slots); from_raw[1].next(P.raw_v); }
+                else { at[0].next(P.k_slots); from_raw[0].next(P.raw_k); }
             }
         }
         ++unit;

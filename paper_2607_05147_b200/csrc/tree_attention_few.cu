@@ -23,6 +23,7 @@
 
 namespace dspark {
 
+constexpr int kSoftmaxWarps = 8;
 constexpr int kFewSmem = 217 * 1024;             // two of P, Q, the ring; tables beside it
 constexpr int kFewPBytes = kAttnTile * 128;      // P^T of one tile: a line of 128 bytes a position
 constexpr float kFewUnset = 1e38f;               // less a reference that every score is above
@@ -44,30 +45,10 @@ struct FewTables {
 };
 
 // whether one of a group's 128 threads says so
-__device__ __forceinline__ bool group_any(int group, bool x)
-{
-    uint32_t r;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-                 : "=r"(r) : "r"((uint32_t)x), "r"(group + 1) : "memory");
-    return r != 0;
-}
+__device__ __forceinline__ bool group_any(int group, bool x) { return barrier_any<128>(group + 1, x); }
 __device__ __forceinline__ void group_sync(int group) { asm volatile("barrier.cta.sync %0, 128;" ::"r"(group + 1) : "memory"); }
-template <int kCols> __device__ __forceinline__ void tmem_read(uint32_t addr, float (&v)[kCols])
-{
-    if constexpr (kCols == 8)
-        asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n\ttcgen05.wait::ld.sync.aligned;"
-                     : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]) : "r"(addr) : "memory");
-    else if constexpr (kCols == 16) tmem_load16(addr, v);
-    else { tmem_load32_issue(addr, v); tmem_load_wait(v); }
-}
-__device__ __forceinline__ void tmem_write8(uint32_t addr, const float (&v)[8])
-{
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
-                 ::"r"(addr), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
-}
-
 // eight warps widen 8-bit tiles where their registers leave the softmax enough
-template <int kKind, int kN> constexpr int kFewConverters = kKind == kAttnWide ? 0 : kN == 64 ? 4 : 8;
+template <int kKind, int kN> constexpr int kFewConverters = kKind == kAttnWide ? 0 : kN == 64 ? 4 : 8;   // eight: four for K, four for V
 template <int kKind, int kN> constexpr int kFewThreads = (kSoftmaxWarps + 3 + kFewConverters<kKind, kN>) * 32;
 
 template <int kKind, int kN>
@@ -76,7 +57,8 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
 {
     constexpr bool kNarrow = kKind != kAttnWide;
     constexpr int kThreads = kFewThreads<kKind, kN>, kProducer = kSoftmaxWarps, kIssuer = kSoftmaxWarps + 1, kIssuerO = kSoftmaxWarps + 2;
-    constexpr int kWarps = kFewConverters<kKind, kN>, kC = kN / 2;               // kC: columns of a group
+    constexpr int kWarps = kFewConverters<kKind, kN>, kOf = kNarrow ? 4 : 1, kC = kN / 2;    // kOf: warps that make one 16-bit tile
+                   // kC: columns of a group
     constexpr uint32_t kO = 128;                 // columns of tensor memory: S^T at 0 and 64, O^T at 128
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);   // swizzle atoms: 1 KB
@@ -91,8 +73,8 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
     unsigned char* raw = ring + slots * tile_bytes;
 
     if (tid == 0) {
-        for (int s = 0; s < slots; ++s) { mbar_init(&S.full[s], kNarrow ? kWarps : 1); mbar_init(&S.empty[s], 1); }
-        for (int s = 0; s < P.raw_slots; ++s) { mbar_init(&S.raw_full[s], 1); mbar_init(&S.raw_empty[s], kNarrow ? kWarps : 1); }
+        for (int s = 0; s < slots; ++s) { mbar_init(&S.full[s], kOf); mbar_init(&S.empty[s], 1); }
+        for (int s = 0; s < P.raw_k + P.raw_v; ++s) { mbar_init(&S.raw_full[s], 1); mbar_init(&S.raw_empty[s], kOf); }
         mbar_init(&S.q_full, kSoftmaxWarps); mbar_init(&S.q_empty, 1);
         for (int t = 0; t < 2; ++t) { mbar_init(&S.s_full[t], 1); mbar_init(&S.p_full[t], kSoftmaxWarps); mbar_init(&S.o_done[t], 1); mbar_init(&S.mma_done[t], 1); }
         for (int i = 0; i < kAttnUnitFlags; ++i) S.bad_value[i] = 0;
@@ -336,10 +318,10 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
 #pragma unroll 1
                         for (int c0 = 0; c0 < kC; c0 += 8) {
                             float s[8];
-                            tmem_read<8>(tS + c0, s);
+                            attn_read<8>(tS + c0, s);
 #pragma unroll
                             for (int c = 0; c < 8; ++c) s[c] = !(seen >> (c0 + c) & 1) ? -INFINITY : bad ? NAN : s[c];
-                            tmem_write8(tS + c0, s);
+                            attn_write<8>(tS + c0, reinterpret_cast<const uint32_t (&)[8]>(s));
                         }
                         tmem_store_wait();
                         if (bad) { k_scale = 1.f; v_scale = 0.f; above = -kAttnNarrowOffset; }
@@ -355,7 +337,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                         }
                     };
                     float y[kC], tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                    tmem_read(tS, y);
+                    attn_read<kC>(tS, y);
                     relative(y);
 #pragma unroll
                     for (int c = 0; c < kC; c += 2) tops[c / 2 % 4] = fmaxf(tops[c / 2 % 4], fmaxf(y[c], y[c + 1]));
@@ -369,7 +351,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
 #pragma unroll 1
                         for (int c0 = 0; c0 < kC; c0 += 8) {
                             float s[8], mine = -INFINITY;
-                            tmem_read<8>(tS + c0, s);
+                            attn_read<8>(tS + c0, s);
 #pragma unroll
                             for (int c = 0; c < 8; ++c) {
                                 const float z = warp_max_f32(s[c] * (kNarrow ? k_scale * T.q[units & 1u][row0 + c0 + c] : k_scale) + above);
@@ -394,14 +376,14 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
 #pragma unroll 1
                             for (int c0 = 0; c0 < kC; c0 += 8) {
                                 float o[8];
-                                tmem_read<8>(tO + c0, o);
+                                attn_read<8>(tO + c0, o);
 #pragma unroll
                                 for (int c = 0; c < 8; ++c) o[c] *= T.scale[row0 + c0 + c];
-                                tmem_write8(tO + c0, o);
+                                attn_write<8>(tO + c0, reinterpret_cast<const uint32_t (&)[8]>(o));
                             }
                             tmem_store_wait();
                         }
-                        tmem_read(tS, y);
+                        attn_read<kC>(tS, y);
                         relative(y);
                     }
                     uint32_t w[kC / 2];
@@ -489,7 +471,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
 #pragma unroll 1
                 for (int h = 0; h < mine; h += 8) {
                     float o[8];
-                    tmem_read<8>(tO + h, o);
+                    attn_read<8>(tO + h, o);
 #pragma unroll
                     for (int c = 0; c < 8; ++c) {
                         if (h + c < mine && pos < d) {
@@ -519,11 +501,13 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
         }
         if (!ok && lane == 0) give_up();
     } else {
-        if constexpr (kNarrow)
-            if (!attn_widen<kKind, kWarps * 32>(P, it, tid - (kSoftmaxWarps + 3) * 32, raw, ring, tile_bytes, S.raw_full, S.raw_empty, S.full, S.empty,
-                                                S.bad_value, abort_flag, [](const AttnUnit&, int) {}, [](int) {}) &&
+        if constexpr (kNarrow) {
+            const int ct = tid - (kSoftmaxWarps + 3) * 32, kv = kWarps == 8 ? ct >> 7 : 0;
+            if (!attn_widen<kKind, 128>(P, it, ct & 127, kv, kWarps == 8 ? kv : 1, raw, ring, tile_bytes, S.raw_full, S.raw_empty, S.full, S.empty,
+                                        S.bad_value, abort_flag, [](const AttnUnit&, int) {}, [](int) {}) &&
                 lane == 0)
                 give_up();
+        }
     }
     tc_fence_before();
     __syncthreads();
@@ -542,12 +526,14 @@ static int few_launch(AttnParams& P, const CUtensorMap& k, const CUtensorMap& v,
     const int tile = P.chunks * kChunkBytes;
     // a chunk is left behind the ring: with up to 64 components the products read one past a tile (and nobody its results)
     int room = kFewSmem - 2 * kFewPBytes - P.chunks * kN * 128 - (P.chunks == 1 ? kChunkBytes : 0);
-    // V tiles stay longer than K tiles: until their weights are there
-    const int slots = kKind != kAttnWide ? 4 : room / tile < kAttnMaxSlots ? room / tile : kAttnMaxSlots;
+    // V tiles stay longer than K tiles: until their weights are there.  8-bit caches: few 16-bit tiles, so that many 8-bit ones can
+    // be on their way.
+    const int slots = kKind != kAttnWide ? (P.chunks == 2 ? 3 : 4) : room / tile < kAttnMaxSlots ? room / tile : kAttnMaxSlots;
     P.k_slots = slots / 2;
     P.v_slots = slots - P.k_slots;
-    room -= slots * tile;
-    P.raw_slots = kKind == kAttnWide ? 0 : room / (kAttnTile * P.c.head_dim) < kAttnMaxRaw ? room / (kAttnTile * P.c.head_dim) : kAttnMaxRaw;
+    const int raw = (room - slots * tile) / (kAttnTile * P.c.head_dim), most = raw < kAttnMaxRaw ? raw : kAttnMaxRaw;
+    P.raw_k = kKind == kAttnWide ? 0 : most / 2;
+    P.raw_v = kKind == kAttnWide ? 0 : most - P.raw_k;
     KernelTimerScope timer(DSPARK_K_TREE_ATTENTION, s);
     launch_pdl(attn_few_kernel<kKind, kN>, dim3((unsigned)sms), dim3(kFewThreads<kKind, kN>), kSmem, s, P, k, v);
     return launch_status();
