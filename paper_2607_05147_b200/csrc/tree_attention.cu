@@ -305,12 +305,15 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                     for (int w = 0; w < 2; ++w) attn_hide(tS + w * 32, half ? seen[2 + w] : seen[w], 0u);
                 }
                 if (warp_live) {
-                    // 32 scores: from tensor memory, with an 8-bit cache times K's scales
-                    auto scores = [&](int c, float (&x)[kAttnCols<kKind>]) {
-                        attn_read<kAttnCols<kKind>>(tS + c, x);
+                    // scores from tensor memory, with an 8-bit cache times K's scales; the next ones are asked for meanwhile
+                    constexpr int kCols = kAttnCols<kKind>;
+                    float ahead[2][kCols];
+                    auto scores = [&](int c, float (&x)[kCols], float (&next)[kCols]) {
+                        attn_wait<kCols>(x);
+                        if (c + kCols < 64) attn_issue<kCols>(tS + c + kCols, next);
                         if constexpr (kNarrow) {
 #pragma unroll
-                            for (int i = 0; i < kAttnCols<kKind>; i += 4) {
+                            for (int i = 0; i < kCols; i += 4) {
                                 const ulonglong2 k = *reinterpret_cast<const ulonglong2*>(fk + c + i);
                                 unpack2(mul2(pack2(x[i], x[i + 1]), k.x), x[i], x[i + 1]);
                                 unpack2(mul2(pack2(x[i + 2], x[i + 3]), k.y), x[i + 2], x[i + 3]);
@@ -318,13 +321,14 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                         }
                     };
                     float top = -INFINITY;
-#pragma unroll 1
-                    for (int c = 0; c < 64; c += kAttnCols<kKind>) {
-                        float x[kAttnCols<kKind>];
-                        scores(c, x);
+                    attn_issue<kCols>(tS, ahead[0]);
+#pragma unroll
+                    for (int c = 0; c < 64; c += kCols) {
+                        float (&x)[kCols] = ahead[c / kCols & 1];
+                        scores(c, x, ahead[c / kCols + 1 & 1]);
                         float a = -INFINITY, b = -INFINITY;
 #pragma unroll
-                        for (int i = 0; i < kAttnCols<kKind>; i += 4) { a = max3(a, x[i], x[i + 1]); b = max3(b, x[i + 2], x[i + 3]); }
+                        for (int i = 0; i < kCols; i += 4) { a = max3(a, x[i], x[i + 1]); b = max3(b, x[i + 2], x[i + 3]); }
                         top = max3(top, a, b);
                     }
                     top = fmaf(top, factor, above);
@@ -354,14 +358,14 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                     any = true;
                     const uint64_t f2 = pack2(factor, factor), b2 = pack2(-ref, -ref);
                     uint64_t s2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
-                    // the loops are not unrolled, so that the code stays near
-#pragma unroll 1
-                    for (int c = 0; c < 64; c += kAttnCols<kKind>) {
-                        float x[kAttnCols<kKind>];
-                        uint32_t w[kAttnCols<kKind> / 2];
-                        scores(c, x);
+                    attn_issue<kCols>(tS, ahead[0]);
 #pragma unroll
-                        for (int i = 0; i < kAttnCols<kKind>; i += 4) {
+                    for (int c = 0; c < 64; c += kCols) {
+                        float (&x)[kCols] = ahead[c / kCols & 1];
+                        uint32_t w[kCols / 2];
+                        scores(c, x, ahead[c / kCols + 1 & 1]);
+#pragma unroll
+                        for (int i = 0; i < kCols; i += 4) {
                             float e[4];
                             unpack2(fma2(pack2(x[i], x[i + 1]), f2, b2), e[0], e[1]);
                             unpack2(fma2(pack2(x[i + 2], x[i + 3]), f2, b2), e[2], e[3]);
@@ -378,7 +382,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                             w[i >> 1] = pack16<kNarrow>(e[0], e[1]);
                             w[(i >> 1) + 1] = pack16<kNarrow>(e[2], e[3]);
                         }
-                        attn_write<kAttnCols<kKind> / 2>(tS + c / 2, w);
+                        attn_write<kCols / 2>(tS + c / 2, w);
                     }
                     float s0, s1;
                     unpack2(add2(s2[0], s2[1]), s0, s1);

@@ -261,6 +261,27 @@ __device__ __forceinline__ void attn_read(uint32_t addr, float (&v)[kCols])
     else if constexpr (kCols == 16) tmem_load16(addr, v);
     else { tmem_load32_issue(addr, v); tmem_load_wait(v); }
 }
+// Asked for; the values are there after attn_wait(), which waits for all that this thread has asked for.
+template <int kCols>
+__device__ __forceinline__ void attn_issue(uint32_t addr, float (&v)[kCols])
+{
+    if constexpr (kCols == 16)
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                     : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+                       "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+                     : "r"(addr) : "memory");
+    else tmem_load32_issue(addr, v);
+}
+template <int kCols>
+__device__ __forceinline__ void attn_wait(float (&v)[kCols])
+{
+    if constexpr (kCols == 16)
+        asm volatile("tcgen05.wait::ld.sync.aligned;"
+                     : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
+                       "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15])
+                     :: "memory");
+    else tmem_load_wait(v);
+}
 template <int kCols>
 __device__ __forceinline__ void attn_write(uint32_t addr, const uint32_t (&v)[kCols])
 {

@@ -25,7 +25,10 @@ namespace dspark {
 
 constexpr int kSoftmaxWarps = 8;
 constexpr int kFewSmem = 217 * 1024;             // two of P, Q, the ring; tables beside it
-constexpr int kFewPBytes = kAttnTile * 128;      // P^T of one tile: a line of 128 bytes a position
+// P^T: a line of 128 bytes a position, of two tiles beside one another where both fit
+constexpr int kFewPBytes = kAttnTile * 128;
+template <int kN> constexpr int kFewPStep = kN <= 32 ? kN * 2 : kFewPBytes;      // from one tile's to the other's
+template <int kN> constexpr int kFewPAll = kN <= 32 ? kFewPBytes : 2 * kFewPBytes;
 constexpr float kFewUnset = 1e38f;               // less a reference that every score is above
 
 struct FewShared {
@@ -67,7 +70,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;    // warp: uniform, and known to be
     const int d = P.c.head_dim, tile_bytes = P.chunks * kChunkBytes;
     unsigned char* sP = smem;
-    unsigned char* sQ = sP + 2 * kFewPBytes;     // per 64 components: kN lines of 128 bytes
+    unsigned char* sQ = sP + kFewPAll<kN>;     // per 64 components: kN lines of 128 bytes
     unsigned char* ring = sQ + P.chunks * kN * 128;
     const int slots = P.k_slots + P.v_slots;
     unsigned char* raw = ring + slots * tile_bytes;
@@ -120,7 +123,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                 if (second) {
                     if (!wait(&S.full[s], ph) || !wait(&S.p_full[b], turn & 1u)) break;
                     tc_fence_after();
-                    const uint32_t v = desc_mn_major(smem_u32(ring)) + s * tile_step, p = desc_mn_major(smem_u32(sP)) + b * (kFewPBytes >> 4);
+                    const uint32_t v = desc_mn_major(smem_u32(ring)) + s * tile_step, p = desc_mn_major(smem_u32(sP)) + b * (kFewPStep<kN> >> 4);
                     if (elect_one()) {
 #pragma unroll
                         for (int k = 0; k < kAttnTile / 16; ++k) mma_ss(tmem + kO, v + k * 128, p + k * 128, idesc_o, i > 0 || k > 0);
@@ -259,7 +262,8 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
             for (int jj = 0; jj < count; ++jj, ++item) {
                 const uint32_t b = item & 1u, turn = item >> 1;
                 const uint32_t tS = tmem + lane_base + b * 64 + row0;
-                unsigned char* p_line = sP + b * kFewPBytes + pos * 128;
+                unsigned char* p_line = sP + (kN <= 32 ? 0 : b * kFewPBytes) + pos * 128;
+                const int p_at = (kN <= 32 ? b * (kN / 8) : 0) + row0 / 8;
                 int start, len;
                 attn_tile_at(P, u.j0 + jj, start, len);
                 const int valid = min(len, u.length - start);               // positions of this tile that exist
@@ -397,7 +401,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                     }
 #pragma unroll
                     for (int c = 0; c < kC / 8; ++c)
-                        *reinterpret_cast<uint4*>(p_line + (((row0 / 8 + c) ^ (pos & 7)) << 4)) = make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+                        *reinterpret_cast<uint4*>(p_line + (((p_at + c) ^ (pos & 7)) << 4)) = make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
                 }
                 if (!kNarrow && masked) {
                     // V of positions that no row sees, or that hold NaN or infinities that only some see, must not meet a
@@ -525,10 +529,10 @@ static int few_launch(AttnParams& P, const CUtensorMap& k, const CUtensorMap& v,
     if (!attn_allow_smem(attn_few_kernel<kKind, kN>, kSmem, ready)) return launch_status();
     const int tile = P.chunks * kChunkBytes;
     // a chunk is left behind the ring: with up to 64 components the products read one past a tile (and nobody its results)
-    int room = kFewSmem - 2 * kFewPBytes - P.chunks * kN * 128 - (P.chunks == 1 ? kChunkBytes : 0);
-    // V tiles stay longer than K tiles: until their weights are there.  8-bit caches: few 16-bit tiles, so that many 8-bit ones can
-    // be on their way.
-    const int slots = kKind != kAttnWide ? (P.chunks == 2 ? 3 : 4) : room / tile < kAttnMaxSlots ? room / tile : kAttnMaxSlots;
+    int room = kFewSmem - kFewPAll<kN> - P.chunks * kN * 128 - (P.chunks == 1 ? kChunkBytes : 0);
+    // V tiles stay longer than K tiles: until their weights are there.  8-bit caches: two of each as 16 bits, the rest for 8-bit
+    // ones on their way.
+    const int slots = kKind != kAttnWide ? 4 : room / tile < kAttnMaxSlots ? room / tile : kAttnMaxSlots;
     P.k_slots = slots / 2;
     P.v_slots = slots - P.k_slots;
     const int raw = (room - slots * tile) / (kAttnTile * P.c.head_dim), most = raw < kAttnMaxRaw ? raw : kAttnMaxRaw;
