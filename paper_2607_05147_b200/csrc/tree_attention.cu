@@ -173,7 +173,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
         uint32_t units = 0, items = 0, merges = 0;
         uint32_t seq = 0;                        // cache tiles of earlier units
         bool ok = true, merged = false;
-        auto wait = [&](uint64_t* bar, uint32_t ph) { ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, ph)); };
+        auto wait = [&](uint64_t* bar, uint32_t ph) { ok = ok && mbar_wait_bounded(bar, ph); };      // each lane for itself
         auto arrive = [&](uint64_t* bar) { __syncwarp(); if (lane == 0) mbar_arrive(bar); };
         auto vote = [&](bool x) { return barrier_any<64>(pair_id + 1, x); };
         // Row `row` of row tile `tile` of a unit into shared memory; in 8-bit mode as fp16, scaled by a power of two so that no
@@ -266,6 +266,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                     }
                 }
                 wait(&S.s_full[t], items & 1u);
+                __syncwarp();
                 ++items;
                 tc_fence_after();
                 const float* fk = nullptr;
@@ -409,6 +410,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
             }
             if (left) { ok = false; break; }                                // both warps
             wait(&S.o_full[t], units & 1u);
+            __syncwarp();
             tc_fence_after();
             // Everything of this unit has been multiplied: Q of the next one takes the place of this one's.
             const AttnUnit done = u;
@@ -484,7 +486,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
             seq += count;
             ++units;
         }
-        if (!ok && lane == 0) give_up();
+        if (!ok) give_up();
     } else {
         // ---------------- 8-bit tiles to 16 bits --------------------------------------------------------------
         if constexpr (kNarrow) {
@@ -498,7 +500,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                 k_now = v_now = 0.f;
                 node = start + ct >= w.first;
                 if (ct >= min(kAttnTile, min(len, w.length - start))) return;
-                const int position = start + ct, page_of = position / P.c.page_size, token = position - page_of * P.c.page_size;
+                const int position = start + ct, page_of = attn_page_of(P, position), token = position - page_of * P.c.page_size;
                 const int page = P.c.block_table[w.r * P.c.table_stride + page_of];
                 if (page < 0 || page >= P.c.n_pages) return;
                 const long long at = ((long long)page * P.c.kv_heads + w.head) * P.c.page_size + token;
@@ -727,6 +729,8 @@ int dspark_tree_attention(const dspark_kv_cache_t* cache, int layer, const void*
     P.tile_tokens = cache->page_size < kAttnTile ? cache->page_size : kAttnTile;
     P.page_boxes = kAttnTile / P.tile_tokens;
     P.page_tiles = (cache->page_size + kAttnTile - 1) / kAttnTile;
+    P.page_shift = -1;
+    for (int i = 3; i <= 7; ++i) if (cache->page_size == 1 << i) P.page_shift = i;
     P.part_rows = w.rows;
     unsigned char* ws = (unsigned char*)workspace;
     P.cuts = (int4*)ws;

@@ -39,6 +39,7 @@ struct AttnParams {
     int k_slots, v_slots;                        // rings: 16-bit tiles of K, of V (behind those of K)
     int raw_k, raw_v;                            // 8-bit tiles, the same way
     int tile_tokens, page_tiles, page_boxes;     // positions of a box; cache tiles of a page (pages above 128) ; boxes of a tile
+    int page_shift;                              // pages of up to 128: log2 of their size; above: -1
     int part_rows;                               // rows of a partial result
     int32_t* dev_status;
     int4* cuts;                                  // workspace: [kAttnSms] (1 + head, last CTA, first row, nodes); 0: none
@@ -61,6 +62,12 @@ __device__ __forceinline__ void attn_tile_at(const AttnParams& P, int j, int& st
     const int page = j / P.page_tiles, at = (j - page * P.page_tiles) * kAttnTile;
     start = page * P.c.page_size + at;
     len = min(kAttnTile, P.c.page_size - at);
+}
+
+// page of a request that a position is in
+__device__ __forceinline__ int attn_page_of(const AttnParams& P, int position)
+{
+    return P.page_shift >= 0 ? position >> P.page_shift : position / P.c.page_size;
 }
 
 struct AttnUnit {
@@ -384,7 +391,7 @@ __device__ __forceinline__ void attn_produce(const AttnParams& P, AttnIter it, c
             int start, len;
             attn_tile_at(P, j, start, len);
             const int boxes = P.page_boxes == 1 ? 1 : (min(kAttnTile, u.length - start) + P.tile_tokens - 1) / P.tile_tokens;
-            const int page_of = start / P.c.page_size, y = P.page_boxes == 1 ? start - page_of * P.c.page_size : 0;
+            const int page_of = attn_page_of(P, start), y = P.page_boxes == 1 ? start - page_of * P.c.page_size : 0;
             int page = 0;
             if (box < boxes) {
                 page = table[page_of + box];

@@ -165,7 +165,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
         const uint32_t tO = tmem + lane_base + kO + row0;
         uint32_t units = 0, item = 0;
         bool ok = true;
-        auto wait = [&](uint64_t* bar, uint32_t ph) { ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, ph)); };
+        auto wait = [&](uint64_t* bar, uint32_t ph) { ok = ok && mbar_wait_bounded(bar, ph); };      // each lane for itself
         auto arrive = [&](uint64_t* bar) { __syncwarp(); if (lane == 0) mbar_arrive(bar); };
         // Q of a unit, this group's rows: 128 / kC threads a row, asked for and later stored.
         constexpr int kPer = 128 / kC, kMost = (kAttnMaxDim / 8 + kPer - 1) / kPer;
@@ -219,11 +219,11 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
         struct Ahead { int page, token; };
         auto page_of = [&](const AttnUnit& w, int jj) {
             Ahead a = {-1, 0};
-            if (kNarrow && w.j0 + jj < w.j1) {
+            if (kNarrow && w.j0 + jj < w.j1 && row0 < min(P.tile_nodes, w.n - w.node0) * P.group) {
                 int start, len;
                 attn_tile_at(P, w.j0 + jj, start, len);
                 if (pos < min(len, w.length - start)) {
-                    const int position = start + pos, page = position / P.c.page_size;
+                    const int position = start + pos, page = attn_page_of(P, position);
                     a.token = position - page * P.c.page_size;
                     a.page = P.c.block_table[w.r * P.c.table_stride + page];
                 }
@@ -312,6 +312,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                 }
                 if (turn) wait(&S.o_done[b], (turn - 1) & 1u);              // P^T that was here before has been multiplied
                 wait(&S.s_full[b], turn & 1u);
+                __syncwarp();
                 tc_fence_after();
                 if (row0 < rows) {
                     __syncwarp();
@@ -450,6 +451,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
             wait(&S.q_empty, units & 1u);        // this unit's Q has been multiplied: the next one's takes its place
             if (have) store_q(units + 1);
             wait(&S.o_done[(item - 1) & 1u], ((item - 1) >> 1) & 1u);
+            __syncwarp();
             tc_fence_after();
             if (group_any(t, !ok)) { ok = false; break; }
             if (row0 < rows) {
@@ -503,7 +505,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
             }
             ++units;
         }
-        if (!ok && lane == 0) give_up();
+        if (!ok) give_up();
     } else {
         if constexpr (kNarrow) {
             const int ct = tid - (kSoftmaxWarps + 3) * 32, kv = kWarps == 8 ? ct >> 7 : 0;
