@@ -518,7 +518,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                 const uint32_t bits = __ballot_sync(0xffffffffu, bad);
                 if (lane == 0) scales.bad[at][ct >> 5] = bits;
             };
-            if (!attn_widen<kKind, kAttnConverters * 32>(P, it, ct, 0, 1, raw, ring, tile_bytes, S.raw_full, S.raw_empty, S.full, S.empty, S.bad_value, abort_flag, load_scales,
+            if (!attn_widen<kKind, kAttnConverters * 32, false>(P, it, ct, 0, 1, raw, ring, tile_bytes, S.raw_full, S.raw_empty, S.full, S.empty, 0u, S.bad_value, abort_flag, load_scales,
                                         store_scales) && lane == 0)
                 give_up();
         }
@@ -615,7 +615,8 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const __grid_co
 
 // ---- host side -------------------------------------------------------------------------------------------
 // One K/V array of a layer as [page][head][token][d]; a box is `tokens` positions of one head of a page.
-static bool cache_map(CUtensorMap* map, const unsigned char* base, const KvView& c, int tokens)
+// `turned`: 8-bit lines of 64 and 128 bytes are swizzled too (widen_line).
+static bool cache_map(CUtensorMap* map, const unsigned char* base, const KvView& c, int tokens, bool turned)
 {
     EncodeTiledFn fn = encode_tiled_fn();
     if (!fn) return false;
@@ -626,7 +627,7 @@ static bool cache_map(CUtensorMap* map, const unsigned char* base, const KvView&
     const cuuint32_t box[4] = {(cuuint32_t)(wide ? 64 : c.head_dim), (cuuint32_t)tokens, 1, 1};
     const cuuint32_t estr[4] = {1, 1, 1, 1};
     return fn(map, wide ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<unsigned char*>(base), dims, strides, box,
-              estr, CU_TENSOR_MAP_INTERLEAVE_NONE, wide ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+              estr, CU_TENSOR_MAP_INTERLEAVE_NONE, wide || (turned && c.head_dim == 128) ? CU_TENSOR_MAP_SWIZZLE_128B : turned && c.head_dim == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE,
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 static int attn_sms()
@@ -737,7 +738,7 @@ int dspark_tree_attention(const dspark_kv_cache_t* cache, int layer, const void*
     P.part_stats = (float2*)(ws + w.stats);
     P.parts = (float*)(ws + w.parts);
     CUtensorMap map_k, map_v;
-    if (!cache_map(&map_k, P.c.k, P.c, P.tile_tokens) || !cache_map(&map_v, P.c.v, P.c, P.tile_tokens)) return DSPARK_ERR_CUDA;
+    if (!cache_map(&map_k, P.c.k, P.c, P.tile_tokens, few) || !cache_map(&map_v, P.c.v, P.c, P.tile_tokens, false)) return DSPARK_ERR_CUDA;
     cudaStream_t s = (cudaStream_t)stream;
     const int sms = attn_sms();
     int rc;

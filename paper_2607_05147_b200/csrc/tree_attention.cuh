@@ -12,7 +12,7 @@ constexpr int kAttnMaxDim = 128;
 constexpr int kAttnSms = 148;                    // a B200's: the workspace's size is known without the device
 constexpr int kAttnTile = 128;                   // rows of a row tile, positions of a cache tile
 constexpr int kChunkBytes = kAttnTile * 128;     // 64 columns of 16 bits of a tile: 128 rows of 128 bytes, swizzled
-constexpr int kAttnMaxSlots = 12, kAttnMaxRaw = 8, kAttnScaleTiles = 4;
+constexpr int kAttnMaxSlots = 12, kAttnMaxRaw = 12, kAttnScaleTiles = 4;
 constexpr int kAttnRingBytes = 6 * 2 * kChunkBytes;           // 192 KB: Q and the rings
 constexpr int kAttnNarrowBytes = 208 * 1024;                  // with 8-bit caches (4 KB of scales beside it)
 constexpr float kAttnLog2e = 1.4426950408889634f;
@@ -473,12 +473,41 @@ __device__ __forceinline__ void widen_tile(const unsigned char* src, unsigned ch
         }
     }
 }
-// kThreads threads: 8-bit tiles as fp16 tiles, as the products read them; K and V (kv 0 and 1), or one of them.  tile(unit, j) is
-// called before the waits for a tile's K, ready(number) between them and the work.  False: a wait ran out.
-template <int kKind, int kThreads, typename Tile, typename Ready>
+// A position's components (line: its place in an 8-bit tile) as fp16 into this thread's lane of tensor memory, two a column.  The copy
+// engine's swizzle has parted the lines of 64 and 128 bytes, so that eight lanes read different banks.
+template <int kKind>
+__device__ __forceinline__ void widen_line(const unsigned char* line, int token, int d, uint32_t addr)
+{
+    const int turn = d == 128 ? token & 7 : d == 64 ? token >> 1 & 3 : 0;
+#pragma unroll 1
+    for (int p0 = 0; p0 < d / 16; p0 += 2) {
+        uint4 w[2];
+        uint32_t x[16];
+#pragma unroll
+        for (int p = 0; p < 2; ++p) w[p] = p0 + p < d / 16 ? *reinterpret_cast<const uint4*>(line + (((p0 + p) ^ turn) << 4)) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const uint32_t y[4] = {w[p].x, w[p].y, w[p].z, w[p].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint2 z = widen4<kKind>(y[i]);
+                x[p * 8 + 2 * i] = z.x;
+                x[p * 8 + 2 * i + 1] = z.y;
+            }
+        }
+        tmem_store16(addr + p0 * 8, x);
+    }
+    tmem_store_wait();
+    tc_fence_before();
+}
+// kThreads threads: 8-bit tiles as fp16 tiles, as the products read them; K and V (kv 0 and 1), or one of them.  kTensorK: K goes to
+// tensor memory at `k_columns`, 64 columns a tile.  tile(unit, j) is called before the waits for a tile's K, ready(number) between
+// them and the work.  False: a wait ran out.
+template <int kKind, int kThreads, bool kTensorK, typename Tile, typename Ready>
 __device__ __forceinline__ bool attn_widen(const AttnParams& P, AttnIter it, int ct, int kv_first, int kv_last, const unsigned char* raw,
                                            unsigned char* ring, int tile_bytes, uint64_t* raw_full, uint64_t* raw_empty, uint64_t* full,
-                                           uint64_t* empty, volatile int* bad_value, volatile int* abort_flag, Tile tile, Ready ready)
+                                           uint64_t* empty, uint32_t k_columns, volatile int* bad_value, volatile int* abort_flag, Tile tile,
+                                           Ready ready)
 {
     const int lane = threadIdx.x & 31, d = P.c.head_dim;
     int number = 0, unit = 0, token0, from0, to0;
@@ -498,10 +527,14 @@ __device__ __forceinline__ bool attn_widen(const AttnParams& P, AttnIter it, int
                 if (kv == 0) ready(number);
                 const unsigned char* src = raw + (size_t)rs * kAttnTile * d;
                 unsigned char* dst = ring + (size_t)s * tile_bytes;
-                if (d == 128) widen_tile<kKind, kThreads, 128>(src, dst, ct, from0, to0, d);
+                if (kTensorK && kv == 0) {               // scores of positions that do not exist are hidden: whatever stands there
+                    tc_fence_after();
+                    const int token = (threadIdx.x >> 5 & 3) * 32 + lane;   // the lanes of tensor memory that this warp may write
+                    widen_line<kKind>(src + token * d, token, d, k_columns + ((uint32_t)(token & ~31) << 16) + at[0].s * 64);
+                } else if (d == 128) widen_tile<kKind, kThreads, 128>(src, dst, ct, from0, to0, d);
                 else if (d == 64) widen_tile<kKind, kThreads, 64>(src, dst, ct, from0, to0, d);
                 else widen_tile<kKind, kThreads, 0>(src, dst, ct, from0, to0, d);
-                if (valid < kAttnTile || (kKind == kAttnE4M3 && kv && tree < kAttnTile)) {
+                if ((kv || !kTensorK) && (valid < kAttnTile || (kKind == kAttnE4M3 && kv && tree < kAttnTile))) {
                     // positions that do not exist: zeros; a NaN among the nodes' values of V: zero here and back in the rows that see
                     // it (attn_bad_values).  Every thread looks at what it has written.
 #pragma unroll 1

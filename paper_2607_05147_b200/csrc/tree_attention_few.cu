@@ -62,7 +62,8 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
     constexpr int kThreads = kFewThreads<kKind, kN>, kProducer = kSoftmaxWarps, kIssuer = kSoftmaxWarps + 1, kIssuerO = kSoftmaxWarps + 2;
     constexpr int kWarps = kFewConverters<kKind, kN>, kOf = kNarrow ? 4 : 1, kC = kN / 2;    // kOf: warps that make one 16-bit tile
                    // kC: columns of a group
-    constexpr uint32_t kO = 128;                 // columns of tensor memory: S^T at 0 and 64, O^T at 128
+    // columns of tensor memory: S^T at 0 and 64, O^T at 128, two K tiles of an 8-bit cache at 192 and 256
+    constexpr uint32_t kO = 128, kK = 192, kColumns = kNarrow ? 512 : 256;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);   // swizzle atoms: 1 KB
     __shared__ FewShared S;
@@ -71,8 +72,8 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
     const int d = P.c.head_dim, tile_bytes = P.chunks * kChunkBytes;
     unsigned char* sP = smem;
     unsigned char* sQ = sP + kFewPAll<kN>;     // per 64 components: kN lines of 128 bytes
-    unsigned char* ring = sQ + P.chunks * kN * 128;
     const int slots = P.k_slots + P.v_slots;
+    unsigned char* ring = sQ + P.chunks * kN * 128 - (kNarrow ? P.k_slots * tile_bytes : 0);       // 8-bit: of V alone
     unsigned char* raw = ring + slots * tile_bytes;
 
     if (tid == 0) {
@@ -85,7 +86,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
         mbar_fence_init();
     }
     if (warp == kIssuer) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&S.tmem_base)), "r"(256) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&S.tmem_base)), "r"(kColumns) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     pdl_wait();
@@ -107,7 +108,6 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
         const uint32_t type = kNarrow ? 0u : 1u;                            // fp16 or bf16 operands, fp32 sums
         const uint32_t idesc_s = (1u << 4) | (type << 7) | (type << 10) | ((uint32_t)(kN >> 3) << 17) | ((uint32_t)(kAttnTile >> 4) << 24);
         const uint32_t idesc_o = idesc_s | (1u << 15) | (1u << 16);
-        const uint32_t tile_step = (uint32_t)tile_bytes >> 4;
         const int first_slot = second ? P.k_slots : 0, ring_slots = second ? P.v_slots : P.k_slots;
         RingPlace place;
         uint32_t units = 0, item = 0;
@@ -123,7 +123,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                 if (second) {
                     if (!wait(&S.full[s], ph) || !wait(&S.p_full[b], turn & 1u)) break;
                     tc_fence_after();
-                    const uint32_t v = desc_mn_major(smem_u32(ring)) + s * tile_step, p = desc_mn_major(smem_u32(sP)) + b * (kFewPStep<kN> >> 4);
+                    const uint32_t v = desc_mn_major(smem_u32(ring + s * tile_bytes)), p = desc_mn_major(smem_u32(sP)) + b * (kFewPStep<kN> >> 4);
                     if (elect_one()) {
 #pragma unroll
                         for (int k = 0; k < kAttnTile / 16; ++k) mma_ss(tmem + kO, v + k * 128, p + k * 128, idesc_o, i > 0 || k > 0);
@@ -134,11 +134,14 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                     // the scores that were here before have been read
                     if ((turn && !wait(&S.p_full[b], (turn - 1) & 1u)) || !wait(&S.full[s], ph)) break;
                     tc_fence_after();
-                    const uint32_t k0 = desc_k_major(smem_u32(ring)) + s * tile_step, q0 = desc_k_major(smem_u32(sQ));
+                    const uint32_t k0 = kNarrow ? 0u : desc_k_major(smem_u32(ring + s * tile_bytes)), q0 = desc_k_major(smem_u32(sQ));
                     if (elect_one()) {
 #pragma unroll
                         for (int k = 0; k < kAttnMaxDim / 16; ++k)
-                            if (k < d / 16)
+                            if (k >= d / 16) break;
+                            else if constexpr (kNarrow)
+                                mma_ts(tmem + b * 64, tmem + kK + s * 64 + k * 8, q0 + (k >> 2) * (kN * 8) + (k & 3) * 2, idesc_s, k > 0);
+                            else
                                 mma_ss(tmem + b * 64, k0 + (k >> 2) * (kChunkBytes >> 4) + (k & 3) * 2, q0 + (k >> 2) * (kN * 8) + (k & 3) * 2, idesc_s, k > 0);
                         umma_commit(&S.s_full[b]);
                         umma_commit(&S.empty[s]);
@@ -509,8 +512,8 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
     } else {
         if constexpr (kNarrow) {
             const int ct = tid - (kSoftmaxWarps + 3) * 32, kv = kWarps == 8 ? ct >> 7 : 0;
-            if (!attn_widen<kKind, 128>(P, it, ct & 127, kv, kWarps == 8 ? kv : 1, raw, ring, tile_bytes, S.raw_full, S.raw_empty, S.full, S.empty,
-                                        S.bad_value, abort_flag, [](const AttnUnit&, int) {}, [](int) {}) &&
+            if (!attn_widen<kKind, 128, true>(P, it, ct & 127, kv, kWarps == 8 ? kv : 1, raw, ring, tile_bytes, S.raw_full, S.raw_empty, S.full, S.empty,
+                                              tmem + kK, S.bad_value, abort_flag, [](const AttnUnit&, int) {}, [](int) {}) &&
                 lane == 0)
                 give_up();
         }
@@ -519,7 +522,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
     __syncthreads();
     if (warp == kIssuer) {
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kColumns) : "memory");
     }
 }
 
@@ -532,12 +535,12 @@ static int few_launch(AttnParams& P, const CUtensorMap& k, const CUtensorMap& v,
     const int tile = P.chunks * kChunkBytes;
     // a chunk is left behind the ring: with up to 64 components the products read one past a tile (and nobody its results)
     int room = kFewSmem - kFewPAll<kN> - P.chunks * kN * 128 - (P.chunks == 1 ? kChunkBytes : 0);
-    // V tiles stay longer than K tiles: until their weights are there.  8-bit caches: two of each as 16 bits, the rest for 8-bit
-    // ones on their way.
-    const int slots = kKind != kAttnWide ? 4 : room / tile < kAttnMaxSlots ? room / tile : kAttnMaxSlots;
-    P.k_slots = slots / 2;
-    P.v_slots = slots - P.k_slots;
-    const int raw = (room - slots * tile) / (kAttnTile * P.c.head_dim), most = raw < kAttnMaxRaw ? raw : kAttnMaxRaw;
+    // V tiles stay longer than K tiles: until their weights are there.  8-bit caches: two of each as 16 bits (K's in tensor memory),
+    // the rest for 8-bit ones on their way: 128 KB of them in flight per SM, or the memory's latency shows.
+    const int slots = room / tile < kAttnMaxSlots ? room / tile : kAttnMaxSlots;
+    P.k_slots = kKind != kAttnWide ? 2 : slots / 2;
+    P.v_slots = kKind != kAttnWide ? 2 : slots - P.k_slots;
+    const int raw = (room - P.v_slots * tile) / (kAttnTile * P.c.head_dim), most = raw < kAttnMaxRaw ? raw : kAttnMaxRaw;
     P.raw_k = kKind == kAttnWide ? 0 : most / 2;
     P.raw_v = kKind == kAttnWide ? 0 : most - P.raw_k;
     KernelTimerScope timer(DSPARK_K_TREE_ATTENTION, s);
