@@ -295,7 +295,14 @@ __device__ __forceinline__ void attn_write(uint32_t addr, const uint32_t (&v)[kC
     if constexpr (kCols == 8)
         asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
                      ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
-    else tmem_store16(addr, v);
+    else if constexpr (kCols == 16) tmem_store16(addr, v);
+    else
+        asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+                     "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+                     ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
+                       "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]),
+                       "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
+                       "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]) : "memory");
 }
 __device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 template <bool kHalf>
@@ -474,20 +481,24 @@ __device__ __forceinline__ void widen_tile(const unsigned char* src, unsigned ch
     }
 }
 // A position's components (line: its place in an 8-bit tile) as fp16 into this thread's lane of tensor memory, two a column.  The copy
-// engine's swizzle has parted the lines of 64 and 128 bytes, so that eight lanes read different banks.
-template <int kKind>
+// engine's swizzle has parted the lines of 64 and 128 bytes, so that eight lanes read different banks.  Of 64 or 128 components
+// (kDim) all are asked for first.
+template <int kKind, int kDim>
 __device__ __forceinline__ void widen_line(const unsigned char* line, int token, int d, uint32_t addr)
 {
-    const int turn = d == 128 ? token & 7 : d == 64 ? token >> 1 & 3 : 0;
-#pragma unroll 1
-    for (int p0 = 0; p0 < d / 16; p0 += 2) {
-        uint4 w[2];
-        uint32_t x[16];
+    constexpr int kBatch = kDim ? 4 : 1, kAll = kDim ? kDim / 16 : 1;
+    const int turn = kDim == 128 ? token & 7 : kDim == 64 ? token >> 1 & 3 : 0;
+    uint4 w[kAll];
 #pragma unroll
-        for (int p = 0; p < 2; ++p) w[p] = p0 + p < d / 16 ? *reinterpret_cast<const uint4*>(line + (((p0 + p) ^ turn) << 4)) : make_uint4(0, 0, 0, 0);
+    for (int p = 0; p < kAll && kDim; ++p) w[p] = *reinterpret_cast<const uint4*>(line + ((p ^ turn) << 4));
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {
-            const uint32_t y[4] = {w[p].x, w[p].y, w[p].z, w[p].w};
+    for (int p0 = 0; p0 < (kDim ? kAll : d / 16); p0 += kBatch) {
+        uint32_t x[kBatch * 8];
+        if (!kDim) w[0] = *reinterpret_cast<const uint4*>(line + (p0 << 4));
+#pragma unroll
+        for (int p = 0; p < kBatch; ++p) {
+            const uint4 v = w[kDim ? p0 + p : 0];
+            const uint32_t y[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const uint2 z = widen4<kKind>(y[i]);
@@ -495,7 +506,7 @@ __device__ __forceinline__ void widen_line(const unsigned char* line, int token,
                 x[p * 8 + 2 * i + 1] = z.y;
             }
         }
-        tmem_store16(addr + p0 * 8, x);
+        attn_write<kBatch * 8>(addr + p0 * 8, x);
     }
     tmem_store_wait();
     tc_fence_before();
@@ -530,7 +541,10 @@ __device__ __forceinline__ bool attn_widen(const AttnParams& P, AttnIter it, int
                 if (kTensorK && kv == 0) {               // scores of positions that do not exist are hidden: whatever stands there
                     tc_fence_after();
                     const int token = (threadIdx.x >> 5 & 3) * 32 + lane;   // the lanes of tensor memory that this warp may write
-                    widen_line<kKind>(src + token * d, token, d, k_columns + ((uint32_t)(token & ~31) << 16) + at[0].s * 64);
+                    const uint32_t to = k_columns + ((uint32_t)(token & ~31) << 16) + at[0].s * 64;
+                    if (d == 128) widen_line<kKind, 128>(src + token * d, token, d, to);
+                    else if (d == 64) widen_line<kKind, 64>(src + token * d, token, d, to);
+                    else widen_line<kKind, 0>(src + token * d, token, d, to);
                 } else if (d == 128) widen_tile<kKind, kThreads, 128>(src, dst, ct, from0, to0, d);
                 else if (d == 64) widen_tile<kKind, kThreads, 64>(src, dst, ct, from0, to0, d);
                 else widen_tile<kKind, kThreads, 0>(src, dst, ct, from0, to0, d);
