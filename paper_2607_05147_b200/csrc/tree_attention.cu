@@ -630,19 +630,7 @@ static bool cache_map(CUtensorMap* map, const unsigned char* base, const KvView&
               estr, CU_TENSOR_MAP_INTERLEAVE_NONE, wide || (turned && c.head_dim == 128) ? CU_TENSOR_MAP_SWIZZLE_128B : turned && c.head_dim == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE,
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-static int attn_sms()
-{
-    static std::atomic<int> sms[64];
-    int dev = 0;
-    cudaGetDevice(&dev);
-    int v = sms[dev & 63].load(std::memory_order_relaxed);
-    if (!v) {
-        cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev);
-        if (v > kAttnSms) v = kAttnSms;
-        sms[dev & 63].store(v, std::memory_order_relaxed);
-    }
-    return v;
-}
+static int attn_sms() { const int sms = current_sms(); return sms < kAttnSms ? sms : kAttnSms; }
 struct AttnWs { size_t stats, parts, total; int rows; };
 static AttnWs attn_ws(long long n_rows, int group, int d)
 {

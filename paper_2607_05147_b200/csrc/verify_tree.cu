@@ -7,47 +7,48 @@
 // A, so a rejection costs one pass over the two rows for the new Z = sum r and nothing is stored.
 //
 // One cluster of eight CTAs per request.  Every CTA makes the walk itself, from the scalars p(x), q(x), u of all nodes, gathered
-// at once; a pass over the vocabulary is shared: 128 warps own a run of it each, and the runs' sums pass through distributed
-// shared memory, so that all CTAs go on with the same numbers.  The sums of the last pass are those of the draw, which only the
-// warp that owns the drawn token's run reads again.  Sums and tests are fp64: what decides is a border between tokens.
+// at once; a pass over the vocabulary is shared: each warp owns a run of it, and the runs' sums pass through distributed
+// shared memory, so that all CTAs go on with the same numbers.  The sums of the last pass are those of the draw, for which only the
+// CTA that owns the drawn token's run reads it again.  Sums and tests are fp64: what decides is a border between tokens.
 //
-// Bound by the chain of dependent loads for few requests, by the rows' bytes for many (one pair of rows a request is read at
-// least, two where the path ends behind an accepted second child).
+// Bound by the chain of dependent steps.  Clocks of one tree (16 nodes, one rejection, 129280 entries): 1300 for the offsets, 3600 for
+// nodes and their scalars, 4000 for the first walk (1200 for later ones), 5000 for the pass over two rows, 2700 to join its sums,
+// 2000 for the draw: 11.4 us.  128 trees of 32 nodes, 2.2 such passes each on average, the slowest 5: 58 us, 188 MB, 3.2 TB/s.
 #include <math.h>
 
 #include "common.cuh"
 
 namespace dspark {
 
-constexpr int kVtCtas = 8, kVtWarps = 16, kVtThreads = kVtWarps * 32, kVtRuns = kVtCtas * kVtWarps;
-constexpr int kVtLoads = 8;                      // vectors of a run in flight in one lane
+constexpr int kVtCtas = 8, kVtMaxWarps = 16, kVtMaxRuns = kVtCtas * kVtMaxWarps;
+constexpr int kVtLoads = 4;                      // vectors of a run in flight in one lane
 
 struct VerifyTreeParams {
     const float* p; long long p_stride;
     const float* q; long long q_stride;
     int V, run;                                  // run: entries of one warp, a multiple of 128
+    int warps;                                   // of a CTA
     const int32_t* tokens; const int32_t* parents; const int32_t* row_offsets;
     int R, n_rows;
     const float* u_accept; const float* u_sample;
     int32_t* accepted_len; int32_t* out_tokens; int32_t* out_path; int32_t* dev_status;
 };
 
-enum VtAction { kVtPass = 0, kVtDraw = 1, kVtVoid = 2 };
+enum VtAction { kVtPass = 0, kVtDraw = 1, kVtVoid = 2, kVtSummed = 4 };
 
 struct VtShared {
-    double sums[2][kVtWarps];                    // read by the other CTAs; one set a pass, in turn
-    double all[kVtRuns];                         // inclusive sums of all runs
+    double sums[2][kVtMaxWarps];                    // read by the other CTAs; one set a pass, in turn
+    double all[kVtMaxRuns];                      // inclusive sums of all runs
     double A;
-    int action, node, length, n_gone, status;
+    double block[2][kVtMaxWarps];
+    int action, node, length, n_gone, status, pick;
     short parent[DSPARK_TREE_MAX_NODES], path[DSPARK_TREE_MAX_NODES];
     int token[DSPARK_TREE_MAX_NODES], gone[DSPARK_TREE_MAX_NODES];
     float p[DSPARK_TREE_MAX_NODES], q[DSPARK_TREE_MAX_NODES], u[DSPARK_TREE_MAX_NODES];
 };
 
-__device__ __forceinline__ void vt_cluster_sync()
-{
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
+__device__ __forceinline__ void vt_cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void vt_cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ double vt_remote(const double* local, uint32_t rank)
 {
     uint32_t a;
@@ -57,46 +58,73 @@ __device__ __forceinline__ double vt_remote(const double* local, uint32_t rank)
     return v;
 }
 
-// What is left of four entries from v on: max(p - A q, 0), or p without the rejected tokens.  Entries from `end` on: 0.
-// NaN stays.
+// The bits of a float in a double's place: its value times 2^-896, exactly, zero and the smallest included.  Two shifts where the
+// conversion, a quarter as wide, would bound the pass.  Not so for a sign, an infinity or NaN: their bits are above those of all others.
+__device__ __forceinline__ double vt_scaled(uint32_t bits) { return __hiloint2double((int)(bits >> 3), (int)(bits << 29)); }
+constexpr uint32_t kVtPlainBits = 0x7f800000u;
+
+// What is left of a row: max(p - A q, 0), or p without the rejected tokens.  NaN stays.
 struct VtRow {
-    const float* p; const float* q;
+    const float* p; const float* q;              // q == nullptr: p alone
     double A;
     const int* gone; int n_gone;
     bool vectors;
-    __device__ __forceinline__ void load(int v, int end, float (&a)[4], float (&b)[4]) const
+    __device__ __forceinline__ double left(int v) const
     {
-        if (vectors && v + 4 <= end) {
-            const float4 x = *reinterpret_cast<const float4*>(p + v);
-            a[0] = x.x; a[1] = x.y; a[2] = x.z; a[3] = x.w;
-            if (q) {
-                const float4 y = *reinterpret_cast<const float4*>(q + v);
-                b[0] = y.x; b[1] = y.y; b[2] = y.z; b[3] = y.w;
-            }
-        } else
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                a[i] = v + i < end ? p[v + i] : 0.f;
-                if (q) b[i] = v + i < end ? q[v + i] : 0.f;
-            }
-    }
-    __device__ __forceinline__ double left(int v, float a, float b) const
-    {
-        double r = q ? (double)a - A * (double)b : (double)a;
+        double r = q ? (double)p[v] - A * (double)q[v] : (double)p[v];
         if (r < 0.0) r = 0.0;
         for (int i = 0; i < n_gone; ++i)
             if (gone[i] == v) r = 0.0;
         return r;
     }
+    // a lane's part of the sum over [v0, v1), by the warp
+    __device__ double sum(int v0, int v1, int lane) const
+    {
+        bool any = false;
+        for (int i = 0; i < n_gone; ++i) any = any || (gone[i] >= v0 && gone[i] < v1);
+        if (vectors && !any) {
+            double s[4] = {0.0, 0.0, 0.0, 0.0};
+            uint32_t most = 0;
+            for (int v = v0; v < v1; v += kVtLoads * 128) {
+                uint4 a[kVtLoads], b[kVtLoads];
+#pragma unroll
+                for (int j = 0; j < kVtLoads; ++j) {
+                    const int at = v + j * 128 + lane * 4;
+                    a[j] = b[j] = make_uint4(0, 0, 0, 0);
+                    if (at + 4 <= v1) {
+                        a[j] = *reinterpret_cast<const uint4*>(p + at);
+                        if (q) b[j] = *reinterpret_cast<const uint4*>(q + at);
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < kVtLoads; ++j) {
+                    const uint32_t x[4] = {a[j].x, a[j].y, a[j].z, a[j].w}, y[4] = {b[j].x, b[j].y, b[j].z, b[j].w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        most = max(most, max(x[i], y[i]));
+                        const double r = vt_scaled(x[i]) - A * vt_scaled(y[i]);
+                        s[i] += r < 0.0 ? 0.0 : r;
+                    }
+                }
+            }
+            double all = ((s[0] + s[1]) + (s[2] + s[3])) * 0x1p896;
+            const int end = v1 & ~3;             // up to three entries are left where the row ends
+            if (end >= v0 && lane < v1 - end) all += left(end + lane);
+            if (!__any_sync(0xffffffffu, most >= kVtPlainBits)) return all;
+        }
+        double all = 0.0;
+#pragma unroll 4
+        for (int v = v0 + lane; v < v1; v += 32) all += left(v);
+        return all;
+    }
 };
 
-__global__ void __cluster_dims__(kVtCtas, 1, 1) __launch_bounds__(kVtThreads) verify_tree_kernel(const __grid_constant__ VerifyTreeParams P)
+__global__ void __cluster_dims__(kVtCtas, 1, 1) __launch_bounds__(kVtMaxWarps * 32, 2) verify_tree_kernel(const __grid_constant__ VerifyTreeParams P)
 {
     __shared__ VtShared S;
     pdl_wait();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int r = blockIdx.x / kVtCtas;
-    const uint32_t rank = blockIdx.x % kVtCtas;
+    const int r = blockIdx.x / kVtCtas, rank = blockIdx.x % kVtCtas, runs = kVtCtas * P.warps;
     const int row0 = P.row_offsets[r], end = P.row_offsets[r + 1], n = end - row0;
     const bool there = row0 >= 0 && end >= row0 && end <= P.n_rows;
     if (!there || n == 0) {
@@ -107,7 +135,7 @@ __global__ void __cluster_dims__(kVtCtas, 1, 1) __launch_bounds__(kVtThreads) ve
     __syncthreads();
     if (n <= DSPARK_TREE_MAX_NODES) {
         int bad = 0;
-        for (int i = 1 + tid; i < n; i += kVtThreads) {
+        for (int i = 1 + tid; i < n; i += blockDim.x) {
             const int parent = P.parents[row0 + i], x = P.tokens[row0 + i];
             const float u = P.u_accept[row0 + i];
             if (parent < 0 || parent >= i) bad |= DSPARK_DEV_BAD_TREE;
@@ -167,40 +195,30 @@ __global__ void __cluster_dims__(kVtCtas, 1, 1) __launch_bounds__(kVtThreads) ve
         }
     };
     VtRow row;
-    int v0 = (int)(rank * kVtWarps + warp) * P.run, v1 = v0 + P.run < P.V ? v0 + P.run : P.V;
+    int v0 = (rank * P.warps + warp) * P.run, v1 = v0 + P.run < P.V ? v0 + P.run : P.V;
     if (v0 > P.V) v0 = P.V;
     // S.all = inclusive sums of the runs, the same in every CTA
     auto sum_rows = [&]() {
         const long long at_row = row0 + S.node;
         row.p = P.p + at_row * P.p_stride;
-        row.q = P.q ? P.q + at_row * P.q_stride : nullptr;
         row.A = S.A;
+        row.q = P.q && row.A != 0.0 ? P.q + at_row * P.q_stride : nullptr;  // nothing rejected: the target alone
         row.gone = S.gone; row.n_gone = S.n_gone;
         row.vectors = (((uintptr_t)row.p | (uintptr_t)row.q) & 15) == 0;
-        double sum = 0.0;
-        for (int v = v0 + lane * 4; v - lane * 4 < v1; v += kVtLoads * 128) {
-            float a[kVtLoads][4], b[kVtLoads][4];
-#pragma unroll
-            for (int j = 0; j < kVtLoads; ++j) row.load(v + j * 128, v1, a[j], b[j]);
-#pragma unroll
-            for (int j = 0; j < kVtLoads; ++j) {
-                double four = 0.0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) four += row.left(v + j * 128 + i, a[j][i], b[j][i]);
-                sum += four;
-            }
-        }
-        sum = warp_sum_f64(sum);
+        const double sum = warp_sum_f64(row.sum(v0, v1, lane));
         if (lane == 0) S.sums[pass & 1][warp] = sum;
-        vt_cluster_sync();
+        vt_cluster_arrive();
+        vt_cluster_wait();
         if (warp == 0) {
             double x[4], run = 0.0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int k = lane * 4 + i;
-                run += vt_remote(&S.sums[pass & 1][k % kVtWarps], k / kVtWarps);
-                x[i] = run;
+                const int k = lane * 4 + i, at = k < runs ? k : 0;
+                x[i] = vt_remote(&S.sums[pass & 1][at % P.warps], at / P.warps);
+                if (k >= runs) x[i] = 0.0;
             }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = run += x[i];
             double before = run;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -215,87 +233,107 @@ __global__ void __cluster_dims__(kVtCtas, 1, 1) __launch_bounds__(kVtThreads) ve
         ++pass;
         __syncthreads();
     };
+    // What warp 0 has come to.  The others read it before sum_rows' last barrier, behind which it may change again.
     auto publish = [&](int action) {
         if (warp == 0 && lane == 0) { S.action = action; S.node = node; S.A = A; S.n_gone = n_gone; S.length = length; }
         __syncthreads();
     };
 
+    bool voided;
     for (;;) {
-        const int length_before = length;
-        int action = warp == 0 ? walk() : 0;
-        if (warp == 0 && length != length_before) summed = false;
-        // a rejection changes A; a rejected chosen token is taken out of the row
-        if (warp == 0 && (action == kVtPass || n_gone > 0)) summed = false;
-        if (warp == 0 && lane == 0) S.action = action | (summed ? 4 : 0);
-        __syncthreads();
-        const int told = S.action;
-        __syncthreads();
-        publish(told & 3);
-        if ((told & 3) == kVtVoid) break;
-        if (!(told & 4)) sum_rows();
+        int action = 0;
+        if (warp == 0) {
+            const int length_before = length;
+            action = walk();
+            // a rejection changes A, or takes a token out of the row
+            if (length != length_before || action == kVtPass || n_gone > 0) summed = false;
+        }
+        publish(action | (summed ? kVtSummed : 0));
+        const int told = S.action & ~kVtSummed;
+        voided = told == kVtVoid;
+        if (voided) break;
+        if (!(S.action & kVtSummed)) sum_rows();
         summed = true;
-        double total = S.all[kVtRuns - 1];
-        if ((told & 3) == kVtDraw && total == 0.0 && (S.A != 0.0 || S.n_gone != 0)) {
+        Z = S.all[kVtMaxRuns - 1];
+        if (told == kVtDraw && Z == 0.0 && (S.A != 0.0 || S.n_gone != 0)) {
             // nothing is left (only rounding can bring this about): the target itself
             A = 0.0; n_gone = 0;
             __syncthreads();
             publish(kVtDraw);
             sum_rows();
-            total = S.all[kVtRuns - 1];
+            Z = S.all[kVtMaxRuns - 1];
         }
-        if (!(total < INFINITY) || ((told & 3) == kVtDraw && !(total > 0.0))) {
-            __syncthreads();
-            if (tid == 0) { S.status |= DSPARK_DEV_BAD_ROW; S.action = kVtVoid; }
-            __syncthreads();
-            break;
+        if (!(Z < INFINITY) || (told == kVtDraw && !(Z > 0.0))) {
+            voided = true;
+            if (tid == 0) S.status |= DSPARK_DEV_BAD_ROW;
         }
-        Z = total;
-        if ((told & 3) == kVtDraw) break;
+        if (voided || told == kVtDraw) break;
     }
-    const bool voided = S.action == kVtVoid;
+    vt_cluster_arrive();
     const int len = voided ? 0 : S.length;
     if (!voided) {
         // the run that the drawn token is in: the first whose inclusive sum exceeds the target, else the last with a share
-        const double total = S.all[kVtRuns - 1], target = (double)P.u_sample[r] * total;
+        const double total = S.all[kVtMaxRuns - 1], target = (double)P.u_sample[r] * total;
         int owner = -1, last = 0;
-        for (int b = 0; b < kVtRuns; b += 32) {
+        for (int b = 0; b < runs; b += 32) {
             const double here = S.all[b + lane], before = b + lane ? S.all[b + lane - 1] : 0.0;
             const uint32_t over = __ballot_sync(0xffffffffu, here > target), some = __ballot_sync(0xffffffffu, here > before);
             if (owner < 0 && over) owner = b + __ffs(over) - 1;
             if (some) last = b + 31 - __clz(some);
         }
         if (owner < 0) owner = last;
-        if (owner == (int)rank * kVtWarps + warp) {
+        if (owner / P.warps == rank) {
+            // The CTA that has it, a block of 128 entries a warp: the first in which the target is passed, else the last with a share.
+            const int begin = owner * P.run, stop = min(begin + P.run, P.V);
             double run = owner ? S.all[owner - 1] : 0.0;
-            int pick = -1, fallback = -1;
-            for (int v = v0; v < v1 && pick < 0; v += 128) {
-                float a[4], b[4];
-                double x[4];
-                row.load(v + lane * 4, v1, a, b);
-                double mine = 0.0;
+            bool found = false;
+            if (tid == 0) S.pick = -1;
+            int round = 0;
+            for (int v = begin; v < stop && !found; v += P.warps * 128, ++round) {
+                const int at = v + warp * 128 + lane * 4;
+                double x[4], upto = 0.0;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) { mine += row.left(v + lane * 4 + i, a[i], b[i]); x[i] = mine; }
-                double before = mine;
+                for (int i = 0; i < 4; ++i) {
+                    const double e = at + i < stop ? row.left(at + i) : 0.0;
+                    x[i] = upto += e;
+                }
+                double before = upto;
 #pragma unroll
                 for (int o = 1; o < 32; o <<= 1) {
                     const double y = __shfl_up_sync(0xffffffffu, before, o);
                     if (lane >= o) before += y;
                 }
-                const double block = __shfl_sync(0xffffffffu, before, 31);
-                before -= mine;
-                int first = -1, with = -1;
+                if (lane == 31) S.block[round & 1][warp] = before;
+                __syncthreads();
+                // the blocks' sums up to each, by every warp
+                const double block = lane < P.warps ? S.block[round & 1][lane] : 0.0;
+                double blocks = block;
 #pragma unroll
-                for (int i = 3; i >= 0; --i) {
-                    if (run + (before + x[i]) > target && x[i] > (i ? x[i - 1] : 0.0)) first = v + lane * 4 + i;
-                    if (with < 0 && x[i] > (i ? x[i - 1] : 0.0)) with = v + lane * 4 + i;
+                for (int o = 1; o < kVtMaxWarps; o <<= 1) {
+                    const double y = __shfl_up_sync(0xffffffffu, blocks, o);
+                    if (lane >= o) blocks += y;
                 }
-                const uint32_t over = __ballot_sync(0xffffffffu, first >= 0), some = __ballot_sync(0xffffffffu, with >= 0);
-                if (over) pick = __shfl_sync(0xffffffffu, first, __ffs(over) - 1);
-                if (some) fallback = __shfl_sync(0xffffffffu, with, 31 - __clz(some));
-                run += block;
+                const uint32_t over = __ballot_sync(0xffffffffu, block > 0.0 && run + blocks > target), some = __ballot_sync(0xffffffffu, block > 0.0);
+                found = over != 0;
+                const int mine = found ? __ffs(over) - 1 : 31 - __clz(some);          // the block to look into
+                const double base = run + __shfl_sync(0xffffffffu, blocks - block, warp);
+                if (warp == mine) {
+                    before -= upto;
+                    int first = -1, last = -1;
+#pragma unroll
+                    for (int i = 3; i >= 0; --i) {
+                        const bool share = x[i] > (i ? x[i - 1] : 0.0);
+                        if (share && base + (before + x[i]) > target) first = at + i;
+                        if (share && last < 0) last = at + i;
+                    }
+                    const uint32_t passed = __ballot_sync(0xffffffffu, first >= 0), shares = __ballot_sync(0xffffffffu, last >= 0);
+                    const int pick = __shfl_sync(0xffffffffu, passed ? first : last, passed ? __ffs(passed) - 1 : 31 - __clz(shares));
+                    if (lane == 0) S.pick = pick;
+                }
+                run += __shfl_sync(0xffffffffu, blocks, P.warps - 1);
             }
-            if (pick < 0) pick = fallback;
-            if (lane == 0) P.out_tokens[row0 + len] = pick;
+            __syncthreads();
+            if (tid == 0) P.out_tokens[row0 + len] = S.pick;
         }
     }
     if (rank == 0) {
@@ -303,13 +341,13 @@ __global__ void __cluster_dims__(kVtCtas, 1, 1) __launch_bounds__(kVtThreads) ve
             P.accepted_len[r] = len;
             if (S.status) atomicOr(P.dev_status, S.status);
         }
-        for (int i = tid; i < n; i += kVtThreads) {
+        for (int i = tid; i < n; i += blockDim.x) {
             const bool on = i < len;
             if (P.out_path) P.out_path[row0 + i] = on ? S.path[i] : -1;
             if (voided || i != len) P.out_tokens[row0 + i] = on ? S.token[S.path[i]] : -1;
         }
     }
-    vt_cluster_sync();                           // no CTA leaves while another may read its sums
+    vt_cluster_wait();                           // no CTA leaves while another may read its sums
 }
 
 }  // namespace dspark
@@ -332,12 +370,17 @@ extern "C" int dspark_verify_tree(const float* target_probs, int64_t target_row_
     P.p = target_probs; P.p_stride = target_row_stride;
     P.q = draft_probs; P.q_stride = draft_row_stride;
     P.V = V;
-    P.run = ((V + kVtRuns - 1) / kVtRuns + 127) / 128 * 128;
+    // 16 warps where the requests fill the device once at most, two CTAs an SM (129280 entries: 1 tree 11.4 us, with 8 warps 12.5; 16 trees
+    // 23.9 and 25.7); else 8, four CTAs an SM, so that more walks run beside each other's passes (40 trees of 32000 entries: 20.6
+    // us, with 16 warps 24.8; 128 of 129280: 57.9 and 74.3)
+    P.warps = R * kVtCtas <= 2 * current_sms() ? kVtMaxWarps : kVtMaxWarps / 2;
+    const int runs = kVtCtas * P.warps;
+    P.run = ((V + runs - 1) / runs + 127) / 128 * 128;
     P.tokens = tokens; P.parents = parents; P.row_offsets = row_offsets; P.R = R; P.n_rows = n_rows;
     P.u_accept = u_accept; P.u_sample = u_sample;
     P.accepted_len = accepted_len; P.out_tokens = out_tokens; P.out_path = out_path; P.dev_status = dev_status;
     cudaStream_t s = (cudaStream_t)stream;
     KernelTimerScope timer(DSPARK_K_VERIFY_TREE, s);
-    launch_pdl(verify_tree_kernel, dim3((unsigned)R * kVtCtas), dim3(kVtThreads), 0, s, P);
+    launch_pdl(verify_tree_kernel, dim3((unsigned)R * kVtCtas), dim3(P.warps * 32), 0, s, P);
     return launch_status();
 }
