@@ -2,9 +2,10 @@
 //
 // A head's row x [d] is stored with one scale,
 //     int8:  s = max|x| / 127, q = rint(127 x / max|x|);      e4m3:  s = max|x| / 448, q = e4m3(448 x / max|x|),
-// and read as s q.  127 x and 448 x of a bf16 x are exact in fp32 (15 and 11 significant bits), and a quotient of such a number
-// by a bf16 one that is not a tie of either target differs from every tie by more than 2^-17 of its size, so that the correctly
-// rounded fp32 quotient decides every rounding as the exact one would.
+// and read as s q.  q needs no division.  127 x and 448 x of a bf16 x have 15 and 11 significant bits, so that their quotient by a
+// bf16 number, where it is not a tie of either target (at most 8 bits), is at least 2^-17 of its size away from every tie.  The product
+// with an approximate reciprocal is off by less than 2^-21; rounded to 19 bits (2^-19) it is on the tie where the quotient is one,
+// and on the quotient's side of it elsewhere, and rounds to the target as the exact quotient would.
 //
 // All three are bound by memory, or, for few rows, by a chain of dependent loads: row_offsets -> first -> block_table -> store.
 // The rows are therefore read before that chain is begun.  A head's row belongs to 8, 16 or 32 neighbouring lanes, 16 bytes of
@@ -20,6 +21,7 @@ constexpr int kKvRows = 4;                       // head rows of one thread
 struct KvStep {
     KvView c;
     const int32_t* first; const int32_t* row_offsets; int R, n_rows;
+    uint32_t heads_reciprocal;                                 // 2^32 / kv_heads, rounded up
     int32_t* dev_status;
     const unsigned char* k; const unsigned char* v;            // kv_write: the rows
     unsigned char* out_k; unsigned char* out_v; int out_f32;   // kv_read
@@ -30,7 +32,7 @@ struct KvStep {
 struct KvSlot { long long at, scale; };
 __device__ __forceinline__ bool kv_slot(const KvView& c, int r, int position, int head, KvSlot& s)
 {
-    const int page_of = position / c.page_size, token = position - page_of * c.page_size;
+    const int page_of = c.page_shift >= 0 ? position >> c.page_shift : position / c.page_size, token = position - page_of * c.page_size;
     const int page = c.block_table[r * c.table_stride + page_of];
     s.at = page * c.page_stride + token * c.token_stride + head * c.head_stride;
     s.scale = ((long long)page * c.kv_heads + head) * c.page_size + token;
@@ -62,33 +64,54 @@ __device__ __forceinline__ uint32_t bf16x2(float lo, float hi)
     return r;
 }
 
+__device__ __forceinline__ uint32_t max_nan_bf16x2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ float rcp_approx(float x)
+{
+    float r;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
 template <int kDtype> __device__ constexpr float kv_whole() { return kDtype == DSPARK_I8 ? 127.f : 448.f; }
 // 8 of a head row's values, 8 bits each; top: the row's largest magnitude, bad: it holds NaN or an infinity
 template <int kLanes, int kDtype>
 __device__ __forceinline__ uint2 kv_quantise(uint4 x, float& top, bool& bad)
 {
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    float e[8];
-    top = 0.f;
+    uint32_t most = max_nan_bf16x2(max_nan_bf16x2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), max_nan_bf16x2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { e[2 * i] = bf16lo(w[i]); e[2 * i + 1] = bf16hi(w[i]); }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) { const float a = fabsf(e[i]); top = (a > top || a != a) ? a : top; }   // NaN stays
-#pragma unroll
-    for (int o = kLanes / 2; o; o >>= 1) {
-        const float a = __shfl_xor_sync(0xffffffffu, top, o);
-        top = (a > top || a != a) ? a : top;
-    }
+    for (int o = kLanes / 2; o; o >>= 1) most = max_nan_bf16x2(most, __shfl_xor_sync(0xffffffffu, most, o));
+    most = max_nan_bf16x2(most, most >> 16 | most << 16);
+    top = bf16lo(most);
     bad = !(top < INFINITY);
     uint32_t q[2] = {0, 0};
     if (!bad && top != 0.f) {
-        // above, whole * x passes the range of fp32: both 2^16 smaller there
-        const float up = top > 1e35f ? kv_whole<kDtype>() * 0x1p-16f : kv_whole<kDtype>(), by = top > 1e35f ? top * 0x1p-16f : top;
+        // x and its maximum, both times a power of two where the reciprocal would leave the range of fp32
+        const float by = top > 1e35f ? 0x1p-16f : top < 1e-35f ? 0x1p64f : 1.f;
+        const float inverse = kv_whole<kDtype>() * rcp_approx(top * by);
+        const uint64_t by2 = pack2(by, by), inverse2 = pack2(inverse, inverse);
 #pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-            const float a = __fdiv_rn(up * e[i], by), b = __fdiv_rn(up * e[i + 1], by);
-            const uint32_t two = kDtype == DSPARK_I8 ? ((uint32_t)(int)rintf(a) & 0xffu) | ((uint32_t)(int)rintf(b) & 0xffu) << 8 : e4m3x2(a, b);
-            q[i >> 2] |= two << (8 * (i & 3));
+        for (int i = 0; i < 4; ++i) {
+            float a, b;
+            unpack2(mul2(mul2(pack2(bf16lo(w[i]), bf16hi(w[i])), by2), inverse2), a, b);
+            a = __uint_as_float((__float_as_uint(a) + 16u) & ~31u);
+            b = __uint_as_float((__float_as_uint(b) + 16u) & ~31u);
+            uint32_t two;
+            if constexpr (kDtype == DSPARK_I8) {
+                // 1.5 2^23 + a: rounded to an integer, which its low bits are
+                a += 12582912.f;
+                b += 12582912.f;
+                two = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040);
+                q[i >> 1] = i & 1 ? __byte_perm(q[i >> 1], two, 0x5410) : two;
+            } else {
+                two = e4m3x2(a, b);
+                q[i >> 1] |= two << (16 * (i & 1));
+            }
         }
     }
     return make_uint2(q[0], q[1]);
@@ -104,8 +127,10 @@ __device__ __forceinline__ void kv_put(unsigned char* out, int sub, uint4 x, flo
 #pragma unroll
         for (int i = 0; i < 4; ++i) { e[2 * i] = bf16lo(w[i]); e[2 * i + 1] = bf16hi(w[i]); }
     } else if constexpr (kDtype == DSPARK_I8) {
+        // a byte + 128 in the low bits of 2^23
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = (float)(int8_t)(w[i >> 2] >> (8 * (i & 3))) * scale;
+        for (int i = 0; i < 8; ++i)
+            e[i] = (__uint_as_float(__byte_perm(w[i >> 2] ^ 0x80808080u, 0x4b000000u, 0x7440 | (i & 3))) - 8388736.f) * scale;
     } else {
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
@@ -123,91 +148,117 @@ __device__ __forceinline__ void kv_put(unsigned char* out, int sub, uint4 x, flo
 }
 
 // Which request a row belongs to: the number of requests that end at or before it.  Up to kCountRequests of them the CTA
-// counts those of its first row, one load a thread, and each row goes on from there; beyond, every row is searched for.
+// counts those of its first row, one load a thread, and each row goes on from there; beyond, every row is searched for.  Up to
+// kKvThreads requests are kept in shared memory with their first tokens, so that no row waits for memory again before its page.
 constexpr int kCountRequests = 1024;
-__device__ __forceinline__ int kv_count_requests(const int32_t* row_offsets, int R, int row)     // all threads of the CTA
+struct KvRequests {
+    const int32_t* first; const int32_t* row_offsets;         // of all requests, in shared or global memory
+    int R, from;                                              // from: request of the CTA's first row
+};
+struct KvRequestsShared { int32_t first[kKvThreads], row_offsets[kKvThreads + 1]; };
+__device__ __forceinline__ KvRequests kv_requests(const int32_t* first, const int32_t* row_offsets, int R, int row, KvRequestsShared& S)
 {
-    int r = 0;
-    for (int i0 = 1; i0 <= R; i0 += kKvThreads) {
-        const int i = i0 + (int)threadIdx.x;
-        r += __syncthreads_count(i <= R && row_offsets[i] <= row);
-    }
-    return r;
+    KvRequests q = {first, row_offsets, R, 0};
+    const int tid = threadIdx.x;
+    if (R <= kKvThreads) {
+        const bool in = tid < R;
+        const int end = in ? row_offsets[tid + 1] : 0;
+        if (in) { S.first[tid] = first[tid]; S.row_offsets[tid + 1] = end; }
+        if (tid == 0) S.row_offsets[0] = row_offsets[0];
+        q.from = __syncthreads_count(in && end <= row);
+        q.first = S.first; q.row_offsets = S.row_offsets;
+    } else if (R <= kCountRequests)
+        for (int i0 = 1; i0 <= R; i0 += kKvThreads) q.from += __syncthreads_count(i0 + tid <= R && row_offsets[i0 + tid] <= row);
+    return q;
 }
-__device__ __forceinline__ int kv_find_request(const int32_t* row_offsets, int R, int row, int from)
+__device__ __forceinline__ int kv_find_request(const KvRequests& q, int row)
 {
-    if (R <= kCountRequests) {
-        while (from < R && row_offsets[from + 1] <= row) ++from;
-        return from;
+    int lo = q.from;
+    if (q.R <= kCountRequests) {
+        while (lo < q.R && q.row_offsets[lo + 1] <= row) ++lo;
+        return lo;
     }
-    int lo = 0, hi = R;
+    int hi = q.R;
     while (lo < hi) {
         const int mid = (lo + hi) >> 1;
-        if (row_offsets[mid + 1] <= row) lo = mid + 1; else hi = mid;
+        if (q.row_offsets[mid + 1] <= row) lo = mid + 1; else hi = mid;
     }
     return lo;
 }
 
-// Head rows [blockIdx.x * per, ...): index = (row * 2 + (0: K, 1: V)) * heads + head.
+// Head rows [blockIdx.x * per, ...).
 template <int kLanes, int kDtype, bool kWrite>
 __global__ void __launch_bounds__(kKvThreads) kv_rows_kernel(const __grid_constant__ KvStep P)
 {
     constexpr int kPer = kKvThreads / kLanes;
+    constexpr int kMost = kPer * kKvRows / 2 + 1;              // rows that a CTA has a part of
+    __shared__ KvRequestsShared S;
+    __shared__ KvSlot slots[kMost];                            // of head 0; at = -1: the row is left alone, -2: it has no page
     pdl_wait();
     const int tid = threadIdx.x, sub = tid & (kLanes - 1), slot = tid / kLanes;
     const int heads = P.c.kv_heads;
+    // index = (row * 2 + (0: K, 1: V)) * heads + head; a product with the reciprocal divides, exact for a CTA's few thousand
     const long long total = (long long)P.n_rows * 2 * heads, base = (long long)blockIdx.x * (kPer * kKvRows);
+    const int row0 = (int)(base / (2 * heads)), base_in = (int)(base - (long long)row0 * 2 * heads);
     const bool in = sub * 8 < P.c.head_dim;
-    int row[kKvRows], head[kKvRows];
+    int local[kKvRows], head[kKvRows];           // row - row0
     bool value[kKvRows], live[kKvRows];
     uint4 x[kKvRows];
+    const unsigned char* k_in = P.k + row0 * P.row_stride;
+    const unsigned char* v_in = P.v + row0 * P.row_stride;
 #pragma unroll
     for (int j = 0; j < kKvRows; ++j) {
-        const long long i = base + j * kPer + slot;
-        live[j] = i < total;
-        const int at = (int)(i / heads);
-        row[j] = at >> 1;
+        const uint32_t i = base_in + j * kPer + slot;
+        live[j] = base + j * kPer + slot < total;
+        const uint32_t at = heads == 1 ? i : __umulhi(i, P.heads_reciprocal);
+        local[j] = (int)(at >> 1);
         value[j] = at & 1;
-        head[j] = (int)(i - (long long)at * heads);
+        head[j] = (int)(i - at * heads);
         if (kWrite) {
             x[j] = make_uint4(0, 0, 0, 0);
             if (live[j] && in)
-                x[j] = *reinterpret_cast<const uint4*>((value[j] ? P.v : P.k) + row[j] * P.row_stride + head[j] * P.head_stride + sub * 16);
+                x[j] = *reinterpret_cast<const uint4*>((value[j] ? v_in : k_in) + local[j] * P.row_stride + head[j] * P.head_stride + sub * 16);
         }
     }
+    // where the CTA's rows are in the cache, one thread a row
     const long long capacity = kv_capacity(P.c);
-    if (blockIdx.x == 0) kv_report(P.first, P.row_offsets, P.R, P.n_rows, capacity, P.dev_status);
-    const int r0 = P.R <= kCountRequests ? kv_count_requests(P.row_offsets, P.R, (int)(base / (2 * heads))) : 0;
-
+    const KvRequests requests = kv_requests(P.first, P.row_offsets, P.R, row0, S);
+    if (tid < kMost) {
+        const int row = row0 + tid;
+        KvSlot at = {-1, 0};
+        const int r = row < P.n_rows ? kv_find_request(requests, row) : P.R;
+        if (r < P.R) {
+            const KvRequest q = kv_request(requests.first, requests.row_offsets, r, P.n_rows, capacity);
+            if (q.n >= 0 && row >= q.row0 && !kv_slot(P.c, r, q.first + row - q.row0, 0, at)) {
+                at.at = -2;
+                atomicOr(P.dev_status, DSPARK_DEV_BAD_PAGE);
+            }
+        }
+        slots[tid] = at;
+    }
+    __syncthreads();
     KvSlot s[kKvRows];
-    bool page_there[kKvRows];
-    bool bad_page = false;
+    bool there[kKvRows];
 #pragma unroll
     for (int j = 0; j < kKvRows; ++j) {
-        const int r = live[j] ? kv_find_request(P.row_offsets, P.R, row[j], r0) : P.R;
-        live[j] = r < P.R;
-        page_there[j] = false;
-        if (live[j]) {
-            const KvRequest q = kv_request(P.first, P.row_offsets, r, P.n_rows, capacity);
-            live[j] = q.n >= 0 && row[j] >= q.row0;
-            if (live[j]) page_there[j] = kv_slot(P.c, r, q.first + row[j] - q.row0, head[j], s[j]);
-            bad_page = bad_page || (live[j] && !page_there[j]);
-        }
+        s[j] = slots[local[j]];
+        live[j] = live[j] && s[j].at != -1;
+        there[j] = live[j] && s[j].at >= 0;
+        s[j].at += head[j] * P.c.head_stride;
+        s[j].scale += head[j] * P.c.page_size;
     }
-    if (bad_page) atomicOr(P.dev_status, DSPARK_DEV_BAD_PAGE);
 
     if constexpr (kWrite) {
 #pragma unroll
         for (int j = 0; j < kKvRows; ++j) {
             unsigned char* cache = value[j] ? P.c.v : P.c.k;
-            const bool store = live[j] && page_there[j];
             if constexpr (kDtype == DSPARK_BF16) {
-                if (store && in) *reinterpret_cast<uint4*>(cache + s[j].at + sub * 16) = x[j];
+                if (there[j] && in) *reinterpret_cast<uint4*>(cache + s[j].at + sub * 16) = x[j];
             } else {
                 bool bad;
                 float top;
                 const uint2 q = kv_quantise<kLanes, kDtype>(x[j], top, bad);
-                if (store && in) {
+                if (there[j] && in) {
                     *reinterpret_cast<uint2*>(cache + s[j].at + sub * 8) = q;
                     if (sub == 0) (value[j] ? P.c.v_scale : P.c.k_scale)[s[j].scale] = bad ? NAN : top / kv_whole<kDtype>();
                 }
@@ -219,7 +270,7 @@ __global__ void __launch_bounds__(kKvThreads) kv_rows_kernel(const __grid_consta
         for (int j = 0; j < kKvRows; ++j) {
             x[j] = make_uint4(0, 0, 0, 0);
             scale[j] = 0.f;
-            if (live[j] && page_there[j] && in) {
+            if (there[j] && in) {
                 const unsigned char* cache = value[j] ? P.c.v : P.c.k;
                 if constexpr (kDtype == DSPARK_BF16) x[j] = *reinterpret_cast<const uint4*>(cache + s[j].at + sub * 16);
                 else {
@@ -232,9 +283,10 @@ __global__ void __launch_bounds__(kKvThreads) kv_rows_kernel(const __grid_consta
 #pragma unroll
         for (int j = 0; j < kKvRows; ++j) {
             unsigned char* out = value[j] ? P.out_v : P.out_k;
-            if (live[j] && in && out) kv_put<kDtype>(out + row[j] * P.row_stride + head[j] * P.head_stride, sub, x[j], scale[j], P.out_f32);
+            if (live[j] && in && out) kv_put<kDtype>(out + row0 * P.row_stride + local[j] * P.row_stride + head[j] * P.head_stride, sub, x[j], scale[j], P.out_f32);
         }
     }
+    if (blockIdx.x == 0) kv_report(P.first, P.row_offsets, P.R, P.n_rows, capacity, P.dev_status);
 }
 
 template <int kLanes, bool kWrite>
@@ -257,10 +309,12 @@ static int kv_rows(const KvStep& P, cudaStream_t s)
 }
 
 // ---- accepted paths ----------------------------------------------------------------------------------------
-// One CTA per request and (layer, K or V).  A thread owns 16 bytes of a position (or one scale) and moves them along the whole
-// path, kBatch positions at a time: path[i] > i and the path ascends, so a position that is read is never one that an earlier
-// batch has written, and within a batch all reads come first.  Different threads touch different bytes: no order among them.
-constexpr int kCommitThreads = 128, kCommitBatch = 8;
+// A CTA has one request and some of the layers' K and V.  Where the path's rows lie, and where they go, is worked out once, a run of
+// kCommitRun nodes at a time, for all layers.  A thread owns 16 bytes of a position (or one scale) and moves them along the
+// path, kCommitBatch positions at a time: path[i] > i and the path ascends, so a position that is read is never one that an
+// earlier batch has written, and within a batch all reads come first.  Different threads touch different bytes: no order among
+// them.
+constexpr int kCommitThreads = 128, kCommitBatch = 8, kCommitRun = 128;
 
 struct KvCommit {
     KvView c;
@@ -273,65 +327,73 @@ struct KvCommit {
 
 __global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(const __grid_constant__ KvCommit P)
 {
-    __shared__ int s_bad;
+    __shared__ KvSlot s_from[kCommitRun], s_to[kCommitRun];   // of head 0; from.at < 0: nothing to move
     pdl_wait();
     const int r = blockIdx.x, tid = threadIdx.x;
-    const KvRequest q = kv_request(P.first, P.row_offsets, r, P.n_rows, kv_capacity(P.c));
+    const KvView& c = P.c;
+    const int accepted = P.accepted[r];
+    const KvRequest q = kv_request(P.first, P.row_offsets, r, P.n_rows, kv_capacity(c));
     const bool tell = blockIdx.y == 0 && tid == 0;
     if (tell && q.status) atomicOr(P.dev_status, q.status);
     if (q.n <= 0) {
         if (tell && P.out_first) P.out_first[r] = q.first;
         return;
     }
-    const int n = P.accepted[r];
-    if (tid == 0) s_bad = (n < 0 || n >= q.n) ? 1 : 0;
-    __syncthreads();
+    const int n = accepted;
     const int32_t* path = P.path + q.row0;
-    if (n > 0 && n < q.n)
-        for (int i = tid; i < n; i += kCommitThreads)
-            if (path[i] >= q.n || path[i] <= (i ? path[i - 1] : 0)) s_bad = 1;
-    __syncthreads();
-    const bool bad = s_bad != 0;
+    bool bad = n < 0 || n >= q.n;
+    if (!bad)
+        for (int i = tid; i < n; i += kCommitThreads) bad = bad || path[i] >= q.n || path[i] <= (i ? path[i - 1] : 0);
+    bad = __syncthreads_or(bad);
     if (tell) {
         if (bad) atomicOr(P.dev_status, DSPARK_DEV_BAD_TREE);
         if (P.out_first) P.out_first[r] = bad ? q.first : q.first + 1 + n;
     }
     if (bad) return;
-    const KvView& c = P.c;
     const int es = c.dtype == DSPARK_BF16 ? 2 : 1, per_head = c.head_dim * es / 16, pieces = per_head * c.kv_heads;
     const int scales = c.dtype == DSPARK_BF16 ? 0 : c.kv_heads;
     bool bad_page = false;
-    for (int lkv = blockIdx.y; lkv < 2 * P.n_layers; lkv += gridDim.y) {
-        const int layer = lkv >> 1;
-        unsigned char* cache = ((lkv & 1) ? c.v : c.k) + layer * P.layer_stride;
-        float* scale = (lkv & 1) ? c.v_scale : c.k_scale;
-        if (scale) scale += layer * P.layer_scales;
-        for (int i = tid; i < pieces + scales; i += kCommitThreads) {
-            const bool row = i < pieces;
-            const int head = row ? i / per_head : i - pieces, piece = row ? i - head * per_head : 0;
-            for (int j0 = 0; j0 < n; j0 += kCommitBatch) {
-                uint4 x[kCommitBatch];
-                KvSlot to[kCommitBatch];
-                bool move[kCommitBatch];
-#pragma unroll
-                for (int j = 0; j < kCommitBatch; ++j) {
-                    move[j] = j0 + j < n && path[j0 + j] != j0 + j + 1;
-                    if (!move[j]) continue;
-                    KvSlot from;
-                    const bool there = kv_slot(c, r, q.first + path[j0 + j], head, from);
-                    move[j] = kv_slot(c, r, q.first + 1 + j0 + j, head, to[j]) && there;
-                    if (!move[j]) { bad_page = true; continue; }
-                    if (row) x[j] = *reinterpret_cast<const uint4*>(cache + from.at + piece * 16);
-                    else x[j].x = __float_as_uint(scale[from.scale]);
-                }
-#pragma unroll
-                for (int j = 0; j < kCommitBatch; ++j)
-                    if (move[j]) {
-                        if (row) *reinterpret_cast<uint4*>(cache + to[j].at + piece * 16) = x[j];
-                        else scale[to[j].scale] = __uint_as_float(x[j].x);
-                    }
+    for (int run0 = 0; run0 < n; run0 += kCommitRun) {
+        const int count = min(kCommitRun, n - run0);
+        for (int i = tid; i < count; i += kCommitThreads) {
+            const int node = path[run0 + i];
+            s_from[i].at = -1;
+            if (node != run0 + i + 1) {
+                KvSlot from, to;
+                const bool there = kv_slot(c, r, q.first + node, 0, from);
+                if (kv_slot(c, r, q.first + 1 + run0 + i, 0, to) && there) { s_from[i] = from; s_to[i] = to; }
+                else bad_page = true;
             }
         }
+        __syncthreads();
+        for (int lkv = blockIdx.y; lkv < 2 * P.n_layers; lkv += gridDim.y) {
+            const int layer = lkv >> 1;
+            unsigned char* cache = ((lkv & 1) ? c.v : c.k) + layer * P.layer_stride;
+            float* scale = (lkv & 1) ? c.v_scale : c.k_scale;
+            if (scale) scale += layer * P.layer_scales;
+            for (int i = tid; i < pieces + scales; i += kCommitThreads) {
+                const bool row = i < pieces;
+                const int head = row ? i / per_head : i - pieces;
+                unsigned char* mine = row ? cache + head * c.head_stride + (i - head * per_head) * 16 : nullptr;
+                float* my_scale = row ? nullptr : scale + (long long)head * c.page_size;
+                for (int j0 = 0; j0 < count; j0 += kCommitBatch) {
+                    uint4 x[kCommitBatch];
+#pragma unroll
+                    for (int j = 0; j < kCommitBatch; ++j)
+                        if (j0 + j < count && s_from[j0 + j].at >= 0) {
+                            if (row) x[j] = *reinterpret_cast<const uint4*>(mine + s_from[j0 + j].at);
+                            else x[j].x = __float_as_uint(my_scale[s_from[j0 + j].scale]);
+                        }
+#pragma unroll
+                    for (int j = 0; j < kCommitBatch; ++j)
+                        if (j0 + j < count && s_from[j0 + j].at >= 0) {
+                            if (row) *reinterpret_cast<uint4*>(mine + s_to[j0 + j].at) = x[j];
+                            else my_scale[s_to[j0 + j].scale] = __uint_as_float(x[j].x);
+                        }
+                }
+            }
+        }
+        __syncthreads();
     }
     if (bad_page) atomicOr(P.dev_status, DSPARK_DEV_BAD_PAGE);
 }
@@ -357,6 +419,7 @@ int dspark_kv_write(const dspark_kv_cache_t* cache, int layer, const void* k, co
     if (((uintptr_t)k | (uintptr_t)v) & 15) return DSPARK_ERR_ALIGNMENT;
     KvStep P = {};
     P.c = kv_view(cache, layer);
+    P.heads_reciprocal = (uint32_t)(((1ull << 32) + cache->kv_heads - 1) / cache->kv_heads);
     P.first = first; P.row_offsets = row_offsets; P.R = R; P.n_rows = n_rows; P.dev_status = dev_status;
     P.k = (const unsigned char*)k; P.v = (const unsigned char*)v;
     P.row_stride = row_stride * 2; P.head_stride = head_stride * 2;
@@ -375,6 +438,7 @@ int dspark_kv_read(const dspark_kv_cache_t* cache, int layer, const int32_t* fir
     if (((uintptr_t)out_k | (uintptr_t)out_v) & 15) return DSPARK_ERR_ALIGNMENT;
     KvStep P = {};
     P.c = kv_view(cache, layer);
+    P.heads_reciprocal = (uint32_t)(((1ull << 32) + cache->kv_heads - 1) / cache->kv_heads);
     P.first = first; P.row_offsets = row_offsets; P.R = R; P.n_rows = n_rows; P.dev_status = dev_status;
     P.out_k = (unsigned char*)out_k; P.out_v = (unsigned char*)out_v; P.out_f32 = out_dtype == DSPARK_F32;
     P.row_stride = out_row_stride * es; P.head_stride = out_head_stride * es;
@@ -397,7 +461,10 @@ int dspark_kv_commit(const dspark_kv_cache_t* cache, const int32_t* first, const
     P.layer_scales = (long long)cache->n_pages * cache->kv_heads * cache->page_size;
     P.n_layers = cache->n_layers;
     KernelTimerScope timer(DSPARK_K_KV_COMMIT, (cudaStream_t)stream);
-    launch_pdl(kv_commit_kernel, dim3((unsigned)R, (unsigned)(2 * cache->n_layers)), dim3(kCommitThreads), 0, (cudaStream_t)stream, P);
+    // as many CTAs as the SMs hold at a time, eight each: more wait for the same path and pages over again
+    const int most = 8 * current_sms() / R, all = 2 * cache->n_layers;
+    const int per = most < 1 ? all : (all + most - 1) / most;             // layers' K and V of a CTA
+    launch_pdl(kv_commit_kernel, dim3((unsigned)R, (unsigned)((all + per - 1) / per)), dim3(kCommitThreads), 0, (cudaStream_t)stream, P);
     return launch_status();
 }
 

@@ -12,6 +12,7 @@ struct KvView {
     unsigned char* k; unsigned char* v;
     float* k_scale; float* v_scale;             // [n_pages][kv_heads][page_size]
     int dtype, n_pages, page_size, kv_heads, head_dim, max_pages;
+    int page_shift;                             // log2 of page_size, or -1
     long long page_stride, token_stride, head_stride;      // bytes
     const int32_t* block_table; long long table_stride;
 };
@@ -84,6 +85,8 @@ inline KvView kv_view(const dspark_kv_cache_t* c, int layer)
     v.v_scale = c->v_scale ? c->v_scale + layer * scales : nullptr;
     v.dtype = c->dtype; v.n_pages = c->n_pages; v.page_size = c->page_size; v.kv_heads = c->kv_heads;
     v.head_dim = c->head_dim; v.max_pages = c->max_pages;
+    v.page_shift = -1;
+    for (int i = 0; i < 31; ++i) if (c->page_size == 1 << i) v.page_shift = i;
     v.page_stride = c->page_stride * es; v.token_stride = c->token_stride * es; v.head_stride = c->head_stride * es;
     v.block_table = c->block_table; v.table_stride = c->block_table_stride;
     return v;
