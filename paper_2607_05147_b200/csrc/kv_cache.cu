@@ -8,15 +8,15 @@
 // and on the quotient's side of it elsewhere, and rounds to the target as the exact quotient would.
 //
 // All three are bound by memory, or, for few rows, by a chain of dependent loads: row_offsets -> first -> block_table -> store.
-// The rows are therefore read before that chain is begun.  A head's row belongs to 8, 16 or 32 neighbouring lanes, 16 bytes of
-// bf16 each, so that the maximum is a few shuffles and neighbouring heads fill whole sectors; a thread has four such rows in
-// flight.
+// The rows are therefore read before that chain is begun.  A head's row belongs to 4, 8 or 16 neighbouring lanes, two pieces of 16
+// bytes of bf16 each, so that the maximum is a few shuffles and neighbouring lanes and heads fill whole sectors; a thread has two
+// such rows in flight.  For many rows instructions come next: where a row lies is worked out by one thread of the CTA.
 #include "kv_cache.cuh"
 
 namespace dspark {
 
 constexpr int kKvThreads = 256;
-constexpr int kKvRows = 4;                       // head rows of one thread
+constexpr int kKvRows = 2;                       // head rows of one thread, two pieces of 8 components each
 
 struct KvStep {
     KvView c;
@@ -78,43 +78,47 @@ __device__ __forceinline__ float rcp_approx(float x)
 }
 
 template <int kDtype> __device__ constexpr float kv_whole() { return kDtype == DSPARK_I8 ? 127.f : 448.f; }
-// 8 of a head row's values, 8 bits each; top: the row's largest magnitude, bad: it holds NaN or an infinity
+// Two times 8 of a head row's values, 8 bits each.  top: the row's largest magnitude; bad: it holds NaN or an infinity
 template <int kLanes, int kDtype>
-__device__ __forceinline__ uint2 kv_quantise(uint4 x, float& top, bool& bad)
+__device__ __forceinline__ void kv_quantise(const uint4 (&x)[2], uint2 (&q)[2], float& top, bool& bad)
 {
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    uint32_t most = max_nan_bf16x2(max_nan_bf16x2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), max_nan_bf16x2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
+    uint32_t most = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        most = max_nan_bf16x2(most, max_nan_bf16x2(max_nan_bf16x2(x[h].x & 0x7fff7fffu, x[h].y & 0x7fff7fffu),
+                                                   max_nan_bf16x2(x[h].z & 0x7fff7fffu, x[h].w & 0x7fff7fffu)));
 #pragma unroll
     for (int o = kLanes / 2; o; o >>= 1) most = max_nan_bf16x2(most, __shfl_xor_sync(0xffffffffu, most, o));
     most = max_nan_bf16x2(most, most >> 16 | most << 16);
     top = bf16lo(most);
     bad = !(top < INFINITY);
-    uint32_t q[2] = {0, 0};
-    if (!bad && top != 0.f) {
-        // x and its maximum, both times a power of two where the reciprocal would leave the range of fp32
-        const float by = top > 1e35f ? 0x1p-16f : top < 1e-35f ? 0x1p64f : 1.f;
-        const float inverse = kv_whole<kDtype>() * rcp_approx(top * by);
-        const uint64_t by2 = pack2(by, by), inverse2 = pack2(inverse, inverse);
+    q[0] = q[1] = make_uint2(0, 0);
+    if (bad || top == 0.f) return;
+    // x and its maximum, both times a power of two where the reciprocal would leave the range of fp32
+    const float by = top > 1e35f ? 0x1p-16f : top < 1e-35f ? 0x1p64f : 1.f;
+    const float inverse = kv_whole<kDtype>() * rcp_approx(top * by);
+    const uint64_t by2 = pack2(by, by), inverse2 = pack2(inverse, inverse);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t w[4] = {x[h].x, x[h].y, x[h].z, x[h].w};
+        uint32_t r[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
+            uint64_t e = pack2(bf16lo(w[i]), bf16hi(w[i]));
+            if (by != 1.f) e = mul2(e, by2);
             float a, b;
-            unpack2(mul2(mul2(pack2(bf16lo(w[i]), bf16hi(w[i])), by2), inverse2), a, b);
+            unpack2(mul2(e, inverse2), a, b);
             a = __uint_as_float((__float_as_uint(a) + 16u) & ~31u);
             b = __uint_as_float((__float_as_uint(b) + 16u) & ~31u);
-            uint32_t two;
             if constexpr (kDtype == DSPARK_I8) {
                 // 1.5 2^23 + a: rounded to an integer, which its low bits are
-                a += 12582912.f;
-                b += 12582912.f;
-                two = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040);
-                q[i >> 1] = i & 1 ? __byte_perm(q[i >> 1], two, 0x5410) : two;
-            } else {
-                two = e4m3x2(a, b);
-                q[i >> 1] |= two << (16 * (i & 1));
-            }
+                unpack2(add2(pack2(a, b), pack2(12582912.f, 12582912.f)), a, b);
+                r[i] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040);
+            } else
+                r[i] = e4m3x2(a, b);
         }
+        q[h] = make_uint2(__byte_perm(r[0], r[1], 0x5410), __byte_perm(r[2], r[3], 0x5410));
     }
-    return make_uint2(q[0], q[1]);
 }
 // 8 values of a head row to `out` (the row's start)
 template <int kDtype>
@@ -129,8 +133,12 @@ __device__ __forceinline__ void kv_put(unsigned char* out, int sub, uint4 x, flo
     } else if constexpr (kDtype == DSPARK_I8) {
         // a byte + 128 in the low bits of 2^23
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            e[i] = (__uint_as_float(__byte_perm(w[i >> 2] ^ 0x80808080u, 0x4b000000u, 0x7440 | (i & 3))) - 8388736.f) * scale;
+        for (int i = 0; i < 8; i += 2) {
+            const uint32_t bytes = w[i >> 2] ^ 0x80808080u;
+            const float a = __uint_as_float(__byte_perm(bytes, 0x4b000000u, 0x7440 | (i & 3)));
+            const float b = __uint_as_float(__byte_perm(bytes, 0x4b000000u, 0x7441 | (i & 3)));
+            unpack2(mul2(add2(pack2(a, b), pack2(-8388736.f, -8388736.f)), pack2(scale, scale)), e[i], e[i + 1]);
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
@@ -188,36 +196,38 @@ __device__ __forceinline__ int kv_find_request(const KvRequests& q, int row)
 
 // Head rows [blockIdx.x * per, ...).
 template <int kLanes, int kDtype, bool kWrite>
-__global__ void __launch_bounds__(kKvThreads) kv_rows_kernel(const __grid_constant__ KvStep P)
+__global__ void __launch_bounds__(kKvThreads, 6) kv_rows_kernel(const __grid_constant__ KvStep P)
 {
     constexpr int kPer = kKvThreads / kLanes;
-    constexpr int kMost = kPer * kKvRows / 2 + 1;              // rows that a CTA has a part of
+    constexpr int kMost = kPer * kKvRows / 2 + 1;             // rows that a CTA has a part of
     __shared__ KvRequestsShared S;
-    __shared__ KvSlot slots[kMost];                            // of head 0; at = -1: the row is left alone, -2: it has no page
+    __shared__ KvSlot slots[kMost];                           // of head 0; at = -1: the row is left alone, -2: it has no page
     pdl_wait();
     const int tid = threadIdx.x, sub = tid & (kLanes - 1), slot = tid / kLanes;
     const int heads = P.c.kv_heads;
     // index = (row * 2 + (0: K, 1: V)) * heads + head; a product with the reciprocal divides, exact for a CTA's few thousand
     const long long total = (long long)P.n_rows * 2 * heads, base = (long long)blockIdx.x * (kPer * kKvRows);
-    const int row0 = (int)(base / (2 * heads)), base_in = (int)(base - (long long)row0 * 2 * heads);
-    const bool in = sub * 8 < P.c.head_dim;
-    int local[kKvRows], head[kKvRows];           // row - row0
-    bool value[kKvRows], live[kKvRows];
-    uint4 x[kKvRows];
-    const unsigned char* k_in = P.k + row0 * P.row_stride;
-    const unsigned char* v_in = P.v + row0 * P.row_stride;
+    const int row0 = total >> 32 ? (int)(base / (2 * heads)) : (int)((uint32_t)base / (uint32_t)(2 * heads));
+    const int base_in = (int)(base - (long long)row0 * 2 * heads);
+    struct Place { int local, head; bool value, live; };                    // local: row - row0
+    auto place = [&](int j) {
+        const uint32_t i = base_in + j * kPer + slot, at = heads == 1 ? i : __umulhi(i, P.heads_reciprocal);
+        return Place{(int)(at >> 1), (int)(i - at * heads), (at & 1) != 0, base + j * kPer + slot < total};
+    };
+    auto in = [&](int h) { return (sub + h * kLanes) * 8 < P.c.head_dim; };       // piece h of this thread exists
+    uint4 x[kKvRows][2];
+    if (kWrite) {
+        const unsigned char* k_in = P.k + row0 * P.row_stride + sub * 16;
+        const unsigned char* v_in = P.v + row0 * P.row_stride + sub * 16;
 #pragma unroll
-    for (int j = 0; j < kKvRows; ++j) {
-        const uint32_t i = base_in + j * kPer + slot;
-        live[j] = base + j * kPer + slot < total;
-        const uint32_t at = heads == 1 ? i : __umulhi(i, P.heads_reciprocal);
-        local[j] = (int)(at >> 1);
-        value[j] = at & 1;
-        head[j] = (int)(i - at * heads);
-        if (kWrite) {
-            x[j] = make_uint4(0, 0, 0, 0);
-            if (live[j] && in)
-                x[j] = *reinterpret_cast<const uint4*>((value[j] ? v_in : k_in) + local[j] * P.row_stride + head[j] * P.head_stride + sub * 16);
+        for (int j = 0; j < kKvRows; ++j) {
+            const Place p = place(j);
+            const unsigned char* from = (p.value ? v_in : k_in) + p.local * P.row_stride + p.head * P.head_stride;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                x[j][h] = make_uint4(0, 0, 0, 0);
+                if (p.live && in(h)) x[j][h] = *reinterpret_cast<const uint4*>(from + h * kLanes * 16);
+            }
         }
     }
     // where the CTA's rows are in the cache, one thread a row
@@ -237,30 +247,28 @@ __global__ void __launch_bounds__(kKvThreads) kv_rows_kernel(const __grid_consta
         slots[tid] = at;
     }
     __syncthreads();
-    KvSlot s[kKvRows];
-    bool there[kKvRows];
-#pragma unroll
-    for (int j = 0; j < kKvRows; ++j) {
-        s[j] = slots[local[j]];
-        live[j] = live[j] && s[j].at != -1;
-        there[j] = live[j] && s[j].at >= 0;
-        s[j].at += head[j] * P.c.head_stride;
-        s[j].scale += head[j] * P.c.page_size;
-    }
 
     if constexpr (kWrite) {
 #pragma unroll
         for (int j = 0; j < kKvRows; ++j) {
-            unsigned char* cache = value[j] ? P.c.v : P.c.k;
+            const Place p = place(j);
+            const KvSlot s = slots[p.local];
+            const bool store = p.live && s.at >= 0;
+            unsigned char* to = (p.value ? P.c.v : P.c.k) + s.at + p.head * P.c.head_stride;
             if constexpr (kDtype == DSPARK_BF16) {
-                if (there[j] && in) *reinterpret_cast<uint4*>(cache + s[j].at + sub * 16) = x[j];
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    if (store && in(h)) *reinterpret_cast<uint4*>(to + (sub + h * kLanes) * 16) = x[j][h];
             } else {
                 bool bad;
                 float top;
-                const uint2 q = kv_quantise<kLanes, kDtype>(x[j], top, bad);
-                if (there[j] && in) {
-                    *reinterpret_cast<uint2*>(cache + s[j].at + sub * 8) = q;
-                    if (sub == 0) (value[j] ? P.c.v_scale : P.c.k_scale)[s[j].scale] = bad ? NAN : top / kv_whole<kDtype>();
+                uint2 q[2];
+                kv_quantise<kLanes, kDtype>(x[j], q, top, bad);
+                if (store) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        if (in(h)) *reinterpret_cast<uint2*>(to + (sub + h * kLanes) * 8) = q[h];
+                    if (sub == 0) (p.value ? P.c.v_scale : P.c.k_scale)[s.scale + p.head * P.c.page_size] = bad ? NAN : top / kv_whole<kDtype>();
                 }
             }
         }
@@ -268,22 +276,35 @@ __global__ void __launch_bounds__(kKvThreads) kv_rows_kernel(const __grid_consta
         float scale[kKvRows];                               // all loads first
 #pragma unroll
         for (int j = 0; j < kKvRows; ++j) {
-            x[j] = make_uint4(0, 0, 0, 0);
+            const Place p = place(j);
+            const KvSlot s = slots[p.local];
+            x[j][0] = x[j][1] = make_uint4(0, 0, 0, 0);
             scale[j] = 0.f;
-            if (there[j] && in) {
-                const unsigned char* cache = value[j] ? P.c.v : P.c.k;
-                if constexpr (kDtype == DSPARK_BF16) x[j] = *reinterpret_cast<const uint4*>(cache + s[j].at + sub * 16);
-                else {
-                    const uint2 q = *reinterpret_cast<const uint2*>(cache + s[j].at + sub * 8);
-                    x[j].x = q.x; x[j].y = q.y;
-                    scale[j] = (value[j] ? P.c.v_scale : P.c.k_scale)[s[j].scale];
+            if (p.live && s.at >= 0) {
+                const unsigned char* from = (p.value ? P.c.v : P.c.k) + s.at + p.head * P.c.head_stride;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (!in(h)) continue;
+                    if constexpr (kDtype == DSPARK_BF16) x[j][h] = *reinterpret_cast<const uint4*>(from + (sub + h * kLanes) * 16);
+                    else {
+                        const uint2 q = *reinterpret_cast<const uint2*>(from + (sub + h * kLanes) * 8);
+                        x[j][h].x = q.x; x[j][h].y = q.y;
+                    }
+                }
+                if constexpr (kDtype != DSPARK_BF16) {
+                    scale[j] = (p.value ? P.c.v_scale : P.c.k_scale)[s.scale + p.head * P.c.page_size];
                 }
             }
         }
 #pragma unroll
         for (int j = 0; j < kKvRows; ++j) {
-            unsigned char* out = value[j] ? P.out_v : P.out_k;
-            if (live[j] && in && out) kv_put<kDtype>(out + row0 * P.row_stride + local[j] * P.row_stride + head[j] * P.head_stride, sub, x[j], scale[j], P.out_f32);
+            const Place p = place(j);
+            unsigned char* out = p.value ? P.out_v : P.out_k;
+            if (!p.live || !out || slots[p.local].at == -1) continue;
+            out += (row0 + p.local) * P.row_stride + p.head * P.head_stride;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (in(h)) kv_put<kDtype>(out, sub + h * kLanes, x[j][h], scale[j], P.out_f32);
         }
     }
     if (blockIdx.x == 0) kv_report(P.first, P.row_offsets, P.R, P.n_rows, capacity, P.dev_status);
@@ -302,9 +323,9 @@ template <bool kWrite>
 static int kv_rows(const KvStep& P, cudaStream_t s)
 {
     KernelTimerScope timer(kWrite ? DSPARK_K_KV_WRITE : DSPARK_K_KV_READ, s);
-    if (P.c.head_dim <= 64) kv_rows_launch<8, kWrite>(P, s);
-    else if (P.c.head_dim <= 128) kv_rows_launch<16, kWrite>(P, s);
-    else kv_rows_launch<32, kWrite>(P, s);
+    if (P.c.head_dim <= 64) kv_rows_launch<4, kWrite>(P, s);
+    else if (P.c.head_dim <= 128) kv_rows_launch<8, kWrite>(P, s);
+    else kv_rows_launch<16, kWrite>(P, s);
     return launch_status();
 }
 
