@@ -532,85 +532,93 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
 }
 
 // ---- joining the parts of divided units ------------------------------------------------------------------
-// A warp a row: the parts' references and sums first, then the weighted sum of their accumulators, in the order of the CTAs.
-constexpr int kJoinThreads = 256;
+// A row's references and sums first, then the weighted sum of its parts' accumulators, in the order of the CTAs.  Where there are
+// many units each has few parts: a warp a row, and blockIdx.x is the CTA whose end divided the unit.  Where there are few, a unit can
+// have a part of every SM: all warps of a CTA for a row, and blockIdx.x counts the divided units.
+constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
 
+template <int kWarps>                            // of a row
 __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const __grid_constant__ AttnParams P, int ctas)
 {
-    __shared__ int4 s_cut[kAttnSms];
-    __shared__ int s_cta[kAttnSms], s_start[kAttnSms + 1], s_cuts;
+    __shared__ int s_count[kJoinWarps], s_cta;
+    __shared__ __align__(16) float s_o[kWarps][kAttnMaxDim];
+    __shared__ float s_sum[kWarps];
+    static_assert(kAttnSms <= kJoinThreads, "a cut a thread");
     pdl_wait();
-    const int tid = threadIdx.x, lane = tid & 31;
-    if (tid < 32) {
-        int n = 0, rows = 0;
-        for (int b0 = 0; b0 < ctas; b0 += 32) {
-            const int b = b0 + lane;
-            int4 cut = make_int4(0, 0, 0, 0);
-            if (b < ctas) cut = P.cuts[b];
-            const uint32_t some = __ballot_sync(0xffffffffu, cut.x != 0);
-            int mine = cut.x ? cut.w * P.group : 0, upto = mine;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    int b = blockIdx.x;
+    if constexpr (kWarps > 1) {
+        const bool some = tid < ctas && P.cuts[tid].x != 0;
+        const uint32_t all = __ballot_sync(0xffffffffu, some);
+        if (lane == 0) s_count[warp] = __popc(all);
+        if (tid == 0) s_cta = -1;
+        __syncthreads();
+        int before = 0;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, upto, o);
-                if (lane >= o) upto += y;
-            }
-            if (cut.x) {
-                const int at = n + __popc(some & ((1u << lane) - 1u));
-                s_cut[at] = cut;
-                s_cta[at] = b;
-                s_start[at] = rows + upto - mine;
-            }
-            n += __popc(some);
-            rows += __shfl_sync(0xffffffffu, upto, 31);
-        }
-        if (lane == 0) { s_cuts = n; s_start[n] = rows; }
+        for (int w = 0; w < kJoinWarps; ++w) before += w < warp ? s_count[w] : 0;
+        if (some && before + __popc(all & ((1u << lane) - 1u)) == (int)blockIdx.x) s_cta = tid;
+        __syncthreads();
+        b = s_cta;
+        if (b < 0) return;
     }
-    __syncthreads();
-    const int cuts = s_cuts, d = P.c.head_dim, tile_rows = P.tile_nodes * P.group;
-    const int rows = s_start[cuts];
-    int at = 0;
-    for (int w = blockIdx.x * (kJoinThreads / 32) + (tid >> 5); w < rows; w += gridDim.x * (kJoinThreads / 32)) {
-        while (s_start[at + 1] <= w) ++at;
-        const int4 cut = s_cut[at];
-        const int b = s_cta[at], i = w - s_start[at], node = i / P.group;
-        const int parts = cut.y - b + 2;
-        const int row = i < tile_rows ? i : kAttnTile + i - tile_rows;       // its place in a partial result
-        auto place = [&](int k) { return (long long)(k == 0 ? 2 * (b - 1) + 1 : 2 * (b - 1 + k)) * P.part_rows + row; };
-        float top = -INFINITY;
-        for (int k = lane; k < parts; k += 32) top = fmaxf(top, P.part_stats[place(k)].x);
-        top = warp_max_f32(top);
-        const float base = top == -INFINITY ? 0.f : top;
-        float sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int k0 = 0; k0 < parts; k0 += 32) {
-            float2 s = make_float2(-INFINITY, 0.f);
-            if (k0 + lane < parts) s = P.part_stats[place(k0 + lane)];
-            const float f = ex2_approx(s.x - base);
-            sum += s.y * f;
-            const int here = min(32, parts - k0);
-            for (int k = 0; k < here; k += 4) {
-                float4 x[4];
+    const int4 cut = P.cuts[b];
+    const int d = P.c.head_dim, tile_rows = P.tile_nodes * P.group, i = kWarps > 1 ? blockIdx.y : blockIdx.y * kJoinWarps + warp;
+    if (cut.x == 0 || i >= cut.w * P.group) return;
+    const int node = i / P.group, parts = cut.y - b + 2, at = lane * 4;
+    const int row = i < tile_rows ? i : kAttnTile + i - tile_rows;           // its place in a partial result
+    auto place = [&](int k) { return (long long)(k == 0 ? 2 * (b - 1) + 1 : 2 * (b - 1 + k)) * P.part_rows + row; };
+    const int k_first = kWarps > 1 ? warp : 0;
+    constexpr int kBatch = 4;
+    float4 x[kBatch];
+    float2 s[kBatch];
+    auto ask = [&](int k0) {
 #pragma unroll
-                for (int m = 0; m < 4; ++m)
-                    if (k + m < here && lane * 4 < d) x[m] = *reinterpret_cast<const float4*>(P.parts + place(k0 + k + m) * d + lane * 4);
-#pragma unroll
-                for (int m = 0; m < 4; ++m) {
-                    const float g = __shfl_sync(0xffffffffu, f, (k + m) & 31);
-                    if (k + m < here && lane * 4 < d) {
-                        o[0] = fmaf(x[m].x, g, o[0]); o[1] = fmaf(x[m].y, g, o[1]);
-                        o[2] = fmaf(x[m].z, g, o[2]); o[3] = fmaf(x[m].w, g, o[3]);
-                    }
-                }
-            }
+        for (int m = 0; m < kBatch; ++m) {
+            const int k = k0 + m * kWarps;
+            x[m] = make_float4(0.f, 0.f, 0.f, 0.f);
+            s[m] = make_float2(-INFINITY, 0.f);
+            if (k >= parts) continue;
+            s[m] = P.part_stats[place(k)];
+            if (at < d) x[m] = *reinterpret_cast<const float4*>(P.parts + place(k) * d + at);
         }
-        sum = warp_sum_f32(sum);
-        const float inverse = 1.f / sum;
-        const int head = (cut.x - 1) * P.group + i % P.group;
-        const long long out_row = cut.z + node;
-        if (lane * 4 < d)
-            *reinterpret_cast<uint2*>(P.out + out_row * P.out_row + head * P.out_head + lane * 8) =
-                make_uint2(pack16<false>(o[0] * inverse, o[1] * inverse), pack16<false>(o[2] * inverse, o[3] * inverse));
-        if (P.out_lse && lane == 0) P.out_lse[out_row * P.q_heads + head] = (top + log2f(sum)) * 0.6931471805599453f;
+    };
+    ask(k_first);
+    float top = -INFINITY;
+    for (int k = lane; k < parts; k += 32) top = fmaxf(top, P.part_stats[place(k)].x);
+    top = warp_max_f32(top);
+    const float base = top == -INFINITY ? 0.f : top;
+    float sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int k0 = k_first; k0 < parts; k0 += kBatch * kWarps) {
+        if (k0 != k_first) ask(k0);
+#pragma unroll
+        for (int m = 0; m < kBatch; ++m) {
+            if (k0 + m * kWarps >= parts) continue;
+            const float g = ex2_approx(s[m].x - base);
+            sum = fmaf(s[m].y, g, sum);
+            o[0] = fmaf(x[m].x, g, o[0]); o[1] = fmaf(x[m].y, g, o[1]);
+            o[2] = fmaf(x[m].z, g, o[2]); o[3] = fmaf(x[m].w, g, o[3]);
+        }
     }
+    if constexpr (kWarps > 1) {
+        if (at < d) *reinterpret_cast<float4*>(&s_o[warp][at]) = make_float4(o[0], o[1], o[2], o[3]);
+        if (lane == 0) s_sum[warp] = sum;
+        __syncthreads();
+        if (warp != 0) return;
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) {
+            sum += s_sum[w];
+            if (at < d)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) o[c] += s_o[w][at + c];
+        }
+    }
+    const float inverse = 1.f / sum;
+    const int head = (cut.x - 1) * P.group + i % P.group;
+    const long long out_row = cut.z + node;
+    if (at < d)
+        *reinterpret_cast<uint2*>(P.out + out_row * P.out_row + head * P.out_head + lane * 8) =
+            make_uint2(pack16<false>(o[0] * inverse, o[1] * inverse), pack16<false>(o[2] * inverse, o[3] * inverse));
+    if (P.out_lse && lane == 0) P.out_lse[out_row * P.q_heads + head] = (top + log2f(sum)) * 0.6931471805599453f;
 }
 
 // ---- host side -------------------------------------------------------------------------------------------
@@ -736,7 +744,13 @@ int dspark_tree_attention(const dspark_kv_cache_t* cache, int layer, const void*
     else rc = attn_launch<kAttnE4M3>(P, map_k, map_v, sms, s);
     if (rc) return rc;
     KernelTimerScope timer(DSPARK_K_TREE_COMBINE, s);
-    launch_pdl(attn_join_kernel, dim3((unsigned)(2 * sms)), dim3(kJoinThreads), 0, s, P, sms);
+    // at most this many units, one of n_rows / unit_nodes whole ones or the last of a request for each K/V head
+    const long long units = ((long long)n_rows / P.unit_nodes + R) * cache->kv_heads;
+    const int join_rows = (n_rows < P.unit_nodes ? n_rows : P.unit_nodes) * P.group;
+    // (one unit of 16 rows over 20000 positions: 18.7 us with a CTA a row for both kernels, 34 with a warp; 8 units of 256 rows: a CTA a
+    // row would be 2048 of them, 257.6 us instead of 253.5)
+    if (units * 8 <= sms && units * join_rows <= 8 * sms) launch_pdl(attn_join_kernel<kJoinWarps>, dim3((unsigned)units, (unsigned)join_rows), dim3(kJoinThreads), 0, s, P, sms);
+    else launch_pdl(attn_join_kernel<1>, dim3((unsigned)sms, (unsigned)((join_rows + kJoinWarps - 1) / kJoinWarps)), dim3(kJoinThreads), 0, s, P, sms);
     return launch_status();
 }
 
