@@ -187,7 +187,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                 float up = 1.f;
                 if constexpr (kNarrow) {
                     float top = 0.f;
-#pragma unroll 4
+#pragma unroll 8
                     for (int c = 0; c < d / 8; ++c) {
                         const uint4 x = src[c];
                         const uint32_t w4[4] = {x.x, x.y, x.z, x.w};
@@ -282,11 +282,18 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                     if (!any) factor = scales.q[tile][row];                 // stored before Q was announced
                     if (!masked) above = attn_exponent(warp_max_f32(attn_finite_max(reinterpret_cast<const float4*>(all)[lane], ~0u, 0.f)));
                     else {                       // of the positions that this row sees
-                        float top = 0.f;
+                        __syncwarp();
+                        float top = 0.f, own = attn_finite_max(reinterpret_cast<const float4*>(all)[lane], ~0u, 0.f);
 #pragma unroll
-                        for (int w = 0; w < 4; ++w)
-#pragma unroll 1
-                            for (int i = 0; i < 32; i += 4) top = attn_finite_max(*reinterpret_cast<const float4*>(all + w * 32 + i), seen[w] >> i, top);
+                        for (int o = 1; o < 8; o <<= 1) own = fmaxf(own, __shfl_xor_sync(0xffffffffu, own, o));     // of 32 positions
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            const float all_32 = __shfl_sync(0xffffffffu, own, w * 8);
+                            if (__all_sync(0xffffffffu, seen[w] == ~0u)) top = fmaxf(top, all_32);
+                            else if (__any_sync(0xffffffffu, seen[w] != 0u))
+#pragma unroll 2
+                                for (int i = 0; i < 32; i += 4) top = attn_finite_max(*reinterpret_cast<const float4*>(all + w * 32 + i), seen[w] >> i, top);
+                        }
                         above = attn_exponent(top);
                     }
                     above -= kAttnNarrowOffset;

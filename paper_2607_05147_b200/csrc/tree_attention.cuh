@@ -432,20 +432,16 @@ __device__ __forceinline__ void attn_produce(const AttnParams& P, AttnIter it, c
         }
 }
 
-// Where 16 bytes x of an 8-bit tile come from and go to (and the next 16 beside).  Eight lanes store to eight different places of a
-// line of 128 bytes: the pieces of two neighbouring positions, which the swizzle parts by an odd number of places; with 128
-// components one position's lie in the other chunk, so that the loads' banks differ too.
-__device__ __forceinline__ void widen_place(int x, int d, int& token, int& from, int& to)
+// Where 16 bytes x of an 8-bit tile of 64 or 128 components come from and go to (and the next 16 beside).  Eight lanes store to eight
+// different places of a line of 128 bytes: the pieces of two neighbouring positions, which the swizzle parts by an odd number of
+// places; with 128 components one position's lie in the other chunk, so that the loads' banks differ too.
+__device__ __forceinline__ void widen_place(int x, int d, int& from, int& to)
 {
-    const int pieces = d / 16;
-    int piece;
-    if (pieces == 8) {
+    int token = x >> 2, piece = x & 3;
+    if (d == 128) {
         const int odd = x >> 2 & 1;
         token = (x >> 4) * 2 + odd;
         piece = ((x >> 3 & 1) ^ odd) * 4 + (x & 3);
-    } else {
-        token = x / pieces;
-        piece = x - token * pieces;
     }
     from = token * d + piece * 16;
     to = (piece >> 2) * kChunkBytes + token * 128 + ((((piece & 3) * 2) ^ (token & 7)) << 4);
@@ -457,28 +453,41 @@ __device__ __forceinline__ void widen16(uint4 w, unsigned char* dst, int to)
     *reinterpret_cast<uint4*>(dst + to) = make_uint4(a.x, a.y, b.x, b.y);
     *reinterpret_cast<uint4*>(dst + (to ^ 16)) = make_uint4(c.x, c.y, e.x, e.y);
 }
-// A tile by kThreads threads; of 64 or 128 components (kDim) a thread's pieces are a fixed number of positions apart.
+// A tile of 64 or 128 components (kDim) by kThreads threads, a thread's pieces a fixed number of positions apart.
 template <int kKind, int kThreads, int kDim>
-__device__ __forceinline__ void widen_tile(const unsigned char* src, unsigned char* dst, int ct, int from0, int to0, int d)
+__device__ __forceinline__ void widen_tile(const unsigned char* src, unsigned char* dst, int from0, int to0)
 {
-    if constexpr (kDim > 0) {
-        constexpr int kPieces = kAttnTile * kDim / 16 / kThreads, kApart = kThreads * 16 / kDim, kBatch = kPieces < 4 ? kPieces : 4;
+    constexpr int kPieces = kAttnTile * kDim / 16 / kThreads, kApart = kThreads * 16 / kDim, kBatch = kPieces < 4 ? kPieces : 4;
 #pragma unroll
-        for (int i0 = 0; i0 < kPieces; i0 += kBatch) {
-            uint4 w[kBatch];
+    for (int i0 = 0; i0 < kPieces; i0 += kBatch) {
+        uint4 w[kBatch];
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) w[i] = *reinterpret_cast<const uint4*>(src + from0 + (i0 + i) * kApart * kDim);
+        for (int i = 0; i < kBatch; ++i) w[i] = *reinterpret_cast<const uint4*>(src + from0 + (i0 + i) * kApart * kDim);
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) widen16<kKind>(w[i], dst, to0 + (i0 + i) * kApart * 128);
-        }
-    } else {
-#pragma unroll 2
-        for (int x = ct; x < kAttnTile * d / 16; x += kThreads) {
-            int token, from, to;
-            widen_place(x, d, token, from, to);
-            widen16<kKind>(*reinterpret_cast<const uint4*>(src + from), dst, to);
-        }
+        for (int i = 0; i < kBatch; ++i) widen16<kKind>(w[i], dst, to0 + (i0 + i) * kApart * 128);
     }
+}
+// A position of a tile of any width, or of a tile's end: zeros where it does not exist; `look`: NaN becomes zero (true: there was some).
+template <int kKind>
+__device__ __forceinline__ bool widen_position(const unsigned char* src, unsigned char* dst, int token, int d, bool exists, bool look)
+{
+    bool any = false;
+#pragma unroll 2
+    for (int piece = 0; piece < d / 16; ++piece) {
+        uint4 x = *reinterpret_cast<const uint4*>(src + token * d + piece * 16);
+        if (!exists) x = make_uint4(0, 0, 0, 0);
+        if (kKind == kAttnE4M3 && look) {
+            uint32_t* w[4] = {&x.x, &x.y, &x.z, &x.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                // bytes of 0x7f or 0xff: the only ones that carry into their highest bit
+                const uint32_t bad = ((*w[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+                if (bad) { *w[i] &= ~(bad | (bad - (bad >> 7))); any = true; }
+            }
+        }
+        widen16<kKind>(x, dst, (piece >> 2) * kChunkBytes + token * 128 + ((((piece & 3) * 2) ^ (token & 7)) << 4));
+    }
+    return any;
 }
 // A position's components (line: its place in an 8-bit tile) as fp16 into this thread's lane of tensor memory, two a column.  The copy
 // engine's swizzle has parted the lines of 64 and 128 bytes, so that eight lanes read different banks.  Of 64 or 128 components
@@ -521,8 +530,9 @@ __device__ __forceinline__ bool attn_widen(const AttnParams& P, AttnIter it, int
                                            Ready ready)
 {
     const int lane = threadIdx.x & 31, d = P.c.head_dim;
-    int number = 0, unit = 0, token0, from0, to0;
-    widen_place(ct, d, token0, from0, to0);
+    static_assert(kThreads == kAttnTile, "a position a thread");
+    int number = 0, unit = 0, from0, to0;
+    widen_place(ct, d, from0, to0);
     RingPlace at[2], from_raw[2];
     AttnUnit u;
     while (!*abort_flag && it.next(P, u)) {
@@ -545,33 +555,13 @@ __device__ __forceinline__ bool attn_widen(const AttnParams& P, AttnIter it, int
                     if (d == 128) widen_line<kKind, 128>(src + token * d, token, d, to);
                     else if (d == 64) widen_line<kKind, 64>(src + token * d, token, d, to);
                     else widen_line<kKind, 0>(src + token * d, token, d, to);
-                } else if (d == 128) widen_tile<kKind, kThreads, 128>(src, dst, ct, from0, to0, d);
-                else if (d == 64) widen_tile<kKind, kThreads, 64>(src, dst, ct, from0, to0, d);
-                else widen_tile<kKind, kThreads, 0>(src, dst, ct, from0, to0, d);
-                if ((kv || !kTensorK) && (valid < kAttnTile || (kKind == kAttnE4M3 && kv && tree < kAttnTile))) {
+                } else {
                     // positions that do not exist: zeros; a NaN among the nodes' values of V: zero here and back in the rows that see
-                    // it (attn_bad_values).  Every thread looks at what it has written.
-#pragma unroll 1
-                    for (int x = ct; x < kAttnTile * d / 16; x += kThreads) {
-                        int token, from, to;
-                        widen_place(x, d, token, from, to);
-#pragma unroll 1
-                        for (int k = 0; k < 2; ++k) {
-                            uint4* p = reinterpret_cast<uint4*>(dst + (to ^ (k * 16)));
-                            if (token >= valid) *p = make_uint4(0, 0, 0, 0);
-                            else if (kKind == kAttnE4M3 && kv && token >= tree) {
-                                uint4 y = *p;
-                                uint32_t* h[4] = {&y.x, &y.y, &y.z, &y.w};
-                                bool bad = false;
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) {
-                                    if ((*h[i] & 0x7c00u) == 0x7c00u) { *h[i] &= 0xffff0000u; bad = true; }
-                                    if ((*h[i] & 0x7c000000u) == 0x7c000000u) { *h[i] &= 0xffffu; bad = true; }
-                                }
-                                if (bad) { *p = y; bad_value[unit % kAttnUnitFlags] = 1; }
-                            }
-                        }
-                    }
+                    // it (attn_bad_values)
+                    const bool look = kKind == kAttnE4M3 && kv && tree < kAttnTile;
+                    if (d == 128 && valid == kAttnTile && !look) widen_tile<kKind, kThreads, 128>(src, dst, from0, to0);
+                    else if (d == 64 && valid == kAttnTile && !look) widen_tile<kKind, kThreads, 64>(src, dst, from0, to0);
+                    else if (widen_position<kKind>(src, dst, ct, d, ct < valid, look && ct >= tree)) bad_value[unit % kAttnUnitFlags] = 1;
                 }
                 fence_async_smem();
                 __syncwarp();
