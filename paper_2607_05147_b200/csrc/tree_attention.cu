@@ -33,7 +33,7 @@ struct AttnShared {
     int abort, bad_value[kAttnUnitFlags];
     AttnList list;
     float2 second[kAttnTile];                    // (reference, sum) of the second group
-    float of_half[2][2][kAttnTile];              // what the two threads of a row tell one another: largest scores, sums
+    float of_half[2][2][kAttnTile], q_half[2][2][kAttnTile];  // what the two threads of a row tell one another: largest scores, sums; of Q
 };
 template <int kKind>
 struct AttnScales {                              // q: per row; bad: a bit for a node's position with a scale that is no number
@@ -67,7 +67,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
     if (tid == 0) {
         for (int s = 0; s < slots; ++s) { mbar_init(&S.full[s], kNarrow ? kAttnConverters : 1); mbar_init(&S.empty[s], 1); }
         for (int s = 0; s < P.raw_k + P.raw_v; ++s) { mbar_init(&S.raw_full[s], 1); mbar_init(&S.raw_empty[s], kAttnConverters); }
-        mbar_init(&S.q_full, kRowWarps / 2);
+        mbar_init(&S.q_full, kRowWarps);
         for (int t = 0; t < 2; ++t) { mbar_init(&S.s_full[t], 1); mbar_init(&S.p_full[t], kRowWarps / 2); mbar_init(&S.o_full[t], 1); }
         for (int i = 0; i < kAttnUnitFlags; ++i) S.bad_value[i] = 0;
         mbar_init(&S.merge_ready, kRowWarps / 2); mbar_init(&S.merge_done, kRowWarps / 2); mbar_init(&S.mma_done, 1);
@@ -176,32 +176,37 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
         auto wait = [&](uint64_t* bar, uint32_t ph) { ok = ok && mbar_wait_bounded(bar, ph); };      // each lane for itself
         auto arrive = [&](uint64_t* bar) { __syncwarp(); if (lane == 0) mbar_arrive(bar); };
         auto vote = [&](bool x) { return barrier_any<64>(pair_id + 1, x); };
-        // Row `row` of row tile `tile` of a unit into shared memory; in 8-bit mode as fp16, scaled by a power of two so that no
-        // value passes the range and what is lost is below 2^-37 of the row's largest.
+        // This thread's half of row `row` of row tile `tile` of a unit into shared memory; in 8-bit mode as fp16, scaled by a power of
+        // two so that no value passes the range and what is lost is below 2^-37 of the row's largest.
         auto load_q = [&](const AttnUnit& w, int tile) {
-            const int node = w.node0 + tile * tile_nodes + row / P.group;
-            if (row < tile_nodes * P.group && node < w.n) {
-                const uint4* src = reinterpret_cast<const uint4*>(P.q + (long long)(w.row0 + node) * P.q_row +
-                                                                  (long long)(w.head * P.group + row % P.group) * P.q_head);
-                unsigned char* dst = sQ + tile * tile_bytes + row * 128;
-                float up = 1.f;
-                if constexpr (kNarrow) {
-                    float top = 0.f;
-#pragma unroll 8
-                    for (int c = 0; c < d / 8; ++c) {
-                        const uint4 x = src[c];
+            const int node = w.node0 + tile * tile_nodes + row / P.group, pieces = d / 16;
+            const bool there = row < tile_nodes * P.group && node < w.n;
+            const uint4* src = reinterpret_cast<const uint4*>(P.q + (long long)(w.row0 + node) * P.q_row +
+                                                              (long long)(w.head * P.group + row % P.group) * P.q_head) + half * pieces;
+            unsigned char* dst = sQ + tile * tile_bytes + row * 128;
+            float up = 1.f;
+            if constexpr (kNarrow) {
+                float top = 0.f;
+                if (there)
+#pragma unroll 4
+                    for (int i = 0; i < pieces; ++i) {
+                        const uint4 x = src[i];
                         const uint32_t w4[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(bf16lo(w4[i])), fabsf(bf16hi(w4[i]))));
+                        for (int k = 0; k < 4; ++k) top = max3(top, fabsf(bf16lo(w4[k])), fabsf(bf16hi(w4[k])));
                     }
-                    // 2^e with the largest value below 2^14: exponent field of top to that of 2^13; at most 2^60
-                    const int e = min(127 + 60, max(1, 254 + 13 - (int)(__float_as_uint(top) >> 23)));
-                    up = __uint_as_float((uint32_t)e << 23);
-                    scales.q[tile][row] = __uint_as_float((uint32_t)(254 - e) << 23);   // the inverse power
-                }
+                S.q_half[t][half][row] = top;
+                barrier_any<64>(pair_id + 1, false);
+                top = fmaxf(top, S.q_half[t][half ^ 1][row]);
+                // 2^e with the largest value below 2^14: exponent field of top to that of 2^13; at most 2^60
+                const int e = min(127 + 60, max(1, 254 + 13 - (int)(__float_as_uint(top) >> 23)));
+                up = __uint_as_float((uint32_t)e << 23);
+                if (there && !half) scales.q[tile][row] = __uint_as_float((uint32_t)(254 - e) << 23);   // the inverse power
+            }
+            if (there)
 #pragma unroll 4
-                for (int c = 0; c < d / 8; ++c) {
-                    uint4 x = src[c];
+                for (int i = 0; i < pieces; ++i) {
+                    uint4 x = src[i];
                     if (kNarrow) {
                         x.x = pack16<true>(bf16lo(x.x) * up, bf16hi(x.x) * up);
                         x.y = pack16<true>(bf16lo(x.y) * up, bf16hi(x.y) * up);
@@ -209,15 +214,14 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                         x.w = pack16<true>(bf16lo(x.w) * up, bf16hi(x.w) * up);
                     }
                     x.x ^= P.q_sign; x.y ^= P.q_sign; x.z ^= P.q_sign; x.w ^= P.q_sign;
+                    const int c = half * pieces + i;
                     *reinterpret_cast<uint4*>(dst + (c >> 3) * kChunkBytes + (((c & 7) ^ (row & 7)) << 4)) = x;
                 }
-            }
             fence_async_smem();
         };
         bool have = it.next(P, u);
         // Q of the first unit; afterwards each unit's is loaded at the end of the one before
         auto prepare_q = [&](const AttnUnit& w) {
-            if (half) return;
             if (w.pair) load_q(w, t);
             else if (t == 1) load_q(w, 0);
             arrive(&S.q_full);
@@ -282,17 +286,42 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                     if (!any) factor = scales.q[tile][row];                 // stored before Q was announced
                     if (!masked) above = attn_exponent(warp_max_f32(attn_finite_max(reinterpret_cast<const float4*>(all)[lane], ~0u, 0.f)));
                     else {                       // of the positions that this row sees
+                        // every lane has four positions' scales: the largest up to each (a chain), or of those before the step (a tree)
                         __syncwarp();
-                        float top = 0.f, own = attn_finite_max(reinterpret_cast<const float4*>(all)[lane], ~0u, 0.f);
+                        const float4 mine = reinterpret_cast<const float4*>(all)[lane];
+                        const int before = P.parents ? u.first - start - lane * 4 : 4;     // that many of the four
+                        float upto[4], top = 0.f;
 #pragma unroll
-                        for (int o = 1; o < 8; o <<= 1) own = fmaxf(own, __shfl_xor_sync(0xffffffffu, own, o));     // of 32 positions
+                        for (int i = 0; i < 4; ++i) {
+                            const float x = i == 0 ? mine.x : i == 1 ? mine.y : i == 2 ? mine.z : mine.w;
+                            upto[i] = top = i < before && x < INFINITY ? fmaxf(top, x) : top;
+                        }
 #pragma unroll
-                        for (int w = 0; w < 4; ++w) {
-                            const float all_32 = __shfl_sync(0xffffffffu, own, w * 8);
-                            if (__all_sync(0xffffffffu, seen[w] == ~0u)) top = fmaxf(top, all_32);
-                            else if (__any_sync(0xffffffffu, seen[w] != 0u))
-#pragma unroll 2
-                                for (int i = 0; i < 32; i += 4) top = attn_finite_max(*reinterpret_cast<const float4*>(all + w * 32 + i), seen[w] >> i, top);
+                        for (int o = 1; o < 32; o <<= 1) {
+                            const float x = __shfl_up_sync(0xffffffffu, top, o);
+                            if (lane >= o) top = fmaxf(top, x);
+                        }
+                        if (P.parents) {
+                            top = __shfl_sync(0xffffffffu, top, 31);
+                            const int tree = max(u.first - start, 0);       // the first node's place
+#pragma unroll
+                            for (int w = 0; w < 4; ++w) {
+                                uint32_t of = tree >= 32 * w + 32 ? 0u : tree > 32 * w ? seen[w] >> (tree - 32 * w) << (tree - 32 * w) : seen[w];
+                                for (; of; of &= of - 1) {
+                                    const float x = all[w * 32 + __ffs(of) - 1];
+                                    if (x < INFINITY) top = fmaxf(top, x);
+                                }
+                            }
+                            __syncwarp();
+                        } else {
+                            const int last = min(u.first + node, start + valid - 1) - start;       // the last that this row sees
+                            const float earlier = __shfl_up_sync(0xffffffffu, top, 1);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float x = __shfl_sync(0xffffffffu, lane ? fmaxf(earlier, upto[i]) : upto[i], max(last, 0) >> 2);
+                                if ((last & 3) == i) top = x;
+                            }
+                            if (last < 0) top = 0.f;
                         }
                         above = attn_exponent(top);
                     }
@@ -416,12 +445,12 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                 arrive(&S.p_full[t]);
             }
             if (left) { ok = false; break; }                                // both warps
+            const AttnUnit done = u;
+            have = it.next(P, u);
             wait(&S.o_full[t], units & 1u);
             __syncwarp();
             tc_fence_after();
             // Everything of this unit has been multiplied: Q of the next one takes the place of this one's.
-            const AttnUnit done = u;
-            have = it.next(P, u);
             if (have) prepare_q(u);
             const bool join = !done.pair && count > 1;
             if (merged) { wait(&S.merge_done, (merges - 1) & 1u); merged = false; }

@@ -317,12 +317,16 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi)
 __device__ __forceinline__ void attn_hide(uint32_t addr, uint32_t on, uint32_t bad)
 {
 #pragma unroll 1
-    for (int c = 0; c < 32; c += 16) {
+    for (int c = 0; c < 32; c += 16, on >>= 16, bad >>= 16) {
+        if (__all_sync(0xffffffffu, (on & 0xffffu) == 0xffffu && (bad & 0xffffu) == 0u)) continue;
         float s[16];
         uint32_t x[16];
         tmem_load16(addr + c, s);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = !(on >> (c + i) & 1u) ? 0xff800000u : (bad >> (c + i) & 1u) ? 0x7fffffffu : __float_as_uint(s[i]);
+        for (int i = 0; i < 16; ++i) x[i] = on & (1u << i) ? __float_as_uint(s[i]) : 0xff800000u;
+        if (__any_sync(0xffffffffu, (on & bad & 0xffffu) != 0u))
+#pragma unroll
+            for (int i = 0; i < 16; ++i) if (on & bad & (1u << i)) x[i] = 0x7fffffffu;
         tmem_store16(addr + c, x);
     }
     tmem_store_wait();
