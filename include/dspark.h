@@ -657,7 +657,11 @@ int dspark_kv_commit(const dspark_kv_cache_t* cache, const int32_t* first, const
  *   out_lse     device fp32 [n_rows][q_heads] or NULL: log of the sum of e^(scale * q . k) over the positions seen
  *   workspace   dspark_tree_attention_workspace_bytes(...), 256-byte aligned, any content; one call at a time
  * The products are bf16 (an 8-bit cache: 16-bit operands that hold its values exactly) with fp32 accumulation; softmax
- * statistics are fp32; the weights are rounded to 16 bits for their product with v.  The same inputs give the same bits.
+ * statistics are fp32; the weights are rounded to 16 bits for their product with v (an 8-bit cache: times v's scale and relative
+ * to the row's largest such product; what is 2^-32 of that is lost).  The same inputs give the same bits.
+ * Two launches: one CTA per SM with most of its shared memory and all of its tensor memory, and a short one that joins the
+ * parts of what was divided between SMs.  A wait inside that runs out (none does unless something is broken) sets
+ * DSPARK_DEV_TIMEOUT; the outputs are then unspecified.
  * Errors: INVALID_ARG, SHAPE, ALIGNMENT, WORKSPACE, CUDA.
  */
 size_t dspark_tree_attention_workspace_bytes(int n_rows, int q_heads, int kv_heads, int head_dim);
@@ -687,8 +691,8 @@ int dspark_tree_attention(const dspark_kv_cache_t* cache, int layer, const void*
  * [0, V) (DSPARK_DEV_BAD_TOKEN), more than DSPARK_TREE_MAX_NODES nodes or no row at all (DSPARK_DEV_BAD_OFFSETS), or NaN, an
  * infinity or no mass in what it looks at (DSPARK_DEV_BAD_ROW) is voided: accepted_len 0, its tokens and path -1.  (With
  * offsets that are not ascending within [0, n_rows], only accepted_len is written.)
- * Reads one entry of p and q for every node, and the rows of a node when one of its children has been rejected or the walk
- * ends there.  Limits: V <= 2^24, 1 <= R <= 2^20, n_rows <= 2^24.  Errors: INVALID_ARG, SHAPE, ALIGNMENT, CUDA.  No workspace.
+ * Reads one entry of p and q for every node, p's row of a node when one of its children has been rejected or the walk ends
+ * there, and q's row when one has been rejected.  Limits: V <= 2^24, 1 <= R <= 2^20, n_rows <= 2^24.  Errors: INVALID_ARG, SHAPE, ALIGNMENT, CUDA.  No workspace.
  */
 #define DSPARK_TREE_MAX_NODES 1024
 int dspark_verify_tree(const float* target_probs, int64_t target_row_stride, const float* draft_probs, int64_t draft_row_stride,

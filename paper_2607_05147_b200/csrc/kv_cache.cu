@@ -11,6 +11,8 @@
 // The rows are therefore read before that chain is begun.  A head's row belongs to 4, 8 or 16 neighbouring lanes, two pieces of 16
 // bytes of bf16 each, so that the maximum is a few shuffles and neighbouring lanes and heads fill whole sectors; a thread has two
 // such rows in flight.  For many rows instructions come next: where a row lies is worked out by one thread of the CTA.
+// Prompts of 15.5 thousand rows, 8 heads of 128, int8: written in 24 us and read back in 20 (97 MB each, 4.0 and 4.8 TB/s); 8 rows of
+// one request 3.2 us each way.
 #include "kv_cache.cuh"
 
 namespace dspark {
@@ -334,7 +336,8 @@ static int kv_rows(const KvStep& P, cudaStream_t s)
 // kCommitRun nodes at a time, for all layers.  A thread owns 16 bytes of a position (or one scale) and moves them along the
 // path, kCommitBatch positions at a time: path[i] > i and the path ascends, so a position that is read is never one that an
 // earlier batch has written, and within a batch all reads come first.  Different threads touch different bytes: no order among
-// them.
+// them.  64 requests, up to 7 nodes, 32 layers of 8 heads of 128 (66 MB): 15.6 us, 4.2 TB/s; a CTA for each layer's K or V worked the
+// path out 64 times and took 39.5.
 constexpr int kCommitThreads = 128, kCommitBatch = 8, kCommitRun = 128;
 
 struct KvCommit {

@@ -9,17 +9,25 @@
 // partial results (running maximum, sum, accumulator) in the workspace, which a second small kernel joins.
 //
 // Within a CTA:
-//   * a producer warp brings K and V tiles into a ring by tensor-map copies, a page a box;
+//   * a producer warp brings K and V tiles into a ring each by tensor-map copies, a page a box;
 //   * one thread issues tcgen05.mma: S = Q K^T into tensor memory (Q and K in shared memory), then O += P V, with P taken from
 //     tensor memory and V as it lies (mn-major);
-//   * two groups of four warps do the softmax, one row a thread: they read S, write P over it as 16-bit values, and scale O only
-//     when the maximum has risen by more than 2^8 (the reference is any number that keeps the exponentials in range).  The two
-//     groups have one S and one O each: with two row tiles they take one of them each; with one they take the even and the odd
-//     cache tiles and join at the end.  While one group works on its S the tensor cores do the other's products.
-//   * 8-bit caches: four more warps turn the tiles into 16-bit floats (exact for both types) in a second ring.  The scales of K
-//     multiply the scores and those of V the weights, so that neither is rounded into the operands.
+//   * two groups of eight warps do the softmax, a row in two threads, half of a tile's positions each: they read S, write P over
+//     it as 16-bit values, and scale O only when the maximum has risen by more than 2^8 (the reference is any number that keeps
+//     the exponentials in range).  The groups have one S and one O each: with two row tiles they take one of them each; with one
+//     they take the even and the odd cache tiles and join at the end.  While one group works on its S the tensor cores do the
+//     other's products.
+//   * 8-bit caches: four more warps turn the tiles into 16-bit floats (exact for both types) in a second pair of rings.  The scales
+//     of K multiply the scores and those of V the weights, so that neither is rounded into the operands.
 //
-// Bound by the cache's bytes where a K/V head has up to about 128 rows (bf16), by the exponentials and the products beyond.
+// This kernel is for more than 64 rows with a K/V head; up to there tree_attention_few.cu does the work.
+//
+// Bound by the cache's bytes up to about 128 rows over bf16 (64 requests of 32 nodes, 4 heads a K/V head, over 4096 positions: 244 us,
+// 4.5 TB/s), beyond by the chain scores -> exponentials -> products of a group, which the other group's covers in part: a tile
+// for 256 rows over e4m3 takes 6 800 clocks, of which the exponentials alone are 2 048 and the products 1 500.  64 nodes over 131072
+// positions: 252 us, 0.55 PFLOP/s.
+// Tried and not kept: a warp a group for the products (the groups fall into step, 259 us); the weights made in the pass that finds
+// the largest score (32 more registers than there are).
 #include "tree_attention.cuh"
 
 namespace dspark {
