@@ -678,9 +678,15 @@ static bool cache_map(CUtensorMap* map, const unsigned char* base, const KvView&
     const cuuint64_t strides[3] = {step(c.token_stride), step(c.head_stride), step(c.page_stride)};
     const cuuint32_t box[4] = {(cuuint32_t)(wide ? 64 : c.head_dim), (cuuint32_t)tokens, 1, 1};
     const cuuint32_t estr[4] = {1, 1, 1, 1};
+    // What the copies bring into the L2 beside their own lines is another head's, and gone before that head's turn, unless a head's
+    // positions lie together: 64 tokens over 8192 positions of int8, 128 bytes a line, read 1.66 GB instead of 1.11 when 256 bytes
+    // were brought at a time.
+    const long long line = c.token_stride == (long long)c.head_dim * (wide ? 2 : 1) ? 256 : c.head_dim * (wide ? 2 : 1);
+    const CUtensorMapL2promotion promotion = line >= 256 ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : line >= 128 ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B
+                                             : line >= 64 ? CU_TENSOR_MAP_L2_PROMOTION_L2_64B : CU_TENSOR_MAP_L2_PROMOTION_NONE;
     return fn(map, wide ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<unsigned char*>(base), dims, strides, box,
               estr, CU_TENSOR_MAP_INTERLEAVE_NONE, wide || (turned && c.head_dim == 128) ? CU_TENSOR_MAP_SWIZZLE_128B : turned && c.head_dim == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE,
-              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+              promotion, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 static int attn_sms() { const int sms = current_sms(); return sms < kAttnSms ? sms : kAttnSms; }
 struct AttnWs { size_t stats, parts, total; int rows; };
