@@ -6,10 +6,14 @@
 // belongs to a position (its scales in an 8-bit cache, whether it exists) belongs to a thread.
 //
 //   * S^T = K Q^T: K as it lies (k-major), Q in shared memory, N = rows rounded up to 16, 32 or 64;
-//   * two groups of four warps have half of the columns each: a thread reads its position's scores, weighs them against one
-//     reference a row and writes 16-bit weights, half a line of the mn-major operand P^T, to shared memory;
+//   * the softmax, two groups of four warps: a thread reads its position's scores, weighs them against one reference a row and
+//     writes 16-bit weights, a part of a line of the mn-major operand P^T, to shared memory;
 //   * O^T += V^T P^T: V as it lies (mn-major), O^T has a row per component and a column per row of Q.
-// S^T and P^T are there twice, so that one tile's products run while the next one's weights are made.
+// Each group has half of the columns of every tile, but for 8-bit caches and up to 16 rows, where the groups take the tiles in turn,
+// with an O^T, references and sums each, joined at the end of a unit: a tile's chain of waits and loads is longer than its
+// bytes take to arrive (128 tokens over 8192 positions of int8, 8 rows: 454 us, 536 with halves; over bf16 the same, and a single
+// token a microsecond slower; with 32 columns a thread of an 8-bit cache has too few registers, 203 us instead of 193).  A group has two
+// S^T and P^T, so that one tile's products run while the next one's weights are made.
 //
 // The maximum of a row would need a reduction over the threads for every row and tile.  It is not needed: any reference serves
 // that keeps the exponentials in range, so the threads only vote whether one of their scores is above its reference by more than
@@ -27,25 +31,28 @@ namespace dspark {
 
 constexpr int kSoftmaxWarps = 8;
 constexpr int kFewSmem = 217 * 1024;             // two of P, Q, the ring; tables beside it
-// P^T: a line of 128 bytes a position, of two tiles beside one another where both fit
+template <int kKind, int kN> constexpr bool kFewTurns = kKind != kAttnWide && kN == 16;      // the groups take the tiles in turn
+template <int kKind, int kN> constexpr int kFewBuffers = kFewTurns<kKind, kN> ? 4 : 2;
+// P^T: a line of 128 bytes a position, of 64 / kN tiles beside one another
 constexpr int kFewPBytes = kAttnTile * 128;
-template <int kN> constexpr int kFewPStep = kN <= 32 ? kN * 2 : kFewPBytes;      // from one tile's to the other's
-template <int kN> constexpr int kFewPAll = kN <= 32 ? kFewPBytes : 2 * kFewPBytes;
+template <int kKind, int kN> constexpr int kFewPAll = (kFewBuffers<kKind, kN> * kN + 63) / 64 * kFewPBytes;
+template <int kN> __device__ __forceinline__ int few_p_line(uint32_t b) { return (int)(b / (64 / kN)) * kFewPBytes; }
+template <int kN> __device__ __forceinline__ int few_p_at(uint32_t b) { return (int)(b % (64 / kN)) * (kN / 8); }      // 16-byte pieces
 constexpr float kFewUnset = 1e38f;               // less a reference that every score is above
 
 struct FewShared {
     uint64_t full[kAttnMaxSlots], empty[kAttnMaxSlots], raw_full[kAttnMaxRaw], raw_empty[kAttnMaxRaw];
-    uint64_t q_full, q_empty, s_full[2], p_full[2], o_done[2], mma_done[2];
+    uint64_t q_full, q_empty, s_full[4], p_full[4], o_done[4], mma_done[2];
     uint32_t tmem_base;
     int abort, bad_value[kAttnUnitFlags];
     AttnList list;
 };
 template <int kN>
 struct FewTables {
-    float less[kN];                              // less the references, in units of log2
-    float scale[kN];                             // what O^T and the sums are multiplied by when they change, and at the end
+    float less[2][kN];                           // less the references, in units of log2, of either group
+    float scale[2][kN];                          // what O^T and the sums are multiplied by when they change, and at the end
     float q[2][kN];                              // 8-bit caches: what a row of Q was divided by, of this unit and the next
-    float top[4][kN], sum[4][kN];                // a warp's maxima; its sums at the end
+    float top[kSoftmaxWarps][kN], sum[kSoftmaxWarps][kN];     // a warp's maxima; its sums at the end
     unsigned long long seen[2][kAttnTile];       // rows that see a position (tiles with nodes), for each group
 };
 
@@ -62,9 +69,11 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
 {
     constexpr bool kNarrow = kKind != kAttnWide;
     constexpr int kThreads = kFewThreads<kKind, kN>, kProducer = kSoftmaxWarps, kIssuer = kSoftmaxWarps + 1, kIssuerO = kSoftmaxWarps + 2;
-    constexpr int kWarps = kFewConverters<kKind, kN>, kOf = kNarrow ? 4 : 1, kC = kN / 2;    // kOf: warps that make one 16-bit tile
-                   // kC: columns of a group
-    // columns of tensor memory: S^T at 0 and 64, O^T at 128, two K tiles of an 8-bit cache at 192 and 256
+    constexpr int kWarps = kFewConverters<kKind, kN>, kOf = kNarrow ? 4 : 1;                 // kOf: warps that make one 16-bit tile
+    constexpr bool kTurns = kFewTurns<kKind, kN>;
+    constexpr int kBuffers = kFewBuffers<kKind, kN>, kS = 128 / kBuffers;          // kS: columns from one S^T to the next
+    constexpr int kE = kN / 2, kC = kTurns ? kN : kE;                       // rows that a group loads and writes; whose weights it makes
+    // columns of tensor memory: S^T from 0 on, O^T at 128 (and 160), two K tiles of an 8-bit cache at 192 and 256
     constexpr uint32_t kO = 128, kK = 192, kColumns = kNarrow ? 512 : 256;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);   // swizzle atoms: 1 KB
@@ -73,7 +82,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;    // warp: uniform, and known to be
     const int d = P.c.head_dim, tile_bytes = P.chunks * kChunkBytes;
     unsigned char* sP = smem;
-    unsigned char* sQ = sP + kFewPAll<kN>;     // per 64 components: kN lines of 128 bytes
+    unsigned char* sQ = sP + kFewPAll<kKind, kN>;     // per 64 components: kN lines of 128 bytes
     const int slots = P.k_slots + P.v_slots;
     unsigned char* ring = sQ + P.chunks * kN * 128 - (kNarrow ? P.k_slots * tile_bytes : 0);       // 8-bit: of V alone
     unsigned char* raw = ring + slots * tile_bytes;
@@ -82,7 +91,8 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
         for (int s = 0; s < slots; ++s) { mbar_init(&S.full[s], kOf); mbar_init(&S.empty[s], 1); }
         for (int s = 0; s < P.raw_k + P.raw_v; ++s) { mbar_init(&S.raw_full[s], 1); mbar_init(&S.raw_empty[s], kOf); }
         mbar_init(&S.q_full, kSoftmaxWarps); mbar_init(&S.q_empty, 1);
-        for (int t = 0; t < 2; ++t) { mbar_init(&S.s_full[t], 1); mbar_init(&S.p_full[t], kSoftmaxWarps); mbar_init(&S.o_done[t], 1); mbar_init(&S.mma_done[t], 1); }
+        for (int b = 0; b < kBuffers; ++b) { mbar_init(&S.s_full[b], 1); mbar_init(&S.p_full[b], kTurns ? 4 : 8); mbar_init(&S.o_done[b], 1); }
+        for (int t = 0; t < 2; ++t) mbar_init(&S.mma_done[t], 1);
         for (int i = 0; i < kAttnUnitFlags; ++i) S.bad_value[i] = 0;
         S.abort = 0;
         mbar_fence_init();
@@ -120,15 +130,17 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
             if (!second && !wait(&S.q_full, units & 1u)) break;
             ++units;
             for (int i = 0; i < n; ++i, ++item) {
-                const uint32_t b = item & 1u, turn = item >> 1;             // which S^T and P^T, for the how-manieth time
+                const uint32_t b = item % kBuffers, turn = item / kBuffers; // which S^T and P^T, for the how-manieth time
                 const uint32_t s = (uint32_t)(first_slot + place.s), ph = place.ph;
                 if (second) {
                     if (!wait(&S.full[s], ph) || !wait(&S.p_full[b], turn & 1u)) break;
                     tc_fence_after();
-                    const uint32_t v = desc_mn_major(smem_u32(ring + s * tile_bytes)), p = desc_mn_major(smem_u32(sP)) + b * (kFewPStep<kN> >> 4);
+                    const uint32_t v = desc_mn_major(smem_u32(ring + s * tile_bytes)), p = desc_mn_major(smem_u32(sP + few_p_line<kN>(b))) + few_p_at<kN>(b);
+                    const uint32_t o = tmem + kO + (kTurns ? (item & 1u) * 32 : 0);
+                    const bool more = i > (kTurns ? 1 : 0);  // not the first of its O^T
                     if (elect_one()) {
 #pragma unroll
-                        for (int k = 0; k < kAttnTile / 16; ++k) mma_ss(tmem + kO, v + k * 128, p + k * 128, idesc_o, i > 0 || k > 0);
+                        for (int k = 0; k < kAttnTile / 16; ++k) mma_ss(o, v + k * 128, p + k * 128, idesc_o, more || k > 0);
                         umma_commit(&S.empty[s]);
                         umma_commit(&S.o_done[b]);
                     }
@@ -142,9 +154,9 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                         for (int k = 0; k < kAttnMaxDim / 16; ++k)
                             if (k >= d / 16) break;
                             else if constexpr (kNarrow)
-                                mma_ts(tmem + b * 64, tmem + kK + s * 64 + k * 8, q0 + (k >> 2) * (kN * 8) + (k & 3) * 2, idesc_s, k > 0);
+                                mma_ts(tmem + b * kS, tmem + kK + s * 64 + k * 8, q0 + (k >> 2) * (kN * 8) + (k & 3) * 2, idesc_s, k > 0);
                             else
-                                mma_ss(tmem + b * 64, k0 + (k >> 2) * (kChunkBytes >> 4) + (k & 3) * 2, q0 + (k >> 2) * (kN * 8) + (k & 3) * 2, idesc_s, k > 0);
+                                mma_ss(tmem + b * kS, k0 + (k >> 2) * (kChunkBytes >> 4) + (k & 3) * 2, q0 + (k >> 2) * (kN * 8) + (k & 3) * 2, idesc_s, k > 0);
                         umma_commit(&S.s_full[b]);
                         umma_commit(&S.empty[s]);
                         if (i + 1 == n) umma_commit(&S.q_empty);
@@ -163,18 +175,22 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
         __syncwarp();
     } else if (warp < kSoftmaxWarps) {
         // ---------------- softmax ---------------------------------------------------------------------------
-        // The groups share nothing but the tiles: each has its rows' references, sums and results.  A wait that runs out makes `ok`
-        // false in its warp; the threads of a group leave together, at the next vote.
-        const int t = warp >> 2, pos = tid & 127, row0 = t * kC;            // group; position in a tile, later component
+        // Within a unit the groups share nothing but the tiles.  A wait that runs out makes `ok` false in its thread; the threads of a
+        // group leave together, at the next vote, and where they take turns both groups, at the votes of a unit's start and end.
+        const int t = warp >> 2, pos = tid & 127;                           // group; position in a tile, later component
+        const int row0 = kTurns ? 0 : t * kC, e0 = t * kE;                  // first of the rows it weighs; of those it loads and writes
         const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t tO = tmem + lane_base + kO + row0;
+        const uint32_t tO = tmem + lane_base + kO, tMine = tO + t * (kTurns ? 32 : kC);          // O^T; that of this group
+        constexpr int kStep = kTurns ? 2 : 1;
+        auto vote = [&](bool x) { return kTurns ? barrier_any<2 * 128>(3, x) : group_any(t, x); };
+        auto first_tile = [&](uint32_t from) { return kTurns ? (int)((from ^ (uint32_t)t) & 1u) : 0; };      // of a unit that starts there
         uint32_t units = 0, item = 0;
         bool ok = true;
         auto wait = [&](uint64_t* bar, uint32_t ph) { ok = ok && mbar_wait_bounded(bar, ph); };      // each lane for itself
         auto arrive = [&](uint64_t* bar) { __syncwarp(); if (lane == 0) mbar_arrive(bar); };
-        // Q of a unit, this group's rows: 128 / kC threads a row, asked for and later stored.
-        constexpr int kPer = 128 / kC, kMost = (kAttnMaxDim / 8 + kPer - 1) / kPer;
-        const int q_row = row0 + pos / kPer, q_sub = pos % kPer, q_node = q_row / P.group, q_head = q_row - q_node * P.group;
+        // Q of a unit, this group's rows: 128 / kE threads a row, asked for and later stored.
+        constexpr int kPer = 128 / kE, kMost = (kAttnMaxDim / 8 + kPer - 1) / kPer;
+        const int q_row = e0 + pos / kPer, q_sub = pos % kPer, q_node = q_row / P.group, q_head = q_row - q_node * P.group;
         uint4 x[kMost];
         auto fetch_q = [&](const AttnUnit& w) {
             const bool live = q_row < P.tile_nodes * P.group && w.node0 + q_node < w.n;
@@ -220,7 +236,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
             fence_async_smem();
             arrive(&S.q_full);
         };
-        // An 8-bit cache's scales of this thread's position, asked for a tile ahead, their page two ahead.
+        // An 8-bit cache's scales of this thread's position, asked for one of the group's tiles ahead, their page two ahead.
         struct Ahead { int page, token; };
         auto page_of = [&](const AttnUnit& w, int jj) {
             Ahead a = {-1, 0};
@@ -245,30 +261,35 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
         };
         Ahead ahead = {-1, 0};
         float2 scale_next = make_float2(0.f, 0.f);
-        auto first_scales = [&]() {
-            scale_next = scales_of(u, page_of(u, 0));
-            ahead = page_of(u, 1);
+        auto first_scales = [&](uint32_t from) {
+            scale_next = scales_of(u, page_of(u, first_tile(from)));
+            ahead = page_of(u, first_tile(from) + kStep);
         };
         bool have = it.next(P, u);
         if (have) {
             fetch_q(u);
             store_q(0);
-            first_scales();
+            first_scales(0);
         }
         while (have) {
-            if (pos < kC) T.less[row0 + pos] = kFewUnset;
+            if (!kTurns && pos < kC) T.less[t][row0 + pos] = kFewUnset;
             if (tid == 0) S.bad_value[(units + kAttnUnitFlags / 2) % kAttnUnitFlags] = 0;
-            if (group_any(t, !ok || *abort_flag)) { ok = false; break; }
+            if (vote(!ok || *abort_flag)) { ok = false; break; }
+            if (kTurns) {                        // both groups have read what there was of the last unit
+                if (pos < kC) T.less[t][pos] = kFewUnset;
+                group_sync(t);
+            }
             uint64_t sums[kC / 2];                                          // of this position's weights, two rows each
 #pragma unroll
             for (int c = 0; c < kC / 2; ++c) sums[c] = pack2(0.f, 0.f);
             const int count = u.j1 - u.j0, rows = min(P.tile_nodes, u.n - u.node0) * P.group;
             bool left = false;
-            for (int jj = 0; jj < count; ++jj, ++item) {
-                const uint32_t b = item & 1u, turn = item >> 1;
-                const uint32_t tS = tmem + lane_base + b * 64 + row0;
-                unsigned char* p_line = sP + (kN <= 32 ? 0 : b * kFewPBytes) + pos * 128;
-                const int p_at = (kN <= 32 ? b * (kN / 8) : 0) + row0 / 8;
+            const int first = first_tile(item);
+            for (int jj = first; jj < count; jj += kStep) {
+                const uint32_t number = item + jj, b = number % kBuffers, turn = number / kBuffers;
+                const uint32_t tS = tmem + lane_base + b * kS + row0;
+                unsigned char* p_line = sP + few_p_line<kN>(b) + pos * 128;
+                const int p_at = few_p_at<kN>(b) + row0 / 8;
                 int start, len;
                 attn_tile_at(P, u.j0 + jj, start, len);
                 const int valid = min(len, u.length - start);               // positions of this tile that exist
@@ -307,7 +328,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                 float k_scale = P.score_factor, v_scale = scale_next.y;
                 const float2 scale = scale_next;
                 scale_next = scales_of(u, ahead);
-                ahead = page_of(u, jj + 2);
+                ahead = page_of(u, jj + 2 * kStep);
                 // an 8-bit V: 2^exponent > its scale; what a weight may be above its reference depends on it
                 float above = 0.f;
                 if constexpr (kNarrow) {
@@ -343,7 +364,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                         for (int c = 0; c < kC; c += 2) {
                             uint64_t k = k2;
                             if constexpr (kNarrow) k = mul2(k, *reinterpret_cast<const uint64_t*>(&T.q[units & 1u][row0 + c]));
-                            unpack2(fma2(pack2(s[c], s[c + 1]), k, *reinterpret_cast<const uint64_t*>(&T.less[row0 + c])), s[c], s[c + 1]);
+                            unpack2(fma2(pack2(s[c], s[c + 1]), k, *reinterpret_cast<const uint64_t*>(&T.less[t][row0 + c])), s[c], s[c + 1]);
                         }
                     };
                     float y[kC], tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -354,7 +375,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                     const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
                     if (group_any(t, !ok || top + above > kAttnLazy)) {
                         // references: the largest score of each row in this tile, where it is that much above
-                        if (jj) wait(&S.o_done[b ^ 1u], ((item - 1) >> 1) & 1u);        // O^T of the tile before
+                        if (jj > first) wait(&S.o_done[(number - kStep) % kBuffers], (number - kStep) / kBuffers & 1u);     // O^T of the tile before
                         if (group_any(t, !ok)) { left = true; break; }
                         tc_fence_after();
                         __syncwarp();
@@ -367,29 +388,29 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                                 const float z = warp_max_f32(s[c] * (kNarrow ? k_scale * T.q[units & 1u][row0 + c0 + c] : k_scale) + above);
                                 if (lane == c) mine = z;
                             }
-                            if (lane < 8) T.top[warp & 3][row0 + c0 + lane] = mine;
+                            if (lane < 8) T.top[warp][row0 + c0 + lane] = mine;
                             __syncwarp();
                         }
                         group_sync(t);
                         if (pos < kC) {
                             const int r = row0 + pos;
-                            const float old = -T.less[r], now = fmaxf(fmaxf(T.top[0][r], T.top[1][r]), fmaxf(T.top[2][r], T.top[3][r]));
+                            const float old = -T.less[t][r], now = fmaxf(fmaxf(T.top[4 * t][r], T.top[4 * t + 1][r]), fmaxf(T.top[4 * t + 2][r], T.top[4 * t + 3][r]));
                             const bool raise = now > old + kAttnLazy;
-                            T.scale[r] = raise ? ex2_approx(old - now) : 1.f;
-                            if (raise) T.less[r] = -now;
+                            T.scale[t][r] = raise ? ex2_approx(old - now) : 1.f;
+                            if (raise) T.less[t][r] = -now;
                         }
                         group_sync(t);
                         __syncwarp();
 #pragma unroll
-                        for (int c = 0; c < kC / 2; ++c) sums[c] = mul2(sums[c], *reinterpret_cast<const uint64_t*>(&T.scale[row0 + 2 * c]));
-                        if (jj) {
+                        for (int c = 0; c < kC / 2; ++c) sums[c] = mul2(sums[c], *reinterpret_cast<const uint64_t*>(&T.scale[t][row0 + 2 * c]));
+                        if (jj > first) {
 #pragma unroll 1
                             for (int c0 = 0; c0 < kC; c0 += 8) {
                                 float o[8];
-                                attn_read<8>(tO + c0, o);
+                                attn_read<8>(tMine + c0, o);
 #pragma unroll
-                                for (int c = 0; c < 8; ++c) o[c] *= T.scale[row0 + c0 + c];
-                                attn_write<8>(tO + c0, reinterpret_cast<const uint32_t (&)[8]>(o));
+                                for (int c = 0; c < 8; ++c) o[c] *= T.scale[t][row0 + c0 + c];
+                                attn_write<8>(tMine + c0, reinterpret_cast<const uint32_t (&)[8]>(o));
                             }
                             tmem_store_wait();
                         }
@@ -412,9 +433,9 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                 if (!kNarrow && masked) {
                     // V of positions that no row sees, or that hold NaN or infinities that only some see, must not meet a
                     // weight of zero in the product: zeros here, the latter added to the rows that see them at the end
-                    const uint32_t s = P.k_slots + item % P.v_slots;
-                    wait(&S.full[s], item / P.v_slots & 1u);
-                    if ((pos & 1) == t && (start + pos >= u.first || pos >= valid))
+                    const uint32_t s = P.k_slots + number % P.v_slots;
+                    wait(&S.full[s], number / P.v_slots & 1u);
+                    if ((kTurns || (pos & 1) == t) && (start + pos >= u.first || pos >= valid))
                         if (attn_clean_values(ring + (size_t)s * tile_bytes + pos * 128, pos, P.chunks, pos < valid))
                             S.bad_value[units % kAttnUnitFlags] = 1;
                 }
@@ -422,13 +443,14 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                 tc_fence_before();
                 arrive(&S.p_full[b]);
             }
-            if (left) { ok = false; break; }                                // all of the group
+            if (left) { if (kTurns) vote(true); ok = false; break; }        // all of the group; the other one learns of it
+            item += count;
             // The next unit's Q and scales, asked for while the products of this one are finished.
             const AttnUnit done = u;
             have = it.next(P, u);
             if (have) {
                 fetch_q(u);
-                first_scales();
+                first_scales(item);
             }
             if (row0 < rows) {
                 // sums over the positions of this warp: half of the rows pass to the other half of the lanes, as long as there are
@@ -451,27 +473,44 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                     } else
                         v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
                 }
-                T.sum[warp & 3][row0 + row] = v[0];                         // the lanes of a row write the same
+                T.sum[warp][row0 + row] = v[0];                         // the lanes of a row write the same
             }
             wait(&S.q_empty, units & 1u);        // this unit's Q has been multiplied: the next one's takes its place
             if (have) store_q(units + 1);
-            wait(&S.o_done[(item - 1) & 1u], ((item - 1) >> 1) & 1u);
+            if (first < count) {                 // the group's last tile
+                const uint32_t last = item - count + first + (count - 1 - first) / kStep * kStep;
+                wait(&S.o_done[last % kBuffers], last / kBuffers & 1u);
+            }
             __syncwarp();
             tc_fence_after();
-            if (group_any(t, !ok)) { ok = false; break; }
-            if (row0 < rows) {
+            if (vote(!ok)) { ok = false; break; }
+            if (e0 < rows) {
                 const bool whole = done.j0 == 0 && done.j1 == done.tiles;
-                const long long part = (long long)(2 * blockIdx.x + (done.j0 > 0 ? 0 : 1)) * P.part_rows + row0;
-                const int mine = min(kC, rows - row0);
-                const int node0 = done.node0 + row0 / P.group, head0 = row0 % P.group;          // of the group's first row
+                const long long part = (long long)(2 * blockIdx.x + (done.j0 > 0 ? 0 : 1)) * P.part_rows + e0;
+                const int mine = min(kE, rows - e0);
+                const int node0 = done.node0 + e0 / P.group, head0 = e0 % P.group;              // of the group's first row
+                // where the groups took turns: both have had a tile?  (one tile: the other's O^T has not been written)
+                const int only = kTurns && count == 1 ? (int)((item - 1) & 1u) : -1;
                 if (pos < mine) {
-                    const int r = row0 + pos;
-                    const float sum = (T.sum[0][r] + T.sum[1][r]) + (T.sum[2][r] + T.sum[3][r]);
-                    T.scale[r] = whole ? 1.f / sum : 1.f;
-                    if (!whole) P.part_stats[part + pos] = make_float2(-T.less[r], sum);
+                    const int r = e0 + pos;
+                    const int g = kTurns ? 0 : t;
+                    float sum = (T.sum[4 * g][r] + T.sum[4 * g + 1][r]) + (T.sum[4 * g + 2][r] + T.sum[4 * g + 3][r]), ref = -T.less[g][r];
+                    float f0 = 1.f, f1 = 0.f;
+                    if (kTurns) {
+                        const float sum1 = (T.sum[4][r] + T.sum[5][r]) + (T.sum[6][r] + T.sum[7][r]), ref1 = -T.less[1][r];
+                        const float top = fmaxf(ref, ref1);
+                        f0 = ex2_approx(ref - top);
+                        f1 = ex2_approx(ref1 - top);
+                        sum = sum * f0 + sum1 * f1;
+                        ref = top;
+                    }
+                    const float inverse = whole ? 1.f / sum : 1.f;
+                    T.scale[kTurns ? 0 : t][r] = f0 * inverse;
+                    if (kTurns) T.scale[1][r] = f1 * inverse;
+                    if (!whole) P.part_stats[part + pos] = make_float2(ref, sum);
                     else if (P.out_lse)
                         P.out_lse[(long long)(done.row0 + done.node0 + r / P.group) * P.q_heads + done.head * P.group + r % P.group] =
-                            (log2f(sum) - T.less[r]) * 0.6931471805599453f;
+                            (log2f(sum) + ref) * 0.6931471805599453f;
                 }
                 group_sync(t);
                 unsigned char* to = P.out + (long long)(done.row0 + node0) * P.out_row + (long long)(done.head * P.group + head0) * P.out_head + pos * 2;
@@ -482,11 +521,19 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
 #pragma unroll 1
                 for (int h = 0; h < mine; h += 8) {
                     float o[8];
-                    attn_read<8>(tO + h, o);
+                    attn_read<8>(tO + (only == 1 ? 32 : 0) + e0 + h, o);
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) o[c] *= T.scale[kTurns ? (only == 1 ? 1 : 0) : t][e0 + h + c];
+                    if (kTurns && only < 0) {
+                        float o1[8];
+                        attn_read<8>(tO + 32 + e0 + h, o1);
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) o[c] = fmaf(o1[c], T.scale[1][e0 + h + c], o[c]);
+                    }
 #pragma unroll
                     for (int c = 0; c < 8; ++c) {
                         if (h + c < mine && pos < d) {
-                            const float value = o[c] * T.scale[row0 + h + c];
+                            const float value = o[c];
                             if (whole) *reinterpret_cast<uint16_t*>(to) = (uint16_t)pack16<false>(value, 0.f);
                             else to_part[(h + c) * d] = value;
                         }
@@ -496,7 +543,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                 }
                 if (kKind != kAttnI8 && pos < d && *(volatile int*)&S.bad_value[units % kAttnUnitFlags] != 0)
                     for (int c = 0; c < mine; ++c) {     // values that were left out, where the row sees them
-                        const int r = row0 + c, node = done.node0 + r / P.group;
+                        const int r = e0 + c, node = done.node0 + r / P.group;
                         const float bad = attn_bad_values<kNarrow>(P, done, node, pos);
                         if (bad == 0.f) continue;
                         if (!whole) P.parts[(part + c) * d + pos] += bad;
@@ -536,7 +583,7 @@ static int few_launch(AttnParams& P, const CUtensorMap& k, const CUtensorMap& v,
     if (!attn_allow_smem(attn_few_kernel<kKind, kN>, kSmem, ready)) return launch_status();
     const int tile = P.chunks * kChunkBytes;
     // a chunk is left behind the ring: with up to 64 components the products read one past a tile (and nobody its results)
-    int room = kFewSmem - kFewPAll<kN> - P.chunks * kN * 128 - (P.chunks == 1 ? kChunkBytes : 0);
+    int room = kFewSmem - kFewPAll<kKind, kN> - P.chunks * kN * 128 - (P.chunks == 1 ? kChunkBytes : 0);
     // V tiles stay longer than K tiles: until their weights are there.  8-bit caches: two of each as 16 bits (K's in tensor memory),
     // the rest for 8-bit ones on their way: 128 KB of them in flight per SM, or the memory's latency shows.
     const int slots = room / tile < kAttnMaxSlots ? room / tile : kAttnMaxSlots;
