@@ -274,3 +274,36 @@ def test_many_requests():
     first, nodes = [(i * 13) % 40 for i in range(R)], [(i % 5) % 3 for i in range(R)]
     cache, q = step(first, nodes, 8, 1, 2, 16, "bf16", seed=16)
     check(cache, q, first, nodes, None, 0.25)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "int8", "e4m3"])
+@pytest.mark.parametrize("group,tree", [(4, "chain"), (4, "tree"), (8, "tree"), (16, "chain")])
+def test_units_of_all_lengths_in_a_run(kind, group, tree):
+    # more tiles than SMs, units of one to nine of them that begin anywhere in an SM's run and end in the next one's
+    first = [(r * 97) % 1100 for r in range(60)]
+    nodes = [1 + (r * 5) % 4 for r in range(60)]
+    parents = None if tree == "chain" else T.random_parents(nodes, 3)
+    cache, q = step(first, nodes, 32, 2, group, 64, kind, seed=11)
+    check(cache, q, first, nodes, parents, 0.125)
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("group", [4, 40])
+def test_what_other_requests_and_branches_hold(kind, group):
+    # eight and eighty rows with a head: NaN scales at positions that a node does not see leave its row alone, also where the tile is the
+    # only one of its unit, and scales far above those that it sees do not cost it its digits
+    first, nodes = [0, 100, 128, 250], [2, 2, 2, 2]
+    parents = [-1, 0] * 4
+    cache, q = step(first, nodes, 16, 2, group, 128, kind, seed=5)
+    for r in range(4):
+        pg, at = cache.slots(r, [first[r] + 1])
+        cache.vs[0, pg, :, at] = 2.0 ** 30 if r % 2 else math.nan
+    off = T.offsets(nodes)
+    got, _, st = T.run_attention(cache, q, T.i32(first), off, T.i32(parents), 0.1)
+    want, bound, _, _ = T.attention(cache, q, first, off.tolist(), parents, 0.1)
+    assert st == 0
+    for r in range(4):
+        root = off[r].item()
+        assert bool(((got[root].double() - want[root]).abs() <= bound[root]).all())
+        if r % 2 == 0:
+            assert bool(got[root + 1].isnan().all())
