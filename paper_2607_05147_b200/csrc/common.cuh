@@ -82,6 +82,8 @@ __device__ __forceinline__ bool mbar_wait_bounded(uint64_t* bar, uint32_t parity
 }
 // Poll limit of the waits of dspark_rms_norm_quant's ring of rows on the current device (norm.cu); a status code
 int norm_set_poll_limit(uint32_t polls);
+// the same for dspark_tree_attention (tree_attention.cu)
+void attn_set_poll_limit(uint32_t polls);
 // 1-D bulk async copy global -> this CTA's shared memory, completion counted on `bar`.
 // dst, src 16-byte aligned, bytes a multiple of 16.
 __device__ __forceinline__ void bulk_g2s(void* dst, const void* src, uint32_t bytes, uint64_t* bar)

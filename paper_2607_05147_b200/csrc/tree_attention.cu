@@ -111,7 +111,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
         uint32_t units = 0, items[2] = {0, 0};
         bool ok = true, issued = false;
         RingPlace k_at, v_at;
-        auto wait = [&](uint64_t* bar, uint32_t ph) { ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, ph)); return ok; };
+        auto wait = [&](uint64_t* bar, uint32_t ph) { ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, ph, P.polls)); return ok; };
         while (ok && !__any_sync(0xffffffffu, *abort_flag) && it.next(P, u)) {
             const int n = (u.j1 - u.j0) << (u.pair ? 1 : 0);
             const bool pair = u.pair;
@@ -181,7 +181,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
         uint32_t units = 0, items = 0, merges = 0;
         uint32_t seq = 0;                        // cache tiles of earlier units
         bool ok = true, merged = false;
-        auto wait = [&](uint64_t* bar, uint32_t ph) { ok = ok && mbar_wait_bounded(bar, ph); };      // each lane for itself
+        auto wait = [&](uint64_t* bar, uint32_t ph) { ok = ok && mbar_wait_bounded(bar, ph, P.polls); };      // each lane for itself
         auto arrive = [&](uint64_t* bar) { __syncwarp(); if (lane == 0) mbar_arrive(bar); };
         auto vote = [&](bool x) { return barrier_any<64>(pair_id + 1, x); };
         // This thread's half of row `row` of row tile `tile` of a unit into shared memory; in 8-bit mode as fp16, scaled by a power of
@@ -723,6 +723,25 @@ static int attn_launch(AttnParams& P, const CUtensorMap& k, const CUtensorMap& v
 
 }  // namespace dspark
 
+// Polls of a wait by device, 0 standing for kWaitPollLimit (dspark_set_wait_poll_limit).  The waits for copies and products under
+// way before a CTA leaves keep their own.
+static std::atomic<uint32_t> g_attn_poll_limit[64];
+namespace dspark {
+void attn_set_poll_limit(uint32_t polls)
+{
+    int dev = 0;
+    cudaGetDevice(&dev);
+    g_attn_poll_limit[dev & 63].store(polls ^ kWaitPollLimit, std::memory_order_relaxed);
+}
+static uint32_t attn_poll_limit()
+{
+    int dev = 0;
+    cudaGetDevice(&dev);
+    const uint32_t polls = g_attn_poll_limit[dev & 63].load(std::memory_order_relaxed) ^ kWaitPollLimit;
+    return polls < kAttnPolls ? polls : kAttnPolls;
+}
+}  // namespace dspark
+
 extern "C" {
 
 size_t dspark_tree_attention_workspace_bytes(int n_rows, int q_heads, int kv_heads, int head_dim)
@@ -779,6 +798,7 @@ int dspark_tree_attention(const dspark_kv_cache_t* cache, int layer, const void*
     P.page_shift = -1;
     for (int i = 3; i <= 7; ++i) if (cache->page_size == 1 << i) P.page_shift = i;
     P.part_rows = w.rows;
+    P.polls = attn_poll_limit();
     unsigned char* ws = (unsigned char*)workspace;
     P.cuts = (int4*)ws;
     P.part_stats = (float2*)(ws + w.stats);

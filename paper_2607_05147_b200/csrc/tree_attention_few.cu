@@ -124,7 +124,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
         RingPlace place;
         uint32_t units = 0, item = 0;
         bool ok = true;
-        auto wait = [&](uint64_t* bar, uint32_t p) { ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, p)); return ok; };
+        auto wait = [&](uint64_t* bar, uint32_t p) { ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, p, P.polls)); return ok; };
         while (ok && !__any_sync(0xffffffffu, *abort_flag) && it.next(P, u)) {
             const int n = u.j1 - u.j0;
             if (!second && !wait(&S.q_full, units & 1u)) break;
@@ -186,7 +186,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
         auto first_tile = [&](uint32_t from) { return kTurns ? (int)((from ^ (uint32_t)t) & 1u) : 0; };      // of a unit that starts there
         uint32_t units = 0, item = 0;
         bool ok = true;
-        auto wait = [&](uint64_t* bar, uint32_t ph) { ok = ok && mbar_wait_bounded(bar, ph); };      // each lane for itself
+        auto wait = [&](uint64_t* bar, uint32_t ph) { ok = ok && mbar_wait_bounded(bar, ph, P.polls); };      // each lane for itself
         auto arrive = [&](uint64_t* bar) { __syncwarp(); if (lane == 0) mbar_arrive(bar); };
         // Q of a unit, this group's rows: 128 / kE threads a row, asked for and later stored.
         constexpr int kPer = 128 / kE, kMost = (kAttnMaxDim / 8 + kPer - 1) / kPer;

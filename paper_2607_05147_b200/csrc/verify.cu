@@ -1343,6 +1343,7 @@ int dspark_set_wait_poll_limit(unsigned int polls)
 {
     const uint32_t v = polls ? polls - 1u : kWaitPollLimit;     // 1: no poll at all, the wait gives up at once
     if (cudaMemcpyToSymbol(g_entry_poll_limit, &v, sizeof(v)) != cudaSuccess) return launch_status();
+    attn_set_poll_limit(v);
     return norm_set_poll_limit(v);
 }
 
