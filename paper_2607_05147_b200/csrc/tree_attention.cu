@@ -41,7 +41,7 @@ struct AttnShared {
     int abort, bad_value[kAttnUnitFlags];
     AttnList list;
     float2 second[kAttnTile];                    // (reference, sum) of the second group
-    float of_half[2][2][kAttnTile], q_half[2][2][kAttnTile];  // what the two threads of a row tell one another: largest scores, sums; of Q
+    float of_half[2][2][kAttnTile];              // what the two threads of a row tell one another: largest scores, sums
 };
 template <int kKind>
 struct AttnScales {                              // q: per row; bad: a bit for a node's position with a scale that is no number
@@ -184,54 +184,53 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
         auto wait = [&](uint64_t* bar, uint32_t ph) { ok = ok && mbar_wait_bounded(bar, ph, P.polls); };      // each lane for itself
         auto arrive = [&](uint64_t* bar) { __syncwarp(); if (lane == 0) mbar_arrive(bar); };
         auto vote = [&](bool x) { return barrier_any<64>(pair_id + 1, x); };
-        // This thread's half of row `row` of row tile `tile` of a unit into shared memory; in 8-bit mode as fp16, scaled by a power of
-        // two so that no value passes the range and what is lost is below 2^-37 of the row's largest.
+        // Row tile `tile` of a unit into shared memory by the eight warps of a group, 16 rows a warp, 16 lanes a row: a row a thread
+        // would ask for 32 lines with every load.  In 8-bit mode as fp16, scaled by a power of two so that no value passes the range
+        // and what is lost is below 2^-37 of the row's largest.
         auto load_q = [&](const AttnUnit& w, int tile) {
-            const int node = w.node0 + tile * tile_nodes + row / P.group, pieces = d / 16;
-            const bool there = row < tile_nodes * P.group && node < w.n;
-            const uint4* src = reinterpret_cast<const uint4*>(P.q + (long long)(w.row0 + node) * P.q_row +
-                                                              (long long)(w.head * P.group + row % P.group) * P.q_head) + half * pieces;
-            unsigned char* dst = sQ + tile * tile_bytes + row * 128;
-            float up = 1.f;
-            if constexpr (kNarrow) {
-                float top = 0.f;
-                if (there)
-#pragma unroll 4
-                    for (int i = 0; i < pieces; ++i) {
-                        const uint4 x = src[i];
-                        const uint32_t w4[4] = {x.x, x.y, x.z, x.w};
+            const int sub = lane & 15;
+            const bool in = sub < d / 8;
+            unsigned char* dst = sQ + tile * tile_bytes + (sub >> 3) * kChunkBytes;
+#pragma unroll 1
+            for (int i0 = 0; i0 < 8; i0 += 4) {
+                const int r0 = (warp & 7) * 16 + i0 * 2 + (lane >> 4);      // and the second, fourth and sixth behind it
+                uint4 x[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = r0 + 2 * i, of = r / P.group, node = w.node0 + tile * tile_nodes + of;
+                    x[i] = make_uint4(0, 0, 0, 0);
+                    if (in && of < tile_nodes && node < w.n)
+                        x[i] = reinterpret_cast<const uint4*>(P.q + (long long)(w.row0 + node) * P.q_row + (long long)(w.head * P.group + r - of * P.group) * P.q_head)[sub];
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = r0 + 2 * i;
+                    if constexpr (kNarrow) {
+                        const uint32_t w4[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+                        float top = 0.f;
 #pragma unroll
                         for (int k = 0; k < 4; ++k) top = max3(top, fabsf(bf16lo(w4[k])), fabsf(bf16hi(w4[k])));
+#pragma unroll
+                        for (int o = 8; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                        // 2^e with the largest value below 2^14: exponent field of top to that of 2^13; at most 2^60
+                        const int e = min(127 + 60, max(1, 254 + 13 - (int)(__float_as_uint(top) >> 23)));
+                        const float up = __uint_as_float((uint32_t)e << 23);
+                        if (sub == 0) scales.q[tile][r] = __uint_as_float((uint32_t)(254 - e) << 23);       // the inverse power
+                        x[i].x = pack16<true>(bf16lo(x[i].x) * up, bf16hi(x[i].x) * up);
+                        x[i].y = pack16<true>(bf16lo(x[i].y) * up, bf16hi(x[i].y) * up);
+                        x[i].z = pack16<true>(bf16lo(x[i].z) * up, bf16hi(x[i].z) * up);
+                        x[i].w = pack16<true>(bf16lo(x[i].w) * up, bf16hi(x[i].w) * up);
                     }
-                S.q_half[t][half][row] = top;
-                barrier_any<64>(pair_id + 1, false);
-                top = fmaxf(top, S.q_half[t][half ^ 1][row]);
-                // 2^e with the largest value below 2^14: exponent field of top to that of 2^13; at most 2^60
-                const int e = min(127 + 60, max(1, 254 + 13 - (int)(__float_as_uint(top) >> 23)));
-                up = __uint_as_float((uint32_t)e << 23);
-                if (there && !half) scales.q[tile][row] = __uint_as_float((uint32_t)(254 - e) << 23);   // the inverse power
-            }
-            if (there)
-#pragma unroll 4
-                for (int i = 0; i < pieces; ++i) {
-                    uint4 x = src[i];
-                    if (kNarrow) {
-                        x.x = pack16<true>(bf16lo(x.x) * up, bf16hi(x.x) * up);
-                        x.y = pack16<true>(bf16lo(x.y) * up, bf16hi(x.y) * up);
-                        x.z = pack16<true>(bf16lo(x.z) * up, bf16hi(x.z) * up);
-                        x.w = pack16<true>(bf16lo(x.w) * up, bf16hi(x.w) * up);
-                    }
-                    x.x ^= P.q_sign; x.y ^= P.q_sign; x.z ^= P.q_sign; x.w ^= P.q_sign;
-                    const int c = half * pieces + i;
-                    *reinterpret_cast<uint4*>(dst + (c >> 3) * kChunkBytes + (((c & 7) ^ (row & 7)) << 4)) = x;
+                    x[i].x ^= P.q_sign; x[i].y ^= P.q_sign; x[i].z ^= P.q_sign; x[i].w ^= P.q_sign;
+                    if (in) *reinterpret_cast<uint4*>(dst + r * 128 + (((sub & 7) ^ (r & 7)) << 4)) = x[i];
                 }
+            }
             fence_async_smem();
         };
         bool have = it.next(P, u);
         // Q of the first unit; afterwards each unit's is loaded at the end of the one before
         auto prepare_q = [&](const AttnUnit& w) {
-            if (w.pair) load_q(w, t);
-            else if (t == 1) load_q(w, 0);
+            if (w.pair || t == 0) load_q(w, t);
             arrive(&S.q_full);
         };
         if (have) prepare_q(u);
@@ -458,8 +457,6 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
             wait(&S.o_full[t], units & 1u);
             __syncwarp();
             tc_fence_after();
-            // Everything of this unit has been multiplied: Q of the next one takes the place of this one's.
-            if (have) prepare_q(u);
             const bool join = !done.pair && count > 1;
             if (merged) { wait(&S.merge_done, (merges - 1) & 1u); merged = false; }
             S.of_half[t][half][row] = sum;
@@ -490,8 +487,14 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                 const long long part = (long long)(2 * blockIdx.x + (done.j0 > 0 ? 0 : 1)) * P.part_rows + tile * kAttnTile + row;
                 const int head = done.head * P.group + row % P.group;
                 const long long out_row = done.row0 + node;
-                const float inverse = 1.f / sum;
+                const float inverse = whole ? 1.f / sum : 1.f;
                 if (warp_live) {
+                    // 16 components of the warp's rows at a time through this unit's Q, which nobody needs any more: neighbouring
+                    // lanes write neighbouring pieces of a row
+                    unsigned char* stage = sQ + tile * tile_bytes + (warp & 7) * 2048;
+                    unsigned char* to = !live ? nullptr : whole ? P.out + out_row * P.out_row + head * P.out_head : reinterpret_cast<unsigned char*>(P.parts + part * d);
+                    auto staged = [&](int r, int piece) { return reinterpret_cast<float4*>(stage + r * 64 + ((piece ^ (r >> 1 & 3)) << 4)); };
+                    auto target = [&](int r) { return reinterpret_cast<unsigned char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(to), r)); };
 #pragma unroll 1
                     for (int c = o_begin; c < o_end; c += 16) {
                         float o[16];
@@ -506,17 +509,27 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                         if (bad_value && live)   // values that were left out of the product, where this row sees them
 #pragma unroll
                             for (int i = 0; i < 16; ++i) o[i] += attn_bad_values<kNarrow>(P, done, node, c + i);
-                        if (live && whole) {
-                            uint32_t w[8];
+                        __syncwarp();
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) w[i] = pack16<false>(o[2 * i] * inverse, o[2 * i + 1] * inverse);
-                            uint4* dst = reinterpret_cast<uint4*>(P.out + out_row * P.out_row + head * P.out_head + c * 2);
-                            dst[0] = make_uint4(w[0], w[1], w[2], w[3]);
-                            dst[1] = make_uint4(w[4], w[5], w[6], w[7]);
-                        } else if (live) {
-                            float4* dst = reinterpret_cast<float4*>(P.parts + part * d + c);
+                        for (int i = 0; i < 4; ++i)
+                            *staged(lane, i) = make_float4(o[4 * i] * inverse, o[4 * i + 1] * inverse, o[4 * i + 2] * inverse, o[4 * i + 3] * inverse);
+                        __syncwarp();
+                        if (whole) {
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) dst[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                            for (int k = 0; k < 2; ++k) {
+                                const int r = k * 16 + (lane >> 1);
+                                unsigned char* at = target(r);
+                                const float4 x = *staged(r, (lane & 1) * 2), y = *staged(r, (lane & 1) * 2 + 1);
+                                if (at) *reinterpret_cast<uint4*>(at + c * 2 + (lane & 1) * 16) = make_uint4(pack16<false>(x.x, x.y), pack16<false>(x.z, x.w), pack16<false>(y.x, y.y), pack16<false>(y.z, y.w));
+                            }
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const int r = k * 8 + (lane >> 2);
+                                unsigned char* at = target(r);
+                                const float4 x = *staged(r, lane & 3);
+                                if (at) *reinterpret_cast<float4*>(at + c * 4 + (lane & 3) * 16) = x;
+                            }
                         }
                     }
                     if (live && !half) {
@@ -527,6 +540,8 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                 __syncwarp();
                 if (join) { tc_fence_before(); arrive(&S.merge_done); }
             }
+            // Q of the next unit: everything of this one has been multiplied, and this group has written what it had to
+            if (have) prepare_q(u);
             seq += count;
             ++units;
         }
