@@ -741,8 +741,9 @@ int dspark_set_stream_path(int path);
  * up still waits, with the long default bound, for the bulk copies it has already issued before it leaves,
  * and its outputs are unspecified.  dspark_rms_norm_quant's waits for rows copied ahead (many rows) have the same
  * limit (a captured graph: the one at its capture); a thread whose wait runs out reads its rows from memory instead, so
- * that its outputs are the same as ever.  dspark_tree_attention's waits have it too, where it is below their own 2^18 polls: a
- * CTA whose wait runs out sets DSPARK_DEV_TIMEOUT and leaves, its outputs unspecified.
+ * that its outputs are the same as ever.  dspark_tree_attention's products and softmax have it too, where it is
+ * below their own 2^16 polls (a captured graph: the one at its capture): a CTA whose wait runs out sets DSPARK_DEV_TIMEOUT and
+ * leaves, its outputs unspecified.
  * Per device (the current one), synchronous; the paper has no counterpart. */
 int dspark_set_wait_poll_limit(unsigned int polls);
 

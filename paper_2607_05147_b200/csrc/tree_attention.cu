@@ -25,7 +25,7 @@
 // Bound by the cache's bytes up to about 128 rows over bf16 (64 requests of 32 nodes, 4 heads a K/V head, over 4096 positions: 244 us,
 // 4.5 TB/s), beyond by the chain scores -> exponentials -> products of a group, which the other group's covers in part: a tile
 // for 256 rows over e4m3 takes 6 800 clocks, of which the exponentials alone are 2 048 and the products 1 500.  64 nodes over 131072
-// positions: 252 us, 0.55 PFLOP/s.
+// positions: 241 us, 0.57 PFLOP/s.
 // Tried and not kept: a warp a group for the products (the groups fall into step, 259 us); the weights made in the pass that finds
 // the largest score (32 more registers than there are).
 #include "tree_attention.cuh"

@@ -14,7 +14,9 @@ constexpr int kAttnTile = 128;                   // rows of a row tile, position
 constexpr int kChunkBytes = kAttnTile * 128;     // 64 columns of 16 bits of a tile: 128 rows of 128 bytes, swizzled
 constexpr int kAttnMaxSlots = 12, kAttnMaxRaw = 12, kAttnScaleTiles = 4;
 constexpr int kAttnRingBytes = 6 * 2 * kChunkBytes;           // 192 KB: Q and the rings
-constexpr uint32_t kAttnPolls = 1u << 18;        // of a wait; the longest sound one takes some hundred
+// Polls of a wait; the longest sound one takes some hundred.  The waits of the copies and of the widening warps always have these: with a
+// count from memory 128 tokens over int8 took 467 us instead of 440.  The others' can be shortened (AttnParams::polls).
+constexpr uint32_t kAttnPolls = 1u << 16;
 constexpr int kAttnNarrowBytes = 208 * 1024;                  // with 8-bit caches (4 KB of scales beside it)
 constexpr float kAttnLog2e = 1.4426950408889634f;
 constexpr float kAttnLazy = 8.f;                 // O is scaled when the maximum rises by more than 2^8
@@ -40,7 +42,7 @@ struct AttnParams {
     int k_slots, v_slots;                        // rings: 16-bit tiles of K, of V (behind those of K)
     int raw_k, raw_v;                            // 8-bit tiles, the same way
     int tile_tokens, page_tiles, page_boxes;     // positions of a box; cache tiles of a page (pages above 128) ; boxes of a tile
-    uint32_t polls;                              // of a wait, before it gives up
+    uint32_t polls;                              // of a wait of the products' and the softmax's warps, before it gives up
     int page_shift;                              // pages of up to 128: log2 of their size; above: -1
     int part_rows;                               // rows of a partial result
     int32_t* dev_status;
@@ -414,7 +416,7 @@ __device__ __forceinline__ void attn_produce(const AttnParams& P, AttnIter it, c
             for (int kv = 0; kv < 2; ++kv) {
                 RingPlace& place = at[kv];
                 const int s = place.s + (kv ? k_slots : 0);
-                ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(&empty[s], place.ph ^ 1u, P.polls));
+                ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(&empty[s], place.ph ^ 1u, kAttnPolls));
                 if (!ok) break;
                 if (lane == 0) mbar_arrive_expect_tx(&full[s], (uint32_t)(boxes * copies * P.tile_tokens * row_bytes));
                 __syncwarp();
@@ -432,7 +434,7 @@ __device__ __forceinline__ void attn_produce(const AttnParams& P, AttnIter it, c
     for (int kv = 0; kv < 2; ++kv)
         for (int i = 0; i < (kv ? v_slots : k_slots); ++i) {
             const int s = at[kv].s + (kv ? k_slots : 0);
-            if (*abort_flag || !mbar_wait_bounded(&empty[s], at[kv].ph ^ 1u, P.polls)) mbar_wait_bounded(&full[s], at[kv].ph ^ 1u, kAttnPolls);
+            if (*abort_flag || !mbar_wait_bounded(&empty[s], at[kv].ph ^ 1u, kAttnPolls)) mbar_wait_bounded(&full[s], at[kv].ph ^ 1u, kAttnPolls);
             at[kv].next(kv ? v_slots : k_slots);
         }
 }
@@ -549,7 +551,7 @@ __device__ __forceinline__ bool attn_widen(const AttnParams& P, AttnIter it, int
             for (int kv = kv_first; kv <= kv_last; ++kv) {
                 const int s = kv ? P.k_slots + at[1].s : at[0].s, rs = kv ? P.raw_k + from_raw[1].s : from_raw[0].s;
                 const uint32_t ph = kv ? at[1].ph : at[0].ph, rph = kv ? from_raw[1].ph : from_raw[0].ph;
-                if (!__all_sync(0xffffffffu, mbar_wait_bounded(&empty[s], ph ^ 1u, P.polls) && mbar_wait_bounded(&raw_full[rs], rph, P.polls))) return false;
+                if (!__all_sync(0xffffffffu, mbar_wait_bounded(&empty[s], ph ^ 1u, kAttnPolls) && mbar_wait_bounded(&raw_full[rs], rph, kAttnPolls))) return false;
                 if (kv == 0) ready(number);
                 const unsigned char* src = raw + (size_t)rs * kAttnTile * d;
                 unsigned char* dst = ring + (size_t)s * tile_bytes;

@@ -11,7 +11,7 @@
 //   * O^T += V^T P^T: V as it lies (mn-major), O^T has a row per component and a column per row of Q.
 // Each group has half of the columns of every tile, but for 8-bit caches and up to 16 rows, where the groups take the tiles in turn,
 // with an O^T, references and sums each, joined at the end of a unit: a tile's chain of waits and loads is longer than its
-// bytes take to arrive (128 tokens over 8192 positions of int8, 8 rows: 454 us, 536 with halves; over bf16 the same, and a single
+// bytes take to arrive (128 tokens over 8192 positions of int8, 8 rows: 454 us when it was made, 536 with halves; over bf16 the same, and a single
 // token a microsecond slower; with 32 columns a thread of an 8-bit cache has too few registers, 203 us instead of 193).  A group has two
 // S^T and P^T, so that one tile's products run while the next one's weights are made.
 //
@@ -22,7 +22,7 @@
 //
 // Bound by the cache's bytes over bf16: 64 trees of 16 nodes, 4 heads a K/V head, over 4096 positions take 212 us, 5.1 TB/s.  An 8-bit
 // cache has half of them and the same work a tile, and two kinds of warps more: 128 tokens, 8 heads a K/V head, over 8192
-// positions of int8 take 550 us, 4.0 TB/s, a tile 1 800 clocks; what bounds that is the softmax warps' chain of waits and loads.
+// positions of int8 take 441 us, 5.0 TB/s, a tile 1 800 clocks: the widening warps' waits, loads and stores, one after the other.
 #include <math.h>
 
 #include "tree_attention.cuh"
