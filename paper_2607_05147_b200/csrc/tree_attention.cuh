@@ -400,7 +400,8 @@ __device__ __forceinline__ void attn_produce(const AttnParams& P, AttnIter it, c
     RingPlace at[2];
     bool ok = true, bad_page = false;
     AttnUnit u;
-    while (ok && !*abort_flag && it.next(P, u)) {
+    // (a vote: lanes that read the flag at different times must not part, the waits below are the whole warp's)
+    while (ok && !__any_sync(0xffffffffu, *abort_flag) && it.next(P, u)) {
         const int32_t* table = P.c.block_table + u.r * P.c.table_stride;
         for (int j = u.j0; ok && j < u.j1; ++j) {
             int start, len;
@@ -542,7 +543,7 @@ __device__ __forceinline__ bool attn_widen(const AttnParams& P, AttnIter it, int
     widen_place(ct, d, from0, to0);
     RingPlace at[2], from_raw[2];
     AttnUnit u;
-    while (!*abort_flag && it.next(P, u)) {
+    while (!__any_sync(0xffffffffu, *abort_flag) && it.next(P, u)) {
         for (int j = u.j0; j < u.j1; ++j, ++number) {
             int start, len;
             attn_tile_at(P, j, start, len);
