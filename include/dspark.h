@@ -692,7 +692,8 @@ int dspark_tree_attention(const dspark_kv_cache_t* cache, int layer, const void*
  * infinity or no mass in what it looks at (DSPARK_DEV_BAD_ROW) is voided: accepted_len 0, its tokens and path -1.  (With
  * offsets that are not ascending within [0, n_rows], only accepted_len is written.)
  * Reads one entry of p and q for every node, p's row of a node when one of its children has been rejected or the walk ends
- * there, and q's row when one has been rejected.  Limits: V <= 2^24, 1 <= R <= 2^20, n_rows <= 2^24.  Errors: INVALID_ARG, SHAPE, ALIGNMENT, CUDA.  No workspace.
+ * there, and q's row when one has been rejected.  No output (nor dev_status) may share memory with another array of the call
+ * (INVALID_ARG).  Limits: V <= 2^24, 1 <= R <= 2^20, n_rows <= 2^24.  Errors: INVALID_ARG, SHAPE, ALIGNMENT, CUDA.  No workspace.
  */
 #define DSPARK_TREE_MAX_NODES 1024
 int dspark_verify_tree(const float* target_probs, int64_t target_row_stride, const float* draft_probs, int64_t draft_row_stride,

@@ -226,6 +226,12 @@ struct KernelTimerScope {
     int slot;
     cudaStream_t stream;
 };
+// whether two ranges of memory share a byte; an absent one (NULL) shares none
+inline bool ranges_meet(const void* a, size_t a_bytes, const void* b, size_t b_bytes)
+{
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return a && b && (x < y ? y - x < a_bytes : x - y < b_bytes);
+}
 int launch_status();   // maps cudaGetLastError() to DSPARK_OK / DSPARK_ERR_CUDA
 
 // Order-preserving 16-bit key of a bf16 pattern (-0 and +0 share a key; NaN is the caller's business) and back.

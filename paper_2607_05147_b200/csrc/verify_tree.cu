@@ -366,6 +366,17 @@ extern "C" int dspark_verify_tree(const float* target_probs, int64_t target_row_
          (uintptr_t)u_accept | (uintptr_t)u_sample | (uintptr_t)accepted_len | (uintptr_t)out_tokens | (uintptr_t)out_path |
          (uintptr_t)dev_status) & 3)
         return DSPARK_ERR_ALIGNMENT;
+    // The CTAs of a cluster make the same walk from the same inputs, at times of their own: one that found a result there in place of an
+    // input would take another way and meet the others at the wrong barrier.
+    const size_t rows = (size_t)n_rows * 4, requests = (size_t)R * 4;
+    const struct { const void* at; size_t bytes; } arrays[] = {
+        {accepted_len, requests}, {out_tokens, rows}, {out_path, rows}, {dev_status, 4},       // the outputs
+        {target_probs, ((size_t)(n_rows - 1) * target_row_stride + V) * 4},
+        {draft_probs, draft_probs ? ((size_t)(n_rows - 1) * draft_row_stride + V) * 4 : 0},
+        {tokens, rows}, {parents, rows}, {row_offsets, requests + 4}, {u_accept, rows}, {u_sample, requests}};
+    for (int i = 0; i < 4; ++i)
+        for (int j = i + 1; j < (int)(sizeof arrays / sizeof arrays[0]); ++j)
+            if (ranges_meet(arrays[i].at, arrays[i].bytes, arrays[j].at, arrays[j].bytes)) return DSPARK_ERR_INVALID_ARG;
     VerifyTreeParams P = {};
     P.p = target_probs; P.p_stride = target_row_stride;
     P.q = draft_probs; P.q_stride = draft_row_stride;
