@@ -636,9 +636,10 @@ int dspark_kv_read(const dspark_kv_cache_t* cache, int layer, const int32_t* fir
  * in order.
  *   accepted_len   device int32 [R]: accepted nodes without the root, n_r
  *   path           device int32 [n_rows]: path[row_offsets[r] + i], i < n_r, the nodes in ascending order (dspark_verify_tree)
- *   out_first      device int32 [R] or NULL, not first itself: first[r] + 1 + n_r, what `first` is in the next step.  A
- *                  request that is left alone, or whose path is not ascending within its nodes (DSPARK_DEV_BAD_TREE: nothing
- *                  is moved), gets first[r]; a request without rows too
+ *   out_first      device int32 [R] or NULL: first[r] + 1 + n_r, what `first` is in the next step.  It may share no memory with
+ *                  first nor with another array of the call (INVALID_ARG).  A request that is left alone, or whose path is not
+ *                  ascending within its nodes (DSPARK_DEV_BAD_TREE: nothing is moved), gets first[r]; a request without rows
+ *                  too.  A row whose old or new position has no page is not moved (DSPARK_DEV_BAD_PAGE)
  * Errors: INVALID_ARG, SHAPE, ALIGNMENT, CUDA.  No workspace.
  */
 int dspark_kv_commit(const dspark_kv_cache_t* cache, const int32_t* first, const int32_t* row_offsets, int R, int n_rows,

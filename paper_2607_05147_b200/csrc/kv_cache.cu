@@ -473,10 +473,16 @@ int dspark_kv_commit(const dspark_kv_cache_t* cache, const int32_t* first, const
                      const int32_t* accepted_len, const int32_t* path, int32_t* out_first, int32_t* dev_status, void* stream)
 {
     using namespace dspark;
-    if (!accepted_len || !path || out_first == first) return DSPARK_ERR_INVALID_ARG;
+    if (!accepted_len || !path) return DSPARK_ERR_INVALID_ARG;
     if (int e = kv_cache_check(cache, 0)) return e;
     if (int e = kv_step_check(first, row_offsets, R, n_rows, dev_status)) return e;
     if (((uintptr_t)accepted_len | (uintptr_t)path | (uintptr_t)out_first) & 3) return DSPARK_ERR_ALIGNMENT;
+    // a request's CTAs (by layers) read these at times of their own, one of them writes its entry of out_first
+    const size_t out = out_first ? (size_t)R * 4 : 0;
+    if (ranges_meet(out_first, out, first, (size_t)R * 4) || ranges_meet(out_first, out, row_offsets, (size_t)R * 4 + 4) ||
+        ranges_meet(out_first, out, accepted_len, (size_t)R * 4) || ranges_meet(out_first, out, path, (size_t)n_rows * 4) ||
+        ranges_meet(out_first, out, dev_status, 4))
+        return DSPARK_ERR_INVALID_ARG;
     KvCommit P = {};
     P.c = kv_view(cache, 0);
     P.first = first; P.row_offsets = row_offsets; P.R = R; P.n_rows = n_rows;

@@ -1,5 +1,7 @@
 """Outputs of the tree step's calls that share memory with another array: refused on the host before anything is launched (no GPU
 needed: the addresses are never used)."""
+import ctypes as C
+
 import pytest
 
 from paper_2607_05147_b200 import binding as B
@@ -30,3 +32,16 @@ def test_verify(out, other):
         a = places(VERIFY)
         a[out] = a[other] + at
         assert verify(a) == INVALID
+
+
+COMMIT = {"first": R * 4, "off": (R + 1) * 4, "acc": R * 4, "path": ROWS * 4, "st": 4}
+
+
+@pytest.mark.parametrize("other", COMMIT)
+def test_commit(other):
+    c = B.KvCacheStruct(k=0x1000000, v=0x2000000, dtype=B.DSPARK_BF16, n_layers=2, n_pages=4, page_size=16, kv_heads=2, head_dim=64,
+                        layer_stride=4 * 16 * 128, page_stride=16 * 128, token_stride=128, head_stride=64, block_table=0x3000000,
+                        block_table_stride=8, max_pages=8)
+    a = places(COMMIT)
+    for at in (0, COMMIT[other] - 4, 4 - R * 4):
+        assert B.lib().dspark_kv_commit(C.byref(c), a["first"], a["off"], R, ROWS, a["acc"], a["path"], a[other] + at, a["st"], None) == INVALID
