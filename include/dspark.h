@@ -689,9 +689,9 @@ int dspark_tree_attention(const dspark_kv_cache_t* cache, int layer, const void*
  *   out_tokens     device int32 [n_rows]: the accepted nodes' tokens, then the drawn one at n_r, -1 behind
  *   out_path       device int32 [n_rows] or NULL: the accepted nodes, -1 from n_r on
  * Sums and tests are fp64.  A request with a node whose parent is not an earlier one (DSPARK_DEV_BAD_TREE), a token outside
- * [0, V) (DSPARK_DEV_BAD_TOKEN), more than DSPARK_TREE_MAX_NODES nodes or no row at all (DSPARK_DEV_BAD_OFFSETS), or NaN, an
- * infinity or no mass in what it looks at (DSPARK_DEV_BAD_ROW) is voided: accepted_len 0, its tokens and path -1.  (With
- * offsets that are not ascending within [0, n_rows], only accepted_len is written.)
+ * [0, V) (DSPARK_DEV_BAD_TOKEN), more than DSPARK_TREE_MAX_NODES nodes (DSPARK_DEV_BAD_OFFSETS), or NaN, an infinity or no mass in
+ * what it looks at (DSPARK_DEV_BAD_ROW) is voided: accepted_len 0, its tokens and path -1.  (With offsets that are not
+ * ascending within [0, n_rows], only accepted_len is written.)  A request without rows gets accepted_len 0.
  * Reads one entry of p and q for every node, p's row of a node when one of its children has been rejected or the walk ends
  * there, and q's row when one has been rejected.  No output (nor dev_status) may share memory with another array of the call
  * (INVALID_ARG).  Limits: V <= 2^24, 1 <= R <= 2^20, n_rows <= 2^24.  Errors: INVALID_ARG, SHAPE, ALIGNMENT, CUDA.  No workspace.

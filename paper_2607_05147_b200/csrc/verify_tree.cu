@@ -127,9 +127,12 @@ __global__ void __cluster_dims__(kVtCtas, 1, 1) __launch_bounds__(kVtMaxWarps * 
     const int r = blockIdx.x / kVtCtas, rank = blockIdx.x % kVtCtas, runs = kVtCtas * P.warps;
     const int row0 = P.row_offsets[r], end = P.row_offsets[r + 1], n = end - row0;
     const bool there = row0 >= 0 && end >= row0 && end <= P.n_rows;
-    if (!there || n == 0) {
-        if (rank == 0 && tid == 0) { P.accepted_len[r] = 0; atomicOr(P.dev_status, DSPARK_DEV_BAD_OFFSETS); }
-        return;                                  // the whole cluster
+    if (!there || n == 0) {                      // the whole cluster; a request without rows is nothing to do
+        if (rank == 0 && tid == 0) {
+            P.accepted_len[r] = 0;
+            if (!there) atomicOr(P.dev_status, DSPARK_DEV_BAD_OFFSETS);
+        }
+        return;
     }
     if (tid == 0) S.status = n > DSPARK_TREE_MAX_NODES ? DSPARK_DEV_BAD_OFFSETS : 0;
     __syncthreads();
