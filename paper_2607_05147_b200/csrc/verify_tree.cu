@@ -39,6 +39,7 @@ enum VtAction { kVtPass = 0, kVtDraw = 1, kVtVoid = 2, kVtSummed = 4 };
 struct VtShared {
     double sums[2][kVtMaxWarps];                    // read by the other CTAs; one set a pass, in turn
     double all[kVtMaxRuns];                      // inclusive sums of all runs
+    double share[kVtMaxRuns];                    // the runs' own sums
     double A;
     double block[2][kVtMaxWarps];
     int action, node, length, n_gone, status, pick;
@@ -200,7 +201,7 @@ __global__ void __cluster_dims__(kVtCtas, 1, 1) __launch_bounds__(kVtMaxWarps * 
     VtRow row;
     int v0 = (rank * P.warps + warp) * P.run, v1 = v0 + P.run < P.V ? v0 + P.run : P.V;
     if (v0 > P.V) v0 = P.V;
-    // S.all = inclusive sums of the runs, the same in every CTA
+    // S.all = inclusive sums of the runs, S.share their own, the same in every CTA
     auto sum_rows = [&]() {
         const long long at_row = row0 + S.node;
         row.p = P.p + at_row * P.p_stride;
@@ -221,7 +222,10 @@ __global__ void __cluster_dims__(kVtCtas, 1, 1) __launch_bounds__(kVtMaxWarps * 
                 if (k >= runs) x[i] = 0.0;
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = run += x[i];
+            for (int i = 0; i < 4; ++i) {
+                S.share[lane * 4 + i] = x[i];
+                x[i] = run += x[i];
+            }
             double before = run;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -275,12 +279,13 @@ __global__ void __cluster_dims__(kVtCtas, 1, 1) __launch_bounds__(kVtMaxWarps * 
     vt_cluster_arrive();
     const int len = voided ? 0 : S.length;
     if (!voided) {
-        // the run that the drawn token is in: the first whose inclusive sum exceeds the target, else the last with a share
+        // the run that the drawn token is in: of those with a share the first whose inclusive sum exceeds the target, else the last
+        // (the inclusive sums are rounded in different orders: one without a share can be a step above the one before it)
         const double total = S.all[kVtMaxRuns - 1], target = (double)P.u_sample[r] * total;
         int owner = -1, last = 0;
         for (int b = 0; b < runs; b += 32) {
-            const double here = S.all[b + lane], before = b + lane ? S.all[b + lane - 1] : 0.0;
-            const uint32_t over = __ballot_sync(0xffffffffu, here > target), some = __ballot_sync(0xffffffffu, here > before);
+            const bool share = S.share[b + lane] > 0.0;
+            const uint32_t over = __ballot_sync(0xffffffffu, share && S.all[b + lane] > target), some = __ballot_sync(0xffffffffu, share);
             if (owner < 0 && over) owner = b + __ffs(over) - 1;
             if (some) last = b + 31 - __clz(some);
         }
