@@ -160,6 +160,8 @@ __device__ __forceinline__ void kv_put(unsigned char* out, int sub, uint4 x, flo
 // Which request a row belongs to: the number of requests that end at or before it.  Up to kCountRequests of them the CTA
 // counts those of its first row, one load a thread, and each row goes on from there; beyond, every row is searched for.  Up to
 // kKvThreads requests are kept in shared memory with their first tokens, so that no row waits for memory again before its page.
+// Offsets that fall somewhere (an error, reported) lead the count and the search astray: a row for which they have found no request
+// is then looked for in all of them.
 constexpr int kCountRequests = 1024;
 struct KvRequests {
     const int32_t* first; const int32_t* row_offsets;         // of all requests, in shared or global memory
@@ -195,7 +197,6 @@ __device__ __forceinline__ int kv_find_request(const KvRequests& q, int row)
     }
     return lo;
 }
-
 // Head rows [blockIdx.x * per, ...).
 template <int kLanes, int kDtype, bool kWrite>
 __global__ void __launch_bounds__(kKvThreads, 6) kv_rows_kernel(const __grid_constant__ KvStep P)
@@ -235,18 +236,31 @@ __global__ void __launch_bounds__(kKvThreads, 6) kv_rows_kernel(const __grid_con
     // where the CTA's rows are in the cache, one thread a row
     const long long capacity = kv_capacity(P.c);
     const KvRequests requests = kv_requests(P.first, P.row_offsets, P.R, row0, S);
-    if (tid < kMost) {
-        const int row = row0 + tid;
+    bool lost = false;                                        // no request was found for this thread's row
+    auto find = [&](int row, int r, bool everywhere) {
+        KvRequest q = {0, -1, 0, 0};
+        lost = row < P.n_rows;
+        for (; r < P.R; ++r) {
+            q = kv_request(requests.first, requests.row_offsets, r, P.n_rows, capacity);
+            lost = q.status == DSPARK_DEV_BAD_OFFSETS || row < q.row0 || (everywhere && row >= requests.row_offsets[r + 1]);
+            if (!lost || !everywhere) break;
+        }
         KvSlot at = {-1, 0};
-        const int r = row < P.n_rows ? kv_find_request(requests, row) : P.R;
-        if (r < P.R) {
-            const KvRequest q = kv_request(requests.first, requests.row_offsets, r, P.n_rows, capacity);
-            if (q.n >= 0 && row >= q.row0 && !kv_slot(P.c, r, q.first + row - q.row0, 0, at)) {
-                at.at = -2;
-                atomicOr(P.dev_status, DSPARK_DEV_BAD_PAGE);
-            }
+        if (!lost && q.n >= 0 && !kv_slot(P.c, r, q.first + (row - q.row0), 0, at)) {
+            at.at = -2;
+            atomicOr(P.dev_status, DSPARK_DEV_BAD_PAGE);
         }
         slots[tid] = at;
+    };
+    if (tid < kMost) {
+        const int row = row0 + tid;
+        find(row, row < P.n_rows ? kv_find_request(requests, row) : P.R, false);
+        if (lost && P.R <= kKvThreads) find(row, 0, true);
+    }
+    if (P.R > kKvThreads && __syncthreads_or(lost)) {
+        bool falls = false;
+        for (int i = tid; i < P.R; i += kKvThreads) falls = falls || P.row_offsets[i + 1] < P.row_offsets[i];
+        if (__syncthreads_or(falls) && lost) find(row0 + tid, 0, true);
     }
     __syncthreads();
 
