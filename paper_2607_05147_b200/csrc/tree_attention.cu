@@ -250,14 +250,15 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                 int start, len;
                 attn_tile_at(P, u.j0 + jj, start, len);
                 const int valid = min(len, u.length - start);               // positions of this tile that exist
-                const bool masked = start + kAttnTile > u.first || valid < kAttnTile;
+                const bool masked = start > u.first - kAttnTile || valid < kAttnTile;
                 // which positions this row sees, a bit each
                 uint32_t seen[4] = {~0u, ~0u, ~0u, ~0u};
                 if (masked && warp_live) {
-                    const int upto = P.parents ? u.first : u.first + node + 1;
+                    // positions from this tile's start on that are before the step (trees) or up to the node (chains)
+                    const int upto = min(u.first - start, kAttnTile) + (P.parents ? 0 : node + 1);
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
-                        const int c = min(min(upto - start, valid) - 32 * w, 32);
+                        const int c = min(min(upto, valid) - 32 * w, 32);
                         seen[w] = c <= 0 ? 0u : c == 32 ? ~0u : (1u << c) - 1u;
                     }
                     if (P.parents && live && start + valid > u.first) {
@@ -321,7 +322,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                             }
                             __syncwarp();
                         } else {
-                            const int last = min(u.first + node, start + valid - 1) - start;       // the last that this row sees
+                            const int last = min(min(u.first - start, kAttnTile) + node, valid - 1);       // the last that this row sees
                             const float earlier = __shfl_up_sync(0xffffffffu, top, 1);
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
@@ -438,7 +439,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                     // weight of zero in the product: zeros here, the latter added to the rows that see them at the end
                     const uint32_t i = seq + jj, s = P.k_slots + i % P.v_slots;
                     wait(&S.full[s], i / P.v_slots & 1u);
-                    if ((row & 1) == half && (start + row >= u.first || row >= valid)) {
+                    if ((row & 1) == half && (row >= u.first - start || row >= valid)) {
                         if (attn_clean_values(ring + (size_t)s * tile_bytes + row * 128, row, P.chunks, row < valid))
                             S.bad_value[units % kAttnUnitFlags] = 1;
                     }
@@ -557,7 +558,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                 int start, len;
                 attn_tile_at(P, j, start, len);
                 k_now = v_now = 0.f;
-                node = start + ct >= w.first;
+                node = ct >= w.first - start;
                 if (ct >= min(kAttnTile, min(len, w.length - start))) return;
                 const int position = start + ct, page_of = attn_page_of(P, position), token = position - page_of * P.c.page_size;
                 const int page = P.c.block_table[w.r * P.c.table_stride + page_of];

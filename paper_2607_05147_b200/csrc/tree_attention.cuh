@@ -55,7 +55,7 @@ struct AttnParams {
 // cache tiles that hold positions 0 .. length - 1
 __device__ __forceinline__ int attn_tiles(const AttnParams& P, int length)
 {
-    if (P.c.page_size <= kAttnTile) return (length + kAttnTile - 1) / kAttnTile;
+    if (P.c.page_size <= kAttnTile) return (int)(((uint32_t)length + kAttnTile - 1) / kAttnTile);     // (lengths up to 2^31 - 1)
     const int pages = length / P.c.page_size;
     return pages * P.page_tiles + (length - pages * P.c.page_size + kAttnTile - 1) / kAttnTile;
 }

@@ -293,11 +293,11 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                 int start, len;
                 attn_tile_at(P, u.j0 + jj, start, len);
                 const int valid = min(len, u.length - start);               // positions of this tile that exist
-                const bool masked = start + kAttnTile > u.first || valid < kAttnTile;
+                const bool masked = start > u.first - kAttnTile || valid < kAttnTile;
                 // rows that see this thread's position, a bit each
                 unsigned long long seen = ~0ull;
                 if (masked) {
-                    const int node = start + pos - u.first;                 // the node at this position
+                    const int node = start - u.first + pos;                 // the node at this position
                     if (pos >= valid) seen = 0;
                     else if (node >= 0 && !P.parents) {
                         const int shift = (node - u.node0) * P.group;
@@ -435,7 +435,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                     // weight of zero in the product: zeros here, the latter added to the rows that see them at the end
                     const uint32_t s = P.k_slots + number % P.v_slots;
                     wait(&S.full[s], number / P.v_slots & 1u);
-                    if ((kTurns || (pos & 1) == t) && (start + pos >= u.first || pos >= valid))
+                    if ((kTurns || (pos & 1) == t) && (pos >= u.first - start || pos >= valid))
                         if (attn_clean_values(ring + (size_t)s * tile_bytes + pos * 128, pos, P.chunks, pos < valid))
                             S.bad_value[units % kAttnUnitFlags] = 1;
                 }
