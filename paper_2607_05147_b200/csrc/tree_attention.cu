@@ -44,9 +44,12 @@ struct AttnShared {
     float of_half[2][2][kAttnTile];              // what the two threads of a row tell one another: largest scores, sums
 };
 template <int kKind>
-struct AttnScales {                              // q: per row; bad: a bit for a node's position with a scale that is no number
+struct AttnScales {                              // q: per row
     float k[kAttnScaleTiles][kAttnTile], v[kAttnScaleTiles][kAttnTile], q[2][kAttnTile];
-    uint32_t bad[kAttnScaleTiles][4];
+    // Nodes' positions, which some rows do not see, whose K scale is not a positive number: a bit each in odd, the scale here and 1
+    // in k.  A score of -infinity has to stay that after the product with k.
+    float odd_k[kAttnScaleTiles][kAttnTile];
+    uint32_t odd[kAttnScaleTiles][4];
 };
 template <> struct AttnScales<kAttnWide> {};
 
@@ -335,19 +338,19 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                     }
                     above -= kAttnNarrowOffset;
                     if (masked) {
-                        // scores of positions that the row does not see: -infinity, in place; NaN where a scale is no number
+                        // scores of positions that the row does not see: -infinity, in place
                         __syncwarp();
 #pragma unroll
                         for (int w = 0; w < 2; ++w) {
-                            const uint32_t on = half ? seen[2 + w] : seen[w], bad = on & scales.bad[at][half * 2 + w];
-                            attn_hide(tS + w * 32, on, bad);
+                            const uint32_t on = half ? seen[2 + w] : seen[w], odd = on & scales.odd[at][half * 2 + w];
+                            attn_hide<true>(tS + w * 32, on, odd, scales.odd_k[at] + half * 64 + w * 32);
                         }
                     }
                     }
                 } else if (masked && warp_live) {
                     __syncwarp();
 #pragma unroll
-                    for (int w = 0; w < 2; ++w) attn_hide(tS + w * 32, half ? seen[2 + w] : seen[w], 0u);
+                    for (int w = 0; w < 2; ++w) attn_hide<false>(tS + w * 32, half ? seen[2 + w] : seen[w], 0u, nullptr);
                 }
                 if (warp_live) {
                     // scores from tensor memory, with an 8-bit cache times K's scales; the next ones are asked for meanwhile
@@ -553,13 +556,14 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
             const int ct = tid - (kRowWarps + 2) * 32;
             // scales of position ct of a tile
             float k_now = 0.f, v_now = 0.f;
-            bool node = false;
+            bool node = false, exists = false;
             auto load_scales = [&](const AttnUnit& w, int j) {
                 int start, len;
                 attn_tile_at(P, j, start, len);
                 k_now = v_now = 0.f;
                 node = ct >= w.first - start;
-                if (ct >= min(kAttnTile, min(len, w.length - start))) return;
+                exists = ct < min(kAttnTile, min(len, w.length - start));
+                if (!exists) return;
                 const int position = start + ct, page_of = attn_page_of(P, position), token = position - page_of * P.c.page_size;
                 const int page = P.c.block_table[w.r * P.c.table_stride + page_of];
                 if (page < 0 || page >= P.c.n_pages) return;
@@ -571,12 +575,14 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                 // free: the scores of tile number - 2 are not computed before the weights of tile number - 4 are there
                 if (ct >= kAttnTile) return;
                 const int at = number % kAttnScaleTiles;
-                const bool bad = node && !(fabsf(k_now) < INFINITY && fabsf(v_now) < INFINITY);
+                const bool bad = node && !(fabsf(k_now) < INFINITY && fabsf(v_now) < INFINITY);     // NaN for the rows that see it
                 const float k = k_now * P.score_factor;
-                scales.k[at][ct] = bad ? 1.f : k < kAttnLeastFactor ? kAttnLeastFactor : k;
+                const bool odd = exists && node && (bad || !(k > 0.f));
+                scales.k[at][ct] = odd || !exists ? 1.f : k;
+                scales.odd_k[at][ct] = bad ? NAN : k;
                 scales.v[at][ct] = bad ? 0.f : v_now;
-                const uint32_t bits = __ballot_sync(0xffffffffu, bad);
-                if (lane == 0) scales.bad[at][ct >> 5] = bits;
+                const uint32_t bits = __ballot_sync(0xffffffffu, odd);
+                if (lane == 0) scales.odd[at][ct >> 5] = bits;
             };
             if (!attn_widen<kKind, kAttnConverters * 32, false>(P, it, ct, 0, 1, raw, ring, tile_bytes, S.raw_full, S.raw_empty, S.full, S.empty, 0u, S.bad_value, abort_flag, load_scales,
                                         store_scales) && lane == 0)
@@ -797,7 +803,8 @@ int dspark_tree_attention(const dspark_kv_cache_t* cache, int layer, const void*
     P.out_lse = out_lse;
     P.first = first; P.row_offsets = row_offsets; P.parents = parents;
     P.R = R; P.n_rows = n_rows; P.q_heads = q_heads;
-    P.score_factor = fmaxf(fabsf(scale) * kAttnLog2e, kAttnLeastFactor);
+    P.score_factor = fabsf(scale) * kAttnLog2e;
+    if (cache->dtype == DSPARK_BF16 && P.score_factor == 0.f) P.score_factor = kAttnLeastFactor;
     P.q_sign = scale < 0.f ? 0x80008000u : 0u;
     P.dev_status = dev_status;
     // rows of a request with one K/V head on average

@@ -22,7 +22,7 @@ constexpr float kAttnLog2e = 1.4426950408889634f;
 constexpr float kAttnLazy = 8.f;                 // O is scaled when the maximum rises by more than 2^8
 constexpr float kAttnNarrowOffset = 7.f;         // fp16 weights: up to 2^(7 + 8) of 65 504, down to 2^-31 of the largest
 constexpr float kAttnUnset = -1e38f;              // a reference that every score is above
-constexpr float kAttnLeastFactor = 1e-20f;       // of a score: -infinity times it is -infinity, a score times it next to nothing
+constexpr float kAttnLeastFactor = 1.4e-45f;     // the smallest number: -infinity times it is -infinity, a score times it next to nothing
 constexpr int kAttnUnitFlags = 8;               // units of one CTA that are under way at a time: at most four
 
 enum AttnKind { kAttnWide = 0, kAttnI8 = 1, kAttnE4M3 = 2 };
@@ -317,20 +317,21 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi)
     else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-// 32 columns of scores: -infinity where `on` has no bit, NaN where `bad` has one
-__device__ __forceinline__ void attn_hide(uint32_t addr, uint32_t on, uint32_t bad)
+// 32 columns of scores: -infinity where `on` has no bit, times the column's entry of `by` where `odd` (of those in `on`) has one
+template <bool kOdd>
+__device__ __forceinline__ void attn_hide(uint32_t addr, uint32_t on, uint32_t odd, const float* by)
 {
 #pragma unroll 1
-    for (int c = 0; c < 32; c += 16, on >>= 16, bad >>= 16) {
-        if (__all_sync(0xffffffffu, (on & 0xffffu) == 0xffffu && (bad & 0xffffu) == 0u)) continue;
+    for (int c = 0; c < 32; c += 16, on >>= 16, odd >>= 16) {
+        if (__all_sync(0xffffffffu, (on & 0xffffu) == 0xffffu && (!kOdd || (odd & 0xffffu) == 0u))) continue;
         float s[16];
         uint32_t x[16];
         tmem_load16(addr + c, s);
+        if (kOdd && __any_sync(0xffffffffu, (odd & 0xffffu) != 0u))
+#pragma unroll
+            for (int i = 0; i < 16; ++i) if (odd & (1u << i)) s[i] *= by[c + i];
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] = on & (1u << i) ? __float_as_uint(s[i]) : 0xff800000u;
-        if (__any_sync(0xffffffffu, (on & bad & 0xffffu) != 0u))
-#pragma unroll
-            for (int i = 0; i < 16; ++i) if (on & bad & (1u << i)) x[i] = 0x7fffffffu;
         tmem_store16(addr + c, x);
     }
     tmem_store_wait();

@@ -333,7 +333,6 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                 float above = 0.f;
                 if constexpr (kNarrow) {
                     k_scale *= scale.x;
-                    if (k_scale < kAttnLeastFactor) k_scale = kAttnLeastFactor;
                     above = attn_exponent(scale.y < INFINITY ? fmaxf(scale.y, 0.f) : 0.f) - kAttnNarrowOffset;
                 }
                 if (turn) wait(&S.o_done[b], (turn - 1) & 1u);              // P^T that was here before has been multiplied
@@ -343,7 +342,8 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                 if (row0 < rows) {
                     __syncwarp();
                     if (masked) {
-                        // scores of rows that do not see the position: -infinity, in place.  Where a scale is no number the
+                        // scores of rows that do not see the position: -infinity, in place; over an 8-bit cache the others times
+                        // K's scale (-infinity times one that is not positive would not stay that).  Where a scale is no number the
                         // position is NaN for the rows that see it, and the scales are not used.
                         const bool bad = kNarrow && !(fabsf(scale.x) < INFINITY && fabsf(scale.y) < INFINITY);
 #pragma unroll 1
@@ -351,11 +351,12 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                             float s[8];
                             attn_read<8>(tS + c0, s);
 #pragma unroll
-                            for (int c = 0; c < 8; ++c) s[c] = !(seen >> (c0 + c) & 1) ? -INFINITY : bad ? NAN : s[c];
+                            for (int c = 0; c < 8; ++c) s[c] = !(seen >> (c0 + c) & 1) ? -INFINITY : bad ? NAN : kNarrow ? s[c] * k_scale : s[c];
                             attn_write<8>(tS + c0, reinterpret_cast<const uint32_t (&)[8]>(s));
                         }
                         tmem_store_wait();
-                        if (bad) { k_scale = 1.f; v_scale = 0.f; above = -kAttnNarrowOffset; }
+                        if (kNarrow) k_scale = 1.f;
+                        if (bad) { v_scale = 0.f; above = -kAttnNarrowOffset; }
                     }
                     // y = score * factor - reference
                     const uint64_t k2 = pack2(k_scale, k_scale);
