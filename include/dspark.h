@@ -595,7 +595,8 @@ int dspark_lm_head_loss_backward_from_loss(const void* hidden, int64_t hidden_ro
  *   k, v               device, element (layer, page, token, head, i) at
  *                      layer * layer_stride + page * page_stride + token * token_stride + head * head_stride + i elements;
  *                      both have these strides.  16-byte aligned, strides multiples of 16 bytes
- *   dtype              DSPARK_BF16, or DSPARK_I8 / DSPARK_E4M3 with one scale per token and head: value = scale * stored
+ *   dtype              DSPARK_BF16, or DSPARK_I8 / DSPARK_E4M3 with one scale (of either sign) per token and head: value = scale *
+ *                      stored
  *   k_scale, v_scale   device fp32 [n_layers][n_pages][kv_heads][page_size] (NULL with DSPARK_BF16), 4-byte aligned
  *   page_size          a power of two from 8 to 128, or any number above 128
  *   head_dim           a multiple of 16, at most 256 (dspark_tree_attention: at most 128)

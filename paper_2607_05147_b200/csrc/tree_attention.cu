@@ -295,7 +295,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                     fk = scales.k[at] + half * 64;
                     fv = scales.v[at] + half * 64;
                     if (!any) factor = scales.q[tile][row];                 // stored before Q was announced
-                    if (!masked) above = attn_exponent(warp_max_f32(attn_finite_max(reinterpret_cast<const float4*>(all)[lane], ~0u, 0.f)));
+                    if (!masked) above = attn_exponent(warp_max_f32(attn_finite_max(reinterpret_cast<const float4*>(all)[lane])));
                     else {                       // of the positions that this row sees
                         // every lane has four positions' scales: the largest up to each (a chain), or of those before the step (a tree)
                         __syncwarp();
@@ -304,7 +304,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                         float upto[4], top = 0.f;
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const float x = i == 0 ? mine.x : i == 1 ? mine.y : i == 2 ? mine.z : mine.w;
+                            const float x = fabsf(i == 0 ? mine.x : i == 1 ? mine.y : i == 2 ? mine.z : mine.w);
                             upto[i] = top = i < before && x < INFINITY ? fmaxf(top, x) : top;
                         }
 #pragma unroll
@@ -319,7 +319,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                             for (int w = 0; w < 4; ++w) {
                                 uint32_t of = tree >= 32 * w + 32 ? 0u : tree > 32 * w ? seen[w] >> (tree - 32 * w) << (tree - 32 * w) : seen[w];
                                 for (; of; of &= of - 1) {
-                                    const float x = all[w * 32 + __ffs(of) - 1];
+                                    const float x = fabsf(all[w * 32 + __ffs(of) - 1]);
                                     if (x < INFINITY) top = fmaxf(top, x);
                                 }
                             }

@@ -351,14 +351,11 @@ __device__ __forceinline__ bool barrier_any(int id, bool x)
                  : "=r"(r) : "r"((uint32_t)x), "r"(id), "n"(kThreads) : "memory");
     return r != 0;
 }
-// the largest of those of four scales that are finite and asked for
-__device__ __forceinline__ float attn_finite_max(float4 x, uint32_t of, float top)
+// the largest magnitude of four scales that is finite
+__device__ __forceinline__ float attn_finite_max(float4 x)
 {
-    if ((of & 1u) && x.x < INFINITY) top = fmaxf(top, x.x);
-    if ((of & 2u) && x.y < INFINITY) top = fmaxf(top, x.y);
-    if ((of & 4u) && x.z < INFINITY) top = fmaxf(top, x.z);
-    if ((of & 8u) && x.w < INFINITY) top = fmaxf(top, x.w);
-    return top;
+    const float a = fabsf(x.x), b = fabsf(x.y), c = fabsf(x.z), d = fabsf(x.w);
+    return max3(fmaxf(a < INFINITY ? a : 0.f, b < INFINITY ? b : 0.f), c < INFINITY ? c : 0.f, d < INFINITY ? d : 0.f);
 }
 // e with 2^e > x, of a size that keeps the softmax's sum in range
 __device__ __forceinline__ float attn_exponent(float x) { return fmaxf((float)((int)(__float_as_uint(x) >> 23) - 126), -60.f); }

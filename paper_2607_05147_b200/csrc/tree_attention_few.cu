@@ -329,11 +329,11 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                 const float2 scale = scale_next;
                 scale_next = scales_of(u, ahead);
                 ahead = page_of(u, jj + 2 * kStep);
-                // an 8-bit V: 2^exponent > its scale; what a weight may be above its reference depends on it
+                // an 8-bit V: 2^exponent > its scale's size; what a weight may be above its reference depends on it
                 float above = 0.f;
                 if constexpr (kNarrow) {
                     k_scale *= scale.x;
-                    above = attn_exponent(scale.y < INFINITY ? fmaxf(scale.y, 0.f) : 0.f) - kAttnNarrowOffset;
+                    above = attn_exponent(fabsf(scale.y) < INFINITY ? fabsf(scale.y) : 0.f) - kAttnNarrowOffset;
                 }
                 if (turn) wait(&S.o_done[b], (turn - 1) & 1u);              // P^T that was here before has been multiplied
                 wait(&S.s_full[b], turn & 1u);

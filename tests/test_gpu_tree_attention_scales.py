@@ -94,3 +94,23 @@ def test_a_node_that_a_row_does_not_see_with_a_negative_scale(kind, shape):
     same = torch.ones(q.shape[0], dtype=torch.bool, device="cuda")
     same[changed] = False
     assert torch.equal(got[same], clean[same])
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("shape", range(len(STEPS)))
+@pytest.mark.parametrize("tree", ["chain", "tree"])
+def test_scales_of_v_of_either_sign(kind, shape, tree):
+    first, nodes, group = STEPS[shape]
+    cache, q = step(first, nodes, 16, 2, group, 64, kind, seed=shape)
+    signs(cache.vs, T.gen(3))
+    check(cache, q, first, nodes, None if tree == "chain" else T.random_parents(nodes, 3), 0.2)
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("shape", range(len(STEPS)))
+@pytest.mark.parametrize("size", [-1.0, -100.0, -1e9, -1e20])
+def test_scales_of_v_all_negative(kind, shape, size):
+    first, nodes, group = STEPS[shape]
+    cache, q = step(first, nodes, 16, 2, group, 64, kind, seed=shape)
+    cache.vs.mul_(size)
+    check(cache, q, first, nodes, T.random_parents(nodes, 3), 0.2)
