@@ -660,7 +660,9 @@ int dspark_kv_commit(const dspark_kv_cache_t* cache, const int32_t* first, const
  *   workspace   dspark_tree_attention_workspace_bytes(...), 256-byte aligned, any content; one call at a time
  * The products are bf16 (an 8-bit cache: 16-bit operands that hold its values exactly) with fp32 accumulation; softmax
  * statistics are fp32; the weights are rounded to 16 bits for their product with v (an 8-bit cache: times v's scale and relative
- * to the row's largest such product; what is 2^-32 of that is lost).  The same inputs give the same bits.
+ * to the row's largest such product; what is 2^-32 of that is lost, and what is below 2^-112 of the largest weight: where all of
+ * v's scales that a row sees are below 2^-80 digits go, and where they are below 2^-112 the row is zero; above 2^100 the small
+ * weights go).  The same inputs give the same bits.
  * Two launches: one CTA per SM with most of its shared memory and all of its tensor memory, and a short one that joins the
  * parts of what was divided between SMs.  A wait inside that runs out (none does unless something is broken) sets
  * DSPARK_DEV_TIMEOUT; the outputs are then unspecified.

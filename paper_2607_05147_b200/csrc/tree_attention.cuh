@@ -357,8 +357,9 @@ __device__ __forceinline__ float attn_finite_max(float4 x)
     const float a = fabsf(x.x), b = fabsf(x.y), c = fabsf(x.z), d = fabsf(x.w);
     return max3(fmaxf(a < INFINITY ? a : 0.f, b < INFINITY ? b : 0.f), c < INFINITY ? c : 0.f, d < INFINITY ? d : 0.f);
 }
-// e with 2^e > x, of a size that keeps the softmax's sum in range
-__device__ __forceinline__ float attn_exponent(float x) { return fmaxf((float)((int)(__float_as_uint(x) >> 23) - 126), -60.f); }
+// e with 2^e > x; not below -80, so that the softmax's sum stays in range: a weight before its product with V's scale is at most
+// 2^(kAttnNarrowOffset + kAttnLazy + 80) of the reference, 2^31 positions' sum 2^126.  (Scales below 2^-80 shrink the fp16 weights.)
+__device__ __forceinline__ float attn_exponent(float x) { return fmaxf((float)((int)(__float_as_uint(x) >> 23) - 126), -80.f); }
 // four 8-bit values as fp16, exactly
 template <int kKind>
 __device__ __forceinline__ uint2 widen4(uint32_t w)

@@ -23,11 +23,14 @@ class Magnitudes:
         self.vs = None if cache.vs is None else cache.vs.abs()
 
 
-def check(cache, q, first, nodes, parents, scale):
+def check(cache, q, first, nodes, parents, scale, lost=0.0):
+    """lost: what is lost of each position beside the bound of T.attention, of the largest weight and stored value."""
     off = T.offsets(nodes)
     got, lse, st = T.run_attention(cache, q, T.i32(first), off, None if parents is None else T.i32(parents), scale)
     assert st == 0
     want, bound, want_lse, lse_bound = T.attention(Magnitudes(cache), q, first, off.tolist(), parents, scale)
+    if lost:
+        bound = bound + lost * max(f + n for f, n in zip(first, nodes)) * (127 if cache.kind == "int8" else 448)
     assert bool(((got.double() - want).abs() <= bound).all()), float(((got.double() - want).abs() / bound).max())
     assert bool(((lse.double() - want_lse).abs() <= lse_bound).all())
     return got
@@ -114,3 +117,30 @@ def test_scales_of_v_all_negative(kind, shape, size):
     cache, q = step(first, nodes, 16, 2, group, 64, kind, seed=shape)
     cache.vs.mul_(size)
     check(cache, q, first, nodes, T.random_parents(nodes, 3), 0.2)
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("shape", range(len(STEPS)))
+@pytest.mark.parametrize("tree", ["chain", "tree"])
+def test_small_scales_of_v(kind, shape, tree):
+    # the largest at 2^-79: no digit is lost
+    first, nodes, group = STEPS[shape]
+    cache, q = step(first, nodes, 16, 2, group, 64, kind, seed=shape)
+    assert not cache.vs.isfinite().all()                      # (places that no request has)
+    seen = torch.where(cache.vs.isfinite(), cache.vs, 0.0)
+    cache.vs.mul_(2.0 ** -79 / float(seen.max()))
+    check(cache, q, first, nodes, None if tree == "chain" else T.random_parents(nodes, 3), 0.2)
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("shape", range(len(STEPS)))
+def test_values_around_1e_minus_26(kind, shape):
+    # scales of 2^-92 and less, as dspark_kv_write stores them: 2^-112 of the largest weight is lost of a position, half a step of
+    # 2^-24 where the reference's weight is 2^7 at a scale of 2^-80; twice that, for the reference may be above the largest weight's
+    first, nodes, group = STEPS[shape]
+    cache, q = step(first, nodes, 16, 2, group, 64, kind, seed=shape)
+    g = T.gen(shape)
+    for r, n in enumerate(f + m for f, m in zip(first, nodes)):
+        x = torch.randn(2, n, 2, 64, generator=g, device="cuda")
+        cache.put(r, range(n), x[0], (x[1] + 0.5) * 1e-26)
+    check(cache, q, first, nodes, T.random_parents(nodes, 3), 0.2, lost=2 * 2.0 ** -112)
