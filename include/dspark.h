@@ -654,7 +654,8 @@ int dspark_kv_commit(const dspark_kv_cache_t* cache, const int32_t* first, const
  *               q_heads = group * kv_heads with group <= 128.  out may be q itself with the same strides
  *   parents     device int32 [n_rows], the parent's index within the request (the root's entry is not read); NULL: chains,
  *               node i sees the nodes up to i.  A parent that is not an earlier node sets DSPARK_DEV_BAD_TREE and ends the
- *               ancestors there
+ *               ancestors there; so does the 4097th ancestor of a node, not counting those in the chain that its request
+ *               begins with (a prompt given with parents is one chain, however long)
  *   scale       finite
  *   out_lse     device fp32 [n_rows][q_heads] or NULL: log of the sum of e^(scale * q . k) over the positions seen
  *   workspace   dspark_tree_attention_workspace_bytes(...), 256-byte aligned, any content; one call at a time

@@ -39,6 +39,7 @@ struct AttnShared {
     uint64_t q_full, s_full[2], p_full[2], o_full[2], merge_ready, merge_done, mma_done;
     uint32_t tmem_base;
     int abort, bad_value[kAttnUnitFlags];
+    AttnStraight straight[16];                   // of each softmax warp
     AttnList list;
     float2 second[kAttnTile];                    // (reference, sum) of the second group
     float of_half[2][2][kAttnTile];              // what the two threads of a row tell one another: largest scores, sums
@@ -82,6 +83,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
         for (int t = 0; t < 2; ++t) { mbar_init(&S.s_full[t], 1); mbar_init(&S.p_full[t], kRowWarps / 2); mbar_init(&S.o_full[t], 1); }
         for (int i = 0; i < kAttnUnitFlags; ++i) S.bad_value[i] = 0;
         mbar_init(&S.merge_ready, kRowWarps / 2); mbar_init(&S.merge_done, kRowWarps / 2); mbar_init(&S.mma_done, 1);
+        for (AttnStraight& x : S.straight) x.of = -1;
         S.abort = 0;
         mbar_fence_init();
     }
@@ -243,6 +245,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
             const int node = u.node0 + tile * tile_nodes + row / P.group;
             const bool live = row < tile_nodes * P.group && node < u.n;
             const bool warp_live = __any_sync(0xffffffffu, live);           // the same in both warps
+            attn_look_at_tree(P, u, S.straight[warp]);
             float factor = P.score_factor;       // 8-bit caches: what the row of Q was scaled by (K's scales hold score_factor)
             if (tid == 0) S.bad_value[(units + kAttnUnitFlags / 2) % kAttnUnitFlags] = 0;
             float ref = kAttnUnset, sum = 0.f;   // O and the sum are relative to 2^ref
@@ -256,28 +259,36 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                 const bool masked = start > u.first - kAttnTile || valid < kAttnTile;
                 // which positions this row sees, a bit each
                 uint32_t seen[4] = {~0u, ~0u, ~0u, ~0u};
+                bool chain = true;               // every node of the unit sees all before it
                 if (masked && warp_live) {
-                    // positions from this tile's start on that are before the step (trees) or up to the node (chains)
-                    const int upto = min(u.first - start, kAttnTile) + (P.parents ? 0 : node + 1);
+                    // positions from this tile's start on that are before the step, or up to a node: a range; other nodes one by one
+                    const int straight = attn_straight_of(P, u, S.straight[warp]), before = min(u.first - start, kAttnTile);
+                    auto see_to = [&](int upto) {
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        const int c = min(min(upto, valid) - 32 * w, 32);
-                        seen[w] = c <= 0 ? 0u : c == 32 ? ~0u : (1u << c) - 1u;
-                    }
-                    if (P.parents && live && start + valid > u.first) {
-                        int a = node;
+                        for (int w = 0; w < 4; ++w) {
+                            const int c = min(min(upto, valid) - 32 * w, 32);
+                            seen[w] = c <= 0 ? 0u : c == 32 ? ~0u : (1u << c) - 1u;
+                        }
+                    };
+                    chain = min(u.n, u.node0 + P.unit_nodes) <= straight;
+                    see_to(before + (node < straight ? node + 1 : 0));
+                    if (node >= straight && live && start + valid > u.first) {
+                        int a = node, steps = 0;
+                        uint32_t one[4] = {0u, 0u, 0u, 0u};
                         for (;;) {
+                            if (a < straight) { see_to(before + a + 1); break; }
                             const int at = u.first + a - start;
                             if (at < 0) break;
                             if (at < valid) {
 #pragma unroll
-                                for (int w = 0; w < 4; ++w) if ((at >> 5) == w) seen[w] |= 1u << (at & 31);
+                                for (int w = 0; w < 4; ++w) if ((at >> 5) == w) one[w] |= 1u << (at & 31);
                             }
                             if (a == 0) break;
-                            const int p = P.parents[u.row0 + a];
-                            if (p < 0 || p >= a) { atomicOr(P.dev_status, DSPARK_DEV_BAD_TREE); break; }
-                            a = p;
+                            a = attn_parent(P, u.row0, a, steps);
+                            if (a < 0) break;
                         }
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) seen[w] |= one[w];
                     }
                 }
                 wait(&S.s_full[t], items & 1u);
@@ -300,7 +311,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                         // every lane has four positions' scales: the largest up to each (a chain), or of those before the step (a tree)
                         __syncwarp();
                         const float4 mine = reinterpret_cast<const float4*>(all)[lane];
-                        const int before = P.parents ? u.first - start - lane * 4 : 4;     // that many of the four
+                        const int before = chain ? 4 : u.first - start - lane * 4;         // that many of the four
                         float upto[4], top = 0.f;
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
@@ -312,7 +323,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                             const float x = __shfl_up_sync(0xffffffffu, top, o);
                             if (lane >= o) top = fmaxf(top, x);
                         }
-                        if (P.parents) {
+                        if (!chain) {
                             top = __shfl_sync(0xffffffffu, top, 31);
                             const int tree = max(u.first - start, 0);       // the first node's place
 #pragma unroll

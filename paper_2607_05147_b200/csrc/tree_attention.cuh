@@ -23,6 +23,8 @@ constexpr float kAttnLazy = 8.f;                 // O is scaled when the maximum
 constexpr float kAttnNarrowOffset = 7.f;         // fp16 weights: up to 2^(7 + 8) of 65 504, down to 2^-31 of the largest
 constexpr float kAttnUnset = -1e38f;              // a reference that every score is above
 constexpr float kAttnLeastFactor = 1.4e-45f;     // the smallest number: -infinity times it is -infinity, a score times it next to nothing
+constexpr int kAttnMaxWalk = 4096;               // ancestors of a node outside the chain that its request begins with
+constexpr int kAttnNoTree = 0x7fffffff;
 constexpr int kAttnUnitFlags = 8;               // units of one CTA that are under way at a time: at most four
 
 enum AttnKind { kAttnWide = 0, kAttnI8 = 1, kAttnE4M3 = 2 };
@@ -214,6 +216,53 @@ __device__ __forceinline__ AttnIter attn_begin(const AttnParams& P, AttnList& S)
     }
     if (tid == 0) P.cuts[blockIdx.x] = cut;
     return it;
+}
+
+// ---- trees -----------------------------------------------------------------------------------------------
+// Nodes 0 .. straight - 1 of a request are a chain, whatever comes behind: what a node in it sees is a range, and a walk to the root
+// ends where it meets it.  A prompt given with parents is one such chain; walked node by node for each of its tiles 8192 tokens took
+// 101 ms instead of 1.3.  Looked for only where a request has more nodes than a tile.  Not inline, like the walks of few rows: with this
+// code among the softmax warps' the SM's roles no longer fit its instruction caches (128 tokens over int8: 732 us instead of 443).
+constexpr int kAttnStraightLoads = 16;
+static __device__ __noinline__ int attn_straight(const int32_t* parents, int n)     // a whole warp
+{
+    const int lane = threadIdx.x & 31;
+    for (int i0 = 1; i0 < n; i0 += kAttnStraightLoads * 32) {
+        int p[kAttnStraightLoads];
+#pragma unroll
+        for (int k = 0; k < kAttnStraightLoads; ++k) {
+            const int i = i0 + k * 32 + lane;
+            p[k] = i < n ? parents[i] : i - 1;
+        }
+#pragma unroll
+        for (int k = 0; k < kAttnStraightLoads; ++k) {
+            const uint32_t off = __ballot_sync(0xffffffffu, p[k] != i0 + k * 32 + lane - 1);
+            if (off) return i0 + k * 32 + __ffs(off) - 1;
+        }
+    }
+    return n;
+}
+// What a warp of the softmax has found of the request it is at; kAttnNoTree where no parents are given.
+struct AttnStraight { int of, length; };
+__device__ __forceinline__ void attn_look_at_tree(const AttnParams& P, const AttnUnit& u, volatile AttnStraight& S)
+{
+    if (!P.parents || u.n <= kAttnTile || S.of == u.r) return;
+    const int length = attn_straight(P.parents + u.row0, u.n);
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) { S.length = length; S.of = u.r; }
+    __syncwarp();
+}
+__device__ __forceinline__ int attn_straight_of(const AttnParams& P, const AttnUnit& u, const volatile AttnStraight& S)
+{
+    return !P.parents ? kAttnNoTree : u.n <= kAttnTile ? 0 : S.length;
+}
+// A walk's next node: the parent of a > 0, -1 where there is none (reported)
+__device__ __forceinline__ int attn_parent(const AttnParams& P, int row0, int a, int& steps)
+{
+    const int p = P.parents[row0 + a];
+    if (p >= 0 && p < a && ++steps <= kAttnMaxWalk) return p;
+    atomicOr(P.dev_status, DSPARK_DEV_BAD_TREE);
+    return -1;
 }
 
 // ---- PTX -------------------------------------------------------------------------------------------------

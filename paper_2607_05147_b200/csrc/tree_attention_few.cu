@@ -45,6 +45,7 @@ struct FewShared {
     uint64_t q_full, q_empty, s_full[4], p_full[4], o_done[4], mma_done[2];
     uint32_t tmem_base;
     int abort, bad_value[kAttnUnitFlags];
+    AttnStraight straight[8];                    // of each softmax warp
     AttnList list;
 };
 template <int kN>
@@ -62,6 +63,27 @@ __device__ __forceinline__ void group_sync(int group) { asm volatile("barrier.ct
 // eight warps widen 8-bit tiles where their registers leave the softmax enough
 template <int kKind, int kN> constexpr int kFewConverters = kKind == kAttnWide ? 0 : kN == 64 ? 4 : 8;   // eight: four for K, four for V
 template <int kKind, int kN> constexpr int kFewThreads = (kSoftmaxWarps + 3 + kFewConverters<kKind, kN>) * 32;
+
+// The tile's positions that node `self` sees (the unit's node number `place`) get the bits of its rows.  first: where the request's
+// nodes begin in the tile.
+static __device__ __noinline__ void few_mark(const AttnParams& P, int row0, int first, int self, int place, int straight, int valid,
+                                             unsigned long long* seen)
+{
+    const unsigned long long bits = (P.group == 64 ? ~0ull : (1ull << P.group) - 1) << (place * P.group);
+    int a = self, steps = 0;
+    for (;;) {
+        const int at = first + a;
+        if (a < straight) {
+            for (int i = max(first, 0); i <= min(at, valid - 1); ++i) atomicOr(&seen[i], bits);
+            return;
+        }
+        if (at < 0) return;
+        if (at < valid) atomicOr(&seen[at], bits);
+        if (a == 0) return;
+        a = attn_parent(P, row0, a, steps);
+        if (a < 0) return;
+    }
+}
 
 template <int kKind, int kN>
 __global__ void __launch_bounds__(kFewThreads<kKind, kN>, 1)
@@ -94,6 +116,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
         for (int b = 0; b < kBuffers; ++b) { mbar_init(&S.s_full[b], 1); mbar_init(&S.p_full[b], kTurns ? 4 : 8); mbar_init(&S.o_done[b], 1); }
         for (int t = 0; t < 2; ++t) mbar_init(&S.mma_done[t], 1);
         for (int i = 0; i < kAttnUnitFlags; ++i) S.bad_value[i] = 0;
+        for (AttnStraight& x : S.straight) x.of = -1;
         S.abort = 0;
         mbar_fence_init();
     }
@@ -285,6 +308,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
             const int count = u.j1 - u.j0, rows = min(P.tile_nodes, u.n - u.node0) * P.group;
             bool left = false;
             const int first = first_tile(item);
+            attn_look_at_tree(P, u, S.straight[warp]);
             for (int jj = first; jj < count; jj += kStep) {
                 const uint32_t number = item + jj, b = number % kBuffers, turn = number / kBuffers;
                 const uint32_t tS = tmem + lane_base + b * kS + row0;
@@ -297,29 +321,18 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                 // rows that see this thread's position, a bit each
                 unsigned long long seen = ~0ull;
                 if (masked) {
+                    const int straight = attn_straight_of(P, u, S.straight[warp]);
+                    const bool chain = min(u.n, u.node0 + P.unit_nodes) <= straight;        // every node of the unit sees all before it
                     const int node = start - u.first + pos;                 // the node at this position
                     if (pos >= valid) seen = 0;
-                    else if (node >= 0 && !P.parents) {
+                    else if (node >= 0 && chain) {
                         const int shift = (node - u.node0) * P.group;
                         seen = shift <= 0 ? ~0ull : shift >= 64 ? 0 : ~0ull << shift;
                     }
-                    if (P.parents && start + valid > u.first) {
+                    if (!chain && start + valid > u.first) {
                         T.seen[t][pos] = 0;
                         group_sync(t);
-                        const int self = u.node0 + pos;
-                        if (pos < P.tile_nodes && self < u.n) {
-                            const unsigned long long bits = (P.group == 64 ? ~0ull : (1ull << P.group) - 1) << (pos * P.group);
-                            int a = self;
-                            for (;;) {
-                                const int at = u.first + a - start;
-                                if (at < 0) break;
-                                if (at < valid) atomicOr(&T.seen[t][at], bits);
-                                if (a == 0) break;
-                                const int p = P.parents[u.row0 + a];
-                                if (p < 0 || p >= a) { atomicOr(P.dev_status, DSPARK_DEV_BAD_TREE); break; }
-                                a = p;
-                            }
-                        }
+                        if (pos < P.tile_nodes && u.node0 + pos < u.n) few_mark(P, u.row0, u.first - start, u.node0 + pos, pos, straight, valid, T.seen[t]);
                         group_sync(t);
                         if (node >= 0 && pos < valid) seen = T.seen[t][pos];
                     }
