@@ -38,7 +38,8 @@ struct AttnShared {
     uint64_t raw_full[kAttnMaxRaw], raw_empty[kAttnMaxRaw];   // 8-bit tiles
     uint64_t q_full, s_full[2], p_full[2], o_full[2], merge_ready, merge_done, mma_done;
     uint32_t tmem_base;
-    int abort, bad_value[kAttnUnitFlags];
+    int abort;
+    uint32_t bad_value[kAttnUnitFlags];          // tiles of a unit whose V had NaN or infinities among the nodes
     AttnStraight straight[16];                   // of each softmax warp
     AttnList list;
     float2 second[kAttnTile];                    // (reference, sum) of the second group
@@ -455,7 +456,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                     wait(&S.full[s], i / P.v_slots & 1u);
                     if ((row & 1) == half && (row >= u.first - start || row >= valid)) {
                         if (attn_clean_values(ring + (size_t)s * tile_bytes + row * 128, row, P.chunks, row < valid))
-                            S.bad_value[units % kAttnUnitFlags] = 1;
+                            atomicOr(&S.bad_value[units % kAttnUnitFlags], attn_tile_bit(u.j0 + jj));
                     }
                     fence_async_smem();
                 }
@@ -498,7 +499,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                     ref = top;
                 }
                 const bool whole = done.j0 == 0 && done.j1 == done.tiles;
-                const bool bad_value = kKind != kAttnI8 && *(volatile int*)&S.bad_value[units % kAttnUnitFlags] != 0;
+                const uint32_t bad_tiles = kKind != kAttnI8 ? *(volatile uint32_t*)&S.bad_value[units % kAttnUnitFlags] : 0u;
                 const long long part = (long long)(2 * blockIdx.x + (done.j0 > 0 ? 0 : 1)) * P.part_rows + tile * kAttnTile + row;
                 const int head = done.head * P.group + row % P.group;
                 const long long out_row = done.row0 + node;
@@ -521,9 +522,12 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
 #pragma unroll
                             for (int i = 0; i < 16; ++i) o[i] = o[i] * f0 + o1[i] * f1;
                         }
-                        if (bad_value && live)   // values that were left out of the product, where this row sees them
+                        if (bad_tiles && live) { // values that were left out of the product, where this row sees them
+                            float bad[16];
+                            attn_bad_values<kNarrow, 16>(P, done, node, attn_straight_of(P, done, S.straight[warp]), bad_tiles, c, bad);
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) o[i] += attn_bad_values<kNarrow>(P, done, node, c + i);
+                            for (int i = 0; i < 16; ++i) o[i] += bad[i];
+                        }
                         __syncwarp();
 #pragma unroll
                         for (int i = 0; i < 4; ++i)

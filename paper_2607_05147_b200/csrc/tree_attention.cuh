@@ -70,6 +70,9 @@ __device__ __forceinline__ void attn_tile_at(const AttnParams& P, int j, int& st
     len = min(kAttnTile, P.c.page_size - at);
 }
 
+// the bit of a cache tile in a set of them that is not exact: there are 32
+__device__ __forceinline__ uint32_t attn_tile_bit(int j) { return 1u << (j & 31); }
+
 // page of a request that a position is in
 __device__ __forceinline__ int attn_page_of(const AttnParams& P, int position)
 {
@@ -582,7 +585,7 @@ __device__ __forceinline__ void widen_line(const unsigned char* line, int token,
 template <int kKind, int kThreads, bool kTensorK, typename Tile, typename Ready>
 __device__ __forceinline__ bool attn_widen(const AttnParams& P, AttnIter it, int ct, int kv_first, int kv_last, const unsigned char* raw,
                                            unsigned char* ring, int tile_bytes, uint64_t* raw_full, uint64_t* raw_empty, uint64_t* full,
-                                           uint64_t* empty, uint32_t k_columns, volatile int* bad_value, volatile int* abort_flag, Tile tile,
+                                           uint64_t* empty, uint32_t k_columns, uint32_t* bad_value, volatile int* abort_flag, Tile tile,
                                            Ready ready)
 {
     const int lane = threadIdx.x & 31, d = P.c.head_dim;
@@ -617,7 +620,7 @@ __device__ __forceinline__ bool attn_widen(const AttnParams& P, AttnIter it, int
                     const bool look = kKind == kAttnE4M3 && kv && tree < kAttnTile;
                     if (d == 128 && valid == kAttnTile && !look) widen_tile<kKind, kThreads, 128>(src, dst, from0, to0);
                     else if (d == 64 && valid == kAttnTile && !look) widen_tile<kKind, kThreads, 64>(src, dst, from0, to0);
-                    else if (widen_position<kKind>(src, dst, ct, d, ct < valid, look && ct >= tree)) bad_value[unit % kAttnUnitFlags] = 1;
+                    else if (widen_position<kKind>(src, dst, ct, d, ct < valid, look && ct >= tree)) atomicOr(&bad_value[unit % kAttnUnitFlags], attn_tile_bit(j));
                 }
                 fence_async_smem();
                 __syncwarp();
@@ -650,30 +653,49 @@ __device__ __forceinline__ bool attn_clean_values(unsigned char* line, int row, 
     }
     return any;
 }
-// What was left out of the product for a node's row: the sum of component i of V over the nodes that it sees in this CTA's part of
-// the unit where that is NaN or an infinity.  Seldom called.
-template <bool kNarrow>
-__device__ __noinline__ float attn_bad_values(const AttnParams& P, const AttnUnit& u, int node, int i)
+// What was left out of the product for a node's row: the sums of kCount components of V from i on over the nodes that it sees in this
+// CTA's part of the unit, where those are NaN or infinities.  tiles: those that hold some.  Seldom called.
+template <bool kNarrow, int kCount>
+__device__ __noinline__ void attn_bad_values(const AttnParams& P, const AttnUnit& u, int node, int straight, uint32_t tiles, int i, float* sum)
 {
-    float sum = 0.f;
-    for (int a = node;;) {
-        const int position = u.first + a, page_of = position / P.c.page_size, token = position - page_of * P.c.page_size;
-        const int j = P.c.page_size <= kAttnTile ? position / kAttnTile : page_of * P.page_tiles + token / kAttnTile;
+    for (int c = 0; c < kCount; ++c) sum[c] = 0.f;
+    auto tile_of = [&](int position) {
+        if (P.c.page_size <= kAttnTile) return position / kAttnTile;
+        const int page_of = position / P.c.page_size;
+        return page_of * P.page_tiles + (position - page_of * P.c.page_size) / kAttnTile;
+    };
+    auto add = [&](int position) {
+        const int page_of = attn_page_of(P, position), token = position - page_of * P.c.page_size;
         const int page = P.c.block_table[u.r * P.c.table_stride + page_of];
-        if (j >= u.j0 && j < u.j1 && page >= 0 && page < P.c.n_pages) {
-            const unsigned char* v = P.c.v + page * P.c.page_stride + token * P.c.token_stride + u.head * P.c.head_stride;
-            if (kNarrow) { if ((v[i] & 0x7fu) == 0x7fu) sum = NAN; }
+        if (page < 0 || page >= P.c.n_pages) return;
+        const unsigned char* v = P.c.v + page * P.c.page_stride + token * P.c.token_stride + u.head * P.c.head_stride;
+#pragma unroll
+        for (int c = 0; c < kCount; ++c) {
+            if (kNarrow) { if ((v[i + c] & 0x7fu) == 0x7fu) sum[c] = NAN; }
             else {
-                const uint32_t x = reinterpret_cast<const uint16_t*>(v)[i];
-                if ((x & 0x7f80u) == 0x7f80u) sum += __uint_as_float(x << 16);
+                const uint32_t x = reinterpret_cast<const uint16_t*>(v)[i + c];
+                if ((x & 0x7f80u) == 0x7f80u) sum[c] += __uint_as_float(x << 16);
             }
         }
-        if (a == 0) break;
-        const int p = P.parents ? P.parents[u.row0 + a] : a - 1;
-        if (p < 0 || p >= a) break;
-        a = p;
+    };
+    int a = node, steps = 0;
+    while (a >= straight) {
+        const int j = tile_of(u.first + a);
+        if (j < u.j0) return;
+        if (j < u.j1 && (tiles & attn_tile_bit(j))) add(u.first + a);
+        if (a == 0) return;
+        a = attn_parent(P, u.row0, a, steps);
     }
-    return sum;
+    if (a < 0) return;
+    const int j_first = max(u.j0, tile_of(u.first)), j_last = min(u.j1 - 1, tile_of(u.first + a));
+    for (int j = j_first; j <= j_last; ++j) {
+        if (!(tiles & attn_tile_bit(j))) continue;
+        int start, len;
+        attn_tile_at(P, j, start, len);
+        const int from = max(start, u.first) - start, to = min(len, u.first - start + a + 1);
+#pragma unroll 4
+        for (int k = from; k < to; ++k) add(start + k);
+    }
 }
 
 // the dynamic shared memory of a kernel, once per device

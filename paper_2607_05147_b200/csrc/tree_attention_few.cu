@@ -44,7 +44,8 @@ struct FewShared {
     uint64_t full[kAttnMaxSlots], empty[kAttnMaxSlots], raw_full[kAttnMaxRaw], raw_empty[kAttnMaxRaw];
     uint64_t q_full, q_empty, s_full[4], p_full[4], o_done[4], mma_done[2];
     uint32_t tmem_base;
-    int abort, bad_value[kAttnUnitFlags];
+    int abort;
+    uint32_t bad_value[kAttnUnitFlags];          // tiles of a unit whose V had NaN or infinities among the nodes
     AttnStraight straight[8];                    // of each softmax warp
     AttnList list;
 };
@@ -451,7 +452,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                     wait(&S.full[s], number / P.v_slots & 1u);
                     if ((kTurns || (pos & 1) == t) && (pos >= u.first - start || pos >= valid))
                         if (attn_clean_values(ring + (size_t)s * tile_bytes + pos * 128, pos, P.chunks, pos < valid))
-                            S.bad_value[units % kAttnUnitFlags] = 1;
+                            atomicOr(&S.bad_value[units % kAttnUnitFlags], attn_tile_bit(u.j0 + jj));
                 }
                 fence_async_smem();
                 tc_fence_before();
@@ -555,18 +556,22 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                     }
                     __syncwarp();
                 }
-                if (kKind != kAttnI8 && pos < d && *(volatile int*)&S.bad_value[units % kAttnUnitFlags] != 0)
-                    for (int c = 0; c < mine; ++c) {     // values that were left out, where the row sees them
+                const uint32_t bad_tiles = kKind != kAttnI8 ? *(volatile uint32_t*)&S.bad_value[units % kAttnUnitFlags] : 0u;
+                if (bad_tiles && pos < d) {
+                    float bad = 0.f;
+                    for (int c = 0, at = -1; c < mine; ++c) {     // values that were left out, where the row sees them
                         const int r = e0 + c, node = done.node0 + r / P.group;
-                        const float bad = attn_bad_values<kNarrow>(P, done, node, pos);
+                        if (node != at) attn_bad_values<kNarrow, 1>(P, done, node, attn_straight_of(P, done, S.straight[warp]), bad_tiles, pos, &bad);
+                        at = node;
                         if (bad == 0.f) continue;
                         if (!whole) P.parts[(part + c) * d + pos] += bad;
                         else {
-                            uint16_t* at = reinterpret_cast<uint16_t*>(P.out + (long long)(done.row0 + node) * P.out_row +
+                            uint16_t* to = reinterpret_cast<uint16_t*>(P.out + (long long)(done.row0 + node) * P.out_row +
                                                                        (long long)(done.head * P.group + r % P.group) * P.out_head) + pos;
-                            *at = (uint16_t)pack16<false>(__uint_as_float((uint32_t)*at << 16) + bad, 0.f);
+                            *to = (uint16_t)pack16<false>(__uint_as_float((uint32_t)*to << 16) + bad, 0.f);
                         }
                     }
+                }
                 tc_fence_before();
             }
             ++units;
