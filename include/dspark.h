@@ -656,7 +656,7 @@ int dspark_kv_commit(const dspark_kv_cache_t* cache, const int32_t* first, const
  *               node i sees the nodes up to i.  A parent that is not an earlier node sets DSPARK_DEV_BAD_TREE and ends the
  *               ancestors there; so does the 4097th ancestor of a node, not counting those in the chain that its request
  *               begins with (a prompt given with parents is one chain, however long)
- *   scale       finite
+ *   scale       at most 2^127 in size
  *   out_lse     device fp32 [n_rows][q_heads] or NULL: log of the sum of e^(scale * q . k) over the positions seen
  *   workspace   dspark_tree_attention_workspace_bytes(...), 256-byte aligned, any content; one call at a time
  * The products are bf16 (an 8-bit cache: 16-bit operands that hold its values exactly) with fp32 accumulation; softmax

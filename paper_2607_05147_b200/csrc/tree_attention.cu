@@ -192,7 +192,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
         auto vote = [&](bool x) { return barrier_any<64>(pair_id + 1, x); };
         // Row tile `tile` of a unit into shared memory by the eight warps of a group, 16 rows a warp, 16 lanes a row: a row a thread
         // would ask for 32 lines with every load.  In 8-bit mode as fp16, scaled by a power of two so that no value passes the range
-        // and what is lost is below 2^-37 of the row's largest.
+        // and what is lost is below 2^-37 of the row's largest (2^-150 at least).
         auto load_q = [&](const AttnUnit& w, int tile) {
             const int sub = lane & 15;
             const bool in = sub < d / 8;
@@ -218,8 +218,9 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                         for (int k = 0; k < 4; ++k) top = max3(top, fabsf(bf16lo(w4[k])), fabsf(bf16hi(w4[k])));
 #pragma unroll
                         for (int o = 8; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                        // 2^e with the largest value below 2^14: exponent field of top to that of 2^13; at most 2^60
-                        const int e = min(127 + 60, max(1, 254 + 13 - (int)(__float_as_uint(top) >> 23)));
+                        // 2^e with the largest value below 2^14: exponent field of top to that of 2^13; at most 2^126, whose
+                        // inverse is no subnormal
+                        const int e = min(127 + 126, max(1, 254 + 13 - (int)(__float_as_uint(top) >> 23)));
                         const float up = __uint_as_float((uint32_t)e << 23);
                         if (sub == 0) scales.q[tile][r] = __uint_as_float((uint32_t)(254 - e) << 23);       // the inverse power
                         x[i].x = pack16<true>(bf16lo(x[i].x) * up, bf16hi(x[i].x) * up);
@@ -793,7 +794,7 @@ int dspark_tree_attention(const dspark_kv_cache_t* cache, int layer, const void*
                           void* workspace, size_t workspace_bytes, void* stream)
 {
     using namespace dspark;
-    if (!q || !out || q_heads < 1 || !isfinite(scale)) return DSPARK_ERR_INVALID_ARG;
+    if (!q || !out || q_heads < 1 || !(fabsf(scale) <= 0x1p127f)) return DSPARK_ERR_INVALID_ARG;
     if (int e = kv_cache_check(cache, layer)) return e;
     if (int e = kv_step_check(first, row_offsets, R, n_rows, dev_status)) return e;
     const int d = cache->head_dim;

@@ -227,7 +227,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
             }
         };
         // With an 8-bit cache as fp16, scaled by a power of two so that no value passes the range and what is lost is below 2^-37
-        // of the row's largest.
+        // of the row's largest (2^-150 at least).
         auto store_q = [&](uint32_t unit) {
             if constexpr (kNarrow) {
                 float top = 0.f;
@@ -239,8 +239,9 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                 }
 #pragma unroll
                 for (int o = kPer / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                // 2^e with the largest value below 2^14: exponent field of top to that of 2^13; at most 2^60
-                const int e = min(127 + 60, max(1, 254 + 13 - (int)(__float_as_uint(top) >> 23)));
+                // 2^e with the largest value below 2^14: exponent field of top to that of 2^13; at most 2^126, whose inverse is no
+                // subnormal
+                const int e = min(127 + 126, max(1, 254 + 13 - (int)(__float_as_uint(top) >> 23)));
                 const float up = __uint_as_float((uint32_t)e << 23);
                 if (q_sub == 0) T.q[unit & 1u][q_row] = __uint_as_float((uint32_t)(254 - e) << 23);
 #pragma unroll
@@ -356,21 +357,23 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                 if (row0 < rows) {
                     __syncwarp();
                     if (masked) {
-                        // scores of rows that do not see the position: -infinity, in place; over an 8-bit cache the others times
-                        // K's scale (-infinity times one that is not positive would not stay that).  Where a scale is no number the
-                        // position is NaN for the rows that see it, and the scales are not used.
+                        // scores of rows that do not see the position: -infinity, in place.  Over an 8-bit cache it has to stay that when
+                        // it is multiplied: the others are multiplied here by K's scale up to one and its sign, below by the rest and
+                        // the row's factor, whose product is at least 2^-126.  Where a scale is no number the position is NaN for the
+                        // rows that see it, and the scales are not used.
                         const bool bad = kNarrow && !(fabsf(scale.x) < INFINITY && fabsf(scale.y) < INFINITY);
+                        const float by = fminf(fmaxf(k_scale, -1.f), 1.f);
+                        if (kNarrow) k_scale = fmaxf(fabsf(k_scale), 1.f);
 #pragma unroll 1
                         for (int c0 = 0; c0 < kC; c0 += 8) {
                             float s[8];
                             attn_read<8>(tS + c0, s);
 #pragma unroll
-                            for (int c = 0; c < 8; ++c) s[c] = !(seen >> (c0 + c) & 1) ? -INFINITY : bad ? NAN : kNarrow ? s[c] * k_scale : s[c];
+                            for (int c = 0; c < 8; ++c) s[c] = !(seen >> (c0 + c) & 1) ? -INFINITY : bad ? NAN : kNarrow ? s[c] * by : s[c];
                             attn_write<8>(tS + c0, reinterpret_cast<const uint32_t (&)[8]>(s));
                         }
                         tmem_store_wait();
-                        if (kNarrow) k_scale = 1.f;
-                        if (bad) { v_scale = 0.f; above = -kAttnNarrowOffset; }
+                        if (bad) { k_scale = 1.f; v_scale = 0.f; above = -kAttnNarrowOffset; }
                     }
                     // y = score * factor - reference
                     const uint64_t k2 = pack2(k_scale, k_scale);

@@ -144,3 +144,16 @@ def test_values_around_1e_minus_26(kind, shape):
         x = torch.randn(2, n, 2, 64, generator=g, device="cuda")
         cache.put(r, range(n), x[0], (x[1] + 0.5) * 1e-26)
     check(cache, q, first, nodes, T.random_parents(nodes, 3), 0.2, lost=2 * 2.0 ** -112)
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("shape", range(len(STEPS)))
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("size", [2.0 ** 100, 2.0 ** -70])
+def test_scales_of_k_far_from_one(kind, shape, sign, size):
+    # scores of an ordinary size: queries as far from one on the other side
+    first, nodes, group = STEPS[shape]
+    cache, q = step(first, nodes, 16, 2, group, 64, kind, seed=shape)
+    cache.ks.mul_(sign * size)
+    q = (q.float() / size).bfloat16()
+    check(cache, q, first, nodes, T.random_parents(nodes, 3), 0.2)
