@@ -60,6 +60,12 @@ constexpr int kAttnConverters = 4;
 template <int kKind> constexpr int kAttnCols = kKind == kAttnWide ? 32 : 16;    // scores in registers at a time
 template <int kKind> constexpr int kAttnThreads = (kRowWarps + 2 + (kKind == kAttnWide ? 0 : kAttnConverters)) * 32;
 
+template <bool kNarrow>
+__device__ __noinline__ void attn_bad_row(const AttnParams& P, AttnPart u, int node, int straight, uint32_t tiles, int i, float* sum)
+{
+    attn_bad_values<kNarrow, 16>(P, u, node, straight, tiles, i, sum);
+}
+
 template <int kKind>
 __global__ void __launch_bounds__(kAttnThreads<kKind>, 1)
 attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v)
@@ -525,7 +531,7 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                         }
                         if (bad_tiles && live) { // values that were left out of the product, where this row sees them
                             float bad[16];
-                            attn_bad_values<kNarrow, 16>(P, done, node, attn_straight_of(P, done, S.straight[warp]), bad_tiles, c, bad);
+                            attn_bad_row<kNarrow>(P, AttnPart(done), node, attn_straight_of(P, done, S.straight[warp]), bad_tiles, c, bad);
 #pragma unroll
                             for (int i = 0; i < 16; ++i) o[i] += bad[i];
                         }

@@ -654,9 +654,15 @@ __device__ __forceinline__ bool attn_clean_values(unsigned char* line, int row, 
     return any;
 }
 // What was left out of the product for a node's row: the sums of kCount components of V from i on over the nodes that it sees in this
-// CTA's part of the unit, where those are NaN or infinities.  tiles: those that hold some.  Seldom called.
+// CTA's part of the unit, where those are NaN or infinities.  tiles: those that hold some.  Seldom done; inline with few rows and a call
+// with many, which is what each kernel's other code is fastest with (64 trees of 16: 211 us, with a call 215; 105 trees of 55 nodes over
+// e4m3: 278 us with a call, else 311).
+struct AttnPart {
+    int r, head, row0, first, j0, j1;
+    explicit __device__ __forceinline__ AttnPart(const AttnUnit& u) : r(u.r), head(u.head), row0(u.row0), first(u.first), j0(u.j0), j1(u.j1) {}
+};
 template <bool kNarrow, int kCount>
-__device__ __noinline__ void attn_bad_values(const AttnParams& P, const AttnUnit& u, int node, int straight, uint32_t tiles, int i, float* sum)
+__device__ __forceinline__ void attn_bad_values(const AttnParams& P, AttnPart u, int node, int straight, uint32_t tiles, int i, float* sum)
 {
     for (int c = 0; c < kCount; ++c) sum[c] = 0.f;
     auto tile_of = [&](int position) {

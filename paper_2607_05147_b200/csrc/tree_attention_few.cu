@@ -47,6 +47,7 @@ struct FewShared {
     int abort;
     uint32_t bad_value[kAttnUnitFlags];          // tiles of a unit whose V had NaN or infinities among the nodes
     AttnStraight straight[8];                    // of each softmax warp
+    AttnUnit unit[2];                            // the one that each group is at, for few_bad
     AttnList list;
 };
 template <int kN>
@@ -83,6 +84,28 @@ static __device__ __noinline__ void few_mark(const AttnParams& P, int row0, int 
         if (a == 0) return;
         a = attn_parent(P, row0, a, steps);
         if (a < 0) return;
+    }
+}
+
+// Values that were left out of the products, to component `pos` of the rows from e0 on that see them: in the output or, where the unit is
+// divided, in the partial result.
+template <bool kNarrow, int kE>
+__device__ __forceinline__ void few_bad(const AttnParams& P, const AttnUnit& u, const AttnStraight& of, uint32_t tiles, int pos, int e0)
+{
+    const int straight = attn_straight_of(P, u, of), rows = min(kE, min(P.tile_nodes, u.n - u.node0) * P.group - e0);
+    const long long part = (long long)(2 * blockIdx.x + (u.j0 > 0 ? 0 : 1)) * P.part_rows + e0;
+    float bad = 0.f;
+    for (int c = 0, at = -1; c < rows; ++c) {
+        const int r = e0 + c, node = u.node0 + r / P.group;
+        if (node != at) attn_bad_values<kNarrow, 1>(P, AttnPart(u), node, straight, tiles, pos, &bad);
+        at = node;
+        if (bad == 0.f) continue;
+        if (u.j0 > 0 || u.j1 < u.tiles) P.parts[(part + c) * P.c.head_dim + pos] += bad;
+        else {
+            uint16_t* to = reinterpret_cast<uint16_t*>(P.out + (long long)(u.row0 + node) * P.out_row +
+                                                       (long long)(u.head * P.group + r % P.group) * P.out_head) + pos;
+            *to = (uint16_t)pack16<false>(__uint_as_float((uint32_t)*to << 16) + bad, 0.f);
+        }
     }
 }
 
@@ -311,6 +334,7 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
             bool left = false;
             const int first = first_tile(item);
             attn_look_at_tree(P, u, S.straight[warp]);
+            if (kKind != kAttnI8 && pos == 0) S.unit[t] = u;
             for (int jj = first; jj < count; jj += kStep) {
                 const uint32_t number = item + jj, b = number % kBuffers, turn = number / kBuffers;
                 const uint32_t tS = tmem + lane_base + b * kS + row0;
@@ -559,22 +583,8 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                     }
                     __syncwarp();
                 }
-                const uint32_t bad_tiles = kKind != kAttnI8 ? *(volatile uint32_t*)&S.bad_value[units % kAttnUnitFlags] : 0u;
-                if (bad_tiles && pos < d) {
-                    float bad = 0.f;
-                    for (int c = 0, at = -1; c < mine; ++c) {     // values that were left out, where the row sees them
-                        const int r = e0 + c, node = done.node0 + r / P.group;
-                        if (node != at) attn_bad_values<kNarrow, 1>(P, done, node, attn_straight_of(P, done, S.straight[warp]), bad_tiles, pos, &bad);
-                        at = node;
-                        if (bad == 0.f) continue;
-                        if (!whole) P.parts[(part + c) * d + pos] += bad;
-                        else {
-                            uint16_t* to = reinterpret_cast<uint16_t*>(P.out + (long long)(done.row0 + node) * P.out_row +
-                                                                       (long long)(done.head * P.group + r % P.group) * P.out_head) + pos;
-                            *to = (uint16_t)pack16<false>(__uint_as_float((uint32_t)*to << 16) + bad, 0.f);
-                        }
-                    }
-                }
+                if (kKind != kAttnI8 && *(volatile uint32_t*)&S.bad_value[units % kAttnUnitFlags] != 0u && pos < d)
+                    few_bad<kNarrow, kE>(P, S.unit[t], S.straight[warp], S.bad_value[units % kAttnUnitFlags], pos, e0);
                 tc_fence_before();
             }
             ++units;
