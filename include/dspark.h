@@ -659,7 +659,8 @@ int dspark_kv_commit(const dspark_kv_cache_t* cache, const int32_t* first, const
  *   scale       at most 2^127 in size
  *   out_lse     device fp32 [n_rows][q_heads] or NULL: log of the sum of e^(scale * q . k) over the positions seen
  *   workspace   dspark_tree_attention_workspace_bytes(...), 256-byte aligned, any content; one call at a time
- * The products are bf16 (an 8-bit cache: 16-bit operands that hold its values exactly) with fp32 accumulation; softmax
+ * The products are bf16 (an 8-bit cache: 16-bit operands that hold its values exactly) with fp32 accumulation, which the tensor
+ * cores cut instead of rounding: at most 2^-11 of the sum of the magnitudes, however long the context; softmax
  * statistics are fp32; the weights are rounded to 16 bits for their product with v (an 8-bit cache: times v's scale and relative
  * to the row's largest such product; what is 2^-32 of that is lost, and what is below 2^-112 of the largest weight: where all of
  * v's scales that a row sees are below 2^-80 digits go, and where they are below 2^-112 the row is zero; above 2^100 the small

@@ -44,6 +44,7 @@ struct AttnShared {
     AttnList list;
     float2 second[kAttnTile];                    // (reference, sum) of the second group
     float of_half[2][2][kAttnTile];              // what the two threads of a row tell one another: largest scores, sums
+    float kept[2][2][kAttnTile];                 // reference of what a row's threads have put by (attn_keep)
 };
 template <int kKind>
 struct AttnScales {                              // q: per row
@@ -59,6 +60,30 @@ constexpr int kRowWarps = 16;                    // of the softmax: two groups o
 constexpr int kAttnConverters = 4;
 template <int kKind> constexpr int kAttnCols = kKind == kAttnWide ? 32 : 16;    // scores in registers at a time
 template <int kKind> constexpr int kAttnThreads = (kRowWarps + 2 + (kKind == kAttnWide ? 0 : kAttnConverters)) * 32;
+
+// A row's components [begin, end) of O, at tensor memory `o`: put by in memory and O zero again, or (back) what was put by added to O.
+// by: 2 to the reference that it was put by with less the present one; 0: nothing was.  kept: NULL for a row that is none.
+static __device__ __noinline__ void attn_keep(uint32_t o, int begin, int end, float* kept, float by, bool back)
+{
+    for (int c = begin; c < end; c += 16) {
+        float x[16];
+        tmem_load16(o + c, x);
+        if (kept)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                float4* at = reinterpret_cast<float4*>(kept + c + i);
+                const float4 k = by != 0.f ? *at : make_float4(0.f, 0.f, 0.f, 0.f);
+                x[i] = fmaf(k.x, by, x[i]); x[i + 1] = fmaf(k.y, by, x[i + 1]);
+                x[i + 2] = fmaf(k.z, by, x[i + 2]); x[i + 3] = fmaf(k.w, by, x[i + 3]);
+                if (!back) *at = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+            }
+        uint32_t w[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w[i] = back ? __float_as_uint(x[i]) : 0u;
+        tmem_store16(o + c, w);
+    }
+    tmem_store_wait();
+}
 
 template <bool kNarrow>
 __device__ __noinline__ void attn_bad_row(const AttnParams& P, AttnPart u, int node, int straight, uint32_t tiles, int i, float* sum)
@@ -240,6 +265,9 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
             }
             fence_async_smem();
         };
+        // Where this row's part of O is put by: the place of the unit's partial result (of a whole unit: that of the CTA's last unit,
+        // which comes later), the second group's behind the first one's.
+        auto keep_row = [&](const AttnUnit& w) { return P.parts + ((long long)(2 * blockIdx.x + (w.j0 > 0 ? 0 : 1)) * P.part_rows + t * kAttnTile + row) * d; };
         bool have = it.next(P, u);
         // Q of the first unit; afterwards each unit's is loaded at the end of the one before
         auto prepare_q = [&](const AttnUnit& w) {
@@ -260,7 +288,9 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
             bool any = false, left = false;      // any: O holds something
             const int step = u.pair ? 1 : 2;
             const int count = u.j1 - u.j0;
-            for (int jj = u.pair ? 0 : t; jj < count; jj += step) {
+            for (int jj = u.pair ? 0 : t; jj < count && !left;) {
+            const int stretch = jj, end = min(count, jj + kAttnKeep * step);
+            for (; jj < end; jj += step) {
                 int start, len;
                 attn_tile_at(P, u.j0 + jj, start, len);
                 const int valid = min(len, u.length - start);               // positions of this tile that exist
@@ -474,12 +504,25 @@ attn_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtens
                 tc_fence_before();
                 arrive(&S.p_full[t]);
             }
+            if (!left && jj < count && warp_live) {
+                wait(&S.s_full[t], items & 1u);  // O is at rest: these scores were issued behind its last products
+                __syncwarp();
+                tc_fence_after();
+                attn_keep(tO, o_begin, o_end, live ? keep_row(u) : nullptr, stretch < step ? 0.f : ex2_approx(S.kept[t][half][row] - ref), false);
+                S.kept[t][half][row] = ref;
+                __syncwarp();
+            }
+            }
             if (left) { ok = false; break; }                                // both warps
             const AttnUnit done = u;
             have = it.next(P, u);
             wait(&S.o_full[t], units & 1u);
             __syncwarp();
             tc_fence_after();
+            if (warp_live && (done.pair ? count : (count - t + 1) >> 1) > kAttnKeep) {
+                attn_keep(tO, o_begin, o_end, live ? keep_row(done) : nullptr, ex2_approx(S.kept[t][half][row] - ref), true);
+                __syncwarp();
+            }
             const bool join = !done.pair && count > 1;
             if (merged) { wait(&S.merge_done, (merges - 1) & 1u); merged = false; }
             S.of_half[t][half][row] = sum;
@@ -738,7 +781,7 @@ static AttnWs attn_ws(long long n_rows, int group, int d)
 {
     AttnWs w;
     const long long rows = n_rows * group;
-    w.rows = rows < 2 * kAttnTile ? (rows <= kAttnTile ? (int)rows : 2 * kAttnTile) : 2 * kAttnTile;
+    w.rows = rows <= 64 ? (int)rows : 2 * kAttnTile;         // more: the kernel for many rows has two accumulators to put by
     w.stats = ((size_t)kAttnSms * sizeof(int4) + 255) / 256 * 256;
     w.parts = w.stats + ((size_t)2 * kAttnSms * w.rows * sizeof(float2) + 255) / 256 * 256;
     w.total = w.parts + (size_t)2 * kAttnSms * w.rows * d * sizeof(float);

@@ -25,6 +25,10 @@ constexpr float kAttnUnset = -1e38f;              // a reference that every scor
 constexpr float kAttnLeastFactor = 1.4e-45f;     // the smallest number: -infinity times it is -infinity, a score times it next to nothing
 constexpr int kAttnMaxWalk = 4096;               // ancestors of a node outside the chain that its request begins with
 constexpr int kAttnNoTree = 0x7fffffff;
+// Tiles of a unit that a group adds up in one accumulator.  The tensor cores cut what an fp32 sum cannot hold: positive values came out
+// 0.6 % too small after 2^20 positions and 10 % after 2^24.  From time to time the accumulator is therefore added to another, rounded, and
+// starts again from zero: 256 tiles of eight products each are off by less than 2^-12.
+constexpr int kAttnKeep = 256;
 constexpr int kAttnUnitFlags = 8;               // units of one CTA that are under way at a time: at most four
 
 enum AttnKind { kAttnWide = 0, kAttnI8 = 1, kAttnE4M3 = 2 };
@@ -579,6 +583,19 @@ __device__ __forceinline__ void widen_line(const unsigned char* line, int token,
     tmem_store_wait();
     tc_fence_before();
 }
+// The widths and places that are not those of most calls, out of line: what the SM's roles run at a time then fits its instruction caches
+// (128 tokens over int8 445 us, inline 529; 96 components 522 and 596, over e4m3 527 and 586; over e4m3 widen_position is inline: 527 us,
+// out of line 650).
+template <int kKind>
+__device__ __noinline__ void widen_line_any(const unsigned char* line, int token, int d, uint32_t addr) { widen_line<kKind, 0>(line, token, d, addr); }
+template <int kKind>
+__device__ __noinline__ void widen_line_64(const unsigned char* line, int token, int d, uint32_t addr) { widen_line<kKind, 64>(line, token, d, addr); }
+template <int kKind, int kThreads>
+__device__ __noinline__ void widen_tile_64(const unsigned char* src, unsigned char* dst, int from0, int to0) { widen_tile<kKind, kThreads, 64>(src, dst, from0, to0); }
+static __device__ __noinline__ void widen_position_i8(const unsigned char* src, unsigned char* dst, int token, int d, bool exists)
+{
+    widen_position<kAttnI8>(src, dst, token, d, exists, false);
+}
 // kThreads threads: 8-bit tiles as fp16 tiles, as the products read them; K and V (kv 0 and 1), or one of them.  kTensorK: K goes to
 // tensor memory at `k_columns`, 64 columns a tile.  tile(unit, j) is called before the waits for a tile's K, ready(number) between
 // them and the work.  False: a wait ran out.
@@ -612,14 +629,15 @@ __device__ __forceinline__ bool attn_widen(const AttnParams& P, AttnIter it, int
                     const int token = (threadIdx.x >> 5 & 3) * 32 + lane;   // the lanes of tensor memory that this warp may write
                     const uint32_t to = k_columns + ((uint32_t)(token & ~31) << 16) + at[0].s * 64;
                     if (d == 128) widen_line<kKind, 128>(src + token * d, token, d, to);
-                    else if (d == 64) widen_line<kKind, 64>(src + token * d, token, d, to);
-                    else widen_line<kKind, 0>(src + token * d, token, d, to);
+                    else if (d == 64) widen_line_64<kKind>(src + token * d, token, d, to);
+                    else widen_line_any<kKind>(src + token * d, token, d, to);
                 } else {
                     // positions that do not exist: zeros; a NaN among the nodes' values of V: zero here and back in the rows that see
                     // it (attn_bad_values)
                     const bool look = kKind == kAttnE4M3 && kv && tree < kAttnTile;
                     if (d == 128 && valid == kAttnTile && !look) widen_tile<kKind, kThreads, 128>(src, dst, from0, to0);
-                    else if (d == 64 && valid == kAttnTile && !look) widen_tile<kKind, kThreads, 64>(src, dst, from0, to0);
+                    else if (d == 64 && valid == kAttnTile && !look) widen_tile_64<kKind, kThreads>(src, dst, from0, to0);
+                    else if constexpr (kKind == kAttnI8) widen_position_i8(src, dst, ct, d, ct < valid);
                     else if (widen_position<kKind>(src, dst, ct, d, ct < valid, look && ct >= tree)) atomicOr(&bad_value[unit % kAttnUnitFlags], attn_tile_bit(j));
                 }
                 fence_async_smem();

@@ -30,7 +30,7 @@
 namespace dspark {
 
 constexpr int kSoftmaxWarps = 8;
-constexpr int kFewSmem = 217 * 1024;             // two of P, Q, the ring; tables beside it
+constexpr int kFewSmem = 216 * 1024;             // two of P, Q, the ring; tables beside it
 template <int kKind, int kN> constexpr bool kFewTurns = kKind != kAttnWide && kN == 16;      // the groups take the tiles in turn
 template <int kKind, int kN> constexpr int kFewBuffers = kFewTurns<kKind, kN> ? 4 : 2;
 // P^T: a line of 128 bytes a position, of 64 / kN tiles beside one another
@@ -56,6 +56,7 @@ struct FewTables {
     float scale[2][kN];                          // what O^T and the sums are multiplied by when they change, and at the end
     float q[2][kN];                              // 8-bit caches: what a row of Q was divided by, of this unit and the next
     float top[kSoftmaxWarps][kN], sum[kSoftmaxWarps][kN];     // a warp's maxima; its sums at the end
+    float kept[2][kN];                           // less the references of what has been put by (few_keep)
     unsigned long long seen[2][kAttnTile];       // rows that see a position (tiles with nodes), for each group
 };
 
@@ -87,6 +88,29 @@ static __device__ __noinline__ void few_mark(const AttnParams& P, int row0, int 
     }
 }
 
+// This thread's component of a group's O^T, `columns` of tensor memory at `o`: put by in as many columns at `kept`, and O^T zero again,
+// or (back) what was put by added to O^T.  less, kept_less: less the references, now and when it was put by; first: nothing was.
+static __device__ __forceinline__ void few_keep(uint32_t o, uint32_t kept, int columns, const float* less, const float* kept_less, bool first, bool back)
+{
+#pragma unroll 1
+    for (int c0 = 0; c0 < columns; c0 += 8) {
+        float x[8], k[8];
+        attn_read<8>(o + c0, x);
+        if (!first) {
+            attn_read<8>(kept + c0, k);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) x[c] = fmaf(k[c], ex2_approx(less[c0 + c] - kept_less[c0 + c]), x[c]);
+        }
+        attn_write<8>(back ? o + c0 : kept + c0, reinterpret_cast<const uint32_t (&)[8]>(x));
+        if (!back) {
+            const uint32_t zero[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+            attn_write<8>(o + c0, zero);
+        }
+    }
+    tmem_store_wait();
+    tc_fence_before();
+}
+
 // Values that were left out of the products, to component `pos` of the rows from e0 on that see them: in the output or, where the unit is
 // divided, in the partial result.
 template <bool kNarrow, int kE>
@@ -109,7 +133,7 @@ __device__ __forceinline__ void few_bad(const AttnParams& P, const AttnUnit& u, 
     }
 }
 
-template <int kKind, int kN>
+template <int kKind, int kN, bool kLong>         // kLong: units of more than 2 kAttnKeep tiles
 __global__ void __launch_bounds__(kFewThreads<kKind, kN>, 1)
 attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v)
 {
@@ -119,8 +143,8 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
     constexpr bool kTurns = kFewTurns<kKind, kN>;
     constexpr int kBuffers = kFewBuffers<kKind, kN>, kS = 128 / kBuffers;          // kS: columns from one S^T to the next
     constexpr int kE = kN / 2, kC = kTurns ? kN : kE;                       // rows that a group loads and writes; whose weights it makes
-    // columns of tensor memory: S^T from 0 on, O^T at 128 (and 160), two K tiles of an 8-bit cache at 192 and 256
-    constexpr uint32_t kO = 128, kK = 192, kColumns = kNarrow ? 512 : 256;
+    // columns of tensor memory: S^T from 0 on, O^T at 128 (and 160), two K tiles of an 8-bit cache at 192 and 256, O^T put by behind
+    constexpr uint32_t kO = 128, kK = 192, kKept = kNarrow ? 320 : 192, kColumns = kNarrow ? 512 : 256;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);   // swizzle atoms: 1 KB
     __shared__ FewShared S;
@@ -335,7 +359,10 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
             const int first = first_tile(item);
             attn_look_at_tree(P, u, S.straight[warp]);
             if (kKind != kAttnI8 && pos == 0) S.unit[t] = u;
-            for (int jj = first; jj < count; jj += kStep) {
+            int jj = first;
+            do {
+            const int stretch = jj, end = kLong ? min(count, jj + kAttnKeep * kStep) : count;
+            for (; jj < end; jj += kStep) {
                 const uint32_t number = item + jj, b = number % kBuffers, turn = number / kBuffers;
                 const uint32_t tS = tmem + lane_base + b * kS + row0;
                 unsigned char* p_line = sP + few_p_line<kN>(b) + pos * 128;
@@ -485,6 +512,16 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
                 tc_fence_before();
                 arrive(&S.p_full[b]);
             }
+            if (kLong && !left && jj < count && row0 < rows) {
+                const uint32_t last = item + jj - kStep;
+                wait(&S.o_done[last % kBuffers], last / kBuffers & 1u);
+                __syncwarp();
+                tc_fence_after();
+                few_keep(tMine, tMine - kO + kKept, kC, T.less[t] + row0, T.kept[t] + row0, stretch == first, false);
+                group_sync(t);
+                if (pos < kC) T.kept[t][row0 + pos] = T.less[t][row0 + pos];
+            }
+            } while (kLong && !left && jj < count);
             if (left) { if (kTurns) vote(true); ok = false; break; }        // all of the group; the other one learns of it
             item += count;
             // The next unit's Q and scales, asked for while the products of this one are finished.
@@ -525,7 +562,10 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
             }
             __syncwarp();
             tc_fence_after();
+            if (kLong && row0 < rows && (count - 1 - first) / kStep >= kAttnKeep)
+                few_keep(tMine, tMine - kO + kKept, kC, T.less[t] + row0, T.kept[t] + row0, false, true);
             if (vote(!ok)) { ok = false; break; }
+            tc_fence_after();
             if (e0 < rows) {
                 const bool whole = done.j0 == 0 && done.j1 == done.tiles;
                 const long long part = (long long)(2 * blockIdx.x + (done.j0 > 0 ? 0 : 1)) * P.part_rows + e0;
@@ -607,12 +647,12 @@ attn_few_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CU
     }
 }
 
-template <int kKind, int kN>
+template <int kKind, int kN, bool kLong>
 static int few_launch(AttnParams& P, const CUtensorMap& k, const CUtensorMap& v, int sms, cudaStream_t s)
 {
     static std::atomic<unsigned long long> ready{0};
     constexpr int kSmem = kFewSmem + 1024;
-    if (!attn_allow_smem(attn_few_kernel<kKind, kN>, kSmem, ready)) return launch_status();
+    if (!attn_allow_smem(attn_few_kernel<kKind, kN, kLong>, kSmem, ready)) return launch_status();
     const int tile = P.chunks * kChunkBytes;
     // a chunk is left behind the ring: with up to 64 components the products read one past a tile (and nobody its results)
     int room = kFewSmem - kFewPAll<kKind, kN> - P.chunks * kN * 128 - (P.chunks == 1 ? kChunkBytes : 0);
@@ -625,8 +665,15 @@ static int few_launch(AttnParams& P, const CUtensorMap& k, const CUtensorMap& v,
     P.raw_k = kKind == kAttnWide ? 0 : most / 2;
     P.raw_v = kKind == kAttnWide ? 0 : most - P.raw_k;
     KernelTimerScope timer(DSPARK_K_TREE_ATTENTION, s);
-    launch_pdl(attn_few_kernel<kKind, kN>, dim3((unsigned)sms), dim3(kFewThreads<kKind, kN>), kSmem, s, P, k, v);
+    launch_pdl(attn_few_kernel<kKind, kN, kLong>, dim3((unsigned)sms), dim3(kFewThreads<kKind, kN>), kSmem, s, P, k, v);
     return launch_status();
+}
+template <int kKind, int kN>
+static int few_launch(AttnParams& P, const CUtensorMap& k, const CUtensorMap& v, int sms, cudaStream_t s)
+{
+    // Room for more than 65536 positions: the kernel that puts its sums by (with that code 128 tokens over 8192 positions of int8 take 467 us,
+    // without it 445; trees of 8 nodes, 64 rows 460 and 448).  Without, 512 tiles are cut by less than 2^-11.
+    return kv_capacity(P.c) > 2 * kAttnKeep * kAttnTile ? few_launch<kKind, kN, true>(P, k, v, sms, s) : few_launch<kKind, kN, false>(P, k, v, sms, s);
 }
 template <int kKind>
 static int few_rows(AttnParams& P, int rows, const CUtensorMap& k, const CUtensorMap& v, int sms, cudaStream_t s)
