@@ -742,14 +742,14 @@ int dspark_set_stream_path(int path);
 
 /* Diagnostic: how many polls the streamed passes of the verifiers spend on an entry wait (a consumer warp
  * waiting for its data, the producer waiting for a free stage or for the launch tag) before they give up,
- * set DSPARK_DEV_TIMEOUT in *dev_status and leave.  0 restores the default (about 4 million polls, on the
- * order of a second); a wait gives up after polls - 1 unsuccessful polls, so 1 makes every such wait run
+ * set DSPARK_DEV_TIMEOUT in *dev_status and leave.  0 restores the default (about 4 million polls of
+ * up to 4 us each); a wait gives up after polls - 1 unsuccessful polls, so 1 makes every such wait run
  * out at once.  That is how the tests reach the give-up path without hanging anything: a kernel that gives
  * up still waits, with the long default bound, for the bulk copies it has already issued before it leaves,
  * and its outputs are unspecified.  dspark_rms_norm_quant's waits for rows copied ahead (many rows) have the same
  * limit (a captured graph: the one at its capture); a thread whose wait runs out reads its rows from memory instead, so
  * that its outputs are the same as ever.  dspark_tree_attention's products and softmax have it too, where it is
- * below their own 2^16 polls (a captured graph: the one at its capture): a CTA whose wait runs out sets DSPARK_DEV_TIMEOUT and
+ * below their own 2^16 polls, 0.26 s (a captured graph: the one at its capture): a CTA whose wait runs out sets DSPARK_DEV_TIMEOUT and
  * leaves, its outputs unspecified.
  * Per device (the current one), synchronous; the paper has no counterpart. */
 int dspark_set_wait_poll_limit(unsigned int polls);

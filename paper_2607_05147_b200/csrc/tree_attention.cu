@@ -13,7 +13,8 @@
 //   * one thread issues tcgen05.mma: S = Q K^T into tensor memory (Q and K in shared memory), then O += P V, with P taken from
 //     tensor memory and V as it lies (mn-major);
 //   * two groups of eight warps do the softmax, a row in two threads, half of a tile's positions each: they read S, write P over
-//     it as 16-bit values, and scale O only when the maximum has risen by more than 2^8 (the reference is any number that keeps
+//     it as 16-bit values (what the product takes: off by half a step of 2^-8 or 2^-11 each, up as often as down, so that the sum is
+//     nearer than the result's own rounding; the sum of the weights is that of the unrounded ones), and scale O only when the maximum has risen by more than 2^8 (the reference is any number that keeps
 //     the exponentials in range).  The groups have one S and one O each: with two row tiles they take one of them each; with one
 //     they take the even and the odd cache tiles and join at the end.  While one group works on its S the tensor cores do the
 //     other's products.
@@ -23,9 +24,9 @@
 // This kernel is for more than 64 rows with a K/V head; up to there tree_attention_few.cu does the work.
 //
 // Bound by the cache's bytes up to about 128 rows over bf16 (64 requests of 32 nodes, 4 heads a K/V head, over 4096 positions: 244 us,
-// 4.5 TB/s), beyond by the chain scores -> exponentials -> products of a group, which the other group's covers in part: a tile
+// 4.5 TB/s, in a replayed graph like the other times here), beyond by the chain scores -> exponentials -> products of a group, which the other group's covers in part: a tile
 // for 256 rows over e4m3 takes 6 800 clocks, of which the exponentials alone are 2 048 and the products 1 500.  64 nodes over 131072
-// positions: 241 us, 0.57 PFLOP/s.
+// positions: 236 us, 0.58 PFLOP/s.  A prompt of 8192, 32 heads: 1.28 ms over bf16, 0.43 PFLOP/s of those that are seen.
 // Tried and not kept: a warp a group for the products (the groups fall into step, 259 us); the weights made in the pass that finds
 // the largest score (32 more registers than there are).
 #include "tree_attention.cuh"

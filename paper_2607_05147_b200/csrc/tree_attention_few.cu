@@ -20,9 +20,12 @@
 // 2^8; then, seldom, the maxima are found, and O^T and the sums scaled.  The sums of the weights stay in the threads until the
 // end of a unit.
 //
-// Bound by the cache's bytes over bf16: 64 trees of 16 nodes, 4 heads a K/V head, over 4096 positions take 212 us, 5.1 TB/s.  An 8-bit
-// cache has half of them and the same work a tile, and two kinds of warps more: 128 tokens, 8 heads a K/V head, over 8192
-// positions of int8 take 441 us, 5.0 TB/s, a tile 1 800 clocks: the widening warps' waits, loads and stores, one after the other.
+// Bound by the cache's bytes over bf16: 64 trees of 16 nodes, 4 heads a K/V head, over 4096 positions take 211 us, 5.2 TB/s (one call after
+// the other in a replayed graph; 232 us, 4.7 TB/s, where every call finds other inputs), 128 tokens, 8 heads a K/V head, over 8192
+// positions 657 us, 6.5 TB/s.  An 8-bit cache has half of the bytes and the same work a tile, and two kinds of warps more: the 128 tokens
+// take 460 us over int8, 4.8 TB/s (508 us, 4.4 TB/s), a tile 1 800 clocks: the widening warps' waits, loads and stores, one after
+// the other.  The roles' code together is about what the SM's instruction caches hold: code that is seldom run stands out of line or
+// inline as measured.
 #include <math.h>
 
 #include "tree_attention.cuh"
