@@ -237,30 +237,45 @@ __global__ void __launch_bounds__(kKvThreads, 6) kv_rows_kernel(const __grid_con
     const long long capacity = kv_capacity(P.c);
     const KvRequests requests = kv_requests(P.first, P.row_offsets, P.R, row0, S);
     bool lost = false;                                        // no request was found for this thread's row
-    auto find = [&](int row, int r, bool everywhere) {
-        KvRequest q = {0, -1, 0, 0};
-        lost = row < P.n_rows;
-        for (; r < P.R; ++r) {
-            q = kv_request(requests.first, requests.row_offsets, r, P.n_rows, capacity);
-            lost = q.status == DSPARK_DEV_BAD_OFFSETS || row < q.row0 || (everywhere && row >= requests.row_offsets[r + 1]);
-            if (!lost || !everywhere) break;
-        }
+    auto put = [&](const KvRequest& q, int r, int row) {
         KvSlot at = {-1, 0};
-        if (!lost && q.n >= 0 && !kv_slot(P.c, r, q.first + (row - q.row0), 0, at)) {
+        if (!kv_slot(P.c, r, q.first + (row - q.row0), 0, at)) {
             at.at = -2;
             atomicOr(P.dev_status, DSPARK_DEV_BAD_PAGE);
         }
         slots[tid] = at;
     };
-    if (tid < kMost) {
-        const int row = row0 + tid;
-        find(row, row < P.n_rows ? kv_find_request(requests, row) : P.R, false);
-        if (lost && P.R <= kKvThreads) find(row, 0, true);
+    auto look_everywhere = [&](int row) {
+        for (int r = 0; r < P.R; ++r) {
+            const KvRequest q = kv_request(requests.first, requests.row_offsets, r, P.n_rows, capacity);
+            if (q.status == DSPARK_DEV_BAD_OFFSETS || row < q.row0 || row >= requests.row_offsets[r + 1]) continue;
+            if (q.n >= 0) put(q, r, row);
+            return;
+        }
+    };
+    if (tid < (kMost + 31) / 32 * 32) {
+        const int row = row0 + tid, r = tid < kMost && row < P.n_rows ? kv_find_request(requests, row) : P.R;
+        if (tid < kMost) slots[tid] = {-1, 0};
+        lost = tid < kMost && row < P.n_rows;
+        if (r < P.R) {
+            const KvRequest q = kv_request(requests.first, requests.row_offsets, r, P.n_rows, capacity);
+            lost = q.status == DSPARK_DEV_BAD_OFFSETS || row < q.row0;
+            if (q.n >= 0 && !lost) put(q, r, row);
+        }
+        if (P.R <= kKvThreads && __any_sync(0xffffffffu, lost)) {
+            bool falls = false;
+#pragma unroll
+            for (int i = 0; i < kKvThreads; i += 32) {
+                const int at = min(i + (tid & 31), P.R - 1);
+                falls |= requests.row_offsets[at + 1] < requests.row_offsets[at];
+            }
+            if (__any_sync(0xffffffffu, falls) && lost) look_everywhere(row);
+        }
     }
     if (P.R > kKvThreads && __syncthreads_or(lost)) {
         bool falls = false;
         for (int i = tid; i < P.R; i += kKvThreads) falls = falls || P.row_offsets[i + 1] < P.row_offsets[i];
-        if (__syncthreads_or(falls) && lost) find(row0 + tid, 0, true);
+        if (__syncthreads_or(falls) && lost) look_everywhere(row0 + tid);
     }
     __syncthreads();
 
