@@ -801,7 +801,7 @@ class KvCache:
     """A paged cache of K and V rows as the step's calls take it: the tensors, checked once.
 
     k, v: CUDA tensors [n_pages, page_size, kv_heads, head_dim], or [n_layers, ...] for several layers, of bfloat16, int8 or
-    float8_e4m3fn; any strides that both share (unit inner stride).  k_scale, v_scale: fp32 [(n_layers,) n_pages, kv_heads,
+    float8_e4m3fn; any strides that both share (unit inner stride).  k_scale, v_scale (of either sign): fp32 [(n_layers,) n_pages, kv_heads,
     page_size], contiguous, with the 8-bit types.  block_table: int32 [R, max_pages]; another one can be set (`set_block_table`).
     """
 
@@ -917,7 +917,7 @@ def dspark_kv_read(cache: KvCache, first: torch.Tensor, row_offsets: torch.Tenso
 
 def dspark_kv_commit(cache: KvCache, first: torch.Tensor, row_offsets: torch.Tensor, accepted_len: torch.Tensor, path: torch.Tensor, *,
                      out_first: Optional[torch.Tensor] = None, dev_status: torch.Tensor) -> None:
-    """Moves the accepted nodes' rows of all layers together behind the root; out_first: the next step's `first`."""
+    """Moves the accepted nodes' rows of all layers together behind the root; out_first: the next step's `first`, in memory of its own."""
     dev, R, fp, op = _step(cache, first, row_offsets)
     n = _need(path, "path").numel()
     rc = lib().dspark_kv_commit(cache.ref, fp, op, R, n, _vec(_need(accepted_len, "accepted_len"), "accepted_len", torch.int32, R, dev),
@@ -957,7 +957,8 @@ def dspark_tree_attention(q: torch.Tensor, cache: KvCache, first: torch.Tensor, 
 def dspark_verify_tree(target_probs: torch.Tensor, draft_probs: Optional[torch.Tensor], tokens: torch.Tensor, parents: torch.Tensor,
                        row_offsets: torch.Tensor, u_accept: torch.Tensor, u_sample: torch.Tensor, *, accepted_len: torch.Tensor,
                        out_tokens: torch.Tensor, out_path: Optional[torch.Tensor] = None, dev_status: torch.Tensor) -> None:
-    """Lossless verification of drafted trees; draft_probs None: the drafted tokens were chosen, not drawn."""
+    """Lossless verification of drafted trees; draft_probs None: the drafted tokens were chosen, not drawn.  No output may share
+    memory with another array of the call."""
     n, V = _matrix(target_probs, "target_probs")
     dev = _device_of(target_probs, "target_probs")
     R = _need(row_offsets, "row_offsets").numel() - 1
