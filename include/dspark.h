@@ -654,7 +654,7 @@ int dspark_kv_commit(const dspark_kv_cache_t* cache, const int32_t* first, const
  *               q_heads = group * kv_heads with group <= 128.  out may be q itself with the same strides
  *   parents     device int32 [n_rows], the parent's index within the request (the root's entry is not read); NULL: chains,
  *               node i sees the nodes up to i.  A parent that is not an earlier node sets DSPARK_DEV_BAD_TREE and ends the
- *               ancestors there; so does the 4097th ancestor of a node, not counting those in the chain that its request
+ *               ancestors there; so does the 65 537th ancestor of a node, not counting those in the chain that its request
  *               begins with (a prompt given with parents is one chain, however long)
  *   scale       at most 2^127 in size
  *   out_lse     device fp32 [n_rows][q_heads] or NULL: log of the sum of e^(scale * q . k) over the positions seen
@@ -749,7 +749,7 @@ int dspark_set_stream_path(int path);
  * and its outputs are unspecified.  dspark_rms_norm_quant's waits for rows copied ahead (many rows) have the same
  * limit (a captured graph: the one at its capture); a thread whose wait runs out reads its rows from memory instead, so
  * that its outputs are the same as ever.  dspark_tree_attention's products and softmax have it too, where it is
- * below their own 2^16 polls, 0.26 s (a captured graph: the one at its capture): a CTA whose wait runs out sets DSPARK_DEV_TIMEOUT and
+ * below their own 2^18 polls, 1 s (a captured graph: the one at its capture): a CTA whose wait runs out sets DSPARK_DEV_TIMEOUT and
  * leaves, its outputs unspecified.
  * Per device (the current one), synchronous; the paper has no counterpart. */
 int dspark_set_wait_poll_limit(unsigned int polls);

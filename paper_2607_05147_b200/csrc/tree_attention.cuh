@@ -14,17 +14,17 @@ constexpr int kAttnTile = 128;                   // rows of a row tile, position
 constexpr int kChunkBytes = kAttnTile * 128;     // 64 columns of 16 bits of a tile: 128 rows of 128 bytes, swizzled
 constexpr int kAttnMaxSlots = 12, kAttnMaxRaw = 12, kAttnScaleTiles = 4;
 constexpr int kAttnRingBytes = 6 * 2 * kChunkBytes;           // 192 KB: Q and the rings
-// Polls of a wait: 0.26 s, a poll in vain takes 4 us.  The longest sound one is for a walk of kAttnMaxWalk nodes by each of a unit's rows
-// (attn_bad_values), some 0.1 s.  The waits of the copies and of the widening warps always have these: with a
+// Polls of a wait: 1 s, a poll in vain takes 4 us.  The longest sound one is for walks of kAttnMaxWalk nodes, one after the other for half of
+// a unit's 64 rows (few_bad).  The waits of the copies and of the widening warps always have these: with a
 // count from memory 128 tokens over int8 took 467 us instead of 440.  The others' can be shortened (AttnParams::polls).
-constexpr uint32_t kAttnPolls = 1u << 16;
+constexpr uint32_t kAttnPolls = 1u << 18;
 constexpr int kAttnNarrowBytes = 208 * 1024;                  // with 8-bit caches (4 KB of scales beside it)
 constexpr float kAttnLog2e = 1.4426950408889634f;
 constexpr float kAttnLazy = 8.f;                 // O is scaled when the maximum rises by more than 2^8
 constexpr float kAttnNarrowOffset = 7.f;         // fp16 weights: up to 2^(7 + 8) of 65 504, down to 2^-31 of the largest
 constexpr float kAttnUnset = -1e38f;              // a reference that every score is above
 constexpr float kAttnLeastFactor = 1.4e-45f;     // the smallest number: -infinity times it is -infinity, a score times it next to nothing
-constexpr int kAttnMaxWalk = 4096;               // ancestors of a node outside the chain that its request begins with
+constexpr int kAttnMaxWalk = 65536;              // ancestors of a node outside the chain that its request begins with
 constexpr int kAttnNoTree = 0x7fffffff;
 // Tiles of a unit that a group adds up in one accumulator.  The tensor cores cut what an fp32 sum cannot hold: positive values came out
 // 0.6 % too small after 2^20 positions and 10 % after 2^24.  From time to time the accumulator is therefore added to another, rounded, and

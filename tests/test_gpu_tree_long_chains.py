@@ -102,19 +102,40 @@ def test_a_tree_behind_a_chain(kind, others, n, m):
 
 @pytest.mark.parametrize("others", [0, 600])
 def test_a_deep_tree(others):
-    # node 1 is a leaf, the others a chain past it: 4096 ancestors are the most that are looked at outside the chain at the beginning
+    # node 1 is a leaf, the others a chain past it
     n = 4097 if others == 0 else 900
     parents = [-1, 0, 0] + list(range(2, n - 1))
     check([(10, parents)] + [(7, chain(1))] * others, "bf16", 1, 1)
 
 
+def test_two_long_branches():
+    # 3000 nodes each from a prompt of 200
+    n = 6200
+    parents = [-1] + [199 if i == 3200 else i - 1 for i in range(1, n)]
+    check([(10, parents), (30, chain(5))], "bf16", 1, 1)
+
+
 def test_more_ancestors_than_are_looked_at():
-    n, parents = 4300, [-1, 0, 0] + list(range(2, 4299))
-    cache, q, first, nodes = batch([(10, parents)], "bf16", 1, 1)
-    got, _, st = T.run_attention(cache, q, T.i32(first), T.offsets(nodes), T.i32(parents), 0.2)
-    assert st == B.DEV_BAD_TREE
-    want, bound = dense(cache, 0, q[:4097], 10, ancestors_of(parents[:4097]), 0.2)
-    assert bool(((got[:4097].double() - want).abs() <= bound).all()) and bool(got.isfinite().all())
+    # 65536 outside the chain that a request begins with; here that chain is node 0 and 1, and node 1 is a leaf
+    n, last = 65536 + 300, 65536
+    parents = [-1, 0, 0] + list(range(2, n - 1))
+    cache = T.Cache([n], 64, 1, 16, "bf16")
+    g = T.gen(1)
+    cache.k.normal_(generator=g)
+    cache.v.normal_(generator=g)
+    q = torch.randn(n, 1, 16, generator=g, device="cuda").bfloat16()
+    got, _, st = T.run_attention(cache, q, T.i32([0]), T.i32([0, n]), T.i32(parents), 0.2)
+    assert st == B.DEV_BAD_TREE and bool(got.isfinite().all())
+    # as a chain without node 1: the rows up to the last whose walk is whole
+    k, v = (x[:, 0] for x in cache.values(0, range(n)))
+    for row in (2, 3, 5000, 40000, last - 100, last, last + 1):
+        seen = torch.tensor([0] + list(range(2, row + 1)), device="cuda")
+        x = q[row, 0].double()
+        w = torch.softmax(k[seen] @ x * 0.2, 0)
+        want, m = w @ v[seen], w @ v[seen].abs()
+        size = float((k[seen].abs() @ x.abs()).max()) * 0.2
+        bound = 2.0 ** -8 * (m + want.abs()) * 1.01 + 2 * (16 * 2.0 ** -23 * size + 2.0 ** -20) * m + 2.0 ** -11 * m
+        assert bool(((got[row, 0].double() - want).abs() <= bound).all()), row
 
 
 @pytest.mark.parametrize("others", [0, 60])
